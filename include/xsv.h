@@ -212,6 +212,48 @@ int xsv_score_noalloc(void* hip_stream, xsv_tensor q, const void* k_mid_bf16, in
  * ascending; keep: int32 [T_first + k + T_cur]. */
 int xsv_topk_keep(void* hip_stream, const float* scores, int P, int k, int T_first, int T_cur, int32_t* keep);
 
+/* ---- operators around the step (DEVICE pointers) ------------------------------------------------
+ * They only enqueue on hip_stream: no allocation, no wait, nothing kept between calls, so they may be captured into a HIP
+ * graph.  Workspaces are the caller's, of the size that the *_workspace function gives for the same arguments, 16-byte aligned;
+ * two calls (or two captured graphs) that may run at the same time need one each.  Outputs must not overlap inputs, or
+ * each other, unless stated.  Tensors are bf16 as everywhere; sums, statistics and angles are fp32 or fp64, and a result is
+ * rounded to bf16 once. */
+
+/* What makes the queries and keys that the entry points above take out of a projection's output: the norm of every row (the
+ * 64 channels of one head of one token), its weight and bias, and the rotation by the token's position,
+ *   y = R(position) (hat * weight + bias),    hat = x                                         (XSV_NORM_NONE)
+ *                                             hat = x / sqrt(mean(x^2) + eps)                 (XSV_NORM_RMS)
+ *                                             hat = (x - mean(x)) / sqrt(var(x) + eps)        (XSV_NORM_LAYER)
+ * With `axes` positions a token (1: its place in a sequence; 2: row and column of a patch) the channels fall into `axes` sections of
+ * w = 64 / axes; pair i of a section, i < w / 2, is channels (i, i + w / 2) of it, or (2 i, 2 i + 1) with `interleaved`, and turns by
+ * position * base^(-2 i / w):  (a, b) -> (a cos - b sin, b cos + a sin).  Angles are reduced in fp64: any int32 position is exact
+ * to fp32.  axes = 0: no rotation, positions are not looked at.  Squares are taken in fp32: elements of 2^60 and more overflow them. */
+enum { XSV_NORM_NONE = 0, XSV_NORM_RMS = 1, XSV_NORM_LAYER = 2 };
+typedef struct {
+  int32_t n;                 /* tokens, >= 0                                                        */
+  int32_t heads_q, heads_k;  /* 0 .. 65536, not both 0; a tensor of 0 heads is not looked at           */
+  int32_t norm;              /* XSV_NORM_*                                                              */
+  int32_t axes;              /* 0 | 1 | 2                                                               */
+  int32_t interleaved;       /* 0 | 1                                                                   */
+  float eps;                 /* > 0 (unless XSV_NORM_NONE)                                              */
+  double base;               /* > 0 (unless axes == 0)                                                  */
+  const int32_t* positions;  /* DEVICE [n][axes]                                                        */
+  const float* q_weight;     /* DEVICE [64] each, shared by the heads; NULL = ones (weight), zeros (bias) */
+  const float* q_bias;
+  const float* k_weight;
+  const float* k_bias;
+} xsv_rotate_config;
+/* q, k: bf16 [heads][n][64] via strides (a packed projection [n][3][H][64] as it is), q_out, k_out likewise; q_out may be q itself,
+ * k_out k itself (same strides). */
+int xsv_norm_rotate(void* hip_stream, const xsv_rotate_config* cfg, xsv_tensor q, xsv_tensor k, xsv_tensor q_out, xsv_tensor k_out);
+/* Its gradient: q, k as given to xsv_norm_rotate, dq_out, dk_out the gradients of its outputs; writes dq, dk (which may be dq_out,
+ * dk_out themselves) and, unless NULL, weight_grads: DEVICE float [4][64], the gradients of q_weight, q_bias, k_weight, k_bias, each
+ * summed over tokens and heads (also of those that are NULL, as if they were ones and zeros; zeros where there are no heads).
+ * The same bits every time.  workspace: needed with weight_grads only. */
+int xsv_norm_rotate_grad(void* hip_stream, const xsv_rotate_config* cfg, xsv_tensor q, xsv_tensor k, xsv_tensor dq_out, xsv_tensor dk_out,
+                         xsv_tensor dq, xsv_tensor dk, float* weight_grads, void* workspace, int64_t workspace_bytes);
+int xsv_norm_rotate_grad_workspace(const xsv_rotate_config* cfg, int64_t* bytes);
+
 const char* xsv_strerror(int code);
 
 #ifdef __cplusplus

@@ -24,6 +24,8 @@ SOURCES = {
     "score_select.hip": ["-ffp-contract=off"],
     "requant.hip": ["-ffp-contract=off"],
     "peaks.hip": [],
+    "operators_api.hip": [],
+    "rotate.hip": [],
 }
 
 

@@ -39,12 +39,23 @@ class xsv_tensor(C.Structure):
     _fields_ = [("ptr", C.c_void_p), ("stride_head", C.c_int64), ("stride_token", C.c_int64)]
 
 
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+
+
+class xsv_rotate_config(C.Structure):
+    _fields_ = [
+        ("n", C.c_int32), ("heads_q", C.c_int32), ("heads_k", C.c_int32), ("norm", C.c_int32), ("axes", C.c_int32),
+        ("interleaved", C.c_int32), ("eps", C.c_float), ("base", C.c_double), ("positions", C.c_void_p),
+        ("q_weight", C.c_void_p), ("q_bias", C.c_void_p), ("k_weight", C.c_void_p), ("k_bias", C.c_void_p),
+    ]
+
+
 # every symbol include/xsv.h declares
 EXPORTS = (
     "xsv_create", "xsv_destroy", "xsv_reset", "xsv_dequant_attend", "xsv_frame_attend", "xsv_score_prune", "xsv_quantize",
     "xsv_step", "xsv_step_all_layers", "xsv_set_overlap", "xsv_join", "xsv_cache_len", "xsv_cache_export",
     "xsv_cache_import", "xsv_last_selection", "xsv_quantize_k", "xsv_quantize_v", "xsv_score", "xsv_score_noalloc",
-    "xsv_topk_keep", "xsv_strerror",
+    "xsv_topk_keep", "xsv_strerror", "xsv_norm_rotate", "xsv_norm_rotate_grad", "xsv_norm_rotate_grad_workspace",
 )
 # every symbol include/xsv_tune.h declares (launch tuning and measurement aids)
 TUNE_EXPORTS = (
@@ -100,6 +111,10 @@ def lib():
         L.xsv_score.argtypes = [vp, T, vp, i32, i32, i32, i32, i32, i32, vp]
         L.xsv_score_noalloc.argtypes = [vp, T, vp, i32, i32, i32, i32, i32, i32, vp]
         L.xsv_topk_keep.argtypes = [vp, vp, i32, i32, i32, i32, vp]
+        R = C.POINTER(xsv_rotate_config)
+        L.xsv_norm_rotate.argtypes = [vp, R, T, T, T, T]
+        L.xsv_norm_rotate_grad.argtypes = [vp, R, T, T, T, T, T, T, vp, vp, C.c_int64]
+        L.xsv_norm_rotate_grad_workspace.argtypes = [R, C.POINTER(C.c_int64)]
         L.xsv_measure_peaks.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(C.c_float)]
         L.xsv_strerror.argtypes = [i32]
         L.xsv_strerror.restype = C.c_char_p
@@ -394,6 +409,146 @@ def topk_keep(scores, k, T_first, T_cur, stream=None):
     _check(lib().xsv_topk_keep(_stream_ptr(stream), scores.data_ptr() if P else None, P, k, T_first, T_cur,
                                keep.data_ptr()), "xsv_topk_keep")
     return keep
+
+
+# ---- operators around the step: asynchronous on the stream (default: the current one of the tensors' device) ------------
+
+_NO_TENSOR = xsv_tensor(None, 0, 0)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _bf16(t, name, shape=None):
+    """The checks that need the torch tensor; the library checks pointers, strides and sizes."""
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or t.dim() != 3 or not t.is_cuda:
+        raise ValueError(f"{name}: expected a bf16 device tensor [heads][tokens][64]")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.shape[2] != 64 or (t.stride(2) != 1 and t.numel()):
+        raise ValueError(f"{name}: expected 64 contiguous channels")
+    return t
+
+
+def _operand(t):
+    """xsv_tensor of a tensor that _bf16 has seen, or of none.  (The strides of an axis of one entry mean nothing to the tensor and are free.)"""
+    if t is None:
+        return _NO_TENSOR
+    sh, st = t.stride(0), t.stride(1)
+    if t.shape[1] == 1:
+        st = 64
+    if t.shape[0] == 1:
+        sh = 0
+    return xsv_tensor(t.data_ptr(), sh, st)
+
+
+def _plain(t, name, dtype, shape, device):
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {device}")
+    return t
+
+
+def _same_device(device, *tensors):
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"all tensors of a call must be on one device: {device} and {t.device}")
+
+
+class _on:
+    """For one call: the tensors' device is the current one, and what the call allocates belongs to the stream it runs on."""
+
+    def __init__(self, device, stream):
+        if stream is not None and stream.device != device:
+            raise ValueError(f"stream of {stream.device}, tensors on {device}")
+        self.device, self.stream = device, stream
+        self.guards = [torch.cuda.device(device)] + ([torch.cuda.stream(stream)] if stream is not None else [])
+
+    def __enter__(self):
+        for g in self.guards:
+            g.__enter__()
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def __exit__(self, *exc):
+        for g in reversed(self.guards):
+            g.__exit__(*exc)
+
+
+def _like(out, name, x):
+    """The caller's output tensor, checked, or a new one."""
+    if out is None:
+        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _bf16(out, name, x.shape)
+    if out.device != x.device:
+        raise ValueError(f"{name}: on {out.device}, the call's tensors on {x.device}")
+    if any(n > 1 and st == 0 for n, st in zip(out.shape, out.stride())):
+        raise ValueError(f"{name}: an output must not be an expanded tensor")
+    return out
+
+
+def _rotate_config(q, k, norm, eps, weights, positions, base, interleaved):
+    if norm not in NORMS:
+        raise ValueError(f"norm must be one of {sorted(NORMS)}")
+    if k is not None and k.shape[1] != q.shape[1]:
+        raise ValueError("q and k must have the same number of tokens")
+    n, dev = q.shape[1], q.device
+    axes = 0
+    if positions is not None:
+        if positions.dim() == 1:
+            positions = positions.view(n, 1) if positions.numel() == n else positions
+        if positions.dim() != 2 or positions.shape[1] not in (1, 2):
+            raise ValueError("positions: expected int32 [tokens] or [tokens][1 or 2]")
+        axes = positions.shape[1]
+        _plain(positions, "positions", torch.int32, (n, axes), dev)
+    for name, w in zip(("q_weight", "q_bias", "k_weight", "k_bias"), weights):
+        if w is not None:
+            _plain(w, name, torch.float32, (64,), dev)
+    return xsv_rotate_config(n, q.shape[0], 0 if k is None else k.shape[0], NORMS[norm], axes, int(bool(interleaved)), eps, base,
+                             _ptr(positions), *[_ptr(w) for w in weights])
+
+
+def norm_rotate(q, k=None, *, norm="layer", eps=1e-5, q_weight=None, q_bias=None, k_weight=None, k_bias=None, positions=None,
+                base=100.0, interleaved=False, out=None, stream=None):
+    """xsv_norm_rotate: norm per head, weight and bias (fp32 [64]) and rotation by `positions` (int32 [tokens] or [tokens][1 or 2];
+    None: no rotation) of queries and, unless None, keys.  Returns (q_out, k_out), contiguous unless `out` gives the two."""
+    _bf16(q, "q")
+    if k is not None:
+        _bf16(k, "k")
+    _same_device(q.device, k)
+    cfg = _rotate_config(q, k, norm, eps, (q_weight, q_bias, k_weight, k_bias), positions, base, interleaved)
+    q_out, k_out = out if out is not None else (None, None)
+    with _on(q.device, stream) as s:
+        q_out = _like(q_out, "out[0]", q)
+        k_out = None if k is None else _like(k_out, "out[1]", k)
+        _check(lib().xsv_norm_rotate(s, C.byref(cfg), _operand(q), _operand(k), _operand(q_out), _operand(k_out)), "xsv_norm_rotate")
+    return q_out, k_out
+
+
+def norm_rotate_grad(dq_out, dk_out, q, k=None, *, norm="layer", eps=1e-5, q_weight=None, q_bias=None, k_weight=None, k_bias=None,
+                     positions=None, base=100.0, interleaved=False, out=None, weight_grads=True, stream=None):
+    """xsv_norm_rotate_grad: (dq, dk, gradients of q_weight, q_bias, k_weight, k_bias as fp32 [4][64]) from the gradients of the
+    outputs of norm_rotate and what it was called with.  weight_grads=False leaves the last out (None)."""
+    _bf16(q, "q")
+    _bf16(dq_out, "dq_out", q.shape)
+    if k is not None:
+        _bf16(k, "k")
+        _bf16(dk_out, "dk_out", k.shape)
+    _same_device(q.device, k, dq_out, dk_out if k is not None else None)
+    cfg = _rotate_config(q, k, norm, eps, (q_weight, q_bias, k_weight, k_bias), positions, base, interleaved)
+    dq, dk = out if out is not None else (None, None)
+    sums = work = None
+    nbytes = C.c_int64()
+    if weight_grads:
+        _check(lib().xsv_norm_rotate_grad_workspace(C.byref(cfg), C.byref(nbytes)), "xsv_norm_rotate_grad_workspace")
+    with _on(q.device, stream) as s:
+        dq = _like(dq, "out[0]", q)
+        dk = None if k is None else _like(dk, "out[1]", k)
+        if weight_grads:
+            sums = torch.empty((4, 64), dtype=torch.float32, device=q.device)
+            work = torch.empty(nbytes.value, dtype=torch.uint8, device=q.device)
+        _check(lib().xsv_norm_rotate_grad(s, C.byref(cfg), _operand(q), _operand(k), _operand(dq_out), _operand(None if k is None else dk_out),
+                                          _operand(dq), _operand(dk), _ptr(sums), _ptr(work), nbytes.value), "xsv_norm_rotate_grad")
+    return dq, dk, sums
 
 
 def key_ranges(cache_tiles, frame_tiles, ranges, last_percent=100, frame_tile_cost=95):

@@ -1,0 +1,220 @@
+"""norm_rotate and its gradient against their definition in 64 bits.
+
+Tolerances.  A result is rounded to bf16 once: 2^-8 of itself.  In front of that everything is fp32: a row's statistics are sums of
+64 terms in 3 + 3 steps (11 roundings), then some ten roundings up to the result, each at most 2^-24 of the row's largest
+magnitude at that place; 2^-18 (64 roundings) of it covers them, where the magnitude is that of the terms, not of what is left
+when they cancel.  Weight gradients stay fp32: 2^-18 of the sum of the terms' magnitudes."""
+import pytest
+import torch
+
+import plain_operators as plain
+from paper_2602_21780_amd import xsv
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+HALF = 2.0 ** -8     # rounding to bf16
+FP32 = 2.0 ** -18    # 64 roundings to fp32
+
+
+def _packed(n, counts, seed, scale=1.0, shift=0.0):
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn((n, sum(counts), 64), generator=g) * scale + shift).to(torch.bfloat16).to(DEV).transpose(0, 1)
+    return list(x.split(counts))
+
+
+def _params(seed, bias):
+    g = torch.Generator().manual_seed(seed)
+    w = [(1 + 0.3 * torch.randn(64, generator=g)).to(DEV) if i % 2 == 0 else (0.5 * torch.randn(64, generator=g)).to(DEV) for i in range(4)]
+    return w if bias else [w[0], None, w[2], None]
+
+
+def _positions(n, axes, kind, seed):
+    if axes == 0:
+        return None
+    g = torch.Generator().manual_seed(seed)
+    if kind == "far":
+        return torch.randint(-2 ** 31, 2 ** 31 - 1, (n, axes), generator=g, dtype=torch.int64).to(torch.int32).to(DEV)
+    return torch.randint(0, 5000, (n, axes), generator=g).to(torch.int32).to(DEV)
+
+
+def _check_pair(q, k, weights, norm, eps, positions, base, interleaved, out=None):
+    form = dict(norm=norm, eps=eps, q_weight=weights[0], q_bias=weights[1], k_weight=weights[2], k_bias=weights[3], positions=positions,
+                base=base, interleaved=interleaved)
+    got = xsv.norm_rotate(q, k, out=out, **form)
+    g = torch.Generator().manual_seed(q.shape[1])
+    dy = [(0.1 * torch.randn(x.shape, generator=g)).to(torch.bfloat16).to(DEV) for x in (q, k)]
+    grads = xsv.norm_rotate_grad(dy[0], dy[1], q, k, **form)
+    torch.cuda.synchronize()
+    pos = None if positions is None else positions.cpu()
+    for i, x in enumerate((q, k)):
+        w, b = weights[2 * i], weights[2 * i + 1]
+        leaf = lambda t, default: (torch.full((64,), default, dtype=torch.float64) if t is None else t.cpu().double()).requires_grad_()
+        x64, w64, b64 = x.cpu().double().requires_grad_(), leaf(w, 1.0), leaf(b, 0.0)
+        y64 = plain.norm_rotate(x64, w64, b64, norm, eps, pos, base, interleaved)
+        mag = (plain.norm_rotate(x64, w64, None, norm, eps, None, base, False).abs().amax(-1, keepdim=True) + b64.abs().max()).detach()
+        err = (got[i].cpu().double() - y64.detach()).abs()
+        assert bool((err <= HALF * y64.detach().abs() + FP32 * mag).all()), (i, float((err / mag).max()))
+        d64 = dy[i].cpu().double()
+        dx64, dw64, db64 = torch.autograd.grad(y64, (x64, w64, b64), d64)
+        g64 = plain.turn(d64, pos, base, interleaved, -1.0)
+        hat = plain.norm_rotate(x64, None, None, norm, eps, None, base, False).detach()
+        if norm == "none":
+            r, terms = 1.0, (g64 * w64).abs().amax(-1, keepdim=True)
+        else:
+            c = x64 - x64.mean(-1, keepdim=True) if norm == "layer" else x64
+            r = 1.0 / torch.sqrt((c * c).mean(-1, keepdim=True) + eps)
+            u = (g64 * w64).abs()
+            # terms that cancel: u, its mean, hat * mean(u hat); and hat itself is off by roundings of x and of its mean
+            off = 1.0 + (r * x64.abs().amax(-1, keepdim=True))
+            terms = r * u.amax(-1, keepdim=True) * (1.0 + hat.abs().amax(-1, keepdim=True) ** 2) * off
+        err = (grads[i].cpu().double() - dx64).abs()
+        assert bool((err <= HALF * dx64.abs() + FP32 * terms.detach()).all()), (i, float((err / terms).max()))
+        # hat is off by roundings of x and of its mean: some of them (a 64th of FP32 each) on the largest x / deviation
+        spread = 1.0 if norm == "none" else 1.0 + (r * x64.abs()).amax().item()
+        for row, exact, total in ((2 * i, dw64, (g64 * hat).abs().sum((0, 1)) + spread / 64 * g64.abs().sum((0, 1))),
+                                  (2 * i + 1, db64, g64.abs().sum((0, 1)))):
+            err = (grads[2][row].cpu().double() - exact).abs()
+            assert bool((err <= FP32 * total.detach() + 1e-30).all()), (row, float(err.max()))
+    return got, grads
+
+
+@pytest.mark.parametrize("norm,axes,interleaved", [(n, a, i) for n in ("none", "rms", "layer") for a, i in ((0, False), (1, False), (1, True), (2, False), (2, True))])
+@pytest.mark.parametrize("n,heads,kv_heads", [(1, 16, 16), (37, 5, 3), (130, 9, 1)])
+def test_every_form_against_64_bits(norm, axes, interleaved, n, heads, kv_heads):
+    print(f"rotate {norm} axes={axes} interleaved={interleaved} n={n} heads={heads},{kv_heads}", flush=True)
+    q, k = _packed(n, [heads, kv_heads], n + heads, 2.0, 0.5)
+    _check_pair(q, k, _params(n, norm != "rms"), norm, 1e-5, _positions(n, axes, "near", n), 100.0, interleaved)
+
+
+@pytest.mark.parametrize("n", [300, 1374])
+def test_many_batches_of_heads_per_wave(n):
+    """More tokens and heads than waves find a place for at once: several batches of heads a wave, the last of them short."""
+    q, k = _packed(n, [36, 9], n, 1.0)
+    _check_pair(q, k, _params(3, True), "layer", 1e-6, _positions(n, 2, "near", n), 10000.0, False)
+
+
+def test_far_positions():
+    """Positions over all of int32: angles of up to 2^31 radians."""
+    q, k = _packed(64, [4, 4], 5)
+    for axes, interleaved in ((1, False), (2, True)):
+        _check_pair(q, k, [None] * 4, "rms", 1e-6, _positions(64, axes, "far", 6), 500000.0, interleaved)
+
+
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+def test_constant_zero_tiny_and_huge_rows(norm):
+    x = torch.randn((3, 8, 64), generator=torch.Generator().manual_seed(2))
+    x[0, 0] = 0.0
+    x[0, 1] = 3.0
+    x[1, 2] *= 1e-12
+    x[1, 3] *= 1e15
+    x[2, 4] = 0.0
+    x[2, 4, 7] = 100.0
+    x = x.to(torch.bfloat16).to(DEV)
+    y, _ = xsv.norm_rotate(x, norm=norm, eps=1e-6)
+    dy = torch.ones_like(x)
+    dy[..., ::3] = -2.0
+    dx, _, _ = xsv.norm_rotate_grad(dy, None, x, norm=norm, eps=1e-6)
+    x64 = x.cpu().double().requires_grad_()
+    y64 = plain.norm_rotate(x64, None, None, norm, 1e-6, None, 1.0, False)
+    dx64, = torch.autograd.grad(y64, x64, dy.cpu().double())
+    assert bool(((y.cpu().double() - y64).abs() <= HALF * y64.abs() + FP32 * (1 + y64.abs().amax(-1, keepdim=True))).all())
+    scale = dx64.abs().amax(-1, keepdim=True)
+    r = dx64.abs().amax(-1, keepdim=True) + 1.0 / torch.sqrt((x64 ** 2).mean(-1, keepdim=True) + 1e-6)
+    assert bool(((dx.cpu().double() - dx64).abs() <= HALF * dx64.abs() + FP32 * 64 * (scale + r)).all())
+
+
+def test_nan_and_infinity_stay_in_their_rows():
+    q, k = _packed(20, [4, 2], 9)
+    q, k = q.clone(), k.clone()
+    clean = xsv.norm_rotate(q, k)
+    q[1, 3, 5] = float("nan")
+    q[2, 19, 0] = float("inf")
+    got = xsv.norm_rotate(q, k)
+    bad = torch.zeros((4, 20), dtype=torch.bool, device=DEV)
+    bad[1, 3] = bad[2, 19] = True
+    assert torch.equal(got[0][~bad], clean[0][~bad]) and torch.equal(got[1], clean[1])
+    assert bool(got[0][bad].isnan().any(-1).all())
+
+
+def test_strided_outputs_in_place_and_neighbours_untouched():
+    """Outputs with strides of their own, rows beside them as they were; and in place."""
+    n, H = 50, 3
+    q, k = _packed(n, [H, H], 12)
+    want = xsv.norm_rotate(q, k, positions=torch.arange(n, dtype=torch.int32, device=DEV))
+    room = torch.full((n + 7, 2 * H + 1, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    view = room[:n].transpose(0, 1)
+    xsv.norm_rotate(q, k, positions=torch.arange(n, dtype=torch.int32, device=DEV), out=(view[:H], view[H:2 * H]))
+    assert torch.equal(view[:H], want[0]) and torch.equal(view[H:2 * H], want[1])
+    assert bool((room[n:] == 7.0).all()) and bool((room[:, 2 * H] == 7.0).all())
+    xsv.norm_rotate(q, k, positions=torch.arange(n, dtype=torch.int32, device=DEV), out=(q, k))
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+
+
+def test_gradient_in_place_without_weight_gradients_and_the_same_bits_twice():
+    q, k = _packed(333, [16, 16], 4)
+    dy = [torch.randn(x.shape, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(DEV) for x in (q, k)]
+    a = xsv.norm_rotate_grad(dy[0], dy[1], q, k)
+    b = xsv.norm_rotate_grad(dy[0], dy[1], q, k)
+    for x, y in zip(a, b):
+        assert torch.equal(x, y)
+    c = xsv.norm_rotate_grad(dy[0], dy[1], q, k, out=(dy[0], dy[1]), weight_grads=False)
+    assert torch.equal(dy[0], a[0]) and torch.equal(dy[1], a[1]) and c[2] is None
+
+
+def test_no_tokens_and_queries_alone():
+    empty = torch.empty((4, 0, 64), dtype=torch.bfloat16, device=DEV)
+    y, z = xsv.norm_rotate(empty, empty)
+    assert y.shape == (4, 0, 64) and z.shape == (4, 0, 64)
+    dx, dz, w = xsv.norm_rotate_grad(empty, empty, empty, empty)
+    assert dx.shape == (4, 0, 64) and not w.any()
+    q, k = _packed(9, [4, 4], 3)
+    both = xsv.norm_rotate(q, k)
+    assert torch.equal(xsv.norm_rotate(q)[0], both[0]) and torch.equal(xsv.norm_rotate(k)[0], both[1])
+    dq, dk, w = xsv.norm_rotate_grad(q, None, q)
+    assert dk is None and not w[2:].any()
+
+
+def test_differences():
+    """The kernel's gradient against differences of the definition, along a few directions."""
+    n = 6
+    q, k = _packed(n, [2, 2], 21)
+    weights = _params(5, True)
+    pos = _positions(n, 2, "near", 1)
+    dy = torch.randn(q.shape, generator=torch.Generator().manual_seed(8)).to(torch.bfloat16).to(DEV)
+    dq, _, w = xsv.norm_rotate_grad(dy, dy, q, k, q_weight=weights[0], q_bias=weights[1], positions=pos)
+    f = lambda x, wt, b: (plain.norm_rotate(x, wt, b, "layer", 1e-5, pos.cpu(), 100.0, False) * dy.cpu().double()).sum()
+    x, wt, b = q.cpu().double(), weights[0].cpu().double(), weights[1].cpu().double()
+    h = 1e-5
+    for seed in range(4):
+        v = torch.randn(x.shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64)
+        diff = (f(x + h * v, wt, b) - f(x - h * v, wt, b)) / (2 * h)
+        # every entry is off by at most a bf16 rounding (and fp32 ones, which are far smaller): 2^-8 |dq| |v|
+        assert abs(float((dq.cpu().double() * v).sum() - diff)) <= float((dq.cpu().double() * v).abs().sum()) * 2.0 ** -7.9 + 1e-4
+        u = v[0, 0]
+        for row, plus, minus in ((0, f(x, wt + h * u, b), f(x, wt - h * u, b)), (1, f(x, wt, b + h * u), f(x, wt, b - h * u))):
+            assert abs(float((w[row].cpu().double() * u).sum() - (plus - minus) / (2 * h))) <= 1e-4 * (1 + float((w[row].cpu().double() * u).abs().sum()))
+
+
+def test_on_another_stream_and_captured_into_a_graph():
+    q, k = _packed(257, [8, 8], 14)
+    dy = [x.clone().contiguous() for x in (q, k)]
+    pos = torch.arange(257, dtype=torch.int32, device=DEV)
+    want = xsv.norm_rotate(q, k, positions=pos)
+    want_grad = xsv.norm_rotate_grad(dy[0], dy[1], q, k, positions=pos)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = xsv.norm_rotate(q, k, positions=pos, stream=s)
+    s.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = xsv.norm_rotate(q, k, positions=pos)
+        g = xsv.norm_rotate_grad(dy[0], dy[1], q, k, positions=pos)
+    for _ in range(3):
+        for t in (*y, *g):
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((*y, *g), (*want, *want_grad)):
+            assert torch.equal(a, b)
+        xsv.norm_rotate_grad(dy[0], dy[1], k, q, positions=pos)   # the program's own work between replays

@@ -1,0 +1,71 @@
+"""What the operators around the step refuse, on the host before anything is launched (CPU only)."""
+import ctypes as C
+import os
+
+import pytest
+import torch
+
+from paper_2602_21780_amd import xsv
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(xsv.LIB_PATH):
+        from paper_2602_21780_amd.build import build
+        build()
+    return xsv.lib()
+
+
+PTR = 1 << 20    # an aligned address that nothing looks at
+
+
+def _rotate(**kw):
+    good = dict(n=4, heads_q=2, heads_k=2, norm=2, axes=1, interleaved=0, eps=1e-5, base=100.0, positions=PTR, q_weight=None, q_bias=None,
+                k_weight=None, k_bias=None)
+    return xsv.xsv_rotate_config(**{**good, **kw})
+
+
+T = xsv.xsv_tensor(PTR, 4 * 64, 64)
+BAD_TENSORS = [xsv.xsv_tensor(None, 256, 64), xsv.xsv_tensor(PTR + 8, 256, 64), xsv.xsv_tensor(PTR, 256, 60), xsv.xsv_tensor(PTR, 256, 68),
+               xsv.xsv_tensor(PTR, -256, 64), xsv.xsv_tensor(PTR, 4, 64), xsv.xsv_tensor(PTR, 256, (1 << 24) + 8)]
+
+
+@pytest.mark.parametrize("bad", [dict(n=-1), dict(heads_q=-1), dict(heads_q=0, heads_k=0), dict(norm=3), dict(norm=-1), dict(axes=3), dict(axes=-1),
+                                 dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(base=0.0),
+                                 dict(base=float("nan")), dict(base=-2.0), dict(positions=None), dict(positions=PTR + 2), dict(q_weight=PTR + 1),
+                                 dict(k_bias=PTR + 3)])
+def test_rotate_refuses_bad_configurations(lib, bad):
+    cfg = _rotate(**bad)
+    nbytes = C.c_int64()
+    assert lib.xsv_norm_rotate(None, C.byref(cfg), T, T, T, T) == xsv.XSV_ERR_ARG
+    assert lib.xsv_norm_rotate_grad(None, C.byref(cfg), T, T, T, T, T, T, None, None, 0) == xsv.XSV_ERR_ARG
+    assert lib.xsv_norm_rotate_grad_workspace(C.byref(cfg), C.byref(nbytes)) == xsv.XSV_ERR_ARG
+
+
+def test_rotate_refuses_bad_tensors_and_workspaces(lib):
+    cfg = _rotate()
+    nbytes = C.c_int64()
+    assert lib.xsv_norm_rotate(None, None, T, T, T, T) == xsv.XSV_ERR_ARG
+    assert lib.xsv_norm_rotate_grad_workspace(C.byref(cfg), None) == xsv.XSV_ERR_ARG
+    assert lib.xsv_norm_rotate_grad_workspace(C.byref(cfg), C.byref(nbytes)) == xsv.XSV_OK and nbytes.value > 0
+    for bad in BAD_TENSORS:
+        for at in range(4):
+            ts = [T] * 4
+            ts[at] = bad
+            assert lib.xsv_norm_rotate(None, C.byref(cfg), *ts) == xsv.XSV_ERR_ARG
+        for at in range(6):
+            ts = [T] * 6
+            ts[at] = bad
+            assert lib.xsv_norm_rotate_grad(None, C.byref(cfg), *ts, None, None, 0) == xsv.XSV_ERR_ARG
+    for sums, work, size in ((PTR, None, nbytes.value), (PTR, PTR, nbytes.value - 1), (PTR, PTR + 8, nbytes.value), (PTR + 2, PTR, nbytes.value)):
+        assert lib.xsv_norm_rotate_grad(None, C.byref(cfg), T, T, T, T, T, T, sums, work, size) == xsv.XSV_ERR_ARG
+    assert lib.xsv_norm_rotate(None, C.byref(_rotate(heads_q=(1 << 16) + 1)), T, T, T, T) == xsv.XSV_ERR_UNSUPPORTED
+    empty = xsv.xsv_tensor(None, 0, 0)
+    assert lib.xsv_norm_rotate(None, C.byref(_rotate(n=0, positions=None)), empty, empty, empty, empty) == xsv.XSV_OK    # nothing to do
+
+
+def test_bindings_refuse_what_is_not_a_bf16_device_tensor():
+    host = torch.zeros((2, 4, 64), dtype=torch.bfloat16)
+    for call in (lambda: xsv.norm_rotate(host, host), lambda: xsv.norm_rotate_grad(host, host, host, host), lambda: xsv.norm_rotate(None)):
+        with pytest.raises(ValueError):
+            call()
