@@ -254,6 +254,33 @@ int xsv_norm_rotate_grad(void* hip_stream, const xsv_rotate_config* cfg, xsv_ten
                          xsv_tensor dq, xsv_tensor dk, float* weight_grads, void* workspace, int64_t workspace_bytes);
 int xsv_norm_rotate_grad_workspace(const xsv_rotate_config* cfg, int64_t* bytes);
 
+/* Attention inside sequences, with what its gradient needs: the form of the frame-wise attention (every frame a sequence) and of the
+ * temporal attention (a clip of frames one sequence, a token sees its own frame and those before it) that a model is trained through.
+ *   S = scale q k^T over the keys a query sees,  lse = log sum exp(S) (natural),  out = exp(S - lse) v
+ * Sequence s is rows [q_begin[s], q_begin[s + 1]) of q, out, dout, dq and rows [k_begin[s], k_begin[s + 1]) of k, v, dk, dv; the
+ * offsets ascend and stay within the tensors (what does not is cut off: no row outside the tensors is touched).  Sequences may be empty
+ * on either side.  Rows in no sequence are neither read nor written.  Query i of n stands at key position i + m - n of m: at the end of its
+ * sequence's keys, so that keys of earlier frames or tokens may lie in front.  A query that sees no key has out = 0 and lse = -inf, and
+ * adds nothing to any gradient.  Values that are not finite in rows that a query does not see do not reach it, nor its gradient. */
+typedef struct {
+  int32_t heads, kv_heads;       /* 1 .. 65536, heads a multiple of kv_heads: head h reads key head h / (heads / kv_heads) */
+  int32_t sequences;             /* >= 0                                                       */
+  int32_t rows_q, rows_k;        /* rows of the tensors, >= 0                                  */
+  int32_t longest_q, longest_k;  /* bounds on the sequences' lengths (<= rows; they size the launch); rows behind them are left out */
+  const int32_t* q_begin;        /* DEVICE [sequences + 1]                                     */
+  const int32_t* k_begin;        /* DEVICE [sequences + 1]; may be q_begin                     */
+  int32_t causal;                /* 0: every key of the sequence is seen.  b > 0: keys come in blocks of b (b = 1: token by token, b =
+                                    tokens_per_frame: frame by frame), a query sees its own block and those before it   */
+  float softmax_scale;           /* >= 0; 0 -> 1/sqrt(64)                                      */
+} xsv_seq_config;
+/* q, out: bf16 [heads][rows_q][64], k, v: bf16 [kv_heads][rows_k][64] via strides; lse: float [heads][rows_q]. */
+int xsv_seq_attend(void* hip_stream, const xsv_seq_config* cfg, xsv_tensor q, xsv_tensor k, xsv_tensor v, xsv_tensor out, float* lse);
+/* Its gradient: out and lse as xsv_seq_attend left them, dout the gradient of out; writes dq, dk, dv (dk and dv summed over the
+ * heads that share a key head).  The same bits every time. */
+int xsv_seq_attend_grad(void* hip_stream, const xsv_seq_config* cfg, xsv_tensor q, xsv_tensor k, xsv_tensor v, xsv_tensor out, const float* lse,
+                        xsv_tensor dout, xsv_tensor dq, xsv_tensor dk, xsv_tensor dv, void* workspace, int64_t workspace_bytes);
+int xsv_seq_attend_grad_workspace(const xsv_seq_config* cfg, int64_t* bytes);
+
 const char* xsv_strerror(int code);
 
 #ifdef __cplusplus

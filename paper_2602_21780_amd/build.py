@@ -26,6 +26,8 @@ SOURCES = {
     "peaks.hip": [],
     "operators_api.hip": [],
     "rotate.hip": [],
+    # (MFMA results in VGPRs, as above)
+    "seq_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 
 

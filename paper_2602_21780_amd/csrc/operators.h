@@ -31,4 +31,24 @@ hipError_t launch_rotate(const RotateArgs& a, int norm, int axes, bool interleav
 hipError_t launch_rotate_grad(const RotateArgs& a, int norm, int axes, bool interleaved, hipStream_t stream);
 int rotate_grad_workgroups(int n, int heads_q, int heads_k);
 
+// Rows of one tensor of a seq_attend call, strides in elements.
+struct SeqRows {
+  const uint16_t* p;
+  int64_t sh, st;
+};
+struct SeqArgs {
+  SeqRows q, k, v, out, dout;  // out: written by the forward pass, read by the gradient
+  SeqRows dq, dk, dv;
+  float* lse;    // [heads][rows_q]
+  float* delta;  // gradient: [heads][rows_q] sums of dout * out, written by the first launch, read by the second
+  const int32_t* q_begin;
+  const int32_t* k_begin;
+  int heads, kv_heads, sequences, rows_q, rows_k, longest_q, longest_k;
+  int causal;
+  float scale;
+};
+hipError_t launch_seq_attend(const SeqArgs& a, hipStream_t stream);
+hipError_t launch_seq_attend_grad(const SeqArgs& a, hipStream_t stream);
+bool seq_attend_fits(const SeqArgs& a);  // its grids stay within what a launch can have
+
 }  // namespace xsv

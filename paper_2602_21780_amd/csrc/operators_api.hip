@@ -43,6 +43,32 @@ RotateArgs rotate_args(const xsv_rotate_config& c) {
   return a;
 }
 
+int check_seq(const xsv_seq_config* c) {
+  if (!c || c->heads < 1 || c->kv_heads < 1 || c->heads % c->kv_heads != 0 || c->sequences < 0 || c->rows_q < 0 || c->rows_k < 0) return XSV_ERR_ARG;
+  if (c->longest_q < 0 || c->longest_k < 0 || c->longest_q > c->rows_q || c->longest_k > c->rows_k || c->causal < 0) return XSV_ERR_ARG;
+  if (!(c->softmax_scale >= 0.0f) || !std::isfinite(c->softmax_scale)) return XSV_ERR_ARG;
+  if (c->sequences > 0 && (!c->q_begin || !c->k_begin || !aligned_to(c->q_begin, 4) || !aligned_to(c->k_begin, 4))) return XSV_ERR_ARG;
+  if (c->heads > (1 << 16)) return XSV_ERR_UNSUPPORTED;
+  return XSV_OK;
+}
+
+SeqArgs seq_args(const xsv_seq_config& c) {
+  SeqArgs a{};
+  a.q_begin = c.q_begin; a.k_begin = c.k_begin;
+  a.heads = c.heads; a.kv_heads = c.kv_heads; a.sequences = c.sequences;
+  a.rows_q = c.rows_q; a.rows_k = c.rows_k; a.longest_q = c.longest_q; a.longest_k = c.longest_k;
+  a.causal = c.causal;
+  a.scale = c.softmax_scale == 0.0f ? 1.0f / std::sqrt((float)kD) : c.softmax_scale;
+  return a;
+}
+
+// A tensor of `rows` rows; one without rows is not looked at.
+bool rows_of(const xsv_tensor& t, int rows, SeqRows* r) {
+  if (rows > 0 && !operand_ok(t)) return false;
+  r->p = static_cast<const uint16_t*>(t.ptr); r->sh = t.stride_head; r->st = t.stride_token;
+  return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -91,6 +117,42 @@ int xsv_norm_rotate_grad(void* hip_stream, const xsv_rotate_config* c, xsv_tenso
     a.weight_grads = weight_grads;
   }
   return launched(launch_rotate_grad(a, c->norm, c->axes, c->interleaved != 0, static_cast<hipStream_t>(hip_stream)));
+}
+
+int xsv_seq_attend(void* hip_stream, const xsv_seq_config* c, xsv_tensor q, xsv_tensor k, xsv_tensor v, xsv_tensor out, float* lse) {
+  const int rc = check_seq(c);
+  if (rc != XSV_OK) return rc;
+  SeqArgs a = seq_args(*c);
+  if (!rows_of(q, c->rows_q, &a.q) || !rows_of(k, c->rows_k, &a.k) || !rows_of(v, c->rows_k, &a.v) || !rows_of(out, c->rows_q, &a.out)) return XSV_ERR_ARG;
+  if (c->rows_q > 0 && (!lse || !aligned_to(lse, 4))) return XSV_ERR_ARG;
+  a.lse = lse;
+  if (!seq_attend_fits(a)) return XSV_ERR_UNSUPPORTED;
+  return launched(launch_seq_attend(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int xsv_seq_attend_grad_workspace(const xsv_seq_config* c, int64_t* bytes) {
+  const int rc = check_seq(c);
+  if (rc != XSV_OK) return rc;
+  if (!bytes) return XSV_ERR_ARG;
+  *bytes = (int64_t)c->heads * c->rows_q * (int64_t)sizeof(float);
+  return XSV_OK;
+}
+
+int xsv_seq_attend_grad(void* hip_stream, const xsv_seq_config* c, xsv_tensor q, xsv_tensor k, xsv_tensor v, xsv_tensor out, const float* lse,
+                        xsv_tensor dout, xsv_tensor dq, xsv_tensor dk, xsv_tensor dv, void* workspace, int64_t workspace_bytes) {
+  int64_t need = 0;
+  const int rc = xsv_seq_attend_grad_workspace(c, &need);
+  if (rc != XSV_OK) return rc;
+  SeqArgs a = seq_args(*c);
+  if (!rows_of(q, c->rows_q, &a.q) || !rows_of(k, c->rows_k, &a.k) || !rows_of(v, c->rows_k, &a.v) || !rows_of(out, c->rows_q, &a.out) ||
+      !rows_of(dout, c->rows_q, &a.dout) || !rows_of(dq, c->rows_q, &a.dq) || !rows_of(dk, c->rows_k, &a.dk) || !rows_of(dv, c->rows_k, &a.dv))
+    return XSV_ERR_ARG;
+  if (c->rows_q > 0 && (!lse || !aligned_to(lse, 4))) return XSV_ERR_ARG;
+  if (need > 0 && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < need)) return XSV_ERR_ARG;
+  a.lse = const_cast<float*>(lse);
+  a.delta = static_cast<float*>(workspace);
+  if (!seq_attend_fits(a)) return XSV_ERR_UNSUPPORTED;
+  return launched(launch_seq_attend_grad(a, static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

@@ -50,12 +50,21 @@ class xsv_rotate_config(C.Structure):
     ]
 
 
+class xsv_seq_config(C.Structure):
+    _fields_ = [
+        ("heads", C.c_int32), ("kv_heads", C.c_int32), ("sequences", C.c_int32), ("rows_q", C.c_int32), ("rows_k", C.c_int32),
+        ("longest_q", C.c_int32), ("longest_k", C.c_int32), ("q_begin", C.c_void_p), ("k_begin", C.c_void_p), ("causal", C.c_int32),
+        ("softmax_scale", C.c_float),
+    ]
+
+
 # every symbol include/xsv.h declares
 EXPORTS = (
     "xsv_create", "xsv_destroy", "xsv_reset", "xsv_dequant_attend", "xsv_frame_attend", "xsv_score_prune", "xsv_quantize",
     "xsv_step", "xsv_step_all_layers", "xsv_set_overlap", "xsv_join", "xsv_cache_len", "xsv_cache_export",
     "xsv_cache_import", "xsv_last_selection", "xsv_quantize_k", "xsv_quantize_v", "xsv_score", "xsv_score_noalloc",
     "xsv_topk_keep", "xsv_strerror", "xsv_norm_rotate", "xsv_norm_rotate_grad", "xsv_norm_rotate_grad_workspace",
+    "xsv_seq_attend", "xsv_seq_attend_grad", "xsv_seq_attend_grad_workspace",
 )
 # every symbol include/xsv_tune.h declares (launch tuning and measurement aids)
 TUNE_EXPORTS = (
@@ -115,6 +124,10 @@ def lib():
         L.xsv_norm_rotate.argtypes = [vp, R, T, T, T, T]
         L.xsv_norm_rotate_grad.argtypes = [vp, R, T, T, T, T, T, T, vp, vp, C.c_int64]
         L.xsv_norm_rotate_grad_workspace.argtypes = [R, C.POINTER(C.c_int64)]
+        S = C.POINTER(xsv_seq_config)
+        L.xsv_seq_attend.argtypes = [vp, S, T, T, T, T, vp]
+        L.xsv_seq_attend_grad.argtypes = [vp, S, T, T, T, T, vp, T, T, T, T, vp, C.c_int64]
+        L.xsv_seq_attend_grad_workspace.argtypes = [S, C.POINTER(C.c_int64)]
         L.xsv_measure_peaks.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(C.c_float)]
         L.xsv_strerror.argtypes = [i32]
         L.xsv_strerror.restype = C.c_char_p
@@ -549,6 +562,62 @@ def norm_rotate_grad(dq_out, dk_out, q, k=None, *, norm="layer", eps=1e-5, q_wei
         _check(lib().xsv_norm_rotate_grad(s, C.byref(cfg), _operand(q), _operand(k), _operand(dq_out), _operand(None if k is None else dk_out),
                                           _operand(dq), _operand(dk), _ptr(sums), _ptr(work), nbytes.value), "xsv_norm_rotate_grad")
     return dq, dk, sums
+
+
+def _seq_config(q, k, v, q_begin, k_begin, longest_q, longest_k, causal, softmax_scale):
+    _bf16(q, "q")
+    _bf16(k, "k")
+    _bf16(v, "v", k.shape)
+    _same_device(q.device, k, v)
+    if k_begin is None:
+        k_begin = q_begin
+    n = q_begin.numel() - 1 if isinstance(q_begin, torch.Tensor) else -1
+    if n < 0:
+        raise ValueError("q_begin: expected int32 [sequences + 1]")
+    for name, t in (("q_begin", q_begin), ("k_begin", k_begin)):
+        _plain(t, name, torch.int32, (n + 1,), q.device)
+    rows_q, rows_k = q.shape[1], k.shape[1]
+    return xsv_seq_config(q.shape[0], k.shape[0], n, rows_q, rows_k, rows_q if longest_q is None else longest_q,
+                          rows_k if longest_k is None else longest_k, _ptr(q_begin), _ptr(k_begin), causal, softmax_scale)
+
+
+def _like_or_zeros(out, name, x):
+    """As _like, but a new tensor is zeros: rows in no sequence are not written."""
+    return torch.zeros(x.shape, dtype=x.dtype, device=x.device) if out is None else _like(out, name, x)
+
+
+def seq_attend(q, k, v, q_begin, k_begin=None, *, longest_q=None, longest_k=None, causal=0, softmax_scale=0.0, out=None, lse=None, stream=None):
+    """xsv_seq_attend: attention of q [heads][rows][64] over k, v [kv_heads][rows][64] inside the sequences that the int32 device tensors
+    q_begin and k_begin (None: the same) bound.  longest_q / longest_k, the lengths of the longest, size the launch (None: all rows).
+    Returns (out, lse); tensors that it makes hold zeros in rows of no sequence."""
+    cfg = _seq_config(q, k, v, q_begin, k_begin, longest_q, longest_k, causal, softmax_scale)
+    with _on(q.device, stream) as s:
+        out = _like_or_zeros(out, "out", q)
+        if lse is None:
+            lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=q.device)
+        _plain(lse, "lse", torch.float32, q.shape[:2], q.device)
+        _check(lib().xsv_seq_attend(s, C.byref(cfg), _operand(q), _operand(k), _operand(v), _operand(out), _ptr(lse)), "xsv_seq_attend")
+    return out, lse
+
+
+def seq_attend_grad(dout, q, k, v, out, lse, q_begin, k_begin=None, *, longest_q=None, longest_k=None, causal=0, softmax_scale=0.0, grads=None,
+                    stream=None):
+    """xsv_seq_attend_grad: (dq, dk, dv) from the gradient of seq_attend's out, what it was called with and what it returned.  `grads`
+    gives the three tensors to write; those that it makes hold zeros in rows of no sequence."""
+    cfg = _seq_config(q, k, v, q_begin, k_begin, longest_q, longest_k, causal, softmax_scale)
+    _bf16(dout, "dout", q.shape)
+    _bf16(out, "out", q.shape)
+    _same_device(q.device, dout, out)
+    _plain(lse, "lse", torch.float32, q.shape[:2], q.device)
+    nbytes = C.c_int64()
+    _check(lib().xsv_seq_attend_grad_workspace(C.byref(cfg), C.byref(nbytes)), "xsv_seq_attend_grad_workspace")
+    dq, dk, dv = grads if grads is not None else (None, None, None)
+    with _on(q.device, stream) as s:
+        dq, dk, dv = _like_or_zeros(dq, "grads[0]", q), _like_or_zeros(dk, "grads[1]", k), _like_or_zeros(dv, "grads[2]", v)
+        work = torch.empty(nbytes.value, dtype=torch.uint8, device=q.device)
+        _check(lib().xsv_seq_attend_grad(s, C.byref(cfg), _operand(q), _operand(k), _operand(v), _operand(out), _ptr(lse), _operand(dout),
+                                         _operand(dq), _operand(dk), _operand(dv), _ptr(work), nbytes.value), "xsv_seq_attend_grad")
+    return dq, dk, dv
 
 
 def key_ranges(cache_tiles, frame_tiles, ranges, last_percent=100, frame_tile_cost=95):

@@ -69,3 +69,53 @@ def test_bindings_refuse_what_is_not_a_bf16_device_tensor():
     for call in (lambda: xsv.norm_rotate(host, host), lambda: xsv.norm_rotate_grad(host, host, host, host), lambda: xsv.norm_rotate(None)):
         with pytest.raises(ValueError):
             call()
+
+
+def _seq(**kw):
+    good = dict(heads=4, kv_heads=2, sequences=1, rows_q=8, rows_k=9, longest_q=8, longest_k=9, q_begin=PTR, k_begin=PTR, causal=0, softmax_scale=0.0)
+    return xsv.xsv_seq_config(**{**good, **kw})
+
+
+@pytest.mark.parametrize("bad", [dict(heads=0), dict(kv_heads=0), dict(kv_heads=3), dict(heads=-4), dict(sequences=-1), dict(rows_q=-1), dict(rows_k=-1),
+                                 dict(longest_q=9), dict(longest_k=10), dict(longest_q=-1), dict(causal=-1), dict(softmax_scale=-1.0),
+                                 dict(softmax_scale=float("nan")), dict(softmax_scale=float("inf")), dict(q_begin=None), dict(k_begin=None),
+                                 dict(q_begin=PTR + 2), dict(k_begin=PTR + 1)])
+def test_seq_attend_refuses_bad_configurations(lib, bad):
+    cfg = _seq(**bad)
+    nbytes = C.c_int64()
+    assert lib.xsv_seq_attend(None, C.byref(cfg), T, T, T, T, PTR) == xsv.XSV_ERR_ARG
+    assert lib.xsv_seq_attend_grad(None, C.byref(cfg), T, T, T, T, PTR, T, T, T, T, PTR, 1 << 20) == xsv.XSV_ERR_ARG
+    assert lib.xsv_seq_attend_grad_workspace(C.byref(cfg), C.byref(nbytes)) == xsv.XSV_ERR_ARG
+
+
+def test_seq_attend_refuses_bad_tensors_workspaces_and_grids(lib):
+    cfg = _seq()
+    nbytes = C.c_int64()
+    assert lib.xsv_seq_attend(None, None, T, T, T, T, PTR) == xsv.XSV_ERR_ARG
+    assert lib.xsv_seq_attend_grad_workspace(C.byref(cfg), None) == xsv.XSV_ERR_ARG
+    assert lib.xsv_seq_attend_grad_workspace(C.byref(cfg), C.byref(nbytes)) == xsv.XSV_OK and nbytes.value >= 4 * 8 * 4
+    for bad in BAD_TENSORS:
+        for at in range(4):
+            ts = [T] * 4
+            ts[at] = bad
+            assert lib.xsv_seq_attend(None, C.byref(cfg), *ts, PTR) == xsv.XSV_ERR_ARG
+        for at in range(8):
+            ts = [T] * 8
+            ts[at] = bad
+            assert lib.xsv_seq_attend_grad(None, C.byref(cfg), *ts[:4], PTR, *ts[4:], PTR, nbytes.value) == xsv.XSV_ERR_ARG
+    for lse in (None, PTR + 2):
+        assert lib.xsv_seq_attend(None, C.byref(cfg), T, T, T, T, lse) == xsv.XSV_ERR_ARG
+        assert lib.xsv_seq_attend_grad(None, C.byref(cfg), T, T, T, T, lse, T, T, T, T, PTR, nbytes.value) == xsv.XSV_ERR_ARG
+    for work, size in ((None, nbytes.value), (PTR + 8, nbytes.value), (PTR, nbytes.value - 1)):
+        assert lib.xsv_seq_attend_grad(None, C.byref(cfg), T, T, T, T, PTR, T, T, T, T, work, size) == xsv.XSV_ERR_ARG
+    huge = _seq(heads=1 << 16, kv_heads=1 << 16, rows_q=1 << 20, rows_k=1 << 20, longest_q=1 << 20, longest_k=1 << 20)
+    assert lib.xsv_seq_attend(None, C.byref(huge), T, T, T, T, PTR) == xsv.XSV_ERR_UNSUPPORTED
+
+
+def test_seq_attend_binding_refuses_what_is_not_a_bf16_device_tensor():
+    host = torch.zeros((2, 4, 64), dtype=torch.bfloat16)
+    begin = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        xsv.seq_attend(host, host, host, begin)
+    with pytest.raises(ValueError):
+        xsv.seq_attend_grad(host, host, host, host, host, torch.zeros((2, 4)), begin)
