@@ -101,6 +101,14 @@ int xsv_dequant_attend(xsv_ctx* ctx, int layer, xsv_tensor q, xsv_tensor k_new, 
  * out: DEVICE bf16 [H][n][64] contiguous. */
 int xsv_frame_attend(xsv_ctx* ctx, xsv_tensor q, xsv_tensor k, xsv_tensor v, void* out);
 
+/* Attention of any few query rows over the layer's cache as it is, without a frame of its own: a single token, a frame's special
+ * tokens, tokens of another model.  out = softmax(scale * q K~^T) V~ over the layer's T cached tokens; nothing is appended, no state is
+ * touched; to be called between steps (not between the stages of one: XSV_ERR_STATE).  q: bf16 [H][rows][64] via strides, rows 0 .. 2^20 (0: nothing
+ * is done).  out: DEVICE bf16 [H][rows][64] contiguous.  lse: DEVICE float [H][rows], log sum exp of the scaled logits (natural), with
+ * which a caller can join this with attention over other keys; or NULL.  Over an empty cache out = 0 and lse = -inf.  In overlap mode 2 it
+ * waits (on the stream) for the layer's outstanding chain. */
+int xsv_query_attend(xsv_ctx* ctx, int layer, xsv_tensor q, int rows, void* out, float* lse);
+
 /* Sec. 3.2 after the append (T = T_cache + n).  If budget == 0, T <= budget, or this is the first
  * frame, everything is kept.  Otherwise, with T_first = T_cur = n, P = T - T_first - T_cur and
  * k = min(max(0, budget - T_first - T_cur), P): the importance of every middle token j is

@@ -27,6 +27,7 @@ SOURCES = {
     "operators_api.hip": [],
     "rotate.hip": [],
     # (MFMA results in VGPRs, as above)
+    "query_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "seq_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 

@@ -622,6 +622,8 @@ int xsv_create(const xsv_config* cfg, void* hip_stream, xsv_ctx** out) {
   ctx->part_rows = part_rows;
   A(&w.attn_o, part_rows * kD, false);
   A(&w.attn_ml, part_rows * 4, false);
+  A(&w.query_parts, (size_t)kQueryPieces * kQueryRows * kQueryPart, false);
+  A(&w.query_done, kQueryPieces, true);
   A(&w.unit_done, (size_t)std::min(c.n_layers, kMaxBatch) * c.n_heads * ((n + 127) / 128) * kMeetStride, true);  // (128 rows: the smallest workgroup)
   if (rc == XSV_OK && hipStreamSynchronize(ctx->stream) != hipSuccess) rc = XSV_ERR_HIP;
   if (rc != XSV_OK) {
@@ -836,6 +838,32 @@ int xsv_frame_attend(xsv_ctx* ctx, xsv_tensor q, xsv_tensor k, xsv_tensor v, voi
   if (!tensor_ok(q) || !tensor_ok(k) || !tensor_ok(v) || !out) return XSV_ERR_ARG;
   void* outs[1] = {out};
   return do_attend(ctx, 0, 1, &q, &k, &v, outs, ctx->splits_single, 0, false, true);
+}
+
+int xsv_query_attend(xsv_ctx* ctx, int layer, xsv_tensor q, int rows, void* out, float* lse) {
+  int rc = check_layer(ctx, layer);
+  if (rc != XSV_OK) return rc;
+  if (rows < 0 || rows > (1 << 20)) return XSV_ERR_ARG;
+  if (ctx->layers[layer].phase != kIdle) return XSV_ERR_STATE;
+  if (rows == 0) return XSV_OK;
+  if (!tensor_ok(q) || !out || reinterpret_cast<uintptr_t>(out) % 16 != 0 || reinterpret_cast<uintptr_t>(lse) % 4 != 0) return XSV_ERR_ARG;
+  if ((rc = join_layers(ctx, layer, 1)) != XSV_OK) return rc;
+  const CachePool& p = ctx->pool;
+  const LayerState& L = ctx->layers[layer];
+  const LayerCache lc = layer_cache(p, L.buf, layer);
+  QueryArgs a{};
+  a.kc = lc.kc; a.ks = lc.ks; a.kz = lc.kz; a.vc = lc.vc; a.vs = lc.vs; a.vz = lc.vz;
+  a.code_head = (size_t)p.Tcap * p.code_row_bytes();
+  a.kparam_head = (size_t)(p.Tcap / p.G) * kD;
+  a.vparam_head = (size_t)p.Tcap * (kD / p.G);
+  a.q = static_cast<const uint16_t*>(q.ptr); a.q_sh = q.stride_head; a.q_st = q.stride_token;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.parts = ctx->ws.query_parts; a.counters = ctx->ws.query_done;
+  a.H = p.H; a.rows = rows; a.T = L.T;
+  if (!plan_query(a)) return XSV_ERR_UNSUPPORTED;
+  a.c2 = ctx->cfg.softmax_scale * 1.4426950408889634f;
+  return launch_query_attend(a, p.bits, p.G, ctx->stream) == hipSuccess ? XSV_OK : hip_fail(ctx);
 }
 
 int xsv_score_prune(xsv_ctx* ctx, int layer, xsv_tensor q) {

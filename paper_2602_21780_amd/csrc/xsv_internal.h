@@ -102,6 +102,8 @@ struct Workspace {
   uint16_t* attn_o;   // [pieces][batch layers][H][ceil(n/32)] blocks of 32 rows x 64 fp16 mantissas of the unnormalized
                       // partial outputs, each block stored [16-byte piece 0..3][lane half][row] (4 KB)
   float* attn_ml;     // [pieces][batch layers][H][n][4]  softmax reference (log2 domain), row sum, row scale, -
+  float* query_parts;      // partial results of query_attend, see QueryArgs
+  uint32_t* query_done;    // its counters, one per (head, row block) whose tokens are cut, zero between launches
   uint32_t* unit_done;  // [units of an attention launch] where the workgroups of a cut unit meet (attend.hip), zero between launches
   int scores_stride;  // Tcap + n
   int sets;           // lists per layer (CachePool::sets)
@@ -261,6 +263,32 @@ struct QuantizeArgs {
   bool wide;  // codes is 16-byte aligned
 };
 hipError_t launch_quantize_plain(const QuantizeArgs& a, int bits, int G, bool keys, hipStream_t stream);
+
+// Attention of a few query rows over one layer's cache (query_attend.hip).
+constexpr int kQueryRows = 16;     // query rows of a column block
+constexpr int kQueryPart = kD + 2;  // floats of a row of a partial result: 64 channels, reference, sum
+constexpr int kQueryPieces = 1024;  // partial results of one column block that the workspace holds
+constexpr int kQueryWide = 4;       // column blocks of a wave where there are more rows than one holds
+struct QueryArgs {
+  const uint8_t* kc;  // head 0
+  const float* ks;
+  const float* kz;
+  const uint8_t* vc;
+  const float* vs;
+  const float* vz;
+  size_t code_head, kparam_head, vparam_head;  // between two heads: bytes, floats, floats
+  const uint16_t* q;
+  int64_t q_sh, q_st;
+  uint16_t* out;  // [H][rows][64]
+  float* lse;     // [H][rows] or null
+  float* parts;
+  uint32_t* counters;  // zero between launches
+  int H, rows, T;
+  int blocks, splits;  // row blocks of a head, workgroups that share the tokens of one (from plan_query)
+  float c2;  // softmax scale * log2(e)
+};
+bool plan_query(QueryArgs& a);  // false: more workgroups than a launch can have
+hipError_t launch_query_attend(const QueryArgs& a, int bits, int G, hipStream_t stream);
 
 // Canonical (one code per byte, untransposed) copies of one layer buffer → device arrays.
 struct UnpackArgs {

@@ -64,7 +64,7 @@ EXPORTS = (
     "xsv_step", "xsv_step_all_layers", "xsv_set_overlap", "xsv_join", "xsv_cache_len", "xsv_cache_export",
     "xsv_cache_import", "xsv_last_selection", "xsv_quantize_k", "xsv_quantize_v", "xsv_score", "xsv_score_noalloc",
     "xsv_topk_keep", "xsv_strerror", "xsv_norm_rotate", "xsv_norm_rotate_grad", "xsv_norm_rotate_grad_workspace",
-    "xsv_seq_attend", "xsv_seq_attend_grad", "xsv_seq_attend_grad_workspace",
+    "xsv_seq_attend", "xsv_seq_attend_grad", "xsv_seq_attend_grad_workspace", "xsv_query_attend",
 )
 # every symbol include/xsv_tune.h declares (launch tuning and measurement aids)
 TUNE_EXPORTS = (
@@ -93,6 +93,7 @@ def lib():
         L.xsv_join.argtypes = [vp]
         L.xsv_dequant_attend.argtypes = [vp, i32, T, T, T, vp]
         L.xsv_frame_attend.argtypes = [vp, T, T, T, vp]
+        L.xsv_query_attend.argtypes = [vp, i32, T, i32, vp, vp]
         L.xsv_score_prune.argtypes = [vp, i32, T]
         L.xsv_quantize.argtypes = [vp, i32, T, T]
         L.xsv_step.argtypes = [vp, i32, T, T, T, vp]
@@ -288,6 +289,23 @@ class Context:
         out = self._out(q, out)
         _check(lib().xsv_frame_attend(self._h, as_tensor(q), as_tensor(k), as_tensor(v), out.data_ptr()), "xsv_frame_attend")
         return out
+
+    def query_attend(self, layer, q, out=None, lse=None):
+        """xsv_query_attend: q [H][rows][64] over the layer's cache, on the context's stream.  Returns (out, lse)."""
+        H, d = self.cfg.n_heads, self.cfg.head_dim
+        if q.dim() != 3 or q.shape[0] != H or q.shape[2] != d:
+            raise ValueError(f"q: expected [{H}][rows][{d}]")
+        rows = q.shape[1]
+        if out is None:
+            out = torch.empty((H, rows, d), dtype=torch.bfloat16, device=q.device)
+        if lse is None:
+            lse = torch.empty((H, rows), dtype=torch.float32, device=q.device)
+        for name, t, dtype, shape in (("out", out, torch.bfloat16, (H, rows, d)), ("lse", lse, torch.float32, (H, rows))):
+            if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != q.device:
+                raise ValueError(f"{name}: expected a contiguous {dtype} tensor {shape} on {q.device}")
+        if rows:
+            _check(lib().xsv_query_attend(self._h, layer, _operand(_bf16(q, "q")), rows, out.data_ptr(), lse.data_ptr()), "xsv_query_attend")
+        return out, lse
 
     def score_prune(self, layer, q):
         _check(lib().xsv_score_prune(self._h, layer, as_tensor(q)), "xsv_score_prune")
