@@ -189,340 +189,239 @@ __device__ __forceinline__ int dealt(int wg, int n) {
   return xcd * q + min(xcd, r) + wg / 8;
 }
 
-// ---- forward --------------------------------------------------------------------------------------------------------
+// ---- what owns queries: forward, and the gradient of the queries ----------------------------------------------------
 
-// A workgroup: 4 waves x 32 QB queries of one head of one sequence.
-template <int QB>
-__global__ __launch_bounds__(256, 2) void seq_attend_kernel(SeqArgs a, int blocks) {
-  __shared__ __align__(16) char lds[2][2][kTileBytes];  // [buffer][keys, values]
-  __shared__ int dirty[2];                             // number + 1 of a cut tile with values that are not finite
-  const int lane = threadIdx.x % 64, h = lane / 32;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int id = dealt(blockIdx.x, gridDim.x);
-  const int unit = id / blocks, block = blocks - 1 - id % blocks;
-  const int head = unit / a.sequences;
-  const Sequence s = sequence_of(a, unit % a.sequences);
-  const int row0 = block * 128 * QB;
-  if (row0 >= s.nq) return;
-  const int kv = head / (a.heads / a.kv_heads);
-  const uint16_t* kb = a.k.p + kv * a.k.sh + s.k0 * a.k.st;
-  const uint16_t* vb = a.v.p + kv * a.v.sh + s.k0 * a.v.st;
-
-  // (rows behind the last query are copies of it that nobody writes)
-  int row[QB], seen[QB];
-  bf16x8 qf[QB][4];
-#pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    row[qb] = row0 + wave * 32 * QB + qb * 32 + lane % 32;
-    const int i = min(row[qb], s.nq - 1);
-    seen[qb] = keys_seen(a, s, i);
-    const uint16_t* src = a.q.p + head * a.q.sh + (int64_t)(s.q0 + i) * a.q.st + 8 * h;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) qf[qb][c] = *reinterpret_cast<const bf16x8*>(src + 16 * c);
+// A workgroup's place: WAVES x 32 queries of one head of one sequence.  Blocks with many keys to see come first.
+struct QueryBlock {
+  Sequence s;
+  int head, kv, row0;
+  int row, seen;              // the lane's query (behind the last: a copy of it that nobody writes) and the keys it sees
+  int wave_least, wave_most;  // keys that all, and any, of the wave's queries see; of the workgroup's
+  int wg_least, tiles;
+  bool any;
+  template <int WAVES>
+  __device__ __forceinline__ static QueryBlock of(const SeqArgs& a, int blocks, int wave, int lane) {
+    QueryBlock b;
+    const int id = dealt(blockIdx.x, gridDim.x);
+    const int unit = id / blocks;
+    b.head = unit / a.sequences;
+    b.kv = b.head / (a.heads / a.kv_heads);
+    b.s = sequence_of(a, unit % a.sequences);
+    b.row0 = (blocks - 1 - id % blocks) * 32 * WAVES;
+    b.any = b.row0 < b.s.nq;
+    if (!b.any) return b;
+    const int last = b.s.nq - 1, first = min(b.row0 + wave * 32, last);
+    b.row = b.row0 + wave * 32 + lane % 32;
+    b.seen = keys_seen(a, b.s, min(b.row, last));
+    b.wave_least = keys_seen(a, b.s, first);  // (rows ascend, and so does what they see)
+    b.wave_most = keys_seen(a, b.s, min(first + 31, last));
+    b.wg_least = keys_seen(a, b.s, b.row0);
+    b.tiles = (keys_seen(a, b.s, min(b.row0 + 32 * WAVES - 1, last)) + 63) / 64;
+    return b;
   }
-  // rows ascend, and so does what they see: the wave's first and last row bound it
-  const int wave_row = min(row0 + wave * 32 * QB, s.nq - 1);
-  const int wave_least = keys_seen(a, s, wave_row), wave_most = keys_seen(a, s, min(wave_row + 32 * QB - 1, s.nq - 1));
-  const int wg_least = keys_seen(a, s, row0), wg_most = keys_seen(a, s, min(row0 + 128 * QB - 1, s.nq - 1));
-  const int tiles = (wg_most + 63) / 64;
+  // the lane's part of a row of queries, outputs or their gradients
+  __device__ __forceinline__ const uint16_t* at(const SeqRows& t, int lane) const {
+    return t.p + head * t.sh + (int64_t)(s.q0 + min(row, s.nq - 1)) * t.st + 8 * (lane / 32);
+  }
+};
 
-  const Reader rd(lane);
-  const float c2 = a.scale * kLog2e;
-  f32x16 o[QB][2] = {};
-  float sum[QB] = {}, ref[QB];  // ref in powers of two; -inf: no finite logit yet
-#pragma unroll
-  for (int qb = 0; qb < QB; ++qb) ref[qb] = -kInf;
-
-  bool left_out = false;  // some of them are to be added
-  if (threadIdx.x < 2) dirty[threadIdx.x] = 0;
-  Stage<256> sk, sv;
+// Tiles of keys and values through two buffers: the next one's loads are on their way while a tile is worked on.
+// work(t, keys, values, masked, dirty): dirty, only where the mask cuts the tile: keys (WATCH = 0) or values (1) that are not finite.
+template <int WAVES, int WATCH, typename F>
+__device__ __forceinline__ void over_keys(const SeqArgs& a, const QueryBlock& b, char (*lds)[2][kTileBytes], int* dirty, F work) {
+  const uint16_t* kb = a.k.p + b.kv * a.k.sh + b.s.k0 * a.k.st;
+  const uint16_t* vb = a.v.p + b.kv * a.v.sh + b.s.k0 * a.v.st;
+  Stage<64 * WAVES> sk, sv;
   auto fetch = [&](int t) {
-    sk.load(kb, a.k.st, 64 * t, s.nk);
-    sv.load(vb, a.v.st, 64 * t, s.nk);
+    sk.load(kb, a.k.st, 64 * t, b.s.nk);
+    sv.load(vb, a.v.st, 64 * t, b.s.nk);
   };
   auto put = [&](int t) {
     sk.store(lds[t & 1][0]);
     sv.store(lds[t & 1][1]);
-    if (64 * (t + 1) > wg_least && __any(sv.any_not_finite())) dirty[t & 1] = t + 1;
+    if (64 * (t + 1) > b.wg_least && __any((WATCH ? sv : sk).any_not_finite())) dirty[t & 1] = t + 1;
   };
+  if (b.tiles <= 0) return;
+  if (threadIdx.x < 2) dirty[threadIdx.x] = 0;
+  __syncthreads();
+  fetch(0);
+  put(0);
+  __syncthreads();
+  for (int t = 0; t < b.tiles; ++t) {
+    if (t + 1 < b.tiles) fetch(t + 1);
+    if (64 * (t + 1) <= b.wave_least) work(t, lds[t & 1][0], lds[t & 1][1], std::false_type{}, false);
+    else if (64 * t < b.wave_most) work(t, lds[t & 1][0], lds[t & 1][1], std::true_type{}, dirty[t & 1] == t + 1);
+    if (t + 1 < b.tiles) put(t + 1);
+    __syncthreads();
+  }
+}
 
-  auto tile = [&](int t, auto masked_) {
+__device__ __forceinline__ void write_columns(uint16_t* dst, const f32x16* x, float f, int h) {
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x2 w = {pack2(x[cb][4 * i] * f, x[cb][4 * i + 1] * f), pack2(x[cb][4 * i + 2] * f, x[cb][4 * i + 3] * f)};
+      *reinterpret_cast<u32x2*>(dst + 32 * cb + 8 * i + 4 * h) = w;
+    }
+}
+
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void seq_attend_kernel(SeqArgs a, int blocks) {
+  __shared__ __align__(16) char lds[2][2][kTileBytes];  // [buffer][keys, values]
+  __shared__ int dirty[2];                             // number + 1 of a cut tile with values that are not finite
+  const int lane = threadIdx.x % 64, h = lane / 32;
+  const QueryBlock b = QueryBlock::of<WAVES>(a, blocks, __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane);
+  if (!b.any) return;
+  bf16x8 qf[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) qf[c] = *reinterpret_cast<const bf16x8*>(b.at(a.q, lane) + 16 * c);
+  const Reader rd(lane);
+  const float c2 = a.scale * kLog2e;
+  f32x16 o[2] = {};
+  float sum = 0.0f, ref = -kInf;  // ref in powers of two; -inf: no finite logit yet
+  bool left_out = false;          // values that are not finite are to be added
+
+  over_keys<WAVES, 1>(a, b, lds, dirty, [&](int t, const char* kt, const char* vt, auto masked_, bool clean_up) {
     constexpr bool kMasked = decltype(masked_)::value;
-    const char* kt = lds[t & 1][0];
-    const char* vt = lds[t & 1][1];
-    const bool clean_up = kMasked && dirty[t & 1] == t + 1;
     if (kMasked) left_out |= clean_up;
+    f32x16 x[2];
+    auto logits = [&]() {
 #pragma unroll
-    for (int kh = 0; kh < 2; ++kh) {
-      f32x16 x[QB];
-      auto logits = [&]() {
-        bf16x8 kf[4];
+      for (int kh = 0; kh < 2; ++kh) {
+        x[kh] = f32x16{};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) kf[c] = rd.along(kt, kh, c);
+        for (int c = 0; c < 4; ++c) x[kh] = mfma(rd.along(kt, kh, c), qf[c], x[kh]);
+        if (kMasked) {
+          const int left = b.seen - (64 * t + 32 * kh + 4 * h);
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-          x[qb] = f32x16{};
-#pragma unroll
-          for (int c = 0; c < 4; ++c) x[qb] = mfma(kf[c], qf[qb][c], x[qb]);
-          if (kMasked) {
-            const int left = seen[qb] - (64 * t + 32 * kh + 4 * h);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[qb][i] = 8 * (i / 4) + i % 4 < left ? x[qb][i] : -kInf;
-          }
+          for (int i = 0; i < 16; ++i) x[kh][i] = 8 * (i / 4) + i % 4 < left ? x[kh][i] : -kInf;
         }
-      };
-      float part[QB];
-      auto probabilities = [&]() {
+      }
+    };
+    float part;
+    auto probabilities = [&]() {
+      const float off = ref == -kInf ? 0.0f : ref;
+      float p[4] = {};
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-          const float off = ref[qb] == -kInf ? 0.0f : ref[qb];
-          float p0 = 0.0f, p1 = 0.0f;
+      for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
-          for (int i = 0; i < 16; i += 2) {
-            x[qb][i] = exp2_(x[qb][i] * c2 - off);
-            x[qb][i + 1] = exp2_(x[qb][i + 1] * c2 - off);
-            p0 += x[qb][i];
-            p1 += x[qb][i + 1];
-          }
-          part[qb] = p0 + p1;
+        for (int i = 0; i < 16; ++i) {
+          x[kh][i] = exp2_(x[kh][i] * c2 - off);
+          p[i % 4] += x[kh][i];
         }
-      };
+      part = (p[0] + p[1]) + (p[2] + p[3]);
+    };
+    logits();
+    probabilities();
+    const bool move = !(part <= kMaxPart) || ref == -kInf;
+    if (__any(move)) {
       logits();
+      float top = x[0][0];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, fmaxf(x[0][i], x[1][i]));
+      // (a query's two lanes move together, and by themselves: its result does not depend on the wave's other queries)
+      const bool moves = half_max(move ? 1.0f : 0.0f) > 0.0f;
+      const float moved = moves ? fmaxf(ref, half_max(top) * c2) : ref;
+      const float f = ref == -kInf || !moves ? 1.0f : exp2_(ref - moved);  // (from no reference: there is nothing to scale)
+      ref = moved;
+      sum *= f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        o[0][i] *= f;
+        o[1][i] *= f;
+      }
       probabilities();
-      bool move[QB], again = false;
+    }
+    sum += part;
+    auto product = [&](auto clean_) {
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) {
-        move[qb] = !(part[qb] <= kMaxPart) || ref[qb] == -kInf;
-        again |= move[qb];
-      }
-      if (__any(again)) {
-        logits();
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-          float top = x[qb][0];
-#pragma unroll
-          for (int i = 1; i < 16; ++i) top = fmaxf(top, x[qb][i]);
-          // (a query's two lanes move together, and by themselves: its result does not depend on the wave's other queries)
-          const bool moves = half_max(move[qb] ? 1.0f : 0.0f) > 0.0f;
-          const float moved = moves ? fmaxf(ref[qb], half_max(top) * c2) : ref[qb];
-          // (from no reference: there is nothing to scale)
-          const float f = ref[qb] == -kInf || !moves ? 1.0f : exp2_(ref[qb] - moved);
-          ref[qb] = moved;
-          sum[qb] *= f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            o[qb][0][i] *= f;
-            o[qb][1][i] *= f;
-          }
-        }
-        probabilities();
-      }
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb) sum[qb] += part[qb];
-      auto product = [&](auto clean_) {
+      for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-          bf16x8 p[QB];
-#pragma unroll
-          for (int qb = 0; qb < QB; ++qb) p[qb] = pack8(x[qb], ks);
+          const bf16x8 p = pack8(x[kh], ks);
 #pragma unroll
           for (int cb = 0; cb < 2; ++cb) {
             bf16x8 vf = rd.across(vt, kh, cb, ks);
             if (decltype(clean_)::value) vf = cleaned(vf);
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) o[qb][cb] = mfma(vf, p[qb], o[qb][cb]);
+            o[cb] = mfma(vf, p, o[cb]);
           }
         }
-      };
-      __builtin_amdgcn_sched_barrier(0);
-      if (clean_up) product(std::true_type{});
-      else product(std::false_type{});
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-
-  if (tiles > 0) {
-    __syncthreads();  // (the flags are cleared)
-    fetch(0);
-    put(0);
-    __syncthreads();
-    for (int t = 0; t < tiles; ++t) {
-      if (t + 1 < tiles) fetch(t + 1);
-      if (64 * (t + 1) <= wave_least) tile(t, std::false_type{});
-      else if (64 * t < wave_most) tile(t, std::true_type{});
-      if (t + 1 < tiles) put(t + 1);
-      __syncthreads();
-    }
-  }
-  if (left_out) {
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
-      add_not_finite(vb, a.v.st, wave_least / 64 * 64, wave_most, lane, [&](int r) { return r < seen[qb]; }, o[qb]);
-  }
-#pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    const float total = half_sum(sum[qb]);
-    if (row[qb] >= s.nq) continue;
-    const bool empty = seen[qb] == 0;
-    const float r = empty ? 0.0f : 1.0f / total;
-    uint16_t* dst = const_cast<uint16_t*>(a.out.p) + head * a.out.sh + (int64_t)(s.q0 + row[qb]) * a.out.st;
-#pragma unroll
-    for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const u32x2 w = {pack2(o[qb][cb][4 * i] * r, o[qb][cb][4 * i + 1] * r), pack2(o[qb][cb][4 * i + 2] * r, o[qb][cb][4 * i + 3] * r)};
-        *reinterpret_cast<u32x2*>(dst + 32 * cb + 8 * i + 4 * h) = w;
-      }
-    if (h == 0)
-      a.lse[(int64_t)head * a.rows_q + s.q0 + row[qb]] = empty ? -kInf : ((ref[qb] == -kInf ? 0.0f : ref[qb]) + log2f(total)) * kLn2;
-  }
+    };
+    if (clean_up) product(std::true_type{});
+    else product(std::false_type{});
+  });
+  if (left_out)
+    add_not_finite(a.v.p + b.kv * a.v.sh + b.s.k0 * a.v.st, a.v.st, b.wave_least / 64 * 64, b.wave_most, lane, [&](int r) { return r < b.seen; }, o);
+  const float total = half_sum(sum);
+  if (b.row >= b.s.nq) return;
+  const bool empty = b.seen == 0;
+  write_columns(const_cast<uint16_t*>(b.at(a.out, 0)), o, empty ? 0.0f : 1.0f / total, h);
+  if (h == 0) a.lse[(int64_t)b.head * a.rows_q + b.s.q0 + b.row] = empty ? -kInf : ((ref == -kInf ? 0.0f : ref) + log2f(total)) * kLn2;
 }
 
-// ---- gradient of the queries (and delta) ----------------------------------------------------------------------------
-
-template <int QB>
-__global__ __launch_bounds__(256, 2) void seq_grad_q_kernel(SeqArgs a, int blocks) {
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void seq_grad_q_kernel(SeqArgs a, int blocks) {
   __shared__ __align__(16) char lds[2][2][kTileBytes];
   __shared__ int dirty[2];
   const int lane = threadIdx.x % 64, h = lane / 32;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int id = dealt(blockIdx.x, gridDim.x);
-  const int unit = id / blocks, block = blocks - 1 - id % blocks;
-  const int head = unit / a.sequences;
-  const Sequence s = sequence_of(a, unit % a.sequences);
-  const int row0 = block * 128 * QB;
-  if (row0 >= s.nq) return;
-  const int kv = head / (a.heads / a.kv_heads);
-  const uint16_t* kb = a.k.p + kv * a.k.sh + s.k0 * a.k.st;
-  const uint16_t* vb = a.v.p + kv * a.v.sh + s.k0 * a.v.st;
-  int row[QB], seen[QB];
-  float lse2[QB], delta[QB];
-  bf16x8 qf[QB][4], df[QB][4];
+  const QueryBlock b = QueryBlock::of<WAVES>(a, blocks, __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane);
+  if (!b.any) return;
+  bf16x8 qf[4], df[4];
+  float dot = 0.0f;
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    row[qb] = row0 + wave * 32 * QB + qb * 32 + lane % 32;
-    const int i = min(row[qb], s.nq - 1);
-    seen[qb] = keys_seen(a, s, i);
-    const uint16_t* q = a.q.p + head * a.q.sh + (int64_t)(s.q0 + i) * a.q.st + 8 * h;
-    const uint16_t* d = a.dout.p + head * a.dout.sh + (int64_t)(s.q0 + i) * a.dout.st + 8 * h;
-    const uint16_t* o = a.out.p + head * a.out.sh + (int64_t)(s.q0 + i) * a.out.st + 8 * h;
-    float dot = 0.0f;
+  for (int c = 0; c < 4; ++c) {
+    qf[c] = *reinterpret_cast<const bf16x8*>(b.at(a.q, lane) + 16 * c);
+    df[c] = *reinterpret_cast<const bf16x8*>(b.at(a.dout, lane) + 16 * c);
+    const bf16x8 of = *reinterpret_cast<const bf16x8*>(b.at(a.out, lane) + 16 * c);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      qf[qb][c] = *reinterpret_cast<const bf16x8*>(q + 16 * c);
-      df[qb][c] = *reinterpret_cast<const bf16x8*>(d + 16 * c);
-      const bf16x8 of = *reinterpret_cast<const bf16x8*>(o + 16 * c);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) dot += (float)df[qb][c][e] * (float)of[e];
-    }
-    delta[qb] = half_sum(dot);
-    const int64_t at = (int64_t)head * a.rows_q + s.q0 + i;
-    lse2[qb] = a.lse[at] * kLog2e;
-    if (h == 0 && row[qb] < s.nq) a.delta[at] = delta[qb];
+    for (int e = 0; e < 8; ++e) dot += (float)df[c][e] * (float)of[e];
   }
-  const int wave_row = min(row0 + wave * 32 * QB, s.nq - 1);
-  const int wave_least = keys_seen(a, s, wave_row), wave_most = keys_seen(a, s, min(wave_row + 32 * QB - 1, s.nq - 1));
-  const int wg_least = keys_seen(a, s, row0), wg_most = keys_seen(a, s, min(row0 + 128 * QB - 1, s.nq - 1));
-  const int tiles = (wg_most + 63) / 64;
+  const float delta = half_sum(dot);
+  const int64_t at = (int64_t)b.head * a.rows_q + b.s.q0 + min(b.row, b.s.nq - 1);
+  const float lse2 = a.lse[at] * kLog2e;
+  if (h == 0 && b.row < b.s.nq) a.delta[at] = delta;
   const Reader rd(lane);
   const float c2 = a.scale * kLog2e;
-  f32x16 g[QB][2] = {};
+  f32x16 g[2] = {};
+  bool left_out = false;
 
-  bool left_out = false;  // some of them are to be added
-  if (threadIdx.x < 2) dirty[threadIdx.x] = 0;
-  Stage<256> sk, sv;
-  auto fetch = [&](int t) {
-    sk.load(kb, a.k.st, 64 * t, s.nk);
-    sv.load(vb, a.v.st, 64 * t, s.nk);
-  };
-  auto put = [&](int t) {
-    sk.store(lds[t & 1][0]);
-    sv.store(lds[t & 1][1]);
-    if (64 * (t + 1) > wg_least && __any(sk.any_not_finite())) dirty[t & 1] = t + 1;
-  };
-  auto tile = [&](int t, auto masked_) {
+  over_keys<WAVES, 0>(a, b, lds, dirty, [&](int t, const char* kt, const char* vt, auto masked_, bool clean_up) {
     constexpr bool kMasked = decltype(masked_)::value;
-    const char* kt = lds[t & 1][0];
-    const char* vt = lds[t & 1][1];
-    const bool clean_up = kMasked && dirty[t & 1] == t + 1;
     if (kMasked) left_out |= clean_up;
 #pragma unroll
     for (int kh = 0; kh < 2; ++kh) {
-      bf16x8 ds[QB][2];
-      {
-        bf16x8 kf[4], vf[4];
+      f32x16 x = {}, y = {};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          kf[c] = rd.along(kt, kh, c);
-          vf[c] = rd.along(vt, kh, c);
-        }
+      for (int c = 0; c < 4; ++c) x = mfma(rd.along(kt, kh, c), qf[c], x);
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-          f32x16 x = {}, y = {};
+      for (int c = 0; c < 4; ++c) y = mfma(rd.along(vt, kh, c), df[c], y);
+      const int left = b.seen - (64 * t + 32 * kh + 4 * h);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) x = mfma(kf[c], qf[qb][c], x);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) y = mfma(vf[c], df[qb][c], y);
-          const int left = seen[qb] - (64 * t + 32 * kh + 4 * h);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float p = exp2_(x[i] * c2 - lse2[qb]);
-            x[i] = p * (y[i] - delta[qb]);
-            if (kMasked) x[i] = 8 * (i / 4) + i % 4 < left ? x[i] : 0.0f;
-          }
-          ds[qb][0] = pack8(x, 0);
-          ds[qb][1] = pack8(x, 1);
-        }
+      for (int i = 0; i < 16; ++i) {
+        const float p = exp2_(x[i] * c2 - lse2);
+        x[i] = p * (y[i] - delta);
+        if (kMasked) x[i] = 8 * (i / 4) + i % 4 < left ? x[i] : 0.0f;
       }
       auto product = [&](auto clean_) {
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
+          const bf16x8 ds = pack8(x, ks);
 #pragma unroll
           for (int cb = 0; cb < 2; ++cb) {
             bf16x8 kf = rd.across(kt, kh, cb, ks);
             if (decltype(clean_)::value) kf = cleaned(kf);
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) g[qb][cb] = mfma(kf, ds[qb][ks], g[qb][cb]);
+            g[cb] = mfma(kf, ds, g[cb]);
           }
         }
       };
-      __builtin_amdgcn_sched_barrier(0);
       if (clean_up) product(std::true_type{});
       else product(std::false_type{});
-      __builtin_amdgcn_sched_barrier(0);
     }
-  };
-  if (tiles > 0) {
-    __syncthreads();
-    fetch(0);
-    put(0);
-    __syncthreads();
-    for (int t = 0; t < tiles; ++t) {
-      if (t + 1 < tiles) fetch(t + 1);
-      if (64 * (t + 1) <= wave_least) tile(t, std::false_type{});
-      else if (64 * t < wave_most) tile(t, std::true_type{});
-      if (t + 1 < tiles) put(t + 1);
-      __syncthreads();
-    }
-  }
-  if (left_out) {
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
-      add_not_finite(kb, a.k.st, wave_least / 64 * 64, wave_most, lane, [&](int r) { return r < seen[qb]; }, g[qb]);
-  }
-#pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    if (row[qb] >= s.nq) continue;
-    uint16_t* dst = const_cast<uint16_t*>(a.dq.p) + head * a.dq.sh + (int64_t)(s.q0 + row[qb]) * a.dq.st;
-#pragma unroll
-    for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const u32x2 w = {pack2(g[qb][cb][4 * i] * a.scale, g[qb][cb][4 * i + 1] * a.scale),
-                         pack2(g[qb][cb][4 * i + 2] * a.scale, g[qb][cb][4 * i + 3] * a.scale)};
-        *reinterpret_cast<u32x2*>(dst + 32 * cb + 8 * i + 4 * h) = w;
-      }
-  }
+  });
+  if (left_out)
+    add_not_finite(a.k.p + b.kv * a.k.sh + b.s.k0 * a.k.st, a.k.st, b.wave_least / 64 * 64, b.wave_most, lane, [&](int r) { return r < b.seen; }, g);
+  if (b.row < b.s.nq) write_columns(const_cast<uint16_t*>(b.at(a.dq, 0)), g, a.scale, h);
 }
 
 // ---- gradients of the keys and values -------------------------------------------------------------------------------
@@ -638,10 +537,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void seq_grad_kv_kernel(SeqArgs a, i
           }
         }
       };
-      __builtin_amdgcn_sched_barrier(0);
       if (clean_up) product(std::true_type{});
       else product(std::false_type{});
-      __builtin_amdgcn_sched_barrier(0);
     }
   };
   if (steps > 0) {
@@ -666,17 +563,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void seq_grad_kv_kernel(SeqArgs a, i
     }
   }
   if (key >= s.nk) return;
-  uint16_t* to_k = const_cast<uint16_t*>(a.dk.p) + kv * a.dk.sh + (int64_t)(s.k0 + key) * a.dk.st;
-  uint16_t* to_v = const_cast<uint16_t*>(a.dv.p) + kv * a.dv.sh + (int64_t)(s.k0 + key) * a.dv.st;
-#pragma unroll
-  for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const u32x2 w = {pack2(dk[cb][4 * i] * a.scale, dk[cb][4 * i + 1] * a.scale), pack2(dk[cb][4 * i + 2] * a.scale, dk[cb][4 * i + 3] * a.scale)};
-      const u32x2 u = {pack2(dv[cb][4 * i], dv[cb][4 * i + 1]), pack2(dv[cb][4 * i + 2], dv[cb][4 * i + 3])};
-      *reinterpret_cast<u32x2*>(to_k + 32 * cb + 8 * i + 4 * h) = w;
-      *reinterpret_cast<u32x2*>(to_v + 32 * cb + 8 * i + 4 * h) = u;
-    }
+  write_columns(const_cast<uint16_t*>(a.dk.p) + kv * a.dk.sh + (int64_t)(s.k0 + key) * a.dk.st, dk, a.scale, h);
+  write_columns(const_cast<uint16_t*>(a.dv.p) + kv * a.dv.sh + (int64_t)(s.k0 + key) * a.dv.st, dv, 1.0f, h);
 }
 
 long long grid_of(int longest, int rows, int heads, int sequences) { return ((long long)longest + rows - 1) / rows * heads * sequences; }
@@ -689,40 +577,28 @@ bool seq_attend_fits(const SeqArgs& a) {
   return grid_of(a.longest_q, 128, a.heads, a.sequences) <= kMostWorkgroups && grid_of(a.longest_k, 128, a.kv_heads, a.sequences) <= kMostWorkgroups;
 }
 
-// Blocks of 256 rows read keys and values half as often as blocks of 128; where they would leave compute units without
-// work, the shorter ones.
+// Eight waves read a tile half as often as two workgroups of four; where blocks of 256 rows would leave compute units
+// without work, the shorter ones.
 hipError_t launch_seq_attend(const SeqArgs& a, hipStream_t stream) {
-  if (grid_of(a.longest_q, 128, a.heads, a.sequences) == 0) return hipSuccess;
-  if (grid_of(a.longest_q, 256, a.heads, a.sequences) >= 512) {
-    const int blocks = (a.longest_q + 255) / 256;
-    seq_attend_kernel<2><<<blocks * a.heads * a.sequences, 256, 0, stream>>>(a, blocks);
-  } else {
-    const int blocks = (a.longest_q + 127) / 128;
-    seq_attend_kernel<1><<<blocks * a.heads * a.sequences, 256, 0, stream>>>(a, blocks);
-  }
+  const long long small = grid_of(a.longest_q, 128, a.heads, a.sequences), large = grid_of(a.longest_q, 256, a.heads, a.sequences);
+  if (small == 0) return hipSuccess;
+  if (large >= 256) seq_attend_kernel<8><<<(int)large, 512, 0, stream>>>(a, (a.longest_q + 255) / 256);
+  else seq_attend_kernel<4><<<(int)small, 256, 0, stream>>>(a, (a.longest_q + 127) / 128);
   return hipGetLastError();
 }
 
 hipError_t launch_seq_attend_grad(const SeqArgs& a, hipStream_t stream) {
-  if (grid_of(a.longest_q, 128, a.heads, a.sequences) > 0) {
-    if (grid_of(a.longest_q, 256, a.heads, a.sequences) >= 512) {
-      const int blocks = (a.longest_q + 255) / 256;
-      seq_grad_q_kernel<2><<<blocks * a.heads * a.sequences, 256, 0, stream>>>(a, blocks);
-    } else {
-      const int blocks = (a.longest_q + 127) / 128;
-      seq_grad_q_kernel<1><<<blocks * a.heads * a.sequences, 256, 0, stream>>>(a, blocks);
-    }
+  const long long small_q = grid_of(a.longest_q, 128, a.heads, a.sequences), large_q = grid_of(a.longest_q, 256, a.heads, a.sequences);
+  const long long small_k = grid_of(a.longest_k, 128, a.kv_heads, a.sequences), large_k = grid_of(a.longest_k, 256, a.kv_heads, a.sequences);
+  if (small_q > 0) {
+    if (large_q >= 256) seq_grad_q_kernel<8><<<(int)large_q, 512, 0, stream>>>(a, (a.longest_q + 255) / 256);
+    else seq_grad_q_kernel<4><<<(int)small_q, 256, 0, stream>>>(a, (a.longest_q + 127) / 128);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (grid_of(a.longest_k, 128, a.kv_heads, a.sequences) > 0) {
-    if (grid_of(a.longest_k, 256, a.kv_heads, a.sequences) >= 256) {
-      const int blocks = (a.longest_k + 255) / 256;
-      seq_grad_kv_kernel<8><<<blocks * a.kv_heads * a.sequences, 512, 0, stream>>>(a, blocks);
-    } else {
-      const int blocks = (a.longest_k + 127) / 128;
-      seq_grad_kv_kernel<4><<<blocks * a.kv_heads * a.sequences, 256, 0, stream>>>(a, blocks);
-    }
+  if (small_k > 0) {
+    if (large_k >= 256) seq_grad_kv_kernel<8><<<(int)large_k, 512, 0, stream>>>(a, (a.longest_k + 255) / 256);
+    else seq_grad_kv_kernel<4><<<(int)small_k, 256, 0, stream>>>(a, (a.longest_k + 127) / 128);
     return hipGetLastError();
   }
   return hipSuccess;
