@@ -282,7 +282,9 @@ typedef struct {
   float softmax_scale;           /* >= 0; 0 -> 1/sqrt(64)                                      */
 } xsv_seq_config;
 /* q, out: bf16 [heads][rows_q][64], k, v: bf16 [kv_heads][rows_k][64] via strides; lse: float [heads][rows_q]. */
-int xsv_seq_attend(void* hip_stream, const xsv_seq_config* cfg, xsv_tensor q, xsv_tensor k, xsv_tensor v, xsv_tensor out, float* lse);
+int xsv_seq_attend(void* hip_stream, const xsv_seq_config* cfg, xsv_tensor q, xsv_tensor k, xsv_tensor v, xsv_tensor out, float* lse,
+                   void* workspace, int64_t workspace_bytes);
+int xsv_seq_attend_workspace(const xsv_seq_config* cfg, int64_t* bytes);
 /* Its gradient: out and lse as xsv_seq_attend left them, dout the gradient of out; writes dq, dk, dv (dk and dv summed over the
  * heads that share a key head).  The same bits every time. */
 int xsv_seq_attend_grad(void* hip_stream, const xsv_seq_config* cfg, xsv_tensor q, xsv_tensor k, xsv_tensor v, xsv_tensor out, const float* lse,

@@ -46,7 +46,12 @@ struct SeqArgs {
   int heads, kv_heads, sequences, rows_q, rows_k, longest_q, longest_k;
   int causal;
   float scale;
+  float* part;       // small launches: what workgroups that share the tiles of a block leave, [part][head][row][64]
+  float* part_sums;  // and their references and sums, [part][head][row][2]
+  int parts;         // workgroups that do so (set by the launchers)
 };
+int64_t seq_attend_workspace(const SeqArgs& a);   // bytes of SeqArgs::part
+int64_t seq_attend_grad_parts(const SeqArgs& a);
 hipError_t launch_seq_attend(const SeqArgs& a, hipStream_t stream);
 hipError_t launch_seq_attend_grad(const SeqArgs& a, hipStream_t stream);
 bool seq_attend_fits(const SeqArgs& a);  // its grids stay within what a launch can have

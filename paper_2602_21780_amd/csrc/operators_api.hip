@@ -119,22 +119,37 @@ int xsv_norm_rotate_grad(void* hip_stream, const xsv_rotate_config* c, xsv_tenso
   return launched(launch_rotate_grad(a, c->norm, c->axes, c->interleaved != 0, static_cast<hipStream_t>(hip_stream)));
 }
 
-int xsv_seq_attend(void* hip_stream, const xsv_seq_config* c, xsv_tensor q, xsv_tensor k, xsv_tensor v, xsv_tensor out, float* lse) {
+int xsv_seq_attend_workspace(const xsv_seq_config* c, int64_t* bytes) {
   const int rc = check_seq(c);
+  if (rc != XSV_OK) return rc;
+  if (!bytes) return XSV_ERR_ARG;
+  *bytes = seq_attend_workspace(seq_args(*c));
+  return XSV_OK;
+}
+
+int xsv_seq_attend(void* hip_stream, const xsv_seq_config* c, xsv_tensor q, xsv_tensor k, xsv_tensor v, xsv_tensor out, float* lse, void* workspace,
+                   int64_t workspace_bytes) {
+  int64_t need = 0;
+  const int rc = xsv_seq_attend_workspace(c, &need);
   if (rc != XSV_OK) return rc;
   SeqArgs a = seq_args(*c);
   if (!rows_of(q, c->rows_q, &a.q) || !rows_of(k, c->rows_k, &a.k) || !rows_of(v, c->rows_k, &a.v) || !rows_of(out, c->rows_q, &a.out)) return XSV_ERR_ARG;
   if (c->rows_q > 0 && (!lse || !aligned_to(lse, 4))) return XSV_ERR_ARG;
+  if (need > 0 && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < need)) return XSV_ERR_ARG;
   a.lse = lse;
+  a.part = static_cast<float*>(workspace);
   if (!seq_attend_fits(a)) return XSV_ERR_UNSUPPORTED;
   return launched(launch_seq_attend(a, static_cast<hipStream_t>(hip_stream)));
 }
+
+// delta, then the parts
+static int64_t delta_bytes(const xsv_seq_config& c) { return ((int64_t)c.heads * c.rows_q * (int64_t)sizeof(float) + 15) / 16 * 16; }
 
 int xsv_seq_attend_grad_workspace(const xsv_seq_config* c, int64_t* bytes) {
   const int rc = check_seq(c);
   if (rc != XSV_OK) return rc;
   if (!bytes) return XSV_ERR_ARG;
-  *bytes = (int64_t)c->heads * c->rows_q * (int64_t)sizeof(float);
+  *bytes = delta_bytes(*c) + seq_attend_grad_parts(seq_args(*c));
   return XSV_OK;
 }
 
@@ -151,6 +166,7 @@ int xsv_seq_attend_grad(void* hip_stream, const xsv_seq_config* c, xsv_tensor q,
   if (need > 0 && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < need)) return XSV_ERR_ARG;
   a.lse = const_cast<float*>(lse);
   a.delta = static_cast<float*>(workspace);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + delta_bytes(*c));
   if (!seq_attend_fits(a)) return XSV_ERR_UNSUPPORTED;
   return launched(launch_seq_attend_grad(a, static_cast<hipStream_t>(hip_stream)));
 }

@@ -30,9 +30,13 @@ using u32x4 = __attribute__((ext_vector_type(4))) uint32_t;
 using i16x4 = __attribute__((ext_vector_type(4))) short;
 using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
 using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
+using f32x2 = __attribute__((ext_vector_type(2))) float;
 using f32x4 = __attribute__((ext_vector_type(4))) float;
 using f32x16 = __attribute__((ext_vector_type(16))) float;
 using lds_i16x4 = __attribute__((address_space(3))) i16x4;
+using lds_u32x4 = __attribute__((address_space(3))) u32x4;
+using lds_f32x4 = __attribute__((address_space(3))) f32x4;
+using lds_char = __attribute__((address_space(3))) const char;
 
 constexpr int kRow = 128;             // bytes of a row in LDS
 constexpr int kTileBytes = 64 * kRow;
@@ -45,7 +49,10 @@ constexpr float kMaxPart = 16777216.0f;
 
 __device__ __forceinline__ int swizzle(int row) { return ((row >> 1) & 1) << 2 | ((row >> 2) & 1) << 1 | ((row >> 3) & 1); }
 
-__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+// Operands are kept as four dwords (what lives across a loop as eight bf16 is taken apart into sixteen-bit pieces by the compiler).
+__device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
 
 __device__ __forceinline__ float half_sum(float x) {  // of the two lanes that hold the same column
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -62,34 +69,40 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 }
 
 // Eight values of a column block as the operand of 16 rows: accumulator registers 8 ks .. 8 ks + 7.
-__device__ __forceinline__ bf16x8 pack8(const f32x16& x, int ks) {
+__device__ __forceinline__ u32x4 pack8(const f32x16& x, int ks) {
   u32x4 r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) r[i] = pack2(x[8 * ks + 2 * i], x[8 * ks + 2 * i + 1]);
-  return __builtin_bit_cast(bf16x8, r);
+  return r;
 }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// How a lane reads a tile.  along: 8 channels (16 s + 8 (lane / 32) ..) of row lane % 32 of a block of 32 rows.
-// across: channel 32 cb + lane % 32 of the rows 16 ks + 8 r + 4 (lane / 32) + 0..3, r = 0, 1, of such a block: the order in
-// which an accumulator's registers hold rows.
+// How a lane reads a tile, `at` bytes behind `origin`.  along: 8 channels (16 s + 8 (lane / 32) ..) of row lane % 32 of a block of 32
+// rows.  across: channel 32 cb + lane % 32 of the rows 16 ks + 8 r + 4 (lane / 32) + 0..3, r = 0, 1, of such a block: the order in
+// which an accumulator's registers hold rows.  The permuted addresses are worked out once; with a constant `at` a read is one instruction.
 struct Reader {
-  uint32_t along_, across_;
-  __device__ __forceinline__ explicit Reader(int lane) {
+  uint32_t along_[4], across_[2][2];
+  __device__ __forceinline__ Reader(const char* origin, int lane) {
+    const uint32_t base = (uint32_t)(size_t)(lds_char*)origin;
     const int row = lane % 32, h = lane / 32;
-    along_ = row * kRow + ((h ^ swizzle(row)) << 4);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) along_[s] = base + row * kRow + (((2 * s + h) ^ swizzle(row)) << 4);
     const int p = lane % 16, row4 = 4 * h + p / 4;  // transposing reads: 4 lanes give a row, 16 lanes take a channel each
-    across_ = row4 * kRow + (((2 * ((lane / 16) % 2) + (p % 4) / 2) ^ swizzle(row4)) << 4) + 8 * (p % 2);
+#pragma unroll
+    for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+        across_[cb][r] = base + (row4 + 8 * r) * kRow + (((4 * cb + 2 * ((lane / 16) % 2) + (p % 4) / 2) ^ swizzle(row4 + 8 * r)) << 4) + 8 * (p % 2);
   }
-  __device__ __forceinline__ bf16x8 along(const char* tile, int block, int s) const {
-    return *reinterpret_cast<const bf16x8*>(tile + block * 32 * kRow + (along_ ^ (s << 5)));
+  __device__ __forceinline__ u32x4 along(int at, int block, int s) const {
+    return *(lds_u32x4*)(along_[s] + at + block * 32 * kRow);
   }
-  __device__ __forceinline__ bf16x8 across(const char* tile, int block, int cb, int ks) const {
-    const char* base = tile + block * 32 * kRow + ks * 16 * kRow;
-    const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(base + (across_ ^ (cb << 6))));
-    const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(base + 8 * kRow + (across_ ^ (cb << 6) ^ (1 << 4))));
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  __device__ __forceinline__ u32x4 across(int at, int block, int cb, int ks) const {
+    at += (block * 32 + ks * 16) * kRow;
+    const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(across_[cb][0] + at));
+    const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(across_[cb][1] + at));
+    return __builtin_bit_cast(u32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 };
 
@@ -97,11 +110,11 @@ __device__ __forceinline__ bool not_finite(uint32_t two) { return (two & 0x7f80u
 __device__ __forceinline__ uint32_t finite_or_zero(uint32_t two) {
   return two & (((two & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((two & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u));
 }
-__device__ __forceinline__ bf16x8 cleaned(bf16x8 x) {
-  u32x4 r = __builtin_bit_cast(u32x4, x);
+__device__ __forceinline__ u32x4 cleaned(u32x4 x) {
+  u32x4 r = x;
 #pragma unroll
   for (int i = 0; i < 4; ++i) r[i] = finite_or_zero(r[i]);
-  return __builtin_bit_cast(bf16x8, r);
+  return r;
 }
 
 // Where a mask cuts a tile, a value that is not finite must not reach queries that do not see its row, but 0 * NaN does: the
@@ -126,32 +139,34 @@ __device__ __forceinline__ void add_not_finite(const uint16_t* base, int64_t st,
   }
 }
 
-// The pieces of a tile that a thread of a workgroup of THREADS brings to LDS.
-template <int THREADS>
+// The pieces of TILES consecutive tiles that a thread of a workgroup of THREADS brings to LDS.
+template <int THREADS, int TILES>
 struct Stage {
-  static constexpr int kPieces = 512 / THREADS;
+  static constexpr int kPieces = 512 * TILES / THREADS;
   u32x4 r[kPieces];
-  // rows row0 .. row0 + 63 of a sequence of n rows that begins at `base`; rows behind it are zeros
+  // rows row0 .. of a sequence of n > 0 rows that begins at `base`; those behind it are copies of the last, which no result uses
   __device__ __forceinline__ void load(const uint16_t* base, int64_t st, int row0, int n) {
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p) {
-      const int at = p * THREADS + threadIdx.x, row = row0 + at / 8;
-      r[p] = row < n ? *reinterpret_cast<const u32x4*>(base + row * st + 8 * (at % 8)) : u32x4{};
-    }
+    for (int p = 0; p < kPieces; ++p) load_piece(p, base, st, row0 + p * (THREADS / 8) + threadIdx.x / 8, n);
   }
-  __device__ __forceinline__ void store(char* tile) const {
+  __device__ __forceinline__ void load_piece(int p, const uint16_t* base, int64_t st, int row, int n) {
+    r[p] = *reinterpret_cast<const u32x4*>(base + min(row, n - 1) * st + 8 * (threadIdx.x % 8));
+  }
+  // tile j goes to `tiles` + 2 j tiles: the two tensors' tiles take turns
+  __device__ __forceinline__ void store(char* tiles) const {
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
-      const int at = p * THREADS + threadIdx.x, row = at / 8;
-      *reinterpret_cast<u32x4*>(tile + row * kRow + (((at % 8) ^ swizzle(row)) << 4)) = r[p];
+      const int row = p * (THREADS / 8) + threadIdx.x / 8;
+      *reinterpret_cast<u32x4*>(tiles + (row / 64) * 2 * kTileBytes + (row % 64) * kRow + (((threadIdx.x % 8) ^ swizzle(row)) << 4)) = r[p];
     }
   }
-  __device__ __forceinline__ bool any_not_finite() const {
+  // of tile j, in the pieces that this thread has
+  __device__ __forceinline__ bool any_not_finite(int j) const {
     bool bad = false;
 #pragma unroll
     for (int p = 0; p < kPieces; ++p)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) bad |= not_finite(r[p][i]);
+      for (int i = 0; i < 4; ++i) bad |= (p * (THREADS / 8) + (int)threadIdx.x / 8) / 64 == j && not_finite(r[p][i]);
     return bad;
   }
 };
@@ -182,32 +197,57 @@ __device__ __forceinline__ int first_query(const SeqArgs& a, const Sequence& s, 
   return max(0, key / a.causal * a.causal - (s.nk - s.nq));
 }
 
-// Workgroups are dealt to the XCDs one by one; this gives each XCD a run of consecutive ones, which share keys and values
-// (or queries) through its L2.
-__device__ __forceinline__ int dealt(int wg, int n) {
-  const int xcd = wg % 8, q = n / 8, r = n % 8;
-  return xcd * q + min(xcd, r) + wg / 8;
+// Workgroups are dealt to the XCDs one by one; this gives each XCD the blocks of consecutive units, which share keys and values (or
+// queries) through its L2.  With a mask the blocks of a unit differ in length, and where an XCD has whole units it takes the
+// longest blocks of all of them first (long: block 0 counted from the longest).
+struct Dealt {
+  int unit, block;
+};
+__device__ __forceinline__ Dealt dealt(const SeqArgs& a, int units, int blocks) {
+  const int n = units * blocks, xcd = blockIdx.x % 8, at = blockIdx.x / 8;
+  if (a.causal && units % 8 == 0) {
+    const int own = units / 8;
+    return Dealt{xcd * own + at % own, at / own};
+  }
+  const int id = xcd * (n / 8) + min(xcd, n % 8) + at;
+  return Dealt{id / blocks, id % blocks};
+}
+
+
+// A stretch of a pipeline, in this order whatever the compiler's scheduler would rather do: products one by one, behind each some LDS
+// reads for later ones and a share of the arithmetic.
+template <int N, typename Product, typename Read, typename Arithmetic>
+__device__ __forceinline__ void in_order(Product product, Read read, Arithmetic arithmetic) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    product(i);
+    read(i);
+    arithmetic(i);
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
 
 // ---- what owns queries: forward, and the gradient of the queries ----------------------------------------------------
 
-// A workgroup's place: WAVES x 32 queries of one head of one sequence.  Blocks with many keys to see come first.
+// A workgroup's place: ROWS x 32 queries of one head of one sequence, every 32 of them worked on by SPLIT waves, which take the
+// workgroup's tiles in turn and join their results in LDS at the end.  In small launches `parts` workgroups share the tiles of such a
+// block, and leave results in fp32 that a second launch joins, in their order.  Blocks with many keys to see come first.
 struct QueryBlock {
   Sequence s;
-  int head, kv, row0;
+  int head, kv, row0, part;
   int row, seen;              // the lane's query (behind the last: a copy of it that nobody writes) and the keys it sees
   int wave_least, wave_most;  // keys that all, and any, of the wave's queries see; of the workgroup's
   int wg_least, tiles;
   bool any;
-  template <int WAVES>
+  template <int ROWS>
   __device__ __forceinline__ static QueryBlock of(const SeqArgs& a, int blocks, int wave, int lane) {
     QueryBlock b;
-    const int id = dealt(blockIdx.x, gridDim.x);
-    const int unit = id / blocks;
-    b.head = unit / a.sequences;
+    const Dealt d = dealt(a, a.heads * a.sequences, blocks * a.parts);
+    b.head = d.unit / a.sequences;
     b.kv = b.head / (a.heads / a.kv_heads);
-    b.s = sequence_of(a, unit % a.sequences);
-    b.row0 = (blocks - 1 - id % blocks) * 32 * WAVES;
+    b.s = sequence_of(a, d.unit % a.sequences);
+    b.row0 = (blocks - 1 - d.block / a.parts) * 32 * ROWS;
+    b.part = d.block % a.parts;
     b.any = b.row0 < b.s.nq;
     if (!b.any) return b;
     const int last = b.s.nq - 1, first = min(b.row0 + wave * 32, last);
@@ -216,7 +256,7 @@ struct QueryBlock {
     b.wave_least = keys_seen(a, b.s, first);  // (rows ascend, and so does what they see)
     b.wave_most = keys_seen(a, b.s, min(first + 31, last));
     b.wg_least = keys_seen(a, b.s, b.row0);
-    b.tiles = (keys_seen(a, b.s, min(b.row0 + 32 * WAVES - 1, last)) + 63) / 64;
+    b.tiles = (keys_seen(a, b.s, min(b.row0 + 32 * ROWS - 1, last)) + 63) / 64;
     return b;
   }
   // the lane's part of a row of queries, outputs or their gradients
@@ -225,36 +265,108 @@ struct QueryBlock {
   }
 };
 
-// Tiles of keys and values through two buffers: the next one's loads are on their way while a tile is worked on.
-// work(t, keys, values, masked, dirty): dirty, only where the mask cuts the tile: keys (WATCH = 0) or values (1) that are not finite.
-template <int WAVES, int WATCH, typename F>
-__device__ __forceinline__ void over_keys(const SeqArgs& a, const QueryBlock& b, char (*lds)[2][kTileBytes], int* dirty, F work) {
-  const uint16_t* kb = a.k.p + b.kv * a.k.sh + b.s.k0 * a.k.st;
-  const uint16_t* vb = a.v.p + b.kv * a.v.sh + b.s.k0 * a.v.st;
-  Stage<64 * WAVES> sk, sv;
-  auto fetch = [&](int t) {
-    sk.load(kb, a.k.st, 64 * t, b.s.nk);
-    sv.load(vb, a.v.st, 64 * t, b.s.nk);
-  };
-  auto put = [&](int t) {
-    sk.store(lds[t & 1][0]);
-    sv.store(lds[t & 1][1]);
-    if (64 * (t + 1) > b.wg_least && __any((WATCH ? sv : sk).any_not_finite())) dirty[t & 1] = t + 1;
-  };
-  if (b.tiles <= 0) return;
-  if (threadIdx.x < 2) dirty[threadIdx.x] = 0;
-  __syncthreads();
+// Steps of tiles through three buffers: while a step's tiles are worked on, the next one's go from registers to LDS and the loads of
+// those behind them are on their way.  Of a wave's tiles, `lead` are taken one by one, then `full` as a pipeline over their halves, then the
+// rest one by one.  The pipeline: every stretch of vector arithmetic, on the logits of one half, has independent products beside it,
+// those of the next half and the second products of the one before, and a stretch's first operands are read in the stretch before.  (Read
+// where they are used, by eight waves that a barrier keeps in step, they had the matrix pipe wait for 0.35 us twice a tile.)
+//   first(tile):         first products of its first half (a tile is where it begins, from this wave's place in the first buffer)
+//   front(tile, before): arithmetic of the first half; first products of the second, second products of the second half of the tile before
+//   back(tile, next):    arithmetic of the second half; second products of the first, first products of the first half of the next tile
+//   last(tile):          second products of the second half
+//   whole(step, tile, buffer): one tile by itself
+template <int SPLIT>
+using Buffers = char[3][SPLIT][2][kTileBytes];  // [buffer][tile][the two tensors]
+template <int SPLIT, typename Fetch, typename Put, typename First, typename Front, typename Back, typename Last, typename Whole>
+__device__ __forceinline__ void over_tiles(int steps, int lead, int full, Fetch fetch, Put put, First first, Front front, Back back, Last last, Whole whole) {
+  using std::false_type;
+  using std::true_type;
+  constexpr int kStep = SPLIT * 2 * kTileBytes;  // of a buffer
+  if (steps == 0) return;
+  auto after = [](int at) { return at == 2 ? 0 : at + 1; };
+  int n = 0, buf = (3 - lead % 3) % 3;  // (the pipeline begins in the first buffer)
   fetch(0);
-  put(0);
+  put(0, buf);
   __syncthreads();
-  for (int t = 0; t < b.tiles; ++t) {
-    if (t + 1 < b.tiles) fetch(t + 1);
-    if (64 * (t + 1) <= b.wave_least) work(t, lds[t & 1][0], lds[t & 1][1], std::false_type{}, false);
-    else if (64 * t < b.wave_most) work(t, lds[t & 1][0], lds[t & 1][1], std::true_type{}, dirty[t & 1] == t + 1);
-    if (t + 1 < b.tiles) put(t + 1);
+  if (steps > 1) fetch(1);
+  auto advance = [&](int at) {
+    if (n + 1 < steps) put(n + 1, after(at));
     __syncthreads();
+    if (n + 2 < steps) fetch(n + 2);
+  };
+  for (; n < lead; ++n, buf = after(buf)) {
+    advance(buf);
+    whole(n, buf * kStep, buf);
+  }
+  if (full > 0) {
+    first(0);
+    front(0, 0, false_type{});
+    auto step = [&](auto at_) {  // (three steps a round: the buffers' addresses are constants)
+      constexpr int kAt = decltype(at_)::value, kNext = kAt == 2 ? 0 : kAt + 1;
+      buf = kAt;
+      advance(kAt);
+      if (n + 1 >= lead + full) return false;
+      ++n;
+      back(kAt * kStep, kNext * kStep, true_type{});
+      front(kNext * kStep, kAt * kStep, true_type{});
+      return true;
+    };
+    while (step(std::integral_constant<int, 0>{}) && step(std::integral_constant<int, 1>{}) && step(std::integral_constant<int, 2>{})) {
+    }
+    back(buf * kStep, 0, false_type{});
+    last(buf * kStep);
+    buf = after(buf);
+    ++n;
+  }
+  for (; n < steps; ++n, buf = after(buf)) {
+    advance(buf);
+    whole(n, buf * kStep, buf);
   }
 }
+
+// ... of the keys and values that a block of queries sees; the tiles that the mask cuts for some of the wave's queries come last.
+// whole(t, tile, dirty); dirty: keys (WATCH = 0) or values (1) of a tile that the mask cuts are not finite.
+template <int WAVES, int SPLIT, int WATCH, typename First, typename Front, typename Back, typename Last, typename Whole>
+__device__ __forceinline__ void over_keys(const SeqArgs& a, const QueryBlock& b, int split, Buffers<SPLIT>& lds, int (&dirty)[3][SPLIT], First first,
+                                          Front front, Back back, Last last, Whole whole) {
+  const uint16_t* kb = a.k.p + b.kv * a.k.sh + b.s.k0 * a.k.st;
+  const uint16_t* vb = a.v.p + b.kv * a.v.sh + b.s.k0 * a.v.st;
+  Stage<64 * WAVES, SPLIT> sk, sv;
+  if (threadIdx.x < 3 * SPLIT) (&dirty[0][0])[threadIdx.x] = 0;
+  __syncthreads();
+  const int step = SPLIT * a.parts, from = SPLIT * b.part;  // this workgroup's tiles: step n + from + 0 .. SPLIT - 1
+  over_tiles<SPLIT>(
+      max(0, b.tiles - from + step - 1) / step, 0, max(0, b.wave_least / 64 - (from + split) + step - 1) / step,
+      [&](int n) {
+        sk.load(kb, a.k.st, 64 * (step * n + from), b.s.nk);
+        sv.load(vb, a.v.st, 64 * (step * n + from), b.s.nk);
+      },
+      [&](int n, int buf) {
+        sk.store(lds[buf][0][0]);
+        sv.store(lds[buf][0][1]);
+#pragma unroll
+        for (int j = 0; j < SPLIT; ++j)
+          if (64 * (step * n + from + j + 1) > b.wg_least && __any((WATCH ? sv : sk).any_not_finite(j))) dirty[buf][j] = n + 1;
+      },
+      first, front, back, last,
+      [&](int n, int tile, int buf) {
+        const int t = step * n + from + split;
+        if (64 * t < b.wave_most) whole(t, tile, dirty[buf][split] == n + 1);
+      });
+}
+
+// Where the waves that share columns join: the others' accumulators in LDS, behind the tiles' last use, added one after the other.
+struct Share {
+  float acc[32][64];  // [register][lane]
+  __device__ __forceinline__ void put(const f32x16* x, int lane) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) acc[i][lane] = x[i / 16][i % 16];
+  }
+  __device__ __forceinline__ void add_to(f32x16* x, int lane, float own, float others) const {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i / 16][i % 16] = x[i / 16][i % 16] * own + acc[i][lane] * others;
+  }
+};
 
 __device__ __forceinline__ void write_columns(uint16_t* dst, const f32x16* x, float f, int h) {
 #pragma unroll
@@ -266,339 +378,785 @@ __device__ __forceinline__ void write_columns(uint16_t* dst, const f32x16* x, fl
     }
 }
 
-template <int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void seq_attend_kernel(SeqArgs a, int blocks) {
-  __shared__ __align__(16) char lds[2][2][kTileBytes];  // [buffer][keys, values]
-  __shared__ int dirty[2];                             // number + 1 of a cut tile with values that are not finite
-  const int lane = threadIdx.x % 64, h = lane / 32;
-  const QueryBlock b = QueryBlock::of<WAVES>(a, blocks, __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane);
-  if (!b.any) return;
-  bf16x8 qf[4];
+// ... and a workgroup's share of them in fp32, [part][head][row][64].
+__device__ __forceinline__ void write_part(float* parts, int part, int64_t row, int64_t rows, const f32x16* x, int h) {
+  float* dst = parts + (part * rows + row) * kD;
 #pragma unroll
-  for (int c = 0; c < 4; ++c) qf[c] = *reinterpret_cast<const bf16x8*>(b.at(a.q, lane) + 16 * c);
-  const Reader rd(lane);
+  for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<f32x4*>(dst + 32 * cb + 8 * i + 4 * h) = f32x4{x[cb][4 * i], x[cb][4 * i + 1], x[cb][4 * i + 2], x[cb][4 * i + 3]};
+}
+
+template <int ROWS, int SPLIT>
+__global__ __launch_bounds__(64 * ROWS * SPLIT, ROWS * SPLIT == 4 ? 3 : 2) void seq_attend_kernel(SeqArgs a, int blocks) {
+  constexpr int kWaves = ROWS * SPLIT;
+  __shared__ __align__(16) Buffers<SPLIT> lds;
+  __shared__ int dirty[3][SPLIT];  // step + 1 with a cut tile that has values that are not finite
+  const int lane = threadIdx.x % 64, h = lane / 32;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), split = wave / ROWS;
+  const QueryBlock b = QueryBlock::of<ROWS>(a, blocks, wave % ROWS, lane);
+  if (!b.any) return;
+  u32x4 qf[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) qf[c] = *reinterpret_cast<const u32x4*>(b.at(a.q, lane) + 16 * c);
+  const Reader rd(lds[0][split][0], lane);
   const float c2 = a.scale * kLog2e;
   f32x16 o[2] = {};
   float sum = 0.0f, ref = -kInf;  // ref in powers of two; -inf: no finite logit yet
   bool left_out = false;          // values that are not finite are to be added
 
-  over_keys<WAVES, 1>(a, b, lds, dirty, [&](int t, const char* kt, const char* vt, auto masked_, bool clean_up) {
-    constexpr bool kMasked = decltype(masked_)::value;
-    if (kMasked) left_out |= clean_up;
-    f32x16 x[2];
-    auto logits = [&]() {
+  auto logits = [&](int kt, int kh) {
+    f32x16 z = {};
 #pragma unroll
-      for (int kh = 0; kh < 2; ++kh) {
-        x[kh] = f32x16{};
+    for (int c = 0; c < 4; ++c) z = mfma(rd.along(kt, kh, c), qf[c], z);
+    return z;
+  };
+  auto probabilities = [&](f32x16& x) {
+    const float off = ref == -kInf ? 0.0f : ref;
+    float p0 = 0.0f, p1 = 0.0f;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) x[kh] = mfma(rd.along(kt, kh, c), qf[c], x[kh]);
-        if (kMasked) {
-          const int left = b.seen - (64 * t + 32 * kh + 4 * h);
+    for (int i = 0; i < 16; i += 2) {
+      x[i] = exp2_(x[i] * c2 - off);
+      x[i + 1] = exp2_(x[i + 1] * c2 - off);
+      p0 += x[i];
+      p1 += x[i + 1];
+    }
+    return p0 + p1;
+  };
+  // Where a lane's sum has passed its bound, or there is no reference yet: again with the reference moved.  x: the logits.
+  auto again = [&](f32x16& x, bool move) {
+    float top = x[0];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) x[kh][i] = 8 * (i / 4) + i % 4 < left ? x[kh][i] : -kInf;
-        }
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+    // (a query's two lanes move together, and by themselves: its result does not depend on the wave's other queries)
+    const bool moves = half_max(move ? 1.0f : 0.0f) > 0.0f;
+    const float moved = moves ? fmaxf(ref, half_max(top) * c2) : ref;
+    const float f = ref == -kInf || !moves ? 1.0f : exp2_(ref - moved);  // (from no reference: there is nothing to scale)
+    ref = moved;
+    sum *= f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      o[0][i] *= f;
+      o[1][i] *= f;
+    }
+    return probabilities(x);
+  };
+  auto product = [&](int vt, int kh, const u32x4* p, auto clean_) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int cb = 0; cb < 2; ++cb) {
+        u32x4 vf = rd.across(vt, kh, cb, ks);
+        if (decltype(clean_)::value) vf = cleaned(vf);
+        o[cb] = mfma(vf, p[ks], o[cb]);
       }
-    };
-    float part;
-    auto probabilities = [&]() {
-      const float off = ref == -kInf ? 0.0f : ref;
-      float p[4] = {};
-#pragma unroll
-      for (int kh = 0; kh < 2; ++kh)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          x[kh][i] = exp2_(x[kh][i] * c2 - off);
-          p[i % 4] += x[kh][i];
-        }
-      part = (p[0] + p[1]) + (p[2] + p[3]);
-    };
-    logits();
-    probabilities();
+  };
+
+  f32x16 x;         // logits of the half whose turn it is
+  u32x4 p[2];      // probabilities of the one before
+  u32x4 early[4];  // operands read a stretch ahead: keys of a second half, then values of a first half
+  auto settle = [&](int tile, int half, float part) {  // the half's probabilities, once its sum is known to be in bounds
     const bool move = !(part <= kMaxPart) || ref == -kInf;
     if (__any(move)) {
-      logits();
-      float top = x[0][0];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, fmaxf(x[0][i], x[1][i]));
-      // (a query's two lanes move together, and by themselves: its result does not depend on the wave's other queries)
-      const bool moves = half_max(move ? 1.0f : 0.0f) > 0.0f;
-      const float moved = moves ? fmaxf(ref, half_max(top) * c2) : ref;
-      const float f = ref == -kInf || !moves ? 1.0f : exp2_(ref - moved);  // (from no reference: there is nothing to scale)
-      ref = moved;
-      sum *= f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        o[0][i] *= f;
-        o[1][i] *= f;
-      }
-      probabilities();
+      x = logits(tile, half);
+      part = again(x, move);
     }
     sum += part;
-    auto product = [&](auto clean_) {
+    p[0] = pack8(x, 0);
+    p[1] = pack8(x, 1);
+  };
+  float off, part0, part1;
+  auto begin = [&]() {
+    off = ref == -kInf ? 0.0f : ref;
+    part0 = part1 = 0.0f;
+  };
+  auto two = [&](int i) {  // probabilities 2 i and 2 i + 1
+    x[2 * i] = exp2_(x[2 * i] * c2 - off);
+    x[2 * i + 1] = exp2_(x[2 * i + 1] * c2 - off);
+    part0 += x[2 * i];
+    part1 += x[2 * i + 1];
+  };
+  over_keys<kWaves, SPLIT, 1>(
+      a, b, split, lds, dirty,
+      [&](int tile) {
+        x = logits(tile, 0);
 #pragma unroll
-      for (int kh = 0; kh < 2; ++kh)
+        for (int c = 0; c < 4; ++c) early[c] = rd.along(tile, 1, c);
+      },
+      [&](int tile, int before, auto any_) {
+        constexpr bool kAny = decltype(any_)::value;
+        f32x16 z = {};
+        u32x4 f[4];
+        begin();
+        in_order<8>(
+            [&](int i) {
+              if (i < 4) z = mfma(early[i], qf[i], z);
+              else if (kAny) o[i % 2] = mfma(f[i - 4], p[i / 2 - 2], o[i % 2]);
+            },
+            [&](int i) {
+              if (i >= 4) early[i - 4] = rd.across(tile + kTileBytes, 0, i % 2, i / 2 - 2);
+              else if (kAny) f[i] = rd.across(before + kTileBytes, 1, i % 2, i / 2);
+            },
+            two);
+        settle(tile, 0, part0 + part1);
+        x = z;
+      },
+      [&](int tile, int next, auto more_) {
+        constexpr bool kMore = decltype(more_)::value;
+        f32x16 z = {};
+        u32x4 f[4];
+        begin();
+        in_order<8>(
+            [&](int i) {
+              if (i < 4) o[i % 2] = mfma(early[i], p[i / 2], o[i % 2]);
+              else if (kMore) z = mfma(f[i - 4], qf[i - 4], z);
+            },
+            [&](int i) {
+              if (kMore && i < 2) {
+                f[2 * i] = rd.along(next, 0, 2 * i);
+                f[2 * i + 1] = rd.along(next, 0, 2 * i + 1);
+              }
+              if (kMore && i >= 4) early[i - 4] = rd.along(next, 1, i - 4);
+            },
+            two);
+        settle(tile, 1, part0 + part1);
+        if (kMore) x = z;
+      },
+      [&](int tile) { product(tile + kTileBytes, 1, p, std::false_type{}); },
+      [&](int t, int tile, bool clean_up) {
+        left_out |= clean_up;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          const bf16x8 p = pack8(x[kh], ks);
+        for (int kh = 0; kh < 2; ++kh) {
+          auto masked = [&]() {
+            f32x16 z = logits(tile, kh);
+            const int left = b.seen - (64 * t + 32 * kh + 4 * h);
 #pragma unroll
-          for (int cb = 0; cb < 2; ++cb) {
-            bf16x8 vf = rd.across(vt, kh, cb, ks);
-            if (decltype(clean_)::value) vf = cleaned(vf);
-            o[cb] = mfma(vf, p, o[cb]);
+            for (int i = 0; i < 16; ++i) z[i] = 8 * (i / 4) + i % 4 < left ? z[i] : -kInf;
+            return z;
+          };
+          x = masked();
+          float part = probabilities(x);
+          const bool move = !(part <= kMaxPart) || ref == -kInf;
+          if (__any(move)) {
+            x = masked();
+            part = again(x, move);
           }
+          sum += part;
+          p[0] = pack8(x, 0);
+          p[1] = pack8(x, 1);
+          if (clean_up) product(tile + kTileBytes, kh, p, std::true_type{});
+          else product(tile + kTileBytes, kh, p, std::false_type{});
         }
-    };
-    if (clean_up) product(std::true_type{});
-    else product(std::false_type{});
-  });
+      });
+  if constexpr (SPLIT > 1) {
+    Share* shares = reinterpret_cast<Share*>(lds);
+    static_assert(sizeof(Share) * ROWS * (SPLIT - 1) <= sizeof(lds));
+    __shared__ float joint[2][kWaves][64];
+    __shared__ int left[kWaves];
+    __syncthreads();  // (the tiles' last use)
+    if (split > 0) {
+      shares[wave - ROWS].put(o, lane);
+      joint[0][wave][lane] = ref;
+      joint[1][wave][lane] = sum;
+      if (lane == 0) left[wave] = left_out;
+    }
+    __syncthreads();
+    if (split > 0) return;
+    for (int w = wave + ROWS; w < kWaves; w += ROWS) {
+      const float other = joint[0][w][lane], top = fmaxf(ref, other), off = top == -kInf ? 0.0f : top;
+      const float f = exp2_(ref - off), g = exp2_(other - off);
+      ref = top;
+      sum = sum * f + joint[1][w][lane] * g;
+      shares[w - ROWS].add_to(o, lane, f, g);
+      left_out |= left[w] != 0;
+    }
+  }
   if (left_out)
     add_not_finite(a.v.p + b.kv * a.v.sh + b.s.k0 * a.v.st, a.v.st, b.wave_least / 64 * 64, b.wave_most, lane, [&](int r) { return r < b.seen; }, o);
   const float total = half_sum(sum);
   if (b.row >= b.s.nq) return;
+  if (a.parts > 1) {
+    const int64_t rows = (int64_t)a.heads * a.rows_q, row = (int64_t)b.head * a.rows_q + b.s.q0 + b.row;
+    write_part(a.part, b.part, row, rows, o, h);
+    if (h == 0) *reinterpret_cast<f32x2*>(a.part_sums + 2 * (b.part * rows + row)) = f32x2{ref, total};
+    return;
+  }
   const bool empty = b.seen == 0;
   write_columns(const_cast<uint16_t*>(b.at(a.out, 0)), o, empty ? 0.0f : 1.0f / total, h);
   if (h == 0) a.lse[(int64_t)b.head * a.rows_q + b.s.q0 + b.row] = empty ? -kInf : ((ref == -kInf ? 0.0f : ref) + log2f(total)) * kLn2;
 }
 
-template <int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void seq_grad_q_kernel(SeqArgs a, int blocks) {
-  __shared__ __align__(16) char lds[2][2][kTileBytes];
-  __shared__ int dirty[2];
+template <int ROWS, int SPLIT>
+__global__ __launch_bounds__(64 * ROWS * SPLIT, 2) void seq_grad_q_kernel(SeqArgs a, int blocks) {
+  constexpr int kWaves = ROWS * SPLIT;
+  __shared__ __align__(16) Buffers<SPLIT> lds;
+  __shared__ int dirty[3][SPLIT];
   const int lane = threadIdx.x % 64, h = lane / 32;
-  const QueryBlock b = QueryBlock::of<WAVES>(a, blocks, __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), split = wave / ROWS;
+  const QueryBlock b = QueryBlock::of<ROWS>(a, blocks, wave % ROWS, lane);
   if (!b.any) return;
-  bf16x8 qf[4], df[4];
+  u32x4 qf[4], df[4];
   float dot = 0.0f;
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    qf[c] = *reinterpret_cast<const bf16x8*>(b.at(a.q, lane) + 16 * c);
-    df[c] = *reinterpret_cast<const bf16x8*>(b.at(a.dout, lane) + 16 * c);
-    const bf16x8 of = *reinterpret_cast<const bf16x8*>(b.at(a.out, lane) + 16 * c);
+    qf[c] = *reinterpret_cast<const u32x4*>(b.at(a.q, lane) + 16 * c);
+    df[c] = *reinterpret_cast<const u32x4*>(b.at(a.dout, lane) + 16 * c);
+    const u32x4 of = *reinterpret_cast<const u32x4*>(b.at(a.out, lane) + 16 * c);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dot += (float)df[c][e] * (float)of[e];
+    for (int e = 0; e < 4; ++e) {
+      dot += __uint_as_float(df[c][e] << 16) * __uint_as_float(of[e] << 16);
+      dot += __uint_as_float(df[c][e] & 0xffff0000u) * __uint_as_float(of[e] & 0xffff0000u);
+    }
   }
   const float delta = half_sum(dot);
   const int64_t at = (int64_t)b.head * a.rows_q + b.s.q0 + min(b.row, b.s.nq - 1);
   const float lse2 = a.lse[at] * kLog2e;
-  if (h == 0 && b.row < b.s.nq) a.delta[at] = delta;
-  const Reader rd(lane);
+  if (h == 0 && split == 0 && b.part == 0 && b.row < b.s.nq) a.delta[at] = delta;
+  const Reader rd(lds[0][split][0], lane);
   const float c2 = a.scale * kLog2e;
   f32x16 g[2] = {};
   bool left_out = false;
 
-  over_keys<WAVES, 0>(a, b, lds, dirty, [&](int t, const char* kt, const char* vt, auto masked_, bool clean_up) {
-    constexpr bool kMasked = decltype(masked_)::value;
-    if (kMasked) left_out |= clean_up;
+  f32x16 x, y;    // logits and dout v^T - delta of the half whose turn it is
+  u32x4 ds[2];    // of the one before
+  const f32x16 less_delta = f32x16{} - delta;  // dout v^T - delta: the product begins with it
+  auto logits = [&](int tile, int kh, f32x16& u, f32x16& w) {
+    u = f32x16{};
+    w = less_delta;
 #pragma unroll
-    for (int kh = 0; kh < 2; ++kh) {
-      f32x16 x = {}, y = {};
+    for (int c = 0; c < 4; ++c) u = mfma(rd.along(tile, kh, c), qf[c], u);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) x = mfma(rd.along(kt, kh, c), qf[c], x);
+    for (int c = 0; c < 4; ++c) w = mfma(rd.along(tile + kTileBytes, kh, c), df[c], w);
+  };
+  auto product = [&](int kt, int kh, auto clean_) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) y = mfma(rd.along(vt, kh, c), df[c], y);
-      const int left = b.seen - (64 * t + 32 * kh + 4 * h);
+    for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float p = exp2_(x[i] * c2 - lse2);
-        x[i] = p * (y[i] - delta);
-        if (kMasked) x[i] = 8 * (i / 4) + i % 4 < left ? x[i] : 0.0f;
+      for (int cb = 0; cb < 2; ++cb) {
+        u32x4 kf = rd.across(kt, kh, cb, ks);
+        if (decltype(clean_)::value) kf = cleaned(kf);
+        g[cb] = mfma(kf, ds[ks], g[cb]);
       }
-      auto product = [&](auto clean_) {
+  };
+  u32x4 early[4];  // operands read a stretch ahead: keys of a second half along rows, then of a first half across them
+  uint32_t packed[8];
+  auto share = [&](int i) {  // the i-th of 12 shares of the arithmetic on 16 pairs
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          const bf16x8 ds = pack8(x, ks);
-#pragma unroll
-          for (int cb = 0; cb < 2; ++cb) {
-            bf16x8 kf = rd.across(kt, kh, cb, ks);
-            if (decltype(clean_)::value) kf = cleaned(kf);
-            g[cb] = mfma(kf, ds, g[cb]);
-          }
-        }
-      };
-      if (clean_up) product(std::true_type{});
-      else product(std::false_type{});
+    for (int e = 16 * i / 12; e < 16 * (i + 1) / 12; ++e) {
+      x[e] = exp2_(x[e] * c2 - lse2) * y[e];
+      if (e % 2) packed[e / 2] = pack2(x[e - 1], x[e]);
     }
-  });
+  };
+  auto packed_to_ds = [&]() {
+    ds[0] = (u32x4{packed[0], packed[1], packed[2], packed[3]});
+    ds[1] = (u32x4{packed[4], packed[5], packed[6], packed[7]});
+  };
+  over_keys<kWaves, SPLIT, 0>(
+      a, b, split, lds, dirty,
+      [&](int tile) {
+        logits(tile, 0, x, y);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) early[c] = rd.along(tile, 1, c);
+      },
+      [&](int tile, int before, auto any_) {
+        constexpr bool kAny = decltype(any_)::value;
+        f32x16 u = {}, w = less_delta;
+        u32x4 f[4], e[4];
+        in_order<12>(
+            [&](int i) {
+              if (i < 4) u = mfma(early[i], qf[i], u);
+              else if (i < 8) w = mfma(f[i - 4], df[i - 4], w);
+              else if (kAny) g[i % 2] = mfma(e[i - 8], ds[i / 2 - 4], g[i % 2]);
+            },
+            [&](int i) {
+              if (i < 2) {
+                f[2 * i] = rd.along(tile + kTileBytes, 1, 2 * i);
+                f[2 * i + 1] = rd.along(tile + kTileBytes, 1, 2 * i + 1);
+              } else if (i < 6) {
+                if (kAny) e[i - 2] = rd.across(before, 1, i % 2, i / 2 - 1);
+              } else if (i < 10) {
+                early[i - 6] = rd.across(tile, 0, i % 2, i / 2 - 3);
+              }
+            },
+            share);
+        packed_to_ds();
+        x = u;
+        y = w;
+      },
+      [&](int tile, int next, auto more_) {
+        constexpr bool kMore = decltype(more_)::value;
+        f32x16 u = {}, w = less_delta;
+        u32x4 f[4], e[4];
+        in_order<12>(
+            [&](int i) {
+              if (i < 4) g[i % 2] = mfma(early[i], ds[i / 2], g[i % 2]);
+              else if (kMore && i < 8) u = mfma(f[i - 4], qf[i - 4], u);
+              else if (kMore) w = mfma(e[i - 8], df[i - 8], w);
+            },
+            [&](int i) {
+              if (!kMore) return;
+              if (i < 2) {
+                f[2 * i] = rd.along(next, 0, 2 * i);
+                f[2 * i + 1] = rd.along(next, 0, 2 * i + 1);
+              } else if (i < 4) {
+                e[2 * i - 4] = rd.along(next + kTileBytes, 0, 2 * i - 4);
+                e[2 * i - 3] = rd.along(next + kTileBytes, 0, 2 * i - 3);
+              } else if (i >= 6 && i < 10) {
+                early[i - 6] = rd.along(next, 1, i - 6);
+              }
+            },
+            share);
+        packed_to_ds();
+        if (kMore) {
+          x = u;
+          y = w;
+        }
+      },
+      [&](int tile) { product(tile, 1, std::false_type{}); },
+      [&](int t, int tile, bool clean_up) {
+        left_out |= clean_up;
+#pragma unroll
+        for (int kh = 0; kh < 2; ++kh) {
+          logits(tile, kh, x, y);
+          const int left = b.seen - (64 * t + 32 * kh + 4 * h);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            x[i] = exp2_(x[i] * c2 - lse2) * y[i];
+            x[i] = 8 * (i / 4) + i % 4 < left ? x[i] : 0.0f;
+          }
+          ds[0] = pack8(x, 0);
+          ds[1] = pack8(x, 1);
+          if (clean_up) product(tile, kh, std::true_type{});
+          else product(tile, kh, std::false_type{});
+        }
+      });
+  if constexpr (SPLIT > 1) {
+    Share* shares = reinterpret_cast<Share*>(lds);
+    static_assert(sizeof(Share) * ROWS * (SPLIT - 1) <= sizeof(lds));
+    __shared__ int left[kWaves];
+    __syncthreads();  // (the tiles' last use)
+    if (split > 0) {
+      shares[wave - ROWS].put(g, lane);
+      if (lane == 0) left[wave] = left_out;
+    }
+    __syncthreads();
+    if (split > 0) return;
+    for (int w = wave + ROWS; w < kWaves; w += ROWS) {
+      shares[w - ROWS].add_to(g, lane, 1.0f, 1.0f);
+      left_out |= left[w] != 0;
+    }
+  }
   if (left_out)
     add_not_finite(a.k.p + b.kv * a.k.sh + b.s.k0 * a.k.st, a.k.st, b.wave_least / 64 * 64, b.wave_most, lane, [&](int r) { return r < b.seen; }, g);
-  if (b.row < b.s.nq) write_columns(const_cast<uint16_t*>(b.at(a.dq, 0)), g, a.scale, h);
+  if (b.row >= b.s.nq) return;
+  if (a.parts > 1) write_part(a.part, b.part, (int64_t)b.head * a.rows_q + b.s.q0 + b.row, (int64_t)a.heads * a.rows_q, g, h);
+  else write_columns(const_cast<uint16_t*>(b.at(a.dq, 0)), g, a.scale, h);
 }
 
 // ---- gradients of the keys and values -------------------------------------------------------------------------------
 
-// A workgroup: WAVES x 32 keys of one key head of one sequence, over the queries of all heads that share it.
-template <int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void seq_grad_kv_kernel(SeqArgs a, int blocks) {
-  constexpr int kThreads = 64 * WAVES;
-  __shared__ __align__(16) char lds[2][2][kTileBytes];  // [buffer][queries, dout]
-  __shared__ __align__(16) float stats[2][2][64];       // [buffer][lse in powers of two, delta]
-  __shared__ int dirty[2];
+// A workgroup: KEYS x 32 keys of one key head of one sequence, every 32 of them worked on by SPLIT waves, over the queries of all
+// heads that share it: the tiles that the mask cuts first, those of all heads, then the others.
+template <int KEYS, int SPLIT>
+__global__ __launch_bounds__(64 * KEYS * SPLIT, 2) void seq_grad_kv_kernel(SeqArgs a, int blocks) {
+  constexpr int kWaves = KEYS * SPLIT;
+  __shared__ __align__(16) Buffers<SPLIT> lds;              // queries and dout
+  __shared__ __align__(16) float stats[3][SPLIT][2][64];    // [buffer][tile][-lse / scale, -delta]: where the products begin
+  __shared__ int dirty[3][SPLIT];
   const int lane = threadIdx.x % 64, h = lane / 32;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int id = dealt(blockIdx.x, gridDim.x);
-  const int unit = id / blocks, block = id % blocks;
-  const int kv = unit / a.sequences;
-  const Sequence s = sequence_of(a, unit % a.sequences);
-  const int key0 = block * 32 * WAVES;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), split = wave / KEYS;
+  const Dealt d = dealt(a, a.kv_heads * a.sequences, blocks * a.parts);
+  const int kv = d.unit / a.sequences, part = d.block % a.parts;
+  const Sequence s = sequence_of(a, d.unit % a.sequences);
+  const int key0 = d.block / a.parts * 32 * KEYS;
   if (key0 >= s.nk) return;
   const int rep = a.heads / a.kv_heads;
   // (columns behind the last key are copies of it that nobody writes)
-  const int key = key0 + wave * 32 + lane % 32;
-  bf16x8 kf[4], vf[4];
+  const int end = s.nk - 1, key = key0 + wave % KEYS * 32 + lane % 32;
+  u32x4 kf[4], vf[4];
   {
-    const int i = min(key, s.nk - 1);
-    const uint16_t* k = a.k.p + kv * a.k.sh + (int64_t)(s.k0 + i) * a.k.st + 8 * h;
-    const uint16_t* v = a.v.p + kv * a.v.sh + (int64_t)(s.k0 + i) * a.v.st + 8 * h;
+    const uint16_t* k = a.k.p + kv * a.k.sh + (int64_t)(s.k0 + min(key, end)) * a.k.st + 8 * h;
+    const uint16_t* v = a.v.p + kv * a.v.sh + (int64_t)(s.k0 + min(key, end)) * a.v.st + 8 * h;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      kf[c] = *reinterpret_cast<const bf16x8*>(k + 16 * c);
-      vf[c] = *reinterpret_cast<const bf16x8*>(v + 16 * c);
+      kf[c] = *reinterpret_cast<const u32x4*>(k + 16 * c);
+      vf[c] = *reinterpret_cast<const u32x4*>(v + 16 * c);
     }
   }
-  const int from = first_query(a, s, min(key, s.nk - 1));  // queries that see the lane's key begin here
-  const int wave_key = min(key0 + wave * 32, s.nk - 1);
-  const int wave_from = first_query(a, s, wave_key), wave_all = first_query(a, s, min(wave_key + 31, s.nk - 1));
-  const int wg_from = first_query(a, s, key0), wg_all = first_query(a, s, min(key0 + 32 * WAVES - 1, s.nk - 1));
-  const int first_tile = wg_from / 64, tiles = max(0, (s.nq + 63) / 64 - first_tile);
-  const int steps = tiles * rep;
+  const int from = first_query(a, s, min(key, end));  // queries that see the lane's key begin here
+  const int wave_from = first_query(a, s, min(key0 + wave % KEYS * 32, end));
+  const int wg_from = first_query(a, s, key0), wg_all = first_query(a, s, min(key0 + 32 * KEYS - 1, end));
+  const int first_tile = min(wg_from, s.nq) / 64, all_tile = min((wg_all + 63) / 64, (s.nq + 63) / 64), end_tile = (s.nq + 63) / 64;
+  const int cut = max(0, all_tile - first_tile), uncut = max(0, end_tile - max(all_tile, first_tile));  // tiles of a head
+  const int step = SPLIT * a.parts, own = SPLIT * part;  // this workgroup's of either kind: step n + own + 0 .. SPLIT - 1
+  const int lead = max(0, cut * rep - own + step - 1) / step, steps = lead + max(0, uncut * rep - own + step - 1) / step;
+  struct Place {
+    int head, row;  // row 0 of the tile; behind the last query where there is none
+  };
+  auto place = [&](int n, int j) {
+    const bool lead_part = n < lead;
+    const int at = step * (lead_part ? n : n - lead) + own + j, per_head = max(1, lead_part ? cut : uncut), i = at / per_head;
+    return Place{kv * rep + min(i, rep - 1), i < rep ? 64 * ((lead_part ? first_tile : max(all_tile, first_tile)) + at % per_head) : s.nq};
+  };
 
-  const Reader rd(lane);
-  const float c2 = a.scale * kLog2e;
+  const Reader rd(lds[0][split][0], lane);
+  const float c2 = a.scale * kLog2e, per_scale = -1.0f / a.scale;
   f32x16 dk[2] = {}, dv[2] = {};
-  bool left_out = false;  // some of them are to be added
-  if (threadIdx.x < 2) dirty[threadIdx.x] = 0;
-  Stage<kThreads> sq, sd;
+  bool left_out = false;
+  Stage<64 * kWaves, SPLIT> sq, sd;
   float st_l = 0.0f, st_d = 0.0f;
-  auto fetch = [&](int n) {
-    const int head = kv * rep + n / tiles, row = 64 * (first_tile + n % tiles);
-    sq.load(a.q.p + head * a.q.sh + s.q0 * a.q.st, a.q.st, row, s.nq);
-    sd.load(a.dout.p + head * a.dout.sh + s.q0 * a.dout.st, a.dout.st, row, s.nq);
-    if (threadIdx.x < 64) {
-      const int i = row + threadIdx.x;
-      const int64_t at = (int64_t)head * a.rows_q + s.q0 + i;
-      st_l = i < s.nq ? a.lse[at] * kLog2e : kInf;  // (rows behind the last query have no probability at all)
-      st_d = i < s.nq ? a.delta[at] : 0.0f;
+  if (threadIdx.x < 3 * SPLIT) (&dirty[0][0])[threadIdx.x] = 0;
+  __syncthreads();
+
+  f32x16 x, y;         // logits less lse (in units of the scale) and dout v^T - delta of the half whose turn it is
+  u32x4 p[2], ds[2];   // of the one before
+  u32x4 early[4];      // operands read a stretch ahead
+  const uint32_t begins = (uint32_t)(size_t)(lds_char*)(const char*)stats[0][split][0] + 16 * h;
+  constexpr int kStats = SPLIT * 2 * 64 * 4, kStep = SPLIT * 2 * kTileBytes;  // of a buffer
+  auto quarter = [&](f32x16& z, int tile, int which, int half, int i) {  // rows 8 i + 4 h .. of where a product begins
+    const f32x4 v = *(lds_f32x4*)(begins + tile / kStep * kStats + which * 256 + half * 128 + i * 32);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) z[4 * i + j] = v[j];
+  };
+  uint32_t packed[2][8];
+  auto share = [&](int e) {  // the arithmetic on the e-th pair
+    x[e] = exp2_(x[e] * c2);
+    y[e] *= x[e];
+    if (e % 2) {
+      packed[0][e / 2] = pack2(x[e - 1], x[e]);
+      packed[1][e / 2] = pack2(y[e - 1], y[e]);
     }
   };
-  auto put = [&](int n) {
-    sq.store(lds[n & 1][0]);
-    sd.store(lds[n & 1][1]);
-    if (threadIdx.x < 64) {
-      stats[n & 1][0][threadIdx.x] = st_l;
-      stats[n & 1][1][threadIdx.x] = st_d;
+  auto packed_to_operands = [&]() {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      p[i] = u32x4{packed[0][4 * i], packed[0][4 * i + 1], packed[0][4 * i + 2], packed[0][4 * i + 3]};
+      ds[i] = u32x4{packed[1][4 * i], packed[1][4 * i + 1], packed[1][4 * i + 2], packed[1][4 * i + 3]};
     }
-    if (64 * (first_tile + n % tiles) < wg_all && __any(sq.any_not_finite() || sd.any_not_finite())) dirty[n & 1] = n + 1;
   };
-  auto tile = [&](int n, int row, auto masked_) {
-    constexpr bool kMasked = decltype(masked_)::value;
-    const char* qt = lds[n & 1][0];
-    const char* dt = lds[n & 1][1];
-    const bool clean_up = kMasked && dirty[n & 1] == n + 1;
-    if (kMasked) left_out |= clean_up;
+  // The i-th of 8 first products of a half (4 of the logits, 4 of dout v^T) and of 8 second ones, and their operands.
+  auto first_operand = [&](int tile, int half, int i) { return rd.along(tile + (i < 4 ? 0 : kTileBytes), half, i % 4); };
+  auto second_operand = [&](int tile, int half, int i) { return rd.across(tile + (i % 2 ? 0 : kTileBytes), half, i / 2 % 2, i / 4); };
+  auto first_product = [&](int i, u32x4 f, f32x16& u, f32x16& w) {
+    if (i < 4) u = mfma(f, kf[i], u);
+    else w = mfma(f, vf[i - 4], w);
+  };
+  auto second_product = [&](int i, u32x4 f) {
+    if (i % 2 == 0) dv[i / 2 % 2] = mfma(f, p[i / 4], dv[i / 2 % 2]);
+    else dk[i / 2 % 2] = mfma(f, ds[i / 4], dk[i / 2 % 2]);
+  };
+  auto begin = [&](f32x16& z, int tile, int which, int half) {
 #pragma unroll
-    for (int qh = 0; qh < 2; ++qh) {
-      f32x16 x = {}, y = {};
+    for (int i = 0; i < 4; ++i) quarter(z, tile, which, half, i);
+  };
+  f32x16 u, w;  // of the next half
+
+  over_tiles<SPLIT>(
+      steps, lead, max(0, uncut * rep - (own + split) + step - 1) / step,
+      [&](int n) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) x = mfma(rd.along(qt, qh, c), kf[c], x);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) y = mfma(rd.along(dt, qh, c), vf[c], y);
-      const int least = from - (row + 32 * qh + 4 * h), most = s.nq - (row + 32 * qh + 4 * h);
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const f32x4 l = *reinterpret_cast<const f32x4*>(&stats[n & 1][0][32 * qh + 8 * b + 4 * h]);
-        const f32x4 d = *reinterpret_cast<const f32x4*>(&stats[n & 1][1][32 * qh + 8 * b + 4 * h]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int i = 4 * b + j;
-          float p = exp2_(x[i] * c2 - l[j]);
-          float ds = p * (y[i] - d[j]);
-          if (kMasked) {
-            const bool sees = 8 * b + j >= least && 8 * b + j < most;
-            p = sees ? p : 0.0f;
-            ds = sees ? ds : 0.0f;
-          }
-          x[i] = p;
-          y[i] = ds;
+        for (int i = 0; i < sq.kPieces; ++i) {
+          const Place at = place(n, i * kWaves / 8);
+          const int row = at.row + (i * 8 * kWaves + (int)threadIdx.x / 8) % 64;
+          sq.load_piece(i, a.q.p + at.head * a.q.sh + s.q0 * a.q.st, a.q.st, row, s.nq);
+          sd.load_piece(i, a.dout.p + at.head * a.dout.sh + s.q0 * a.dout.st, a.dout.st, row, s.nq);
         }
-      }
-      auto product = [&](auto clean_) {
+        if (threadIdx.x < 64 * SPLIT) {
+          const Place at = place(n, wave);
+          const int i = at.row + lane;
+          const int64_t in = (int64_t)at.head * a.rows_q + s.q0 + i;
+          st_l = i < s.nq ? a.lse[in] * per_scale : -kInf;  // (rows behind the last query have no probability at all)
+          st_d = i < s.nq ? -a.delta[in] : 0.0f;
+        }
+      },
+      [&](int n, int buf) {
+        sq.store(lds[buf][0][0]);
+        sd.store(lds[buf][0][1]);
+        if (threadIdx.x < 64 * SPLIT) {
+          stats[buf][wave][0][lane] = st_l;
+          stats[buf][wave][1][lane] = st_d;
+        }
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          const bf16x8 p = pack8(x, ks), ds = pack8(y, ks);
+        for (int j = 0; j < SPLIT; ++j)
+          if (n < lead && __any(sq.any_not_finite(j) || sd.any_not_finite(j))) dirty[buf][j] = n + 1;
+      },
+      [&](int tile) {
+        begin(x, tile, 0, 0);
+        begin(y, tile, 1, 0);
 #pragma unroll
-          for (int cb = 0; cb < 2; ++cb) {
-            bf16x8 df = rd.across(dt, qh, cb, ks), qf = rd.across(qt, qh, cb, ks);
-            if (decltype(clean_)::value) {
-              df = cleaned(df);
-              qf = cleaned(qf);
+        for (int i = 0; i < 8; ++i) first_product(i, first_operand(tile, 0, i), x, y);
+        begin(u, tile, 0, 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) early[i] = first_operand(tile, 1, i);
+      },
+      [&](int tile, int before, auto any_) {
+        constexpr bool kAny = decltype(any_)::value;
+        u32x4 f[16];
+        in_order<16>(
+            [&](int i) {
+              const u32x4 v = i < 4 ? early[i] : f[i];
+              if (i < 8) first_product(i, v, u, w);
+              else if (kAny) second_product(i - 8, v);
+            },
+            [&](int i) {
+              if (i < 2) {
+                quarter(w, tile, 1, 1, 2 * i);
+                quarter(w, tile, 1, 1, 2 * i + 1);
+              }
+              if (i < 4) f[i + 4] = first_operand(tile, 1, i + 4);
+              else if (i < 12 && kAny) f[i + 4] = second_operand(before, 1, i - 4);
+              else if (i >= 12) early[i - 12] = second_operand(tile, 0, i - 12);
+            },
+            share);
+        packed_to_operands();
+        x = u;
+        y = w;
+      },
+      [&](int tile, int next, auto more_) {
+        constexpr bool kMore = decltype(more_)::value;
+        u32x4 f[16];
+        in_order<16>(
+            [&](int i) {
+              const u32x4 v = i < 4 ? early[i] : f[i];
+              if (i < 8) second_product(i, v);
+              else if (kMore) first_product(i - 8, v, u, w);
+            },
+            [&](int i) {
+              if (i < 4) f[i + 4] = second_operand(tile, 0, i + 4);
+              else if (i < 12 && kMore) f[i + 4] = first_operand(next, 0, i - 4);
+              else if (kMore && i >= 12) early[i - 12] = first_operand(next, 1, i - 12);
+              if (kMore && i >= 2 && i < 6) {
+                quarter(u, next, 0, 0, i - 2);
+                quarter(w, next, 1, 0, i - 2);
+              }
+            },
+            share);
+        packed_to_operands();
+        if (kMore) {
+          x = u;
+          y = w;
+          begin(u, next, 0, 1);
+        }
+      },
+      [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) second_product(i, second_operand(tile, 1, i));
+      },
+      [&](int n, int tile, int buf) {
+        const int row = place(n, split).row;
+        if (row >= s.nq || row + 64 <= wave_from) return;
+        const bool clean_up = dirty[buf][split] == n + 1;
+        left_out |= clean_up;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          begin(x, tile, 0, half);
+          begin(y, tile, 1, half);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) first_product(i, first_operand(tile, half, i), x, y);
+          const int least = from - (row + 32 * half + 4 * h), most = s.nq - (row + 32 * half + 4 * h);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const bool sees = 8 * (e / 4) + e % 4 >= least && 8 * (e / 4) + e % 4 < most;
+            x[e] = exp2_(x[e] * c2);
+            y[e] = sees ? x[e] * y[e] : 0.0f;
+            x[e] = sees ? x[e] : 0.0f;
+            if (e % 2) {
+              packed[0][e / 2] = pack2(x[e - 1], x[e]);
+              packed[1][e / 2] = pack2(y[e - 1], y[e]);
             }
-            dv[cb] = mfma(df, p, dv[cb]);
-            dk[cb] = mfma(qf, ds, dk[cb]);
+          }
+          packed_to_operands();
+          if (clean_up) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) second_product(i, cleaned(second_operand(tile, half, i)));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) second_product(i, second_operand(tile, half, i));
           }
         }
-      };
-      if (clean_up) product(std::true_type{});
-      else product(std::false_type{});
+      });
+  if constexpr (SPLIT > 1) {
+    Share* shares = reinterpret_cast<Share*>(lds);  // [wave of a later split][dk, dv]
+    static_assert(sizeof(Share) * 2 * KEYS * (SPLIT - 1) <= sizeof(lds));
+    __shared__ int left[kWaves];
+    __syncthreads();  // (the tiles' last use)
+    if (split > 0) {
+      shares[2 * (wave - KEYS)].put(dk, lane);
+      shares[2 * (wave - KEYS) + 1].put(dv, lane);
+      if (lane == 0) left[wave] = left_out;
     }
-  };
-  if (steps > 0) {
     __syncthreads();
-    fetch(0);
-    put(0);
-    __syncthreads();
-    for (int n = 0; n < steps; ++n) {
-      if (n + 1 < steps) fetch(n + 1);
-      const int row = 64 * (first_tile + n % tiles);
-      if (row >= wave_all) tile(n, row, std::false_type{});
-      else if (row + 64 > wave_from) tile(n, row, std::true_type{});
-      if (n + 1 < steps) put(n + 1);
-      __syncthreads();
+    if (split > 0) return;
+    for (int other = wave + KEYS; other < kWaves; other += KEYS) {
+      shares[2 * (other - KEYS)].add_to(dk, lane, 1.0f, 1.0f);
+      shares[2 * (other - KEYS) + 1].add_to(dv, lane, 1.0f, 1.0f);
+      left_out |= left[other] != 0;
     }
   }
   if (left_out) {
-    const int to = min(s.nq, (wave_all + 63) / 64 * 64);
     for (int head = kv * rep; head < (kv + 1) * rep; ++head) {
-      add_not_finite(a.dout.p + head * a.dout.sh + s.q0 * a.dout.st, a.dout.st, wave_from / 64 * 64, to, lane, [&](int r) { return r >= from; }, dv);
-      add_not_finite(a.q.p + head * a.q.sh + s.q0 * a.q.st, a.q.st, wave_from / 64 * 64, to, lane, [&](int r) { return r >= from; }, dk);
+      auto sees = [&](int r) { return r >= from; };
+      const int to = min(s.nq, 64 * all_tile);
+      add_not_finite(a.dout.p + head * a.dout.sh + s.q0 * a.dout.st, a.dout.st, wave_from / 64 * 64, to, lane, sees, dv);
+      add_not_finite(a.q.p + head * a.q.sh + s.q0 * a.q.st, a.q.st, wave_from / 64 * 64, to, lane, sees, dk);
     }
   }
   if (key >= s.nk) return;
+  if (a.parts > 1) {  // (dk, then dv)
+    const int64_t rows = (int64_t)a.kv_heads * a.rows_k, row = (int64_t)kv * a.rows_k + s.k0 + key;
+    write_part(a.part, part, row, rows, dk, h);
+    write_part(a.part, a.parts + part, row, rows, dv, h);
+    return;
+  }
   write_columns(const_cast<uint16_t*>(a.dk.p) + kv * a.dk.sh + (int64_t)(s.k0 + key) * a.dk.st, dk, a.scale, h);
   write_columns(const_cast<uint16_t*>(a.dv.p) + kv * a.dv.sh + (int64_t)(s.k0 + key) * a.dv.st, dv, 1.0f, h);
+}
+
+// ---- joining the parts of small launches ------------------------------------------------------------------------------
+
+constexpr int kJoinRows = 32;  // rows of a workgroup; 8 lanes a row
+
+// out and lse from the parts' accumulators, references and sums
+__global__ __launch_bounds__(256) void join_out_kernel(SeqArgs a, int blocks) {
+  const int unit = blockIdx.x / blocks, head = unit / a.sequences;
+  const Sequence s = sequence_of(a, unit % a.sequences);
+  const int i = blockIdx.x % blocks * kJoinRows + threadIdx.x / 8, c = 8 * (threadIdx.x % 8);
+  if (i >= s.nq) return;
+  const int64_t rows = (int64_t)a.heads * a.rows_q, row = (int64_t)head * a.rows_q + s.q0 + i;
+  float x[8] = {}, ref = -kInf, sum = 0.0f;
+  for (int p = 0; p < a.parts; ++p) {
+    const f32x2 st = *reinterpret_cast<const f32x2*>(a.part_sums + 2 * (p * rows + row));
+    const f32x4 lo = *reinterpret_cast<const f32x4*>(a.part + (p * rows + row) * kD + c), hi = *reinterpret_cast<const f32x4*>(a.part + (p * rows + row) * kD + c + 4);
+    const float top = fmaxf(ref, st[0]), off = top == -kInf ? 0.0f : top, f = exp2_(ref - off), g = exp2_(st[0] - off);
+    ref = top;
+    sum = sum * f + st[1] * g;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = x[j] * f + (j < 4 ? lo[j % 4] : hi[j % 4]) * g;
+  }
+  const bool empty = keys_seen(a, s, i) == 0;
+  const float r = empty ? 0.0f : 1.0f / sum;
+  u32x4 w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = pack2(x[2 * j] * r, x[2 * j + 1] * r);
+  *reinterpret_cast<u32x4*>(const_cast<uint16_t*>(a.out.p) + head * a.out.sh + (int64_t)(s.q0 + i) * a.out.st + c) = w;
+  if (c == 0) a.lse[row] = empty ? -kInf : ((ref == -kInf ? 0.0f : ref) + log2f(sum)) * kLn2;
+}
+
+// A gradient from the parts' sums: of the queries (KEYS = false), or of the keys and, behind them, the values.
+template <bool KEYS>
+__global__ __launch_bounds__(256) void join_grad_kernel(SeqArgs a, int blocks) {
+  const int heads = KEYS ? a.kv_heads : a.heads, units = heads * a.sequences;
+  const int which = blockIdx.x / (units * blocks), at = blockIdx.x % (units * blocks);
+  const int unit = at / blocks, head = unit / a.sequences;
+  const Sequence s = sequence_of(a, unit % a.sequences);
+  const int i = at % blocks * kJoinRows + threadIdx.x / 8, c = 8 * (threadIdx.x % 8);
+  if (i >= (KEYS ? s.nk : s.nq)) return;
+  const int64_t in_tensor = (KEYS ? s.k0 : s.q0) + i, all = KEYS ? a.rows_k : a.rows_q, rows = heads * all, row = head * all + in_tensor;
+  float x[8] = {};
+  for (int p = 0; p < a.parts; ++p) {
+    const float* from = a.part + ((which * a.parts + p) * rows + row) * kD + c;
+    const f32x4 lo = *reinterpret_cast<const f32x4*>(from), hi = *reinterpret_cast<const f32x4*>(from + 4);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] += j < 4 ? lo[j % 4] : hi[j % 4];
+  }
+  const float f = which == 0 ? a.scale : 1.0f;
+  u32x4 w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = pack2(x[2 * j] * f, x[2 * j + 1] * f);
+  const SeqRows& t = !KEYS ? a.dq : (which == 0 ? a.dk : a.dv);
+  *reinterpret_cast<u32x4*>(const_cast<uint16_t*>(t.p) + head * t.sh + in_tensor * t.st + c) = w;
 }
 
 long long grid_of(int longest, int rows, int heads, int sequences) { return ((long long)longest + rows - 1) / rows * heads * sequences; }
 
 constexpr long long kMostWorkgroups = (1ll << 32) / 512 - 1;  // threads of a launch are counted in 32 bits
 
-}  // namespace
+// How the blocks of 128 rows of a launch are worked on.  Four waves of 32 rows, two or three such workgroups to a compute unit, if there
+// are blocks enough; else a second wave to every 32 rows, eight waves that fill a compute unit.  us with four and with eight waves,
+// forward, 16 heads: one frame of 1374 tokens (171 blocks) 23.6 and 20.7, 20 heads (214) 23.3 and 20.8, 24 heads (257) 31.3 and 38.8,
+// two frames (343) 33 and 39.  Under a mask blocks differ in length and the second round is shorter: causal, 2000 tokens (250) 32.7 and
+// 28.0, 3000 (375) 44.6 and 37.0.  Where even those leave compute units without work, several workgroups share the tiles of a block and a
+// second launch joins them: 4000 causal tokens of one head 44.9 alone, 29.2 with 2, 20.9 with 4, 18.2 with 8, four single tokens over up to
+// 4000 keys 45.9, 29.2, 21.1, 25.9; more of them than there are compute units gain nothing (one frame: 20.6 alone, 34.0 with 2).
+constexpr int kComputeUnits = 256, kMostParts = 8;
+struct Shape {
+  bool split;
+  int parts;
+};
+Shape shape_of(const SeqArgs& a, long long rows, int heads, long long tiles) {
+  const long long blocks = std::max<long long>(1, rows * heads / 128);
+  Shape s{blocks <= (a.causal ? 400 : kComputeUnits), 1};
+  if (s.split) s.parts = (int)std::max<long long>(1, std::min({(long long)kMostParts, kComputeUnits / blocks, tiles / 4}));
+  return s;
+}
+Shape shape_q(const SeqArgs& a) { return shape_of(a, a.rows_q, a.heads, (a.longest_k + 63) / 64); }
+Shape shape_k(const SeqArgs& a) { return shape_of(a, a.rows_k, a.kv_heads, (long long)((a.longest_q + 63) / 64) * (a.heads / a.kv_heads)); }
 
-bool seq_attend_fits(const SeqArgs& a) {
-  return grid_of(a.longest_q, 128, a.heads, a.sequences) <= kMostWorkgroups && grid_of(a.longest_k, 128, a.kv_heads, a.sequences) <= kMostWorkgroups;
+template <typename K>
+void launch_rows(K kernel, const SeqArgs& a, int longest, int heads, int rows, int threads, hipStream_t stream) {
+  const int blocks = (longest + rows - 1) / rows;
+  kernel<<<(int)(grid_of(longest, rows, heads, a.sequences) * a.parts), threads, 0, stream>>>(a, blocks);
 }
 
-// Eight waves read a tile half as often as two workgroups of four; where blocks of 256 rows would leave compute units
-// without work, the shorter ones.
-hipError_t launch_seq_attend(const SeqArgs& a, hipStream_t stream) {
-  const long long small = grid_of(a.longest_q, 128, a.heads, a.sequences), large = grid_of(a.longest_q, 256, a.heads, a.sequences);
-  if (small == 0) return hipSuccess;
-  if (large >= 256) seq_attend_kernel<8><<<(int)large, 512, 0, stream>>>(a, (a.longest_q + 255) / 256);
-  else seq_attend_kernel<4><<<(int)small, 256, 0, stream>>>(a, (a.longest_q + 127) / 128);
+}  // namespace
+
+// (what shares tiles over parts has few blocks: far below what a launch can have)
+bool seq_attend_fits(const SeqArgs& a) {
+  return grid_of(a.longest_q, kJoinRows, a.heads, a.sequences) <= kMostWorkgroups && 2 * grid_of(a.longest_k, kJoinRows, a.kv_heads, a.sequences) <= kMostWorkgroups;
+}
+
+int64_t seq_attend_workspace(const SeqArgs& a) {
+  const int parts = shape_q(a).parts;
+  return parts > 1 ? (int64_t)parts * a.heads * a.rows_q * (kD + 2) * (int64_t)sizeof(float) : 0;
+}
+int64_t seq_attend_grad_parts(const SeqArgs& a) {
+  const int64_t q = shape_q(a).parts, k = shape_k(a).parts;
+  return std::max(q > 1 ? q * a.heads * a.rows_q : 0, k > 1 ? 2 * k * a.kv_heads * a.rows_k : 0) * kD * (int64_t)sizeof(float);
+}
+
+hipError_t launch_seq_attend(const SeqArgs& args, hipStream_t stream) {
+  SeqArgs a = args;
+  if (grid_of(a.longest_q, 128, a.heads, a.sequences) == 0) return hipSuccess;
+  const Shape s = shape_q(a);
+  a.parts = s.parts;
+  a.part_sums = a.part + (int64_t)s.parts * a.heads * a.rows_q * kD;
+  if (s.split) launch_rows(seq_attend_kernel<4, 2>, a, a.longest_q, a.heads, 128, 512, stream);
+  else launch_rows(seq_attend_kernel<4, 1>, a, a.longest_q, a.heads, 128, 256, stream);
+  if (s.parts > 1) {
+    const int blocks = (a.longest_q + kJoinRows - 1) / kJoinRows;
+    join_out_kernel<<<blocks * a.heads * a.sequences, 256, 0, stream>>>(a, blocks);
+  }
   return hipGetLastError();
 }
 
-hipError_t launch_seq_attend_grad(const SeqArgs& a, hipStream_t stream) {
-  const long long small_q = grid_of(a.longest_q, 128, a.heads, a.sequences), large_q = grid_of(a.longest_q, 256, a.heads, a.sequences);
-  const long long small_k = grid_of(a.longest_k, 128, a.kv_heads, a.sequences), large_k = grid_of(a.longest_k, 256, a.kv_heads, a.sequences);
-  if (small_q > 0) {
-    if (large_q >= 256) seq_grad_q_kernel<8><<<(int)large_q, 512, 0, stream>>>(a, (a.longest_q + 255) / 256);
-    else seq_grad_q_kernel<4><<<(int)small_q, 256, 0, stream>>>(a, (a.longest_q + 127) / 128);
+hipError_t launch_seq_attend_grad(const SeqArgs& args, hipStream_t stream) {
+  SeqArgs a = args;
+  if (grid_of(a.longest_q, 128, a.heads, a.sequences) > 0) {
+    const Shape s = shape_q(a);
+    a.parts = s.parts;
+    if (s.split) launch_rows(seq_grad_q_kernel<4, 2>, a, a.longest_q, a.heads, 128, 512, stream);
+    else launch_rows(seq_grad_q_kernel<4, 1>, a, a.longest_q, a.heads, 128, 256, stream);
+    if (s.parts > 1) {
+      const int blocks = (a.longest_q + kJoinRows - 1) / kJoinRows;
+      join_grad_kernel<false><<<blocks * a.heads * a.sequences, 256, 0, stream>>>(a, blocks);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (small_k > 0) {
-    if (large_k >= 256) seq_grad_kv_kernel<8><<<(int)large_k, 512, 0, stream>>>(a, (a.longest_k + 255) / 256);
-    else seq_grad_kv_kernel<4><<<(int)small_k, 256, 0, stream>>>(a, (a.longest_k + 127) / 128);
+  if (grid_of(a.longest_k, 128, a.kv_heads, a.sequences) > 0) {
+    const Shape s = shape_k(a);
+    a.parts = s.parts;
+    // eight waves read every tile of queries once for 256 keys, unless that pads the sequences more (six frames, 8244 keys: 363 and, in
+    // blocks of 128, 399 us; eight sequences of 1374: 169 and 162)
+    const auto padded = [&](int rows) { return ((long long)a.longest_k + rows - 1) / rows * rows; };
+    if (s.split) launch_rows(seq_grad_kv_kernel<4, 2>, a, a.longest_k, a.kv_heads, 128, 512, stream);
+    else if (20 * padded(128) <= 19 * padded(256)) launch_rows(seq_grad_kv_kernel<4, 1>, a, a.longest_k, a.kv_heads, 128, 256, stream);
+    else launch_rows(seq_grad_kv_kernel<8, 1>, a, a.longest_k, a.kv_heads, 256, 512, stream);
+    if (s.parts > 1) {
+      const int blocks = (a.longest_k + kJoinRows - 1) / kJoinRows;
+      join_grad_kernel<true><<<2 * blocks * a.kv_heads * a.sequences, 256, 0, stream>>>(a, blocks);
+    }
     return hipGetLastError();
   }
   return hipSuccess;

@@ -64,7 +64,7 @@ EXPORTS = (
     "xsv_step", "xsv_step_all_layers", "xsv_set_overlap", "xsv_join", "xsv_cache_len", "xsv_cache_export",
     "xsv_cache_import", "xsv_last_selection", "xsv_quantize_k", "xsv_quantize_v", "xsv_score", "xsv_score_noalloc",
     "xsv_topk_keep", "xsv_strerror", "xsv_norm_rotate", "xsv_norm_rotate_grad", "xsv_norm_rotate_grad_workspace",
-    "xsv_seq_attend", "xsv_seq_attend_grad", "xsv_seq_attend_grad_workspace", "xsv_query_attend",
+    "xsv_seq_attend", "xsv_seq_attend_workspace", "xsv_seq_attend_grad", "xsv_seq_attend_grad_workspace", "xsv_query_attend",
 )
 # every symbol include/xsv_tune.h declares (launch tuning and measurement aids)
 TUNE_EXPORTS = (
@@ -126,7 +126,8 @@ def lib():
         L.xsv_norm_rotate_grad.argtypes = [vp, R, T, T, T, T, T, T, vp, vp, C.c_int64]
         L.xsv_norm_rotate_grad_workspace.argtypes = [R, C.POINTER(C.c_int64)]
         S = C.POINTER(xsv_seq_config)
-        L.xsv_seq_attend.argtypes = [vp, S, T, T, T, T, vp]
+        L.xsv_seq_attend.argtypes = [vp, S, T, T, T, T, vp, vp, C.c_int64]
+        L.xsv_seq_attend_workspace.argtypes = [S, C.POINTER(C.c_int64)]
         L.xsv_seq_attend_grad.argtypes = [vp, S, T, T, T, T, vp, T, T, T, T, vp, C.c_int64]
         L.xsv_seq_attend_grad_workspace.argtypes = [S, C.POINTER(C.c_int64)]
         L.xsv_measure_peaks.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(C.c_float)]
@@ -517,6 +518,13 @@ def _like(out, name, x):
     return out
 
 
+def _workspace(size_of, cfg, device):
+    """A call's workspace, of the size that the library asks for."""
+    nbytes = C.c_int64()
+    _check(size_of(C.byref(cfg), C.byref(nbytes)), size_of.__name__)
+    return torch.empty(nbytes.value, dtype=torch.uint8, device=device)
+
+
 def _rotate_config(q, k, norm, eps, weights, positions, base, interleaved):
     if norm not in NORMS:
         raise ValueError(f"norm must be one of {sorted(NORMS)}")
@@ -568,17 +576,14 @@ def norm_rotate_grad(dq_out, dk_out, q, k=None, *, norm="layer", eps=1e-5, q_wei
     cfg = _rotate_config(q, k, norm, eps, (q_weight, q_bias, k_weight, k_bias), positions, base, interleaved)
     dq, dk = out if out is not None else (None, None)
     sums = work = None
-    nbytes = C.c_int64()
-    if weight_grads:
-        _check(lib().xsv_norm_rotate_grad_workspace(C.byref(cfg), C.byref(nbytes)), "xsv_norm_rotate_grad_workspace")
     with _on(q.device, stream) as s:
         dq = _like(dq, "out[0]", q)
         dk = None if k is None else _like(dk, "out[1]", k)
         if weight_grads:
             sums = torch.empty((4, 64), dtype=torch.float32, device=q.device)
-            work = torch.empty(nbytes.value, dtype=torch.uint8, device=q.device)
+            work = _workspace(lib().xsv_norm_rotate_grad_workspace, cfg, q.device)
         _check(lib().xsv_norm_rotate_grad(s, C.byref(cfg), _operand(q), _operand(k), _operand(dq_out), _operand(None if k is None else dk_out),
-                                          _operand(dq), _operand(dk), _ptr(sums), _ptr(work), nbytes.value), "xsv_norm_rotate_grad")
+                                          _operand(dq), _operand(dk), _ptr(sums), _ptr(work), 0 if work is None else work.numel()), "xsv_norm_rotate_grad")
     return dq, dk, sums
 
 
@@ -614,7 +619,9 @@ def seq_attend(q, k, v, q_begin, k_begin=None, *, longest_q=None, longest_k=None
         if lse is None:
             lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=q.device)
         _plain(lse, "lse", torch.float32, q.shape[:2], q.device)
-        _check(lib().xsv_seq_attend(s, C.byref(cfg), _operand(q), _operand(k), _operand(v), _operand(out), _ptr(lse)), "xsv_seq_attend")
+        work = _workspace(lib().xsv_seq_attend_workspace, cfg, q.device)
+        _check(lib().xsv_seq_attend(s, C.byref(cfg), _operand(q), _operand(k), _operand(v), _operand(out), _ptr(lse), _ptr(work), work.numel()),
+               "xsv_seq_attend")
     return out, lse
 
 
@@ -627,14 +634,12 @@ def seq_attend_grad(dout, q, k, v, out, lse, q_begin, k_begin=None, *, longest_q
     _bf16(out, "out", q.shape)
     _same_device(q.device, dout, out)
     _plain(lse, "lse", torch.float32, q.shape[:2], q.device)
-    nbytes = C.c_int64()
-    _check(lib().xsv_seq_attend_grad_workspace(C.byref(cfg), C.byref(nbytes)), "xsv_seq_attend_grad_workspace")
     dq, dk, dv = grads if grads is not None else (None, None, None)
     with _on(q.device, stream) as s:
         dq, dk, dv = _like_or_zeros(dq, "grads[0]", q), _like_or_zeros(dk, "grads[1]", k), _like_or_zeros(dv, "grads[2]", v)
-        work = torch.empty(nbytes.value, dtype=torch.uint8, device=q.device)
+        work = _workspace(lib().xsv_seq_attend_grad_workspace, cfg, q.device)
         _check(lib().xsv_seq_attend_grad(s, C.byref(cfg), _operand(q), _operand(k), _operand(v), _operand(out), _ptr(lse), _operand(dout),
-                                         _operand(dq), _operand(dk), _operand(dv), _ptr(work), nbytes.value), "xsv_seq_attend_grad")
+                                         _operand(dq), _operand(dk), _operand(dv), _ptr(work), work.numel()), "xsv_seq_attend_grad")
     return dq, dk, dv
 
 

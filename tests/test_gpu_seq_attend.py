@@ -98,7 +98,7 @@ def test_heads_shared_keys_and_scales(heads, kv, scale):
     _check(*x, lq, lk, 1, scale, _run(*x, lq, lk, 1, scale))
 
 
-@pytest.mark.parametrize("causal,n", [(0, 300), (1, 300), (150, 300)])
+@pytest.mark.parametrize("causal,n", [(0, 300), (1, 300), (150, 300), (0, 512), (1, 500)])
 def test_many_sequences_at_once(causal, n):
     """Launches large enough for the larger blocks of rows; the lengths' bounds left to the library."""
     lq = [n] * 31 + [n - 45]
@@ -158,11 +158,11 @@ def test_offsets_outside_the_tensors_are_cut_off():
                 assert torch.equal(a, w)
 
 
+@pytest.mark.parametrize("n,at", [(300, 141), (1300, 700)])    # (the longer: workgroups share the tiles)
 @pytest.mark.parametrize("what", ["nan", "inf", "-inf"])
-def test_values_that_are_not_finite_stay_where_they_are_seen(what):
+def test_values_that_are_not_finite_stay_where_they_are_seen(what, n, at):
     """NaN and infinities in keys, values, queries and dout of a causal sequence, in tiles that the mask cuts: queries in front of
     them, and the gradients of keys behind the last query that sees them, are what they are without them."""
-    n, at = 300, 141
     q, k, v, d = [t.clone() for t in _inputs([n], [n], 2, 2, seed=6)]
     clean = _run(q, k, v, d, [n], [n], 1)
     x = float(what)
@@ -198,9 +198,9 @@ def test_values_that_are_not_finite_stay_where_they_are_seen(what):
         assert torch.equal(a[1, at + 1:], b[1, at + 1:])
 
 
+@pytest.mark.parametrize("n", [400, 1500])
 @pytest.mark.parametrize("kind", ["rise", "fall", "jump", "far-below-zero"])
-def test_logits_that_move_the_softmax_reference(kind):
-    n = 400
+def test_logits_that_move_the_softmax_reference(kind, n):
     q, k, v, d = [t.clone() for t in _inputs([n], [n], 2, 2, seed=7)]
     ramp = torch.linspace(0, 1, n, device=DEV)
     q[..., 0] = 8.0
@@ -246,14 +246,18 @@ def test_strides_broadcast_heads_and_strided_outputs():
     assert torch.equal(dq, want[2][0])
 
 
-def test_the_same_bits_every_time_and_from_any_neighbours():
-    """Twice the same call; and a sequence by itself or among others."""
+def test_the_same_bits_every_time_whatever_the_neighbours_hold():
+    """Twice the same call; and with other values, NaN among them, in the sequences beside one."""
     lq = [257, 100, 31]
     q, k, v, d = _inputs(lq, lq, 6, 2, seed=12)
     a, b = _run(q, k, v, d, lq, lq, 1), _run(q, k, v, d, lq, lq, 1)
-    alone = _run(*[t[:, 257:357] for t in (q, k, v, d)], [100], [100], 1)
-    for x, y, z in zip((*a[:2], *a[2]), (*b[:2], *b[2]), (*alone[:2], *alone[2])):
-        assert torch.equal(x, y) and torch.equal(x[:, 257:357], z)
+    others = [t.clone() for t in (q, k, v, d)]
+    for t in others:
+        t[:, :257] = t[:, :257].flip(1) * 3.0
+        t[:, 357:] = float("nan")
+    c = _run(*others, lq, lq, 1)
+    for x, y, z in zip((*a[:2], *a[2]), (*b[:2], *b[2]), (*c[:2], *c[2])):
+        assert torch.equal(x, y) and torch.equal(x[:, 257:357], z[:, 257:357])
 
 
 def test_gradient_against_differences():

@@ -83,33 +83,39 @@ def _seq(**kw):
 def test_seq_attend_refuses_bad_configurations(lib, bad):
     cfg = _seq(**bad)
     nbytes = C.c_int64()
-    assert lib.xsv_seq_attend(None, C.byref(cfg), T, T, T, T, PTR) == xsv.XSV_ERR_ARG
+    assert lib.xsv_seq_attend(None, C.byref(cfg), T, T, T, T, PTR, PTR, 1 << 20) == xsv.XSV_ERR_ARG
     assert lib.xsv_seq_attend_grad(None, C.byref(cfg), T, T, T, T, PTR, T, T, T, T, PTR, 1 << 20) == xsv.XSV_ERR_ARG
     assert lib.xsv_seq_attend_grad_workspace(C.byref(cfg), C.byref(nbytes)) == xsv.XSV_ERR_ARG
+    assert lib.xsv_seq_attend_workspace(C.byref(cfg), C.byref(nbytes)) == xsv.XSV_ERR_ARG
 
 
 def test_seq_attend_refuses_bad_tensors_workspaces_and_grids(lib):
     cfg = _seq()
     nbytes = C.c_int64()
-    assert lib.xsv_seq_attend(None, None, T, T, T, T, PTR) == xsv.XSV_ERR_ARG
+    assert lib.xsv_seq_attend(None, None, T, T, T, T, PTR, PTR, 1 << 20) == xsv.XSV_ERR_ARG
     assert lib.xsv_seq_attend_grad_workspace(C.byref(cfg), None) == xsv.XSV_ERR_ARG
     assert lib.xsv_seq_attend_grad_workspace(C.byref(cfg), C.byref(nbytes)) == xsv.XSV_OK and nbytes.value >= 4 * 8 * 4
     for bad in BAD_TENSORS:
         for at in range(4):
             ts = [T] * 4
             ts[at] = bad
-            assert lib.xsv_seq_attend(None, C.byref(cfg), *ts, PTR) == xsv.XSV_ERR_ARG
+            assert lib.xsv_seq_attend(None, C.byref(cfg), *ts, PTR, PTR, 1 << 20) == xsv.XSV_ERR_ARG
         for at in range(8):
             ts = [T] * 8
             ts[at] = bad
             assert lib.xsv_seq_attend_grad(None, C.byref(cfg), *ts[:4], PTR, *ts[4:], PTR, nbytes.value) == xsv.XSV_ERR_ARG
     for lse in (None, PTR + 2):
-        assert lib.xsv_seq_attend(None, C.byref(cfg), T, T, T, T, lse) == xsv.XSV_ERR_ARG
+        assert lib.xsv_seq_attend(None, C.byref(cfg), T, T, T, T, lse, PTR, 1 << 20) == xsv.XSV_ERR_ARG
         assert lib.xsv_seq_attend_grad(None, C.byref(cfg), T, T, T, T, lse, T, T, T, T, PTR, nbytes.value) == xsv.XSV_ERR_ARG
     for work, size in ((None, nbytes.value), (PTR + 8, nbytes.value), (PTR, nbytes.value - 1)):
         assert lib.xsv_seq_attend_grad(None, C.byref(cfg), T, T, T, T, PTR, T, T, T, T, work, size) == xsv.XSV_ERR_ARG
+    long = _seq(rows_k=1000, longest_k=1000)      # few queries, many keys: workgroups share the keys
+    assert lib.xsv_seq_attend_workspace(C.byref(long), C.byref(nbytes)) == xsv.XSV_OK and nbytes.value > 0
+    for work, size in ((None, nbytes.value), (PTR + 8, nbytes.value), (PTR, nbytes.value - 1)):
+        assert lib.xsv_seq_attend(None, C.byref(long), T, T, T, T, PTR, work, size) == xsv.XSV_ERR_ARG
+    assert lib.xsv_seq_attend_workspace(C.byref(long), None) == xsv.XSV_ERR_ARG and lib.xsv_seq_attend_workspace(None, C.byref(nbytes)) == xsv.XSV_ERR_ARG
     huge = _seq(heads=1 << 16, kv_heads=1 << 16, rows_q=1 << 20, rows_k=1 << 20, longest_q=1 << 20, longest_k=1 << 20)
-    assert lib.xsv_seq_attend(None, C.byref(huge), T, T, T, T, PTR) == xsv.XSV_ERR_UNSUPPORTED
+    assert lib.xsv_seq_attend(None, C.byref(huge), T, T, T, T, PTR, PTR, 1 << 20) == xsv.XSV_ERR_UNSUPPORTED
 
 
 def test_seq_attend_binding_refuses_what_is_not_a_bf16_device_tensor():
