@@ -14,6 +14,7 @@
 // The tokens are cut over the waves of a workgroup (joined in LDS) and over workgroups, so that few rows still use the whole chip;
 // the workgroup that ends last in a (head, row block) joins their partial results, in their order.
 #include <algorithm>
+#include <type_traits>
 
 #include "xsv_internal.h"
 
@@ -28,10 +29,14 @@ using f32x4 = __attribute__((ext_vector_type(4))) float;
 
 constexpr int kWaves = 4;
 constexpr int kRows = kQueryRows;  // query rows of a column block
+constexpr int kJoinRows = 4;       // rows that are joined at a time, one a wave
+static_assert(kJoinRows == kWaves);
 constexpr float kInf = __builtin_inff();
 constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ float off_of(float ref) { return ref == -kInf ? 0.0f : ref; }  // (nothing finite seen yet)
 
 __device__ __forceinline__ float column_max(float x) {  // over the four lanes of a query
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -69,7 +74,9 @@ struct Run {
   }
   __device__ __forceinline__ void codes(int s, float* x) const {  // 8 s ..
     if constexpr (BITS == 4) {
-      const uint32_t even = w[s] & 0x0f0f0f0fu, odd = (w[s] >> 4) & 0x0f0f0f0fu;
+      uint32_t even = w[s] & 0x0f0f0f0fu, odd = (w[s] >> 4) & 0x0f0f0f0fu;
+      // (opaque to the optimizer, which would rather have a bit-field extract for every code than a conversion of a byte)
+      asm("" : "+v"(even), "+v"(odd));
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         x[2 * i] = (float)((even >> (8 * i)) & 0xffu);
@@ -78,7 +85,8 @@ struct Run {
     } else if constexpr (BITS == 2) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const uint32_t every = (w[0] >> (2 * k)) & 0x03030303u;  // codes k, k + 4, ..
+        uint32_t every = (w[0] >> (2 * k)) & 0x03030303u;  // codes k, k + 4, ..
+        asm("" : "+v"(every));
         x[k] = (float)((every >> (16 * s)) & 0xffu);
         x[4 + k] = (float)((every >> (16 * s + 8)) & 0xffu);
       }
@@ -116,6 +124,7 @@ template <int BITS, int G, int QB>
 __global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs a) {
   __shared__ __align__(16) float acc[kWaves][kRows][kD + 4];
   __shared__ float refs[kWaves][kRows], sums[kWaves][kRows];
+  __shared__ float shares[kWaves][kJoinRows][kD];
   __shared__ int last;
   const int lane = threadIdx.x % 64, col = lane % 16, u = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -143,7 +152,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs 
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) ref[qb] = -kInf;
 
-  for (int t = begin + wave; t < end; t += kWaves) {
+  auto tile = [&](int t, auto cut_) {  // cut: some of its tokens lie behind the last
+    constexpr bool kCut = decltype(cut_)::value;
     Run<BITS> kr[4], vr[4];
     float kss[16], kzz[16], vss[16 * kGroups], vzz[16 * kGroups];
 #pragma unroll
@@ -175,7 +185,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs 
       }
     }
     const int left = a.T - t * kTile - 16 * u;  // of the lane's 16 tokens
-    const bool cut = (t + 1) * kTile > a.T;
     bool moves = false;
     float top[QB];
 #pragma unroll
@@ -185,7 +194,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs 
       for (int b = 0; b < 4; ++b)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          if (cut) x[qb][b][j] = 4 * b + j < left ? x[qb][b][j] : -kInf;
+          if (kCut) x[qb][b][j] = 4 * b + j < left ? x[qb][b][j] : -kInf;
           m = fmaxf(m, x[qb][b][j]);
         }
       top[qb] = column_max(m) * a.c2;
@@ -204,7 +213,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs 
     bf16x8 p[QB][2];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-      const float off = ref[qb] == -kInf ? 0.0f : ref[qb];
+      const float off = off_of(ref[qb]);
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -232,7 +241,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs 
           }
         }
         bf16x8 v = view<BITS>(vr[cb], s, sc, ze);
-        if (cut) {  // rows behind the last token hold whatever the cache held there before
+        if (kCut) {  // rows behind the last token hold whatever the cache held there before
           u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -244,7 +253,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs 
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) o[qb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[qb][s], o[qb][cb], 0, 0, 0);
       }
-  }
+  };
+  const int whole = min(end, a.T / kTile);  // (the last tile of all may be cut)
+  for (int t = begin + wave; t < whole; t += kWaves) tile(t, std::false_type{});
+  if (whole < end && (whole - begin) % kWaves == wave) tile(whole, std::true_type{});
 
   // The waves' results, 16 rows at a time: lane (col, u) has channels 16 cb + 4 u + 0..3 of row col.
   float* piece = a.parts + ((size_t)unit * a.splits + split) * kRows * QB * kQueryPart;
@@ -265,7 +277,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs 
       float top = -kInf;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) top = fmaxf(top, refs[w][r]);
-      const float off = top == -kInf ? 0.0f : top;
+      const float off = off_of(top);
       float l = 0.0f, v = 0.0f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
@@ -296,24 +308,60 @@ __global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs 
   }
   __syncthreads();
   if (!last) return;
+  // Join: thread (g, c) takes the parts g, g + 4, .. of channel c, four rows at a time, all loads independent of each other; the four
+  // threads of a channel add up in LDS.  (The fence lets them be plain loads: one after the other, as loads of agent scope are issued, 64
+  // parts took 40 us.)
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   const float* parts = a.parts + (size_t)unit * a.splits * kRows * QB * kQueryPart;
-  for (int i = threadIdx.x; i < kRows * QB * kD; i += 64 * kWaves) {
-    const int r = i / kD, c = i % kD, row = row0 + r;
-    if (row >= a.rows) break;
-    float top = -kInf, l = 0.0f, v = 0.0f;
-    for (int s = 0; s < a.splits; ++s) {
-      const float* from = parts + ((size_t)s * kRows * QB + r) * kQueryPart;
-      const float x = __hip_atomic_load(from + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const float m = __hip_atomic_load(from + kD, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const float n = __hip_atomic_load(from + kD + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const float to = fmaxf(top, m), off = to == -kInf ? 0.0f : to;
-      const float f = exp2_(top - off), g = exp2_(m - off);
-      v = v * f + x * g;
-      l = l * f + n * g;
-      top = to;
+  constexpr size_t kPart = (size_t)kRows * QB * kQueryPart;
+  const int g = threadIdx.x / kD, c = threadIdx.x % kD, rows = min(kRows * QB, a.rows - row0);
+  static_assert(sizeof(acc) >= (size_t)kJoinRows * kQueryPieces * sizeof(float));
+  float (*const weight)[kQueryPieces] = reinterpret_cast<float (*)[kQueryPieces]>(&acc[0][0][0]);  // [row][part]
+  for (int r0 = 0; r0 < rows; r0 += kJoinRows) {
+    const int n = min(kJoinRows, rows - r0);
+    if (wave < n) {  // a wave per row: the parts' weights, the reference and the sum of all
+      const float* of_row = parts + (size_t)(r0 + wave) * kQueryPart + kD;
+      float top = -kInf, l = 0.0f;
+      for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, of_row[s * kPart]);
+#pragma unroll
+      for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+      const float off = off_of(top);
+      for (int s = lane; s < a.splits; s += 64) {
+        const float w = exp2_(of_row[s * kPart] - off);
+        weight[wave][s] = w;
+        l += of_row[s * kPart + 1] * w;
+      }
+#pragma unroll
+      for (int m = 1; m < 64; m *= 2) l += __shfl_xor(l, m);
+      if (lane == 0) {
+        refs[0][wave] = top;
+        sums[0][wave] = l;
+      }
     }
-    a.out[((size_t)head * a.rows + row) * kD + c] = (uint16_t)pack2(v / l, 0.0f);
-    if (c == 0 && a.lse) a.lse[(size_t)head * a.rows + row] = ((top == -kInf ? 0.0f : top) + log2f(l)) * kLn2;
+    __syncthreads();
+    float v[kJoinRows] = {};
+    if (n == kJoinRows) {
+#pragma unroll 4
+      for (int s = g; s < a.splits; s += kWaves)
+#pragma unroll
+        for (int r = 0; r < kJoinRows; ++r) v[r] += parts[s * kPart + (r0 + r) * kQueryPart + c] * weight[r][s];
+    } else {
+#pragma unroll 8
+      for (int s = g; s < a.splits; s += kWaves)
+        for (int r = 0; r < n; ++r) v[r] += parts[s * kPart + (r0 + r) * kQueryPart + c] * weight[r][s];
+    }
+#pragma unroll
+    for (int r = 0; r < kJoinRows; ++r) shares[g][r][c] = v[r];
+    __syncthreads();
+    if (g < n) {
+      float x = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) x += shares[w][g][c];
+      const size_t row = (size_t)head * a.rows + row0 + r0 + g;
+      a.out[row * kD + c] = (uint16_t)pack2(x / sums[0][g], 0.0f);
+      if (c == 0 && a.lse) a.lse[row] = (off_of(refs[0][g]) + log2f(sums[0][g])) * kLn2;
+    }
+    __syncthreads();
   }
 }
 
