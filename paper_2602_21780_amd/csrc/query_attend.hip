@@ -121,7 +121,7 @@ __device__ __forceinline__ void load16(const float* p, float* x) {
 
 // A workgroup: one head, 16 QB query rows, tiles [begin, end) of 64 tokens.
 template <int BITS, int G, int QB>
-__global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs a) {
+__global__ __launch_bounds__(64 * kWaves, QB == 1 ? 3 : 2) void query_attend_kernel(QueryArgs a) {
   __shared__ __align__(16) float acc[kWaves][kRows][kD + 4];
   __shared__ float refs[kWaves][kRows], sums[kWaves][kRows];
   __shared__ float shares[kWaves][kJoinRows][kD];
@@ -152,24 +152,30 @@ __global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs 
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) ref[qb] = -kInf;
 
+  // A tile's keys are fetched while the values of the wave's tile before are worked on, its values while its keys are.
+  Run<BITS> kr[4];
+  float kss[16], kzz[16];
+  auto fetch_keys = [&](int t) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b) kr[b].load(kc + ((size_t)t * kTile + 16 * (col / 4) + 4 * b + col % 4) * kRowBytes + u * kRunBytes);
+    if constexpr (BITS != 16) {
+      const size_t at = ((size_t)t * (kTile / G) + (G == 32 ? col / 8 : 0)) * kD + 16 * u;
+      load16(ks + at, kss);
+      load16(kz + at, kzz);
+    }
+  };
   auto tile = [&](int t, auto cut_) {  // cut: some of its tokens lie behind the last
     constexpr bool kCut = decltype(cut_)::value;
-    Run<BITS> kr[4], vr[4];
-    float kss[16], kzz[16], vss[16 * kGroups], vzz[16 * kGroups];
+    Run<BITS> vr[4];
+    float vss[16 * kGroups], vzz[16 * kGroups];
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      kr[b].load(kc + ((size_t)t * kTile + 16 * (col / 4) + 4 * b + col % 4) * kRowBytes + u * kRunBytes);
-      vr[b].load(vc + ((size_t)t * kTile + 16 * b + col) * kRowBytes + u * kRunBytes);
-    }
+    for (int b = 0; b < 4; ++b) vr[b].load(vc + ((size_t)t * kTile + 16 * b + col) * kRowBytes + u * kRunBytes);
     if constexpr (BITS != 16) {
-      const size_t kg = ((size_t)t * (kTile / G) + (G == 32 ? col / 8 : 0)) * kD + 16 * u;
-      load16(ks + kg, kss);
-      load16(kz + kg, kzz);
-      const size_t vg = ((size_t)t * kTile + 16 * u) * kGroups;
+      const size_t at = ((size_t)t * kTile + 16 * u) * kGroups;
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
-        load16(vs + vg + 16 * g, vss + 16 * g);
-        load16(vz + vg + 16 * g, vzz + 16 * g);
+        load16(vs + at + 16 * g, vss + 16 * g);
+        load16(vz + at + 16 * g, vzz + 16 * g);
       }
     }
     f32x4 x[QB][4];
@@ -184,6 +190,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs 
         for (int qb = 0; qb < QB; ++qb) x[qb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[qb][s], x[qb][b], 0, 0, 0);
       }
     }
+    if (t + kWaves < end) fetch_keys(t + kWaves);
     const int left = a.T - t * kTile - 16 * u;  // of the lane's 16 tokens
     bool moves = false;
     float top[QB];
@@ -255,6 +262,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs 
       }
   };
   const int whole = min(end, a.T / kTile);  // (the last tile of all may be cut)
+  if (begin + wave < end) fetch_keys(begin + wave);
   for (int t = begin + wave; t < whole; t += kWaves) tile(t, std::false_type{});
   if (whole < end && (whole - begin) % kWaves == wave) tile(whole, std::true_type{});
 
@@ -322,17 +330,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs 
     if (wave < n) {  // a wave per row: the parts' weights, the reference and the sum of all
       const float* of_row = parts + (size_t)(r0 + wave) * kQueryPart + kD;
       float top = -kInf, l = 0.0f;
-      for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, of_row[s * kPart]);
+#pragma unroll 2
+      for (int s = lane; s < a.splits; s += 64) {
+        const float m = of_row[s * kPart], n = of_row[s * kPart + 1], to = fmaxf(top, m), off = off_of(to);
+        l = l * exp2_(top - off) + n * exp2_(m - off);
+        top = to;
+        weight[wave][s] = m;
+      }
+      const float own = top;
 #pragma unroll
       for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
       const float off = off_of(top);
-      for (int s = lane; s < a.splits; s += 64) {
-        const float w = exp2_(of_row[s * kPart] - off);
-        weight[wave][s] = w;
-        l += of_row[s * kPart + 1] * w;
-      }
+      l *= exp2_(own - off);
 #pragma unroll
       for (int m = 1; m < 64; m *= 2) l += __shfl_xor(l, m);
+      for (int s = lane; s < a.splits; s += 64) weight[wave][s] = exp2_(weight[wave][s] - off);
       if (lane == 0) {
         refs[0][wave] = top;
         sums[0][wave] = l;
@@ -340,15 +352,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void query_attend_kernel(QueryArgs 
     }
     __syncthreads();
     float v[kJoinRows] = {};
+    const float* from = parts + (size_t)r0 * kQueryPart + c;
     if (n == kJoinRows) {
-#pragma unroll 4
-      for (int s = g; s < a.splits; s += kWaves)
-#pragma unroll
-        for (int r = 0; r < kJoinRows; ++r) v[r] += parts[s * kPart + (r0 + r) * kQueryPart + c] * weight[r][s];
-    } else {
 #pragma unroll 8
       for (int s = g; s < a.splits; s += kWaves)
-        for (int r = 0; r < n; ++r) v[r] += parts[s * kPart + (r0 + r) * kQueryPart + c] * weight[r][s];
+#pragma unroll
+        for (int r = 0; r < kJoinRows; ++r) v[r] += from[s * kPart + r * kQueryPart] * weight[r][s];
+    } else {
+#pragma unroll
+      for (int r = 0; r < kJoinRows - 1; ++r)
+        if (r < n)
+#pragma unroll 16
+          for (int s = g; s < a.splits; s += kWaves) v[r] += from[s * kPart + r * kQueryPart] * weight[r][s];
     }
 #pragma unroll
     for (int r = 0; r < kJoinRows; ++r) shares[g][r][c] = v[r];
@@ -375,14 +390,15 @@ hipError_t launch(const QueryArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-// Up to 16 rows one column block; more share the dequantized elements, 64 to a wave.  Workgroups enough for the chip, each with
-// a tile for every wave, and no more partial results than the workspace holds.
+// Up to 16 rows one column block; more share the dequantized elements, 64 to a wave.  As many workgroups as the chip holds at once (16 heads
+// of 65536 tokens in 1024: 33 us, in 768: 29), each with a tile for every wave, and no more partial results than the workspace holds.
 bool plan_query(QueryArgs& a) {
   const int rows_wg = a.rows <= kRows ? kRows : kQueryWide * kRows, tiles = (a.T + kTile - 1) / kTile;
   a.blocks = (a.rows + rows_wg - 1) / rows_wg;
   const long long units = (long long)a.H * a.blocks;
   if (units > (1ll << 32) / (64 * kWaves) - 1) return false;  // threads of a launch are counted in 32 bits
-  const long long most = kQueryPieces * (long long)kRows / rows_wg / units;
+  const long long places = a.rows <= kRows ? 3 * 256 : 2 * 256;  // workgroups that the chip holds at once
+  const long long most = std::min(kQueryPieces * (long long)kRows / rows_wg, places) / units;
   a.splits = (int)std::max<long long>(1, std::min<long long>((tiles + kWaves - 1) / kWaves, most));
   return true;
 }
