@@ -390,8 +390,7 @@ hipError_t launch(const QueryArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-// Up to 16 rows one column block; more share the dequantized elements, 64 to a wave.  As many workgroups as the chip holds at once (16 heads
-// of 65536 tokens in 1024: 33 us, in 768: 29), each with a tile for every wave, and no more partial results than the workspace holds.
+// Up to 16 rows one column block; more share the dequantized elements, 64 to a wave.  As many workgroups as the chip holds at once, each with a tile for every wave, and no more partial results than the workspace holds.
 bool plan_query(QueryArgs& a) {
   const int rows_wg = a.rows <= kRows ? kRows : kQueryWide * kRows, tiles = (a.T + kTile - 1) / kTile;
   a.blocks = (a.rows + rows_wg - 1) / rows_wg;

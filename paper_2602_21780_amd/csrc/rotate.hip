@@ -44,11 +44,22 @@ __device__ inline u32x4 pack8(const float* x) {  // to bf16, nearest even
   return r;
 }
 
+// A value of another lane of the same row, without a round trip through LDS.
+template <int CTRL>
+__device__ inline float from_lane(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+constexpr int kLane1 = 0xb1, kLane2 = 0x4e, kReverse4 = 0x1b, kReverse8 = 0x141;  // lane ^ 1, lane ^ 2, 3 - lane in four, 7 - lane in eight
+template <int MASK>
+__device__ inline float mate_of(float v) {  // of lane ^ MASK
+  static_assert(MASK == 2 || MASK == 4);
+  if (MASK == 2) return from_lane<kLane2>(v);
+  return from_lane<kReverse4>(from_lane<kReverse8>(v));
+}
 __device__ inline float row_sum(float v) {  // over the 8 lanes of a row
-  v += __shfl_xor(v, 1);
-  v += __shfl_xor(v, 2);
-  v += __shfl_xor(v, 4);
-  return v;
+  v += from_lane<kLane1>(v);
+  v += from_lane<kLane2>(v);
+  return v + from_lane<kReverse8>(v);  // (the four lanes of either half hold the same)
 }
 
 // Cosine and sine of the pairs that this lane's channels 8c .. 8c + 7 belong to.
@@ -91,7 +102,7 @@ struct Turn {
     const bool upper = (lane & kMate) != 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float mate = __shfl_xor(x[j], kMate);
+      const float mate = mate_of<kMate>(x[j]);
       const float s = SIGN * sin_[j];
       x[j] = x[j] * cos_[j] + (upper ? mate * s : -(mate * s));
     }
@@ -215,13 +226,17 @@ __global__ __launch_bounds__(64 * kWaves) void rotate_grad_kernel(RotateArgs a, 
       turn.template apply<-1>(u, lane);
       const float r = normalize<NORM>(x, a.eps);
       float su = 0.0f, sux = 0.0f;
+      auto add = [&](float* to_w, float* to_b) {  // (a lane without a head holds zeros and adds nothing)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {  // (a lane without a head holds zeros and adds nothing)
-        const float gx = u[j] * x[j];
-        dw[0][j] += which == 0 ? gx : 0.0f;
-        dw[1][j] += which == 0 ? 0.0f : gx;
-        db[0][j] += which == 0 ? u[j] : 0.0f;
-        db[1][j] += which == 0 ? 0.0f : u[j];
+        for (int j = 0; j < 8; ++j) {
+          to_w[j] += u[j] * x[j];
+          to_b[j] += u[j];
+        }
+      };
+      if (which == 0) add(dw[0], db[0]);
+      else add(dw[1], db[1]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
         u[j] *= w[j];
         su += u[j];
         sux += u[j] * x[j];
@@ -259,19 +274,20 @@ __global__ __launch_bounds__(64 * kWaves) void rotate_grad_kernel(RotateArgs a, 
   a.partials[(size_t)blockIdx.x * 4 * kD + i] = s;
 }
 
-constexpr int kSumColumns = 16;
-__global__ __launch_bounds__(256) void rotate_grad_sum(const float* partials, float* weight_grads, int n_partials) {
-  __shared__ float part[16][kSumColumns];
+constexpr int kSumColumns = 16, kSumSlices = 64;
+__global__ __launch_bounds__(kSumColumns * kSumSlices) void rotate_grad_sum(const float* partials, float* weight_grads, int n_partials) {
+  __shared__ float part[kSumSlices][kSumColumns];
   const int col = threadIdx.x % kSumColumns, slice = threadIdx.x / kSumColumns;
   const int at = blockIdx.x * kSumColumns + col;
   float s = 0.0f;
-  for (int p = slice; p < n_partials; p += 16) s += partials[(size_t)p * 4 * kD + at];
+#pragma unroll 8
+  for (int p = slice; p < n_partials; p += kSumSlices) s += partials[(size_t)p * 4 * kD + at];
   part[slice][col] = s;
   __syncthreads();
   if (slice == 0) {
     float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sum += part[i][col];
+    for (int i = 0; i < kSumSlices; ++i) sum += part[i][col];
     weight_grads[at] = sum;
   }
 }
@@ -331,7 +347,7 @@ hipError_t launch_rotate_grad(const RotateArgs& a, int norm, int axes, bool inte
     if (e != hipSuccess) return e;
   }
   if (!a.weight_grads) return hipSuccess;
-  rotate_grad_sum<<<4 * kD / kSumColumns, 256, 0, stream>>>(a.partials, a.weight_grads, blocks);  // (no tokens: zeros)
+  rotate_grad_sum<<<4 * kD / kSumColumns, kSumColumns * kSumSlices, 0, stream>>>(a.partials, a.weight_grads, blocks);  // (no tokens: zeros)
   return hipGetLastError();
 }
 
