@@ -456,7 +456,7 @@ def _bf16(t, name, shape=None):
     """The checks that need the torch tensor; the library checks pointers, strides and sizes."""
     if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or t.dim() != 3 or not t.is_cuda:
         raise ValueError(f"{name}: expected a bf16 device tensor [heads][tokens][64]")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.shape[2] != 64 or (t.stride(2) != 1 and t.numel()):
         raise ValueError(f"{name}: expected 64 contiguous channels")
@@ -467,16 +467,13 @@ def _operand(t):
     """xsv_tensor of a tensor that _bf16 has seen, or of none.  (The strides of an axis of one entry mean nothing to the tensor and are free.)"""
     if t is None:
         return _NO_TENSOR
-    sh, st = t.stride(0), t.stride(1)
-    if t.shape[1] == 1:
-        st = 64
-    if t.shape[0] == 1:
-        sh = 0
-    return xsv_tensor(t.data_ptr(), sh, st)
+    sh, st, _ = t.stride()
+    heads, rows, _ = t.shape
+    return xsv_tensor(t.data_ptr(), 0 if heads == 1 else sh, 64 if rows == 1 else st)
 
 
 def _plain(t, name, dtype, shape, device):
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {device}")
     return t
 
@@ -490,11 +487,16 @@ def _same_device(device, *tensors):
 class _on:
     """For one call: the tensors' device is the current one, and what the call allocates belongs to the stream it runs on."""
 
+    __slots__ = ("device", "guards")
+
     def __init__(self, device, stream):
-        if stream is not None and stream.device != device:
-            raise ValueError(f"stream of {stream.device}, tensors on {device}")
-        self.device, self.stream = device, stream
-        self.guards = [torch.cuda.device(device)] + ([torch.cuda.stream(stream)] if stream is not None else [])
+        self.device, self.guards = device, ()
+        if stream is not None:
+            if stream.device != device:
+                raise ValueError(f"stream of {stream.device}, tensors on {device}")
+            self.guards = (torch.cuda.device(device), torch.cuda.stream(stream))
+        elif device.index != torch.cuda.current_device():
+            self.guards = (torch.cuda.device(device),)
 
     def __enter__(self):
         for g in self.guards:
@@ -513,7 +515,8 @@ def _like(out, name, x):
     _bf16(out, name, x.shape)
     if out.device != x.device:
         raise ValueError(f"{name}: on {out.device}, the call's tensors on {x.device}")
-    if any(n > 1 and st == 0 for n, st in zip(out.shape, out.stride())):
+    heads, rows, _ = out.shape
+    if (heads > 1 and out.stride(0) == 0) or (rows > 1 and out.stride(1) == 0):
         raise ValueError(f"{name}: an output must not be an expanded tensor")
     return out
 
