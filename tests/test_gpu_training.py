@@ -1,0 +1,132 @@
+"""The operators around the step as they are used together: a layer's attention in training, and the streaming step fed by them.
+Each is held to its definition in tests of its own; here what is between them counts."""
+import numpy as np
+import pytest
+import torch
+
+import plain_operators as plain
+from paper_2602_21780_amd import autograd, xsv
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _layer(n, heads, kv, seed):
+    """What a layer's projection wrote, packed, and the norms' parameters."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((n, heads + 2 * kv, 64), generator=g).to(torch.bfloat16).to(DEV)
+    weights = [(1 + 0.2 * torch.randn(64, generator=g)).to(DEV), (0.1 * torch.randn(64, generator=g)).to(DEV),
+               (1 + 0.2 * torch.randn(64, generator=g)).to(DEV), (0.1 * torch.randn(64, generator=g)).to(DEV)]
+    positions = torch.stack([torch.arange(n) % 59 // 8, torch.arange(n) % 59 % 8], 1).to(torch.int32).to(DEV)
+    return x, weights, positions
+
+
+@pytest.mark.parametrize("frames,n,heads,kv,causal", [(3, 59, 4, 4, 59), (4, 64, 6, 2, 0), (1, 300, 2, 1, 1)])
+def test_a_layers_attention_in_training(frames, n, heads, kv, causal):
+    """norm and rotation, attention frame by frame or across frames, a loss: the gradients of the packed projection and of the
+    norms' parameters are what the functions of the library give one after the other."""
+    total = frames * n
+    x, weights, positions = _layer(total, heads, kv, 3 * n + heads)
+    begin = torch.arange(0, total + 1, total if causal else n, dtype=torch.int32, device=DEV)
+    form = dict(longest_q=total if causal else n, longest_k=total if causal else n, causal=causal)
+    names = ("q_weight", "q_bias", "k_weight", "k_bias")
+    leaf, params = x.clone().requires_grad_(), [w.clone().requires_grad_() for w in weights]
+    q, k, v = leaf.transpose(0, 1).split([heads, kv, kv])
+    qr, kr = autograd.norm_rotate(q, k, positions=positions, **dict(zip(names, params)))
+    out, lse = autograd.seq_attend(qr, kr, v, begin, **form)
+    target = torch.randn(out.shape, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(DEV)
+    (out.float() * target.float()).sum().backward()
+
+    q, k, v = x.transpose(0, 1).split([heads, kv, kv])
+    qr2, kr2 = xsv.norm_rotate(q, k, positions=positions, **dict(zip(names, weights)))
+    out2, lse2 = xsv.seq_attend(qr2, kr2, v, begin, **form)
+    assert torch.equal(out, out2) and torch.equal(lse, lse2)
+    dq, dk, dv = xsv.seq_attend_grad(target, qr2, kr2, v, out2, lse2, begin, **form)
+    dq, dk, dw = xsv.norm_rotate_grad(dq, dk, q, k, positions=positions, **dict(zip(names, weights)))
+    assert torch.equal(leaf.grad, torch.cat([dq, dk, dv]).transpose(0, 1))
+    for p, w in zip(params, dw):
+        assert torch.equal(p.grad, w)
+
+    # and against all of it in 64 bits.  Roundings to bf16 of q and k (2^-8 of each, which move a logit by up to 2 * 2^-8 of the sum of its
+    # terms' magnitudes), of P, dS, out and both gradients: a few 2^-8 of every result's size; 0.04 is ten of them, as rms.
+    leaf64, params64 = x.cpu().double().requires_grad_(), [w.cpu().double().requires_grad_() for w in weights]
+    q, k, v = leaf64.transpose(0, 1).split([heads, kv, kv])
+    q = plain.norm_rotate(q, params64[0], params64[1], "layer", 1e-5, positions.cpu(), 100.0, False)
+    k = plain.norm_rotate(k, params64[2], params64[3], "layer", 1e-5, positions.cpu(), 100.0, False)
+    outs = []
+    size = form["longest_q"]
+    see = plain.sees(size, size, causal)
+    for a in range(0, total, size):
+        heads_out = []
+        for h in range(heads):
+            g = h * kv // heads
+            s = (q[h, a:a + size] @ k[g, a:a + size].t()) * 0.125
+            heads_out.append(torch.softmax(s.masked_fill(~see, float("-inf")), 1) @ v[g, a:a + size])
+        outs.append(torch.stack(heads_out))
+    out64 = torch.cat(outs, 1)
+    (out64 * target.cpu().double()).sum().backward()
+    rel = lambda a, b: float(((a.detach().cpu().double() - b.detach()).pow(2).mean() / b.detach().pow(2).mean()).sqrt())
+    errors = [rel(out, out64), rel(leaf.grad, leaf64.grad)] + [rel(p.grad, p64.grad) for p, p64 in zip(params, params64)]
+    assert max(errors) <= 0.04, errors
+
+
+def test_gradients_that_autograd_hands_over_expanded_and_inputs_that_need_none():
+    n, heads = 70, 3
+    x, weights, positions = _layer(n, heads, heads, 5)
+    begin = torch.tensor([0, 30, n], dtype=torch.int32, device=DEV)
+    q, k, v = (t.contiguous() for t in x.transpose(0, 1).split(heads))
+    v.requires_grad_()
+    out, _ = autograd.seq_attend(q, k, v, begin, longest_q=40, longest_k=40)
+    out.sum().backward()                                    # an expanded gradient of ones
+    want = xsv.seq_attend_grad(torch.ones_like(q), q, k, v.detach(), out.detach(), xsv.seq_attend(q, k, v.detach(), begin)[1], begin, longest_q=40, longest_k=40)
+    assert torch.equal(v.grad, want[2]) and q.grad is None
+    w = weights[0].clone().requires_grad_()
+    y, none = autograd.norm_rotate(q, q_weight=w, positions=positions)
+    assert none is None
+    y.sum().backward()
+    assert torch.equal(w.grad, xsv.norm_rotate_grad(torch.ones_like(q), None, q, q_weight=weights[0], positions=positions)[2][0])
+    with torch.no_grad():
+        assert torch.equal(autograd.norm_rotate(q, q_weight=w, positions=positions)[0], y.detach())
+
+
+def test_a_key_head_given_to_several_by_expansion_gets_the_sum_of_their_gradients():
+    n, heads = 90, 4
+    x, _, _ = _layer(n, heads, 1, 6)
+    begin = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    q, k, v = (t.contiguous() for t in x.transpose(0, 1).split([heads, 1, 1]))
+    shared = [t.clone().requires_grad_() for t in (k, v)]
+    wide = [t.clone().requires_grad_() for t in (k, v)]
+    autograd.seq_attend(q, *shared, begin, causal=1)[0].float().pow(2).sum().backward()
+    autograd.seq_attend(q, *[t.expand(heads, n, 64) for t in wide], begin, causal=1)[0].float().pow(2).sum().backward()
+    for a, b in zip(shared, wide):
+        # each of the four heads' gradients and their sums are rounded to bf16 on the second way: 2^-8 of the terms' magnitudes, twice
+        terms = 4 * torch.maximum(a.grad.abs().float(), b.grad.abs().float()).amax()
+        assert float((a.grad.float() - b.grad.float()).abs().max()) <= 2 * 2.0 ** -8 * float(terms)
+
+
+def test_streaming_frames_through_norm_rotation_step_and_single_tokens():
+    """A stream whose queries and keys come out of norm_rotate: the step's outputs are attention over what the cache showed before it and
+    the frame, and single tokens in between see the cache that the step left."""
+    H, n = 4, 64
+    ctx = xsv.Context(1, H, 64, n, 5, 3 * n, 4, 32)
+    single, weights, positions = _layer(1, H, H, 9)
+    for f in range(6):
+        x, _, _ = _layer(n, H, H, 20 + f)
+        _, _, pos = _layer(n, H, H, 0)
+        q, k, v = x.transpose(0, 1).split(H)
+        q, k = xsv.norm_rotate(q, k, q_weight=weights[0], q_bias=weights[1], k_weight=weights[2], k_bias=weights[3], positions=pos)
+        before = ctx.cache_export(0) if f else None
+        out = ctx.step(0, q, k, v)
+        qs, _ = xsv.norm_rotate(single.transpose(0, 1)[:H], q_weight=weights[0], q_bias=weights[1], positions=positions)
+        one, lse = ctx.query_attend(0, qs)
+        view = lambda a: torch.from_numpy((a.astype(np.uint32) << 16).view(np.float32))
+        after = ctx.cache_export(0)
+        for h in range(H):
+            keys, values = k[h].cpu().float(), v[h].cpu().float()
+            if f:
+                keys, values = torch.cat([view(before.k_bf16)[h], keys]), torch.cat([view(before.v_bf16)[h], values])
+            e = plain.Attention(q[h].cpu().float(), keys, values, 0, 0.125)
+            assert float((out[h].cpu().double() - e.out).abs().max()) <= 2e-2      # (the step's documented bound)
+            e = plain.Attention(qs[h].cpu().float(), view(after.k_bf16)[h], view(after.v_bf16)[h], 0, 0.125)
+            assert bool(((one[h].cpu().double() - e.out).abs() <= e.out_tol).all()) and bool(((lse[h].cpu().double() - e.lse).abs() <= e.lse_tol).all())
+    ctx.destroy()
