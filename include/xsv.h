@@ -244,7 +244,7 @@ typedef struct {
   int32_t axes;              /* 0 | 1 | 2                                                               */
   int32_t interleaved;       /* 0 | 1                                                                   */
   float eps;                 /* > 0 (unless XSV_NORM_NONE)                                              */
-  double base;               /* > 0 (unless axes == 0)                                                  */
+  double base;               /* >= 1 (unless axes == 0)                                                 */
   const int32_t* positions;  /* DEVICE [n][axes]                                                        */
   const float* q_weight;     /* DEVICE [64] each, shared by the heads; NULL = ones (weight), zeros (bias) */
   const float* q_bias;
@@ -269,7 +269,8 @@ int xsv_norm_rotate_grad_workspace(const xsv_rotate_config* cfg, int64_t* bytes)
  * offsets ascend and stay within the tensors (what does not is cut off: no row outside the tensors is touched).  Sequences may be empty
  * on either side.  Rows in no sequence are neither read nor written.  Query i of n stands at key position i + m - n of m: at the end of its
  * sequence's keys, so that keys of earlier frames or tokens may lie in front.  A query that sees no key has out = 0 and lse = -inf, and
- * adds nothing to any gradient.  Values that are not finite in rows that a query does not see do not reach it, nor its gradient. */
+ * adds nothing to any gradient.  Values that are not finite in rows that a query does not see do not reach it, nor its gradient.  (Unnormalized sums are fp32:
+ * values of 2^80 and more may overflow them.) */
 typedef struct {
   int32_t heads, kv_heads;       /* 1 .. 65536, heads a multiple of kv_heads: head h reads key head h / (heads / kv_heads) */
   int32_t sequences;             /* >= 0                                                       */
@@ -279,7 +280,7 @@ typedef struct {
   const int32_t* k_begin;        /* DEVICE [sequences + 1]; may be q_begin                     */
   int32_t causal;                /* 0: every key of the sequence is seen.  b > 0: keys come in blocks of b (b = 1: token by token, b =
                                     tokens_per_frame: frame by frame), a query sees its own block and those before it   */
-  float softmax_scale;           /* >= 0; 0 -> 1/sqrt(64)                                      */
+  float softmax_scale;           /* 0 -> 1/sqrt(64), else 1e-20 .. 1e20                        */
 } xsv_seq_config;
 /* q, out: bf16 [heads][rows_q][64], k, v: bf16 [kv_heads][rows_k][64] via strides; lse: float [heads][rows_q]. */
 int xsv_seq_attend(void* hip_stream, const xsv_seq_config* cfg, xsv_tensor q, xsv_tensor k, xsv_tensor v, xsv_tensor out, float* lse,

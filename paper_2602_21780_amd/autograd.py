@@ -2,7 +2,8 @@
 
 Same arguments as the functions of `xsv` without outputs and streams: they run on the current stream of the tensors' device, the
 gradient on the stream of the forward pass.  Nothing else is computed here.  Gradients are bf16 like the tensors, those of the
-norm's weights and biases fp32; there are no second derivatives.
+norm's weights and biases fp32; there are no second derivatives.  (As with every function of torch: capture a backward pass into a graph
+only while no eager graph over the same leaves is alive.)
 """
 from __future__ import annotations
 

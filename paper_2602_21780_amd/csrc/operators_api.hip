@@ -23,7 +23,7 @@ int check_rotate(const xsv_rotate_config* c) {
   if (!c || c->n < 0 || c->heads_q < 0 || c->heads_k < 0 || c->heads_q + (long long)c->heads_k == 0) return XSV_ERR_ARG;
   if (c->norm < XSV_NORM_NONE || c->norm > XSV_NORM_LAYER || c->axes < 0 || c->axes > 2) return XSV_ERR_ARG;
   if (c->norm != XSV_NORM_NONE && !(c->eps > 0.0f && std::isfinite(c->eps))) return XSV_ERR_ARG;
-  if (c->axes > 0 && !(c->base > 0.0 && std::isfinite(c->base))) return XSV_ERR_ARG;
+  if (c->axes > 0 && !(c->base >= 1.0 && std::isfinite(c->base))) return XSV_ERR_ARG;
   if (c->axes > 0 && c->n > 0 && (!c->positions || !aligned_to(c->positions, 4))) return XSV_ERR_ARG;
   for (const float* p : {c->q_weight, c->q_bias, c->k_weight, c->k_bias})
     if (!aligned_to(p, 4)) return XSV_ERR_ARG;
@@ -46,7 +46,7 @@ RotateArgs rotate_args(const xsv_rotate_config& c) {
 int check_seq(const xsv_seq_config* c) {
   if (!c || c->heads < 1 || c->kv_heads < 1 || c->heads % c->kv_heads != 0 || c->sequences < 0 || c->rows_q < 0 || c->rows_k < 0) return XSV_ERR_ARG;
   if (c->longest_q < 0 || c->longest_k < 0 || c->longest_q > c->rows_q || c->longest_k > c->rows_k || c->causal < 0) return XSV_ERR_ARG;
-  if (!(c->softmax_scale >= 0.0f) || !std::isfinite(c->softmax_scale)) return XSV_ERR_ARG;
+  if (c->softmax_scale != 0.0f && !(c->softmax_scale >= 1e-20f && c->softmax_scale <= 1e20f)) return XSV_ERR_ARG;
   if (c->sequences > 0 && (!c->q_begin || !c->k_begin || !aligned_to(c->q_begin, 4) || !aligned_to(c->k_begin, 4))) return XSV_ERR_ARG;
   if (c->heads > (1 << 16)) return XSV_ERR_UNSUPPORTED;
   return XSV_OK;

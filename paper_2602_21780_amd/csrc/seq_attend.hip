@@ -1074,18 +1074,18 @@ constexpr long long kMostWorkgroups = (1ll << 32) / 512 - 1;  // threads of a la
 
 // How the blocks of 128 rows of a launch are worked on.  Four waves of 32 rows, two or three such workgroups to a compute unit, if there
 // are blocks enough; else a second wave to every 32 rows, eight waves that fill a compute unit.  us with four and with eight waves,
-// forward, 16 heads: one frame of 1374 tokens (171 blocks) 23.6 and 20.7, 20 heads (214) 23.3 and 20.8, 24 heads (257) 31.3 and 38.8,
-// two frames (343) 33 and 39.  Under a mask blocks differ in length and the second round is shorter: causal, 2000 tokens (250) 32.7 and
-// 28.0, 3000 (375) 44.6 and 37.0.  Where even those leave compute units without work, several workgroups share the tiles of a block and a
-// second launch joins them: 4000 causal tokens of one head 44.9 alone, 29.2 with 2, 20.9 with 4, 18.2 with 8, four single tokens over up to
-// 4000 keys 45.9, 29.2, 21.1, 25.9; more of them than there are compute units gain nothing (one frame: 20.6 alone, 34.0 with 2).
+// forward, 16 heads: one frame of 1374 tokens (171 blocks) 24.0 and 21.2, 20 heads (214) 23.3 and 20.8, 24 heads (257) 32.8 and 39.4,
+// two frames (343) 34 and 40.  Under a mask blocks differ in length and the second round is shorter: causal, 2000 tokens (250) 32.7 and
+// 29.1, 3000 (375) 45.4 and 37.2.  Where even those leave compute units without work, several workgroups share the tiles of a block and a
+// second launch joins them: 4000 causal tokens of one head 44.5 alone, 28.9 with 2, 20.3 with 4, 17.5 with 8, four single tokens over up to
+// 4000 keys 45.7, 28.7, 20.3, 25.2; more of them than there are compute units gain nothing (one frame: 21.2 alone, 34.5 with 2).
 constexpr int kComputeUnits = 256, kMostParts = 8;
 struct Shape {
   bool split;
   int parts;
 };
 Shape shape_of(const SeqArgs& a, long long rows, int heads, long long tiles) {
-  const long long blocks = std::max<long long>(1, rows * heads / 128);
+  const long long blocks = std::max<long long>(1, heads * std::max<long long>(rows / 128, a.sequences));
   Shape s{blocks <= (a.causal ? 400 : kComputeUnits), 1};
   if (s.split) s.parts = (int)std::max<long long>(1, std::min({(long long)kMostParts, kComputeUnits / blocks, tiles / 4}));
   return s;
@@ -1101,9 +1101,9 @@ void launch_rows(K kernel, const SeqArgs& a, int longest, int heads, int rows, i
 
 }  // namespace
 
-// (what shares tiles over parts has few blocks: far below what a launch can have)
+// (parts and their joins: at most kComputeUnits / 2 heads of sequences, far below what a launch can have)
 bool seq_attend_fits(const SeqArgs& a) {
-  return grid_of(a.longest_q, kJoinRows, a.heads, a.sequences) <= kMostWorkgroups && 2 * grid_of(a.longest_k, kJoinRows, a.kv_heads, a.sequences) <= kMostWorkgroups;
+  return grid_of(a.longest_q, 128, a.heads, a.sequences) <= kMostWorkgroups && grid_of(a.longest_k, 128, a.kv_heads, a.sequences) <= kMostWorkgroups;
 }
 
 int64_t seq_attend_workspace(const SeqArgs& a) {

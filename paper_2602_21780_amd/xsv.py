@@ -294,18 +294,13 @@ class Context:
     def query_attend(self, layer, q, out=None, lse=None):
         """xsv_query_attend: q [H][rows][64] over the layer's cache, on the context's stream.  Returns (out, lse)."""
         H, d = self.cfg.n_heads, self.cfg.head_dim
-        if q.dim() != 3 or q.shape[0] != H or q.shape[2] != d:
-            raise ValueError(f"q: expected [{H}][rows][{d}]")
-        rows = q.shape[1]
-        if out is None:
-            out = torch.empty((H, rows, d), dtype=torch.bfloat16, device=q.device)
-        if lse is None:
-            lse = torch.empty((H, rows), dtype=torch.float32, device=q.device)
-        for name, t, dtype, shape in (("out", out, torch.bfloat16, (H, rows, d)), ("lse", lse, torch.float32, (H, rows))):
-            if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != q.device:
-                raise ValueError(f"{name}: expected a contiguous {dtype} tensor {shape} on {q.device}")
-        if rows:
-            _check(lib().xsv_query_attend(self._h, layer, _operand(_bf16(q, "q")), rows, out.data_ptr(), lse.data_ptr()), "xsv_query_attend")
+        _bf16(q, "q", (H, q.shape[1], d) if isinstance(q, torch.Tensor) and q.dim() == 3 else None)
+        rows, dev = q.shape[1], q.device
+        with _on(dev, self._stream):
+            out = torch.empty((H, rows, d), dtype=torch.bfloat16, device=dev) if out is None else _plain(out, "out", torch.bfloat16, (H, rows, d), dev)
+            lse = torch.empty((H, rows), dtype=torch.float32, device=dev) if lse is None else _plain(lse, "lse", torch.float32, (H, rows), dev)
+            if rows:
+                _check(lib().xsv_query_attend(self._h, layer, _operand(q), rows, out.data_ptr(), lse.data_ptr()), "xsv_query_attend")
         return out, lse
 
     def score_prune(self, layer, q):

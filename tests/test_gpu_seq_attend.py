@@ -110,6 +110,17 @@ def test_many_sequences_at_once(causal, n):
         assert torch.equal(a, b)
 
 
+def test_more_sequences_than_rows():
+    """Nearly all of 3000 sequences empty, one long among them; and 700 of one to nine tokens."""
+    lq = [0] * 2000 + [400] + [0] * 999
+    x = _inputs(lq, lq, 2, 1, seed=2)
+    _check(*x, [400], [400], 1, 0.0, _run(*x, lq, lq, 1))
+    lq = [1 + i % 9 for i in range(700)]
+    lk = [1 + (3 * i) % 11 for i in range(700)]
+    x = _inputs(lq, lk, 4, 2, seed=3)
+    _check(*x, lq, lk, 1, 0.0, _run(*x, lq, lk, 1), sequences=range(0, 700, 37))
+
+
 def test_frame_causal_clip():
     lq = [6 * 239]
     x = _inputs(lq, lq, 3, 3, seed=8)

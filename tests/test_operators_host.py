@@ -32,7 +32,7 @@ BAD_TENSORS = [xsv.xsv_tensor(None, 256, 64), xsv.xsv_tensor(PTR + 8, 256, 64), 
 
 @pytest.mark.parametrize("bad", [dict(n=-1), dict(heads_q=-1), dict(heads_q=0, heads_k=0), dict(norm=3), dict(norm=-1), dict(axes=3), dict(axes=-1),
                                  dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(base=0.0),
-                                 dict(base=float("nan")), dict(base=-2.0), dict(positions=None), dict(positions=PTR + 2), dict(q_weight=PTR + 1),
+                                 dict(base=float("nan")), dict(base=-2.0), dict(base=0.5), dict(base=float("inf")), dict(positions=None), dict(positions=PTR + 2), dict(q_weight=PTR + 1),
                                  dict(k_bias=PTR + 3)])
 def test_rotate_refuses_bad_configurations(lib, bad):
     cfg = _rotate(**bad)
@@ -78,7 +78,7 @@ def _seq(**kw):
 
 @pytest.mark.parametrize("bad", [dict(heads=0), dict(kv_heads=0), dict(kv_heads=3), dict(heads=-4), dict(sequences=-1), dict(rows_q=-1), dict(rows_k=-1),
                                  dict(longest_q=9), dict(longest_k=10), dict(longest_q=-1), dict(causal=-1), dict(softmax_scale=-1.0),
-                                 dict(softmax_scale=float("nan")), dict(softmax_scale=float("inf")), dict(q_begin=None), dict(k_begin=None),
+                                 dict(softmax_scale=float("nan")), dict(softmax_scale=float("inf")), dict(softmax_scale=1e-30), dict(softmax_scale=1e30), dict(q_begin=None), dict(k_begin=None),
                                  dict(q_begin=PTR + 2), dict(k_begin=PTR + 1)])
 def test_seq_attend_refuses_bad_configurations(lib, bad):
     cfg = _seq(**bad)
