@@ -2,8 +2,11 @@
 //
 //   out = softmax(scale q K~^T) V~,   lse = log sum exp(scale q K~^T),   K~, V~ = bf16((code - zero) * scale)
 //
-// What bounds it is the cache: every packed byte is read once per block of query rows (0.625 bytes per element at 4 bits),
-// and a few vector instructions per element turn it into the same bf16 view that the rest of the library attends to.
+// It reads every packed byte once per block of query rows (0.625 bytes per element at 4 bits and groups of 64), and a few vector instructions per
+// element turn it into the same bf16 view that the rest of the library attends to.  Measured at 16 heads, one row over 65536 tokens: a bf16 cache
+// 43 us, which is 6.2 TB/s and the memory's bound (the cache fits the last-level one); 4 bits 29 us, 2.8 TB/s, and 2 bits 31 us: there the arithmetic
+// of the view bounds it, about 640 vector instructions per wave and 64 tokens, the vector units active in 72 % of the cycles.  A call of one
+// row over 4096 tokens takes 10.8 us: the launch, one tile for each wave, and the join of 16 parts, each a wait for memory.
 //
 // A wave takes 64 tokens at a time straight from memory into registers: keys as the A operand of 16x16x32 MFMAs (transposed
 // logits, a lane holds 16 tokens of one query), values, which the cache keeps transposed, as the A operand of the second
@@ -12,7 +15,7 @@
 // 16 (R / 4) + 4 B + R % 4, which puts tokens 16 u .. into the accumulators of quarter u as well.
 //
 // The tokens are cut over the waves of a workgroup (joined in LDS) and over workgroups, so that few rows still use the whole chip;
-// the workgroup that ends last in a (head, row block) joins their partial results, in their order.
+// the workgroup that ends last in a (head, row block), or with many rows a second launch, joins their partial results, in their order.
 #include <algorithm>
 #include <type_traits>
 
@@ -31,6 +34,10 @@ constexpr int kWaves = 4;
 constexpr int kRows = kQueryRows;  // query rows of a column block
 constexpr int kJoinRows = 4;       // rows that are joined at a time, one a wave
 static_assert(kJoinRows == kWaves);
+// Up to so many rows are joined by the workgroup that ends last, one after the other; more by a second launch (16 heads over 4096 tokens: 2 rows 11.5
+// us inside, 4 rows inside 13.6 and by a launch 12.4; over 65536
+// tokens 4 rows inside 33.7 and by a launch 31.0; 16 rows over 20000: 36 and 17.5).
+constexpr int kRowsInside = 2;
 constexpr float kInf = __builtin_inff();
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -119,19 +126,102 @@ __device__ __forceinline__ void load16(const float* p, float* x) {
   }
 }
 
+// Over a wave, in every lane: lanes of a row of 16 by DPP, rows by swaps.
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+template <typename F>
+__device__ __forceinline__ float over_wave(float x, F f) {
+  x = f(x, from_lane<0xb1>(x));   // lane ^ 1
+  x = f(x, from_lane<0x4e>(x));   // lane ^ 2
+  x = f(x, from_lane<0x141>(x));  // 7 - lane of eight: the other four
+  x = f(x, from_lane<0x140>(x));  // 15 - lane of sixteen: the other eight
+  const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = f(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+
+// Joins rows r0 .. r0 + n - 1 (n <= 4) of a (head, row block) from its parts, a whole workgroup.  Every wave works out the weights of 64 parts, one a
+// lane; thread (g, c) takes the values of the parts g, g + 4, .. of channel c, whose loads do not wait for the weights; the four threads of a
+// channel add up in LDS.
+// ROWS: as many rows' loads are on their way together; rows from n on are copies of the last and not stored.
+using Shares = float[kWaves][kJoinRows][kD];
+template <int ROWS>
+__device__ __forceinline__ void join(const QueryArgs& a, int unit, int head, int row0, int r0, int n, int rows_wg, Shares& shares) {
+  const int lane = threadIdx.x % 64, g = __builtin_amdgcn_readfirstlane(threadIdx.x / kD), c = threadIdx.x % kD;
+  const size_t stride = (size_t)rows_wg * kQueryPart;  // between two parts
+  float own_top = -kInf, own_sum = 0.0f;  // of row g
+  float top_of[ROWS], l_of[ROWS], v_of[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    top_of[r] = -kInf;
+    l_of[r] = v_of[r] = 0.0f;
+  }
+  for (int s0 = 0; s0 < a.splits; s0 += 64) {
+    const int last = a.splits - 1;
+    float m_of[ROWS], x_of[ROWS], value_of[ROWS][16];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const float* parts = a.parts + (size_t)unit * a.splits * stride + (size_t)(r0 + min(r, n - 1)) * kQueryPart;
+      const float* own = parts + min(s0 + lane, last) * stride + kD;
+      m_of[r] = s0 + lane <= last ? own[0] : -kInf;
+      x_of[r] = own[1];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) value_of[r][i] = parts[min(s0 + g + i * kWaves, last) * stride + c];
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      float &top = top_of[r], &l = l_of[r], &v = v_of[r];
+      const float m = m_of[r], x = x_of[r];
+      const float* value = value_of[r];
+      const float to = fmaxf(top, over_wave(m, [](float p, float q) { return fmaxf(p, q); })), off = off_of(to);
+      const float f = exp2_(top - off), w = exp2_(m - off);
+      l = l * f + over_wave(s0 + lane <= last ? x * w : 0.0f, [](float p, float q) { return p + q; });
+      v *= f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float part = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), g + i * kWaves));
+        v += s0 + g + i * kWaves <= last ? value[i] * part : 0.0f;
+      }
+      top = to;
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    shares[g][r][c] = v_of[r];
+    if (r == g) {
+      own_top = top_of[r];
+      own_sum = l_of[r];
+    }
+  }
+  __syncthreads();
+  if (g < n) {
+    float x = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) x += shares[w][g][c];
+    const size_t row = (size_t)head * a.rows + row0 + r0 + g;
+    a.out[row * kD + c] = (uint16_t)pack2(x / own_sum, 0.0f);
+    if (c == 0 && a.lse) a.lse[row] = (off_of(own_top) + log2f(own_sum)) * kLn2;
+  }
+  __syncthreads();
+}
+
 // A workgroup: one head, 16 QB query rows, tiles [begin, end) of 64 tokens.
 template <int BITS, int G, int QB>
 __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 3 : 2) void query_attend_kernel(QueryArgs a) {
   __shared__ __align__(16) float acc[kWaves][kRows][kD + 4];
   __shared__ float refs[kWaves][kRows], sums[kWaves][kRows];
-  __shared__ float shares[kWaves][kJoinRows][kD];
+  __shared__ Shares shares;
   __shared__ int last;
   const int lane = threadIdx.x % 64, col = lane % 16, u = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits, block = unit % a.blocks, head = unit / a.blocks;
   const int row0 = block * kRows * QB;
   const int tiles = (a.T + kTile - 1) / kTile;
-  const int begin = (int)((long long)tiles * split / a.splits), end = (int)((long long)tiles * (split + 1) / a.splits);
+  // (at most 2^18 tiles and 2^10 parts)
+  const int begin = (int)((uint32_t)tiles * (uint32_t)split / (uint32_t)a.splits), end = (int)((uint32_t)tiles * (uint32_t)(split + 1) / (uint32_t)a.splits);
   constexpr int kRowBytes = kD * BITS / 8, kRunBytes = 2 * BITS, kGroups = kD / G;
   const uint8_t* kc = a.kc + (size_t)head * a.code_head;
   const uint8_t* vc = a.vc + (size_t)head * a.code_head;
@@ -306,7 +396,7 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 3 : 2) void query_attend_ker
       }
     }
   }
-  if (a.splits == 1) return;
+  if (a.splits == 1 || a.rows > kRowsInside) return;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part has reached memory
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -316,68 +406,18 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 3 : 2) void query_attend_ker
   }
   __syncthreads();
   if (!last) return;
-  // Join: thread (g, c) takes the parts g, g + 4, .. of channel c, four rows at a time, all loads independent of each other; the four
-  // threads of a channel add up in LDS.  (The fence lets them be plain loads: one after the other, as loads of agent scope are issued, 64
-  // parts took 40 us.)
+  // (The fence lets the join read what other XCDs wrote with plain loads, all on their way at once: one after the other, as loads of
+  // agent scope are issued, 64 parts took 40 us.)
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-  const float* parts = a.parts + (size_t)unit * a.splits * kRows * QB * kQueryPart;
-  constexpr size_t kPart = (size_t)kRows * QB * kQueryPart;
-  const int g = threadIdx.x / kD, c = threadIdx.x % kD, rows = min(kRows * QB, a.rows - row0);
-  static_assert(sizeof(acc) >= (size_t)kJoinRows * kQueryPieces * sizeof(float));
-  float (*const weight)[kQueryPieces] = reinterpret_cast<float (*)[kQueryPieces]>(&acc[0][0][0]);  // [row][part]
-  for (int r0 = 0; r0 < rows; r0 += kJoinRows) {
-    const int n = min(kJoinRows, rows - r0);
-    if (wave < n) {  // a wave per row: the parts' weights, the reference and the sum of all
-      const float* of_row = parts + (size_t)(r0 + wave) * kQueryPart + kD;
-      float top = -kInf, l = 0.0f;
-#pragma unroll 2
-      for (int s = lane; s < a.splits; s += 64) {
-        const float m = of_row[s * kPart], n = of_row[s * kPart + 1], to = fmaxf(top, m), off = off_of(to);
-        l = l * exp2_(top - off) + n * exp2_(m - off);
-        top = to;
-        weight[wave][s] = m;
-      }
-      const float own = top;
-#pragma unroll
-      for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
-      const float off = off_of(top);
-      l *= exp2_(own - off);
-#pragma unroll
-      for (int m = 1; m < 64; m *= 2) l += __shfl_xor(l, m);
-      for (int s = lane; s < a.splits; s += 64) weight[wave][s] = exp2_(weight[wave][s] - off);
-      if (lane == 0) {
-        refs[0][wave] = top;
-        sums[0][wave] = l;
-      }
-    }
-    __syncthreads();
-    float v[kJoinRows] = {};
-    const float* from = parts + (size_t)r0 * kQueryPart + c;
-    if (n == kJoinRows) {
-#pragma unroll 8
-      for (int s = g; s < a.splits; s += kWaves)
-#pragma unroll
-        for (int r = 0; r < kJoinRows; ++r) v[r] += from[s * kPart + r * kQueryPart] * weight[r][s];
-    } else {
-#pragma unroll
-      for (int r = 0; r < kJoinRows - 1; ++r)
-        if (r < n)
-#pragma unroll 16
-          for (int s = g; s < a.splits; s += kWaves) v[r] += from[s * kPart + r * kQueryPart] * weight[r][s];
-    }
-#pragma unroll
-    for (int r = 0; r < kJoinRows; ++r) shares[g][r][c] = v[r];
-    __syncthreads();
-    if (g < n) {
-      float x = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) x += shares[w][g][c];
-      const size_t row = (size_t)head * a.rows + row0 + r0 + g;
-      a.out[row * kD + c] = (uint16_t)pack2(x / sums[0][g], 0.0f);
-      if (c == 0 && a.lse) a.lse[row] = (off_of(refs[0][g]) + log2f(sums[0][g])) * kLn2;
-    }
-    __syncthreads();
-  }
+  for (int r = 0; r < a.rows; ++r) join<1>(a, unit, head, row0, r, 1, kRows * QB, shares);
+}
+
+// The join of many rows, four to a workgroup.
+__global__ __launch_bounds__(64 * kWaves) void query_join_kernel(QueryArgs a, int rows_wg) {
+  __shared__ Shares shares;
+  const int groups = (a.rows + kJoinRows - 1) / kJoinRows, head = blockIdx.x / groups, row = blockIdx.x % groups * kJoinRows;
+  const int block = row / rows_wg, row0 = block * rows_wg;
+  join<kJoinRows>(a, head * a.blocks + block, head, row0, row - row0, min(kJoinRows, a.rows - row), rows_wg, shares);
 }
 
 template <int BITS, int G>
@@ -385,12 +425,16 @@ hipError_t launch(const QueryArgs& a, hipStream_t stream) {
   const int workgroups = a.H * a.blocks * a.splits;
   if (a.rows <= kRows) query_attend_kernel<BITS, G, 1><<<workgroups, 64 * kWaves, 0, stream>>>(a);
   else query_attend_kernel<BITS, G, kQueryWide><<<workgroups, 64 * kWaves, 0, stream>>>(a);
+  if (a.splits > 1 && a.rows > kRowsInside)
+    query_join_kernel<<<a.H * ((a.rows + kJoinRows - 1) / kJoinRows), 64 * kWaves, 0, stream>>>(a, a.rows <= kRows ? kRows : kQueryWide * kRows);
   return hipGetLastError();
 }
 
 }  // namespace
 
-// Up to 16 rows one column block; more share the dequantized elements, 64 to a wave.  As many workgroups as the chip holds at once, each with a tile for every wave, and no more partial results than the workspace holds.
+// Up to 16 rows one column block; more share the dequantized elements, 64 to a wave (20000 tokens: 16 rows 17.6 us, 17 rows 25, 64 rows 27, so
+// two passes of 16 rows would already take longer).  As many workgroups as the chip holds at once, each with a tile for every wave, and no more partial
+// results than the workspace holds.
 bool plan_query(QueryArgs& a) {
   const int rows_wg = a.rows <= kRows ? kRows : kQueryWide * kRows, tiles = (a.T + kTile - 1) / kTile;
   a.blocks = (a.rows + rows_wg - 1) / rows_wg;
