@@ -40,7 +40,7 @@ struct SeqArgs {
   SeqRows q, k, v, out, dout;  // out: written by the forward pass, read by the gradient
   SeqRows dq, dk, dv;
   float* lse;    // [heads][rows_q]
-  float* delta;  // gradient: [heads][rows_q] sums of dout * out, written by the first launch, read by the second
+  float* delta;  // gradient: [heads][rows_q] sums of dout * out, written by the first launch, read by the others
   const int32_t* q_begin;
   const int32_t* k_begin;
   int heads, kv_heads, sequences, rows_q, rows_k, longest_q, longest_k;

@@ -11,8 +11,8 @@
 // dk and dv compute them the other way (queries x keys) for the same reason: a lane holds 16 queries of one key.  The second
 // product reads its other operand (v, k, dout, q) across its rows with transposing LDS reads.
 //
-// The gradient is two launches that share nothing but delta, and recompute S and dout v^T each (7 products instead of 5): one
-// that owns queries, for dq, and one that owns keys, for dk and dv.  So no gradient is added up by atomics, heads that share
+// The gradient has workgroups that own queries, for dq, and ones that own keys, for dk and dv, which share nothing but delta and
+// recompute S and dout v^T each (7 products instead of 5).  So no gradient is added up by atomics, heads that share
 // a key head are summed in registers, in order, and the results are the same bits every time.
 //
 // A tile is 64 rows of 128 bytes, its 16-byte pieces permuted within the row by bits 1..3 of the row number (`swizzle`): both the
@@ -206,13 +206,13 @@ __device__ __forceinline__ int first_query(const SeqArgs& a, const Sequence& s, 
 struct Dealt {
   int head, sequence, block;
 };
-__device__ __forceinline__ Dealt dealt(const SeqArgs& a, int heads, int blocks) {
+__device__ __forceinline__ Dealt dealt(const SeqArgs& a, int number, int heads, int blocks) {
   const int units = heads * a.sequences;
   if (a.causal) {
-    const int block = blockIdx.x / units, first = blockIdx.x % units, unit = heads % 8 ? (first + block) % units : first;
+    const int block = number / units, first = number % units, unit = heads % 8 ? (first + block) % units : first;
     return Dealt{unit % heads, unit / heads, block};
   }
-  const int n = units * blocks, xcd = blockIdx.x % 8, id = xcd * (n / 8) + min(xcd, n % 8) + blockIdx.x / 8, unit = id / blocks;
+  const int n = units * blocks, xcd = number % 8, id = xcd * (n / 8) + min(xcd, n % 8) + number / 8, unit = id / blocks;
   return Dealt{unit / a.sequences, unit % a.sequences, id % blocks};
 }
 
@@ -245,9 +245,9 @@ struct QueryBlock {
   int wg_least, tiles;
   bool any;
   template <int ROWS>
-  __device__ __forceinline__ static QueryBlock of(const SeqArgs& a, int blocks, int wave, int lane) {
+  __device__ __forceinline__ static QueryBlock of(const SeqArgs& a, int number, int blocks, int wave, int lane) {
     QueryBlock b;
-    const Dealt d = dealt(a, a.heads, blocks * a.parts);
+    const Dealt d = dealt(a, number, a.heads, blocks * a.parts);
     b.head = d.head;
     b.kv = b.head / (a.heads / a.kv_heads);
     b.s = sequence_of(a, d.sequence);
@@ -400,7 +400,7 @@ __global__ __launch_bounds__(64 * ROWS * SPLIT, ROWS * SPLIT == 4 ? 3 : 2) void 
   __shared__ int dirty[3][SPLIT];  // step + 1 with a cut tile that has values that are not finite
   const int lane = threadIdx.x % 64, h = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), split = wave / ROWS;
-  const QueryBlock b = QueryBlock::of<ROWS>(a, blocks, wave % ROWS, lane);
+  const QueryBlock b = QueryBlock::of<ROWS>(a, blockIdx.x, blocks, wave % ROWS, lane);
   if (!b.any) return;
   u32x4 qf[4];
 #pragma unroll
@@ -592,33 +592,23 @@ __global__ __launch_bounds__(64 * ROWS * SPLIT, ROWS * SPLIT == 4 ? 3 : 2) void 
   if (h == 0) a.lse[(int64_t)b.head * a.rows_q + b.s.q0 + b.row] = empty ? -kInf : ((ref == -kInf ? 0.0f : ref) + log2f(total)) * kLn2;
 }
 
-template <int ROWS, int SPLIT>
-__global__ __launch_bounds__(64 * ROWS * SPLIT, 2) void seq_grad_q_kernel(SeqArgs a, int blocks) {
-  constexpr int kWaves = ROWS * SPLIT;
-  __shared__ __align__(16) Buffers<SPLIT> lds;
-  __shared__ int dirty[3][SPLIT];
+// Workgroup `number` of those that own ROWS x 32 queries, a wave to every 32: g = sum of dS K with dS = P (dout V^T - delta).
+template <int ROWS>
+__device__ __forceinline__ void grad_q(const SeqArgs& a, int number, int blocks, Buffers<1>& lds) {
+  __shared__ int dirty[3][1];
   const int lane = threadIdx.x % 64, h = lane / 32;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), split = wave / ROWS;
-  const QueryBlock b = QueryBlock::of<ROWS>(a, blocks, wave % ROWS, lane);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const QueryBlock b = QueryBlock::of<ROWS>(a, number, blocks, wave, lane);
   if (!b.any) return;
   u32x4 qf[4], df[4];
-  float dot = 0.0f;
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
     qf[c] = *reinterpret_cast<const u32x4*>(b.at(a.q, lane) + 16 * c);
     df[c] = *reinterpret_cast<const u32x4*>(b.at(a.dout, lane) + 16 * c);
-    const u32x4 of = *reinterpret_cast<const u32x4*>(b.at(a.out, lane) + 16 * c);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      dot += __uint_as_float(df[c][e] << 16) * __uint_as_float(of[e] << 16);
-      dot += __uint_as_float(df[c][e] & 0xffff0000u) * __uint_as_float(of[e] & 0xffff0000u);
-    }
   }
-  const float delta = half_sum(dot);
   const int64_t at = (int64_t)b.head * a.rows_q + b.s.q0 + min(b.row, b.s.nq - 1);
-  const float lse2 = a.lse[at] * kLog2e;
-  if (h == 0 && split == 0 && b.part == 0 && b.row < b.s.nq) a.delta[at] = delta;
-  const Reader rd(lds[0][split][0], lane);
+  const float lse2 = a.lse[at] * kLog2e, delta = a.delta[at];
+  const Reader rd(lds[0][0][0], lane);
   const float c2 = a.scale * kLog2e;
   f32x16 g[2] = {};
   bool left_out = false;
@@ -657,8 +647,8 @@ __global__ __launch_bounds__(64 * ROWS * SPLIT, 2) void seq_grad_q_kernel(SeqArg
     ds[0] = (u32x4{packed[0], packed[1], packed[2], packed[3]});
     ds[1] = (u32x4{packed[4], packed[5], packed[6], packed[7]});
   };
-  over_keys<kWaves, SPLIT, 0>(
-      a, b, split, lds, dirty,
+  over_keys<ROWS, 1, 0>(
+      a, b, 0, lds, dirty,
       [&](int tile) {
         logits(tile, 0, x, y);
 #pragma unroll
@@ -736,22 +726,6 @@ __global__ __launch_bounds__(64 * ROWS * SPLIT, 2) void seq_grad_q_kernel(SeqArg
           else product(tile, kh, std::false_type{});
         }
       });
-  if constexpr (SPLIT > 1) {
-    Share* shares = reinterpret_cast<Share*>(lds);
-    static_assert(sizeof(Share) * ROWS * (SPLIT - 1) <= sizeof(lds));
-    __shared__ int left[kWaves];
-    __syncthreads();  // (the tiles' last use)
-    if (split > 0) {
-      shares[wave - ROWS].put(g, lane);
-      if (lane == 0) left[wave] = left_out;
-    }
-    __syncthreads();
-    if (split > 0) return;
-    for (int w = wave + ROWS; w < kWaves; w += ROWS) {
-      shares[w - ROWS].add_to(g, lane, 1.0f, 1.0f);
-      left_out |= left[w] != 0;
-    }
-  }
   if (left_out)
     add_not_finite(a.k.p + b.kv * a.k.sh + b.s.k0 * a.k.st, a.k.st, b.wave_least / 64 * 64, b.wave_most, lane, [&](int r) { return r < b.seen; }, g);
   if (b.row >= b.s.nq) return;
@@ -761,24 +735,22 @@ __global__ __launch_bounds__(64 * ROWS * SPLIT, 2) void seq_grad_q_kernel(SeqArg
 
 // ---- gradients of the keys and values -------------------------------------------------------------------------------
 
-// A workgroup: KEYS x 32 keys of one key head of one sequence, every 32 of them worked on by SPLIT waves, over the queries of all
+// Workgroup `number` of those that own KEYS x 32 keys of one key head of one sequence, a wave to every 32, over the queries of all
 // heads that share it: the tiles that the mask cuts first, those of all heads, then the others.
-template <int KEYS, int SPLIT>
-__global__ __launch_bounds__(64 * KEYS * SPLIT, 2) void seq_grad_kv_kernel(SeqArgs a, int blocks) {
-  constexpr int kWaves = KEYS * SPLIT;
-  __shared__ __align__(16) Buffers<SPLIT> lds;              // queries and dout
-  __shared__ __align__(16) float stats[3][SPLIT][2][64];    // [buffer][tile][-lse / scale, -delta]: where the products begin
-  __shared__ int dirty[3][SPLIT];
+template <int KEYS>
+__device__ __forceinline__ void grad_kv(const SeqArgs& a, int number, int blocks, Buffers<1>& lds) {  // lds: queries and dout
+  __shared__ __align__(16) float stats[3][2][64];  // [buffer][-lse / scale, -delta]: where the products begin
+  __shared__ int dirty[3];
   const int lane = threadIdx.x % 64, h = lane / 32;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), split = wave / KEYS;
-  const Dealt d = dealt(a, a.kv_heads, blocks * a.parts);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const Dealt d = dealt(a, number, a.kv_heads, blocks * a.parts);
   const int kv = d.head, part = d.block % a.parts;
   const Sequence s = sequence_of(a, d.sequence);
   const int key0 = d.block / a.parts * 32 * KEYS;
   if (key0 >= s.nk) return;
   const int rep = a.heads / a.kv_heads;
   // (columns behind the last key are copies of it that nobody writes)
-  const int end = s.nk - 1, key = key0 + wave % KEYS * 32 + lane % 32;
+  const int end = s.nk - 1, key = key0 + wave * 32 + lane % 32;
   u32x4 kf[4], vf[4];
   {
     const uint16_t* k = a.k.p + kv * a.k.sh + (int64_t)(s.k0 + min(key, end)) * a.k.st + 8 * h;
@@ -790,35 +762,35 @@ __global__ __launch_bounds__(64 * KEYS * SPLIT, 2) void seq_grad_kv_kernel(SeqAr
     }
   }
   const int from = first_query(a, s, min(key, end));  // queries that see the lane's key begin here
-  const int wave_from = first_query(a, s, min(key0 + wave % KEYS * 32, end));
+  const int wave_from = first_query(a, s, min(key0 + wave * 32, end));
   const int wg_from = first_query(a, s, key0), wg_all = first_query(a, s, min(key0 + 32 * KEYS - 1, end));
   const int first_tile = min(wg_from, s.nq) / 64, all_tile = min((wg_all + 63) / 64, (s.nq + 63) / 64), end_tile = (s.nq + 63) / 64;
   const int cut = max(0, all_tile - first_tile), uncut = max(0, end_tile - max(all_tile, first_tile));  // tiles of a head
-  const int step = SPLIT * a.parts, own = SPLIT * part;  // this workgroup's of either kind: step n + own + 0 .. SPLIT - 1
-  const int lead = max(0, cut * rep - own + step - 1) / step, steps = lead + max(0, uncut * rep - own + step - 1) / step;
+  // this workgroup's of either kind: a.parts n + part
+  const int lead = max(0, cut * rep - part + a.parts - 1) / a.parts, full = max(0, uncut * rep - part + a.parts - 1) / a.parts, steps = lead + full;
   struct Place {
     int head, row;  // row 0 of the tile; behind the last query where there is none
   };
-  auto place = [&](int n, int j) {
+  auto place = [&](int n) {
     const bool lead_part = n < lead;
-    const int at = step * (lead_part ? n : n - lead) + own + j, per_head = max(1, lead_part ? cut : uncut), i = at / per_head;
+    const int at = a.parts * (lead_part ? n : n - lead) + part, per_head = max(1, lead_part ? cut : uncut), i = at / per_head;
     return Place{kv * rep + min(i, rep - 1), i < rep ? 64 * ((lead_part ? first_tile : max(all_tile, first_tile)) + at % per_head) : s.nq};
   };
 
-  const Reader rd(lds[0][split][0], lane);
+  const Reader rd(lds[0][0][0], lane);
   const float c2 = a.scale * kLog2e, per_scale = -1.0f / a.scale;
   f32x16 dk[2] = {}, dv[2] = {};
   bool left_out = false;
-  Stage<64 * kWaves, SPLIT> sq, sd;
+  Stage<64 * KEYS, 1> sq, sd;
   float st_l = 0.0f, st_d = 0.0f;
-  if (threadIdx.x < 3 * SPLIT) (&dirty[0][0])[threadIdx.x] = 0;
+  if (threadIdx.x < 3) dirty[threadIdx.x] = 0;
   __syncthreads();
 
   f32x16 x, y;         // logits less lse (in units of the scale) and dout v^T - delta of the half whose turn it is
   u32x4 p[2], ds[2];   // of the one before
   u32x4 early[4];      // operands read a stretch ahead
-  const uint32_t begins = (uint32_t)(size_t)(lds_char*)(const char*)stats[0][split][0] + 16 * h;
-  constexpr int kStats = SPLIT * 2 * 64 * 4, kStep = SPLIT * 2 * kTileBytes;  // of a buffer
+  const uint32_t begins = (uint32_t)(size_t)(lds_char*)(const char*)stats[0][0] + 16 * h;
+  constexpr int kStats = 2 * 64 * 4, kStep = 2 * kTileBytes;  // of a buffer
   auto quarter = [&](f32x16& z, int tile, int which, int half, int i) {  // rows 8 i + 4 h .. of where a product begins
     const f32x4 v = *(lds_f32x4*)(begins + tile / kStep * kStats + which * 256 + half * 128 + i * 32);
 #pragma unroll
@@ -857,18 +829,13 @@ __global__ __launch_bounds__(64 * KEYS * SPLIT, 2) void seq_grad_kv_kernel(SeqAr
   };
   f32x16 u, w;  // of the next half
 
-  over_tiles<SPLIT>(
-      steps, lead, max(0, uncut * rep - (own + split) + step - 1) / step,
+  over_tiles<1>(
+      steps, lead, full,
       [&](int n) {
-#pragma unroll
-        for (int i = 0; i < sq.kPieces; ++i) {
-          const Place at = place(n, i * kWaves / 8);
-          const int row = at.row + (i * 8 * kWaves + (int)threadIdx.x / 8) % 64;
-          sq.load_piece(i, a.q.p + at.head * a.q.sh + s.q0 * a.q.st, a.q.st, row, s.nq);
-          sd.load_piece(i, a.dout.p + at.head * a.dout.sh + s.q0 * a.dout.st, a.dout.st, row, s.nq);
-        }
-        if (threadIdx.x < 64 * SPLIT) {
-          const Place at = place(n, wave);
+        const Place at = place(n);
+        sq.load(a.q.p + at.head * a.q.sh + s.q0 * a.q.st, a.q.st, at.row, s.nq);
+        sd.load(a.dout.p + at.head * a.dout.sh + s.q0 * a.dout.st, a.dout.st, at.row, s.nq);
+        if (threadIdx.x < 64) {
           const int i = at.row + lane;
           const int64_t in = (int64_t)at.head * a.rows_q + s.q0 + i;
           st_l = i < s.nq ? a.lse[in] * per_scale : -kInf;  // (rows behind the last query have no probability at all)
@@ -878,13 +845,11 @@ __global__ __launch_bounds__(64 * KEYS * SPLIT, 2) void seq_grad_kv_kernel(SeqAr
       [&](int n, int buf) {
         sq.store(lds[buf][0][0]);
         sd.store(lds[buf][0][1]);
-        if (threadIdx.x < 64 * SPLIT) {
-          stats[buf][wave][0][lane] = st_l;
-          stats[buf][wave][1][lane] = st_d;
+        if (threadIdx.x < 64) {
+          stats[buf][0][lane] = st_l;
+          stats[buf][1][lane] = st_d;
         }
-#pragma unroll
-        for (int j = 0; j < SPLIT; ++j)
-          if (n < lead && __any(sq.any_not_finite(j) || sd.any_not_finite(j))) dirty[buf][j] = n + 1;
+        if (n < lead && __any(sq.any_not_finite(0) || sd.any_not_finite(0))) dirty[buf] = n + 1;
       },
       [&](int tile) {
         begin(x, tile, 0, 0);
@@ -949,9 +914,9 @@ __global__ __launch_bounds__(64 * KEYS * SPLIT, 2) void seq_grad_kv_kernel(SeqAr
         for (int i = 0; i < 8; ++i) second_product(i, second_operand(tile, 1, i));
       },
       [&](int n, int tile, int buf) {
-        const int row = place(n, split).row;
+        const int row = place(n).row;
         if (row >= s.nq || row + 64 <= wave_from) return;
-        const bool clean_up = dirty[buf][split] == n + 1;
+        const bool clean_up = dirty[buf] == n + 1;
         left_out |= clean_up;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -981,24 +946,6 @@ __global__ __launch_bounds__(64 * KEYS * SPLIT, 2) void seq_grad_kv_kernel(SeqAr
           }
         }
       });
-  if constexpr (SPLIT > 1) {
-    Share* shares = reinterpret_cast<Share*>(lds);  // [wave of a later split][dk, dv]
-    static_assert(sizeof(Share) * 2 * KEYS * (SPLIT - 1) <= sizeof(lds));
-    __shared__ int left[kWaves];
-    __syncthreads();  // (the tiles' last use)
-    if (split > 0) {
-      shares[2 * (wave - KEYS)].put(dk, lane);
-      shares[2 * (wave - KEYS) + 1].put(dv, lane);
-      if (lane == 0) left[wave] = left_out;
-    }
-    __syncthreads();
-    if (split > 0) return;
-    for (int other = wave + KEYS; other < kWaves; other += KEYS) {
-      shares[2 * (other - KEYS)].add_to(dk, lane, 1.0f, 1.0f);
-      shares[2 * (other - KEYS) + 1].add_to(dv, lane, 1.0f, 1.0f);
-      left_out |= left[other] != 0;
-    }
-  }
   if (left_out) {
     for (int head = kv * rep; head < (kv + 1) * rep; ++head) {
       auto sees = [&](int r) { return r >= from; };
@@ -1016,6 +963,36 @@ __global__ __launch_bounds__(64 * KEYS * SPLIT, 2) void seq_grad_kv_kernel(SeqAr
   }
   write_columns(const_cast<uint16_t*>(a.dk.p) + kv * a.dk.sh + (int64_t)(s.k0 + key) * a.dk.st, dk, a.scale, h);
   write_columns(const_cast<uint16_t*>(a.dv.p) + kv * a.dv.sh + (int64_t)(s.k0 + key) * a.dv.st, dv, 1.0f, h);
+}
+
+// The gradients in one launch: the workgroups of the kind whose blocks take longer come first (k_first: the number of the first of the keys').
+// One launch behind the other ended twice with compute units that wait for the last blocks: us in two launches and in one, the
+// six-frame clip 620 and 578, of 12 heads 533 and 470, the eight frames 280 and 255, one frame 53 and 44.
+template <int BLOCK>
+__global__ __launch_bounds__(64 * BLOCK, 2) void seq_grad_kernel(SeqArgs k, SeqArgs q, int k_blocks, int q_blocks, int k_first, int k_workgroups) {
+  __shared__ __align__(16) Buffers<1> lds;
+  const int number = blockIdx.x - k_first;
+  if (number >= 0 && number < k_workgroups) grad_kv<BLOCK>(k, number, k_blocks, lds);
+  else grad_q<BLOCK>(q, k_first > 0 ? blockIdx.x : number - k_workgroups, q_blocks, lds);
+}
+
+// delta = sum of dout * out, which both need: 8 lanes a row, all rows of the tensors.
+__global__ __launch_bounds__(256) void delta_kernel(SeqArgs a) {
+  const int c = 8 * (threadIdx.x % 8);
+  for (int64_t at = (int64_t)blockIdx.x * 32 + threadIdx.x / 8; at < (int64_t)a.heads * a.rows_q; at += (int64_t)gridDim.x * 32) {
+    const int64_t head = at / a.rows_q, row = at % a.rows_q;
+    const u32x4 x = *reinterpret_cast<const u32x4*>(a.dout.p + head * a.dout.sh + row * a.dout.st + c);
+    const u32x4 y = *reinterpret_cast<const u32x4*>(a.out.p + head * a.out.sh + row * a.out.st + c);
+    float dot = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      dot += __uint_as_float(x[e] << 16) * __uint_as_float(y[e] << 16);
+      dot += __uint_as_float(x[e] & 0xffff0000u) * __uint_as_float(y[e] & 0xffff0000u);
+    }
+#pragma unroll
+    for (int i = 1; i < 8; i *= 2) dot += __shfl_xor(dot, i);
+    if (c == 0) a.delta[at] = dot;
+  }
 }
 
 // ---- joining the parts of small launches ------------------------------------------------------------------------------
@@ -1050,9 +1027,9 @@ __global__ __launch_bounds__(256) void join_out_kernel(SeqArgs a, int blocks) {
 
 // A gradient from the parts' sums: of the queries (KEYS = false), or of the keys and, behind them, the values.
 template <bool KEYS>
-__global__ __launch_bounds__(256) void join_grad_kernel(SeqArgs a, int blocks) {
+__device__ __forceinline__ void join_grad(const SeqArgs& a, int number, int blocks) {
   const int heads = KEYS ? a.kv_heads : a.heads, units = heads * a.sequences;
-  const int which = blockIdx.x / (units * blocks), at = blockIdx.x % (units * blocks);
+  const int which = number / (units * blocks), at = number % (units * blocks);
   const int unit = at / blocks, head = unit / a.sequences;
   const Sequence s = sequence_of(a, unit % a.sequences);
   const int i = at % blocks * kJoinRows + threadIdx.x / 8, c = 8 * (threadIdx.x % 8);
@@ -1072,99 +1049,121 @@ __global__ __launch_bounds__(256) void join_grad_kernel(SeqArgs a, int blocks) {
   const SeqRows& t = !KEYS ? a.dq : (which == 0 ? a.dk : a.dv);
   *reinterpret_cast<u32x4*>(const_cast<uint16_t*>(t.p) + head * t.sh + in_tensor * t.st + c) = w;
 }
+__global__ __launch_bounds__(256) void join_grad_kernel(SeqArgs k, SeqArgs q, int k_blocks, int q_blocks, int k_workgroups) {
+  const int number = blockIdx.x;
+  if (number < k_workgroups) join_grad<true>(k, number, k_blocks);
+  else join_grad<false>(q, number - k_workgroups, q_blocks);
+}
 
 long long grid_of(int longest, int rows, int heads, int sequences) { return ((long long)longest + rows - 1) / rows * heads * sequences; }
 
 constexpr long long kMostWorkgroups = (1ll << 32) / 512 - 1;  // threads of a launch are counted in 32 bits
 
-// How the blocks of 128 rows of a launch are worked on.  Four waves of 32 rows, two or three such workgroups to a compute unit, if there
+constexpr int kComputeUnits = 256, kMostParts = 8;
+// (the offsets of the sequences are device data: how many blocks of 128 rows there are is only estimated)
+long long blocks_of(const SeqArgs& a, long long rows, int heads) { return std::max<long long>({1, rows * heads / 128, (long long)heads * a.sequences}); }
+
+// How the forward pass's blocks of 128 rows are worked on.  Four waves of 32 rows, two or three such workgroups to a compute unit, if there
 // are blocks enough; else a second wave to every 32 rows, eight waves that fill a compute unit.  us with four and with eight waves,
-// forward, 16 heads: one frame of 1374 tokens (171 blocks) 24.0 and 21.2, 20 heads (214) 23.3 and 20.8, 24 heads (257) 32.8 and 39.4,
+// 16 heads: one frame of 1374 tokens (171 blocks) 24.0 and 21.2, 20 heads (214) 23.3 and 20.8, 24 heads (257) 32.8 and 39.4,
 // two frames (343) 34 and 40.  Under a mask blocks differ in length and the second round is shorter: causal, 2000 tokens (250) 32.7 and
 // 29.1, 3000 (375) 45.4 and 37.2.  Where even those leave compute units without work, several workgroups share the tiles of a block and a
 // second launch joins them: 4000 causal tokens of one head 44.5 alone, 28.9 with 2, 20.3 with 4, 17.5 with 8, four single tokens over up to
 // 4000 keys 45.7, 28.7, 20.3, 25.2; more of them than there are compute units gain nothing (one frame: 21.2 alone, 34.5 with 2).
-constexpr int kComputeUnits = 256, kMostParts = 8;
+// Under a mask and with many keys four waves and parts up to four workgroups to a compute unit even the blocks out better than eight
+// waves: the six-frame clip of 5 heads (322 blocks) 97 with eight waves, 133 with four, 84 with those and 3 parts, 16000 causal tokens of 4
+// heads (500 blocks) 177, 242 and, with 2 parts, 174.
 struct Shape {
   bool split;
   int parts;
 };
-Shape shape_of(const SeqArgs& a, long long rows, int heads, long long tiles) {
-  const long long blocks = std::max<long long>({1, rows * heads / 128, (long long)heads * a.sequences});
-  Shape s{blocks <= (a.causal ? 400 : kComputeUnits), 1};
-  if (s.split) s.parts = (int)std::max<long long>(1, std::min({(long long)kMostParts, kComputeUnits / blocks, tiles / 4}));
+Shape shape_of(const SeqArgs& a) {
+  const long long blocks = blocks_of(a, a.rows_q, a.heads), tiles = (a.longest_k + 63) / 64;
+  const bool uneven = a.causal && tiles > 64;
+  Shape s{!uneven && blocks <= (a.causal ? 400 : kComputeUnits), 1};
+  if (s.split || uneven)
+    s.parts = (int)std::max<long long>(1, std::min({(long long)kMostParts, kComputeUnits * (uneven ? 4 : 1) / blocks, tiles / 4}));
   return s;
 }
-Shape shape_q(const SeqArgs& a) { return shape_of(a, a.rows_q, a.heads, (a.longest_k + 63) / 64); }
-Shape shape_k(const SeqArgs& a) { return shape_of(a, a.rows_k, a.kv_heads, (long long)((a.longest_q + 63) / 64) * (a.heads / a.kv_heads)); }
 
-template <typename K>
-void launch_rows(K kernel, const SeqArgs& a, int longest, int heads, int rows, int threads, hipStream_t stream) {
-  const int blocks = (longest + rows - 1) / rows;
-  kernel<<<(int)(grid_of(longest, rows, heads, a.sequences) * a.parts), threads, 0, stream>>>(a, blocks);
+// And the gradient's.  A block whose work is more than twice a place's share (two workgroups to a compute unit; under a mask blocks have half
+// of what is counted here) is shared by workgroups, and a second launch joins what they leave: the key blocks of grouped heads above all.
+// us alone and so: ragged sequences of 12 heads that share 4 keys' 126 and 56, 8000 causal tokens of such heads 665 and 390, 4000 causal tokens of
+// one head 100 and 35.  More of them cost (one frame: 44 alone, 57 with blocks over one share in two).
+// Eight waves read every tile once for 256 rows, which long sequences gain (six-frame clip: 590 with four, 578 with eight, 20 heads 810
+// and 758, four sequences of 4000 490 and 451) and shorter ones lose by padding and unequal work (frames of 1374: 253 and 264; ragged, up to 2000: 120 and
+// 139; a few thousand: the same).
+struct GradShape {
+  int block;  // waves of 32 rows to a workgroup
+  int k_parts, q_parts;
+  bool q_first;  // the queries' workgroups
+};
+GradShape grad_shape_of(const SeqArgs& a) {
+  const long long k_tiles = (a.longest_k + 63) / 64, q_tiles = (a.longest_q + 63) / 64 * (long long)(a.heads / a.kv_heads);
+  const double k_work = 8.0 * q_tiles, q_work = 6.0 * k_tiles;  // of a block: products of 32 x 32 per tile and wave, four of them the unit
+  const double all = k_work * blocks_of(a, a.rows_k, a.kv_heads) + q_work * blocks_of(a, a.rows_q, a.heads);
+  const double share = all / (2 * kComputeUnits) / (a.causal ? 2 : 1);
+  // (an eighth is let go, so that blocks of just two shares are cut)
+  const auto parts = [&](double work, long long tiles) {
+    return (int)std::max<long long>(1, std::min({(long long)kMostParts, (long long)(1.125 * work / std::max(share, 1.0)), tiles / 4}));
+  };
+  GradShape s{4, parts(k_work, q_tiles), parts(q_work, k_tiles), false};
+  s.q_first = q_work / s.q_parts > k_work / s.k_parts;
+  if (std::min(a.rows_q, a.rows_k) / std::max(1, a.sequences) >= 3500) s.block = 8;
+  return s;
 }
 
 }  // namespace
 
 // (parts and their joins: at most kComputeUnits / 2 heads of sequences, far below what a launch can have)
 bool seq_attend_fits(const SeqArgs& a) {
-  return grid_of(a.longest_q, 128, a.heads, a.sequences) <= kMostWorkgroups && grid_of(a.longest_k, 128, a.kv_heads, a.sequences) <= kMostWorkgroups;
+  return grid_of(a.longest_q, 128, a.heads, a.sequences) + grid_of(a.longest_k, 128, a.kv_heads, a.sequences) <= kMostWorkgroups;
 }
 
 int64_t seq_attend_workspace(const SeqArgs& a) {
-  const int parts = shape_q(a).parts;
+  const int parts = shape_of(a).parts;
   return parts > 1 ? (int64_t)parts * a.heads * a.rows_q * (kD + 2) * (int64_t)sizeof(float) : 0;
 }
 int64_t seq_attend_grad_parts(const SeqArgs& a) {
-  const int64_t q = shape_q(a).parts, k = shape_k(a).parts;
-  return std::max(q > 1 ? q * a.heads * a.rows_q : 0, k > 1 ? 2 * k * a.kv_heads * a.rows_k : 0) * kD * (int64_t)sizeof(float);
+  const GradShape s = grad_shape_of(a);
+  return ((s.q_parts > 1 ? (int64_t)s.q_parts * a.heads * a.rows_q : 0) + (s.k_parts > 1 ? (int64_t)2 * s.k_parts * a.kv_heads * a.rows_k : 0)) * kD *
+         (int64_t)sizeof(float);
 }
 
 hipError_t launch_seq_attend(const SeqArgs& args, hipStream_t stream) {
   SeqArgs a = args;
-  if (grid_of(a.longest_q, 128, a.heads, a.sequences) == 0) return hipSuccess;
-  const Shape s = shape_q(a);
+  const Shape s = shape_of(a);
   a.parts = s.parts;
   a.part_sums = a.part + (int64_t)s.parts * a.heads * a.rows_q * kD;
-  if (s.split) launch_rows(seq_attend_kernel<4, 2>, a, a.longest_q, a.heads, 128, 512, stream);
-  else launch_rows(seq_attend_kernel<4, 1>, a, a.longest_q, a.heads, 128, 256, stream);
+  const int blocks = (a.longest_q + 127) / 128, workgroups = (int)(grid_of(a.longest_q, 128, a.heads, a.sequences) * s.parts);
+  if (workgroups == 0) return hipSuccess;
+  if (s.split) seq_attend_kernel<4, 2><<<workgroups, 512, 0, stream>>>(a, blocks);
+  else seq_attend_kernel<4, 1><<<workgroups, 256, 0, stream>>>(a, blocks);
   if (s.parts > 1) {
-    const int blocks = (a.longest_q + kJoinRows - 1) / kJoinRows;
-    join_out_kernel<<<blocks * a.heads * a.sequences, 256, 0, stream>>>(a, blocks);
+    const int joins = (a.longest_q + kJoinRows - 1) / kJoinRows;
+    join_out_kernel<<<joins * a.heads * a.sequences, 256, 0, stream>>>(a, joins);
   }
   return hipGetLastError();
 }
 
 hipError_t launch_seq_attend_grad(const SeqArgs& args, hipStream_t stream) {
-  SeqArgs a = args;
-  if (grid_of(a.longest_q, 128, a.heads, a.sequences) > 0) {
-    const Shape s = shape_q(a);
-    a.parts = s.parts;
-    if (s.split) launch_rows(seq_grad_q_kernel<4, 2>, a, a.longest_q, a.heads, 128, 512, stream);
-    else launch_rows(seq_grad_q_kernel<4, 1>, a, a.longest_q, a.heads, 128, 256, stream);
-    if (s.parts > 1) {
-      const int blocks = (a.longest_q + kJoinRows - 1) / kJoinRows;
-      join_grad_kernel<false><<<blocks * a.heads * a.sequences, 256, 0, stream>>>(a, blocks);
-    }
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  if (grid_of(a.longest_k, 128, a.kv_heads, a.sequences) > 0) {
-    const Shape s = shape_k(a);
-    a.parts = s.parts;
-    // eight waves read every tile of queries once for 256 keys, unless that pads the sequences more (six frames, 8244 keys: 363 and, in
-    // blocks of 128, 399 us; eight sequences of 1374: 169 and 162)
-    const auto padded = [&](int rows) { return ((long long)a.longest_k + rows - 1) / rows * rows; };
-    if (s.split) launch_rows(seq_grad_kv_kernel<4, 2>, a, a.longest_k, a.kv_heads, 128, 512, stream);
-    else if (20 * padded(128) <= 19 * padded(256)) launch_rows(seq_grad_kv_kernel<4, 1>, a, a.longest_k, a.kv_heads, 128, 256, stream);
-    else launch_rows(seq_grad_kv_kernel<8, 1>, a, a.longest_k, a.kv_heads, 256, 512, stream);
-    if (s.parts > 1) {
-      const int blocks = (a.longest_k + kJoinRows - 1) / kJoinRows;
-      join_grad_kernel<true><<<2 * blocks * a.kv_heads * a.sequences, 256, 0, stream>>>(a, blocks);
-    }
-    return hipGetLastError();
-  }
-  return hipSuccess;
+  const GradShape s = grad_shape_of(args);
+  SeqArgs k = args, q = args;
+  k.parts = s.k_parts;
+  q.parts = s.q_parts;
+  q.part += s.k_parts > 1 ? (int64_t)2 * s.k_parts * k.kv_heads * k.rows_k * kD : 0;
+  const int rows = 32 * s.block, k_blocks = (k.longest_k + rows - 1) / rows, q_blocks = (q.longest_q + rows - 1) / rows;
+  const int k_workgroups = k_blocks * k.kv_heads * k.sequences * k.parts, workgroups = k_workgroups + q_blocks * q.heads * q.sequences * q.parts;
+  if (workgroups == 0) return hipSuccess;
+  const int k_first = s.q_first ? workgroups - k_workgroups : 0;
+  const long long delta = std::min(((long long)q.heads * q.rows_q + 31) / 32, kMostWorkgroups);
+  if (delta > 0) delta_kernel<<<(int)delta, 256, 0, stream>>>(q);
+  if (s.block == 4) seq_grad_kernel<4><<<workgroups, 256, 0, stream>>>(k, q, k_blocks, q_blocks, k_first, k_workgroups);
+  else seq_grad_kernel<8><<<workgroups, 512, 0, stream>>>(k, q, k_blocks, q_blocks, k_first, k_workgroups);
+  const int k_rows = k.parts > 1 ? (k.longest_k + kJoinRows - 1) / kJoinRows : 0, q_rows = q.parts > 1 ? (q.longest_q + kJoinRows - 1) / kJoinRows : 0;
+  const int k_joins = 2 * k_rows * k.kv_heads * k.sequences, joins = k_joins + q_rows * q.heads * q.sequences;
+  if (joins > 0) join_grad_kernel<<<joins, 256, 0, stream>>>(k, q, k_rows, q_rows, k_joins);
+  return hipGetLastError();
 }
 
 }  // namespace xsv

@@ -110,6 +110,15 @@ def test_many_sequences_at_once(causal, n):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("lq,lk,heads,kv,causal", [([4500], [4500], 2, 1, 1), ([3600, 4100], [3600, 4203], 2, 2, 0), ([3521], [9000], 1, 1, 1500),
+                                                   ([7001], [3500], 1, 1, 1), ([5000], [5000], 4, 4, 1000)])
+def test_long_sequences(lq, lk, heads, kv, causal):
+    """Lengths at which the gradient takes blocks of 256 rows, and workgroups share the tiles of the forward pass and of both gradients."""
+    print(f"seq_attend {lq} {lk} heads={heads} causal={causal}", flush=True)
+    x = _inputs(lq, lk, heads, kv, seed=sum(lq) + causal, behind=5)
+    _check(*x, lq, lk, causal, 0.0, _run(*x, lq, lk, causal), heads=(heads - 1,) if kv == heads else None)
+
+
 def test_more_sequences_than_rows():
     """Nearly all of 3000 sequences empty, one long among them; and 700 of one to nine tokens."""
     lq = [0] * 2000 + [400] + [0] * 999
@@ -169,7 +178,7 @@ def test_offsets_outside_the_tensors_are_cut_off():
                 assert torch.equal(a, w)
 
 
-@pytest.mark.parametrize("n,at", [(300, 141), (1300, 700)])    # (the longer: workgroups share the tiles)
+@pytest.mark.parametrize("n,at", [(300, 141), (1300, 700), (3700, 1999)])  # (1300: workgroups share the tiles, 3700: blocks of 256 rows)
 @pytest.mark.parametrize("what", ["nan", "inf", "-inf"])
 def test_values_that_are_not_finite_stay_where_they_are_seen(what, n, at):
     """NaN and infinities in keys, values, queries and dout of a causal sequence, in tiles that the mask cuts: queries in front of
