@@ -6,7 +6,9 @@
 //   gradient:  g = R^T dy,  d weight = sum g * hat,  d bias = sum g,  u = g * weight,
 //              dx = (u - [layer] mean(u) - hat * mean(u * hat)) / sqrt(..)
 // Everything between the load and the one rounding of the result is fp32.  What bounds both is memory: 4 (6) bytes per
-// element against a few operations.
+// element against a few operations.  Measured: 40000 tokens of 40 heads (410 MB) 81 us, 5.1 TB/s; the gradient of 32976 tokens of 32 heads
+// (405 MB) 91 us and 5 us for the sums, 4.5 TB/s; a large copy reaches 4.8.  One frame of 1374 tokens takes 5 us, one token 2.6: a launch
+// and two waits for memory.
 //
 // A wave takes one token and eight of its heads at a time: 8 lanes hold a row, 16 bytes each, so that a load
 // instruction covers eight whole rows, the sums over a row are three steps among its lanes, and the 32 angles of the
@@ -294,8 +296,13 @@ __global__ __launch_bounds__(kSumColumns * kSumSlices) void rotate_grad_sum(cons
 
 int batches_of(int heads) { return (heads + kRowsAtOnce - 1) / kRowsAtOnce; }
 
-constexpr long long kManyUnits = 4096;  // waves with one batch each that no longer find a place at once
-
+// Batches of eight heads in a launch from which on a wave takes several of a token: their loads are in flight together and they share one
+// set of angles, but there are fewer waves.  us with one and with four, 32 heads in all: 1 token 2.6 and 4.2, 1000 (4000 batches) 4.1 and 6.0, 10000
+// (40000) 19.2 and 20.0, 32976 (131904) 56.5 and 48.9.  The gradient, with one and with two: 100 tokens 7.9 and 8.3, 500 (2000) 11.0 and
+// 9.8, 1000 14.8 and 12.0, 32976 101 and 94; it has each wave's sums to add up too.
+constexpr long long kManyUnits = 65536, kManyGradUnits = 1024;
+bool many_units(int n, int batches) { return (long long)n * batches > kManyUnits; }
+bool many_grad_units(int n, int batches) { return (long long)n * batches > kManyGradUnits; }
 
 #define XSV_ROTATE_CASES(KERNEL, AT_ONCE)                                                           \
   [&]() {                                                                                           \
@@ -314,9 +321,7 @@ constexpr long long kManyUnits = 4096;  // waves with one batch each that no lon
 
 hipError_t launch_rotate(const RotateArgs& a, int norm, int axes, bool interleaved, hipStream_t stream) {
   const int batches_q = batches_of(a.t[0].heads), batches = batches_q + batches_of(a.t[1].heads);
-  // four batches a wave (their loads in flight together, one set of angles) unless the launch is so small that one batch a
-  // wave still finds a place for every wave
-  const bool many = (long long)a.n * batches > kManyUnits;
+  const bool many = many_units(a.n, batches);
   const int at_once = many ? 4 : 1;
   const int units_per_token = (batches + at_once - 1) / at_once;
   const long long units = (long long)a.n * units_per_token;
@@ -328,14 +333,14 @@ hipError_t launch_rotate(const RotateArgs& a, int norm, int axes, bool interleav
 
 int rotate_grad_workgroups(int n, int heads_q, int heads_k) {
   const int batches = batches_of(heads_q) + batches_of(heads_k);
-  const bool many = (long long)n * batches > kManyUnits;
+  const bool many = many_grad_units(n, batches);
   const long long units = (long long)n * (many ? (batches + 1) / 2 : batches);
   return (int)std::min<long long>((units + kWaves - 1) / kWaves, 1024);
 }
 
 hipError_t launch_rotate_grad(const RotateArgs& a, int norm, int axes, bool interleaved, hipStream_t stream) {
   const int batches_q = batches_of(a.t[0].heads), batches = batches_q + batches_of(a.t[1].heads);
-  const bool many = (long long)a.n * batches > kManyUnits;
+  const bool many = many_grad_units(a.n, batches);
   const int at_once = many ? 2 : 1;
   const int units_per_token = (batches + at_once - 1) / at_once;
   const long long units = (long long)a.n * units_per_token;

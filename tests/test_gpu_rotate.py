@@ -93,6 +93,22 @@ def test_many_batches_of_heads_per_wave(n):
     _check_pair(q, k, _params(3, True), "layer", 1e-6, _positions(n, 2, "near", n), 10000.0, False)
 
 
+@pytest.mark.parametrize("n,heads,kv_heads", [(5001, 100, 5), (7000, 81, 0)])
+def test_launches_that_fill_the_chip_many_times(n, heads, kv_heads):
+    """Large enough for a wave to take several batches of heads in the forward pass too; 14 batches a token, and 11, of which the last is one head."""
+    q, k = _packed(n, [heads, max(kv_heads, 1)], seed=n)
+    w, pos = _params(n, True), _positions(n, 2, "near", n)
+    if kv_heads:
+        _check_pair(q, k, w, "layer", 1e-5, pos, 100.0, False)
+        return
+    y, none = xsv.norm_rotate(q, norm="rms", q_weight=w[0], positions=pos, interleaved=True)
+    rows = torch.arange(0, n, 97)
+    x64 = q[:, rows.to(DEV)].cpu().double()
+    want = plain.norm_rotate(x64, w[0].cpu().double(), None, "rms", 1e-5, pos.cpu()[rows], 100.0, True)
+    mag = plain.norm_rotate(x64, w[0].cpu().double(), None, "rms", 1e-5, None, 100.0, False).abs().amax(-1, keepdim=True)
+    assert none is None and bool(((y[:, rows.to(DEV)].cpu().double() - want).abs() <= HALF * want.abs() + FP32 * mag).all())
+
+
 def test_far_positions():
     """Positions over all of int32: angles of up to 2^31 radians."""
     q, k = _packed(64, [4, 4], 5)
