@@ -1,4 +1,4 @@
-// Host side of the stateless operators around the step: checks of arguments, then one or two launches on the caller's stream.
+// Host side of the stateless operators around the step: checks of arguments, then the launches, three at most, on the caller's stream.
 // Nothing here allocates, waits, keeps anything between calls or throws.
 #include "../../include/xsv.h"
 
@@ -39,7 +39,7 @@ RotateArgs rotate_args(const xsv_rotate_config& c) {
   a.eps = c.eps;
   a.n = c.n;
   const int half = c.axes ? kAngles / c.axes : 1;  // pairs of one axis
-  for (int i = 0; c.axes && i < kAngles; ++i) a.turns[i] = std::pow(c.base, -(double)(i % half) / half) / (2.0 * M_PI);
+  for (int i = 0; c.axes && i < kAngles; ++i) a.turns[i] = i < half ? std::pow(c.base, -(double)i / half) / (2.0 * M_PI) : a.turns[i - half];
   return a;
 }
 
