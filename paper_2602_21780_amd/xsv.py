@@ -294,13 +294,13 @@ class Context:
     def query_attend(self, layer, q, out=None, lse=None):
         """xsv_query_attend: q [H][rows][64] over the layer's cache, on the context's stream.  Returns (out, lse)."""
         H, d = self.cfg.n_heads, self.cfg.head_dim
-        _bf16(q, "q", (H, q.shape[1], d) if isinstance(q, torch.Tensor) and q.dim() == 3 else None)
+        tq = _tensor(q, "q", shape=(H, q.shape[1], d) if isinstance(q, torch.Tensor) and q.dim() == 3 else None)
         rows, dev = q.shape[1], q.device
         with _on(dev, self._stream):
             out = torch.empty((H, rows, d), dtype=torch.bfloat16, device=dev) if out is None else _plain(out, "out", torch.bfloat16, (H, rows, d), dev)
             lse = torch.empty((H, rows), dtype=torch.float32, device=dev) if lse is None else _plain(lse, "lse", torch.float32, (H, rows), dev)
             if rows:
-                _check(lib().xsv_query_attend(self._h, layer, _operand(q), rows, out.data_ptr(), lse.data_ptr()), "xsv_query_attend")
+                _check(lib().xsv_query_attend(self._h, layer, tq, rows, out.data_ptr(), lse.data_ptr()), "xsv_query_attend")
         return out, lse
 
     def score_prune(self, layer, q):
@@ -447,23 +447,23 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _bf16(t, name, shape=None):
-    """The checks that need the torch tensor; the library checks pointers, strides and sizes."""
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or t.dim() != 3 or not t.is_cuda:
+def _tensor(t, name, beside=None, shape=None, written=False):
+    """xsv_tensor of a bf16 device tensor [heads][rows][64], after the checks that need the torch tensor; the library checks pointers, strides
+    and sizes.  beside: a tensor of the call on whose device it has to be.  (Every torch attribute costs some 0.1 us: each is asked for once.)"""
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or t.dim() != 3 or not t.is_cuda:
         raise ValueError(f"{name}: expected a bf16 device tensor [heads][tokens][64]")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.shape[2] != 64 or (t.stride(2) != 1 and t.numel()):
+    size = t.shape
+    if shape is not None and size != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(size)}")
+    heads, rows, channels = size
+    sh, st, sc = t.stride()
+    if channels != 64 or (sc != 1 and heads and rows):
         raise ValueError(f"{name}: expected 64 contiguous channels")
-    return t
-
-
-def _operand(t):
-    """xsv_tensor of a tensor that _bf16 has seen, or of none.  (The strides of an axis of one entry mean nothing to the tensor and are free.)"""
-    if t is None:
-        return _NO_TENSOR
-    sh, st, _ = t.stride()
-    heads, rows, _ = t.shape
+    if beside is not None and t.get_device() != beside.get_device():
+        raise ValueError(f"all tensors of a call must be on one device: {name} on {t.device}, others on {beside.device}")
+    if written and ((heads > 1 and sh == 0) or (rows > 1 and st == 0)):
+        raise ValueError(f"{name}: an output must not be an expanded tensor")
+    # (the strides of an axis of one entry mean nothing to the tensor and are free)
     return xsv_tensor(t.data_ptr(), 0 if heads == 1 else sh, 64 if rows == 1 else st)
 
 
@@ -471,12 +471,6 @@ def _plain(t, name, dtype, shape, device):
     if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {device}")
     return t
-
-
-def _same_device(device, *tensors):
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"all tensors of a call must be on one device: {device} and {t.device}")
 
 
 class _on:
@@ -505,32 +499,32 @@ class _on:
             g.__exit__(*exc)
 
 
-def _like(out, name, x):
-    """The caller's output tensor, checked, or a new one."""
+def _output(out, name, x, new=torch.empty):
+    """The caller's output tensor, checked, or a new one like x, and its xsv_tensor."""
     if out is None:
-        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _bf16(out, name, x.shape)
-    if out.device != x.device:
-        raise ValueError(f"{name}: on {out.device}, the call's tensors on {x.device}")
-    heads, rows, _ = out.shape
-    if (heads > 1 and out.stride(0) == 0) or (rows > 1 and out.stride(1) == 0):
-        raise ValueError(f"{name}: an output must not be an expanded tensor")
-    return out
+        out = new(x.shape, dtype=torch.bfloat16, device=x.device)
+        return out, xsv_tensor(out.data_ptr(), out.stride(0), 64)
+    return out, _tensor(out, name, x, x.shape, written=True)
 
 
 def _workspace(size_of, cfg, device):
-    """A call's workspace, of the size that the library asks for."""
+    """A call's workspace, of the size that the library asks for (None: it asks for none), and that size."""
     nbytes = C.c_int64()
     _check(size_of(C.byref(cfg), C.byref(nbytes)), size_of.__name__)
-    return torch.empty(nbytes.value, dtype=torch.uint8, device=device)
+    n = nbytes.value
+    return (torch.empty(n, dtype=torch.uint8, device=device) if n else None), n
 
 
-def _rotate_config(q, k, norm, eps, weights, positions, base, interleaved):
+def _rotate_config(q, k, norm, eps, q_weight, q_bias, k_weight, k_bias, positions, base, interleaved):
     if norm not in NORMS:
         raise ValueError(f"norm must be one of {sorted(NORMS)}")
-    if k is not None and k.shape[1] != q.shape[1]:
-        raise ValueError("q and k must have the same number of tokens")
-    n, dev = q.shape[1], q.device
+    heads, n, _ = q.shape
+    heads_k = 0
+    if k is not None:
+        heads_k, n_k, _ = k.shape
+        if n_k != n:
+            raise ValueError("q and k must have the same number of tokens")
+    dev = q.device
     axes = 0
     if positions is not None:
         if positions.dim() == 1:
@@ -539,27 +533,25 @@ def _rotate_config(q, k, norm, eps, weights, positions, base, interleaved):
             raise ValueError("positions: expected int32 [tokens] or [tokens][1 or 2]")
         axes = positions.shape[1]
         _plain(positions, "positions", torch.int32, (n, axes), dev)
-    for name, w in zip(("q_weight", "q_bias", "k_weight", "k_bias"), weights):
+    for name, w in (("q_weight", q_weight), ("q_bias", q_bias), ("k_weight", k_weight), ("k_bias", k_bias)):
         if w is not None:
             _plain(w, name, torch.float32, (64,), dev)
-    return xsv_rotate_config(n, q.shape[0], 0 if k is None else k.shape[0], NORMS[norm], axes, int(bool(interleaved)), eps, base,
-                             _ptr(positions), *[_ptr(w) for w in weights])
+    return xsv_rotate_config(n, heads, heads_k, NORMS[norm], axes, int(bool(interleaved)), eps, base, _ptr(positions), _ptr(q_weight),
+                             _ptr(q_bias), _ptr(k_weight), _ptr(k_bias))
 
 
 def norm_rotate(q, k=None, *, norm="layer", eps=1e-5, q_weight=None, q_bias=None, k_weight=None, k_bias=None, positions=None,
                 base=100.0, interleaved=False, out=None, stream=None):
     """xsv_norm_rotate: norm per head, weight and bias (fp32 [64]) and rotation by `positions` (int32 [tokens] or [tokens][1 or 2];
     None: no rotation) of queries and, unless None, keys.  Returns (q_out, k_out), contiguous unless `out` gives the two."""
-    _bf16(q, "q")
-    if k is not None:
-        _bf16(k, "k")
-    _same_device(q.device, k)
-    cfg = _rotate_config(q, k, norm, eps, (q_weight, q_bias, k_weight, k_bias), positions, base, interleaved)
+    tq = _tensor(q, "q")
+    tk = _NO_TENSOR if k is None else _tensor(k, "k", q)
+    cfg = _rotate_config(q, k, norm, eps, q_weight, q_bias, k_weight, k_bias, positions, base, interleaved)
     q_out, k_out = out if out is not None else (None, None)
     with _on(q.device, stream) as s:
-        q_out = _like(q_out, "out[0]", q)
-        k_out = None if k is None else _like(k_out, "out[1]", k)
-        _check(lib().xsv_norm_rotate(s, C.byref(cfg), _operand(q), _operand(k), _operand(q_out), _operand(k_out)), "xsv_norm_rotate")
+        q_out, tq_out = _output(q_out, "out[0]", q)
+        k_out, tk_out = (None, _NO_TENSOR) if k is None else _output(k_out, "out[1]", k)
+        _check(lib().xsv_norm_rotate(s, C.byref(cfg), tq, tk, tq_out, tk_out), "xsv_norm_rotate")
     return q_out, k_out
 
 
@@ -567,31 +559,26 @@ def norm_rotate_grad(dq_out, dk_out, q, k=None, *, norm="layer", eps=1e-5, q_wei
                      positions=None, base=100.0, interleaved=False, out=None, weight_grads=True, stream=None):
     """xsv_norm_rotate_grad: (dq, dk, gradients of q_weight, q_bias, k_weight, k_bias as fp32 [4][64]) from the gradients of the
     outputs of norm_rotate and what it was called with.  weight_grads=False leaves the last out (None)."""
-    _bf16(q, "q")
-    _bf16(dq_out, "dq_out", q.shape)
+    tq = _tensor(q, "q")
+    tdq_out = _tensor(dq_out, "dq_out", q, q.shape)
+    tk = tdk_out = _NO_TENSOR
     if k is not None:
-        _bf16(k, "k")
-        _bf16(dk_out, "dk_out", k.shape)
-    _same_device(q.device, k, dq_out, dk_out if k is not None else None)
-    cfg = _rotate_config(q, k, norm, eps, (q_weight, q_bias, k_weight, k_bias), positions, base, interleaved)
+        tk, tdk_out = _tensor(k, "k", q), _tensor(dk_out, "dk_out", q, k.shape)
+    cfg = _rotate_config(q, k, norm, eps, q_weight, q_bias, k_weight, k_bias, positions, base, interleaved)
     dq, dk = out if out is not None else (None, None)
-    sums = work = None
+    sums, work, n_work = None, None, 0
     with _on(q.device, stream) as s:
-        dq = _like(dq, "out[0]", q)
-        dk = None if k is None else _like(dk, "out[1]", k)
+        dq, tdq = _output(dq, "out[0]", q)
+        dk, tdk = (None, _NO_TENSOR) if k is None else _output(dk, "out[1]", k)
         if weight_grads:
             sums = torch.empty((4, 64), dtype=torch.float32, device=q.device)
-            work = _workspace(lib().xsv_norm_rotate_grad_workspace, cfg, q.device)
-        _check(lib().xsv_norm_rotate_grad(s, C.byref(cfg), _operand(q), _operand(k), _operand(dq_out), _operand(None if k is None else dk_out),
-                                          _operand(dq), _operand(dk), _ptr(sums), _ptr(work), 0 if work is None else work.numel()), "xsv_norm_rotate_grad")
+            work, n_work = _workspace(lib().xsv_norm_rotate_grad_workspace, cfg, q.device)
+        _check(lib().xsv_norm_rotate_grad(s, C.byref(cfg), tq, tk, tdq_out, tdk_out, tdq, tdk, _ptr(sums), _ptr(work), n_work),
+               "xsv_norm_rotate_grad")
     return dq, dk, sums
 
 
-def _seq_config(q, k, v, q_begin, k_begin, longest_q, longest_k, causal, softmax_scale):
-    _bf16(q, "q")
-    _bf16(k, "k")
-    _bf16(v, "v", k.shape)
-    _same_device(q.device, k, v)
+def _seq_config(q, k, q_begin, k_begin, longest_q, longest_k, causal, softmax_scale):
     if k_begin is None:
         k_begin = q_begin
     n = q_begin.numel() - 1 if isinstance(q_begin, torch.Tensor) else -1
@@ -599,29 +586,26 @@ def _seq_config(q, k, v, q_begin, k_begin, longest_q, longest_k, causal, softmax
         raise ValueError("q_begin: expected int32 [sequences + 1]")
     for name, t in (("q_begin", q_begin), ("k_begin", k_begin)):
         _plain(t, name, torch.int32, (n + 1,), q.device)
-    rows_q, rows_k = q.shape[1], k.shape[1]
-    return xsv_seq_config(q.shape[0], k.shape[0], n, rows_q, rows_k, rows_q if longest_q is None else longest_q,
+    (heads, rows_q, _), (kv_heads, rows_k, _) = q.shape, k.shape
+    return xsv_seq_config(heads, kv_heads, n, rows_q, rows_k, rows_q if longest_q is None else longest_q,
                           rows_k if longest_k is None else longest_k, _ptr(q_begin), _ptr(k_begin), causal, softmax_scale)
-
-
-def _like_or_zeros(out, name, x):
-    """As _like, but a new tensor is zeros: rows in no sequence are not written."""
-    return torch.zeros(x.shape, dtype=x.dtype, device=x.device) if out is None else _like(out, name, x)
 
 
 def seq_attend(q, k, v, q_begin, k_begin=None, *, longest_q=None, longest_k=None, causal=0, softmax_scale=0.0, out=None, lse=None, stream=None):
     """xsv_seq_attend: attention of q [heads][rows][64] over k, v [kv_heads][rows][64] inside the sequences that the int32 device tensors
     q_begin and k_begin (None: the same) bound.  longest_q / longest_k, the lengths of the longest, size the launch (None: all rows).
     Returns (out, lse); tensors that it makes hold zeros in rows of no sequence."""
-    cfg = _seq_config(q, k, v, q_begin, k_begin, longest_q, longest_k, causal, softmax_scale)
+    tq, tk = _tensor(q, "q"), _tensor(k, "k", q)
+    tv = _tensor(v, "v", q, k.shape)
+    cfg = _seq_config(q, k, q_begin, k_begin, longest_q, longest_k, causal, softmax_scale)
     with _on(q.device, stream) as s:
-        out = _like_or_zeros(out, "out", q)
+        out, t_out = _output(out, "out", q, torch.zeros)
         if lse is None:
             lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=q.device)
-        _plain(lse, "lse", torch.float32, q.shape[:2], q.device)
-        work = _workspace(lib().xsv_seq_attend_workspace, cfg, q.device)
-        _check(lib().xsv_seq_attend(s, C.byref(cfg), _operand(q), _operand(k), _operand(v), _operand(out), _ptr(lse), _ptr(work), work.numel()),
-               "xsv_seq_attend")
+        else:
+            _plain(lse, "lse", torch.float32, q.shape[:2], q.device)
+        work, n_work = _workspace(lib().xsv_seq_attend_workspace, cfg, q.device)
+        _check(lib().xsv_seq_attend(s, C.byref(cfg), tq, tk, tv, t_out, lse.data_ptr(), _ptr(work), n_work), "xsv_seq_attend")
     return out, lse
 
 
@@ -629,17 +613,17 @@ def seq_attend_grad(dout, q, k, v, out, lse, q_begin, k_begin=None, *, longest_q
                     stream=None):
     """xsv_seq_attend_grad: (dq, dk, dv) from the gradient of seq_attend's out, what it was called with and what it returned.  `grads`
     gives the three tensors to write; those that it makes hold zeros in rows of no sequence."""
-    cfg = _seq_config(q, k, v, q_begin, k_begin, longest_q, longest_k, causal, softmax_scale)
-    _bf16(dout, "dout", q.shape)
-    _bf16(out, "out", q.shape)
-    _same_device(q.device, dout, out)
+    tq, tk = _tensor(q, "q"), _tensor(k, "k", q)
+    tv, tdout, t_out = _tensor(v, "v", q, k.shape), _tensor(dout, "dout", q, q.shape), _tensor(out, "out", q, q.shape)
+    cfg = _seq_config(q, k, q_begin, k_begin, longest_q, longest_k, causal, softmax_scale)
     _plain(lse, "lse", torch.float32, q.shape[:2], q.device)
     dq, dk, dv = grads if grads is not None else (None, None, None)
     with _on(q.device, stream) as s:
-        dq, dk, dv = _like_or_zeros(dq, "grads[0]", q), _like_or_zeros(dk, "grads[1]", k), _like_or_zeros(dv, "grads[2]", v)
-        work = _workspace(lib().xsv_seq_attend_grad_workspace, cfg, q.device)
-        _check(lib().xsv_seq_attend_grad(s, C.byref(cfg), _operand(q), _operand(k), _operand(v), _operand(out), _ptr(lse), _operand(dout),
-                                         _operand(dq), _operand(dk), _operand(dv), _ptr(work), work.numel()), "xsv_seq_attend_grad")
+        (dq, tdq), (dk, tdk) = _output(dq, "grads[0]", q, torch.zeros), _output(dk, "grads[1]", k, torch.zeros)
+        dv, tdv = _output(dv, "grads[2]", v, torch.zeros)
+        work, n_work = _workspace(lib().xsv_seq_attend_grad_workspace, cfg, q.device)
+        _check(lib().xsv_seq_attend_grad(s, C.byref(cfg), tq, tk, tv, t_out, lse.data_ptr(), tdout, tdq, tdk, tdv, _ptr(work), n_work),
+               "xsv_seq_attend_grad")
     return dq, dk, dv
 
 
