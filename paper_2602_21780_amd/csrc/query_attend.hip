@@ -5,7 +5,7 @@
 // It reads every packed byte once per block of query rows (0.625 bytes per element at 4 bits and groups of 64), and a few vector instructions per
 // element turn it into the same bf16 view that the rest of the library attends to.  Measured at 16 heads, one row over 65536 tokens: a bf16 cache
 // 43 us, which is 6.2 TB/s and the memory's bound (the cache fits the last-level one); 4 bits 29 us, 2.8 TB/s, and 2 bits 31 us: there the arithmetic
-// of the view bounds it, about 640 vector instructions per wave and 64 tokens, the vector units active in 72 % of the cycles.  A call of one
+// of the view bounds it, about 640 vector instructions per wave and 64 tokens, the vector units active in 79 % of the cycles.  A call of one
 // row over 4096 tokens takes 10.8 us: the launch, one tile for each wave, and the join of 16 parts, each a wait for memory.
 //
 // A wave takes 64 tokens at a time straight from memory into registers: keys as the A operand of 16x16x32 MFMAs (transposed
