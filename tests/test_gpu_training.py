@@ -130,3 +130,39 @@ def test_streaming_frames_through_norm_rotation_step_and_single_tokens():
             e = plain.Attention(qs[h].cpu().float(), view(after.k_bf16)[h], view(after.v_bf16)[h], 0, 0.125)
             assert bool(((one[h].cpu().double() - e.out).abs() <= e.out_tol).all()) and bool(((lse[h].cpu().double() - e.lse).abs() <= e.lse_tol).all())
     ctx.destroy()
+
+
+def test_offsets_that_pass_32_bits():
+    """Rows 2^24 channels apart, the largest stride there is: element offsets beyond 2^31 and byte offsets beyond 2^32 in every tensor."""
+    n, far = 300, 1 << 24
+    if torch.cuda.mem_get_info()[0] < 3 * n * far * 2:
+        pytest.skip("10 GB of device memory are not free")
+    whole = torch.empty((n, far), dtype=torch.bfloat16, device=DEV)
+    used = iter(range(0, far, 128))
+
+    def spread(t):  # [heads][n][64] into columns of their own
+        at = next(used)
+        place = whole.as_strided((t.shape[0], n, 64), (128, far, 1), at)
+        for _ in range(t.shape[0] - 1):
+            next(used)
+        place.copy_(t)
+        return place
+
+    g = torch.Generator().manual_seed(8)
+    make = lambda h: torch.randn((h, n, 64), generator=g).to(torch.bfloat16).to(DEV)
+    q, k, v, d = make(4), make(2), make(2), make(4)
+    pos = torch.arange(n, dtype=torch.int32, device=DEV)
+    begin = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    want = xsv.norm_rotate(q, k, positions=pos)
+    got = xsv.norm_rotate(spread(q), spread(k), positions=pos, out=(spread(torch.zeros_like(q)), spread(torch.zeros_like(k))))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    want = xsv.norm_rotate_grad(d, k, q, v, positions=pos)
+    got = xsv.norm_rotate_grad(spread(d), spread(k), spread(q), spread(v), positions=pos, out=(spread(torch.zeros_like(q)), spread(torch.zeros_like(k))))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    out, lse = xsv.seq_attend(q, k, v, begin, causal=1)
+    far_out, far_lse = xsv.seq_attend(spread(q), spread(k), spread(v), begin, causal=1, out=spread(torch.zeros_like(q)))
+    assert torch.equal(far_out, out) and torch.equal(far_lse, lse)
+    want = xsv.seq_attend_grad(d, q, k, v, out, lse, begin, causal=1)
+    got = xsv.seq_attend_grad(spread(d), spread(q), spread(k), spread(v), far_out, lse, begin, causal=1,
+                              grads=[spread(torch.zeros_like(t)) for t in (q, k, v)])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
