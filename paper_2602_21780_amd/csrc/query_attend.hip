@@ -15,7 +15,7 @@
 // 16 (R / 4) + 4 B + R % 4, which puts tokens 16 u .. into the accumulators of quarter u as well.
 //
 // The tokens are cut over the waves of a workgroup (joined in LDS) and over workgroups, so that few rows still use the whole chip;
-// the workgroup that ends last in a (head, row block), or with many rows a second launch, joins their partial results, in their order.
+// for a single row the workgroup of a head that ends last, else a second launch, joins their partial results, in their order.
 #include <algorithm>
 #include <type_traits>
 
@@ -34,10 +34,9 @@ constexpr int kWaves = 4;
 constexpr int kRows = kQueryRows;  // query rows of a column block
 constexpr int kJoinRows = 4;       // rows that are joined at a time, one a wave
 static_assert(kJoinRows == kWaves);
-// Up to so many rows are joined by the workgroup that ends last, one after the other; more by a second launch (16 heads over 4096 tokens: 2 rows 11.5
-// us inside, 4 rows inside 13.6 and by a launch 12.4; over 65536
-// tokens 4 rows inside 33.7 and by a launch 31.0; 16 rows over 20000: 36 and 17.5).
-constexpr int kRowsInside = 2;
+// A single row is joined by the workgroup that ends last, more rows by a second launch (16 heads, us inside and by a launch: one row over 300 tokens 7.5
+// and 10.6, over 4096 10.1 and 10.9; two rows over 4096 11.5 and 10.3; 4 rows over 65536 33.7 and 31.0; 16 rows over 20000: 36 and 17.5).
+constexpr int kRowsInside = 1;
 constexpr float kInf = __builtin_inff();
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -396,7 +395,7 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 3 : 2) void query_attend_ker
       }
     }
   }
-  if (a.splits == 1 || a.rows > kRowsInside) return;
+  if (QB > 1 || a.splits == 1 || a.rows > kRowsInside) return;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part has reached memory
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -409,7 +408,7 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 3 : 2) void query_attend_ker
   // (The fence lets the join read what other XCDs wrote with plain loads, all on their way at once: one after the other, as loads of
   // agent scope are issued, 64 parts took 40 us.)
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-  for (int r = 0; r < a.rows; ++r) join<1>(a, unit, head, row0, r, 1, kRows * QB, shares);
+  join<1>(a, unit, head, row0, 0, 1, kRows * QB, shares);
 }
 
 // The join of many rows, four to a workgroup.

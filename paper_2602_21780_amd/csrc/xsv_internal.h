@@ -103,7 +103,7 @@ struct Workspace {
                       // partial outputs, each block stored [16-byte piece 0..3][lane half][row] (4 KB)
   float* attn_ml;     // [pieces][batch layers][H][n][4]  softmax reference (log2 domain), row sum, row scale, -
   float* query_parts;      // partial results of query_attend, see QueryArgs
-  uint32_t* query_done;    // its counters, one per (head, row block) whose tokens are cut, zero between launches
+  uint32_t* query_done;    // its counters, one per head whose tokens are cut, zero between launches
   uint32_t* unit_done;  // [units of an attention launch] where the workgroups of a cut unit meet (attend.hip), zero between launches
   int scores_stride;  // Tcap + n
   int sets;           // lists per layer (CachePool::sets)
