@@ -275,7 +275,8 @@ typedef struct {
   int32_t heads, kv_heads;       /* 1 .. 65536, heads a multiple of kv_heads: head h reads key head h / (heads / kv_heads) */
   int32_t sequences;             /* >= 0                                                       */
   int32_t rows_q, rows_k;        /* rows of the tensors, >= 0                                  */
-  int32_t longest_q, longest_k;  /* bounds on the sequences' lengths (<= rows; they size the launch); rows behind them are left out */
+  int32_t longest_q, longest_k;  /* bounds on the sequences' lengths (<= rows; they size the launch).  A longer sequence's rows behind a
+                                    bound are left out of every result and not written; the others keep their positions */
   const int32_t* q_begin;        /* DEVICE [sequences + 1]                                     */
   const int32_t* k_begin;        /* DEVICE [sequences + 1]; may be q_begin                     */
   int32_t causal;                /* 0: every key of the sequence is seen.  b > 0: keys come in blocks of b (b = 1: token by token, b =

@@ -178,29 +178,32 @@ struct Stage {
 };
 
 struct Sequence {
-  int q0, nq, k0, nk;
+  int q0, nq, k0, nk;  // rows worked on: the bounds on the lengths leave those behind them out
+  int ahead;           // the key position of query 0, from the whole lengths: what a bound leaves out moves no other row
 };
 // Offsets are device data: whatever they hold, no row outside the tensors is touched.
 __device__ __forceinline__ Sequence sequence_of(const SeqArgs& a, int s) {
   Sequence r;
   r.q0 = min(max(a.q_begin[s], 0), a.rows_q);
-  r.nq = min(min(max(a.q_begin[s + 1], r.q0), a.rows_q) - r.q0, a.longest_q);
   r.k0 = min(max(a.k_begin[s], 0), a.rows_k);
-  r.nk = min(min(max(a.k_begin[s + 1], r.k0), a.rows_k) - r.k0, a.longest_k);
+  const int n = min(max(a.q_begin[s + 1], r.q0), a.rows_q) - r.q0, m = min(max(a.k_begin[s + 1], r.k0), a.rows_k) - r.k0;
+  r.nq = min(n, a.longest_q);
+  r.nk = min(m, a.longest_k);
+  r.ahead = m - n;
   return r;
 }
-// Query i of a sequence sees the keys in front of this one: query i stands at key position i + nk - nq, and sees the keys
+// Query i of a sequence sees the keys in front of this one: it stands at key position i + ahead, and sees the keys
 // up to the end of the block of `causal` keys that it stands in.
 __device__ __forceinline__ int keys_seen(const SeqArgs& a, const Sequence& s, int i) {
   if (a.causal == 0) return s.nk;
-  const int pos = i + s.nk - s.nq;
+  const int pos = i + s.ahead;
   if (pos < 0) return 0;
   return (int)min((int64_t)s.nk, ((int64_t)(pos / a.causal) + 1) * a.causal);
 }
-// ... and a key is seen by the queries from this one on.
+// ... and a key is seen by the queries from this one on (there may be none such within the bound).
 __device__ __forceinline__ int first_query(const SeqArgs& a, const Sequence& s, int key) {
   if (a.causal == 0) return 0;
-  return max(0, key / a.causal * a.causal - (s.nk - s.nq));
+  return max(0, key / a.causal * a.causal - s.ahead);
 }
 
 // Workgroups start in the order of their numbers and are dealt to the XCDs one by one.

@@ -347,3 +347,29 @@ def test_nothing_to_do():
     marks = [torch.full(t.shape, 2.0, dtype=t.dtype, device=DEV) for t in (none, k, v)]
     xsv.seq_attend_grad(none, none, k, v, out, lse, _begin([0]), _begin([9]), grads=marks)
     assert not marks[1].any() and not marks[2].any()
+
+
+@pytest.mark.parametrize("causal", [0, 1, 64, 150])
+@pytest.mark.parametrize("lq,lk,longest_q,longest_k", [([300, 20, 90], [300, 20, 90], 64, None), ([300, 20, 90], [300, 20, 90], None, 100),
+                                                       ([300, 90], [350, 200], 129, 130), ([40, 300], [33, 310], 31, 250), ([4500], [4600], 200, None),
+                                                       ([4500], [4600], None, 4200)])
+def test_bounds_below_a_sequences_length_leave_rows_out_and_move_no_other(lq, lk, longest_q, longest_k, causal, monkeypatch):
+    """The rows within the bounds keep their positions, and so what they see; those behind are in no result and not written."""
+    print(f"seq_attend {lq} {lk} bounds {longest_q} {longest_k} causal={causal}", flush=True)
+    q, k, v, d = _inputs(lq, lk, 2, 1, seed=sum(lq) + causal)
+    form = dict(q_begin=_begin(lq), k_begin=_begin(lk), causal=causal, longest_q=longest_q, longest_k=longest_k)
+    out, lse = xsv.seq_attend(q, k, v, **form)
+    grads = xsv.seq_attend_grad(d, q, k, v, out, lse, **form)
+    torch.cuda.synchronize()
+    whole_mask = plain.sees
+    a = b = 0
+    for n, m in zip(lq, lk):
+        kept_q, kept_k = min(n, longest_q or n), min(m, longest_k or m)
+        monkeypatch.setattr(plain, "sees", lambda _n, _m, c: whole_mask(n, m, c)[:_n, :_m])
+        at = lambda t, start, rows: t[:, start:start + rows]
+        kept = [at(t, a, kept_q) for t in (q, d, out, lse, grads[0])], [at(t, b, kept_k) for t in (k, v, *grads[1:])]
+        (kq, kd, ko, kl, kdq), (kk, kv, kdk, kdv) = kept
+        _check(kq, kk, kv, kd, [kept_q], [kept_k], causal, 0.0, (ko, kl, (kdq, kdk, kdv)))
+        for t, start, rows, length in ((out, a, kept_q, n), (lse, a, kept_q, n), (grads[0], a, kept_q, n), (grads[1], b, kept_k, m), (grads[2], b, kept_k, m)):
+            assert not t[:, start + rows:start + length].any()     # (as the binding made them)
+        a, b = a + n, b + m
