@@ -124,8 +124,9 @@ __device__ __forceinline__ u32x4 cleaned(u32x4 x) {
 }
 
 // Where a mask cuts a tile, a value that is not finite must not reach queries that do not see its row, but 0 * NaN does: the
-// second product of such a tile takes its finite values only, and behind the loop this adds the others, of rows [from, to), to
-// the columns (queries, or keys) that see their rows.  visible(row) is the lane's answer for its column.
+// second product of such a tile takes its finite values only, and this adds the others, of rows [from, to), to the columns (queries, or keys) that
+// see their rows: to outputs with each such tile, since waves and workgroups that share tiles weigh theirs in the join and a weight of 0 (a query that
+// sees no key of theirs) times infinity is NaN; to gradients, which are only added up, behind the loop.  visible(row) is the lane's answer for its column.
 template <typename F>
 __device__ __forceinline__ void add_not_finite(const uint16_t* base, int64_t st, int from, int to, int lane, F visible, f32x16* acc) {
 #pragma unroll 1
@@ -418,7 +419,6 @@ __global__ __launch_bounds__(64 * ROWS * SPLIT, ROWS * SPLIT == 4 ? 3 : 2) void 
   const float c2 = a.scale * kLog2e;
   f32x16 o[2] = {};
   float sum = 0.0f, ref = -kInf;  // ref in powers of two; -inf: no finite logit yet
-  bool left_out = false;          // values that are not finite are to be added
 
   auto logits = [&](int kt, int kh) {
     f32x16 z = {};
@@ -539,7 +539,6 @@ __global__ __launch_bounds__(64 * ROWS * SPLIT, ROWS * SPLIT == 4 ? 3 : 2) void 
       },
       [&](int tile) { product(tile + kTileBytes, 1, p, std::false_type{}); },
       [&](int t, int tile, bool clean_up) {
-        left_out |= clean_up;
 #pragma unroll
         for (int kh = 0; kh < 2; ++kh) {
           auto masked = [&]() {
@@ -562,18 +561,18 @@ __global__ __launch_bounds__(64 * ROWS * SPLIT, ROWS * SPLIT == 4 ? 3 : 2) void 
           if (clean_up) product(tile + kTileBytes, kh, p, std::true_type{});
           else product(tile + kTileBytes, kh, p, std::false_type{});
         }
+        if (clean_up)
+          add_not_finite(a.v.p + b.kv * a.v.sh + b.s.k0 * a.v.st, a.v.st, 64 * t, min(64 * t + 64, b.wave_most), lane, [&](int r) { return r < b.seen; }, o);
       });
   if constexpr (SPLIT > 1) {
     Share* shares = reinterpret_cast<Share*>(lds);
     static_assert(sizeof(Share) * ROWS * (SPLIT - 1) <= sizeof(lds));
     __shared__ float joint[2][kWaves][64];
-    __shared__ int left[kWaves];
     __syncthreads();  // (the tiles' last use)
     if (split > 0) {
       shares[wave - ROWS].put(o, lane);
       joint[0][wave][lane] = ref;
       joint[1][wave][lane] = sum;
-      if (lane == 0) left[wave] = left_out;
     }
     __syncthreads();
     if (split > 0) return;
@@ -583,11 +582,8 @@ __global__ __launch_bounds__(64 * ROWS * SPLIT, ROWS * SPLIT == 4 ? 3 : 2) void 
       ref = top;
       sum = sum * f + joint[1][w][lane] * g;
       shares[w - ROWS].add_to(o, lane, f, g);
-      left_out |= left[w] != 0;
     }
   }
-  if (left_out)
-    add_not_finite(a.v.p + b.kv * a.v.sh + b.s.k0 * a.v.st, a.v.st, b.wave_least / 64 * 64, b.wave_most, lane, [&](int r) { return r < b.seen; }, o);
   const float total = half_sum(sum);
   if (b.row >= b.s.nq) return;
   if (a.parts > 1) {

@@ -373,3 +373,22 @@ def test_bounds_below_a_sequences_length_leave_rows_out_and_move_no_other(lq, lk
         for t, start, rows, length in ((out, a, kept_q, n), (lse, a, kept_q, n), (grads[0], a, kept_q, n), (grads[1], b, kept_k, m), (grads[2], b, kept_k, m)):
             assert not t[:, start + rows:start + length].any()     # (as the binding made them)
         a, b = a + n, b + m
+
+
+@pytest.mark.parametrize("n", [300, 1300, 4300])  # (1300: waves share the tiles, 4300: workgroups do)
+@pytest.mark.parametrize("seen,later", [("inf", "nan"), ("inf", "-inf"), ("-inf", "inf"), ("nan", "inf")])
+def test_values_that_are_not_finite_in_neighbouring_tiles(seen, later, n):
+    """A row that a query sees, and one of the next tile that it does not, both in tiles that the mask cuts for the same wave: keys begin 40
+    in front of the queries, so that 32 queries end in two tiles."""
+    q, k, v, _ = [t.clone() for t in _inputs([n], [n + 40], 1, 1, seed=17)]
+    form = dict(q_begin=_begin([n]), k_begin=_begin([n + 40]), causal=1)
+    clean, clean_lse = xsv.seq_attend(q, k, v, **form)
+    first, second = 2 * 64 + 43, 3 * 64 + 2
+    v[0, first, 5], v[0, second, 5] = float(seen), float(later)
+    got, lse = xsv.seq_attend(q, k, v, **form)
+    assert torch.equal(lse, clean_lse)
+    rest = torch.arange(64, device=DEV) != 5
+    assert torch.equal(got[..., rest], clean[..., rest])
+    pos = torch.arange(n, device=DEV) + 40
+    want = torch.where(pos < first, clean[0, :, 5].float(), torch.where(pos < second, float(seen), float(seen) + float(later)))
+    assert torch.equal(got[0, :, 5].float().nan_to_num(nan=12345.0), want.nan_to_num(nan=12345.0))
