@@ -1120,9 +1120,18 @@ GradShape grad_shape_of(const SeqArgs& a) {
 
 }  // namespace
 
-// (parts and their joins: at most kComputeUnits / 2 heads of sequences, far below what a launch can have)
+// Whether every launch of the forward pass and of the gradient has threads that can be counted: without sharing, and with the workgroups that share blocks
+// and those that join them.
 bool seq_attend_fits(const SeqArgs& a) {
-  return grid_of(a.longest_q, 128, a.heads, a.sequences) + grid_of(a.longest_k, 128, a.kv_heads, a.sequences) <= kMostWorkgroups;
+  if (grid_of(a.longest_q, 128, a.heads, a.sequences) + grid_of(a.longest_k, 128, a.kv_heads, a.sequences) > kMostWorkgroups) return false;
+  const auto queries = [&](int rows) { return grid_of(a.longest_q, rows, a.heads, a.sequences); };
+  const auto keys = [&](int rows) { return grid_of(a.longest_k, rows, a.kv_heads, a.sequences); };
+  const auto fits = [](long long workgroups, int threads) { return workgroups < (1ll << 32) / threads; };
+  const Shape f = shape_of(a);
+  const GradShape g = grad_shape_of(a);
+  return fits(queries(128) * f.parts, f.split ? 512 : 256) && (f.parts == 1 || fits(queries(kJoinRows), 256)) &&
+         fits(queries(32 * g.block) * g.q_parts + keys(32 * g.block) * g.k_parts, 64 * g.block) &&
+         fits((g.q_parts > 1 ? queries(kJoinRows) : 0) + (g.k_parts > 1 ? 2 * keys(kJoinRows) : 0), 256);
 }
 
 int64_t seq_attend_workspace(const SeqArgs& a) {
