@@ -14,9 +14,9 @@ from . import xsv
 
 
 def _readable(g):
-    """A gradient as the library reads it: autograd also hands over expanded ones and any strides."""
-    fits = g.stride(2) == 1 and g.stride(0) % 8 == 0 and g.stride(1) % 8 == 0 and g.stride(1) >= 64 and g.data_ptr() % 16 == 0
-    return g if fits else g.contiguous()
+    """A gradient as the library reads it: autograd also hands over expanded ones, any strides and any place in another tensor."""
+    fits = g.stride(2) == 1 and g.stride(0) % 8 == 0 and g.stride(1) % 8 == 0 and 64 <= g.stride(1) <= 1 << 24 and g.data_ptr() % 16 == 0
+    return g if fits else g.clone(memory_format=torch.contiguous_format)  # (contiguous() gives back what is contiguous, aligned or not)
 
 
 class _NormRotate(torch.autograd.Function):

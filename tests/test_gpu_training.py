@@ -166,3 +166,23 @@ def test_offsets_that_pass_32_bits():
     got = xsv.seq_attend_grad(spread(d), spread(q), spread(k), spread(v), far_out, lse, begin, causal=1,
                               grads=[spread(torch.zeros_like(t)) for t in (q, k, v)])
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("at", [1, 4])
+def test_gradients_that_autograd_hands_over_misaligned(at):
+    """A contiguous gradient that begins inside another tensor, at an element that is not 16-byte aligned."""
+    n, heads = 50, 2
+    x, weights, positions = _layer(n, heads, heads, 7)
+    begin = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    q, k, v = (t.contiguous().requires_grad_() for t in x.transpose(0, 1).split(heads))
+    flat = torch.randn(heads * n * 64 + 8, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(DEV)
+    g = flat[at:at + heads * n * 64].view(heads, n, 64)
+    assert g.is_contiguous() and g.data_ptr() % 16 != 0
+    out, lse = autograd.seq_attend(q, k, v, begin)
+    got = torch.autograd.grad(out, (q, k, v), g)
+    want = xsv.seq_attend_grad(g.clone(), q.detach(), k.detach(), v.detach(), out.detach(), lse, begin)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    qr, kr = autograd.norm_rotate(q, k, positions=positions)
+    got = torch.autograd.grad((qr, kr), (q, k), (g, g))
+    want = xsv.norm_rotate_grad(g.clone(), g.clone(), q.detach(), k.detach(), positions=positions)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
