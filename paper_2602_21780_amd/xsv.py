@@ -188,9 +188,10 @@ class Context:
                  pool_size=16, softmax_scale=0.0, max_frames=0, stream=None, score_mode=0, value_mode=0):
         self.cfg = xsv_config(n_layers, n_heads, head_dim, tokens_per_frame, n_special, budget, kv_bits, group_size,
                               pool_size, score_mode, softmax_scale, max_frames, value_mode)
-        self._stream = stream
         self._h = C.c_void_p()
-        _check(lib().xsv_create(C.byref(self.cfg), _stream_ptr(stream), C.byref(self._h)), "xsv_create")
+        # (the library works on this stream whatever the current one is later, and so what a call allocates belongs to it)
+        self._stream = torch.cuda.current_stream() if stream is None else stream
+        _check(lib().xsv_create(C.byref(self.cfg), _stream_ptr(self._stream), C.byref(self._h)), "xsv_create")
 
     @classmethod
     def from_spec(cls, spec, stream=None, **over):
@@ -276,8 +277,9 @@ class Context:
 
     def _out(self, q, out):
         if out is None:
-            out = torch.empty((self.cfg.n_heads, self.cfg.tokens_per_frame, self.cfg.head_dim), dtype=torch.bfloat16,
-                              device=q.device)
+            with _on(q.device, self._stream):
+                out = torch.empty((self.cfg.n_heads, self.cfg.tokens_per_frame, self.cfg.head_dim), dtype=torch.bfloat16,
+                                  device=q.device)
         return out
 
     def dequant_attend(self, layer, q, k_new, v_new, out=None):
@@ -331,8 +333,9 @@ class Context:
     def step_all_layers(self, q=None, k_new=None, v_new=None, out=None, packed=None):
         if packed is None:
             if out is None:
-                out = torch.empty((self.cfg.n_layers, self.cfg.n_heads, self.cfg.tokens_per_frame, self.cfg.head_dim),
-                                  dtype=torch.bfloat16, device=q[0].device)
+                with _on(q[0].device, self._stream):
+                    out = torch.empty((self.cfg.n_layers, self.cfg.n_heads, self.cfg.tokens_per_frame, self.cfg.head_dim),
+                                      dtype=torch.bfloat16, device=q[0].device)
             packed = self.pack_layers(q, k_new, v_new, out)
         _check(lib().xsv_step_all_layers(self._h, *packed), "xsv_step_all_layers")
         return out

@@ -204,3 +204,25 @@ def test_refusals():
         ctx.query_attend(0, x, out=out)
     torch.cuda.synchronize()
     ctx.destroy()
+
+
+def test_a_context_called_under_another_stream_than_it_was_made_under():
+    """Outputs that the calls make come from the memory of the stream that they run on, not from a block that the current stream may still use."""
+    H, T, m = 4, 1000, 40
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        ctx = _filled(H, 100, T, 4, 64, seed=21)       # (no stream= of its own)
+    q, x = _queries(H, m, 3), _queries(H, 100, 4)
+    torch.cuda.synchronize()
+    held = [torch.empty((H, rows, 64), dtype=torch.bfloat16, device=DEV) for rows in (m, 100)] + [torch.empty((H, m), device=DEV)]
+    free = {t.data_ptr() for t in held}
+    del held                                           # the current stream's next blocks of these sizes
+    out, lse = ctx.query_attend(0, q)
+    step = ctx.step(0, x, x, x)
+    s.synchronize()
+    assert not {out.data_ptr(), lse.data_ptr(), step.data_ptr()} & free
+    same = _filled(H, 100, T, 4, 64, seed=21)
+    want, want_lse = same.query_attend(0, q)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse) and torch.equal(step, same.step(0, x, x, x))
+    ctx.destroy()
+    same.destroy()

@@ -125,3 +125,36 @@ def test_seq_attend_binding_refuses_what_is_not_a_bf16_device_tensor():
         xsv.seq_attend(host, host, host, begin)
     with pytest.raises(ValueError):
         xsv.seq_attend_grad(host, host, host, host, host, torch.zeros((2, 4)), begin)
+
+
+class _Stream:
+    cuda_stream, device = 1234, torch.device("cuda", 0)
+
+
+def test_what_a_contexts_calls_allocate_belongs_to_the_stream_it_was_made_on(monkeypatch):
+    """Without a stream= of its own a context keeps the one that is current when it is made; the library enqueues on that one later, too."""
+    made, entered = [], []
+
+    class Library:
+        xsv_create = staticmethod(lambda cfg, stream, handle: made.append(stream) or xsv.XSV_OK)
+
+    class Entered(Exception):
+        pass
+
+    def on(device, stream):
+        entered.append(stream)
+        raise Entered
+
+    monkeypatch.setattr(xsv, "lib", lambda: Library)
+    monkeypatch.setattr(xsv, "_on", on)
+    monkeypatch.setattr(xsv, "_tensor", lambda *a, **kw: None)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: _Stream)
+    ctx = xsv.Context(2, 2, 64, 8, 0, 0, 4, 64)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: None)
+    assert made == [1234]
+    x = torch.zeros((2, 8, 64), dtype=torch.bfloat16)
+    for call in (lambda: ctx.query_attend(0, x), lambda: ctx.step(0, x, x, x), lambda: ctx.frame_attend(x, x, x), lambda: ctx.dequant_attend(0, x, x, x),
+                 lambda: ctx.step_all_layers([x, x], [x, x], [x, x])):
+        with pytest.raises(Entered):
+            call()
+    assert entered == [_Stream] * 5
