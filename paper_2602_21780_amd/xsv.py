@@ -590,8 +590,12 @@ def _seq_config(q, k, q_begin, k_begin, longest_q, longest_k, causal, softmax_sc
     for name, t in (("q_begin", q_begin), ("k_begin", k_begin)):
         _plain(t, name, torch.int32, (n + 1,), q.device)
     (heads, rows_q, _), (kv_heads, rows_k, _) = q.shape, k.shape
-    return xsv_seq_config(heads, kv_heads, n, rows_q, rows_k, rows_q if longest_q is None else longest_q,
-                          rows_k if longest_k is None else longest_k, _ptr(q_begin), _ptr(k_begin), causal, softmax_scale)
+    longest_q = rows_q if longest_q is None else longest_q
+    longest_k = rows_k if longest_k is None else longest_k
+    # (ctypes cuts integers down to 32 bits, and rounds a scale to fp32: to 0, which would ask for the usual one)
+    if max(longest_q, longest_k, causal) >= 1 << 31 or min(longest_q, longest_k, causal) < -(1 << 31) or 0.0 < abs(softmax_scale) < 1e-40:
+        raise ValueError("longest_q, longest_k and causal must fit 32 bits, softmax_scale fp32")
+    return xsv_seq_config(heads, kv_heads, n, rows_q, rows_k, longest_q, longest_k, _ptr(q_begin), _ptr(k_begin), causal, softmax_scale)
 
 
 def seq_attend(q, k, v, q_begin, k_begin=None, *, longest_q=None, longest_k=None, causal=0, softmax_scale=0.0, out=None, lse=None, stream=None):

@@ -158,3 +158,14 @@ def test_what_a_contexts_calls_allocate_belongs_to_the_stream_it_was_made_on(mon
         with pytest.raises(Entered):
             call()
     assert entered == [_Stream] * 5
+
+
+@pytest.mark.parametrize("bad", [dict(longest_q=(1 << 32) + 5), dict(longest_k=(1 << 32) + 5), dict(causal=1 << 32), dict(causal=(1 << 32) + 1),
+                                 dict(causal=1 << 31), dict(softmax_scale=1e-60), dict(softmax_scale=-1e-60)])
+def test_seq_attend_binding_refuses_numbers_that_the_librarys_types_would_change(bad):
+    """Bounds and blocks of 2^32 and more would arrive as small ones, and a scale too small for fp32 as 0, which asks for the usual scale."""
+    x, begin = torch.zeros((2, 8, 64), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    good = dict(longest_q=None, longest_k=None, causal=1, softmax_scale=0.0)
+    assert xsv._seq_config(x, x, begin, None, **good).longest_q == 8
+    with pytest.raises(ValueError):
+        xsv._seq_config(x, x, begin, None, **{**good, **bad})
