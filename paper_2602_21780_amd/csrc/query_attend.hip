@@ -15,7 +15,7 @@
 // 16 (R / 4) + 4 B + R % 4, which puts tokens 16 u .. into the accumulators of quarter u as well.
 //
 // The tokens are cut over the waves of a workgroup (joined in LDS) and over workgroups, so that few rows still use the whole chip;
-// for a single row the workgroup of a head that ends last, else a second launch, joins their partial results, in their order.
+// the workgroup of a head that ends last, or a second launch, joins their partial results, in their order.
 #include <algorithm>
 #include <type_traits>
 
@@ -34,9 +34,15 @@ constexpr int kWaves = 4;
 constexpr int kRows = kQueryRows;  // query rows of a column block
 constexpr int kJoinRows = 4;       // rows that are joined at a time, one a wave
 static_assert(kJoinRows == kWaves);
-// A single row is joined by the workgroup that ends last, more rows by a second launch (16 heads, us inside and by a launch: one row over 300 tokens 7.5
-// and 10.6, over 4096 10.1 and 10.9; two rows over 4096 11.5 and 10.3; 4 rows over 65536 33.7 and 31.0; 16 rows over 20000: 36 and 17.5).
-constexpr int kRowsInside = 1;
+// A single row whose tokens are cut over a few workgroups is joined by the one that ends last in its head, others by a second launch: the parts, counters and
+// fence of many workgroups take longer than a launch.  us inside and by a launch, one row, groups of 64: one head over 300 tokens (2 workgroups in
+// all) 5.7 and 6.6, 16 heads over 300 (32) 6.5 and 6.8, over 1024 (64) 7.1 and 7.3, over 2048 (128) 8.2 and 7.1, over 4096 (256) 9.7 and 7.4, over 16384
+// (768) 17.7 and 11.7.  Two rows inside: 16 heads over 300 tokens 7.6 and 7.3, over 4096 10.9 and 7.3.
+constexpr int kInside = 64;
+__host__ __device__ bool joins_inside(const QueryArgs& a) { return a.rows == 1 && a.H * a.splits <= kInside; }
+// The second launch has a workgroup to a row, and where rows of all heads are many, to four: us with one and with four, 16 heads over 4096 tokens, 1 row
+// 7.4 and 8.7, 16 rows 8.1 and 9.4, 64 (1024 in all) 15.0 and 15.1, 200 28.1 and 26.6; one head over 65536, 1 row 9.8 and 15.6, 200 22.9 and 24.7.
+constexpr int kJoinApart = 1024;
 constexpr float kInf = __builtin_inff();
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -395,7 +401,7 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 3 : 2) void query_attend_ker
       }
     }
   }
-  if (QB > 1 || a.splits == 1 || a.rows > kRowsInside) return;
+  if (QB > 1 || a.splits == 1 || !joins_inside(a)) return;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part has reached memory
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -411,21 +417,23 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 3 : 2) void query_attend_ker
   join<1>(a, unit, head, row0, 0, 1, kRows * QB, shares);
 }
 
-// The join of many rows, four to a workgroup.
+// The join as a launch of its own, ROWS rows to a workgroup.
+template <int ROWS>
 __global__ __launch_bounds__(64 * kWaves) void query_join_kernel(QueryArgs a, int rows_wg) {
   __shared__ Shares shares;
-  const int groups = (a.rows + kJoinRows - 1) / kJoinRows, head = blockIdx.x / groups, row = blockIdx.x % groups * kJoinRows;
+  const int groups = (a.rows + ROWS - 1) / ROWS, head = blockIdx.x / groups, row = blockIdx.x % groups * ROWS;
   const int block = row / rows_wg, row0 = block * rows_wg;
-  join<kJoinRows>(a, head * a.blocks + block, head, row0, row - row0, min(kJoinRows, a.rows - row), rows_wg, shares);
+  join<ROWS>(a, head * a.blocks + block, head, row0, row - row0, min(ROWS, a.rows - row), rows_wg, shares);
 }
 
 template <int BITS, int G>
 hipError_t launch(const QueryArgs& a, hipStream_t stream) {
-  const int workgroups = a.H * a.blocks * a.splits;
+  const int workgroups = a.H * a.blocks * a.splits, rows_wg = a.rows <= kRows ? kRows : kQueryWide * kRows;
   if (a.rows <= kRows) query_attend_kernel<BITS, G, 1><<<workgroups, 64 * kWaves, 0, stream>>>(a);
   else query_attend_kernel<BITS, G, kQueryWide><<<workgroups, 64 * kWaves, 0, stream>>>(a);
-  if (a.splits > 1 && a.rows > kRowsInside)
-    query_join_kernel<<<a.H * ((a.rows + kJoinRows - 1) / kJoinRows), 64 * kWaves, 0, stream>>>(a, a.rows <= kRows ? kRows : kQueryWide * kRows);
+  if (a.splits == 1 || joins_inside(a)) return hipGetLastError();
+  if ((long long)a.H * a.rows <= kJoinApart) query_join_kernel<1><<<a.H * a.rows, 64 * kWaves, 0, stream>>>(a, rows_wg);
+  else query_join_kernel<kJoinRows><<<a.H * ((a.rows + kJoinRows - 1) / kJoinRows), 64 * kWaves, 0, stream>>>(a, rows_wg);
   return hipGetLastError();
 }
 

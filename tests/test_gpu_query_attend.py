@@ -226,3 +226,17 @@ def test_a_context_called_under_another_stream_than_it_was_made_under():
     assert torch.equal(out, want) and torch.equal(lse, want_lse) and torch.equal(step, same.step(0, x, x, x))
     ctx.destroy()
     same.destroy()
+
+
+@pytest.mark.parametrize("H,T,m", [(1, 300, 1), (16, 1024, 1), (16, 1090, 1), (16, 300, 2), (2, 5000, 3), (16, 500, 64), (16, 500, 65), (16, 1000, 71)])
+def test_every_way_of_joining_the_parts(H, T, m):
+    """Inside the launch and by a second one, a row to a workgroup and four, on both sides of where one takes over from the other; twice the same bits."""
+    print(f"query_attend joins H={H} T={T} m={m}", flush=True)
+    ctx = _filled(H, 60, T, 4, 64, seed=T + m)
+    q = _queries(H, m, m)
+    first = ctx.query_attend(0, q)
+    _compare(ctx, q, first, heads=(0, H - 1))
+    for _ in range(2):
+        for a, b in zip(first, ctx.query_attend(0, q)):
+            assert torch.equal(a, b)
+    ctx.destroy()
