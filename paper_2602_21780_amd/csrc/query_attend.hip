@@ -5,8 +5,10 @@
 // It reads every packed byte once per block of query rows (0.625 bytes per element at 4 bits and groups of 64), and a few vector instructions per
 // element turn it into the same bf16 view that the rest of the library attends to.  Measured at 16 heads, one row over 65536 tokens: a bf16 cache
 // 43 us, which is 6.2 TB/s and the memory's bound (the cache fits the last-level one); 4 bits 29 us, 2.8 TB/s, and 2 bits 31 us: there the arithmetic
-// of the view bounds it, about 640 vector instructions per wave and 64 tokens, the vector units active in 79 % of the cycles.  A call of one
-// row over 4096 tokens takes 10.8 us: the launch, one tile for each wave, and the join of 16 parts, each a wait for memory.
+// of the view bounds it, about 640 vector instructions per wave and 64 tokens, the vector units active in 79 % of the cycles.  One
+// row over 4096 tokens takes 7.5 us, call behind call: 4.6 for one tile for each wave and 3.1 for the launch that joins 16 parts, each a chain of waits
+// for memory.  17 to 64 rows share the view, but the workspace's parts cut their tokens over half of the workgroups that the chip holds: one
+// wave a SIMD, with nothing to hide its loads behind (64 rows over 20000 tokens 29 us).
 //
 // A wave takes 64 tokens at a time straight from memory into registers: keys as the A operand of 16x16x32 MFMAs (transposed
 // logits, a lane holds 16 tokens of one query), values, which the cache keeps transposed, as the A operand of the second
@@ -35,10 +37,11 @@ constexpr int kRows = kQueryRows;  // query rows of a column block
 constexpr int kJoinRows = 4;       // rows that are joined at a time, one a wave
 static_assert(kJoinRows == kWaves);
 // A single row whose tokens are cut over a few workgroups is joined by the one that ends last in its head, others by a second launch: the parts, counters and
-// fence of many workgroups take longer than a launch.  us inside and by a launch, one row, groups of 64: one head over 300 tokens (2 workgroups in
-// all) 5.7 and 6.6, 16 heads over 300 (32) 6.5 and 6.8, over 1024 (64) 7.1 and 7.3, over 2048 (128) 8.2 and 7.1, over 4096 (256) 9.7 and 7.4, over 16384
-// (768) 17.7 and 11.7.  Two rows inside: 16 heads over 300 tokens 7.6 and 7.3, over 4096 10.9 and 7.3.
-constexpr int kInside = 64;
+// fence of many workgroups take longer than a launch.  us on the GPU inside and by a launch, one row: one head over 300 tokens (2 workgroups in all) 5.7 and
+// 6.6, 16 heads over 300 (32) 6.5 and 6.8, over 1024 (64) 7.1 and 7.3, over 2048 (128) 8.2 and 7.1, over 4096 (256) 9.7 and 7.5, over 16384 (768) 17.7 and 12.4.
+// A launch also costs the host 2 us, which bounds the calls of single tokens from Python: over 4096 tokens 9.7 and 10.1 there, one head over 20000 (79)
+// 7.9 and 10.4; so up to a workgroup to each compute unit stays inside.  Two rows inside: 16 heads over 300 tokens 7.6 and 7.1, over 4096 10.9 and 7.4.
+constexpr int kInside = 256;
 __host__ __device__ bool joins_inside(const QueryArgs& a) { return a.rows == 1 && a.H * a.splits <= kInside; }
 // The second launch has a workgroup to a row, and where rows of all heads are many, to four: us with one and with four, 16 heads over 4096 tokens, 1 row
 // 7.4 and 8.7, 16 rows 8.1 and 9.4, 64 (1024 in all) 15.0 and 15.1, 200 28.1 and 26.6; one head over 65536, 1 row 9.8 and 15.6, 200 22.9 and 24.7.
@@ -439,7 +442,7 @@ hipError_t launch(const QueryArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-// Up to 16 rows one column block; more share the dequantized elements, 64 to a wave (20000 tokens: 16 rows 17.6 us, 17 rows 25, 64 rows 27, so
+// Up to 16 rows one column block; more share the dequantized elements, 64 to a wave (20000 tokens: 16 rows 14.7 us, 17 rows 25, 64 rows 29, so
 // two passes of 16 rows would already take longer).  As many workgroups as the chip holds at once, each with a tile for every wave, and no more partial
 // results than the workspace holds.
 bool plan_query(QueryArgs& a) {

@@ -228,7 +228,7 @@ def test_a_context_called_under_another_stream_than_it_was_made_under():
     same.destroy()
 
 
-@pytest.mark.parametrize("H,T,m", [(1, 300, 1), (16, 1024, 1), (16, 1090, 1), (16, 300, 2), (2, 5000, 3), (16, 500, 64), (16, 500, 65), (16, 1000, 71)])
+@pytest.mark.parametrize("H,T,m", [(1, 300, 1), (16, 1024, 1), (16, 1090, 1), (16, 4096, 1), (16, 4160, 1), (1, 20000, 1), (16, 300, 2), (2, 5000, 3), (16, 500, 64), (16, 500, 65), (16, 1000, 71)])
 def test_every_way_of_joining_the_parts(H, T, m):
     """Inside the launch and by a second one, a row to a workgroup and four, on both sides of where one takes over from the other; twice the same bits."""
     print(f"query_attend joins H={H} T={T} m={m}", flush=True)
