@@ -106,7 +106,9 @@ int xsv_frame_attend(xsv_ctx* ctx, xsv_tensor q, xsv_tensor k, xsv_tensor v, voi
  * touched; to be called between steps (not between the stages of one: XSV_ERR_STATE).  q: bf16 [H][rows][64] via strides, rows 0 .. 2^20 (0: nothing
  * is done).  out: DEVICE bf16 [H][rows][64] contiguous.  lse: DEVICE float [H][rows], log sum exp of the scaled logits (natural), with
  * which a caller can join this with attention over other keys; or NULL.  Over an empty cache out = 0 and lse = -inf.  In overlap mode 2 it
- * waits (on the stream) for the layer's outstanding chain. */
+ * waits (on the stream) for the layer's outstanding chain.  It only enqueues and may be captured into a HIP graph (in that
+ * mode after xsv_join).  A replay reads the buffer and the number of tokens that the layer's cache had at the capture, so it is for before the next
+ * step, import or reset; and it works in the context's workspace, so on the context's stream or ordered with it. */
 int xsv_query_attend(xsv_ctx* ctx, int layer, xsv_tensor q, int rows, void* out, float* lse);
 
 /* Sec. 3.2 after the append (T = T_cache + n).  If budget == 0, T <= budget, or this is the first
@@ -267,7 +269,7 @@ int xsv_norm_rotate_grad_workspace(const xsv_rotate_config* cfg, int64_t* bytes)
  *   S = scale q k^T over the keys a query sees,  lse = log sum exp(S) (natural),  out = exp(S - lse) v
  * Sequence s is rows [q_begin[s], q_begin[s + 1]) of q, out, dout, dq and rows [k_begin[s], k_begin[s + 1]) of k, v, dk, dv; the
  * offsets ascend and stay within the tensors (what does not is cut off: no row outside the tensors is touched).  Sequences may be empty
- * on either side.  Rows in no sequence are neither read nor written.  Query i of n stands at key position i + m - n of m: at the end of its
+ * on either side.  Rows in no sequence are in no result, whatever they hold, and not written.  Query i of n stands at key position i + m - n of m: at the end of its
  * sequence's keys, so that keys of earlier frames or tokens may lie in front.  A query that sees no key has out = 0 and lse = -inf, and
  * adds nothing to any gradient.  Values that are not finite in rows that a query does not see do not reach it, nor its gradient.  (Unnormalized sums are fp32:
  * values of 2^80 and more may overflow them.) */

@@ -6,9 +6,9 @@
 // element turn it into the same bf16 view that the rest of the library attends to.  Measured at 16 heads, one row over 65536 tokens: a bf16 cache
 // 43 us, which is 6.2 TB/s and the memory's bound (the cache fits the last-level one); 4 bits 29 us, 2.8 TB/s, and 2 bits 31 us: there the arithmetic
 // of the view bounds it, about 640 vector instructions per wave and 64 tokens, the vector units active in 79 % of the cycles.  One
-// row over 4096 tokens takes 7.5 us, call behind call: 4.6 for one tile for each wave and 3.1 for the launch that joins 16 parts, each a chain of waits
-// for memory.  17 to 64 rows share the view, but the workspace's parts cut their tokens over half of the workgroups that the chip holds: one
-// wave a SIMD, with nothing to hide its loads behind (64 rows over 20000 tokens 29 us).
+// row over 4096 tokens takes 9.8 us: the launch, one tile for each wave, 16 parts and their join, each a chain of waits for memory.  17 to 64 rows share
+// the view, but the workspace's parts cut their tokens over half of the workgroups that the chip holds: one wave a SIMD, with nothing to hide its loads
+// behind (64 rows over 20000 tokens 29 us).
 //
 // A wave takes 64 tokens at a time straight from memory into registers: keys as the A operand of 16x16x32 MFMAs (transposed
 // logits, a lane holds 16 tokens of one query), values, which the cache keeps transposed, as the A operand of the second

@@ -4,7 +4,8 @@
 //   dv = P^T dout,  dS = P (dout v^T - delta),  delta = sum_c dout out,  dq = scale dS k,  dk = scale dS^T q
 //
 // Everything is 32x32x16 MFMA products of tiles; logits, probabilities, sums and accumulators are fp32, and what enters a second
-// product (P, dS) is rounded to bf16 once, like the inputs.  The probabilities of the gradient are worked out again from lse.
+// product (P, dS) is rounded to bf16 once, like the inputs, since the products take bf16: outputs are off by 0.0020 to 0.0023 of themselves (rms) and
+// gradients by 0.0025, where the rounding of a result alone makes 0.0016.  The probabilities of the gradient are worked out again from lse.
 //
 // The forward pass and dq compute transposed logits (keys x queries): a lane then holds 16 keys of ONE query, sums over
 // keys stay in a lane, lse and delta are one register, and the packed result already is the operand of the second product.
@@ -18,11 +19,13 @@
 // A tile is 64 rows of 128 bytes, its 16-byte pieces permuted within the row by bits 1..3 of the row number (`swizzle`): both the
 // reads along rows (16 rows, one piece) and the transposing ones (4 rows, 4 pieces) then touch every bank once.
 //
-// What bounds it is the issue of MFMAs and vector arithmetic on a SIMD, which hardly overlap: per 32 x 32 logits the forward pass has 8
-// MFMAs of 32 cycles and 16 exponentials, 16 multiply-adds, 16 additions and 8 conversions (16 cycles the one, 4 the others); the gradient
-// 28 MFMAs and twice the exponentials.  Six frames of 1374 tokens, frame-causal, 16 heads: forward 210 us = 770 TFLOP/s, matrix pipe
-// busy 39 % of the cycles, vector units 63 %; gradient 576 us = 705 TFLOP/s of the 10 D operations a pair that it cannot do without, 48 % and 45 %.
-// Eight frames apart, gradient: 262 us = 590 TFLOP/s, 44 % and 45 %: keys and queries are padded to 1408, and 1408 workgroups of each kind end unevenly.
+// What it takes: per 32 x 32 logits the forward pass has 8 MFMAs of 32 cycles and 16 exponentials, 16 multiply-adds, 16 additions and 8
+// conversions (16 cycles the one, 4 the others), which overlap across the waves of a SIMD and hardly within one; the gradient 28 MFMAs and twice
+// the exponentials.  Besides, to fetch a tile takes 27 vector instructions a wave (13 in workgroups of eight), 12 of them integer multiplies of rows by strides,
+// beside some 120 of the softmax, and the waves of a workgroup meet at a barrier in every tile.  Neither unit is full: six frames of 1374 tokens,
+// frame-causal, 16 heads, forward 213 us = 760 TFLOP/s, matrix pipe busy 39 % of the cycles, vector units 63 %, where a loop of the bare mix at three waves
+// a SIMD would need some 120 to 140 us; gradient 587 us = 690 TFLOP/s of the 10 D operations a pair that it cannot do without, 48 % and 45 %.
+// Eight frames apart, gradient: 267 us = 580 TFLOP/s, 44 % and 45 %: keys and queries are padded to 1408, and 1408 workgroups of each kind end unevenly.
 #include "operators.h"
 
 #include <algorithm>
