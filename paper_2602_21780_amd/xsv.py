@@ -182,7 +182,8 @@ class CacheDump:
 
 
 class Context:
-    """Owner of an xsv_ctx.  Method names follow the C entry points."""
+    """Owner of an xsv_ctx.  Method names follow the C entry points.  Its calls run on `stream` (None: the one that is current when it is made),
+    whatever the current one is then, and outputs that they make belong to that stream."""
 
     def __init__(self, n_layers, n_heads, head_dim, tokens_per_frame, n_special, budget, kv_bits, group_size,
                  pool_size=16, softmax_scale=0.0, max_frames=0, stream=None, score_mode=0, value_mode=0):
