@@ -295,6 +295,66 @@ int xsv_seq_attend_grad(void* hip_stream, const xsv_seq_config* cfg, xsv_tensor 
                         xsv_tensor dout, xsv_tensor dq, xsv_tensor dk, xsv_tensor dv, void* workspace, int64_t workspace_bytes);
 int xsv_seq_attend_grad_workspace(const xsv_seq_config* cfg, int64_t* bytes);
 
+/* A cache in pages of 64 tokens, in 8 bits: one pool holds the whole histories of many sequences, which grow by any number of tokens and are
+ * read whole or by the pages that matter.  The caller owns the pool and says which page holds which tokens; entry j of a sequence's row of
+ * the table is the page of its tokens [64 j, 64 j + 64).  An entry that is no page of the pool (-1) holds nothing: its tokens are seen by
+ * nobody, are not written and not read.
+ *   Of a page and key head, keys and values each:  scale = 2^e, the smallest e in -100 .. 120 with 448 2^e >= max |x| over the finite elements;
+ *   code = x / scale to the nearest e4m3 number (ties to even), NaN where x is not finite;  a code stands for code * scale.
+ * All calls take the lengths that the sequences have with the call's own rows: row i of the n rows [begin[s], begin[s + 1]) of sequence s
+ * stands at token i + lengths[s] - n of it (a row in front of its first token is not written, not read, and sees nothing).  What begin and lengths hold is
+ * cut off at the tensors' rows and the table's width: nothing outside them is touched.  Rows of no sequence are not written. */
+typedef struct {
+  int32_t pages;            /* of the pool, >= 0                                               */
+  int32_t kv_heads;         /* 1 .. 65536                                                      */
+  void* k;                  /* DEVICE e4m3 [pages][kv_heads][64 tokens][64 channels], 16-byte aligned    */
+  void* v;                  /* DEVICE e4m3 [pages][kv_heads][64 channels][64 tokens], 16-byte aligned    */
+  float* k_scale;           /* DEVICE [pages][kv_heads]                                        */
+  float* v_scale;           /* DEVICE [pages][kv_heads]                                        */
+  void* k_bounds;           /* DEVICE fp16 [pages][kv_heads][2][64], 16-byte aligned: of every channel, twice the largest and the smallest
+                               code of the page's tokens, rounded up and down to whole numbers.  For xsv_pages_select; NULL without it */
+  int32_t sequences;        /* >= 0                                                            */
+  int32_t table_width;      /* 0 .. 2^24                                                       */
+  const int32_t* table;     /* DEVICE [sequences][table_width]                                 */
+  const int32_t* lengths;   /* DEVICE [sequences], tokens                                      */
+} xsv_pages;
+/* Writes rows of k and v, bf16 [kv_heads][rows][64] via strides, behind what the sequences hold.  begin: DEVICE [sequences + 1], ascending.
+ * longest: a bound on a sequence's rows (<= rows; it sizes the launch; rows behind it are not written).  Where a page already holds tokens
+ * its scale becomes the larger of its own and that of the new rows, and codes that are there are rounded anew, code 2^(e old - e new), which changes
+ * only codes below 2^-6; its bounds become those of all its tokens.  Places behind the last token of a page that the call begins are
+ * cleared, in other pages they stay.  Pages that a call writes into must be in one place of the table only; others may be shared. */
+int xsv_pages_write(void* hip_stream, const xsv_pages* pages, const int32_t* begin, int rows, int longest, xsv_tensor k, xsv_tensor v);
+/* The other way round: what the sequences' last rows stand for, exact in bf16, into k and v. */
+int xsv_pages_read(void* hip_stream, const xsv_pages* pages, const int32_t* begin, int rows, int longest, xsv_tensor k, xsv_tensor v);
+
+typedef struct {
+  int32_t heads;                 /* 1 .. 65536, a multiple of kv_heads: head h reads key head h / (heads / kv_heads) */
+  int32_t rows;                  /* of q, >= 0                                                 */
+  int32_t longest_q, longest_k;  /* bounds on the sequences' rows (<= rows) and tokens (>= 0); they size the launch.  Rows and tokens behind a bound
+                                    are left out of every result; the others keep their positions */
+  const int32_t* q_begin;        /* DEVICE [sequences + 1]                                     */
+  int32_t causal;                /* as in xsv_seq_config                                       */
+  float softmax_scale;           /* 0 -> 1/sqrt(64), else 1e-20 .. 1e20                        */
+  const int32_t* chosen;         /* DEVICE [rows][kv_heads][count] or NULL; xsv_pages_attend only */
+  int32_t count;                 /* 0 .. 2^24                                                  */
+  int32_t first, last;           /* >= 0; xsv_pages_select only                                */
+} xsv_pages_query;
+/* S = scale q k^T over the tokens that a row sees, lse = log sum exp(S) (natural), out = exp(S - lse) v, as xsv_seq_attend with the sequences'
+ * tokens as keys.  With `chosen` (and count > 0) row r of key head g sees only tokens of the pages chosen[r][g][..], each a number of
+ * a page of its sequence (entry of its row of the table), in any order; what is none, or none that it sees a token of, is left out, and a page
+ * that is listed twice counts twice.  A row that sees no token has out = 0 and lse = -inf.  A NaN reaches exactly the rows that see its token.  q, out: bf16 [heads][rows][64]
+ * via strides; lse: float [heads][rows].  The same bits every time. */
+int xsv_pages_attend(void* hip_stream, const xsv_pages* pages, const xsv_pages_query* cfg, xsv_tensor q, xsv_tensor out, float* lse, void* workspace,
+                     int64_t workspace_bytes);
+int xsv_pages_attend_workspace(const xsv_pages* pages, const xsv_pages_query* cfg, int64_t* bytes);
+/* For every row and key head, which of the n pages that hold a token it sees to look at, for xsv_pages_attend: the first `first` and the last `last` of them
+ * and of the others those with the largest scores, equal ones in order, `count` in all (>= first + last, >= 1); fewer if there are no more.
+ *   score_j = max over the key head's heads of 2^clamp(t + e_j - 1, -100, 100) sum_c max(q'_c hi_c, q'_c lo_c),
+ *   q' = q / 2^t rounded to whole numbers (ties to even; 0 where q is not finite),  t = floor(log2 max(|q|, 2^-119)) - 7,  hi, lo and e the keys' bounds and scale
+ * of page j: an upper bound of the largest logit (unscaled) but for the rounding of q, in whole numbers that fp32 holds exactly, so that the choice does not
+ * depend on the order of sums.  chosen: DEVICE [rows][kv_heads][count], ascending, -1 behind the last.  At most 32768 pages (longest_k <= 2^21). */
+int xsv_pages_select(void* hip_stream, const xsv_pages* pages, const xsv_pages_query* cfg, xsv_tensor q, int32_t* chosen);
+
 const char* xsv_strerror(int code);
 
 #ifdef __cplusplus

@@ -29,6 +29,9 @@ SOURCES = {
     # (MFMA results in VGPRs, as above)
     "query_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "seq_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "pages.hip": [],
+    "pages_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "pages_select.hip": [],
 }
 
 

@@ -56,4 +56,37 @@ hipError_t launch_seq_attend(const SeqArgs& a, hipStream_t stream);
 hipError_t launch_seq_attend_grad(const SeqArgs& a, hipStream_t stream);
 bool seq_attend_fits(const SeqArgs& a);  // its grids stay within what a launch can have
 
+// A pool of pages in 8 bits, the sequences that it holds, and the rows that a call writes, reads or asks with.
+struct PagesArgs {
+  uint8_t* k;         // [pages][kv_heads][64 tokens][64 channels]
+  uint8_t* v;         // [pages][kv_heads][64 channels][64 tokens]
+  float* k_scale;     // [pages][kv_heads]
+  float* v_scale;
+  uint16_t* bounds;   // fp16 [pages][kv_heads][2][64]
+  const int32_t* table;
+  const int32_t* lengths;
+  const int32_t* begin;
+  int pages, kv_heads, sequences, width;
+  int rows, longest, longest_k;  // of `begin`; bounds on a sequence's rows and tokens: those behind them are left out
+  SeqRows keys, values;          // written or read
+  SeqRows q, out;
+  float* lse;                    // [heads][rows]
+  int heads, causal;
+  float scale;
+  const int32_t* chosen;         // [rows][kv_heads][count]; null: all pages
+  int32_t* choice;               // the same, written
+  int count, first, last;
+  float* part;                   // attention cut over workgroups: what each leaves, [part][head][row][64]
+  float* part_sums;              // and its reference and sum, [part][head][row][2]
+  int parts, chunk;              // how many share a block of rows, pages for each (set by the launchers)
+};
+hipError_t launch_pages_write(const PagesArgs& a, hipStream_t stream);
+hipError_t launch_pages_read(const PagesArgs& a, hipStream_t stream);
+hipError_t launch_pages_attend(const PagesArgs& a, hipStream_t stream);
+hipError_t launch_pages_select(const PagesArgs& a, hipStream_t stream);
+int64_t pages_attend_workspace(const PagesArgs& a);  // bytes of PagesArgs::part
+bool pages_move_fits(const PagesArgs& a);            // their grids stay within what a launch can have
+bool pages_attend_fits(const PagesArgs& a);
+bool pages_select_fits(const PagesArgs& a);
+
 }  // namespace xsv

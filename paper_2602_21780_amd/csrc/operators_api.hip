@@ -2,6 +2,7 @@
 // Nothing here allocates, waits, keeps anything between calls or throws.
 #include "../../include/xsv.h"
 
+#include <algorithm>
 #include <cmath>
 
 #include "operators.h"
@@ -62,11 +63,64 @@ SeqArgs seq_args(const xsv_seq_config& c) {
   return a;
 }
 
+bool check_pages(const xsv_pages* p) {
+  if (!p || p->pages < 0 || p->kv_heads < 1 || p->sequences < 0 || p->table_width < 0) return false;
+  if (p->pages > 0 && (!p->k || !p->v || !p->k_scale || !p->v_scale)) return false;
+  if (!aligned_to(p->k, 16) || !aligned_to(p->v, 16) || !aligned_to(p->k_bounds, 16) || !aligned_to(p->k_scale, 4) || !aligned_to(p->v_scale, 4)) return false;
+  if (p->sequences > 0 && (!p->lengths || (p->table_width > 0 && !p->table))) return false;
+  return aligned_to(p->table, 4) && aligned_to(p->lengths, 4);
+}
+bool pages_supported(const xsv_pages& p) { return p.kv_heads <= (1 << 16) && p.table_width <= (1 << 24); }
+
+PagesArgs pages_args(const xsv_pages& p) {
+  PagesArgs a{};
+  a.k = static_cast<uint8_t*>(p.k); a.v = static_cast<uint8_t*>(p.v);
+  a.k_scale = p.k_scale; a.v_scale = p.v_scale;
+  a.bounds = static_cast<uint16_t*>(p.k_bounds);
+  a.table = p.table; a.lengths = p.lengths;
+  a.pages = p.pages; a.kv_heads = p.kv_heads; a.sequences = p.sequences; a.width = p.table_width;
+  a.longest_k = 1 << 30;  // (the most that a table holds)
+  return a;
+}
+
+int check_query(const xsv_pages* p, const xsv_pages_query* c) {
+  if (!check_pages(p) || !c || c->heads < 1 || c->heads % p->kv_heads != 0 || c->rows < 0 || c->longest_q < 0 || c->longest_q > c->rows || c->longest_k < 0)
+    return XSV_ERR_ARG;
+  if (c->causal < 0 || c->count < 0 || c->first < 0 || c->last < 0) return XSV_ERR_ARG;
+  if (c->softmax_scale != 0.0f && !(c->softmax_scale >= 1e-20f && c->softmax_scale <= 1e20f)) return XSV_ERR_ARG;
+  if (!aligned_to(c->q_begin, 4) || !aligned_to(c->chosen, 4) || (p->sequences > 0 && !c->q_begin)) return XSV_ERR_ARG;
+  if (!pages_supported(*p) || c->heads > (1 << 16) || c->count > (1 << 24)) return XSV_ERR_UNSUPPORTED;
+  return XSV_OK;
+}
+
+PagesArgs query_args(const xsv_pages& p, const xsv_pages_query& c) {
+  PagesArgs a = pages_args(p);
+  a.begin = c.q_begin;
+  a.rows = c.rows; a.longest = c.longest_q;
+  a.longest_k = std::min(c.longest_k, p.table_width * 64);
+  a.heads = c.heads; a.causal = c.causal;
+  a.scale = c.softmax_scale == 0.0f ? 1.0f / std::sqrt((float)kD) : c.softmax_scale;
+  a.count = c.count; a.first = c.first; a.last = c.last;
+  a.chosen = c.count > 0 ? c.chosen : nullptr;
+  return a;
+}
+
 // A tensor of `rows` rows; one without rows is not looked at.
 bool rows_of(const xsv_tensor& t, int rows, SeqRows* r) {
   if (rows > 0 && !operand_ok(t)) return false;
   r->p = static_cast<const uint16_t*>(t.ptr); r->sh = t.stride_head; r->st = t.stride_token;
   return true;
+}
+
+// The rows that a call writes or reads.
+int move_args(const xsv_pages* p, const int32_t* begin, int rows, int longest, const xsv_tensor& k, const xsv_tensor& v, PagesArgs* a) {
+  if (!check_pages(p) || rows < 0 || longest < 0 || longest > rows || !aligned_to(begin, 4) || (p->sequences > 0 && !begin)) return XSV_ERR_ARG;
+  if (!pages_supported(*p)) return XSV_ERR_UNSUPPORTED;
+  *a = pages_args(*p);
+  a->begin = begin;
+  a->rows = rows; a->longest = longest;
+  if (!rows_of(k, rows, &a->keys) || !rows_of(v, rows, &a->values)) return XSV_ERR_ARG;
+  return pages_move_fits(*a) ? XSV_OK : XSV_ERR_UNSUPPORTED;
 }
 
 }  // namespace
@@ -169,6 +223,53 @@ int xsv_seq_attend_grad(void* hip_stream, const xsv_seq_config* c, xsv_tensor q,
   a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + delta_bytes(*c));
   if (!seq_attend_fits(a)) return XSV_ERR_UNSUPPORTED;
   return launched(launch_seq_attend_grad(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int xsv_pages_write(void* hip_stream, const xsv_pages* p, const int32_t* begin, int rows, int longest, xsv_tensor k, xsv_tensor v) {
+  PagesArgs a;
+  const int rc = move_args(p, begin, rows, longest, k, v, &a);
+  return rc != XSV_OK ? rc : launched(launch_pages_write(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int xsv_pages_read(void* hip_stream, const xsv_pages* p, const int32_t* begin, int rows, int longest, xsv_tensor k, xsv_tensor v) {
+  PagesArgs a;
+  const int rc = move_args(p, begin, rows, longest, k, v, &a);
+  return rc != XSV_OK ? rc : launched(launch_pages_read(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int xsv_pages_attend_workspace(const xsv_pages* p, const xsv_pages_query* c, int64_t* bytes) {
+  const int rc = check_query(p, c);
+  if (rc != XSV_OK) return rc;
+  if (!bytes) return XSV_ERR_ARG;
+  const PagesArgs a = query_args(*p, *c);
+  if (!pages_attend_fits(a)) return XSV_ERR_UNSUPPORTED;
+  *bytes = pages_attend_workspace(a);
+  return XSV_OK;
+}
+
+int xsv_pages_attend(void* hip_stream, const xsv_pages* p, const xsv_pages_query* c, xsv_tensor q, xsv_tensor out, float* lse, void* workspace,
+                     int64_t workspace_bytes) {
+  int64_t need = 0;
+  const int rc = xsv_pages_attend_workspace(p, c, &need);
+  if (rc != XSV_OK) return rc;
+  PagesArgs a = query_args(*p, *c);
+  if (!rows_of(q, c->rows, &a.q) || !rows_of(out, c->rows, &a.out)) return XSV_ERR_ARG;
+  if (c->rows > 0 && (!lse || !aligned_to(lse, 4))) return XSV_ERR_ARG;
+  if (need > 0 && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < need)) return XSV_ERR_ARG;
+  a.lse = lse;
+  a.part = static_cast<float*>(workspace);
+  return launched(launch_pages_attend(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int xsv_pages_select(void* hip_stream, const xsv_pages* p, const xsv_pages_query* c, xsv_tensor q, int32_t* chosen) {
+  const int rc = check_query(p, c);
+  if (rc != XSV_OK) return rc;
+  if ((long long)c->first + c->last > c->count || c->count < 1 || (p->pages > 0 && !p->k_bounds)) return XSV_ERR_ARG;
+  PagesArgs a = query_args(*p, *c);
+  if (!rows_of(q, c->rows, &a.q) || (c->rows > 0 && (!chosen || !aligned_to(chosen, 4)))) return XSV_ERR_ARG;
+  a.choice = chosen;
+  if (!pages_select_fits(a)) return XSV_ERR_UNSUPPORTED;
+  return launched(launch_pages_select(a, static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

@@ -1,0 +1,258 @@
+// A paged cache in 8 bits: rows written into it and read back.
+//
+//   scale = 2^e, the smallest e in -100 .. 120 with 448 2^e >= max |x| over the finite elements of a page's keys (values) of one head,
+//   code = e4m3(x / scale), to nearest even; what is not finite becomes NaN
+//
+// e4m3 keeps four significant bits at any size down to 2^-15 of the largest, so a few channels of large keys do not cost the others
+// their bits, as they would with whole numbers under one scale.  With powers of two the division is exact, and so is a later change of the
+// page's scale, but for codes below 2^-6, which e4m3 holds in steps of 2^-9: a page that grows token by token is what it would be if
+// written at once, but for those.  The bounds are over the codes, in halves, so that they are whole numbers up to 896, which fp16 and
+// sums of their products with whole numbers in fp32 hold exactly.
+//
+// A workgroup has one page of one head: a thread 16 channels of a token on the row side, 16 bytes of a line of the page on the other; values change
+// sides in LDS.
+#include "pages.h"
+
+namespace xsv {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kLine = 64 + 16;  // bytes of a channel's 64 codes in LDS
+
+// The pages that a sequence's rows are in: the one that page number `i` of the launch is, and the places in it.
+struct Touched {
+  Held h;
+  int ordinal, page;     // of the sequence; of the pool, -1: none
+  int from, to;          // places [from, to) are the rows first .. of the call
+  int first;
+  bool any;
+};
+__device__ __forceinline__ Touched touched(const PagesArgs& a, int s, int i) {
+  Touched t;
+  t.h = held(a, s);
+  const int start = max(t.h.ahead, 0), end = t.h.ahead + t.h.n;  // (rows in front of the first token have no place)
+  t.ordinal = start / kPage + i;
+  const int p0 = t.ordinal * kPage;
+  t.from = max(start - p0, 0);
+  t.to = min(end - p0, kPage);
+  t.any = end > start && t.from < t.to;
+  t.first = t.h.row0 + p0 + t.from - t.h.ahead;
+  t.page = t.any ? a.table[(int64_t)s * a.width + t.ordinal] : -1;
+  t.any = t.any && t.page >= 0 && t.page < a.pages;
+  return t;
+}
+
+// e of the largest |x|, given by its bits
+__device__ __forceinline__ int exponent_of(uint32_t largest) {
+  // |x| = m 2^p, m in [1, 2): 448 = 1.75 2^8
+  const int p = (int)(largest >> 23) - 127 + ((largest & 0x7fffffu) > 0x600000u);
+  return min(max(p - 8, -100), 120);
+}
+__device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
+__device__ __forceinline__ int power_of(float scale) { return (int)((__float_as_uint(scale) >> 23) & 0xff) - 127; }
+
+// four numbers of at most 448, or NaN, as codes
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+}
+__device__ __forceinline__ uint32_t rescaled(uint32_t w, float f) {
+  const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+  return codes4(a[0] * f, a[1] * f, b[0] * f, b[1] * f);
+}
+__device__ __forceinline__ float finite_or_nan(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? __builtin_nanf("") : x; }
+
+// the bytes of a dword that stand for places `at` .. at + 3 and lie in [from, to)
+__device__ __forceinline__ uint32_t within(int at, int from, int to) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m |= at + i >= from && at + i < to ? 0xffu << (8 * i) : 0u;
+  return m;
+}
+
+struct Row16 {  // 16 channels of a token
+  u32x4 r[2];
+  __device__ __forceinline__ void load(const uint16_t* p) {
+    r[0] = *reinterpret_cast<const u32x4*>(p);
+    r[1] = *reinterpret_cast<const u32x4*>(p + 8);
+  }
+  __device__ __forceinline__ uint32_t largest() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t lo = (r[i / 4][i % 4] << 16) & 0x7fff0000u, hi = r[i / 4][i % 4] & 0x7fff0000u;
+      m = max(m, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+    }
+    return m;
+  }
+  __device__ __forceinline__ u32x4 codes(float f) const {
+    u32x4 c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t a = r[i / 2][i % 2 * 2], b = r[i / 2][i % 2 * 2 + 1];
+      c[i] = codes4(finite_or_nan(bf16_low(a)) * f, finite_or_nan(bf16_high(a)) * f, finite_or_nan(bf16_low(b)) * f, finite_or_nan(bf16_high(b)) * f);
+    }
+    return c;
+  }
+};
+
+__device__ __forceinline__ uint32_t wave_largest(uint32_t x) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) x = max(x, (uint32_t)__shfl_xor((int)x, d));
+  return x;
+}
+
+__global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int most) {
+  __shared__ __align__(16) uint8_t lines[2][kD][kLine];  // the codes of keys and values by channel
+  __shared__ uint32_t top[2][kThreads / 64];
+  const int tid = threadIdx.x, number = blockIdx.x;
+  const int head = number % a.kv_heads, i = number / a.kv_heads % most, s = number / a.kv_heads / most;
+  const Touched t = touched(a, s, i);
+  if (!t.any) return;
+  const size_t unit = (size_t)t.page * a.kv_heads + head;
+  const int token = tid / 4, ch0 = tid % 4 * 16;    // the row side, and keys in the page
+  const bool is_new = token >= t.from && token < t.to, is_old = token < t.from;
+  Row16 k{}, v{};
+  u32x4 old_k{}, old_v{};  // of this thread's 16 bytes of the page: channels ch0 .. of its token; places ch0 .. of channel `token`
+  uint8_t* to_k = a.k + unit * kPageBytes + tid * 16;
+  uint8_t* to_v = a.v + unit * kPageBytes + tid * 16;
+  if (is_new) {
+    const int64_t row = t.first + token - t.from;
+    k.load(a.keys.p + head * a.keys.sh + row * a.keys.st + ch0);
+    v.load(a.values.p + head * a.values.sh + row * a.values.st + ch0);
+  }
+  if (t.from > 0) {
+    if (is_old) old_k = *reinterpret_cast<const u32x4*>(to_k);
+    old_v = *reinterpret_cast<const u32x4*>(to_v);
+  }
+  const uint32_t mk = wave_largest(k.largest()), mv = wave_largest(v.largest());
+  if (tid % 64 == 0) {
+    top[0][tid / 64] = mk;
+    top[1][tid / 64] = mv;
+  }
+  __syncthreads();
+  int e[2], grown[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) m = max(m, top[x][w]);
+    const int e_old = t.from > 0 ? power_of((x ? a.v_scale : a.k_scale)[unit]) : -100;
+    e[x] = max(exponent_of(m), e_old);
+    grown[x] = t.from > 0 ? e[x] - e_old : 0;
+  }
+  u32x4 ck = k.codes(power(-e[0])), cv = v.codes(power(-e[1]));
+  if (is_old) {
+    ck = old_k;
+    if (grown[0] > 0)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) ck[j] = rescaled(old_k[j], power(max(-grown[0], -126)));
+  }
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    lines[0][ch0 + j][token] = (uint8_t)(ck[j / 4] >> (8 * (j % 4)));
+    lines[1][ch0 + j][token] = (uint8_t)(cv[j / 4] >> (8 * (j % 4)));
+  }
+  if (is_new || (is_old && grown[0] > 0) || t.from == 0) *reinterpret_cast<u32x4*>(to_k) = ck;  // (behind the rows of a page begun: zeros)
+  __syncthreads();
+  // values: this thread's places ch0 .. of channel `token`
+  const int channel = token, place = ch0;
+  u32x4 nv = *reinterpret_cast<const u32x4*>(&lines[1][channel][place]);
+  if (t.from > 0) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t fresh = within(place + 4 * j, t.from, t.to), before = grown[1] > 0 ? within(place + 4 * j, 0, t.from) : 0u;
+      const uint32_t was = before ? rescaled(old_v[j], power(max(-grown[1], -126))) : 0u;
+      nv[j] = (nv[j] & fresh) | (was & before) | (old_v[j] & ~(fresh | before));
+    }
+  }
+  if (t.from == 0 || (place + 16 > t.from && place < t.to) || (grown[1] > 0 && place < t.from)) *reinterpret_cast<u32x4*>(to_v) = nv;
+  if (tid == 0) {
+    a.k_scale[unit] = power(e[0]);
+    a.v_scale[unit] = power(e[1]);
+  }
+  if (!a.bounds) return;
+  const u32x4 line = *reinterpret_cast<const u32x4*>(&lines[0][channel][place]);
+  float hi = -kInf, lo = kInf;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(line[j], false), y = __builtin_amdgcn_cvt_pk_f32_fp8(line[j], true);
+    const float four[4] = {x[0], x[1], y[0], y[1]};
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+      if (place + 4 * j + b < t.to && four[b] == four[b]) {
+        hi = fmaxf(hi, four[b]);
+        lo = fminf(lo, four[b]);
+      }
+  }
+#pragma unroll
+  for (int d = 1; d < 4; d *= 2) {
+    hi = fmaxf(hi, __shfl_xor(hi, d));
+    lo = fminf(lo, __shfl_xor(lo, d));
+  }
+  if (hi < lo) hi = lo = 0.0f;  // nothing but NaN
+  _Float16* bounds = reinterpret_cast<_Float16*>(a.bounds) + unit * 2 * kD;
+  if (place == 0) bounds[channel] = (_Float16)ceilf(2.0f * hi);
+  if (place == 16) bounds[kD + channel] = (_Float16)floorf(2.0f * lo);
+}
+
+__global__ __launch_bounds__(kThreads) void pages_read_kernel(PagesArgs a, int most) {
+  __shared__ __align__(16) uint8_t lines[kD][kLine];
+  const int tid = threadIdx.x, number = blockIdx.x;
+  const int head = number % a.kv_heads, i = number / a.kv_heads % most, s = number / a.kv_heads / most;
+  const Touched t = touched(a, s, i);
+  if (!t.any) return;
+  const size_t unit = (size_t)t.page * a.kv_heads + head;
+  const u32x4 ck = *reinterpret_cast<const u32x4*>(a.k + unit * kPageBytes + tid * 16);
+  *reinterpret_cast<u32x4*>(&lines[tid / 4][tid % 4 * 16]) = *reinterpret_cast<const u32x4*>(a.v + unit * kPageBytes + tid * 16);
+  const float ks = a.k_scale[unit], vs = a.v_scale[unit];
+  __syncthreads();
+  const int token = tid / 4, ch0 = tid % 4 * 16;
+  if (token < t.from || token >= t.to) return;
+  const int64_t row = t.first + token - t.from;
+  uint16_t* k = const_cast<uint16_t*>(a.keys.p) + head * a.keys.sh + row * a.keys.st + ch0;
+  uint16_t* v = const_cast<uint16_t*>(a.values.p) + head * a.values.sh + row * a.values.st + ch0;
+  u32x4 rk[2], rv[2];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) w |= (uint32_t)lines[ch0 + 4 * j + b][token] << (8 * b);
+    f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(ck[j], false), y = __builtin_amdgcn_cvt_pk_f32_fp8(ck[j], true);
+    rk[j / 2][j % 2 * 2] = pack2(x[0] * ks, x[1] * ks);
+    rk[j / 2][j % 2 * 2 + 1] = pack2(y[0] * ks, y[1] * ks);
+    x = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
+    y = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+    rv[j / 2][j % 2 * 2] = pack2(x[0] * vs, x[1] * vs);
+    rv[j / 2][j % 2 * 2 + 1] = pack2(y[0] * vs, y[1] * vs);
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    *reinterpret_cast<u32x4*>(k + 8 * j) = rk[j];
+    *reinterpret_cast<u32x4*>(v + 8 * j) = rv[j];
+  }
+}
+
+int most_pages(const PagesArgs& a) { return (int)(((long long)a.longest + kPage - 2) / kPage + 1); }
+
+}  // namespace
+
+bool pages_move_fits(const PagesArgs& a) {
+  return (long long)most_pages(a) * a.kv_heads <= (1ll << 24) && (long long)most_pages(a) * a.kv_heads * a.sequences <= (1ll << 32) / kThreads - 1;
+}
+
+hipError_t launch_pages_write(const PagesArgs& a, hipStream_t stream) {
+  if (a.sequences == 0 || a.longest == 0 || a.pages == 0) return hipSuccess;
+  const int most = most_pages(a);
+  pages_write_kernel<<<a.sequences * a.kv_heads * most, kThreads, 0, stream>>>(a, most);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_read(const PagesArgs& a, hipStream_t stream) {
+  if (a.sequences == 0 || a.longest == 0 || a.pages == 0) return hipSuccess;
+  const int most = most_pages(a);
+  pages_read_kernel<<<a.sequences * a.kv_heads * most, kThreads, 0, stream>>>(a, most);
+  return hipGetLastError();
+}
+
+}  // namespace xsv

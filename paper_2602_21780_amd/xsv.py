@@ -58,6 +58,20 @@ class xsv_seq_config(C.Structure):
     ]
 
 
+class xsv_pages(C.Structure):
+    _fields_ = [
+        ("pages", C.c_int32), ("kv_heads", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+        ("k_bounds", C.c_void_p), ("sequences", C.c_int32), ("table_width", C.c_int32), ("table", C.c_void_p), ("lengths", C.c_void_p),
+    ]
+
+
+class xsv_pages_query(C.Structure):
+    _fields_ = [
+        ("heads", C.c_int32), ("rows", C.c_int32), ("longest_q", C.c_int32), ("longest_k", C.c_int32), ("q_begin", C.c_void_p),
+        ("causal", C.c_int32), ("softmax_scale", C.c_float), ("chosen", C.c_void_p), ("count", C.c_int32), ("first", C.c_int32), ("last", C.c_int32),
+    ]
+
+
 # every symbol include/xsv.h declares
 EXPORTS = (
     "xsv_create", "xsv_destroy", "xsv_reset", "xsv_dequant_attend", "xsv_frame_attend", "xsv_score_prune", "xsv_quantize",
@@ -65,6 +79,7 @@ EXPORTS = (
     "xsv_cache_import", "xsv_last_selection", "xsv_quantize_k", "xsv_quantize_v", "xsv_score", "xsv_score_noalloc",
     "xsv_topk_keep", "xsv_strerror", "xsv_norm_rotate", "xsv_norm_rotate_grad", "xsv_norm_rotate_grad_workspace",
     "xsv_seq_attend", "xsv_seq_attend_workspace", "xsv_seq_attend_grad", "xsv_seq_attend_grad_workspace", "xsv_query_attend",
+    "xsv_pages_write", "xsv_pages_read", "xsv_pages_attend", "xsv_pages_attend_workspace", "xsv_pages_select",
 )
 # every symbol include/xsv_tune.h declares (launch tuning and measurement aids)
 TUNE_EXPORTS = (
@@ -130,6 +145,12 @@ def lib():
         L.xsv_seq_attend_workspace.argtypes = [S, C.POINTER(C.c_int64)]
         L.xsv_seq_attend_grad.argtypes = [vp, S, T, T, T, T, vp, T, T, T, T, vp, C.c_int64]
         L.xsv_seq_attend_grad_workspace.argtypes = [S, C.POINTER(C.c_int64)]
+        P, Q = C.POINTER(xsv_pages), C.POINTER(xsv_pages_query)
+        L.xsv_pages_write.argtypes = [vp, P, vp, i32, i32, T, T]
+        L.xsv_pages_read.argtypes = [vp, P, vp, i32, i32, T, T]
+        L.xsv_pages_attend.argtypes = [vp, P, Q, T, T, vp, vp, C.c_int64]
+        L.xsv_pages_attend_workspace.argtypes = [P, Q, C.POINTER(C.c_int64)]
+        L.xsv_pages_select.argtypes = [vp, P, Q, T, vp]
         L.xsv_measure_peaks.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(C.c_float)]
         L.xsv_strerror.argtypes = [i32]
         L.xsv_strerror.restype = C.c_char_p
@@ -633,6 +654,140 @@ def seq_attend_grad(dout, q, k, v, out, lse, q_begin, k_begin=None, *, longest_q
         _check(lib().xsv_seq_attend_grad(s, C.byref(cfg), tq, tk, tv, t_out, lse.data_ptr(), tdout, tdq, tdk, tdv, _ptr(work), n_work),
                "xsv_seq_attend_grad")
     return dq, dk, dv
+
+
+class Pages:
+    """A pool of pages of 64 tokens in 8 bits (see xsv_pages): k float8_e4m3fn [pages][kv_heads][64 tokens][64 channels], v the same with channels
+    in front of tokens, their scales float32 [pages][kv_heads], and unless None the keys' bounds float16 [pages][kv_heads][2][64].  The caller keeps
+    which page holds which tokens: `table` int32 [sequences][width] and `lengths` int32 [sequences] on the pool's device."""
+
+    def __init__(self, k, v, k_scale, v_scale, k_bounds=None):
+        if not isinstance(k, torch.Tensor) or k.dim() != 4 or not k.is_cuda:
+            raise ValueError("k: expected a float8_e4m3fn device tensor [pages][kv_heads][64][64]")
+        n, heads, dev = k.shape[0], k.shape[1], k.device
+        for name, t in (("k", k), ("v", v)):
+            _plain(t, name, torch.float8_e4m3fn, (n, heads, 64, 64), dev)
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            _plain(t, name, torch.float32, (n, heads), dev)
+        if k_bounds is not None:
+            _plain(k_bounds, "k_bounds", torch.float16, (n, heads, 2, 64), dev)
+        self.k, self.v, self.k_scale, self.v_scale, self.k_bounds = k, v, k_scale, v_scale, k_bounds
+        self.count, self.kv_heads, self.device = n, heads, dev
+        self._fields = (n, heads, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(k_bounds))
+
+    @classmethod
+    def empty(cls, count, kv_heads, device="cuda", bounds=True):
+        """A pool of `count` pages that hold nothing yet."""
+        new = lambda *shape, dtype: torch.zeros((count, kv_heads) + shape, dtype=dtype, device=device)
+        codes = [new(64, 64, dtype=torch.uint8).view(torch.float8_e4m3fn) for _ in range(2)]
+        scales = [new(dtype=torch.float32) for _ in range(2)]
+        return cls(*codes, *scales, new(2, 64, dtype=torch.float16) if bounds else None)
+
+    def _at(self, begin, table, lengths):
+        """xsv_pages of a call, after the checks that need the torch tensors."""
+        n = lengths.numel() if isinstance(lengths, torch.Tensor) else -1
+        if n < 0 or not isinstance(table, torch.Tensor) or table.dim() != 2:
+            raise ValueError("table: expected int32 [sequences][width], lengths: int32 [sequences]")
+        width = table.shape[1]
+        _plain(table, "table", torch.int32, (n, width), self.device)
+        _plain(lengths, "lengths", torch.int32, (n,), self.device)
+        _plain(begin, "begin", torch.int32, (n + 1,), self.device)
+        return xsv_pages(*self._fields, n, width, table.data_ptr(), lengths.data_ptr())
+
+
+def _bound(value, most, name):
+    """A bound on lengths (None: `most`); ctypes would cut it down to 32 bits."""
+    if value is None:
+        return most
+    if not 0 <= value < 1 << 31:
+        raise ValueError(f"{name} must be in 0 .. 2^31 - 1")
+    return value
+
+
+def pages_write(pages, k, v, begin, table, lengths, *, longest=None, stream=None):
+    """xsv_pages_write: rows [begin[s], begin[s + 1]) of k, v (bf16 [kv_heads][rows][64]) become the last of the `lengths[s]` tokens of sequence s.
+    longest: a bound on a sequence's rows (None: all)."""
+    tk = _tensor(k, "k", pages.k)
+    tv = _tensor(v, "v", pages.k, k.shape)
+    rows = k.shape[1]
+    if k.shape[0] != pages.kv_heads:
+        raise ValueError(f"k: expected {pages.kv_heads} heads")
+    at = pages._at(begin, table, lengths)
+    with _on(pages.device, stream) as s:
+        _check(lib().xsv_pages_write(s, C.byref(at), begin.data_ptr(), rows, _bound(longest, rows, "longest"), tk, tv), "xsv_pages_write")
+
+
+def pages_read(pages, begin, table, lengths, *, rows=None, longest=None, out=None, stream=None):
+    """xsv_pages_read: (k, v), bf16 [kv_heads][rows][64], with the last begin[s + 1] - begin[s] tokens of sequence s in rows [begin[s], begin[s + 1]).
+    Either `rows` or `out`, the two tensors to write, is given; tensors that it makes hold zeros in rows of no token."""
+    if (rows is None) == (out is None):
+        raise ValueError("give either rows or out")
+    at = pages._at(begin, table, lengths)
+    with _on(pages.device, stream) as s:
+        if out is None:
+            out = [torch.zeros((pages.kv_heads, rows, 64), dtype=torch.bfloat16, device=pages.device) for _ in range(2)]
+        k, v = out
+        tk = _tensor(k, "out[0]", pages.k, written=True)
+        tv = _tensor(v, "out[1]", pages.k, k.shape, written=True)
+        rows = k.shape[1]
+        if k.shape[0] != pages.kv_heads:
+            raise ValueError(f"out: expected {pages.kv_heads} heads")
+        _check(lib().xsv_pages_read(s, C.byref(at), begin.data_ptr(), rows, _bound(longest, rows, "longest"), tk, tv), "xsv_pages_read")
+    return k, v
+
+
+def _pages_query(pages, q, q_begin, table, lengths, longest_q, longest_k, causal, softmax_scale, chosen, count, first, last):
+    at = pages._at(q_begin, table, lengths)
+    heads, rows, _ = q.shape
+    if not 0 <= causal < 1 << 31 or 0.0 < abs(softmax_scale) < 1e-40:   # (ctypes cuts and rounds what does not fit)
+        raise ValueError("causal must fit 32 bits, softmax_scale fp32")
+    return at, xsv_pages_query(heads, rows, _bound(longest_q, rows, "longest_q"), _bound(longest_k, min(64 * table.shape[1], (1 << 31) - 1), "longest_k"),
+                               q_begin.data_ptr(), causal, softmax_scale, _ptr(chosen), count, first, last)
+
+
+def pages_attend(pages, q, q_begin, table, lengths, *, chosen=None, causal=0, softmax_scale=0.0, longest_q=None, longest_k=None, out=None, lse=None,
+                 stream=None):
+    """xsv_pages_attend: attention of q [heads][rows][64] over the sequences' pages, or over `chosen` ones (int32 [rows][kv_heads][count], as
+    pages_select gives them).  longest_q / longest_k, bounds on a sequence's rows and tokens, size the launch (None: all rows, the table's width).
+    Returns (out, lse); tensors that it makes hold zeros in rows of no sequence."""
+    tq = _tensor(q, "q", pages.k)
+    count = 0
+    if chosen is not None:
+        count = chosen.shape[2] if isinstance(chosen, torch.Tensor) and chosen.dim() == 3 else 0
+        _plain(chosen, "chosen", torch.int32, (q.shape[1], pages.kv_heads, count), pages.device)
+        if count == 0:
+            raise ValueError("chosen: expected at least one page per row")
+    at, cfg = _pages_query(pages, q, q_begin, table, lengths, longest_q, longest_k, causal, softmax_scale, chosen, count, 0, 0)
+    with _on(pages.device, stream) as s:
+        out, t_out = _output(out, "out", q, torch.zeros)
+        if lse is None:
+            lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=q.device)
+        else:
+            _plain(lse, "lse", torch.float32, q.shape[:2], q.device)
+        nbytes = C.c_int64()
+        _check(lib().xsv_pages_attend_workspace(C.byref(at), C.byref(cfg), C.byref(nbytes)), "xsv_pages_attend_workspace")
+        work = torch.empty(nbytes.value, dtype=torch.uint8, device=q.device) if nbytes.value else None
+        _check(lib().xsv_pages_attend(s, C.byref(at), C.byref(cfg), tq, t_out, lse.data_ptr(), _ptr(work), nbytes.value), "xsv_pages_attend")
+    return out, lse
+
+
+def pages_select(pages, q, q_begin, table, lengths, count, *, first=1, last=1, causal=0, longest_q=None, longest_k=None, out=None, stream=None):
+    """xsv_pages_select: int32 [rows][kv_heads][count], the pages that every row of q [heads][rows][64] looks at: the first `first` and the last
+    `last` that it sees, and of the others those whose keys could have the largest logits; -1 behind them (and in rows of no sequence of a tensor that it makes)."""
+    tq = _tensor(q, "q", pages.k)
+    if not 1 <= count < 1 << 31 or not 0 <= first < 1 << 31 or not 0 <= last < 1 << 31:
+        raise ValueError("count, first and last must be whole numbers that fit 32 bits, count at least 1")
+    if pages.k_bounds is None:
+        raise ValueError("a choice of pages needs a pool with bounds")
+    at, cfg = _pages_query(pages, q, q_begin, table, lengths, longest_q, longest_k, causal, 0.0, None, count, first, last)
+    shape = (q.shape[1], pages.kv_heads, count)
+    with _on(pages.device, stream) as s:
+        if out is None:
+            out = torch.full(shape, -1, dtype=torch.int32, device=q.device)
+        else:
+            _plain(out, "out", torch.int32, shape, q.device)
+        _check(lib().xsv_pages_select(s, C.byref(at), C.byref(cfg), tq, out.data_ptr()), "xsv_pages_select")
+    return out
 
 
 def key_ranges(cache_tiles, frame_tiles, ranges, last_percent=100, frame_tile_cost=95):
