@@ -3,8 +3,13 @@
 //   q' = q 2^-t rounded to whole numbers, t = floor(log2 max |q|) - 7, so |q'| <= 255 (and the largest are exact)
 //   I_j = sum_c max(q'_c hi_c, q'_c lo_c),   score_j = max over the key head's query heads of I_j 2^(t + e_j - 1)
 //
-// hi, lo are whole numbers up to 896 and I_j below 64 * 255 * 896 < 2^24, so every sum is exact in fp32 in any order: the same pages whatever
+// Since hi >= lo, I_j = max(q', 0) . hi_j + min(q', 0) . lo_j: a product of 128 numbers for matrix instructions in fp16.  hi, lo are whole numbers up to 896
+// and all partial sums below 64 * 255 * 896 < 2^24, so that fp32 holds each exactly in any order: the same pages whatever
 // computes them, and equal scores are equal.  A row's `first` and `last` pages are chosen whatever their scores; equal scores go to the lower page.
+//
+// A workgroup has some queries of one key head, 32 rows (query, head) of a product if it can, whose pages it scores together, 32 a wave and turn, from
+// the pool into keys in LDS; then a wave takes a query, its keys in registers, and halves the interval of keys that its last chosen one lies in
+// until as many keys as wanted lie above it.
 #include <algorithm>
 
 #include "pages.h"
@@ -12,134 +17,236 @@
 namespace xsv {
 namespace {
 
-constexpr int kThreads = 256;
+using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
+using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
+using f32x16 = __attribute__((ext_vector_type(16))) float;
+
 constexpr int kMostPages = 32768;  // scores of a row's pages are held in LDS
+constexpr int kMostKeys = 32768;   // of a workgroup
+constexpr int kHole = INT32_MIN;
 
 __device__ __forceinline__ uint32_t ordered(float x) {  // larger numbers, larger keys; 0 and the largest are for other uses
-  const uint32_t b = __float_as_uint(x == 0.0f ? 0.0f : x);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  const uint32_t b = __float_as_uint(x + 0.0f);         // (0 of either sign is +0)
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
 
-__device__ __forceinline__ float channel_sum(float x) {  // over a wave
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
-  return x;
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const f16x2 p = {(_Float16)a, (_Float16)b};
+  return __builtin_bit_cast(uint32_t, p);
 }
 
-__global__ __launch_bounds__(kThreads) void pages_select_kernel(PagesArgs a) {
-  extern __shared__ __align__(16) uint32_t keys[];
-  __shared__ float whole[kD];
-  __shared__ int unit_of, hist[256], found[2], counts[kThreads / 64], all;
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  const int rep = a.heads / a.kv_heads;
-  const int kv = blockIdx.x % a.kv_heads, i = blockIdx.x / a.kv_heads % a.longest, s = blockIdx.x / a.kv_heads / a.longest;
+// N: keys of a query that a lane holds (0: as many as there are, from LDS each time).
+template <int WAVES, int N>
+__global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, int queries, int pitch) {
+  extern __shared__ __align__(16) uint32_t keys[];  // [queries][pitch]
+  __shared__ __align__(16) int exponents[WAVES][32];
+  const int lane = threadIdx.x % 64, g = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int rep = a.heads / a.kv_heads, groups = (a.longest + queries - 1) / queries;
+  const int kv = blockIdx.x % a.kv_heads, group = blockIdx.x / a.kv_heads % groups, s = blockIdx.x / a.kv_heads / groups;
   const Held h = held(a, s);
-  if (i >= h.n) return;
-  const int pages = (tokens_seen(a, h, i) + kPage - 1) / kPage;
-  const int64_t row = h.row0 + i;
+  const int query0 = group * queries, n = min(queries, h.n - query0);
+  if (n <= 0) return;
   const int32_t* table = a.table + (int64_t)s * a.width;
-  int32_t* out = a.choice + (row * a.kv_heads + kv) * a.count;
-  for (int r = 0; r < rep; ++r) {
+  const int pages = (tokens_seen(a, h, query0 + n - 1) + kPage - 1) / kPage;  // (queries ascend, and so does what they see)
+  const int turns = a.pages > 0 ? (pages + 31) / 32 : 0;
+  if (rep > 1 || turns == 0) {
+    for (int i = threadIdx.x; i < n * pitch; i += 64 * WAVES) keys[i] = 0;
     __syncthreads();
-    if (tid < 64) {
-      const uint16_t bits = a.q.p[(int64_t)(kv * rep + r) * a.q.sh + row * a.q.st + tid];
-      const bool finite = (bits & 0x7f80u) != 0x7f80u;
-      const float x = finite ? __uint_as_float((uint32_t)bits << 16) : 0.0f;
-      float m = fabsf(x);
-      for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-      const int t = max((int)(__float_as_uint(m) >> 23) - 127, -119) - 7;  // (below 2^-119: as if it were 2^-119, which fp32 can turn round)
-      whole[tid] = rintf(x * power(-t));
-      if (tid == 0) unit_of = t;
-    }
-    __syncthreads();
-    for (int j = tid; j < pages; j += kThreads) {
-      const int page = table[j];
-      uint32_t key = 0;
-      if (page >= 0 && page < a.pages) {
-        const int64_t unit = (int64_t)page * a.kv_heads + kv;
-        const _Float16* b = reinterpret_cast<const _Float16*>(a.bounds) + unit * 2 * kD;
-        float sum = 0.0f;
-        for (int c = 0; c < kD; ++c) sum += whole[c] * (float)(whole[c] > 0.0f ? b[c] : b[kD + c]);
-        const int e = unit_of + (int)((__float_as_uint(a.k_scale[unit]) >> 23) & 0xffu) - 128;
-        key = ordered(sum * power(min(max(e, -100), 100)));
-        if (j < a.first || j >= pages - a.last) key = 0xffffffffu;
+  }
+  for (int c0 = 0; c0 < n * rep; c0 += 32) {
+    // The lane's column, a query of a head, and its channels 32 g .. (columns behind the last are copies of it that change nothing)
+    const int col = min(c0 + lane % 32, n * rep - 1), query = col / rep;
+    f16x8 above[4], below[4];
+    int t;
+    {
+      const uint16_t* q = a.q.p + (int64_t)(kv * rep + col % rep) * a.q.sh + (h.row0 + query0 + query) * a.q.st + 32 * g;
+      float x[32], m = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(q + 8 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[8 * i + 2 * j] = (w[j] & 0x7f80u) == 0x7f80u ? 0.0f : bf16_low(w[j]);
+          x[8 * i + 2 * j + 1] = (w[j] & 0x7f800000u) == 0x7f800000u ? 0.0f : bf16_high(w[j]);
+        }
       }
-      keys[j] = r ? max(keys[j], key) : key;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) m = fmaxf(m, fabsf(x[i]));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      t = max((int)(__float_as_uint(m) >> 23) - 127, -119) - 7;  // (below 2^-119: as if it were 2^-119, which fp32 can turn round)
+      const float f = power(-t);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        u32x4 up, down;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float y = rintf(x[8 * i + 2 * j] * f), z = rintf(x[8 * i + 2 * j + 1] * f);
+          up[j] = pack_f16(fmaxf(y, 0.0f), fmaxf(z, 0.0f));
+          down[j] = pack_f16(fminf(y, 0.0f), fminf(z, 0.0f));
+        }
+        above[i] = __builtin_bit_cast(f16x8, up);
+        below[i] = __builtin_bit_cast(f16x8, down);
+      }
+    }
+    for (int turn = wave; turn < turns; turn += WAVES) {
+      const int ordinal = turn * 32 + lane % 32;
+      const int id = ordinal < pages ? table[ordinal] : -1;
+      const bool some = id >= 0 && id < a.pages;
+      const size_t unit = (size_t)(some ? id : 0) * a.kv_heads + kv;
+      const u32x4* b = reinterpret_cast<const u32x4*>(a.bounds + unit * 2 * kD) + 4 * g;
+      u32x4 hi[4], lo[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        hi[i] = b[i];
+        lo[i] = b[8 + i];
+      }
+      const int e = some ? (int)((__float_as_uint(a.k_scale[unit]) >> 23) & 0xffu) - 128 : kHole;
+      if (g == 0) exponents[wave][lane] = e;  // (read by this wave alone, whose LDS accesses stay in order)
+      f32x16 sum = {};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, hi[i]), above[i], sum, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lo[i]), below[i], sum, 0, 0, 0);
+      __builtin_amdgcn_wave_barrier();
+      // the lane has pages 8 i + 4 g + 0..3 of the 32 for its column
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        u32x4 key;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int e = exponents[wave][8 * i + 4 * g + j];
+          const uint32_t k = ordered(sum[4 * i + j] * power(min(max(t + max(e, -1000), -100), 100)));
+          key[j] = e == kHole ? 0u : k;
+        }
+        uint32_t* to = keys + query * pitch + turn * 32 + 8 * i + 4 * g;
+        if (rep == 1) {
+          *reinterpret_cast<u32x4*>(to) = key;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) atomicMax(to + j, key[j]);
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
     }
   }
-  // The `want`-th largest key, a byte at a time.
   __syncthreads();
-  if (tid == 0) all = 0;
-  __syncthreads();
-  for (int j = tid; j < pages; j += kThreads)
-    if (keys[j]) atomicAdd(&all, 1);
-  __syncthreads();
-  int want = min(a.count, all), left = want;  // left: how many of the keys that begin as the `want`-th does
-  uint32_t prefix = 0;
-  for (int shift = 24; shift >= 0 && want > 0; shift -= 8) {
-    hist[tid] = 0;
-    __syncthreads();
-    for (int j = tid; j < pages; j += kThreads)
-      if (keys[j] && (shift == 24 || keys[j] >> (shift + 8) == prefix >> (shift + 8))) atomicAdd(&hist[keys[j] >> shift & 255], 1);
-    __syncthreads();
-    if (tid == 0) {
-      int n = 0, bin = 255;
-      while (n + hist[bin] < left) n += hist[bin--];
-      found[0] = bin;
-      found[1] = left - n;
+  for (int query = wave; query < n; query += WAVES) {
+    const int np = (tokens_seen(a, h, query0 + query) + kPage - 1) / kPage, steps = (np + 63) / 64;
+    uint32_t* row = keys + query * pitch;
+    auto forced = [&](int j) { return j < a.first || j >= np - a.last; };
+    uint32_t held_keys[N ? N : 1];
+    auto key_at = [&](int i) {  // of page 64 i + lane
+      const int j = 64 * i + lane;
+      const uint32_t k = j < np ? row[j] : 0u;
+      return k && forced(j) ? 0xffffffffu : k;
+    };
+    if constexpr (N > 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) held_keys[i] = i < steps ? key_at(i) : 0u;
     }
-    __syncthreads();
-    prefix |= (uint32_t)found[0] << shift;
-    left = found[1];
+    auto over = [&](auto f) {  // f(step, key) for every step of 64 pages
+      if constexpr (N > 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (i < steps) f(i, held_keys[i]);
+      } else {
+        for (int i = 0; i < steps; ++i) f(i, key_at(i));
+      }
+    };
+    auto count_above = [&](uint32_t x) {
+      int c = 0;
+      over([&](int, uint32_t k) { c += __popcll(__ballot(k > x)); });
+      return c;
+    };
+    // More than `want` keys are above lo, at most `want` above hi, which all forced ones are.
+    const int all = count_above(0), want = min(a.count, all);
+    uint32_t lo = 0, hi = 0xfffffffeu;
+    int above_hi = 0;
+    if (all == want) {
+      hi = 0;
+      above_hi = want;
+    } else {
+      uint32_t least = 0xfffffffeu, most = 1;
+      over([&](int, uint32_t k) {
+        if (k && k != 0xffffffffu) {
+          least = min(least, k);
+          most = max(most, k);
+        }
+      });
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        least = min(least, (uint32_t)__shfl_xor((int)least, d));
+        most = max(most, (uint32_t)__shfl_xor((int)most, d));
+      }
+      lo = __builtin_amdgcn_readfirstlane(least) - 1;
+      hi = __builtin_amdgcn_readfirstlane(most);
+      above_hi = count_above(hi);
+      while (above_hi != want && hi - lo > 1) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        const int c = count_above(mid);
+        if (c > want) lo = mid;
+        else {
+          hi = mid;
+          above_hi = c;
+        }
+      }
+    }
+    // In order: the keys above hi, and of those that equal it as many of the first as are left.
+    int32_t* out = a.choice + ((int64_t)(h.row0 + query0 + query) * a.kv_heads + kv) * a.count;
+    int done = 0, left = want - above_hi;
+    const uint64_t before = (1ull << lane) - 1;
+    over([&](int i, uint32_t k) {
+      uint64_t takes = __ballot(k > hi);
+      if (left > 0) {
+        const uint64_t ties = __ballot(k == hi);
+        const bool tie = k == hi && __popcll(ties & before) < left;
+        takes |= __ballot(tie);
+        left = max(left - __popcll(ties), 0);
+      }
+      if (takes >> lane & 1) out[done + __popcll(takes & before)] = 64 * i + lane;
+      done += __popcll(takes);
+    });
+    for (int j = done + lane; j < a.count; j += 64) out[j] = -1;
   }
-  // In order: keys above it, and the first `left` that equal it.
-  int done = 0, equal = 0;
-  for (int j0 = 0; j0 < pages; j0 += kThreads) {
-    const int j = j0 + tid;
-    const uint32_t key = j < pages ? keys[j] : 0;
-    const bool same = want > 0 && key == prefix && key;
-    __syncthreads();
-    if (lane == 0) counts[wave] = 0;
-    const uint64_t ties = __ballot(same);
-    if (lane == 0) counts[wave] = __popcll(ties);
-    __syncthreads();
-    int before = equal + __popcll(ties & ((1ull << lane) - 1));
-    for (int w = 0; w < kThreads / 64; ++w) {
-      if (w < wave) before += counts[w];
-      equal += counts[w];
-    }
-    const bool take = want > 0 && (key > prefix || (same && before < left));
-    const uint64_t takes = __ballot(take);
-    __syncthreads();
-    if (lane == 0) counts[wave] = __popcll(takes);
-    __syncthreads();
-    int at = done + __popcll(takes & ((1ull << lane) - 1));
-    for (int w = 0; w < kThreads / 64; ++w) {
-      if (w < wave) at += counts[w];
-      done += counts[w];
-    }
-    if (take) out[at] = j;
-  }
-  for (int j = done + tid; j < a.count; j += kThreads) out[j] = -1;
 }
 
 int pages_held(const PagesArgs& a) { return std::min(a.width, (int)(((long long)a.longest_k + kPage - 1) / kPage)); }
 
+struct Plan {
+  int queries, pitch;  // of a workgroup; keys of a query (four more than a multiple of 64: queries side by side are in different banks)
+};
+Plan plan_of(const PagesArgs& a) {
+  Plan p;
+  p.pitch = (std::max(pages_held(a), 1) + 63) / 64 * 64 + 4;
+  p.queries = std::max(std::min({32 / (a.heads / a.kv_heads), a.longest, kMostKeys / (p.pitch - 4)}), 1);
+  return p;
+}
+
+template <int WAVES, int N>
+hipError_t launch(const PagesArgs& a, const Plan& p, hipStream_t stream) {
+  const int bytes = p.queries * p.pitch * (int)sizeof(uint32_t), groups = (a.longest + p.queries - 1) / p.queries;
+  if (bytes > (48 << 10)) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_select_kernel<WAVES, N>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+  }
+  pages_select_kernel<WAVES, N><<<a.sequences * groups * a.kv_heads, 64 * WAVES, bytes, stream>>>(a, p.queries, p.pitch);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 bool pages_select_fits(const PagesArgs& a) {
-  const long long most = (1ll << 32) / kThreads - 1;
+  const long long most = (1ll << 32) / 1024 - 1;
   return pages_held(a) <= kMostPages && (long long)a.longest * a.kv_heads <= most && (long long)a.longest * a.kv_heads * a.sequences <= most;
 }
 
 hipError_t launch_pages_select(const PagesArgs& a, hipStream_t stream) {
   if (a.sequences == 0 || a.longest == 0 || a.count == 0) return hipSuccess;
-  const int bytes = std::max(pages_held(a), 1) * (int)sizeof(uint32_t);
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_select_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e != hipSuccess) return e;
-  pages_select_kernel<<<a.sequences * a.longest * a.kv_heads, kThreads, bytes, stream>>>(a);
-  return hipGetLastError();
+  const Plan p = plan_of(a);
+  const int held = pages_held(a);
+  if (p.queries <= 4) return held <= 512 ? launch<4, 8>(a, p, stream) : held <= 2048 ? launch<4, 32>(a, p, stream) : launch<4, 0>(a, p, stream);
+  return held <= 512 ? launch<16, 8>(a, p, stream) : held <= 2048 ? launch<16, 32>(a, p, stream) : launch<16, 0>(a, p, stream);
 }
 
 }  // namespace xsv
