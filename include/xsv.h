@@ -310,7 +310,7 @@ typedef struct {
   void* k;                  /* DEVICE e4m3 [pages][kv_heads][64 tokens][64 channels], 16-byte aligned    */
   void* v;                  /* DEVICE e4m3 [pages][kv_heads][64 channels][64 tokens], 16-byte aligned    */
   float* k_scale;           /* DEVICE [pages][kv_heads]                                        */
-  float* v_scale;           /* DEVICE [pages][kv_heads]                                        */
+  float* v_scale;           /* DEVICE [pages][kv_heads], negative where a code of the page is NaN  */
   void* k_bounds;           /* DEVICE fp16 [pages][kv_heads][2][64], 16-byte aligned: of every channel, twice the largest and the smallest
                                code of the page's tokens, rounded up and down to whole numbers.  For xsv_pages_select; NULL without it */
   int32_t sequences;        /* >= 0                                                            */
@@ -342,7 +342,7 @@ typedef struct {
 /* S = scale q k^T over the tokens that a row sees, lse = log sum exp(S) (natural), out = exp(S - lse) v, as xsv_seq_attend with the sequences'
  * tokens as keys.  With `chosen` (and count > 0) row r of key head g sees only tokens of the pages chosen[r][g][..], each a number of
  * a page of its sequence (entry of its row of the table), in any order; what is none, or none that it sees a token of, is left out, and a page
- * that is listed twice counts twice.  A row that sees no token has out = 0 and lse = -inf.  A NaN reaches exactly the rows that see its token.  q, out: bf16 [heads][rows][64]
+ * that is listed twice counts once.  A row that sees no token has out = 0 and lse = -inf.  A NaN reaches exactly the rows that see its token.  q, out: bf16 [heads][rows][64]
  * via strides; lse: float [heads][rows].  The same bits every time. */
 int xsv_pages_attend(void* hip_stream, const xsv_pages* pages, const xsv_pages_query* cfg, xsv_tensor q, xsv_tensor out, float* lse, void* workspace,
                      int64_t workspace_bytes);

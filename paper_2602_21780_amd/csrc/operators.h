@@ -78,7 +78,7 @@ struct PagesArgs {
   int count, first, last;
   float* part;                   // attention cut over workgroups: what each leaves, [part][head][row][64]
   float* part_sums;              // and its reference and sum, [part][head][row][2]
-  int parts, chunk;              // how many share a block of rows, pages for each (set by the launchers)
+  int parts, chunk, group;       // how many share a block of rows, pages for each; queries that share a list of pages (set by the launchers)
 };
 hipError_t launch_pages_write(const PagesArgs& a, hipStream_t stream);
 hipError_t launch_pages_read(const PagesArgs& a, hipStream_t stream);

@@ -7,7 +7,8 @@
 // their bits, as they would with whole numbers under one scale.  With powers of two the division is exact, and so is a later change of the
 // page's scale, but for codes below 2^-6, which e4m3 holds in steps of 2^-9: a page that grows token by token is what it would be if
 // written at once, but for those.  The bounds are over the codes, in halves, so that they are whole numbers up to 896, which fp16 and
-// sums of their products with whole numbers in fp32 hold exactly.
+// sums of their products with whole numbers in fp32 hold exactly.  A page's scale of values is negative once one of its values is NaN, so that attention has
+// to look for them nowhere else.
 //
 // A workgroup has one page of one head: a thread 16 channels of a token on the row side, 16 bytes of a line of the page on the other; values change
 // sides in LDS.
@@ -60,6 +61,7 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t w, float f) {
   const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
   return codes4(a[0] * f, a[1] * f, b[0] * f, b[1] * f);
 }
+__device__ __forceinline__ bool has_nan(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; }  // 0x7f and 0xff are NaN
 __device__ __forceinline__ float finite_or_nan(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? __builtin_nanf("") : x; }
 
 // the bytes of a dword that stand for places `at` .. at + 3 and lie in [from, to)
@@ -105,6 +107,7 @@ __device__ __forceinline__ uint32_t wave_largest(uint32_t x) {
 __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int most) {
   __shared__ __align__(16) uint8_t lines[2][kD][kLine];  // the codes of keys and values by channel
   __shared__ uint32_t top[2][kThreads / 64];
+  __shared__ int none[kThreads / 64];  // a wave's values are not all numbers
   const int tid = threadIdx.x, number = blockIdx.x;
   const int head = number % a.kv_heads, i = number / a.kv_heads % most, s = number / a.kv_heads / most;
   const Touched t = touched(a, s, i);
@@ -142,6 +145,8 @@ __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int 
     grown[x] = t.from > 0 ? e[x] - e_old : 0;
   }
   u32x4 ck = k.codes(power(-e[0])), cv = v.codes(power(-e[1]));
+  const bool nan = __any(has_nan(cv[0]) || has_nan(cv[1]) || has_nan(cv[2]) || has_nan(cv[3]));
+  if (tid % 64 == 0) none[tid / 64] = nan;
   if (is_old) {
     ck = old_k;
     if (grown[0] > 0)
@@ -168,8 +173,11 @@ __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int 
   }
   if (t.from == 0 || (place + 16 > t.from && place < t.to) || (grown[1] > 0 && place < t.from)) *reinterpret_cast<u32x4*>(to_v) = nv;
   if (tid == 0) {
+    bool negative = t.from > 0 && a.v_scale[unit] < 0.0f;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) negative |= none[w] != 0;
     a.k_scale[unit] = power(e[0]);
-    a.v_scale[unit] = power(e[1]);
+    a.v_scale[unit] = negative ? -power(e[1]) : power(e[1]);
   }
   if (!a.bounds) return;
   const u32x4 line = *reinterpret_cast<const u32x4*>(&lines[0][channel][place]);
@@ -205,7 +213,7 @@ __global__ __launch_bounds__(kThreads) void pages_read_kernel(PagesArgs a, int m
   const size_t unit = (size_t)t.page * a.kv_heads + head;
   const u32x4 ck = *reinterpret_cast<const u32x4*>(a.k + unit * kPageBytes + tid * 16);
   *reinterpret_cast<u32x4*>(&lines[tid / 4][tid % 4 * 16]) = *reinterpret_cast<const u32x4*>(a.v + unit * kPageBytes + tid * 16);
-  const float ks = a.k_scale[unit], vs = a.v_scale[unit];
+  const float ks = a.k_scale[unit], vs = fabsf(a.v_scale[unit]);
   __syncthreads();
   const int token = tid / 4, ch0 = tid % 4 * 16;
   if (token < t.from || token >= t.to) return;

@@ -99,7 +99,6 @@ def check_attend(pool, q, got, begin, table, lengths, causal=0, scale=0.125, cho
     out, lse = (x.cpu().double() for x in got)
     q = q.cpu()
     H, rep = q.shape[0], q.shape[0] // pool.k.shape[1]
-    worst = 0.0
     for s, m in enumerate(lengths):
         a, n = begin[s], begin[s + 1] - begin[s]
         for h in range(H) if heads is None else heads:
@@ -111,7 +110,7 @@ def check_attend(pool, q, got, begin, table, lengths, causal=0, scale=0.125, cho
                 seen = at < limit(r[0], n, m, causal)
                 ks, vs = k[seen], v[seen]
                 if chosen is not None:
-                    parts = [(at[seen] // PAGE == int(j)).nonzero()[:, 0] for j in chosen[a + r[0], h // rep] if j >= 0]
+                    parts = [(at[seen] // PAGE == j).nonzero()[:, 0] for j in sorted(set(chosen[a + r[0], h // rep].tolist())) if j >= 0]
                     pick = torch.cat(parts) if parts else torch.zeros(0, dtype=torch.long)
                     ks, vs = ks[pick], vs[pick]
                 e = plain.Attention(q[h, a + r[0]:a + r[-1] + 1], ks, vs, 0, scale)
@@ -126,7 +125,6 @@ def check_attend(pool, q, got, begin, table, lengths, causal=0, scale=0.125, cho
                 assert bool((off <= e.out_tol + 1e-30).all()), (s, h, list(r), float((off / e.out_tol).max()))
                 off = (l - e.lse).abs()
                 assert bool((off <= e.lse_tol).all()), (s, h, list(r), float((off / e.lse_tol).max()))
-    return worst
 
 
 def select(pool, q, begin, table, lengths, count, first, last, causal):

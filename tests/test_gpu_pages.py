@@ -290,12 +290,8 @@ def test_nan_reaches_the_rows_that_see_its_token(rows):
     def edit(k, v):
         v[0, 150, 3], v[0, 199, 60], v[1, 20, 5] = math.nan, math.inf, math.nan
         k[1, 195, 2] = math.nan
-    pages, table, pool = _filled([200], 2, 35, edit=edit)
-    # what lies behind a sequence's last token: NaN too
-    p = table[0][3]
-    raw = pages.k.view(torch.uint8)
-    raw[p, :, 200 % 64:] = 0x7f
-    pages.v.view(torch.uint8)[p, :, :, 200 % 64:] = 0xff
+        k[:, 200:], v[:, 200:] = math.nan, math.nan     # tokens that are taken back
+    pages, table, pool = _filled([230], 2, 35, edit=edit)
     q = _randn(4, 4, rows, 64).to(torch.bfloat16).to(DEV)
     for causal in (0, 1, 59):
         got = xsv.pages_attend(pages, q, _int([0, rows]), _int(table), _int([200]), causal=causal)
