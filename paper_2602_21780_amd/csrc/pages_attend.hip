@@ -13,20 +13,75 @@ namespace xsv {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kCols = 16;     // rows of a block: (query, head of the key head) pairs, heads first
 constexpr int kMostParts = 64;
+constexpr int kListRows = 16;  // rows that share a list of chosen pages
+// Probabilities are taken against a reference logit per row, which moves when the sum over what a lane has of a page passes this:
+// probabilities above 1 are as exact as below.
+constexpr float kMaxPart = 16777216.0f;
+using f32x16 = __attribute__((ext_vector_type(16))) float;
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float off_of(float ref) { return ref == -kInf ? 0.0f : ref; }  // (nothing finite seen yet)
 
-__device__ __forceinline__ float column_max(float x) {  // over the four lanes of a row
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ __forceinline__ float column_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
-}
+// Products of 16 or 32 columns (rows of queries): D = A B with A the keys, or the values' channels, and a lane's `quarter` its 16 (32: half its 32) lanes.
+// A lane then has logits of one row: of tokens 16 quarter + e of the page with 16 columns, 32 (e / 16) + 16 quarter + e % 16 with 32, because
+// the rows of A are dealt so that they are runs; and the packed probabilities already are the B operand of the second product.
+template <int COLS>
+struct Shape;
+template <>
+struct Shape<16> {
+  using Acc = f32x4;
+  static constexpr int kKeys = 4, kChannels = 4, kLogits = 16;  // blocks of A in a page's keys and in the channels
+  __device__ static __forceinline__ Acc mfma(bf16x8 a, bf16x8 b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  // where in a page the lane's piece i of its four 16-byte pieces of keys, or of values, is
+  __device__ static __forceinline__ int key_at(int col, int quarter, int i) { return (16 * (col / 4) + 4 * i + col % 4) * kD + 16 * quarter; }
+  __device__ static __forceinline__ int value_at(int col, int quarter, int i) { return (16 * i + col) * kPage + 16 * quarter; }
+  __device__ static __forceinline__ int query_at(int quarter) { return 16 * quarter; }
+  // key piece i feeds block and steps (of 8 channels a lane); value piece i its block and steps
+  static constexpr int key_block(int i) { return i; }
+  static constexpr int key_step(int i) { return 0; }
+  static constexpr int value_block(int i) { return i; }
+  static constexpr int value_step(int i) { return 0; }
+  static constexpr int token(int e) { return e; }  // behind 16 * quarter
+  __device__ static __forceinline__ int channel(int block, int quarter, int j) { return 16 * block + 4 * quarter + j; }
+  __device__ static __forceinline__ float column_max(float x) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+  }
+  __device__ static __forceinline__ float column_sum(float x) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+  }
+};
+template <>
+struct Shape<32> {
+  using Acc = f32x16;
+  static constexpr int kKeys = 2, kChannels = 2, kLogits = 32;
+  __device__ static __forceinline__ Acc mfma(bf16x8 a, bf16x8 b, Acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  __device__ static __forceinline__ int key_at(int col, int quarter, int i) {
+    return (32 * (i / 2) + 16 * (col / 4 % 2) + 4 * (col / 8) + col % 4) * kD + 32 * quarter + 16 * (i % 2);
+  }
+  __device__ static __forceinline__ int value_at(int col, int quarter, int i) { return (32 * (i % 2) + col) * kPage + 32 * (i / 2) + 16 * quarter; }
+  __device__ static __forceinline__ int query_at(int quarter) { return 32 * quarter; }
+  static constexpr int key_block(int i) { return i / 2; }
+  static constexpr int key_step(int i) { return i % 2 * 2; }
+  static constexpr int value_block(int i) { return i % 2; }
+  static constexpr int value_step(int i) { return i / 2 * 2; }
+  static constexpr int token(int e) { return 32 * (e / 16) + e % 16; }  // behind 16 * quarter
+  __device__ static __forceinline__ int channel(int block, int quarter, int j) { return 32 * block + 8 * (j / 4) + 4 * quarter + j % 4; }
+  __device__ static __forceinline__ float column_max(float x) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  }
+  __device__ static __forceinline__ float column_sum(float x) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  }
+};
 
 // 8 codes as bf16
 __device__ __forceinline__ bf16x8 view8(uint32_t a, uint32_t b) {
@@ -44,7 +99,7 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   return m;
 }
 
-// A block of up to 16 rows of a key head of a sequence.
+// A block of up to COLS rows of a key head of a sequence.
 struct Block {
   Held h;
   int s, kv;
@@ -56,27 +111,38 @@ struct Block {
   int query0, queries; // chosen pages: the queries of the block
 };
 
-// All pages: rows (query, head) 16 at a time.  Chosen pages: `group` queries with their heads, or 16 heads of a query that has more.
-template <bool CHOSEN>
-__device__ __forceinline__ bool block_of(const PagesArgs& a, int number, int blocks, int col, Block* b) {
+// All pages: rows (query, head) COLS at a time.  Chosen pages: `group` queries with their heads, or 16 heads of a query that has more.
+// The last blocks of all sequences come first: under a mask they see the most.  Workgroups are dealt to the XCDs one by one; where eight divides the key
+// heads, each XCD has its own, one after the other, whose pages are then in one L2, and all of whose blocks go through them at about the same time.
+template <int COLS, bool CHOSEN>
+__device__ __forceinline__ bool block_of(const PagesArgs& a, int number, int parts, int blocks, int col, Block* b) {
   const int rep = a.heads / a.kv_heads;
-  b->part = number % a.parts;
-  const int unit = number / a.parts, block = unit / a.kv_heads % blocks;
-  b->kv = unit % a.kv_heads;
-  b->s = unit / a.kv_heads / blocks;
+  const int heads = a.kv_heads % 8 ? a.kv_heads : a.kv_heads / 8, at = a.kv_heads % 8 ? number : number / 8;
+  const int unit = at / parts;
+  b->part = at % parts;
+  int block;
+  if (a.kv_heads % 8) {
+    b->kv = unit % heads;
+    b->s = unit / heads % a.sequences;
+    block = blocks - 1 - unit / heads / a.sequences;
+  } else {
+    b->s = unit % a.sequences;
+    block = blocks - 1 - unit / a.sequences % blocks;
+    b->kv = number % 8 * heads + unit / a.sequences / blocks;
+  }
   b->h = held(a, b->s);
-  const int per = CHOSEN && rep > kCols ? (rep + kCols - 1) / kCols : 1;  // blocks of a query
+  const int per = CHOSEN && rep > COLS ? (rep + COLS - 1) / COLS : 1;  // blocks of a query
   b->query0 = CHOSEN ? block / per * a.group : 0;
   b->queries = CHOSEN ? min(a.group, b->h.n - b->query0) : b->h.n;
-  const int row0 = (CHOSEN ? block % per : block) * kCols, rows = b->queries * rep;
+  const int64_t row0 = (int64_t)(CHOSEN ? block % per : block) * COLS, rows = (int64_t)b->queries * rep;
   if (b->queries <= 0 || row0 >= rows) return false;
-  const int row = min(row0 + col, rows - 1), last = min(row0 + kCols, rows) - 1;
+  const int64_t row = min(row0 + col, rows - 1), last = min(row0 + COLS, rows) - 1;
   b->real = row0 + col < rows;
-  b->query = b->query0 + row / rep;
-  b->head = b->kv * rep + row % rep;
+  b->query = b->query0 + (int)((uint32_t)row / (uint32_t)rep);   // (below 2^32: blocks of a launch are fewer than 2^24)
+  b->head = b->kv * rep + (int)((uint32_t)row % (uint32_t)rep);
   b->seen = tokens_seen(a, b->h, b->query);
-  b->least = tokens_seen(a, b->h, b->query0 + row0 / rep);
-  b->pages = (tokens_seen(a, b->h, b->query0 + last / rep) + kPage - 1) / kPage;
+  b->least = tokens_seen(a, b->h, b->query0 + (int)((uint32_t)row0 / (uint32_t)rep));
+  b->pages = (tokens_seen(a, b->h, b->query0 + (int)((uint32_t)last / (uint32_t)rep)) + kPage - 1) / kPage;
   b->used = CHOSEN ? a.parts : min(max((b->pages + a.chunk - 1) / a.chunk, 1), a.parts);
   return b->part < b->used;
 }
@@ -100,14 +166,14 @@ __device__ __forceinline__ int list_window(const PagesArgs& a, const Block& b, i
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, rep = a.heads / a.kv_heads, words = min(kWindow, b.pages - w0);
   for (int i = tid; i < words; i += 64 * kWaves) l.rows[i] = 0;
   __syncthreads();
-  for (int q = 0; q < b.queries; ++q) {
-    const int32_t* list = a.chosen + ((int64_t)(b.h.row0 + b.query0 + q) * a.kv_heads + b.kv) * a.count;
+  // (the lists of all queries at once: one after the other, each would wait for memory)
+  const int entries = b.queries * a.count;  // (more than one query: at most 16 times what a table holds)
+  for (int i = tid; i < entries; i += 64 * kWaves) {
+    const int q = (int)((uint32_t)i / (uint32_t)a.count);
+    const int j = a.chosen[((int64_t)(b.h.row0 + b.query0 + q) * a.kv_heads + b.kv) * a.count + (i - q * a.count)];
     const int end = (tokens_seen(a, b.h, b.query0 + q) + kPage - 1) / kPage;
-    const uint32_t rows = rep >= kCols ? 0xffffu : ((1u << rep) - 1u) << (q * rep);
-    for (int i = tid; i < a.count; i += 64 * kWaves) {
-      const int j = list[i];
-      if (j >= w0 && j < end && j - w0 < words) atomicOr(&l.rows[j - w0], rows);
-    }
+    const uint32_t rows = rep >= kListRows ? 0xffffu : ((1u << rep) - 1u) << (q * rep);
+    if (j >= w0 && j < end && j - w0 < words) atomicOr(&l.rows[j - w0], rows);
   }
   __syncthreads();
   constexpr int kEach = kWindow / (64 * kWaves);
@@ -141,24 +207,26 @@ __device__ __forceinline__ int list_window(const PagesArgs& a, const Block& b, i
 
 struct Empty {};
 
-template <bool CHOSEN>
-__global__ __launch_bounds__(64 * kWaves, CHOSEN ? 3 : 4) void pages_attend_kernel(PagesArgs a, int blocks) {
-  __shared__ __align__(16) float acc[kWaves][kCols][kD + 4];
-  __shared__ float refs[kWaves][kCols], sums[kWaves][kCols];
+template <int COLS, bool CHOSEN>
+__global__ __launch_bounds__(64 * kWaves, COLS == 32 || CHOSEN ? 3 : 4) void pages_attend_kernel(PagesArgs a, int blocks) {
+  using S = Shape<COLS>;
+  __shared__ __align__(16) float acc[kWaves][COLS][kD + 4];
+  __shared__ float refs[kWaves][COLS], sums[kWaves][COLS];
   __shared__ std::conditional_t<CHOSEN, Lists, Empty> lists;
-  const int lane = threadIdx.x % 64, col = lane % 16, u = lane / 16;
+  const int lane = threadIdx.x % 64, col = lane % COLS, quarter = lane / COLS;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   Block b;
-  if (!block_of<CHOSEN>(a, blockIdx.x, blocks, col, &b)) return;
+  if (!block_of<COLS, CHOSEN>(a, blockIdx.x, a.parts, blocks, col, &b)) return;
   const int32_t* table = a.table + (int64_t)b.s * a.width;
 
-  bf16x8 qf[2];
+  constexpr int kSteps = COLS / 8;  // of 8 channels, and of 8 tokens, a lane
+  bf16x8 qf[kSteps];
   {
-    const uint16_t* q = a.q.p + b.head * a.q.sh + (int64_t)(b.h.row0 + b.query) * a.q.st + 16 * u;
+    const uint16_t* q = a.q.p + b.head * a.q.sh + (int64_t)(b.h.row0 + b.query) * a.q.st + S::query_at(quarter);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) qf[i] = *reinterpret_cast<const bf16x8*>(q + 8 * i);
+    for (int i = 0; i < kSteps; ++i) qf[i] = *reinterpret_cast<const bf16x8*>(q + 8 * i);
   }
-  f32x4 o[4] = {};
+  typename S::Acc o[S::kChannels] = {};
   float ref = -kInf, sum = 0.0f;
   const float c2 = a.scale * kLog2e;
 
@@ -183,71 +251,81 @@ __global__ __launch_bounds__(64 * kWaves, CHOSEN ? 3 : 4) void pages_attend_kern
     return n;
   };
   u32x4 kr[4];
-  const int key_at = (16 * (col / 4) + col % 4) * kD + 16 * u, value_at = col * kPage + 16 * u;
   auto fetch_keys = [&](int page) {
-    const uint8_t* p = a.k + ((size_t)page * a.kv_heads + b.kv) * kPageBytes + key_at;
+    const uint8_t* p = a.k + ((size_t)page * a.kv_heads + b.kv) * kPageBytes;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) kr[i] = *reinterpret_cast<const u32x4*>(p + 4 * i * kD);
+    for (int i = 0; i < 4; ++i) kr[i] = *reinterpret_cast<const u32x4*>(p + S::key_at(col, quarter, i));
   };
-  auto tile = [&](int page, int ordinal, uint32_t rows, float ks, float vs, int next) {
-    u32x4 vr[4];
-    const uint8_t* p = a.v + ((size_t)page * a.kv_heads + b.kv) * kPageBytes + value_at;
+  constexpr int kEach = S::kLogits / S::kKeys;
+  u32x4 vr[4];
+  typename S::Acc x[S::kKeys];
+  u32x4 pr[kSteps];
+  float part;  // sum of the lane's probabilities in a page
+  auto fetch_values = [&](int page) {
+    const uint8_t* p = a.v + ((size_t)page * a.kv_heads + b.kv) * kPageBytes;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) vr[i] = *reinterpret_cast<const u32x4*>(p + 16 * i * kPage);
-    f32x4 x[4];
+    for (int i = 0; i < 4; ++i) vr[i] = *reinterpret_cast<const u32x4*>(p + S::value_at(col, quarter, i));
+  };
+  auto first_products = [&] {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(view8(kr[i][0], kr[i][1]), qf[0], f32x4{}, 0, 0, 0);
-      x[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(view8(kr[i][2], kr[i][3]), qf[1], x[i], 0, 0, 0);
-    }
-    if (next >= 0) fetch_keys(next);
-    const bool cut = (ordinal + 1) * kPage > b.least;         // some row does not see some of the page's tokens
-    const bool mine = !CHOSEN || (rows >> col & 1);
-    const int left = mine ? b.seen - ordinal * kPage - 16 * u : 0;  // of the lane's 16 tokens
-    if (cut)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[i][j] = 4 * i + j < left ? x[i][j] : -kInf;
-    float m = -kInf;
+    for (int i = 0; i < S::kKeys; ++i) x[i] = typename S::Acc{};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) m = fmaxf(m, x[i][j]);
-    const float cs = c2 * ks;
-    const float top = mine ? column_max(m) * cs : -kInf;
-    if (__any(top > ref)) {
-      const float to = fmaxf(top, ref), f = ref == -kInf || to == ref ? 1.0f : exp2_(ref - to);
-      ref = to;
-      sum *= f;
+      for (int k = 0; k < 2; ++k)
+        x[S::key_block(i)] = S::mfma(view8(kr[i][2 * k], kr[i][2 * k + 1]), qf[S::key_step(i) + k], x[S::key_block(i)]);
+  };
+  // The values' scale 2^ev goes into the exponent: what enters the second product is in the values' own units.
+  auto weigh = [&](float cs, int ev, bool mine) {
+    const float off = off_of(ref) - (float)ev;
+    float one = 0.0f, other = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] *= f;
+    for (int e = 0; e < S::kLogits; e += 2) {
+      const float p = exp2_(x[e / kEach][e % kEach] * cs - off), q = exp2_(x[e / kEach][e % kEach + 1] * cs - off);
+      one += p;
+      other += q;
+      pr[e / 8][e % 8 / 2] = pack2(p, q);
     }
-    const float off = off_of(ref), size = fabsf(vs);
-    float part = 0.0f;
-    u32x4 pr[2];
+    part = (one + other) * __int_as_float((127 - ev) << 23);
+    if (CHOSEN) {
+      if (!mine) part = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        x[i][j] = exp2_(x[i][j] * cs - off);
-        part += x[i][j];
-        x[i][j] *= size;
-      }
-      pr[i / 2][i % 2 * 2] = pack2(x[i][0], x[i][1]);
-      pr[i / 2][i % 2 * 2 + 1] = pack2(x[i][2], x[i][3]);
+      for (int i = 0; i < 4 * kSteps; ++i) pr[i / 4][i % 4] = mine ? pr[i / 4][i % 4] : 0u;
     }
-    sum += mine ? part : 0.0f;
-    if constexpr (CHOSEN)
+  };
+  auto second_products = [&] {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) pr[i / 4][i % 4] = mine ? pr[i / 4][i % 4] : 0u;
-    if (vs < 0.0f) {
-      // 0 times NaN is NaN: values that are NaN are taken out of the product, and reach the rows that see their tokens by one of their own
-      u32x4 sees[2];
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int k = 0; k < 2; ++k)
+        o[S::value_block(i)] = S::mfma(view8(vr[i][2 * k], vr[i][2 * k + 1]), __builtin_bit_cast(bf16x8, pr[S::value_step(i) + k]), o[S::value_block(i)]);
+  };
+  auto exponent_of = [](float scale) { return (int)((__float_as_uint(scale) >> 23) & 0xffu) - 127; };
+  // A page with all that may happen: rows that do not see some of it, references that move, values that are NaN.
+  auto whole = [&](int ordinal, uint32_t rows, float ks, float vs, int next_page) {
+    const bool mine = !CHOSEN || (rows >> col & 1);
+    const int left = mine ? b.seen - ordinal * kPage - 16 * quarter : -kPage;  // of the tokens from the lane's first on
+    const float cs = c2 * ks;
+    first_products();
+    fetch_keys(next_page);
+    float m = -kInf;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sees[k][i] = (8 * k + 2 * i < left ? 0x3f80u : 0u) | (8 * k + 2 * i + 1 < left ? 0x3f800000u : 0u);
+    for (int e = 0; e < S::kLogits; ++e) {
+      const float y = S::token(e) < left ? x[e / kEach][e % kEach] : -kInf;
+      x[e / kEach][e % kEach] = y;
+      m = fmaxf(m, y);
+    }
+    m = S::column_max(m) * cs;
+    const float to = fmaxf(m, ref), f = ref == -kInf || to == ref ? 1.0f : exp2_(ref - to);
+    ref = to;
+    sum *= f;
+#pragma unroll
+    for (int i = 0; i < S::kChannels; ++i) o[i] *= f;
+    weigh(cs, exponent_of(vs), mine);
+    sum += part;
+    if (vs < 0.0f) {
+      // 0 times NaN is NaN: values that are NaN are taken out of the product, and reach the rows that see their tokens by one of their own
+      typename S::Acc count[S::kChannels] = {};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         u32x4 nan;
@@ -257,20 +335,26 @@ __global__ __launch_bounds__(64 * kWaves, CHOSEN ? 3 : 4) void pages_attend_kern
           vr[i][j] &= ~nan[j];
           nan[j] &= 0x38383838u;  // 1
         }
-        f32x4 count = {};
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-          count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(view8(nan[2 * k], nan[2 * k + 1]), __builtin_bit_cast(bf16x8, sees[k]), count, 0, 0, 0);
+        for (int k = 0; k < 2; ++k) {
+          u32x4 sees;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[i][j] = count[j] > 0.0f ? __builtin_nanf("") : o[i][j];
+          for (int j = 0; j < 4; ++j) {
+            const int e = 8 * (S::value_step(i) + k) + 2 * j;
+            sees[j] = (S::token(e) < left ? 0x3f80u : 0u) | (S::token(e + 1) < left ? 0x3f800000u : 0u);
+          }
+          count[S::value_block(i)] = S::mfma(view8(nan[2 * k], nan[2 * k + 1]), __builtin_bit_cast(bf16x8, sees), count[S::value_block(i)]);
+        }
       }
+#pragma unroll
+      for (int i = 0; i < S::kChannels; ++i)
+#pragma unroll
+        for (int j = 0; j < (int)(sizeof(typename S::Acc) / 4); ++j) o[i][j] = count[i][j] > 0.0f ? __builtin_nanf("") : o[i][j];
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(view8(vr[i][2 * k], vr[i][2 * k + 1]), __builtin_bit_cast(bf16x8, pr[k]), o[i], 0, 0, 0);
+    second_products();
   };
+  // Pages one after the other.  The inner loop has those that need nothing but the arithmetic: the accumulators stay where they are (changed on a way of
+  // its own inside the loop, they were copied on the others too, in every page).
   auto over = [&](int begin, int end, int w0) {
     for (int from = begin + wave; from < end; from += kWaves * 64) {
       const Next n = look(from, end, w0);
@@ -279,11 +363,41 @@ __global__ __launch_bounds__(64 * kWaves, CHOSEN ? 3 : 4) void pages_attend_kern
       int i = __builtin_ctzll(mask), page = __builtin_amdgcn_readlane(n.page, i);
       fetch_keys(page);
       while (true) {
-        mask &= mask - 1;
-        const int next = mask ? __builtin_ctzll(mask) : -1, next_page = __builtin_amdgcn_readlane(n.page, max(next, 0));
-        tile(page, __builtin_amdgcn_readlane(n.ordinal, i), CHOSEN ? __builtin_amdgcn_readlane(n.rows, i) : 0u,
-             __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(n.ks), i)), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(n.vs), i)),
-             mask ? next_page : -1);
+        int ordinal;
+        uint32_t rows;
+        float ks, vs;
+        bool fetched = true, done = false;  // `kr` has this page's keys; the last page is behind
+        int next, next_page;
+        while (true) {
+          ordinal = __builtin_amdgcn_readlane(n.ordinal, i);
+          rows = CHOSEN ? __builtin_amdgcn_readlane(n.rows, i) : 0u;
+          ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(n.ks), i));
+          vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(n.vs), i));
+          mask &= mask - 1;
+          next = mask ? __builtin_ctzll(mask) : i;  // (the last one's keys are fetched again)
+          next_page = __builtin_amdgcn_readlane(n.page, next);
+          fetch_values(page);
+          if ((ordinal + 1) * kPage > b.least || vs < 0.0f) break;  // some row does not see some of its tokens, or NaN
+          const bool mine = !CHOSEN || (rows >> col & 1);
+          if (__any(mine && ref == -kInf)) break;  // a row's first page
+          first_products();
+          __builtin_amdgcn_sched_barrier(0);
+          fetch_keys(next_page);
+          weigh(c2 * ks, exponent_of(vs), mine);
+          fetched = false;
+          if (__any(part > kMaxPart)) break;
+          __builtin_amdgcn_sched_barrier(0);
+          sum += part;
+          second_products();
+          done = !mask;
+          if (done) break;
+          i = next;
+          page = next_page;
+          fetched = true;
+        }
+        if (done) break;
+        if (!fetched) fetch_keys(page);
+        whole(ordinal, rows, ks, vs, next_page);
         if (!mask) break;
         i = next;
         page = next_page;
@@ -293,25 +407,28 @@ __global__ __launch_bounds__(64 * kWaves, CHOSEN ? 3 : 4) void pages_attend_kern
   if constexpr (CHOSEN) {
     for (int w0 = 0; w0 < b.pages; w0 += kWindow) {
       const int total = list_window(a, b, w0, lists);
-      over((int)((int64_t)total * b.part / b.used), (int)((int64_t)total * (b.part + 1) / b.used), w0);
+      over((int)((uint32_t)(total * b.part) / (uint32_t)b.used), (int)((uint32_t)(total * (b.part + 1)) / (uint32_t)b.used), w0);  // (2048 pages, 64 parts)
       __syncthreads();
     }
   } else {
     over(b.part * a.chunk, b.part == b.used - 1 ? b.pages : (b.part + 1) * a.chunk, 0);
   }
 
-  // The waves' results: lane (col, u) has channels 16 i + 4 u + 0..3 of row col.
-  const float total = column_sum(sum);
+  // The waves' results.
+  const float total = S::column_sum(sum);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(&acc[wave][col][16 * i + 4 * u]) = o[i];
-  if (u == 0) {
+  for (int i = 0; i < S::kChannels; ++i)
+#pragma unroll
+    for (int j = 0; j < (int)(sizeof(typename S::Acc) / 4); j += 4)
+      *reinterpret_cast<f32x4*>(&acc[wave][col][S::channel(i, quarter, j)]) = f32x4{o[i][j], o[i][j + 1], o[i][j + 2], o[i][j + 3]};
+  if (quarter == 0) {
     refs[wave][col] = ref;
     sums[wave][col] = total;
   }
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < kCols / kWaves; ++j) {
-    const int r = wave * (kCols / kWaves) + j, c = lane;
+  for (int j = 0; j < COLS / kWaves; ++j) {
+    const int r = wave * (COLS / kWaves) + j, c = lane;
     // (row r's place is what lane r has)
     if (!__builtin_amdgcn_readlane(b.real, r)) continue;
     const int head = __builtin_amdgcn_readlane(b.head, r);
@@ -357,13 +474,13 @@ __device__ __forceinline__ float over_wave(float x, F f) {
 
 // Rows whose pages several workgroups shared: their parts in order, a wave to a row.  The weight of a part is worked out by a lane of its own,
 // and the loads of 16 parts' values do not wait for one another or for the weights.
-template <bool CHOSEN>
+template <int COLS, bool CHOSEN>
 __global__ __launch_bounds__(64 * kWaves) void pages_join_kernel(PagesArgs a, int blocks) {
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   Block b;
-  if (!block_of<CHOSEN>(a, blockIdx.x * a.parts, blocks, lane % 16, &b) || b.used == 1) return;
+  if (!block_of<COLS, CHOSEN>(a, blockIdx.x, 1, blocks, lane % COLS, &b) || b.used == 1) return;
 #pragma unroll 1
-  for (int r = wave; r < kCols; r += kWaves) {
+  for (int r = wave; r < COLS; r += kWaves) {
     if (!__builtin_amdgcn_readlane(b.real, r)) break;
     const int head = __builtin_amdgcn_readlane(b.head, r);
     const int64_t row = b.h.row0 + __builtin_amdgcn_readlane(b.query, r);
@@ -394,7 +511,7 @@ __global__ __launch_bounds__(64 * kWaves) void pages_join_kernel(PagesArgs a, in
 
 struct Plan {
   long long blocks, units;  // of a sequence and key head; of all
-  int parts, chunk, group;
+  int parts, chunk, group, cols;
 };
 constexpr long long kMostWorkgroups = (1ll << 32) / (64 * kWaves) - 1;  // threads of a launch are counted in 32 bits
 long long times(long long a, long long b) { return b != 0 && a > kMostWorkgroups / b ? kMostWorkgroups + 1 : a * b; }  // as far as it matters
@@ -403,13 +520,15 @@ Plan plan_of(const PagesArgs& a) {
   const int rep = a.heads / a.kv_heads;
   p.chunk = 1;
   p.group = 1;
+  p.cols = 16;
   if (a.chosen) {
-    if (rep <= kCols) p.group = std::min(kCols / rep, std::max(a.longest, 1));
-    p.blocks = ((long long)a.longest + p.group - 1) / p.group * ((rep + kCols - 1) / kCols);
+    if (rep <= kListRows) p.group = std::min(kListRows / rep, std::max(a.longest, 1));
+    p.blocks = ((long long)a.longest + p.group - 1) / p.group * ((rep + kListRows - 1) / kListRows);
     p.units = times(times(p.blocks, a.kv_heads), a.sequences);
     p.parts = (int)std::max<long long>(std::min<long long>(512 / std::max(p.units, 1ll), (a.count + kWaves - 1) / kWaves), 1);
   } else {
-    p.blocks = ((long long)a.longest * rep + kCols - 1) / kCols;
+    if ((long long)a.longest * rep > 16) p.cols = 32;
+    p.blocks = ((long long)a.longest * rep + p.cols - 1) / p.cols;
     p.units = times(times(p.blocks, a.kv_heads), a.sequences);
     const long long items = ((long long)a.longest_k + kPage - 1) / kPage;
     const long long most = std::min<long long>(std::max<long long>(1024 / std::max(p.units, 1ll), 1), kMostParts);
@@ -420,15 +539,14 @@ Plan plan_of(const PagesArgs& a) {
   return p;
 }
 
-template <bool CHOSEN>
-hipError_t launch(PagesArgs a, hipStream_t stream) {
-  const Plan p = plan_of(a);
+template <int COLS, bool CHOSEN>
+hipError_t launch(PagesArgs a, const Plan& p, hipStream_t stream) {
   a.parts = p.parts;
   a.chunk = p.chunk;
   a.group = p.group;
   a.part_sums = a.part + (int64_t)a.parts * a.heads * a.rows * kD;
-  pages_attend_kernel<CHOSEN><<<(int)(p.units * p.parts), 64 * kWaves, 0, stream>>>(a, (int)p.blocks);
-  if (p.parts > 1) pages_join_kernel<CHOSEN><<<(int)p.units, 64 * kWaves, 0, stream>>>(a, (int)p.blocks);
+  pages_attend_kernel<COLS, CHOSEN><<<(int)(p.units * p.parts), 64 * kWaves, 0, stream>>>(a, (int)p.blocks);
+  if (p.parts > 1) pages_join_kernel<COLS, CHOSEN><<<(int)p.units, 64 * kWaves, 0, stream>>>(a, (int)p.blocks);
   return hipGetLastError();
 }
 
@@ -446,7 +564,8 @@ bool pages_attend_fits(const PagesArgs& a) {
 
 hipError_t launch_pages_attend(const PagesArgs& a, hipStream_t stream) {
   if (a.sequences == 0 || a.longest == 0) return hipSuccess;
-  return a.chosen ? launch<true>(a, stream) : launch<false>(a, stream);
+  const Plan p = plan_of(a);
+  return a.chosen ? launch<16, true>(a, p, stream) : p.cols == 16 ? launch<16, false>(a, p, stream) : launch<32, false>(a, p, stream);
 }
 
 }  // namespace xsv
