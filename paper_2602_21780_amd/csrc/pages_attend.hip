@@ -12,8 +12,16 @@
 namespace xsv {
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4;       // of a workgroup, or all that a compute unit holds
+constexpr int kManyWaves = 16;
 constexpr int kMostParts = 64;
+// Pages that the waves of a workgroup share where every sequence has one block: their lengths are known on the device alone, so a long one is cut as if it were
+// alone, and workgroups without a share end at once.  64 streams of 60 to 32768 tokens, 8 key heads, us: 32 pages 78, 48 77, 64 77, 80 77, 128 91, 256 91.
+constexpr int kLongest = 64;
+// Short caches of few blocks: one workgroup of 16 waves to a block instead of parts and their join, which is a launch more.  us from Python, one workgroup and parts: 16 blocks
+// over 512 to 4096 tokens 12 and 16, over 8192 20 and 16; 64 over 4096 13 and 16, over 8192 20 and 18; 256 over 4096 27 and 33 (over 8192 49 and 56, but
+// there sequences of different lengths would leave compute units empty).
+constexpr int kManyUnits = 256, kManyPages = 64;
 constexpr int kListRows = 16;  // rows that share a list of chosen pages
 // Probabilities are taken against a reference logit per row, which moves when the sum over what a lane has of a page passes this:
 // probabilities above 1 are as exact as below.
@@ -112,26 +120,30 @@ struct Block {
 };
 
 // All pages: rows (query, head) COLS at a time.  Chosen pages: `group` queries with their heads, or 16 heads of a query that has more.
-// The last blocks of all sequences come first: under a mask they see the most.  Workgroups are dealt to the XCDs one by one; where eight divides the key
-// heads, each XCD has its own, one after the other, whose pages are then in one L2, and all of whose blocks go through them at about the same time.
+// Sequences' blocks are counted from their ends, so that under a mask those that see the most come first, and those of a short sequence behind a long
+// cache, which see as much, among them.  Workgroups are dealt to the XCDs one by one; where eight divides the key
+// heads, each XCD has its own, one after the other, whose pages are then in one L2, and all of whose blocks go through them at about the same time.  A block's parts are far apart: side by side, with eight of them,
+// those of short sequences, which have little or nothing to do, were dealt to the same compute units (64 streams 89 us, 77).
 template <int COLS, bool CHOSEN>
-__device__ __forceinline__ bool block_of(const PagesArgs& a, int number, int parts, int blocks, int col, Block* b) {
+__device__ __forceinline__ bool block_of(const PagesArgs& a, int number, int blocks, int col, Block* b) {
   const int rep = a.heads / a.kv_heads;
   const int heads = a.kv_heads % 8 ? a.kv_heads : a.kv_heads / 8, at = a.kv_heads % 8 ? number : number / 8;
-  const int unit = at / parts;
-  b->part = at % parts;
-  int block;
+  const int units = heads * a.sequences * blocks, unit = at % units;
+  b->part = at / units;
+  int back;  // blocks behind this one
   if (a.kv_heads % 8) {
     b->kv = unit % heads;
     b->s = unit / heads % a.sequences;
-    block = blocks - 1 - unit / heads / a.sequences;
+    back = unit / heads / a.sequences;
   } else {
     b->s = unit % a.sequences;
-    block = blocks - 1 - unit / a.sequences % blocks;
+    back = unit / a.sequences % blocks;
     b->kv = number % 8 * heads + unit / a.sequences / blocks;
   }
   b->h = held(a, b->s);
   const int per = CHOSEN && rep > COLS ? (rep + COLS - 1) / COLS : 1;  // blocks of a query
+  const int block = (CHOSEN ? (b->h.n + a.group - 1) / a.group * per : (int)(((int64_t)b->h.n * rep + COLS - 1) / COLS)) - 1 - back;
+  if (block < 0) return false;
   b->query0 = CHOSEN ? block / per * a.group : 0;
   b->queries = CHOSEN ? min(a.group, b->h.n - b->query0) : b->h.n;
   const int64_t row0 = (int64_t)(CHOSEN ? block % per : block) * COLS, rows = (int64_t)b->queries * rep;
@@ -207,16 +219,16 @@ __device__ __forceinline__ int list_window(const PagesArgs& a, const Block& b, i
 
 struct Empty {};
 
-template <int COLS, bool CHOSEN>
-__global__ __launch_bounds__(64 * kWaves, COLS == 32 || CHOSEN ? 3 : 4) void pages_attend_kernel(PagesArgs a, int blocks) {
+template <int COLS, bool CHOSEN, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || CHOSEN) ? 4 : 3) void pages_attend_kernel(PagesArgs a, int blocks) {
   using S = Shape<COLS>;
-  __shared__ __align__(16) float acc[kWaves][COLS][kD + 4];
-  __shared__ float refs[kWaves][COLS], sums[kWaves][COLS];
+  __shared__ __align__(16) float acc[WAVES][COLS][kD + 4];
+  __shared__ float refs[WAVES][COLS], sums[WAVES][COLS];
   __shared__ std::conditional_t<CHOSEN, Lists, Empty> lists;
   const int lane = threadIdx.x % 64, col = lane % COLS, quarter = lane / COLS;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   Block b;
-  if (!block_of<COLS, CHOSEN>(a, blockIdx.x, a.parts, blocks, col, &b)) return;
+  if (!block_of<COLS, CHOSEN>(a, blockIdx.x, blocks, col, &b)) return;
   const int32_t* table = a.table + (int64_t)b.s * a.width;
 
   constexpr int kSteps = COLS / 8;  // of 8 channels, and of 8 tokens, a lane
@@ -230,15 +242,17 @@ __global__ __launch_bounds__(64 * kWaves, COLS == 32 || CHOSEN ? 3 : 4) void pag
   float ref = -kInf, sum = 0.0f;
   const float c2 = a.scale * kLog2e;
 
-  // Of the pages (or entries of the list) `from`, `from` + kWaves, .. below `end`.
-  auto look = [&](int from, int end, int w0) {
+  // Of the pages (or entries of the list) `from`, `from` + WAVES, .. below `end`.
+  // Lists from their end: the pages that all rows have listed, the last ones for the most part, then come before those of single rows, and a row's first
+  // page is more work.
+  auto look = [&](int from, int begin, int end, int w0) {
     Next n;
-    const int at = from + kWaves * lane;
+    const int at = from + WAVES * lane;
     bool some = at < end;
     n.ordinal = at;
     n.rows = 0;
     if constexpr (CHOSEN) {
-      const uint32_t entry = some ? lists.found[at] : 0u;
+      const uint32_t entry = some ? lists.found[begin + end - 1 - at] : 0u;
       n.ordinal = w0 + (int)(entry & 0xffffu);
       n.rows = entry >> 16;
     }
@@ -356,8 +370,8 @@ __global__ __launch_bounds__(64 * kWaves, COLS == 32 || CHOSEN ? 3 : 4) void pag
   // Pages one after the other.  The inner loop has those that need nothing but the arithmetic: the accumulators stay where they are (changed on a way of
   // its own inside the loop, they were copied on the others too, in every page).
   auto over = [&](int begin, int end, int w0) {
-    for (int from = begin + wave; from < end; from += kWaves * 64) {
-      const Next n = look(from, end, w0);
+    for (int from = begin + wave; from < end; from += WAVES * 64) {
+      const Next n = look(from, begin, end, w0);
       uint64_t mask = n.mask;
       if (!mask) continue;
       int i = __builtin_ctzll(mask), page = __builtin_amdgcn_readlane(n.page, i);
@@ -427,19 +441,19 @@ __global__ __launch_bounds__(64 * kWaves, COLS == 32 || CHOSEN ? 3 : 4) void pag
   }
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < COLS / kWaves; ++j) {
-    const int r = wave * (COLS / kWaves) + j, c = lane;
+  for (int j = 0; j < COLS / std::min(WAVES, COLS); ++j) {
+    const int r = wave + j * WAVES, c = lane;
     // (row r's place is what lane r has)
-    if (!__builtin_amdgcn_readlane(b.real, r)) continue;
+    if (!__builtin_amdgcn_readlane(b.real, r)) break;  // (rows that there are come first)
     const int head = __builtin_amdgcn_readlane(b.head, r);
     const int64_t row = b.h.row0 + __builtin_amdgcn_readlane(b.query, r);
     float top = -kInf;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, refs[w][r]);
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, refs[w][r]);
     const float off = off_of(top);
     float l = 0.0f, v = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       const float f = exp2_(refs[w][r] - off);
       l += sums[w][r] * f;
       v += acc[w][r][c] * f;
@@ -478,7 +492,7 @@ template <int COLS, bool CHOSEN>
 __global__ __launch_bounds__(64 * kWaves) void pages_join_kernel(PagesArgs a, int blocks) {
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   Block b;
-  if (!block_of<COLS, CHOSEN>(a, blockIdx.x, 1, blocks, lane % COLS, &b) || b.used == 1) return;
+  if (!block_of<COLS, CHOSEN>(a, blockIdx.x, blocks, lane % COLS, &b) || b.used == 1) return;
 #pragma unroll 1
   for (int r = wave; r < COLS; r += kWaves) {
     if (!__builtin_amdgcn_readlane(b.real, r)) break;
@@ -511,13 +525,14 @@ __global__ __launch_bounds__(64 * kWaves) void pages_join_kernel(PagesArgs a, in
 
 struct Plan {
   long long blocks, units;  // of a sequence and key head; of all
-  int parts, chunk, group, cols;
+  int parts, chunk, group, cols, waves;
 };
 constexpr long long kMostWorkgroups = (1ll << 32) / (64 * kWaves) - 1;  // threads of a launch are counted in 32 bits
 long long times(long long a, long long b) { return b != 0 && a > kMostWorkgroups / b ? kMostWorkgroups + 1 : a * b; }  // as far as it matters
 Plan plan_of(const PagesArgs& a) {
   Plan p;
   const int rep = a.heads / a.kv_heads;
+  const long long items = ((long long)a.longest_k + kPage - 1) / kPage;
   p.chunk = 1;
   p.group = 1;
   p.cols = 16;
@@ -530,22 +545,28 @@ Plan plan_of(const PagesArgs& a) {
     if ((long long)a.longest * rep > 16) p.cols = 32;
     p.blocks = ((long long)a.longest * rep + p.cols - 1) / p.cols;
     p.units = times(times(p.blocks, a.kv_heads), a.sequences);
-    const long long items = ((long long)a.longest_k + kPage - 1) / kPage;
     const long long most = std::min<long long>(std::max<long long>(1024 / std::max(p.units, 1ll), 1), kMostParts);
     p.chunk = (int)std::max<long long>((items + most - 1) / most, kWaves);
+    if (p.blocks == 1) p.chunk = (int)std::min<long long>(p.chunk, std::max<long long>(kLongest, (items + kMostParts - 1) / kMostParts));
     p.parts = (int)std::max<long long>((items + p.chunk - 1) / p.chunk, 1);
   }
   p.parts = std::min(p.parts, kMostParts);
+  p.waves = kWaves;
+  if (!a.chosen && p.cols == 16 && p.parts > 1 && p.units <= kManyUnits && items <= kManyPages) {
+    p.waves = kManyWaves;
+    p.parts = 1;
+    p.chunk = (int)std::max<long long>(items, 1);
+  }
   return p;
 }
 
-template <int COLS, bool CHOSEN>
+template <int COLS, bool CHOSEN, int WAVES = kWaves>
 hipError_t launch(PagesArgs a, const Plan& p, hipStream_t stream) {
   a.parts = p.parts;
   a.chunk = p.chunk;
   a.group = p.group;
   a.part_sums = a.part + (int64_t)a.parts * a.heads * a.rows * kD;
-  pages_attend_kernel<COLS, CHOSEN><<<(int)(p.units * p.parts), 64 * kWaves, 0, stream>>>(a, (int)p.blocks);
+  pages_attend_kernel<COLS, CHOSEN, WAVES><<<(int)(p.units * p.parts), 64 * WAVES, 0, stream>>>(a, (int)p.blocks);
   if (p.parts > 1) pages_join_kernel<COLS, CHOSEN><<<(int)p.units, 64 * kWaves, 0, stream>>>(a, (int)p.blocks);
   return hipGetLastError();
 }
@@ -565,6 +586,7 @@ bool pages_attend_fits(const PagesArgs& a) {
 hipError_t launch_pages_attend(const PagesArgs& a, hipStream_t stream) {
   if (a.sequences == 0 || a.longest == 0) return hipSuccess;
   const Plan p = plan_of(a);
+  if (p.waves == kManyWaves) return launch<16, false, kManyWaves>(a, p, stream);
   return a.chosen ? launch<16, true>(a, p, stream) : p.cols == 16 ? launch<16, false>(a, p, stream) : launch<32, false>(a, p, stream);
 }
 
