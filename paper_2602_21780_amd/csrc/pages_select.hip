@@ -36,6 +36,17 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   return __builtin_bit_cast(uint32_t, p);
 }
 
+// The n-th largest of a wave's keys, one a lane (0 if there are fewer).
+__device__ __forceinline__ uint32_t nth_largest(uint32_t key, int n) {
+  uint32_t x = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t y = x | 1u << bit;
+    x = __popcll(__ballot(key >= y)) >= n ? y : x;
+  }
+  return x;
+}
+
 // N: keys of a query that a lane holds (0: as many as there are, from LDS each time).
 template <int WAVES, int N>
 __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, int queries, int pitch) {
@@ -137,19 +148,64 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
     auto forced = [&](int j) { return j < a.first || j >= np - a.last; };
     uint32_t held_keys[N ? N : 1];
     auto key_at = [&](int i) {  // of page 64 i + lane
-      const int j = 64 * i + lane;
-      const uint32_t k = j < np ? row[j] : 0u;
-      return k && forced(j) ? 0xffffffffu : k;
+      uint32_t k = row[64 * i + lane];
+      if (64 * i < a.first || 64 * i + 64 > np - a.last) {
+        const int j = 64 * i + lane;
+        k = j < np ? k : 0u;
+        k = k && forced(j) ? 0xffffffffu : k;
+      }
+      return k;
     };
+    int32_t* out = a.choice + ((int64_t)(h.row0 + query0 + query) * a.kv_heads + kv) * a.count;
+    const uint64_t before = (1ull << lane) - 1;
     if constexpr (N > 0) {
+      uint32_t most = 0;  // of this lane's keys
 #pragma unroll
-      for (int i = 0; i < N; ++i) held_keys[i] = i < steps ? key_at(i) : 0u;
+      for (int i = 0; i < N; ++i) {
+        held_keys[i] = i < steps ? key_at(i) : 0u;
+        most = max(most, held_keys[i]);
+      }
+      // As many lanes as pages are wanted have a key of at least `least`, so what is below it is not chosen; what is not is rarely more than a key a lane.
+      const int some = __popcll(__ballot(most > 0));
+      if (steps == 1 || some >= a.count) {
+        const int want = min(a.count, some);
+        uint32_t key = most;
+        int page = lane, found = some;
+        if (steps > 1) {
+          const uint32_t least = nth_largest(most, want);
+          found = 0;
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const uint64_t some = __ballot(held_keys[i] >= least);
+            if (some) {
+              const int place = found + __popcll(some & before);
+              if ((some >> lane & 1) && place < 64) {
+                row[place] = held_keys[i];  // (its keys are all in registers)
+                row[64 + place] = 64 * i + lane;
+              }
+              found += __popcll(some);
+            }
+          }
+          if (found <= 64) {
+            key = lane < found ? row[lane] : 0u;
+            page = (int)row[64 + lane];
+          }
+        }
+        if (found <= 64) {
+          const uint32_t nth = want > 0 ? nth_largest(key, want) : 0xffffffffu;
+          const int ties = want - __popcll(__ballot(key > nth));
+          const uint64_t same = __ballot(key == nth && key > 0), takes = __ballot(key > nth || (key == nth && key > 0 && __popcll(same & before) < ties));
+          if (takes >> lane & 1) out[__popcll(takes & before)] = page;
+          for (int j = want + lane; j < a.count; j += 64) out[j] = -1;
+          continue;
+        }
+      }
     }
     auto over = [&](auto f) {  // f(step, key) for every step of 64 pages
       if constexpr (N > 0) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-          if (i < steps) f(i, held_keys[i]);
+          f(i, held_keys[i]);
       } else {
         for (int i = 0; i < steps; ++i) f(i, key_at(i));
       }
@@ -193,9 +249,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
       }
     }
     // In order: the keys above hi, and of those that equal it as many of the first as are left.
-    int32_t* out = a.choice + ((int64_t)(h.row0 + query0 + query) * a.kv_heads + kv) * a.count;
     int done = 0, left = want - above_hi;
-    const uint64_t before = (1ull << lane) - 1;
     over([&](int i, uint32_t k) {
       uint64_t takes = __ballot(k > hi);
       if (left > 0) {
@@ -234,6 +288,16 @@ hipError_t launch(const PagesArgs& a, const Plan& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <int WAVES>
+hipError_t launch_for(const PagesArgs& a, const Plan& p, hipStream_t stream) {
+  const int held = pages_held(a);
+  if (held <= 256) return launch<WAVES, 4>(a, p, stream);
+  if (held <= 512) return launch<WAVES, 8>(a, p, stream);
+  if (held <= 1024) return launch<WAVES, 16>(a, p, stream);
+  if (held <= 2048) return launch<WAVES, 32>(a, p, stream);
+  return launch<WAVES, 0>(a, p, stream);
+}
+
 }  // namespace
 
 bool pages_select_fits(const PagesArgs& a) {
@@ -244,9 +308,8 @@ bool pages_select_fits(const PagesArgs& a) {
 hipError_t launch_pages_select(const PagesArgs& a, hipStream_t stream) {
   if (a.sequences == 0 || a.longest == 0 || a.count == 0) return hipSuccess;
   const Plan p = plan_of(a);
-  const int held = pages_held(a);
-  if (p.queries <= 4) return held <= 512 ? launch<4, 8>(a, p, stream) : held <= 2048 ? launch<4, 32>(a, p, stream) : launch<4, 0>(a, p, stream);
-  return held <= 512 ? launch<16, 8>(a, p, stream) : held <= 2048 ? launch<16, 32>(a, p, stream) : launch<16, 0>(a, p, stream);
+  if (p.queries <= 4) return launch_for<4>(a, p, stream);
+  return launch_for<16>(a, p, stream);
 }
 
 }  // namespace xsv
