@@ -27,6 +27,7 @@ constexpr int kListRows = 16;  // rows that share a list of chosen pages
 // probabilities above 1 are as exact as below.
 constexpr float kMaxPart = 16777216.0f;
 using f32x16 = __attribute__((ext_vector_type(16))) float;
+using lds_byte = __attribute__((address_space(3))) const uint8_t;
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float off_of(float ref) { return ref == -kInf ? 0.0f : ref; }  // (nothing finite seen yet)
@@ -36,6 +37,28 @@ __device__ __forceinline__ float off_of(float ref) { return ref == -kInf ? 0.0f 
 // the rows of A are dealt so that they are runs; and the packed probabilities already are the B operand of the second product.
 template <int COLS>
 struct Shape;
+
+// Pages go through LDS.  A lane's pieces are 64 bytes apart, a row of the page each, and the 16 lanes whose loads the memory path takes together would ask
+// for eight lines; it then takes 30 cycles for a load of 1 KB that takes 16 in order.  In order, each load brings 16 rows to LDS by itself, without
+// registers in between, and the lanes read their pieces there.  The four 16-byte pieces of a row are turned by an amount that goes by the row, so that the
+// eight lanes that read together are in different banks: keys' rows by key_turn(row of 4, which 16 rows), values' by value_turn(row).
+constexpr int kStagedBytes = 2 * kPageBytes;  // of a wave: keys and values of a page
+__device__ __forceinline__ int key_turn(int row, int rows) { return row / 2 % 2 + 2 * (rows % 2); }
+__device__ __forceinline__ int value_turn(int row) { return row / 2 % 4; }
+__device__ __forceinline__ int turned(int piece, int by) { return (piece + by) % 4 * 16; }
+// The 64 rows of a page, in four loads of 1 KB, to LDS at `to`; this lane's piece of 16 rows is `even` bytes behind them in the first and third, `odd`
+// in the others.  (What is in LDS has been read: the wait.  The scalar operands may come from a vector instruction: the wait states.)
+__device__ __forceinline__ void stage(const uint8_t* page, int even, int odd, uint32_t to) {
+  asm volatile(
+      "s_waitcnt lgkmcnt(0)\n\ts_mov_b32 m0, %0\n\ts_nop 4\n\t"
+      "global_load_lds_dwordx4 %1, %3\n\t"
+      "global_load_lds_dwordx4 %2, %3 offset:%4\n\t"
+      "global_load_lds_dwordx4 %1, %3 offset:%5\n\t"
+      "global_load_lds_dwordx4 %2, %3 offset:%6" ::"s"(to), "v"(even), "v"(odd), "s"(page), "i"(16 * kD), "i"(2 * 16 * kD), "i"(3 * 16 * kD) : "memory", "m0");
+}
+__device__ __forceinline__ void wait_for_all() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void wait_for_all_but_four() { asm volatile("s_waitcnt vmcnt(4)" ::: "memory"); }
+
 template <>
 struct Shape<16> {
   using Acc = f32x4;
@@ -48,6 +71,9 @@ struct Shape<16> {
   // key piece i feeds block and steps (of 8 channels a lane); value piece i its block and steps
   static constexpr int key_block(int i) { return i; }
   static constexpr int key_step(int i) { return 0; }
+  // the same pieces in a page that stage() has brought to LDS: `first` and constants
+  __device__ static __forceinline__ int staged_key(int col, int quarter, int i) { return col / 4 * 1024 + col % 4 * 64 + turned(quarter, key_turn(col % 4, col / 4)) + 256 * i; }
+  __device__ static __forceinline__ int staged_value(int col, int quarter, int i) { return col * 64 + turned(quarter, value_turn(col)) + 1024 * i; }
   static constexpr int value_block(int i) { return i; }
   static constexpr int value_step(int i) { return 0; }
   static constexpr int token(int e) { return e; }  // behind 16 * quarter
@@ -77,6 +103,10 @@ struct Shape<32> {
   __device__ static __forceinline__ int query_at(int quarter) { return 32 * quarter; }
   static constexpr int key_block(int i) { return i / 2; }
   static constexpr int key_step(int i) { return i % 2 * 2; }
+  __device__ static __forceinline__ int staged_key(int col, int quarter, int i) {
+    return col / 4 % 2 * 1024 + (4 * (col / 8) + col % 4) * 64 + turned(2 * quarter + i % 2, key_turn(col % 4, col / 4 % 2)) + 2048 * (i / 2);
+  }
+  __device__ static __forceinline__ int staged_value(int col, int quarter, int i) { return col * 64 + turned(2 * (i / 2) + quarter, value_turn(col % 16)) + 2048 * (i % 2); }
   static constexpr int value_block(int i) { return i % 2; }
   static constexpr int value_step(int i) { return i / 2 * 2; }
   static constexpr int token(int e) { return 32 * (e / 16) + e % 16; }  // behind 16 * quarter
@@ -222,7 +252,12 @@ struct Empty {};
 template <int COLS, bool CHOSEN, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || CHOSEN) ? 4 : 3) void pages_attend_kernel(PagesArgs a, int blocks) {
   using S = Shape<COLS>;
-  __shared__ __align__(16) float acc[WAVES][COLS][kD + 4];
+  constexpr bool kStaged = WAVES == kWaves;  // (the destination of such a load has 16 bits: 64 KB)
+  union Share {  // of a wave: its page, later its results, 16-byte pieces of row r in the order of their number xor r
+    uint8_t page[kStagedBytes];
+    f32x4 acc[COLS][kD / 4];
+  };
+  __shared__ __align__(16) Share shares[WAVES];
   __shared__ float refs[WAVES][COLS], sums[WAVES][COLS];
   __shared__ std::conditional_t<CHOSEN, Lists, Empty> lists;
   const int lane = threadIdx.x % 64, col = lane % COLS, quarter = lane / COLS;
@@ -264,21 +299,47 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
     n.mask = __ballot(some);
     return n;
   };
-  u32x4 kr[4];
+  u32x4 kr[4], vr[4];
+  [[maybe_unused]] const uint8_t* staged = shares[wave].page;
+  [[maybe_unused]] const uint32_t staged_at = (uint32_t)(size_t)(lds_byte*)staged;
+  // (what this lane brings: piece lane % 4 of row lane / 4 of 16, which is another one of the row's)
+  [[maybe_unused]] const int key_from = lane / 4 * 64 + (lane - key_turn(lane / 4 % 4, 0)) % 4 * 16, value_from = lane / 4 * 64 + (lane + 4 - value_turn(lane / 4)) % 4 * 16;
   auto fetch_keys = [&](int page) {
     const uint8_t* p = a.k + ((size_t)page * a.kv_heads + b.kv) * kPageBytes;
+    if constexpr (kStaged) {
+      stage(p, key_from, key_from ^ 32, staged_at);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) kr[i] = *reinterpret_cast<const u32x4*>(p + S::key_at(col, quarter, i));
+      for (int i = 0; i < 4; ++i) kr[i] = *reinterpret_cast<const u32x4*>(p + S::key_at(col, quarter, i));
+    }
   };
   constexpr int kEach = S::kLogits / S::kKeys;
-  u32x4 vr[4];
   typename S::Acc x[S::kKeys];
   u32x4 pr[kSteps];
   float part;  // sum of the lane's probabilities in a page
   auto fetch_values = [&](int page) {
     const uint8_t* p = a.v + ((size_t)page * a.kv_heads + b.kv) * kPageBytes;
+    if constexpr (kStaged) {
+      stage(p, value_from, value_from, staged_at + kPageBytes);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) vr[i] = *reinterpret_cast<const u32x4*>(p + S::value_at(col, quarter, i));
+      for (int i = 0; i < 4; ++i) vr[i] = *reinterpret_cast<const u32x4*>(p + S::value_at(col, quarter, i));
+    }
+  };
+  // Staged pages: what is read has been fetched, and at most the last four loads are still on their way.
+  auto take_keys = [&] {
+    if constexpr (kStaged) {
+      wait_for_all_but_four();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) kr[i] = *reinterpret_cast<const u32x4*>(staged + S::staged_key(col, quarter, i));
+    }
+  };
+  auto take_values = [&] {
+    if constexpr (kStaged) {
+      wait_for_all_but_four();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vr[i] = *reinterpret_cast<const u32x4*>(staged + kPageBytes + S::staged_value(col, quarter, i));
+    }
   };
   auto first_products = [&] {
 #pragma unroll
@@ -320,8 +381,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
     const bool mine = !CHOSEN || (rows >> col & 1);
     const int left = mine ? b.seen - ordinal * kPage - 16 * quarter : -kPage;  // of the tokens from the lane's first on
     const float cs = c2 * ks;
+    if constexpr (kStaged) wait_for_all();
+    take_keys();
     first_products();
     fetch_keys(next_page);
+    take_values();
     float m = -kInf;
 #pragma unroll
     for (int e = 0; e < S::kLogits; ++e) {
@@ -371,9 +435,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
   // its own inside the loop, they were copied on the others too, in every page).
   auto over = [&](int begin, int end, int w0) {
     for (int from = begin + wave; from < end; from += WAVES * 64) {
-      const Next n = look(from, begin, end, w0);
+      Next n = look(from, begin, end, w0);
       uint64_t mask = n.mask;
       if (!mask) continue;
+      asm volatile("" : "+v"(n.page), "+v"(n.ordinal), "+v"(n.ks), "+v"(n.vs));  // (what look() loads is there: nothing waits for it, and so for the pages, in the loop)
+      if constexpr (kStaged) wait_for_all();  // (the last page's keys, fetched again)
       int i = __builtin_ctzll(mask), page = __builtin_amdgcn_readlane(n.page, i);
       fetch_keys(page);
       while (true) {
@@ -394,6 +460,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
           if ((ordinal + 1) * kPage > b.least || vs < 0.0f) break;  // some row does not see some of its tokens, or NaN
           const bool mine = !CHOSEN || (rows >> col & 1);
           if (__any(mine && ref == -kInf)) break;  // a row's first page
+          take_keys();
           first_products();
           __builtin_amdgcn_sched_barrier(0);
           fetch_keys(next_page);
@@ -402,6 +469,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
           if (__any(part > kMaxPart)) break;
           __builtin_amdgcn_sched_barrier(0);
           sum += part;
+          take_values();
           second_products();
           done = !mask;
           if (done) break;
@@ -410,7 +478,10 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
           fetched = true;
         }
         if (done) break;
-        if (!fetched) fetch_keys(page);
+        if (!fetched) {
+          if constexpr (kStaged) wait_for_all();  // (what is on its way there is not this page's)
+          fetch_keys(page);
+        }
         whole(ordinal, rows, ks, vs, next_page);
         if (!mask) break;
         i = next;
@@ -429,12 +500,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
   }
 
   // The waves' results.
+  if constexpr (kStaged) wait_for_all();  // (the last page's keys, fetched again)
   const float total = S::column_sum(sum);
 #pragma unroll
   for (int i = 0; i < S::kChannels; ++i)
 #pragma unroll
     for (int j = 0; j < (int)(sizeof(typename S::Acc) / 4); j += 4)
-      *reinterpret_cast<f32x4*>(&acc[wave][col][S::channel(i, quarter, j)]) = f32x4{o[i][j], o[i][j + 1], o[i][j + 2], o[i][j + 3]};
+      shares[wave].acc[col][(S::channel(i, quarter, j) / 4) ^ (col % 16)] = f32x4{o[i][j], o[i][j + 1], o[i][j + 2], o[i][j + 3]};
   if (quarter == 0) {
     refs[wave][col] = ref;
     sums[wave][col] = total;
@@ -456,7 +528,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
     for (int w = 0; w < WAVES; ++w) {
       const float f = exp2_(refs[w][r] - off);
       l += sums[w][r] * f;
-      v += acc[w][r][c] * f;
+      v += shares[w].acc[r][(c / 4) ^ (r % 16)][c % 4] * f;
     }
     if (b.used == 1) {
       const_cast<uint16_t*>(a.out.p)[head * a.out.sh + row * a.out.st + c] = (uint16_t)pack2(l == 0.0f ? 0.0f : v / l, 0.0f);

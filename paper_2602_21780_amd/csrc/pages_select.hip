@@ -11,6 +11,7 @@
 // the pool into keys in LDS; then a wave takes a query, its keys in registers, and halves the interval of keys that its last chosen one lies in
 // until as many keys as wanted lie above it.
 #include <algorithm>
+#include <type_traits>
 
 #include "pages.h"
 
@@ -36,13 +37,32 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   return __builtin_bit_cast(uint32_t, p);
 }
 
-// The n-th largest of a wave's keys, one a lane (0 if there are fewer).
+// Over a wave, in every lane.
+template <typename F>
+__device__ __forceinline__ uint32_t over_wave(uint32_t x, F f) {
+  auto from = [](uint32_t v, auto ctrl) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, decltype(ctrl)::value, 0xf, 0xf, true); };
+  x = f(x, from(x, std::integral_constant<int, 0xb1>{}));   // lane ^ 1
+  x = f(x, from(x, std::integral_constant<int, 0x4e>{}));   // lane ^ 2
+  x = f(x, from(x, std::integral_constant<int, 0x141>{}));  // 7 - lane of eight: the other four
+  x = f(x, from(x, std::integral_constant<int, 0x140>{}));  // 15 - lane of sixteen: the other eight
+  const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = f(p[0], p[1]);
+  const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return f(q[0], q[1]);
+}
+
+// A number that n of a wave's keys, one a lane, are at least (n keys that there are), or more only if they equal it: the n-th largest, or one
+// between it and the next.  Bit by bit, those that the keys have in common left out.
 __device__ __forceinline__ uint32_t nth_largest(uint32_t key, int n) {
-  uint32_t x = 0;
-#pragma unroll
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t y = x | 1u << bit;
-    x = __popcll(__ballot(key >= y)) >= n ? y : x;
+  const uint32_t any = __builtin_amdgcn_readfirstlane(over_wave(key, [](uint32_t x, uint32_t y) { return x | y; }));
+  const uint32_t all = __builtin_amdgcn_readfirstlane(over_wave(key, [](uint32_t x, uint32_t y) { return x & y; }));
+  uint32_t x = all;
+  for (uint32_t left = any & ~all; left;) {
+    const uint32_t bit = 0x80000000u >> __builtin_clz(left);
+    left ^= bit;
+    const int c = __popcll(__ballot(key >= (x | bit)));
+    if (c >= n) x |= bit;
+    if (c == n) break;
   }
   return x;
 }
@@ -65,7 +85,13 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
     for (int i = threadIdx.x; i < n * pitch; i += 64 * WAVES) keys[i] = 0;
     __syncthreads();
   }
+  auto id_of = [&](int turn) {  // the page that the lane looks up for a turn, or none
+    const int ordinal = turn * 32 + lane % 32;
+    const int id = ordinal < pages ? table[ordinal] : -1;
+    return id < a.pages ? id : -1;
+  };
   for (int c0 = 0; c0 < n * rep; c0 += 32) {
+    int id = id_of(wave), id_next = id_of(wave + WAVES);
     // The lane's column, a query of a head, and its channels 32 g .. (columns behind the last are copies of it that change nothing)
     const int col = min(c0 + lane % 32, n * rep - 1), query = col / rep;
     f16x8 above[4], below[4];
@@ -101,9 +127,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
       }
     }
     for (int turn = wave; turn < turns; turn += WAVES) {
-      const int ordinal = turn * 32 + lane % 32;
-      const int id = ordinal < pages ? table[ordinal] : -1;
-      const bool some = id >= 0 && id < a.pages;
+      const bool some = id >= 0;
       const size_t unit = (size_t)(some ? id : 0) * a.kv_heads + kv;
       const u32x4* b = reinterpret_cast<const u32x4*>(a.bounds + unit * 2 * kD) + 4 * g;
       u32x4 hi[4], lo[4];
@@ -113,6 +137,8 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
         lo[i] = b[8 + i];
       }
       const int e = some ? (int)((__float_as_uint(a.k_scale[unit]) >> 23) & 0xffu) - 128 : kHole;
+      id = id_next;
+      id_next = id_of(turn + 2 * WAVES);
       if (g == 0) exponents[wave][lane] = e;  // (read by this wave alone, whose LDS accesses stay in order)
       f32x16 sum = {};
 #pragma unroll
@@ -145,24 +171,23 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
   for (int query = wave; query < n; query += WAVES) {
     const int np = (tokens_seen(a, h, query0 + query) + kPage - 1) / kPage, steps = (np + 63) / 64;
     uint32_t* row = keys + query * pitch;
-    auto forced = [&](int j) { return j < a.first || j >= np - a.last; };
+    // Forced pages' keys are the largest, those behind the last are none.
+    for (int j = lane; j < min(a.first, np); j += 64)
+      if (row[j]) row[j] = 0xffffffffu;
+    for (int j = max(np - a.last, 0) + lane; j < 64 * steps; j += 64) row[j] = j < np && row[j] ? 0xffffffffu : 0u;
     uint32_t held_keys[N ? N : 1];
-    auto key_at = [&](int i) {  // of page 64 i + lane
-      uint32_t k = row[64 * i + lane];
-      if (64 * i < a.first || 64 * i + 64 > np - a.last) {
-        const int j = 64 * i + lane;
-        k = j < np ? k : 0u;
-        k = k && forced(j) ? 0xffffffffu : k;
-      }
-      return k;
-    };
+    auto key_at = [&](int i) { return row[64 * i + lane]; };  // of page 64 i + lane
     int32_t* out = a.choice + ((int64_t)(h.row0 + query0 + query) * a.kv_heads + kv) * a.count;
     const uint64_t before = (1ull << lane) - 1;
+    if (steps == 0) {
+      for (int j = lane; j < a.count; j += 64) out[j] = -1;
+      continue;
+    }
     if constexpr (N > 0) {
       uint32_t most = 0;  // of this lane's keys
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        held_keys[i] = i < steps ? key_at(i) : 0u;
+        held_keys[i] = key_at(min(i, steps - 1)) & (i < steps ? 0xffffffffu : 0u);
         most = max(most, held_keys[i]);
       }
       // As many lanes as pages are wanted have a key of at least `least`, so what is below it is not chosen; what is not is rarely more than a key a lane.
