@@ -149,28 +149,57 @@ struct Block {
   int query0, queries; // chosen pages: the queries of the block
 };
 
+// Block number `*block` of all sequences' blocks of a key head (at most 64 sequences), those of the sequences that see the most pages first, of a sequence the
+// last first: it becomes the number of blocks behind it in its sequence.  A lane looks a sequence up.
+template <int COLS>
+__device__ __forceinline__ bool ranked_block(const PagesArgs& a, int* block, int* sequence, Held* h) {
+  const int lane = threadIdx.x % 64, rep = a.heads / a.kv_heads;
+  Held own{};
+  int blocks = 0, cost = -1, before = 0;
+  if (lane < a.sequences) {
+    own = held(a, lane);
+    blocks = (int)(((int64_t)own.n * rep + COLS - 1) / COLS);
+    cost = own.n > 0 ? tokens_seen(a, own, own.n - 1) : 0;
+  }
+  for (int s = 0; s < a.sequences; ++s) {
+    const int other = __builtin_amdgcn_readlane(cost, s), n = __builtin_amdgcn_readlane(blocks, s);
+    before += other > cost || (other == cost && s < lane) ? n : 0;
+  }
+  const uint64_t here = __ballot(lane < a.sequences && before <= *block && *block < before + blocks);
+  if (!here) return false;
+  const int s = __builtin_ctzll(here);
+  *sequence = s;
+  *block -= __builtin_amdgcn_readlane(before, s);
+  *h = Held{__builtin_amdgcn_readlane(own.row0, s), __builtin_amdgcn_readlane(own.n, s), __builtin_amdgcn_readlane(own.m, s), __builtin_amdgcn_readlane(own.ahead, s)};
+  return true;
+}
+
 // All pages: rows (query, head) COLS at a time.  Chosen pages: `group` queries with their heads, or 16 heads of a query that has more.
 // Sequences' blocks are counted from their ends, so that under a mask those that see the most come first, and those of a short sequence behind a long
-// cache, which see as much, among them.  Workgroups are dealt to the XCDs one by one; where eight divides the key
+// cache, which see as much, among them; up to 64 sequences go by what they see (sequences of 0 to 1374 rows over up to 5470 tokens 55 -> 47 us).  Workgroups are dealt to the XCDs one by one; where eight divides the key
 // heads, each XCD has its own, one after the other, whose pages are then in one L2, and all of whose blocks go through them at about the same time.  A block's parts are far apart: side by side, with eight of them,
 // those of short sequences, which have little or nothing to do, were dealt to the same compute units (64 streams 89 us, 77).
 template <int COLS, bool CHOSEN>
 __device__ __forceinline__ bool block_of(const PagesArgs& a, int number, int blocks, int col, Block* b) {
   const int rep = a.heads / a.kv_heads;
   const int heads = a.kv_heads % 8 ? a.kv_heads : a.kv_heads / 8, at = a.kv_heads % 8 ? number : number / 8;
-  const int units = heads * a.sequences * blocks, unit = at % units;
+  const int sequences = a.ranked ? 1 : a.sequences, units = heads * sequences * blocks, unit = at % units;
   b->part = at / units;
-  int back;  // blocks behind this one
+  int back;  // blocks of the sequence behind this one
   if (a.kv_heads % 8) {
     b->kv = unit % heads;
-    b->s = unit / heads % a.sequences;
-    back = unit / heads / a.sequences;
+    b->s = unit / heads % sequences;
+    back = unit / heads / sequences;
   } else {
-    b->s = unit % a.sequences;
-    back = unit / a.sequences % blocks;
-    b->kv = number % 8 * heads + unit / a.sequences / blocks;
+    b->s = unit % sequences;
+    back = unit / sequences % blocks;
+    b->kv = number % 8 * heads + unit / sequences / blocks;
   }
-  b->h = held(a, b->s);
+  if (a.ranked) {
+    if (!ranked_block<COLS>(a, &back, &b->s, &b->h)) return false;
+  } else {
+    b->h = held(a, b->s);
+  }
   const int per = CHOSEN && rep > COLS ? (rep + COLS - 1) / COLS : 1;  // blocks of a query
   const int block = (CHOSEN ? (b->h.n + a.group - 1) / a.group * per : (int)(((int64_t)b->h.n * rep + COLS - 1) / COLS)) - 1 - back;
   if (block < 0) return false;
@@ -598,11 +627,12 @@ __global__ __launch_bounds__(64 * kWaves) void pages_join_kernel(PagesArgs a, in
 struct Plan {
   long long blocks, units;  // of a sequence and key head; of all
   int parts, chunk, group, cols, waves;
+  bool ranked;                 // `blocks` are those of all sequences, which go by what they see
 };
 constexpr long long kMostWorkgroups = (1ll << 32) / (64 * kWaves) - 1;  // threads of a launch are counted in 32 bits
 long long times(long long a, long long b) { return b != 0 && a > kMostWorkgroups / b ? kMostWorkgroups + 1 : a * b; }  // as far as it matters
 Plan plan_of(const PagesArgs& a) {
-  Plan p;
+  Plan p{};
   const int rep = a.heads / a.kv_heads;
   const long long items = ((long long)a.longest_k + kPage - 1) / kPage;
   p.chunk = 1;
@@ -616,10 +646,12 @@ Plan plan_of(const PagesArgs& a) {
   } else {
     if ((long long)a.longest * rep > 16) p.cols = 32;
     p.blocks = ((long long)a.longest * rep + p.cols - 1) / p.cols;
-    p.units = times(times(p.blocks, a.kv_heads), a.sequences);
+    p.ranked = p.blocks > 1 && a.sequences > 1 && a.sequences <= 64;
+    if (p.ranked) p.blocks = std::min(p.blocks * a.sequences, ((long long)a.rows * rep + p.cols - 1) / p.cols + a.sequences);  // of all sequences
+    p.units = times(times(p.blocks, a.kv_heads), p.ranked ? 1 : a.sequences);
     const long long most = std::min<long long>(std::max<long long>(1024 / std::max(p.units, 1ll), 1), kMostParts);
     p.chunk = (int)std::max<long long>((items + most - 1) / most, kWaves);
-    if (p.blocks == 1) p.chunk = (int)std::min<long long>(p.chunk, std::max<long long>(kLongest, (items + kMostParts - 1) / kMostParts));
+    if (!p.ranked && p.blocks == 1) p.chunk = (int)std::min<long long>(p.chunk, std::max<long long>(kLongest, (items + kMostParts - 1) / kMostParts));
     p.parts = (int)std::max<long long>((items + p.chunk - 1) / p.chunk, 1);
   }
   p.parts = std::min(p.parts, kMostParts);
@@ -637,6 +669,7 @@ hipError_t launch(PagesArgs a, const Plan& p, hipStream_t stream) {
   a.parts = p.parts;
   a.chunk = p.chunk;
   a.group = p.group;
+  a.ranked = p.ranked;
   a.part_sums = a.part + (int64_t)a.parts * a.heads * a.rows * kD;
   pages_attend_kernel<COLS, CHOSEN, WAVES><<<(int)(p.units * p.parts), 64 * WAVES, 0, stream>>>(a, (int)p.blocks);
   if (p.parts > 1) pages_join_kernel<COLS, CHOSEN><<<(int)p.units, 64 * kWaves, 0, stream>>>(a, (int)p.blocks);
