@@ -41,7 +41,8 @@ struct Shape;
 // Pages go through LDS.  A lane's pieces are 64 bytes apart, a row of the page each, and the 16 lanes whose loads the memory path takes together would ask
 // for eight lines; it then takes 30 cycles for a load of 1 KB that takes 16 in order.  In order, each load brings 16 rows to LDS by itself, without
 // registers in between, and the lanes read their pieces there.  The four 16-byte pieces of a row are turned by an amount that goes by the row, so that the
-// eight lanes that read together are in different banks: keys' rows by key_turn(row of 4, which 16 rows), values' by value_turn(row).
+// eight lanes that read together are in different banks: keys' rows by key_turn(row of 4, which 16 rows), values' by value_turn(row).  (64 streams 82 -> 79 us,
+// a frame over chosen pages 121 -> 115.  With 32 columns arithmetic hides it, and loads to registers are faster: a frame 49 us, 51 through LDS.)
 constexpr int kStagedBytes = 2 * kPageBytes;  // of a wave: keys and values of a page
 __device__ __forceinline__ int key_turn(int row, int rows) { return row / 2 % 2 + 2 * (rows % 2); }
 __device__ __forceinline__ int value_turn(int row) { return row / 2 % 4; }
@@ -281,7 +282,7 @@ struct Empty {};
 template <int COLS, bool CHOSEN, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || CHOSEN) ? 4 : 3) void pages_attend_kernel(PagesArgs a, int blocks) {
   using S = Shape<COLS>;
-  constexpr bool kStaged = WAVES == kWaves;  // (the destination of such a load has 16 bits: 64 KB)
+  constexpr bool kStaged = COLS == 16 && WAVES == kWaves;  // (the destination of such a load has 16 bits: 64 KB)
   union Share {  // of a wave: its page, later its results, 16-byte pieces of row r in the order of their number xor r
     uint8_t page[kStagedBytes];
     f32x4 acc[COLS][kD / 4];

@@ -7,11 +7,10 @@
 // and all partial sums below 64 * 255 * 896 < 2^24, so that fp32 holds each exactly in any order: the same pages whatever
 // computes them, and equal scores are equal.  A row's `first` and `last` pages are chosen whatever their scores; equal scores go to the lower page.
 //
-// A workgroup has some queries of one key head, 32 rows (query, head) of a product if it can, whose pages it scores together, 32 a wave and turn, from
-// the pool into keys in LDS; then a wave takes a query, its keys in registers, and halves the interval of keys that its last chosen one lies in
-// until as many keys as wanted lie above it.
+// A workgroup has some queries of one key head, 32 rows (query, head) of a product if it can, whose pages it scores together, 16 a wave and turn, from
+// the pool into keys in LDS; then a wave takes a query, its keys in registers: the n-th largest of each lane's largest is a bound that few more than n keys
+// pass, and those are looked at one a lane.
 #include <algorithm>
-#include <type_traits>
 
 #include "pages.h"
 
@@ -20,14 +19,13 @@ namespace {
 
 using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
 using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
-using f32x16 = __attribute__((ext_vector_type(16))) float;
 
 constexpr int kMostPages = 32768;  // scores of a row's pages are held in LDS
-constexpr int kMostKeys = 32768;   // of a workgroup
-constexpr int kHole = INT32_MIN;
+constexpr int kMostKeys = 32768;   // of a workgroup: 128 KB, and 32 for the scoring waves' pieces
+constexpr int kHole = -(1 << 20);  // the exponent of a page that is none
 
 __device__ __forceinline__ uint32_t ordered(float x) {  // larger numbers, larger keys; 0 and the largest are for other uses
-  const uint32_t b = __float_as_uint(x + 0.0f);         // (0 of either sign is +0)
+  const uint32_t b = __float_as_uint(x);                // (a sum that begins with +0 is never -0)
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
@@ -37,32 +35,19 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   return __builtin_bit_cast(uint32_t, p);
 }
 
-// Over a wave, in every lane.
-template <typename F>
-__device__ __forceinline__ uint32_t over_wave(uint32_t x, F f) {
-  auto from = [](uint32_t v, auto ctrl) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, decltype(ctrl)::value, 0xf, 0xf, true); };
-  x = f(x, from(x, std::integral_constant<int, 0xb1>{}));   // lane ^ 1
-  x = f(x, from(x, std::integral_constant<int, 0x4e>{}));   // lane ^ 2
-  x = f(x, from(x, std::integral_constant<int, 0x141>{}));  // 7 - lane of eight: the other four
-  x = f(x, from(x, std::integral_constant<int, 0x140>{}));  // 15 - lane of sixteen: the other eight
-  const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  x = f(p[0], p[1]);
-  const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-  return f(q[0], q[1]);
-}
+constexpr int kPieceWords = 16 * kD;  // of LDS a scoring wave, to bring 16 pages' bounds into the order of a product's rows
+// Where a query's keys are turned to, so that what 16 queries side by side write is in different banks.
+__device__ __forceinline__ int key_turn(int query) { return query % 16 * 4; }
 
-// A number that n of a wave's keys, one a lane, are at least (n keys that there are), or more only if they equal it: the n-th largest, or one
-// between it and the next.  Bit by bit, those that the keys have in common left out.
+// The first BITS bits of the n-th largest of a wave's keys, one a lane (0 if there are fewer), two bits at a time: the three counts do not wait for one another.
+template <int BITS>
 __device__ __forceinline__ uint32_t nth_largest(uint32_t key, int n) {
-  const uint32_t any = __builtin_amdgcn_readfirstlane(over_wave(key, [](uint32_t x, uint32_t y) { return x | y; }));
-  const uint32_t all = __builtin_amdgcn_readfirstlane(over_wave(key, [](uint32_t x, uint32_t y) { return x & y; }));
-  uint32_t x = all;
-  for (uint32_t left = any & ~all; left;) {
-    const uint32_t bit = 0x80000000u >> __builtin_clz(left);
-    left ^= bit;
-    const int c = __popcll(__ballot(key >= (x | bit)));
-    if (c >= n) x |= bit;
-    if (c == n) break;
+  uint32_t x = 0;
+#pragma unroll
+  for (int bit = 30; bit > 30 - BITS; bit -= 2) {
+    const uint32_t y1 = x | 1u << bit, y2 = x | 2u << bit, y3 = x | 3u << bit;
+    const int c1 = __popcll(__ballot(key >= y1)), c2 = __popcll(__ballot(key >= y2)), c3 = __popcll(__ballot(key >= y3));
+    x = c3 >= n ? y3 : c2 >= n ? y2 : c1 >= n ? y1 : x;
   }
   return x;
 }
@@ -70,9 +55,8 @@ __device__ __forceinline__ uint32_t nth_largest(uint32_t key, int n) {
 // N: keys of a query that a lane holds (0: as many as there are, from LDS each time).
 template <int WAVES, int N>
 __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, int queries, int pitch) {
-  extern __shared__ __align__(16) uint32_t keys[];  // [queries][pitch]
-  __shared__ __align__(16) int exponents[WAVES][32];
-  const int lane = threadIdx.x % 64, g = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  extern __shared__ __align__(16) uint32_t keys[];  // [queries][pitch], of page j of query r at j ^ key_turn(r); behind them a piece of each scoring wave
+  const int lane = threadIdx.x % 64, u = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int rep = a.heads / a.kv_heads, groups = (a.longest + queries - 1) / queries;
   const int kv = blockIdx.x % a.kv_heads, group = blockIdx.x / a.kv_heads % groups, s = blockIdx.x / a.kv_heads / groups;
   const Held h = held(a, s);
@@ -80,28 +64,58 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
   if (n <= 0) return;
   const int32_t* table = a.table + (int64_t)s * a.width;
   const int pages = (tokens_seen(a, h, query0 + n - 1) + kPage - 1) / kPage;  // (queries ascend, and so does what they see)
-  const int turns = a.pages > 0 ? (pages + 31) / 32 : 0;
+  const int turns = a.pages > 0 ? (pages + 15) / 16 : 0;
   if (rep > 1 || turns == 0) {
     for (int i = threadIdx.x; i < n * pitch; i += 64 * WAVES) keys[i] = 0;
     __syncthreads();
   }
-  auto id_of = [&](int turn) {  // the page that the lane looks up for a turn, or none
-    const int ordinal = turn * 32 + lane % 32;
+  constexpr int kScoring = WAVES < 8 ? WAVES : 8;  // waves that score: their pieces of LDS are all that the keys leave
+  uint32_t* piece = keys + queries * pitch + wave * kPieceWords;
+  auto id_of = [&](int ordinal) {  // a page of the pool, or none
     const int id = ordinal < pages ? table[ordinal] : -1;
     return id < a.pages ? id : -1;
   };
-  for (int c0 = 0; c0 < n * rep; c0 += 32) {
-    int id = id_of(wave), id_next = id_of(wave + WAVES);
-    // The lane's column, a query of a head, and its channels 32 g .. (columns behind the last are copies of it that change nothing)
-    const int col = min(c0 + lane % 32, n * rep - 1), query = col / rep;
-    f16x8 above[4], below[4];
-    int t;
-    {
-      const uint16_t* q = a.q.p + (int64_t)(kv * rep + col % rep) * a.q.sh + (h.row0 + query0 + query) * a.q.st + 32 * g;
-      float x[32], m = 0.0f;
+  for (int c0 = 0; c0 < n * rep && wave < kScoring; c0 += 32) {
+    // Of a turn's 16 pages the lane has page lane % 16 in the product, and 16 bytes of the bounds of pages 4 (lane / 16) + i on their way there: 16 lanes
+    // side by side take a page's 256 bytes (with a page to a lane, every lane asks for a line of its own, and a load takes the memory path 59 cycles, not 16).
+    // Pages are looked up two turns ahead, and their bounds fetched one.
+    struct Ahead {
+      int ids[4];
+    };
+    struct Way {
+      u32x4 bounds[4];
+      int exponents[4];
+    };
+    auto look = [&](int turn) {
+      Ahead n;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) n.ids[i] = id_of(16 * turn + 4 * u + i);
+      return n;
+    };
+    auto fetch = [&](const Ahead& n) {
+      Way w;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(q + 8 * i);
+        const size_t unit = (size_t)max(n.ids[i], 0) * a.kv_heads + kv;
+        w.bounds[i] = *reinterpret_cast<const u32x4*>(a.bounds + unit * 2 * kD + lane % 16 * 8);
+        const int e = (int)((__float_as_uint(a.k_scale[unit]) >> 23) & 0xffu) - 128;
+        w.exponents[i] = n.ids[i] >= 0 ? e : kHole;
+      }
+      return w;
+    };
+    Ahead ahead = look(wave);
+    // The lane's two columns, a query of a head each, and 8 channels of each half (columns behind the last are copies of it that change nothing)
+    int query[2], t[2];
+    f16x8 rows[2][4];  // channels 8 u .., 32 + 8 u .. above zero, and below
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int col = min(c0 + 16 * c + lane % 16, n * rep - 1);
+      query[c] = col / rep;
+      const uint16_t* q = a.q.p + (int64_t)(kv * rep + col % rep) * a.q.sh + (h.row0 + query0 + query[c]) * a.q.st + 8 * u;
+      float x[16], m = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(q + 32 * i);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           x[8 * i + 2 * j] = (w[j] & 0x7f80u) == 0x7f80u ? 0.0f : bf16_low(w[j]);
@@ -109,12 +123,13 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
         }
       }
 #pragma unroll
-      for (int i = 0; i < 32; ++i) m = fmaxf(m, fabsf(x[i]));
+      for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[i]));
+      m = fmaxf(m, __shfl_xor(m, 16));
       m = fmaxf(m, __shfl_xor(m, 32));
-      t = max((int)(__float_as_uint(m) >> 23) - 127, -119) - 7;  // (below 2^-119: as if it were 2^-119, which fp32 can turn round)
-      const float f = power(-t);
+      t[c] = max((int)(__float_as_uint(m) >> 23) - 127, -119) - 7;  // (below 2^-119: as if it were 2^-119, which fp32 can turn round)
+      const float f = power(-t[c]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 2; ++i) {
         u32x4 up, down;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -122,41 +137,37 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
           up[j] = pack_f16(fmaxf(y, 0.0f), fmaxf(z, 0.0f));
           down[j] = pack_f16(fminf(y, 0.0f), fminf(z, 0.0f));
         }
-        above[i] = __builtin_bit_cast(f16x8, up);
-        below[i] = __builtin_bit_cast(f16x8, down);
+        rows[c][i] = __builtin_bit_cast(f16x8, up);
+        rows[c][2 + i] = __builtin_bit_cast(f16x8, down);
       }
     }
-    for (int turn = wave; turn < turns; turn += WAVES) {
-      const bool some = id >= 0;
-      const size_t unit = (size_t)(some ? id : 0) * a.kv_heads + kv;
-      const u32x4* b = reinterpret_cast<const u32x4*>(a.bounds + unit * 2 * kD) + 4 * g;
-      u32x4 hi[4], lo[4];
+    auto score = [&](const Way& w, int turn) {
+      // through this wave's piece of LDS (its accesses stay in order); a page's 16-byte pieces are turned so that lanes that read together are in different banks
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        hi[i] = b[i];
-        lo[i] = b[8 + i];
+        const int r = 4 * u + i;
+        *reinterpret_cast<u32x4*>(piece + r * kD + ((lane % 16) ^ (r % 8)) * 4) = w.bounds[i];
       }
-      const int e = some ? (int)((__float_as_uint(a.k_scale[unit]) >> 23) & 0xffu) - 128 : kHole;
-      id = id_next;
-      id_next = id_of(turn + 2 * WAVES);
-      if (g == 0) exponents[wave][lane] = e;  // (read by this wave alone, whose LDS accesses stay in order)
-      f32x16 sum = {};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, hi[i]), above[i], sum, 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lo[i]), below[i], sum, 0, 0, 0);
       __builtin_amdgcn_wave_barrier();
-      // the lane has pages 8 i + 4 g + 0..3 of the 32 for its column
+      f16x8 b[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int s = 0; s < 4; ++s) b[s] = *reinterpret_cast<const f16x8*>(piece + lane % 16 * kD + ((4 * s + u) ^ (lane % 8)) * 4);
+      __builtin_amdgcn_wave_barrier();
+      f32x4 sum[2] = {};
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[s], rows[c][s], sum[c], 0, 0, 0);
+      // the lane has pages 4 u + 0..3 of the 16 for its columns
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
         u32x4 key;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int e = exponents[wave][8 * i + 4 * g + j];
-          const uint32_t k = ordered(sum[4 * i + j] * power(min(max(t + max(e, -1000), -100), 100)));
-          key[j] = e == kHole ? 0u : k;
+          const uint32_t k = ordered(__builtin_amdgcn_ldexpf(sum[c][j], min(max(t[c] + w.exponents[j], -100), 100)));
+          key[j] = w.exponents[j] == kHole ? 0u : k;
         }
-        uint32_t* to = keys + query * pitch + turn * 32 + 8 * i + 4 * g;
+        uint32_t* to = keys + query[c] * pitch + ((turn * 16 + 4 * u) ^ key_turn(query[c]));
         if (rep == 1) {
           *reinterpret_cast<u32x4*>(to) = key;
         } else {
@@ -164,7 +175,19 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
           for (int j = 0; j < 4; ++j) atomicMax(to + j, key[j]);
         }
       }
-      __builtin_amdgcn_wave_barrier();
+    };
+    Way way = fetch(ahead), other;
+    ahead = look(wave + kScoring);
+    for (int turn = wave; turn < turns;) {
+      other = fetch(ahead);
+      ahead = look(turn + 2 * kScoring);
+      score(way, turn);
+      turn += kScoring;
+      if (turn >= turns) break;
+      way = fetch(ahead);
+      ahead = look(turn + 2 * kScoring);
+      score(other, turn);
+      turn += kScoring;
     }
   }
   __syncthreads();
@@ -172,11 +195,12 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
     const int np = (tokens_seen(a, h, query0 + query) + kPage - 1) / kPage, steps = (np + 63) / 64;
     uint32_t* row = keys + query * pitch;
     // Forced pages' keys are the largest, those behind the last are none.
+    const int turned = key_turn(query);
     for (int j = lane; j < min(a.first, np); j += 64)
-      if (row[j]) row[j] = 0xffffffffu;
-    for (int j = max(np - a.last, 0) + lane; j < 64 * steps; j += 64) row[j] = j < np && row[j] ? 0xffffffffu : 0u;
+      if (row[j ^ turned]) row[j ^ turned] = 0xffffffffu;
+    for (int j = max(np - a.last, 0) + lane; j < 64 * steps; j += 64) row[j ^ turned] = j < np && row[j ^ turned] ? 0xffffffffu : 0u;
     uint32_t held_keys[N ? N : 1];
-    auto key_at = [&](int i) { return row[64 * i + lane]; };  // of page 64 i + lane
+    auto key_at = [&](int i) { return row[64 * i + (lane ^ turned)]; };  // of page 64 i + lane
     int32_t* out = a.choice + ((int64_t)(h.row0 + query0 + query) * a.kv_heads + kv) * a.count;
     const uint64_t before = (1ull << lane) - 1;
     if (steps == 0) {
@@ -197,7 +221,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
         uint32_t key = most;
         int page = lane, found = some;
         if (steps > 1) {
-          const uint32_t least = nth_largest(most, want);
+          const uint32_t least = nth_largest<20>(most, want);  // (or a little less)
           found = 0;
 #pragma unroll
           for (int i = 0; i < N; ++i) {
@@ -217,7 +241,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
           }
         }
         if (found <= 64) {
-          const uint32_t nth = want > 0 ? nth_largest(key, want) : 0xffffffffu;
+          const uint32_t nth = want > 0 ? nth_largest<32>(key, want) : 0xffffffffu;
           const int ties = want - __popcll(__ballot(key > nth));
           const uint64_t same = __ballot(key == nth && key > 0), takes = __ballot(key > nth || (key == nth && key > 0 && __popcll(same & before) < ties));
           if (takes >> lane & 1) out[__popcll(takes & before)] = page;
@@ -293,18 +317,18 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
 int pages_held(const PagesArgs& a) { return std::min(a.width, (int)(((long long)a.longest_k + kPage - 1) / kPage)); }
 
 struct Plan {
-  int queries, pitch;  // of a workgroup; keys of a query (four more than a multiple of 64: queries side by side are in different banks)
+  int queries, pitch;  // of a workgroup; keys of a query
 };
 Plan plan_of(const PagesArgs& a) {
   Plan p;
-  p.pitch = (std::max(pages_held(a), 1) + 63) / 64 * 64 + 4;
-  p.queries = std::max(std::min({32 / (a.heads / a.kv_heads), a.longest, kMostKeys / (p.pitch - 4)}), 1);
+  p.pitch = (std::max(pages_held(a), 1) + 63) / 64 * 64;
+  p.queries = std::max(std::min({32 / (a.heads / a.kv_heads), a.longest, kMostKeys / p.pitch}), 1);
   return p;
 }
 
 template <int WAVES, int N>
 hipError_t launch(const PagesArgs& a, const Plan& p, hipStream_t stream) {
-  const int bytes = p.queries * p.pitch * (int)sizeof(uint32_t), groups = (a.longest + p.queries - 1) / p.queries;
+  const int bytes = (p.queries * p.pitch + std::min(WAVES, 8) * kPieceWords) * (int)sizeof(uint32_t), groups = (a.longest + p.queries - 1) / p.queries;
   if (bytes > (48 << 10)) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_select_kernel<WAVES, N>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
