@@ -20,6 +20,7 @@ namespace {
 using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
 using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
 
+constexpr int kFewTurns = 2;
 constexpr int kMostPages = 32768;  // scores of a row's pages are held in LDS
 constexpr int kMostKeys = 32768;   // of a workgroup: 128 KB, and 32 for the scoring waves' pieces
 constexpr int kHole = -(1 << 20);  // the exponent of a page that is none
@@ -64,8 +65,9 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
   if (n <= 0) return;
   const int32_t* table = a.table + (int64_t)s * a.width;
   const int pages = (tokens_seen(a, h, query0 + n - 1) + kPage - 1) / kPage;  // (queries ascend, and so does what they see)
-  const int turns = a.pages > 0 ? (pages + 15) / 16 : 0;
-  if (rep > 1 || turns == 0) {
+  constexpr int kTurns = WAVES == 4 ? kFewTurns : 4, kChunk = 16 * kTurns;  // pages that a wave looks up together
+  const int chunks = a.pages > 0 ? (pages + kChunk - 1) / kChunk : 0;
+  if (rep > 1 || chunks == 0) {
     for (int i = threadIdx.x; i < n * pitch; i += 64 * WAVES) keys[i] = 0;
     __syncthreads();
   }
@@ -75,35 +77,24 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
     const int id = ordinal < pages ? table[ordinal] : -1;
     return id < a.pages ? id : -1;
   };
-  for (int c0 = 0; c0 < n * rep && wave < kScoring; c0 += 32) {
-    // Of a turn's 16 pages the lane has page lane % 16 in the product, and 16 bytes of the bounds of pages 4 (lane / 16) + i on their way there: 16 lanes
-    // side by side take a page's 256 bytes (with a page to a lane, every lane asks for a line of its own, and a load takes the memory path 59 cycles, not 16).
-    // Pages are looked up two turns ahead, and their bounds fetched one.
-    struct Ahead {
-      int ids[4];
-    };
+  for (int c0 = 0; c0 < n * rep && wave < min(kScoring, chunks); c0 += 32) {
+    // A wave takes kChunk pages, one to a lane, that are looked up together while those before them are worked on, and then 16 at a time.  Of those, the lane has
+    // page lane % 16 in the product, and 16 bytes of the bounds of pages 4 (lane / 16) + i on their way there: 16 lanes side by side take a page's 256 bytes (with
+    // a page to a lane, every lane asks for a line of its own, and a load takes the memory path 59 cycles instead of 16).
     struct Way {
       u32x4 bounds[4];
-      int exponents[4];
     };
-    auto look = [&](int turn) {
-      Ahead n;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) n.ids[i] = id_of(16 * turn + 4 * u + i);
-      return n;
-    };
-    auto fetch = [&](const Ahead& n) {
+    auto fetch = [&](int id, int turn) {
       Way w;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const size_t unit = (size_t)max(n.ids[i], 0) * a.kv_heads + kv;
-        w.bounds[i] = *reinterpret_cast<const u32x4*>(a.bounds + unit * 2 * kD + lane % 16 * 8);
-        const int e = (int)((__float_as_uint(a.k_scale[unit]) >> 23) & 0xffu) - 128;
-        w.exponents[i] = n.ids[i] >= 0 ? e : kHole;
-      }
+      for (int i = 0; i < 4; ++i)
+        w.bounds[i] = *reinterpret_cast<const u32x4*>(a.bounds + ((size_t)max(__shfl(id, 16 * turn + 4 * u + i), 0) * a.kv_heads + kv) * 2 * kD + lane % 16 * 8);
       return w;
     };
-    Ahead ahead = look(wave);
+    auto exponent_of = [&](int id) {
+      return id >= 0 ? (int)((__float_as_uint(a.k_scale[(size_t)id * a.kv_heads + kv]) >> 23) & 0xffu) - 128 : kHole;
+    };
+    int id = id_of(kChunk * wave + lane);
     // The lane's two columns, a query of a head each, and 8 channels of each half (columns behind the last are copies of it that change nothing)
     int query[2], t[2];
     f16x8 rows[2][4];  // channels 8 u .., 32 + 8 u .. above zero, and below
@@ -141,7 +132,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
         rows[c][2 + i] = __builtin_bit_cast(f16x8, down);
       }
     }
-    auto score = [&](const Way& w, int turn) {
+    auto score = [&](const Way& w, int exponent, int chunk, int turn) {
       // through this wave's piece of LDS (its accesses stay in order); a page's 16-byte pieces are turned so that lanes that read together are in different banks
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -159,15 +150,18 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
 #pragma unroll
         for (int c = 0; c < 2; ++c) sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[s], rows[c][s], sum[c], 0, 0, 0);
       // the lane has pages 4 u + 0..3 of the 16 for its columns
+      int e[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) e[j] = __shfl(exponent, 16 * turn + 4 * u + j);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         u32x4 key;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t k = ordered(__builtin_amdgcn_ldexpf(sum[c][j], min(max(t[c] + w.exponents[j], -100), 100)));
-          key[j] = w.exponents[j] == kHole ? 0u : k;
+          const uint32_t k = ordered(__builtin_amdgcn_ldexpf(sum[c][j], min(max(t[c] + e[j], -100), 100)));
+          key[j] = e[j] == kHole ? 0u : k;
         }
-        uint32_t* to = keys + query[c] * pitch + ((turn * 16 + 4 * u) ^ key_turn(query[c]));
+        uint32_t* to = keys + query[c] * pitch + ((kChunk * chunk + 16 * turn + 4 * u) ^ key_turn(query[c]));
         if (rep == 1) {
           *reinterpret_cast<u32x4*>(to) = key;
         } else {
@@ -176,18 +170,16 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
         }
       }
     };
-    Way way = fetch(ahead), other;
-    ahead = look(wave + kScoring);
-    for (int turn = wave; turn < turns;) {
-      other = fetch(ahead);
-      ahead = look(turn + 2 * kScoring);
-      score(way, turn);
-      turn += kScoring;
-      if (turn >= turns) break;
-      way = fetch(ahead);
-      ahead = look(turn + 2 * kScoring);
-      score(other, turn);
-      turn += kScoring;
+    Way way = fetch(id, 0);
+    for (int chunk = wave; chunk < chunks; chunk += kScoring) {
+      const int next = id_of(kChunk * (chunk + kScoring) + lane), exponent = exponent_of(id);
+#pragma unroll
+      for (int turn = 0; turn < kTurns; ++turn) {
+        const Way now = way;
+        way = turn < kTurns - 1 ? fetch(id, turn + 1) : fetch(next, 0);
+        score(now, exponent, chunk, turn);
+      }
+      id = next;
     }
   }
   __syncthreads();
