@@ -124,7 +124,10 @@ __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int 
     k.load(a.keys.p + head * a.keys.sh + row * a.keys.st + ch0);
     v.load(a.values.p + head * a.values.sh + row * a.values.st + ch0);
   }
+  float scale_k = 0.0f, scale_v = 0.0f;  // that the page has (exponents below those of any: none)
   if (t.from > 0) {
+    scale_k = a.k_scale[unit];
+    scale_v = a.v_scale[unit];
     if (is_old) old_k = *reinterpret_cast<const u32x4*>(to_k);
     old_v = *reinterpret_cast<const u32x4*>(to_v);
   }
@@ -140,7 +143,7 @@ __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int 
     uint32_t m = 0;
 #pragma unroll
     for (int w = 0; w < kThreads / 64; ++w) m = max(m, top[x][w]);
-    const int e_old = t.from > 0 ? power_of((x ? a.v_scale : a.k_scale)[unit]) : -100;
+    const int e_old = t.from > 0 ? power_of(x ? scale_v : scale_k) : -100;
     e[x] = max(exponent_of(m), e_old);
     grown[x] = t.from > 0 ? e[x] - e_old : 0;
   }
@@ -173,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int 
   }
   if (t.from == 0 || (place + 16 > t.from && place < t.to) || (grown[1] > 0 && place < t.from)) *reinterpret_cast<u32x4*>(to_v) = nv;
   if (tid == 0) {
-    bool negative = t.from > 0 && a.v_scale[unit] < 0.0f;
+    bool negative = scale_v < 0.0f;
 #pragma unroll
     for (int w = 0; w < kThreads / 64; ++w) negative |= none[w] != 0;
     a.k_scale[unit] = power(e[0]);

@@ -405,12 +405,15 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
       for (int k = 0; k < 2; ++k)
         o[S::value_block(i)] = S::mfma(view8(vr[i][2 * k], vr[i][2 * k + 1]), __builtin_bit_cast(bf16x8, pr[S::value_step(i) + k]), o[S::value_block(i)]);
   };
-  auto exponent_of = [](float scale) { return (int)((__float_as_uint(scale) >> 23) & 0xffu) - 127; };
+  // (a page that was never written may have any scale: 0 would leave nothing of its probabilities)
+  auto exponent_of = [](float scale) { return min(max((int)((__float_as_uint(scale) >> 23) & 0xffu) - 127, -100), 120); };
+  // What logits of a page are multiplied by, never 0: masked ones are -inf.
+  auto factor_of = [&](float scale) { return fmaxf(c2 * scale, 1.17549435e-38f); };
   // A page with all that may happen: rows that do not see some of it, references that move, values that are NaN.
   auto whole = [&](int ordinal, uint32_t rows, float ks, float vs, int next_page) {
     const bool mine = !CHOSEN || (rows >> col & 1);
     const int left = mine ? b.seen - ordinal * kPage - 16 * quarter : -kPage;  // of the tokens from the lane's first on
-    const float cs = c2 * ks;
+    const float cs = factor_of(ks);
     if constexpr (kStaged) wait_for_all();
     take_keys();
     first_products();
@@ -468,10 +471,10 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
       Next n = look(from, begin, end, w0);
       uint64_t mask = n.mask;
       if (!mask) continue;
-      asm volatile("" : "+v"(n.page), "+v"(n.ordinal), "+v"(n.ks), "+v"(n.vs));  // (what look() loads is there: nothing waits for it, and so for the pages, in the loop)
       if constexpr (kStaged) wait_for_all();  // (the last page's keys, fetched again)
       int i = __builtin_ctzll(mask), page = __builtin_amdgcn_readlane(n.page, i);
       fetch_keys(page);
+      asm volatile("" : "+v"(n.ks), "+v"(n.vs));  // (what look() loads is there: nothing waits for it, and so for the pages, in the loop)
       while (true) {
         int ordinal;
         uint32_t rows;
@@ -494,7 +497,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
           first_products();
           __builtin_amdgcn_sched_barrier(0);
           fetch_keys(next_page);
-          weigh(c2 * ks, exponent_of(vs), mine);
+          weigh(factor_of(ks), exponent_of(vs), mine);
           fetched = false;
           if (__any(part > kMaxPart)) break;
           __builtin_amdgcn_sched_barrier(0);

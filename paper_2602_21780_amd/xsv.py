@@ -672,7 +672,7 @@ class Pages:
         if k_bounds is not None:
             _plain(k_bounds, "k_bounds", torch.float16, (n, heads, 2, 64), dev)
         self.k, self.v, self.k_scale, self.v_scale, self.k_bounds = k, v, k_scale, v_scale, k_bounds
-        self.count, self.kv_heads, self.device = n, heads, dev
+        self.count, self.kv_heads, self.device, self.index = n, heads, dev, k.get_device()
         self._fields = (n, heads, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(k_bounds))
 
     @classmethod
@@ -685,14 +685,15 @@ class Pages:
 
     def _at(self, begin, table, lengths):
         """xsv_pages of a call, after the checks that need the torch tensors."""
-        n = lengths.numel() if isinstance(lengths, torch.Tensor) else -1
-        if n < 0 or not isinstance(table, torch.Tensor) or table.dim() != 2:
-            raise ValueError("table: expected int32 [sequences][width], lengths: int32 [sequences]")
-        width = table.shape[1]
-        _plain(table, "table", torch.int32, (n, width), self.device)
-        _plain(lengths, "lengths", torch.int32, (n,), self.device)
-        _plain(begin, "begin", torch.int32, (n + 1,), self.device)
-        return xsv_pages(*self._fields, n, width, table.data_ptr(), lengths.data_ptr())
+        index = self.index
+        for name, t in (("begin", begin), ("table", table), ("lengths", lengths)):
+            if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or not t.is_contiguous() or t.get_device() != index:
+                raise ValueError(f"{name}: expected a contiguous int32 tensor on {self.device}")
+        n = lengths.shape[0] if lengths.dim() == 1 else -1
+        shape = table.shape
+        if len(shape) != 2 or shape[0] != n or begin.shape != (n + 1,):
+            raise ValueError("expected begin [sequences + 1], table [sequences][width] and lengths [sequences]")
+        return xsv_pages(*self._fields, n, shape[1], table.data_ptr(), lengths.data_ptr())
 
 
 def _bound(value, most, name):

@@ -322,6 +322,57 @@ def test_pages_of_very_different_scales():
         plain.check_attend(pool, q, got, [0, 90], table, [500], causal)
 
 
+def test_scales_whose_product_fp32_does_not_hold():
+    """Tiny keys and a tiny scale: logits of 0, and what is masked stays masked."""
+    pages, table, pool = _filled([130], 1, 42, scale=1e-29)
+    for rows in (2, 40):
+        q = _randn(6, 2, rows, 64).to(torch.bfloat16).to(DEV)
+        got = xsv.pages_attend(pages, q, _int([0, rows]), _int(table), _int([130]), causal=1, softmax_scale=1e-20)
+        plain.check_attend(pool, q, got, [0, rows], table, [130], 1, 1e-20)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+@pytest.mark.parametrize("step", [0.4, 30.0, 400.0])
+def test_logits_that_rise_and_fall_along_a_sequence(rows, step):
+    """Logits that rise with the page (by 2^24 and by more than fp32 holds), then fall: references that move, weights that vanish."""
+    direction = torch.zeros(64)
+    direction[:8] = 1.0
+
+    def edit(k, v):
+        for i in range(20):
+            k[:, 64 * i:64 * i + 64] += direction * step * (min(i, 14) - 2.0 * max(i - 14, 0))
+    pages, table, pool = _filled([64 * 20 - 7], 2, 47, edit=edit)
+    q = (_randn(9, 4, rows, 64) * 0.3 + direction).to(torch.bfloat16).to(DEV)
+    for causal in (0, 1):
+        got = xsv.pages_attend(pages, q, _int([0, rows]), _int(table), _int([64 * 20 - 7]), causal=causal)
+        plain.check_attend(pool, q, got, [0, rows], table, [64 * 20 - 7], causal)
+    lists = torch.tensor([1, 3, 7, 14, 15, 19], dtype=torch.int32).expand(rows, 2, 6).clone()
+    lists[:, 1, ::2] = -1
+    got = xsv.pages_attend(pages, q, _int([0, rows]), _int(table), _int([64 * 20 - 7]), causal=1, chosen=lists.to(DEV))
+    plain.check_attend(pool, q, got, [0, rows], table, [64 * 20 - 7], 1, chosen=lists)
+
+
+@pytest.mark.parametrize("kv_heads", [3, 8])
+def test_many_sequences_of_several_blocks(kv_heads):
+    """Up to 64 sequences' blocks go by what they see, those of more by their place."""
+    rng = random.Random(kv_heads)
+    for count in (5, 66):
+        new = [rng.choice([0, 1, 3, 20, 37]) for _ in range(count)]
+        lengths = [max(n + rng.choice([-2, 0, 0, 5, 200]), 0) for n in new]
+        pages, table, pool = _filled(lengths, kv_heads, 48 + count)
+        q = _randn(10, 2 * kv_heads, sum(new), 64).to(torch.bfloat16).to(DEV)
+        got = xsv.pages_attend(pages, q, _int(_begin(new)), _table_tensor(table), _int(lengths), causal=1, longest_q=max(new), longest_k=max(lengths))
+        plain.check_attend(pool, q, got, _begin(new), table, lengths, 1, heads=[0, 2 * kv_heads - 1])
+
+
+def test_tokens_of_pages_that_were_never_written_are_zeros():
+    pages = xsv.Pages.empty(4, 2, DEV)
+    for rows in (1, 40):
+        q = _randn(11, 4, rows, 64).to(torch.bfloat16).to(DEV)
+        out, lse = xsv.pages_attend(pages, q, _int([0, rows]), _int([[2, 0, 1]]), _int([150]))
+        assert not out.any() and bool(((lse - math.log(150.0)).abs() <= 1e-5).all())
+
+
 def test_strided_queries_and_outputs():
     pages, table, pool = _filled([400, 90], 2, 45)
     q = _randn(8, 70, 6, 64).to(torch.bfloat16).to(DEV).transpose(0, 1)
@@ -349,6 +400,22 @@ def test_attention_over_listed_pages(heads, kv_heads, count):
     for causal in (0, 1):
         got = xsv.pages_attend(pages, q, _int(begin), _table_tensor(table), _int(lengths), causal=causal, chosen=chosen.to(DEV))
         plain.check_attend(pool, q, got, begin, table, lengths, causal, chosen=chosen, heads=None if heads <= 8 else [0, heads // 2, heads - 1])
+
+
+def test_lists_over_many_pages_and_shared_by_workgroups():
+    """More pages than are listed at a time; lists of one query long enough to be shared."""
+    m = 64 * 4200 + 9
+    pages, table, pool = _filled([m], 1, 63)
+    rng = random.Random(3)
+    for rows, count in ((3, 6), (1, 40)):
+        lists = torch.tensor([[sorted(rng.sample(range(4201), count), key=lambda _: rng.random())] for _ in range(rows)], dtype=torch.int32)
+        lists[0, 0, :4] = torch.tensor([2047, 2048, 4200, 0])
+        q = _randn(14, 2, rows, 64).to(torch.bfloat16).to(DEV)
+        got = xsv.pages_attend(pages, q, _int([0, rows]), _int(table), _int([m]), causal=1, chosen=lists.to(DEV))
+        plain.check_attend(pool, q, got, [0, rows], table, [m], 1, chosen=lists)
+        for _ in range(2):
+            again = xsv.pages_attend(pages, q, _int([0, rows]), _int(table), _int([m]), causal=1, chosen=lists.flip(2).contiguous().to(DEV))
+            assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])     # the order of a list changes nothing
 
 
 def test_all_pages_listed_is_attention_over_all():
@@ -425,6 +492,36 @@ def test_choice_among_many_pages_and_within_a_bound():
     got = xsv.pages_select(pages, q, _int([0, 2]), _int(table), _int(lengths), 8, causal=0, longest_k=1000).cpu()
     want = plain.select(pool, q, [0, 2], table, [1000], 8, 1, 1, 0)
     assert all(got[r, 0].tolist() == want[r, 0] for r in range(2))
+
+
+@pytest.mark.parametrize("count,pages_in_all", [(65, 700), (100, 90), (200, 300), (64, 64)])
+def test_choice_of_more_pages_than_lanes(count, pages_in_all):
+    pages, table, pool = _filled([64 * pages_in_all - 1], 2, 86)
+    q = _randn(19, 4, 2, 64).to(torch.bfloat16).to(DEV)
+    _check_select(pages, pool, q, [0, 2], table, [64 * pages_in_all - 1], count, 3, 1, 1)
+
+
+def test_choice_in_a_graph_with_much_shared_memory():
+    lengths = [64 * 600]
+    pages, table, pool = _filled(lengths, 1, 88)
+    q = _randn(20, 2, 40, 64).to(torch.bfloat16).to(DEV)
+    where = (_int([0, 40]), _int(table), _int(lengths))
+    out = torch.empty((40, 1, 9), dtype=torch.int32, device=DEV)
+    call = lambda: xsv.pages_select(pages, q, *where, 9, first=2, last=1, causal=1, out=out)
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for i in range(3):
+        q.copy_(_randn(21 + i, 2, 40, 64).to(torch.bfloat16))
+        want = call().clone()
+        out.fill_(7)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    want = plain.select(pool, q, [0, 40], table, lengths, 9, 2, 1, 1)
+    assert all(out[r, 0].tolist() == want[r, 0] for r in range(40))
 
 
 def test_choice_of_a_whole_frame():
