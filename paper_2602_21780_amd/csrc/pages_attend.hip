@@ -142,13 +142,28 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
 struct Block {
   Held h;
   int s, kv;
-  int query, head;     // of the lane's row (behind the last: a copy of it that nobody writes)
-  bool real;
-  int seen;            // tokens that the lane's row sees
+  int64_t row0, rows;  // the first, among the `rows` of its sequence (chosen pages: of its queries)
   int least, pages;    // tokens that all rows see; pages that any row sees one of
   int part, used;      // this workgroup of those that share the pages
   int query0, queries; // chosen pages: the queries of the block
 };
+
+// Its row i (behind the last: a copy of it that nobody writes).
+struct Row {
+  int query, head;
+  int seen;  // tokens
+  bool real;
+};
+__device__ __forceinline__ Row row_of(const PagesArgs& a, const Block& b, int i) {
+  const int rep = a.heads / a.kv_heads;
+  const uint32_t row = (uint32_t)min(b.row0 + i, b.rows - 1);  // (below 2^32: blocks of a launch are fewer than 2^24)
+  Row r;
+  r.query = b.query0 + (int)(row / (uint32_t)rep);
+  r.head = b.kv * rep + (int)(row % (uint32_t)rep);
+  r.seen = tokens_seen(a, b.h, r.query);
+  r.real = b.row0 + i < b.rows;
+  return r;
+}
 
 // Block number `*block` of all sequences' blocks of a key head (at most 64 sequences), those of the sequences that see the most pages first, of a sequence the
 // last first: it becomes the number of blocks behind it in its sequence.  A lane looks a sequence up.
@@ -181,7 +196,7 @@ __device__ __forceinline__ bool ranked_block(const PagesArgs& a, int* block, int
 // heads, each XCD has its own, one after the other, whose pages are then in one L2, and all of whose blocks go through them at about the same time.  A block's parts are far apart: side by side, with eight of them,
 // those of short sequences, which have little or nothing to do, were dealt to the same compute units (64 streams 89 us, 77).
 template <int COLS, bool CHOSEN>
-__device__ __forceinline__ bool block_of(const PagesArgs& a, int number, int blocks, int col, Block* b) {
+__device__ __forceinline__ bool block_of(const PagesArgs& a, int number, int blocks, Block* b) {
   const int rep = a.heads / a.kv_heads;
   const int heads = a.kv_heads % 8 ? a.kv_heads : a.kv_heads / 8, at = a.kv_heads % 8 ? number : number / 8;
   const int sequences = a.ranked ? 1 : a.sequences, units = heads * sequences * blocks, unit = at % units;
@@ -206,15 +221,11 @@ __device__ __forceinline__ bool block_of(const PagesArgs& a, int number, int blo
   if (block < 0) return false;
   b->query0 = CHOSEN ? block / per * a.group : 0;
   b->queries = CHOSEN ? min(a.group, b->h.n - b->query0) : b->h.n;
-  const int64_t row0 = (int64_t)(CHOSEN ? block % per : block) * COLS, rows = (int64_t)b->queries * rep;
-  if (b->queries <= 0 || row0 >= rows) return false;
-  const int64_t row = min(row0 + col, rows - 1), last = min(row0 + COLS, rows) - 1;
-  b->real = row0 + col < rows;
-  b->query = b->query0 + (int)((uint32_t)row / (uint32_t)rep);   // (below 2^32: blocks of a launch are fewer than 2^24)
-  b->head = b->kv * rep + (int)((uint32_t)row % (uint32_t)rep);
-  b->seen = tokens_seen(a, b->h, b->query);
-  b->least = tokens_seen(a, b->h, b->query0 + (int)((uint32_t)row0 / (uint32_t)rep));
-  b->pages = (tokens_seen(a, b->h, b->query0 + (int)((uint32_t)last / (uint32_t)rep)) + kPage - 1) / kPage;
+  b->row0 = (int64_t)(CHOSEN ? block % per : block) * COLS;
+  b->rows = (int64_t)b->queries * rep;
+  if (b->queries <= 0 || b->row0 >= b->rows) return false;
+  b->least = row_of(a, *b, 0).seen;
+  b->pages = (row_of(a, *b, COLS - 1).seen + kPage - 1) / kPage;
   b->used = CHOSEN ? a.parts : min(max((b->pages + a.chunk - 1) / a.chunk, 1), a.parts);
   return b->part < b->used;
 }
@@ -293,13 +304,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
   const int lane = threadIdx.x % 64, col = lane % COLS, quarter = lane / COLS;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   Block b;
-  if (!block_of<COLS, CHOSEN>(a, blockIdx.x, blocks, col, &b)) return;
+  if (!block_of<COLS, CHOSEN>(a, blockIdx.x, blocks, &b)) return;
+  const Row own = row_of(a, b, col);
   const int32_t* table = a.table + (int64_t)b.s * a.width;
 
   constexpr int kSteps = COLS / 8;  // of 8 channels, and of 8 tokens, a lane
   bf16x8 qf[kSteps];
   {
-    const uint16_t* q = a.q.p + b.head * a.q.sh + (int64_t)(b.h.row0 + b.query) * a.q.st + S::query_at(quarter);
+    const uint16_t* q = a.q.p + own.head * a.q.sh + (int64_t)(b.h.row0 + own.query) * a.q.st + S::query_at(quarter);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) qf[i] = *reinterpret_cast<const bf16x8*>(q + 8 * i);
   }
@@ -412,7 +424,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
   // A page with all that may happen: rows that do not see some of it, references that move, values that are NaN.
   auto whole = [&](int ordinal, uint32_t rows, float ks, float vs, int next_page) {
     const bool mine = !CHOSEN || (rows >> col & 1);
-    const int left = mine ? b.seen - ordinal * kPage - 16 * quarter : -kPage;  // of the tokens from the lane's first on
+    const int left = mine ? own.seen - ordinal * kPage - 16 * quarter : -kPage;  // of the tokens from the lane's first on
     const float cs = factor_of(ks);
     if constexpr (kStaged) wait_for_all();
     take_keys();
@@ -545,32 +557,47 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
     sums[wave][col] = total;
   }
   __syncthreads();
+  // All rows at once, a thread some channels of one: 4 threads further on the next 4 if it has more than 4, so that 8 side by side read different banks.
+  constexpr int kRowThreads = 64 * WAVES / COLS, kChannels = kD / kRowThreads, kWide = std::min(kChannels, 4);
+  const int r = threadIdx.x / kRowThreads, first = threadIdx.x % kRowThreads;
+  const Row to = row_of(a, b, r);
+  if (!to.real) return;
+  const int64_t row = b.h.row0 + to.query;
+  float top = -kInf;
 #pragma unroll
-  for (int j = 0; j < COLS / std::min(WAVES, COLS); ++j) {
-    const int r = wave + j * WAVES, c = lane;
-    // (row r's place is what lane r has)
-    if (!__builtin_amdgcn_readlane(b.real, r)) break;  // (rows that there are come first)
-    const int head = __builtin_amdgcn_readlane(b.head, r);
-    const int64_t row = b.h.row0 + __builtin_amdgcn_readlane(b.query, r);
-    float top = -kInf;
+  for (int w = 0; w < WAVES; ++w) top = fmaxf(top, refs[w][r]);
+  const float off = off_of(top);
+  float l = 0.0f, f[WAVES];
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, refs[w][r]);
-    const float off = off_of(top);
-    float l = 0.0f, v = 0.0f;
+  for (int w = 0; w < WAVES; ++w) {
+    f[w] = exp2_(refs[w][r] - off);
+    l += sums[w][r] * f[w];
+  }
+  const int64_t at = ((int64_t)b.part * a.heads + to.head) * a.rows + row;  // of the workspace
+  const float whole_of = b.used > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int j = 0; j < kChannels / kWide; ++j) {
+    const int c = kWide * (first + j * kRowThreads);
+    float v[kWide] = {};
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-      const float f = exp2_(refs[w][r] - off);
-      l += sums[w][r] * f;
-      v += shares[w].acc[r][(c / 4) ^ (r % 16)][c % 4] * f;
+      const float* x = reinterpret_cast<const float*>(&shares[w].acc[r][(c / 4) ^ (r % 16)]) + c % 4;
+#pragma unroll
+      for (int i = 0; i < kWide; ++i) v[i] += x[i] * f[w];
     }
-    if (b.used == 1) {
-      const_cast<uint16_t*>(a.out.p)[head * a.out.sh + row * a.out.st + c] = (uint16_t)pack2(l == 0.0f ? 0.0f : v / l, 0.0f);
-      if (c == 0) a.lse[(int64_t)head * a.rows + row] = (off + log2f(l)) * kLn2;
+#pragma unroll
+    for (int i = 0; i < kWide; ++i) v[i] *= whole_of;
+    uint16_t* out = const_cast<uint16_t*>(a.out.p) + to.head * a.out.sh + row * a.out.st + c;
+    if constexpr (kWide == 4) {
+      if (b.used == 1) *reinterpret_cast<u32x2*>(out) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+      else *reinterpret_cast<f32x4*>(a.part + at * kD + c) = f32x4{v[0], v[1], v[2], v[3]};
     } else {
-      const int64_t at = ((int64_t)b.part * a.heads + head) * a.rows + row;
-      a.part[at * kD + c] = v;
-      if (c < 2) a.part_sums[2 * at + c] = c ? l : top;
+      *out = (uint16_t)pack2(v[0], 0.0f);  // (16 waves: nobody shares a block)
     }
+  }
+  if (first == 0) {
+    if (b.used == 1) a.lse[(int64_t)to.head * a.rows + row] = (off + log2f(l)) * kLn2;
+    else *reinterpret_cast<f32x2*>(a.part_sums + 2 * at) = f32x2{top, l};
   }
 }
 
@@ -597,12 +624,13 @@ template <int COLS, bool CHOSEN>
 __global__ __launch_bounds__(64 * kWaves) void pages_join_kernel(PagesArgs a, int blocks) {
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   Block b;
-  if (!block_of<COLS, CHOSEN>(a, blockIdx.x, blocks, lane % COLS, &b) || b.used == 1) return;
+  if (!block_of<COLS, CHOSEN>(a, blockIdx.x, blocks, &b) || b.used == 1) return;
 #pragma unroll 1
   for (int r = wave; r < COLS; r += kWaves) {
-    if (!__builtin_amdgcn_readlane(b.real, r)) break;
-    const int head = __builtin_amdgcn_readlane(b.head, r);
-    const int64_t row = b.h.row0 + __builtin_amdgcn_readlane(b.query, r);
+    const Row to = row_of(a, b, r);
+    if (!to.real) break;
+    const int head = to.head;
+    const int64_t row = b.h.row0 + to.query;
     const int64_t at = (int64_t)head * a.rows + row, step = (int64_t)a.heads * a.rows;
     const int last = b.used - 1;
     const float* sums = a.part_sums + 2 * (at + min(lane, last) * step);
