@@ -22,6 +22,10 @@ constexpr int kLongest = 64;
 // over 512 to 4096 tokens 12 and 16, over 8192 20 and 16; 64 over 4096 13 and 16, over 8192 20 and 18; 256 over 4096 27 and 33 (over 8192 49 and 56, but
 // there sequences of different lengths would leave compute units empty).
 constexpr int kManyUnits = 256, kManyPages = 64;
+// 64 rows to a wave, if that fills the card: two workgroups on each of 256 compute units.  us, 64 rows and 32 (16 heads): 10992 rows over 16384 tokens 756 and 860,
+// 2748 over 8192 109 and 124, 2048 behind 6144 of their own (512 blocks) 75 and 79; 1374 over 5470 (352 blocks) 51 and 46.  Fewer blocks if all parts of their pages are
+// long: 512 over 65536 tokens (4 parts of 256 pages) 172 and 187, 128 over 131072 (16 of 128) 109 and 114, but 256 over 8192 (8 of 16) 40 and 32.
+constexpr long long kFull = 512, kLongPart = 128;
 constexpr int kListRows = 16;  // rows that share a list of chosen pages
 // Probabilities are taken against a reference logit per row, which moves when the sum over what a lane has of a page passes this:
 // probabilities above 1 are as exact as below.
@@ -58,6 +62,7 @@ __device__ __forceinline__ void stage(const uint8_t* page, int even, int odd, ui
       "global_load_lds_dwordx4 %2, %3 offset:%6" ::"s"(to), "v"(even), "v"(odd), "s"(page), "i"(16 * kD), "i"(2 * 16 * kD), "i"(3 * 16 * kD) : "memory", "m0");
 }
 __device__ __forceinline__ void wait_for_all() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void wait_for_all_but_eight() { asm volatile("s_waitcnt vmcnt(8)" ::: "memory"); }
 __device__ __forceinline__ void wait_for_all_but_four() { asm volatile("s_waitcnt vmcnt(4)" ::: "memory"); }
 
 template <>
@@ -286,6 +291,53 @@ __device__ __forceinline__ int list_window(const PagesArgs& a, const Block& b, i
     if (mine[i]) l.found[at++] = (uint32_t)(tid * kEach + i) | mine[i] << 16;
   __syncthreads();
   return total;
+}
+
+// The waves' results, each [COLS][64] of `pitch` pieces, 16-byte pieces of row r in the order of their number xor r, put together: a block's, or this part of them.
+template <int COLS, int WAVES>
+__device__ __forceinline__ void leave(const PagesArgs& a, const Block& b, const f32x4* acc, int pitch, const float* refs, const float* sums) {
+  // All rows at once, a thread some channels of one: 4 threads further on the next 4 if it has more than 4, so that 8 side by side read different banks.
+  constexpr int kRowThreads = 64 * WAVES / COLS, kChannels = kD / kRowThreads, kWide = std::min(kChannels, 4);
+  const int r = threadIdx.x / kRowThreads, first = threadIdx.x % kRowThreads;
+  const Row to = row_of(a, b, r);
+  if (!to.real) return;
+  const int64_t row = b.h.row0 + to.query;
+  float top = -kInf;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) top = fmaxf(top, refs[w * COLS + r]);
+  const float off = off_of(top);
+  float l = 0.0f, f[WAVES];
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    f[w] = exp2_(refs[w * COLS + r] - off);
+    l += sums[w * COLS + r] * f[w];
+  }
+  const int64_t at = ((int64_t)b.part * a.heads + to.head) * a.rows + row;  // of the workspace
+  const float whole_of = b.used > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int j = 0; j < kChannels / kWide; ++j) {
+    const int c = kWide * (first + j * kRowThreads);
+    float v[kWide] = {};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float* x = reinterpret_cast<const float*>(acc + w * pitch + r * (kD / 4) + ((c / 4) ^ (r % 16))) + c % 4;
+#pragma unroll
+      for (int i = 0; i < kWide; ++i) v[i] += x[i] * f[w];
+    }
+#pragma unroll
+    for (int i = 0; i < kWide; ++i) v[i] *= whole_of;
+    uint16_t* out = const_cast<uint16_t*>(a.out.p) + to.head * a.out.sh + row * a.out.st + c;
+    if constexpr (kWide == 4) {
+      if (b.used == 1) *reinterpret_cast<u32x2*>(out) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+      else *reinterpret_cast<f32x4*>(a.part + at * kD + c) = f32x4{v[0], v[1], v[2], v[3]};
+    } else {
+      *out = (uint16_t)pack2(v[0], 0.0f);  // (16 waves: nobody shares a block)
+    }
+  }
+  if (first == 0) {
+    if (b.used == 1) a.lse[(int64_t)to.head * a.rows + row] = (off + log2f(l)) * kLn2;
+    else *reinterpret_cast<f32x2*>(a.part_sums + 2 * at) = f32x2{top, l};
+  }
 }
 
 struct Empty {};
@@ -557,48 +609,270 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
     sums[wave][col] = total;
   }
   __syncthreads();
-  // All rows at once, a thread some channels of one: 4 threads further on the next 4 if it has more than 4, so that 8 side by side read different banks.
-  constexpr int kRowThreads = 64 * WAVES / COLS, kChannels = kD / kRowThreads, kWide = std::min(kChannels, 4);
-  const int r = threadIdx.x / kRowThreads, first = threadIdx.x % kRowThreads;
-  const Row to = row_of(a, b, r);
-  if (!to.real) return;
-  const int64_t row = b.h.row0 + to.query;
-  float top = -kInf;
+  leave<COLS, WAVES>(a, b, shares[0].acc[0], sizeof(Share) / sizeof(f32x4), refs[0], sums[0]);
+}
+
+// Many rows of a sequence, 64 of them at a time, which share a page's conversion to bf16.  A wave goes through units of 32 tokens and 32 rows; while it works on the
+// probabilities of one, its matrix instructions make the logits of the next and add up what the one before weighs.
+__global__ __launch_bounds__(64 * kWaves, 2) void pages_attend_rows_kernel(PagesArgs a, int blocks) {
+  using S = Shape<32>;
+  constexpr int kTiles = 2, kRows = 32 * kTiles;
+  union Share {  // of a wave: two pages, later its results
+    uint8_t page[2][kStagedBytes];
+    f32x4 acc[kRows][kD / 4];
+  };
+  __shared__ struct {
+    Share of[kWaves];  // (the first 64 KB: the destination of a load to LDS has 16 bits)
+    float refs[kWaves][kRows], sums[kWaves][kRows];
+  } shares;
+  const int lane = threadIdx.x % 64, col = lane % 32, quarter = lane / 32;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  Block b;
+  if (!block_of<kRows, false>(a, blockIdx.x, blocks, &b)) return;
+  const int32_t* table = a.table + (int64_t)b.s * a.width;
+  bf16x8 q[kTiles][4];
+  int seen[kTiles];
+  f32x16 o[kTiles][2] = {};
+  float ref[kTiles], sum[kTiles];
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) top = fmaxf(top, refs[w][r]);
-  const float off = off_of(top);
-  float l = 0.0f, f[WAVES];
+  for (int t = 0; t < kTiles; ++t) {
+    const Row own = row_of(a, b, 32 * t + col);
+    const uint16_t* from = a.q.p + own.head * a.q.sh + (int64_t)(b.h.row0 + own.query) * a.q.st + S::query_at(quarter);
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    f[w] = exp2_(refs[w][r] - off);
-    l += sums[w][r] * f[w];
+    for (int i = 0; i < 4; ++i) q[t][i] = *reinterpret_cast<const bf16x8*>(from + 8 * i);
+    seen[t] = own.seen;
+    ref[t] = -kInf;
+    sum[t] = 0.0f;
   }
-  const int64_t at = ((int64_t)b.part * a.heads + to.head) * a.rows + row;  // of the workspace
-  const float whole_of = b.used > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+  const float c2 = a.scale * kLog2e;
+
+  // Pages go through LDS, two of a wave's at a time: the one at hand is in place `at_hand`, the next on its way to the other.
+  int at_hand = 0;
+  const uint32_t staged_at = (uint32_t)(size_t)(lds_byte*)shares.of[wave].page[0];
+  const int key_from = lane / 4 * 64 + (lane - key_turn(lane / 4 % 4, 0)) % 4 * 16, value_from = lane / 4 * 64 + (lane + 4 - value_turn(lane / 4)) % 4 * 16;
+  auto fetch = [&](int page, int place) {
+    const size_t unit = ((size_t)page * a.kv_heads + b.kv) * kPageBytes;
+    stage(a.k + unit, key_from, key_from ^ 32, staged_at + place * kStagedBytes);
+    stage(a.v + unit, value_from, value_from, staged_at + place * kStagedBytes + kPageBytes);
+  };
+  const int staged_key = S::staged_key(col, quarter, 0), staged_key1 = S::staged_key(col, quarter, 1), staged_value = S::staged_value(col, quarter, 0), staged_value1 = S::staged_value(col, quarter, 2);
+  u32x4 kr[2], vr[2];   // 32 tokens as they are
+  bf16x8 kb[4], vb[4];  // 32 tokens in bf16: keys by steps of channels, values by blocks of channels and steps of tokens
+  auto read_keys = [&](int place, int h) {
+    const uint8_t* p = shares.of[wave].page[place] + 2048 * h;
+    kr[0] = *reinterpret_cast<const u32x4*>(p + staged_key);
+    kr[1] = *reinterpret_cast<const u32x4*>(p + staged_key1);
+  };
+  auto read_values = [&](int place, int h) {
+    const uint8_t* p = shares.of[wave].page[place] + kPageBytes + (h ? staged_value1 : staged_value);
+    vr[0] = *reinterpret_cast<const u32x4*>(p);
+    vr[1] = *reinterpret_cast<const u32x4*>(p + 2048);
+  };
+  auto take_keys = [&] {
 #pragma unroll
-  for (int j = 0; j < kChannels / kWide; ++j) {
-    const int c = kWide * (first + j * kRowThreads);
-    float v[kWide] = {};
+    for (int i = 0; i < 4; ++i) kb[i] = view8(kr[i / 2][i % 2 * 2], kr[i / 2][i % 2 * 2 + 1]);
+  };
+  auto take_values = [&] {
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      const float* x = reinterpret_cast<const float*>(&shares[w].acc[r][(c / 4) ^ (r % 16)]) + c % 4;
+    for (int i = 0; i < 4; ++i) vb[i] = view8(vr[i / 2][i % 2 * 2], vr[i / 2][i % 2 * 2 + 1]);
+  };
+  auto logits = [&](int t) {
+    f32x16 x = {};
 #pragma unroll
-      for (int i = 0; i < kWide; ++i) v[i] += x[i] * f[w];
+    for (int i = 0; i < 4; ++i) x = S::mfma(kb[i], q[t][i], x);
+    return x;
+  };
+  auto add_values = [&](int t, const u32x4 (&pr)[2]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[t][i / 2] = S::mfma(vb[i], __builtin_bit_cast(bf16x8, pr[i % 2]), o[t][i / 2]);
+  };
+  // (the values' scale 2^ev is in `off`, as above)
+  auto weigh = [&](const f32x16& x, float cs, float off, u32x4 (&pr)[2]) {
+    float one = 0.0f, other = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      const float p = exp2_(x[e] * cs - off), r = exp2_(x[e + 1] * cs - off);
+      one += p;
+      other += r;
+      pr[e / 8][e % 8 / 2] = pack2(p, r);
     }
+    return one + other;
+  };
+  auto exponent_of = [](float scale) { return min(max((int)((__float_as_uint(scale) >> 23) & 0xffu) - 127, -100), 120); };
+  auto factor_of = [&](float scale) { return fmaxf(c2 * scale, 1.17549435e-38f); };
+
+  // The page at hand with all that may happen, but for its first `skip` units.
+  auto whole = [&](int ordinal, int skip, float ks, float vs) {
+    const float cs = factor_of(ks);
+    const int ev = exponent_of(vs);
+    const float un = __int_as_float((127 - ev) << 23);
+    wait_for_all_but_eight();
 #pragma unroll
-    for (int i = 0; i < kWide; ++i) v[i] *= whole_of;
-    uint16_t* out = const_cast<uint16_t*>(a.out.p) + to.head * a.out.sh + row * a.out.st + c;
-    if constexpr (kWide == 4) {
-      if (b.used == 1) *reinterpret_cast<u32x2*>(out) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
-      else *reinterpret_cast<f32x4*>(a.part + at * kD + c) = f32x4{v[0], v[1], v[2], v[3]};
-    } else {
-      *out = (uint16_t)pack2(v[0], 0.0f);  // (16 waves: nobody shares a block)
+    for (int h = 0; h < 2; ++h) {
+      read_keys(at_hand, h);
+      read_values(at_hand, h);
+      take_keys();
+      bf16x8 nb[4] = {};
+      if (vs < 0.0f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t nan[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int at = i % 2 * 2 + j;
+            nan[j] = nan_bytes(vr[i / 2][at]);
+            vr[i / 2][at] &= ~nan[j];
+          }
+          nb[i] = view8(nan[0] & 0x38383838u, nan[1] & 0x38383838u);  // ones
+        }
+      }
+      take_values();
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        if (h * kTiles + t < skip) continue;
+        const int left = seen[t] - ordinal * kPage - 32 * h - 16 * quarter;
+        f32x16 x = logits(t);
+        float m = -kInf;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          x[e] = e < left ? x[e] : -kInf;
+          m = fmaxf(m, x[e]);
+        }
+        m = S::column_max(m) * cs;
+        const float to = fmaxf(m, ref[t]), f = ref[t] == -kInf || to == ref[t] ? 1.0f : exp2_(ref[t] - to);
+        ref[t] = to;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) o[t][i] *= f;
+        u32x4 pr[2];
+        sum[t] = sum[t] * f + weigh(x, cs, off_of(to) - (float)ev, pr) * un;
+        add_values(t, pr);
+        if (vs < 0.0f) {
+          // 0 times NaN is NaN: values that are NaN are taken out of the product, and reach the rows that see their tokens by one of their own
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            f32x16 count = {};
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              u32x4 sees;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) sees[j] = (8 * k + 2 * j < left ? 0x3f80u : 0u) | (8 * k + 2 * j + 1 < left ? 0x3f800000u : 0u);
+              count = S::mfma(nb[2 * i + k], __builtin_bit_cast(bf16x8, sees), count);
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[t][i][j] = count[j] > 0.0f ? __builtin_nanf("") : o[t][i][j];
+          }
+        }
+      }
+    }
+  };
+
+  const int begin = b.part * a.chunk, end = b.part == b.used - 1 ? b.pages : (b.part + 1) * a.chunk;
+  for (int from = begin + wave; from < end; from += kWaves * 64) {
+    const int at = from + kWaves * lane;
+    const int lane_page = at < end ? table[at] : -1;
+    const bool some = lane_page >= 0 && lane_page < a.pages;
+    const int64_t unit = some ? (int64_t)lane_page * a.kv_heads + b.kv : 0;
+    float lane_ks = some ? a.k_scale[unit] : 0.0f, lane_vs = some ? a.v_scale[unit] : 0.0f;
+    uint64_t mask = __ballot(some);
+    if (!mask) continue;
+    int i = __builtin_ctzll(mask), next = 0, ordinal = 0;
+    float ks = 0.0f, vs = 0.0f;
+    fetch(__builtin_amdgcn_readlane(lane_page, i), at_hand);
+    asm volatile("" : "+v"(lane_ks), "+v"(lane_vs));  // (they are there: nothing waits for them in the loop)
+    auto look_at = [&] {  // page i; the next one's (behind the last: the same one's) loads begin
+      ordinal = from + kWaves * i;
+      ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lane_ks), i));
+      vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lane_vs), i));
+      mask &= mask - 1;
+      next = mask ? __builtin_ctzll(mask) : i;
+      fetch(__builtin_amdgcn_readlane(lane_page, next), at_hand ^ 1);
+    };
+    auto plain = [&] { return (ordinal + 1) * kPage <= b.least && vs >= 0.0f; };
+    look_at();
+    while (true) {
+      bool begun = true;
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) begun = begun && !__any(ref[t] == -kInf);
+      int skip = 0;
+      bool last = false;  // no page is left
+      if (begun && plain()) {
+        bool done = true;  // with all units
+        f32x16 xa, xb;
+        u32x4 pa[2], pb[2] = {};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) vb[k] = bf16x8{};
+        wait_for_all_but_eight();
+        read_keys(at_hand, 0);
+        take_keys();
+        xa = logits(0);
+        while (true) {
+          const float cs = factor_of(ks);
+          const int ev = exponent_of(vs);
+          const float un = __int_as_float((127 - ev) << 23);
+          auto unit_of = [&](auto number, const f32x16& x, f32x16& x_next, u32x4 (&pr)[2], const u32x4 (&before)[2]) {
+            constexpr int u = decltype(number)::value, t = u % 2;
+            __builtin_amdgcn_sched_barrier(0);
+            if (u == 0) {
+              read_keys(at_hand, 1);
+              read_values(at_hand, 0);
+            }
+            if (u == 2) {
+              wait_for_all();
+              read_keys(at_hand ^ 1, 0);
+              read_values(at_hand, 1);
+            }
+            if (u % 2 == 1) take_keys();
+            x_next = logits(1 - t);
+            if (u % 2 == 1) take_values();
+            add_values(1 - t, before);
+            const float part = weigh(x, cs, ref[t] - (float)ev, pr) * un;
+            asm volatile("" : "+v"(pr[0]), "+v"(pr[1]));  // (here, and not behind the branch: until then there would be twice as many registers)
+            if (__any(part > kMaxPart)) {
+              skip = u;
+              done = false;
+              return false;
+            }
+            sum[t] += part;
+            return true;
+          };
+          if (!unit_of(std::integral_constant<int, 0>{}, xa, xb, pa, pb)) break;
+          if (!unit_of(std::integral_constant<int, 1>{}, xb, xa, pb, pa)) break;
+          if (!unit_of(std::integral_constant<int, 2>{}, xa, xb, pa, pb)) break;
+          if (!unit_of(std::integral_constant<int, 3>{}, xb, xa, pb, pa)) break;
+          last = !mask;
+          if (last) break;
+          i = next;
+          at_hand ^= 1;
+          look_at();
+          if (!plain()) break;
+        }
+        if (done) add_values(1, pb);
+        if (last) break;
+      }
+      whole(ordinal, skip, ks, vs);
+      if (!mask) break;
+      i = next;
+      at_hand ^= 1;
+      look_at();
+    }
+    wait_for_all();  // (the last page once more)
+  }
+
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    const float total = S::column_sum(sum[t]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; j += 4)
+        shares.of[wave].acc[32 * t + col][(S::channel(i, quarter, j) / 4) ^ (col % 16)] = f32x4{o[t][i][j], o[t][i][j + 1], o[t][i][j + 2], o[t][i][j + 3]};
+    if (quarter == 0) {
+      shares.refs[wave][32 * t + col] = ref[t];
+      shares.sums[wave][32 * t + col] = total;
     }
   }
-  if (first == 0) {
-    if (b.used == 1) a.lse[(int64_t)to.head * a.rows + row] = (off + log2f(l)) * kLn2;
-    else *reinterpret_cast<f32x2*>(a.part_sums + 2 * at) = f32x2{top, l};
-  }
+  __syncthreads();
+  leave<kRows, kWaves>(a, b, shares.of[0].acc[0], sizeof(Share) / sizeof(f32x4), shares.refs[0], shares.sums[0]);
 }
 
 // Over a wave, in every lane: lanes of a row of 16 by DPP, rows by swaps.
@@ -676,12 +950,24 @@ Plan plan_of(const PagesArgs& a) {
     p.units = times(times(p.blocks, a.kv_heads), a.sequences);
     p.parts = (int)std::max<long long>(std::min<long long>(512 / std::max(p.units, 1ll), (a.count + kWaves - 1) / kWaves), 1);
   } else {
-    if ((long long)a.longest * rep > 16) p.cols = 32;
-    p.blocks = ((long long)a.longest * rep + p.cols - 1) / p.cols;
-    p.ranked = p.blocks > 1 && a.sequences > 1 && a.sequences <= 64;
-    if (p.ranked) p.blocks = std::min(p.blocks * a.sequences, ((long long)a.rows * rep + p.cols - 1) / p.cols + a.sequences);  // of all sequences
-    p.units = times(times(p.blocks, a.kv_heads), p.ranked ? 1 : a.sequences);
-    const long long most = std::min<long long>(std::max<long long>(1024 / std::max(p.units, 1ll), 1), kMostParts);
+    const long long rows = (long long)a.longest * rep;
+    auto cut = [&](int cols) {
+      p.cols = cols;
+      p.blocks = (rows + cols - 1) / cols;
+      p.ranked = p.blocks > 1 && a.sequences > 1 && a.sequences <= 64;
+      if (p.ranked) p.blocks = std::min(times(p.blocks, a.sequences), ((long long)a.rows * rep + cols - 1) / cols + a.sequences);  // of all sequences
+      p.units = times(times(p.blocks, a.kv_heads), p.ranked ? 1 : a.sequences);
+    };
+    long long workgroups = 1024;
+    bool wide = false;
+    if (rows > 32) {
+      cut(64);
+      const long long parts = kFull / std::max(p.units, 1ll);
+      wide = p.units >= kFull || (p.units * parts * 16 >= kFull * 15 && items >= kLongPart * parts);
+    }
+    if (wide) workgroups = kFull;
+    else cut(rows > 16 ? 32 : 16);
+    const long long most = std::min<long long>(std::max<long long>(workgroups / std::max(p.units, 1ll), 1), kMostParts);
     p.chunk = (int)std::max<long long>((items + most - 1) / most, kWaves);
     if (!p.ranked && p.blocks == 1) p.chunk = (int)std::min<long long>(p.chunk, std::max<long long>(kLongest, (items + kMostParts - 1) / kMostParts));
     p.parts = (int)std::max<long long>((items + p.chunk - 1) / p.chunk, 1);
@@ -696,14 +982,15 @@ Plan plan_of(const PagesArgs& a) {
   return p;
 }
 
-template <int COLS, bool CHOSEN, int WAVES = kWaves>
+template <bool CHOSEN, int COLS, int WAVES = kWaves>
 hipError_t launch(PagesArgs a, const Plan& p, hipStream_t stream) {
   a.parts = p.parts;
   a.chunk = p.chunk;
   a.group = p.group;
   a.ranked = p.ranked;
   a.part_sums = a.part + (int64_t)a.parts * a.heads * a.rows * kD;
-  pages_attend_kernel<COLS, CHOSEN, WAVES><<<(int)(p.units * p.parts), 64 * WAVES, 0, stream>>>(a, (int)p.blocks);
+  if constexpr (COLS > 32) pages_attend_rows_kernel<<<(int)(p.units * p.parts), 64 * WAVES, 0, stream>>>(a, (int)p.blocks);
+  else pages_attend_kernel<COLS, CHOSEN, WAVES><<<(int)(p.units * p.parts), 64 * WAVES, 0, stream>>>(a, (int)p.blocks);
   if (p.parts > 1) pages_join_kernel<COLS, CHOSEN><<<(int)p.units, 64 * kWaves, 0, stream>>>(a, (int)p.blocks);
   return hipGetLastError();
 }
@@ -723,8 +1010,9 @@ bool pages_attend_fits(const PagesArgs& a) {
 hipError_t launch_pages_attend(const PagesArgs& a, hipStream_t stream) {
   if (a.sequences == 0 || a.longest == 0) return hipSuccess;
   const Plan p = plan_of(a);
-  if (p.waves == kManyWaves) return launch<16, false, kManyWaves>(a, p, stream);
-  return a.chosen ? launch<16, true>(a, p, stream) : p.cols == 16 ? launch<16, false>(a, p, stream) : launch<32, false>(a, p, stream);
+  if (p.waves == kManyWaves) return launch<false, 16, kManyWaves>(a, p, stream);
+  if (a.chosen) return launch<true, 16>(a, p, stream);
+  return p.cols == 16 ? launch<false, 16>(a, p, stream) : p.cols == 32 ? launch<false, 32>(a, p, stream) : launch<false, 64>(a, p, stream);
 }
 
 }  // namespace xsv

@@ -352,6 +352,77 @@ def test_logits_that_rise_and_fall_along_a_sequence(rows, step):
     plain.check_attend(pool, q, got, [0, rows], table, [64 * 20 - 7], 1, chosen=lists)
 
 
+# Launches with many blocks take 64 rows at a time: rows of no sequence behind those of some make one of any call.
+MANY = 2048
+
+
+def _many(q):
+    """q behind which rows of no sequence are, NaN."""
+    out = torch.full((q.shape[0], MANY, 64), math.nan, dtype=torch.bfloat16)
+    out[:, :q.shape[1]] = q
+    return out.to(DEV)
+
+
+def _attend_many(pages, q, begin, table, lengths, **kw):
+    got = xsv.pages_attend(pages, _many(q), _int(begin), _table_tensor(table), _int(lengths), **kw)
+    assert not got[0][:, q.shape[1]:].any() and not got[1][:, q.shape[1]:].any()
+    return [x[:, :q.shape[1]].contiguous() for x in got]
+
+
+@pytest.mark.parametrize("causal", [0, 1, 59])
+@pytest.mark.parametrize("new,lengths", [([1], [1]), ([70], [500]), ([300], [300]), ([33, 0, 64, 129, 5], [33, 9, 300, 128, 700])])
+def test_many_blocks_of_rows(new, lengths, causal):
+    print(f"pages_attend of 64 rows new={new} lengths={lengths} causal={causal}", flush=True)
+    pages, table, pool = _filled(lengths, 8, 61 + sum(new))
+    q = (_randn(12, 16, sum(new), 64) * 1.5).to(torch.bfloat16)
+    got = _attend_many(pages, q, _begin(new), table, lengths, causal=causal)
+    plain.check_attend(pool, q, got, _begin(new), table, lengths, causal, heads=[0, 15])
+
+
+def test_many_blocks_of_rows_over_a_long_sequence():
+    """More pages than a wave looks up at once, some of them none."""
+    pages, table, pool = _filled([18000], 8, 62)
+    table[0][3], table[0][100], table[0][255:262] = -1, 1 << 20, [-1] * 7
+    q = (_randn(13, 16, 40, 64) * 1.5).to(torch.bfloat16)
+    got = _attend_many(pages, q, [0, 40], table, [18000])
+    assert all(torch.equal(a, b) for a, b in zip(got, _attend_many(pages, q, [0, 40], table, [18000])))
+    seen = [j for j in range(len(table[0])) if 0 <= table[0][j] < pages.count]      # (check_attend's rows see all: one product a head)
+    assert len(seen) == 282 - 9
+    plain.check_attend(pool, q, got, [0, 40], table, [18000], 0, heads=[0, 9])
+
+
+def test_nan_among_many_blocks_of_rows():
+    def edit(k, v):
+        v[0, 150, 3], v[0, 199, 60], v[1, 20, 5] = math.nan, math.inf, math.nan
+        k[1, 195, 2] = math.nan
+        k[:, 200:], v[:, 200:] = math.nan, math.nan     # tokens that are taken back
+    pages, table, pool = _filled([230], 8, 63, edit=edit)
+    q = _randn(14, 16, 70, 64).to(torch.bfloat16)
+    for causal in (0, 1, 59):
+        got = _attend_many(pages, q, [0, 70], table, [200], causal=causal)
+        plain.check_attend(pool, q, got, [0, 70], table, [200], causal, heads=[0, 1, 2, 3, 15])
+
+
+@pytest.mark.parametrize("step", [0.4, 30.0, 400.0])
+@pytest.mark.parametrize("tile", [0, 1])
+@pytest.mark.parametrize("half", [0, 1])
+def test_logits_that_rise_in_one_of_many_blocks(half, tile, step):
+    """In some tokens of a page and for some rows of 64 only, by less and by more than the weights' reference bears."""
+    direction = torch.zeros(64)
+    direction[:8] = 1.0
+
+    def edit(k, v):
+        for i in (3, 4, 9, 10, 13):
+            k[:, 64 * i + 32 * half:64 * i + 32 * half + 32] += direction * step * i
+    pages, table, pool = _filled([64 * 20 - 7], 8, 64, edit=edit)
+    q = _randn(15, 16, 64, 64) * 0.3
+    q[:, 16 * tile:16 * tile + 16] += direction     # (two heads a key head: rows 32 tile .. of the first 64)
+    q = q.to(torch.bfloat16)
+    for causal in (0, 1):
+        got = _attend_many(pages, q, [0, 64], table, [64 * 20 - 7], causal=causal)
+        plain.check_attend(pool, q, got, [0, 64], table, [64 * 20 - 7], causal, heads=[0, 7])
+
+
 @pytest.mark.parametrize("kv_heads", [3, 8])
 def test_many_sequences_of_several_blocks(kv_heads):
     """Up to 64 sequences' blocks go by what they see, those of more by their place."""
