@@ -21,13 +21,27 @@ using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
 using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
 
 constexpr int kFewTurns = 2;
+constexpr int kLeastBits = 16;   // of a bound on the scores that are chosen: sign, exponent and 7 more
 constexpr int kMostPages = 32768;  // scores of a row's pages are held in LDS
 constexpr int kMostKeys = 32768;   // of a workgroup: 128 KB, and 32 for the scoring waves' pieces
 constexpr int kHole = -(1 << 20);  // the exponent of a page that is none
 
-__device__ __forceinline__ uint32_t ordered(float x) {  // larger numbers, larger keys; 0 and the largest are for other uses
-  const uint32_t b = __float_as_uint(x);                // (a sum that begins with +0 is never -0)
+constexpr float kNone = -kInf;  // the score of a page that is none
+// Larger numbers, larger keys, and back.  (A sum that begins with +0 is never -0.)
+__device__ __forceinline__ uint32_t ordered(float x) {
+  const uint32_t b = __float_as_uint(x);
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t k) { return __uint_as_float(k >> 31 ? k ^ 0x80000000u : ~k); }
+// The sum over lanes up to and with this one: rows of 16 by DPP, then what the rows before have.
+__device__ __forceinline__ int sum_upto(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 of a row to the next, rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2 and 3
+  return x;
 }
 __device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
 
@@ -56,7 +70,7 @@ __device__ __forceinline__ uint32_t nth_largest(uint32_t key, int n) {
 // N: keys of a query that a lane holds (0: as many as there are, from LDS each time).
 template <int WAVES, int N>
 __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, int queries, int pitch) {
-  extern __shared__ __align__(16) uint32_t keys[];  // [queries][pitch], of page j of query r at j ^ key_turn(r); behind them a piece of each scoring wave
+  extern __shared__ __align__(16) float keys[];  // [queries][pitch], scores of page j of query r at j ^ key_turn(r); behind them a piece of each scoring wave
   const int lane = threadIdx.x % 64, u = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int rep = a.heads / a.kv_heads, groups = (a.longest + queries - 1) / queries;
   const int kv = blockIdx.x % a.kv_heads, group = blockIdx.x / a.kv_heads % groups, s = blockIdx.x / a.kv_heads / groups;
@@ -68,11 +82,12 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
   constexpr int kTurns = WAVES == 4 ? kFewTurns : 4, kChunk = 16 * kTurns;  // pages that a wave looks up together
   const int chunks = a.pages > 0 ? (pages + kChunk - 1) / kChunk : 0;
   if (rep > 1 || chunks == 0) {
-    for (int i = threadIdx.x; i < n * pitch; i += 64 * WAVES) keys[i] = 0;
+    for (int i = threadIdx.x; i < n * pitch; i += 64 * WAVES) keys[i] = kNone;
     __syncthreads();
   }
   constexpr int kScoring = WAVES < 8 ? WAVES : 8;  // waves that score: their pieces of LDS are all that the keys leave
-  uint32_t* piece = keys + queries * pitch + wave * kPieceWords;
+  uint32_t* pieces = reinterpret_cast<uint32_t*>(keys + queries * pitch);
+  uint32_t* piece = pieces + wave * kPieceWords;
   auto id_of = [&](int ordinal) {  // a page of the pool, or none
     const int id = ordinal < pages ? table[ordinal] : -1;
     return id < a.pages ? id : -1;
@@ -155,18 +170,18 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
       for (int j = 0; j < 4; ++j) e[j] = __shfl(exponent, 16 * turn + 4 * u + j);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        u32x4 key;
+        f32x4 key;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t k = ordered(__builtin_amdgcn_ldexpf(sum[c][j], min(max(t[c] + e[j], -100), 100)));
-          key[j] = e[j] == kHole ? 0u : k;
+          const float k = __builtin_amdgcn_ldexpf(sum[c][j], min(max(t[c] + e[j], -100), 100));
+          key[j] = e[j] == kHole ? kNone : k;
         }
-        uint32_t* to = keys + query[c] * pitch + ((kChunk * chunk + 16 * turn + 4 * u) ^ key_turn(query[c]));
+        float* to = keys + query[c] * pitch + ((kChunk * chunk + 16 * turn + 4 * u) ^ key_turn(query[c]));
         if (rep == 1) {
-          *reinterpret_cast<u32x4*>(to) = key;
+          *reinterpret_cast<f32x4*>(to) = key;
         } else {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) atomicMax(to + j, key[j]);
+          for (int j = 0; j < 4; ++j) __hip_atomic_fetch_max(to + j, key[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
         }
       }
     };
@@ -183,125 +198,164 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
     }
   }
   __syncthreads();
+  // Then a wave takes a query.
+  uint32_t* scratch = pieces + wave * (kScoring * kPieceWords / WAVES);
   for (int query = wave; query < n; query += WAVES) {
-    const int np = (tokens_seen(a, h, query0 + query) + kPage - 1) / kPage, steps = (np + 63) / 64;
-    uint32_t* row = keys + query * pitch;
-    // Forced pages' keys are the largest, those behind the last are none.
-    const int turned = key_turn(query);
-    for (int j = lane; j < min(a.first, np); j += 64)
-      if (row[j ^ turned]) row[j ^ turned] = 0xffffffffu;
-    for (int j = max(np - a.last, 0) + lane; j < 64 * steps; j += 64) row[j ^ turned] = j < np && row[j ^ turned] ? 0xffffffffu : 0u;
-    uint32_t held_keys[N ? N : 1];
-    auto key_at = [&](int i) { return row[64 * i + (lane ^ turned)]; };  // of page 64 i + lane
+    const int np = (tokens_seen(a, h, query0 + query) + kPage - 1) / kPage, turned = key_turn(query);
+    float* row = keys + query * pitch;
     int32_t* out = a.choice + ((int64_t)(h.row0 + query0 + query) * a.kv_heads + kv) * a.count;
     const uint64_t before = (1ull << lane) - 1;
-    if (steps == 0) {
-      for (int j = lane; j < a.count; j += 64) out[j] = -1;
-      continue;
+    const int begin = min(a.first, np), end = max(np - a.last, begin);  // of the pages that are chosen by their scores
+    int done = 0, left = a.count;
+    for (int j0 = 0; j0 < begin; j0 += 64) {
+      const int j = j0 + lane;
+      const uint64_t some = __ballot(j < begin && row[j ^ turned] != kNone);
+      if (j < begin) row[j ^ turned] = kNone;
+      if (some >> lane & 1) out[done + __popcll(some & before)] = j;
+      done += __popcll(some);
     }
-    if constexpr (N > 0) {
-      uint32_t most = 0;  // of this lane's keys
+    auto last_some = [&](int j0) { return __ballot(j0 + lane < np && row[(j0 + lane) ^ turned] != kNone); };
+    const uint64_t last = end < np ? last_some(end) : 0;
+    left -= done + __popcll(last);
+    for (int j0 = end + 64; j0 < np; j0 += 64) left -= __popcll(last_some(j0));
+    if (lane == 0 && end % 2) row[end ^ turned] = kNone;  // (scores are read two at a time)
+
+    // The `left` largest scores of pages [begin, end).
+    const int steps = (end + 63) / 64;
+    bool chosen = left <= 0 || end <= begin;
+    if (!chosen && (N > 0 || steps == 1)) {
+      // A lane has `run` pages side by side, so that lanes are in the order of pages.  As many lanes as pages are wanted have a score of at least `least`, so what is below
+      // is not chosen; what is not is rarely more than one a lane, and is then dealt out one a lane.
+      float score = kNone;
+      int page = lane, found = 0;
+      if (steps == 1) {
+        score = lane < end ? row[lane ^ turned] : kNone;
+        found = 64;
+      } else if constexpr (N > 0) {
+        const int run = (steps + 1) / 2 * 2;
+        float held_scores[N], most = kNone;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        held_keys[i] = key_at(min(i, steps - 1)) & (i < steps ? 0xffffffffu : 0u);
-        most = max(most, held_keys[i]);
-      }
-      // As many lanes as pages are wanted have a key of at least `least`, so what is below it is not chosen; what is not is rarely more than a key a lane.
-      const int some = __popcll(__ballot(most > 0));
-      if (steps == 1 || some >= a.count) {
-        const int want = min(a.count, some);
-        uint32_t key = most;
-        int page = lane, found = some;
-        if (steps > 1) {
-          const uint32_t least = nth_largest<20>(most, want);  // (or a little less)
-          found = 0;
+        for (int i = 0; i < N; i += 2) {
+          const int at = run * lane + i;
+          f32x2 two = {kNone, kNone};
+          if (i < run && at < end) two = *reinterpret_cast<const f32x2*>(row + (at ^ turned));
+          held_scores[i] = two[0];
+          held_scores[i + 1] = two[1];
+          most = fmaxf(most, fmaxf(two[0], two[1]));
+        }
+        if (__popcll(__ballot(most != kNone)) >= left) {
+          const float least = unordered(nth_largest<kLeastBits>(ordered(most), left));
+          uint32_t those = 0;
 #pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const uint64_t some = __ballot(held_keys[i] >= least);
-            if (some) {
-              const int place = found + __popcll(some & before);
-              if ((some >> lane & 1) && place < 64) {
-                row[place] = held_keys[i];  // (its keys are all in registers)
-                row[64 + place] = 64 * i + lane;
-              }
-              found += __popcll(some);
-            }
-          }
+          for (int i = N - 1; i >= 0; --i) those = 2 * those + (held_scores[i] >= least);
+          const int own = __popc(those), upto = sum_upto(own);
+          found = __builtin_amdgcn_readlane(upto, 63);
           if (found <= 64) {
-            key = lane < found ? row[lane] : 0u;
-            page = (int)row[64 + lane];
+            for (int to = upto - own; __any(those != 0); ++to) {
+              if (those) {
+                const int at = run * lane + __builtin_ctz(those);
+                scratch[to] = __float_as_uint(row[at ^ turned]);
+                scratch[64 + to] = at;
+                those &= those - 1;
+              }
+            }
+            __builtin_amdgcn_wave_barrier();
+            score = lane < found ? __uint_as_float(scratch[lane]) : kNone;
+            page = (int)scratch[64 + lane];
+            __builtin_amdgcn_wave_barrier();
+          } else {
+            found = 0;
           }
         }
-        if (found <= 64) {
-          const uint32_t nth = want > 0 ? nth_largest<32>(key, want) : 0xffffffffu;
-          const int ties = want - __popcll(__ballot(key > nth));
-          const uint64_t same = __ballot(key == nth && key > 0), takes = __ballot(key > nth || (key == nth && key > 0 && __popcll(same & before) < ties));
-          if (takes >> lane & 1) out[__popcll(takes & before)] = page;
-          for (int j = want + lane; j < a.count; j += 64) out[j] = -1;
-          continue;
+      }
+      if (found > 0) {
+        uint64_t takes = __ballot(score != kNone);
+        if (__popcll(takes) > left) {
+          int rank = 0;  // scores that are larger
+          for (int i = 0; i < found; i += 4)  // (behind the last, none)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) rank += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(score), i + k)) > score;
+          takes &= __ballot(rank < left);
+          const int over = __popcll(takes) - left;
+          if (over > 0) {  // of equal ones that are not all chosen, those of the first pages
+            int most = takes >> lane & 1 ? rank : 0;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) most = max(most, __shfl_xor(most, d));
+            uint64_t same = takes & __ballot(rank == most);
+            const bool stays = __popcll(same & before) < __popcll(same) - over;
+            takes &= ~same | __ballot(stays);
+          }
         }
+        if (takes >> lane & 1) out[done + __popcll(takes & before)] = page;
+        done += __popcll(takes);
+        chosen = true;
       }
     }
-    auto over = [&](auto f) {  // f(step, key) for every step of 64 pages
-      if constexpr (N > 0) {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          f(i, held_keys[i]);
+    if (!chosen) {
+      auto over = [&](auto f) {  // f(step, key) for every step of 64 pages; none: 0
+        for (int i = 0; i < steps; ++i) {
+          const int j = 64 * i + lane;
+          const float x = j < end ? row[j ^ turned] : kNone;
+          f(i, x == kNone ? 0u : ordered(x));
+        }
+      };
+      auto count_above = [&](uint32_t x) {
+        int c = 0;
+        over([&](int, uint32_t k) { c += __popcll(__ballot(k > x)); });
+        return c;
+      };
+      // More than `left` keys are above lo, at most `left` above hi.
+      const int all = count_above(0), want = min(left, all);
+      uint32_t lo = 0, hi = 0xffffffffu;
+      int above_hi = 0;
+      if (all == want) {
+        hi = 0;
+        above_hi = want;
       } else {
-        for (int i = 0; i < steps; ++i) f(i, key_at(i));
-      }
-    };
-    auto count_above = [&](uint32_t x) {
-      int c = 0;
-      over([&](int, uint32_t k) { c += __popcll(__ballot(k > x)); });
-      return c;
-    };
-    // More than `want` keys are above lo, at most `want` above hi, which all forced ones are.
-    const int all = count_above(0), want = min(a.count, all);
-    uint32_t lo = 0, hi = 0xfffffffeu;
-    int above_hi = 0;
-    if (all == want) {
-      hi = 0;
-      above_hi = want;
-    } else {
-      uint32_t least = 0xfffffffeu, most = 1;
-      over([&](int, uint32_t k) {
-        if (k && k != 0xffffffffu) {
-          least = min(least, k);
-          most = max(most, k);
-        }
-      });
+        uint32_t least = 0xfffffffeu, most = 1;
+        over([&](int, uint32_t k) {
+          if (k) {
+            least = min(least, k);
+            most = max(most, k);
+          }
+        });
 #pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        least = min(least, (uint32_t)__shfl_xor((int)least, d));
-        most = max(most, (uint32_t)__shfl_xor((int)most, d));
-      }
-      lo = __builtin_amdgcn_readfirstlane(least) - 1;
-      hi = __builtin_amdgcn_readfirstlane(most);
-      above_hi = count_above(hi);
-      while (above_hi != want && hi - lo > 1) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        const int c = count_above(mid);
-        if (c > want) lo = mid;
-        else {
-          hi = mid;
-          above_hi = c;
+        for (int d = 1; d < 64; d *= 2) {
+          least = min(least, (uint32_t)__shfl_xor((int)least, d));
+          most = max(most, (uint32_t)__shfl_xor((int)most, d));
+        }
+        lo = __builtin_amdgcn_readfirstlane(least) - 1;
+        hi = __builtin_amdgcn_readfirstlane(most);
+        above_hi = count_above(hi);
+        while (above_hi != want && hi - lo > 1) {
+          const uint32_t mid = lo + (hi - lo) / 2;
+          const int c = count_above(mid);
+          if (c > want) lo = mid;
+          else {
+            hi = mid;
+            above_hi = c;
+          }
         }
       }
+      // In order: the keys above hi, and of those that equal it as many of the first as are wanted.
+      int equal = want - above_hi;
+      over([&](int i, uint32_t k) {
+        uint64_t takes = __ballot(k > hi);
+        if (equal > 0) {
+          const uint64_t ties = __ballot(k == hi);
+          const bool tie = k == hi && __popcll(ties & before) < equal;
+          takes |= __ballot(tie);
+          equal = max(equal - __popcll(ties), 0);
+        }
+        if (takes >> lane & 1) out[done + __popcll(takes & before)] = 64 * i + lane;
+        done += __popcll(takes);
+      });
     }
-    // In order: the keys above hi, and of those that equal it as many of the first as are left.
-    int done = 0, left = want - above_hi;
-    over([&](int i, uint32_t k) {
-      uint64_t takes = __ballot(k > hi);
-      if (left > 0) {
-        const uint64_t ties = __ballot(k == hi);
-        const bool tie = k == hi && __popcll(ties & before) < left;
-        takes |= __ballot(tie);
-        left = max(left - __popcll(ties), 0);
-      }
-      if (takes >> lane & 1) out[done + __popcll(takes & before)] = 64 * i + lane;
-      done += __popcll(takes);
-    });
+    for (int j0 = end; j0 < np; j0 += 64) {
+      const uint64_t some = j0 == end ? last : last_some(j0);
+      if (some >> lane & 1) out[done + __popcll(some & before)] = j0 + lane;
+      done += __popcll(some);
+    }
     for (int j = done + lane; j < a.count; j += 64) out[j] = -1;
   }
 }
