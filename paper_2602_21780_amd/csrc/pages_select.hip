@@ -23,7 +23,7 @@ using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
 constexpr int kFewTurns = 2;
 constexpr int kLeastBits = 16;   // of a bound on the scores that are chosen: sign, exponent and 7 more
 constexpr int kMostPages = 32768;  // scores of a row's pages are held in LDS
-constexpr int kMostKeys = 32768;   // of a workgroup: 128 KB, and 32 for the scoring waves' pieces
+constexpr int kMostKeys = 32768;   // of a workgroup: 128 KB, and 32 for the waves' pieces
 constexpr int kHole = -(1 << 20);  // the exponent of a page that is none
 
 constexpr float kNone = -kInf;  // the score of a page that is none
@@ -50,7 +50,7 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   return __builtin_bit_cast(uint32_t, p);
 }
 
-constexpr int kPieceWords = 16 * kD;  // of LDS a scoring wave, to bring 16 pages' bounds into the order of a product's rows
+constexpr int kPieceWords = 16 * kD / 2;  // of a wave: LDS to bring one of 16 pages' bounds, upper or lower, into the order of a product's rows
 // Where a query's keys are turned to, so that what 16 queries side by side write is in different banks.
 __device__ __forceinline__ int key_turn(int query) { return query % 16 * 4; }
 
@@ -85,16 +85,14 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
     for (int i = threadIdx.x; i < n * pitch; i += 64 * WAVES) keys[i] = kNone;
     __syncthreads();
   }
-  constexpr int kScoring = WAVES < 8 ? WAVES : 8;  // waves that score: their pieces of LDS are all that the keys leave
-  uint32_t* pieces = reinterpret_cast<uint32_t*>(keys + queries * pitch);
-  uint32_t* piece = pieces + wave * kPieceWords;
+  uint32_t* piece = reinterpret_cast<uint32_t*>(keys + queries * pitch) + wave * kPieceWords;
   auto id_of = [&](int ordinal) {  // a page of the pool, or none
     const int id = ordinal < pages ? table[ordinal] : -1;
     return id < a.pages ? id : -1;
   };
-  for (int c0 = 0; c0 < n * rep && wave < min(kScoring, chunks); c0 += 32) {
+  for (int c0 = 0; c0 < n * rep && wave < min(WAVES, chunks); c0 += 32) {
     // A wave takes kChunk pages, one to a lane, that are looked up together while those before them are worked on, and then 16 at a time.  Of those, the lane has
-    // page lane % 16 in the product, and 16 bytes of the bounds of pages 4 (lane / 16) + i on their way there: 16 lanes side by side take a page's 256 bytes (with
+    // page lane % 16 in the product, and 16 bytes of one of the bounds of pages lane / 8 and 8 + lane / 8 on their way there: 8 lanes side by side take 128 bytes (with
     // a page to a lane, every lane asks for a line of its own, and a load takes the memory path 59 cycles instead of 16).
     struct Way {
       u32x4 bounds[4];
@@ -103,7 +101,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
       Way w;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        w.bounds[i] = *reinterpret_cast<const u32x4*>(a.bounds + ((size_t)max(__shfl(id, 16 * turn + 4 * u + i), 0) * a.kv_heads + kv) * 2 * kD + lane % 16 * 8);
+        w.bounds[i] = *reinterpret_cast<const u32x4*>(a.bounds + ((size_t)max(__shfl(id, 16 * turn + 8 * (i % 2) + lane / 8), 0) * a.kv_heads + kv) * 2 * kD + i / 2 * kD + lane % 8 * 8);
       return w;
     };
     auto exponent_of = [&](int id) {
@@ -149,21 +147,22 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
     }
     auto score = [&](const Way& w, int exponent, int chunk, int turn) {
       // through this wave's piece of LDS (its accesses stay in order); a page's 16-byte pieces are turned so that lanes that read together are in different banks
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = 4 * u + i;
-        *reinterpret_cast<u32x4*>(piece + r * kD + ((lane % 16) ^ (r % 8)) * 4) = w.bounds[i];
-      }
-      __builtin_amdgcn_wave_barrier();
-      f16x8 b[4];
-#pragma unroll
-      for (int s = 0; s < 4; ++s) b[s] = *reinterpret_cast<const f16x8*>(piece + lane % 16 * kD + ((4 * s + u) ^ (lane % 8)) * 4);
-      __builtin_amdgcn_wave_barrier();
       f32x4 sum[2] = {};
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+      for (int half = 0; half < 2; ++half) {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[s], rows[c][s], sum[c], 0, 0, 0);
+        for (int i = 0; i < 2; ++i)
+          *reinterpret_cast<u32x4*>(piece + (8 * i + lane / 8) * (kD / 2) + ((lane % 8) ^ (lane / 8)) * 4) = w.bounds[2 * half + i];
+        __builtin_amdgcn_wave_barrier();
+        f16x8 b[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) b[s] = *reinterpret_cast<const f16x8*>(piece + lane % 16 * (kD / 2) + ((4 * s + u) ^ (lane % 8)) * 4);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[s], rows[c][2 * half + s], sum[c], 0, 0, 0);
+      }
       // the lane has pages 4 u + 0..3 of the 16 for its columns
       int e[4];
 #pragma unroll
@@ -186,8 +185,8 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
       }
     };
     Way way = fetch(id, 0);
-    for (int chunk = wave; chunk < chunks; chunk += kScoring) {
-      const int next = id_of(kChunk * (chunk + kScoring) + lane), exponent = exponent_of(id);
+    for (int chunk = wave; chunk < chunks; chunk += WAVES) {
+      const int next = id_of(kChunk * (chunk + WAVES) + lane), exponent = exponent_of(id);
 #pragma unroll
       for (int turn = 0; turn < kTurns; ++turn) {
         const Way now = way;
@@ -199,7 +198,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
   }
   __syncthreads();
   // Then a wave takes a query.
-  uint32_t* scratch = pieces + wave * (kScoring * kPieceWords / WAVES);
+  uint32_t* scratch = piece;
   for (int query = wave; query < n; query += WAVES) {
     const int np = (tokens_seen(a, h, query0 + query) + kPage - 1) / kPage, turned = key_turn(query);
     float* row = keys + query * pitch;
@@ -374,7 +373,7 @@ Plan plan_of(const PagesArgs& a) {
 
 template <int WAVES, int N>
 hipError_t launch(const PagesArgs& a, const Plan& p, hipStream_t stream) {
-  const int bytes = (p.queries * p.pitch + std::min(WAVES, 8) * kPieceWords) * (int)sizeof(uint32_t), groups = (a.longest + p.queries - 1) / p.queries;
+  const int bytes = (p.queries * p.pitch + WAVES * kPieceWords) * (int)sizeof(uint32_t), groups = (a.longest + p.queries - 1) / p.queries;
   if (bytes > (48 << 10)) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_select_kernel<WAVES, N>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
