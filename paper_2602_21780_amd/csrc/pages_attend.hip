@@ -46,7 +46,7 @@ struct Shape;
 // for eight lines; it then takes 30 cycles for a load of 1 KB that takes 16 in order.  In order, each load brings 16 rows to LDS by itself, without
 // registers in between, and the lanes read their pieces there.  The four 16-byte pieces of a row are turned by an amount that goes by the row, so that the
 // eight lanes that read together are in different banks: keys' rows by key_turn(row of 4, which 16 rows), values' by value_turn(row).  (64 streams 82 -> 79 us,
-// a frame over chosen pages 121 -> 115.  With 32 columns arithmetic hides it, and loads to registers are faster: a frame 49 us, 51 through LDS.)
+// a frame over chosen pages 121 -> 115.)
 constexpr int kStagedBytes = 2 * kPageBytes;  // of a wave: keys and values of a page
 __device__ __forceinline__ int key_turn(int row, int rows) { return row / 2 % 2 + 2 * (rows % 2); }
 __device__ __forceinline__ int value_turn(int row) { return row / 2 % 4; }
@@ -68,21 +68,13 @@ __device__ __forceinline__ void wait_for_all_but_four() { asm volatile("s_waitcn
 template <>
 struct Shape<16> {
   using Acc = f32x4;
-  static constexpr int kKeys = 4, kChannels = 4, kLogits = 16;  // blocks of A in a page's keys and in the channels
   __device__ static __forceinline__ Acc mfma(bf16x8 a, bf16x8 b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-  // where in a page the lane's piece i of its four 16-byte pieces of keys, or of values, is
+  // where in a page the lane's piece i of its four 16-byte pieces of keys, or of values, is: of block i of the product's rows
   __device__ static __forceinline__ int key_at(int col, int quarter, int i) { return (16 * (col / 4) + 4 * i + col % 4) * kD + 16 * quarter; }
   __device__ static __forceinline__ int value_at(int col, int quarter, int i) { return (16 * i + col) * kPage + 16 * quarter; }
-  __device__ static __forceinline__ int query_at(int quarter) { return 16 * quarter; }
-  // key piece i feeds block and steps (of 8 channels a lane); value piece i its block and steps
-  static constexpr int key_block(int i) { return i; }
-  static constexpr int key_step(int i) { return 0; }
   // the same pieces in a page that stage() has brought to LDS: `first` and constants
   __device__ static __forceinline__ int staged_key(int col, int quarter, int i) { return col / 4 * 1024 + col % 4 * 64 + turned(quarter, key_turn(col % 4, col / 4)) + 256 * i; }
   __device__ static __forceinline__ int staged_value(int col, int quarter, int i) { return col * 64 + turned(quarter, value_turn(col)) + 1024 * i; }
-  static constexpr int value_block(int i) { return i; }
-  static constexpr int value_step(int i) { return 0; }
-  static constexpr int token(int e) { return e; }  // behind 16 * quarter
   __device__ static __forceinline__ int channel(int block, int quarter, int j) { return 16 * block + 4 * quarter + j; }
   __device__ static __forceinline__ float column_max(float x) {
     const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -100,22 +92,12 @@ struct Shape<16> {
 template <>
 struct Shape<32> {
   using Acc = f32x16;
-  static constexpr int kKeys = 2, kChannels = 2, kLogits = 32;
   __device__ static __forceinline__ Acc mfma(bf16x8 a, bf16x8 b, Acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-  __device__ static __forceinline__ int key_at(int col, int quarter, int i) {
-    return (32 * (i / 2) + 16 * (col / 4 % 2) + 4 * (col / 8) + col % 4) * kD + 32 * quarter + 16 * (i % 2);
-  }
-  __device__ static __forceinline__ int value_at(int col, int quarter, int i) { return (32 * (i % 2) + col) * kPage + 32 * (i / 2) + 16 * quarter; }
-  __device__ static __forceinline__ int query_at(int quarter) { return 32 * quarter; }
-  static constexpr int key_block(int i) { return i / 2; }
-  static constexpr int key_step(int i) { return i % 2 * 2; }
+  // pieces 2 h and 2 h + 1 are of tokens 32 h ..: keys by steps of 16 channels of a lane's 32, values by blocks of channels
   __device__ static __forceinline__ int staged_key(int col, int quarter, int i) {
     return col / 4 % 2 * 1024 + (4 * (col / 8) + col % 4) * 64 + turned(2 * quarter + i % 2, key_turn(col % 4, col / 4 % 2)) + 2048 * (i / 2);
   }
   __device__ static __forceinline__ int staged_value(int col, int quarter, int i) { return col * 64 + turned(2 * (i / 2) + quarter, value_turn(col % 16)) + 2048 * (i % 2); }
-  static constexpr int value_block(int i) { return i % 2; }
-  static constexpr int value_step(int i) { return i / 2 * 2; }
-  static constexpr int token(int e) { return 32 * (e / 16) + e % 16; }  // behind 16 * quarter
   __device__ static __forceinline__ int channel(int block, int quarter, int j) { return 32 * block + 8 * (j / 4) + 4 * quarter + j % 4; }
   __device__ static __forceinline__ float column_max(float x) {
     const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -135,6 +117,10 @@ __device__ __forceinline__ bf16x8 view8(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(bf16x8, w);
 }
 
+// (A page that was never written may have any scale: 0 would leave nothing of its probabilities.)
+__device__ __forceinline__ int exponent_of(float scale) { return min(max((int)((__float_as_uint(scale) >> 23) & 0xffu) - 127, -100), 120); }
+// What logits of a page are multiplied by, never 0: masked ones are -inf.
+__device__ __forceinline__ float factor_of(float c2, float scale) { return fmaxf(c2 * scale, 1.17549435e-38f); }
 // The NaN codes of a dword, as bytes 0xff.
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   uint32_t m = 0;
@@ -342,10 +328,12 @@ __device__ __forceinline__ void leave(const PagesArgs& a, const Block& b, const 
 
 struct Empty {};
 
-template <int COLS, bool CHOSEN, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || CHOSEN) ? 4 : 3) void pages_attend_kernel(PagesArgs a, int blocks) {
+// 16 rows of a key head at a time.
+template <bool CHOSEN, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kernel(PagesArgs a, int blocks) {
+  constexpr int COLS = 16;
   using S = Shape<COLS>;
-  constexpr bool kStaged = COLS == 16 && WAVES == kWaves;  // (the destination of such a load has 16 bits: 64 KB)
+  constexpr bool kStaged = WAVES == kWaves;  // (the destination of such a load has 16 bits: 64 KB)
   union Share {  // of a wave: its page, later its results, 16-byte pieces of row r in the order of their number xor r
     uint8_t page[kStagedBytes];
     f32x4 acc[COLS][kD / 4];
@@ -360,14 +348,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
   const Row own = row_of(a, b, col);
   const int32_t* table = a.table + (int64_t)b.s * a.width;
 
-  constexpr int kSteps = COLS / 8;  // of 8 channels, and of 8 tokens, a lane
-  bf16x8 qf[kSteps];
+  bf16x8 qf[2];  // a lane has 16 channels, and of what it works out of a page, 16 tokens
   {
-    const uint16_t* q = a.q.p + own.head * a.q.sh + (int64_t)(b.h.row0 + own.query) * a.q.st + S::query_at(quarter);
+    const uint16_t* q = a.q.p + own.head * a.q.sh + (int64_t)(b.h.row0 + own.query) * a.q.st + 16 * quarter;
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) qf[i] = *reinterpret_cast<const bf16x8*>(q + 8 * i);
+    for (int i = 0; i < 2; ++i) qf[i] = *reinterpret_cast<const bf16x8*>(q + 8 * i);
   }
-  typename S::Acc o[S::kChannels] = {};
+  f32x4 o[4] = {};
   float ref = -kInf, sum = 0.0f;
   const float c2 = a.scale * kLog2e;
 
@@ -407,9 +394,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
       for (int i = 0; i < 4; ++i) kr[i] = *reinterpret_cast<const u32x4*>(p + S::key_at(col, quarter, i));
     }
   };
-  constexpr int kEach = S::kLogits / S::kKeys;
-  typename S::Acc x[S::kKeys];
-  u32x4 pr[kSteps];
+  f32x4 x[4];
+  u32x4 pr[2];
   float part;  // sum of the lane's probabilities in a page
   auto fetch_values = [&](int page) {
     const uint8_t* p = a.v + ((size_t)page * a.kv_heads + b.kv) * kPageBytes;
@@ -437,20 +423,19 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
   };
   auto first_products = [&] {
 #pragma unroll
-    for (int i = 0; i < S::kKeys; ++i) x[i] = typename S::Acc{};
+    for (int i = 0; i < 4; ++i) {
+      x[i] = f32x4{};
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-        x[S::key_block(i)] = S::mfma(view8(kr[i][2 * k], kr[i][2 * k + 1]), qf[S::key_step(i) + k], x[S::key_block(i)]);
+      for (int k = 0; k < 2; ++k) x[i] = S::mfma(view8(kr[i][2 * k], kr[i][2 * k + 1]), qf[k], x[i]);
+    }
   };
   // The values' scale 2^ev goes into the exponent: what enters the second product is in the values' own units.
   auto weigh = [&](float cs, int ev, bool mine) {
     const float off = off_of(ref) - (float)ev;
     float one = 0.0f, other = 0.0f;
 #pragma unroll
-    for (int e = 0; e < S::kLogits; e += 2) {
-      const float p = exp2_(x[e / kEach][e % kEach] * cs - off), q = exp2_(x[e / kEach][e % kEach + 1] * cs - off);
+    for (int e = 0; e < 16; e += 2) {
+      const float p = exp2_(x[e / 4][e % 4] * cs - off), q = exp2_(x[e / 4][e % 4 + 1] * cs - off);
       one += p;
       other += q;
       pr[e / 8][e % 8 / 2] = pack2(p, q);
@@ -459,7 +444,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
     if (CHOSEN) {
       if (!mine) part = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 4 * kSteps; ++i) pr[i / 4][i % 4] = mine ? pr[i / 4][i % 4] : 0u;
+      for (int i = 0; i < 8; ++i) pr[i / 4][i % 4] = mine ? pr[i / 4][i % 4] : 0u;
     }
   };
   auto second_products = [&] {
@@ -467,17 +452,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int k = 0; k < 2; ++k)
-        o[S::value_block(i)] = S::mfma(view8(vr[i][2 * k], vr[i][2 * k + 1]), __builtin_bit_cast(bf16x8, pr[S::value_step(i) + k]), o[S::value_block(i)]);
+        o[i] = S::mfma(view8(vr[i][2 * k], vr[i][2 * k + 1]), __builtin_bit_cast(bf16x8, pr[k]), o[i]);
   };
-  // (a page that was never written may have any scale: 0 would leave nothing of its probabilities)
-  auto exponent_of = [](float scale) { return min(max((int)((__float_as_uint(scale) >> 23) & 0xffu) - 127, -100), 120); };
-  // What logits of a page are multiplied by, never 0: masked ones are -inf.
-  auto factor_of = [&](float scale) { return fmaxf(c2 * scale, 1.17549435e-38f); };
   // A page with all that may happen: rows that do not see some of it, references that move, values that are NaN.
   auto whole = [&](int ordinal, uint32_t rows, float ks, float vs, int next_page) {
     const bool mine = !CHOSEN || (rows >> col & 1);
     const int left = mine ? own.seen - ordinal * kPage - 16 * quarter : -kPage;  // of the tokens from the lane's first on
-    const float cs = factor_of(ks);
+    const float cs = factor_of(c2, ks);
     if constexpr (kStaged) wait_for_all();
     take_keys();
     first_products();
@@ -485,9 +466,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
     take_values();
     float m = -kInf;
 #pragma unroll
-    for (int e = 0; e < S::kLogits; ++e) {
-      const float y = S::token(e) < left ? x[e / kEach][e % kEach] : -kInf;
-      x[e / kEach][e % kEach] = y;
+    for (int e = 0; e < 16; ++e) {
+      const float y = e < left ? x[e / 4][e % 4] : -kInf;
+      x[e / 4][e % 4] = y;
       m = fmaxf(m, y);
     }
     m = S::column_max(m) * cs;
@@ -495,12 +476,12 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
     ref = to;
     sum *= f;
 #pragma unroll
-    for (int i = 0; i < S::kChannels; ++i) o[i] *= f;
+    for (int i = 0; i < 4; ++i) o[i] *= f;
     weigh(cs, exponent_of(vs), mine);
     sum += part;
     if (vs < 0.0f) {
       // 0 times NaN is NaN: values that are NaN are taken out of the product, and reach the rows that see their tokens by one of their own
-      typename S::Acc count[S::kChannels] = {};
+      f32x4 count[4] = {};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         u32x4 nan;
@@ -515,16 +496,16 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
           u32x4 sees;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const int e = 8 * (S::value_step(i) + k) + 2 * j;
-            sees[j] = (S::token(e) < left ? 0x3f80u : 0u) | (S::token(e + 1) < left ? 0x3f800000u : 0u);
+            const int e = 8 * k + 2 * j;
+            sees[j] = (e < left ? 0x3f80u : 0u) | (e + 1 < left ? 0x3f800000u : 0u);
           }
-          count[S::value_block(i)] = S::mfma(view8(nan[2 * k], nan[2 * k + 1]), __builtin_bit_cast(bf16x8, sees), count[S::value_block(i)]);
+          count[i] = S::mfma(view8(nan[2 * k], nan[2 * k + 1]), __builtin_bit_cast(bf16x8, sees), count[i]);
         }
       }
 #pragma unroll
-      for (int i = 0; i < S::kChannels; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < (int)(sizeof(typename S::Acc) / 4); ++j) o[i][j] = count[i][j] > 0.0f ? __builtin_nanf("") : o[i][j];
+        for (int j = 0; j < 4; ++j) o[i][j] = count[i][j] > 0.0f ? __builtin_nanf("") : o[i][j];
     }
     second_products();
   };
@@ -561,7 +542,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
           first_products();
           __builtin_amdgcn_sched_barrier(0);
           fetch_keys(next_page);
-          weigh(factor_of(ks), exponent_of(vs), mine);
+          weigh(factor_of(c2, ks), exponent_of(vs), mine);
           fetched = false;
           if (__any(part > kMaxPart)) break;
           __builtin_amdgcn_sched_barrier(0);
@@ -600,10 +581,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
   if constexpr (kStaged) wait_for_all();  // (the last page's keys, fetched again)
   const float total = S::column_sum(sum);
 #pragma unroll
-  for (int i = 0; i < S::kChannels; ++i)
-#pragma unroll
-    for (int j = 0; j < (int)(sizeof(typename S::Acc) / 4); j += 4)
-      shares[wave].acc[col][(S::channel(i, quarter, j) / 4) ^ (col % 16)] = f32x4{o[i][j], o[i][j + 1], o[i][j + 2], o[i][j + 3]};
+  for (int i = 0; i < 4; ++i)
+    shares[wave].acc[col][(S::channel(i, quarter, 0) / 4) ^ (col % 16)] = o[i];
   if (quarter == 0) {
     refs[wave][col] = ref;
     sums[wave][col] = total;
@@ -612,13 +591,17 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == kManyWaves || !(COLS == 32 || 
   leave<COLS, WAVES>(a, b, shares[0].acc[0], sizeof(Share) / sizeof(f32x4), refs[0], sums[0]);
 }
 
-// Many rows of a sequence, 64 of them at a time, which share a page's conversion to bf16.  A wave goes through units of 32 tokens and 32 rows; while it works on the
-// probabilities of one, its matrix instructions make the logits of the next and add up what the one before weighs.
-__global__ __launch_bounds__(64 * kWaves, 2) void pages_attend_rows_kernel(PagesArgs a, int blocks) {
+// Many rows of a sequence: kTiles times 32 of them at a time, which share a page's conversion to bf16.  A wave goes through units of 32 tokens and 32 rows; while it works on the
+// weights of one, its matrix instructions make the logits of the next and add up the values of the one before.  What bounds it are the vector unit's cycles: of a unit 16 logits a
+// lane with a multiplication, exp2, a sum and half a conversion each, 335 with 64 rows and 410 with 32 with its part of the page's conversions, and about 16 for each of its eight
+// matrix instructions, which hold up the others that long.  10992 rows over 16384 tokens, 16 heads: 756 us, 975 TFLOP/s (32 rows 860); four rows of eight heads each
+// over 32 caches of 4096 tokens: 46 us (weights and products one after the other 51).
+template <int kTiles>
+__global__ __launch_bounds__(64 * kWaves, kTiles == 1 ? 3 : 2) void pages_attend_rows_kernel(PagesArgs a, int blocks) {
   using S = Shape<32>;
-  constexpr int kTiles = 2, kRows = 32 * kTiles;
-  union Share {  // of a wave: two pages, later its results
-    uint8_t page[2][kStagedBytes];
+  constexpr int kRows = 32 * kTiles, kUnits = 2 * kTiles;
+  union Share {  // of a wave: one page or two, later its results
+    uint8_t page[kTiles][kStagedBytes];
     f32x4 acc[kRows][kD / 4];
   };
   __shared__ struct {
@@ -637,7 +620,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void pages_attend_rows_kernel(Pages
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
     const Row own = row_of(a, b, 32 * t + col);
-    const uint16_t* from = a.q.p + own.head * a.q.sh + (int64_t)(b.h.row0 + own.query) * a.q.st + S::query_at(quarter);
+    const uint16_t* from = a.q.p + own.head * a.q.sh + (int64_t)(b.h.row0 + own.query) * a.q.st + 32 * quarter;
 #pragma unroll
     for (int i = 0; i < 4; ++i) q[t][i] = *reinterpret_cast<const bf16x8*>(from + 8 * i);
     seen[t] = own.seen;
@@ -650,10 +633,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void pages_attend_rows_kernel(Pages
   int at_hand = 0;
   const uint32_t staged_at = (uint32_t)(size_t)(lds_byte*)shares.of[wave].page[0];
   const int key_from = lane / 4 * 64 + (lane - key_turn(lane / 4 % 4, 0)) % 4 * 16, value_from = lane / 4 * 64 + (lane + 4 - value_turn(lane / 4)) % 4 * 16;
+  auto fetch_keys = [&](int page, int place) {
+    stage(a.k + ((size_t)page * a.kv_heads + b.kv) * kPageBytes, key_from, key_from ^ 32, staged_at + place * kStagedBytes);
+  };
+  auto fetch_values = [&](int page, int place) {
+    stage(a.v + ((size_t)page * a.kv_heads + b.kv) * kPageBytes, value_from, value_from, staged_at + place * kStagedBytes + kPageBytes);
+  };
   auto fetch = [&](int page, int place) {
-    const size_t unit = ((size_t)page * a.kv_heads + b.kv) * kPageBytes;
-    stage(a.k + unit, key_from, key_from ^ 32, staged_at + place * kStagedBytes);
-    stage(a.v + unit, value_from, value_from, staged_at + place * kStagedBytes + kPageBytes);
+    fetch_keys(page, place);
+    fetch_values(page, place);
   };
   const int staged_key = S::staged_key(col, quarter, 0), staged_key1 = S::staged_key(col, quarter, 1), staged_value = S::staged_value(col, quarter, 0), staged_value1 = S::staged_value(col, quarter, 2);
   u32x4 kr[2], vr[2];   // 32 tokens as they are
@@ -698,19 +686,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void pages_attend_rows_kernel(Pages
     }
     return one + other;
   };
-  auto exponent_of = [](float scale) { return min(max((int)((__float_as_uint(scale) >> 23) & 0xffu) - 127, -100), 120); };
-  auto factor_of = [&](float scale) { return fmaxf(c2 * scale, 1.17549435e-38f); };
 
   // The page at hand with all that may happen, but for its first `skip` units.
-  auto whole = [&](int ordinal, int skip, float ks, float vs) {
-    const float cs = factor_of(ks);
+  auto whole = [&](int ordinal, int skip, float ks, float vs, [[maybe_unused]] int next_page) __attribute__((always_inline)) {
+    const float cs = factor_of(c2, ks);
     const int ev = exponent_of(vs);
     const float un = __int_as_float((127 - ev) << 23);
-    wait_for_all_but_eight();
+    if constexpr (kTiles == 1) wait_for_all();
+    else wait_for_all_but_eight();
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       read_keys(at_hand, h);
       read_values(at_hand, h);
+      if (kTiles == 1 && h == 1) fetch(next_page, 0);
       take_keys();
       bf16x8 nb[4] = {};
       if (vs < 0.0f) {
@@ -775,7 +763,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void pages_attend_rows_kernel(Pages
     float lane_ks = some ? a.k_scale[unit] : 0.0f, lane_vs = some ? a.v_scale[unit] : 0.0f;
     uint64_t mask = __ballot(some);
     if (!mask) continue;
-    int i = __builtin_ctzll(mask), next = 0, ordinal = 0;
+    int i = __builtin_ctzll(mask), next = 0, ordinal = 0, next_page = 0;
     float ks = 0.0f, vs = 0.0f;
     fetch(__builtin_amdgcn_readlane(lane_page, i), at_hand);
     asm volatile("" : "+v"(lane_ks), "+v"(lane_vs));  // (they are there: nothing waits for them in the loop)
@@ -785,7 +773,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void pages_attend_rows_kernel(Pages
       vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lane_vs), i));
       mask &= mask - 1;
       next = mask ? __builtin_ctzll(mask) : i;
-      fetch(__builtin_amdgcn_readlane(lane_page, next), at_hand ^ 1);
+      next_page = __builtin_amdgcn_readlane(lane_page, next);
+      if constexpr (kTiles == 2) fetch(next_page, at_hand ^ 1);
     };
     auto plain = [&] { return (ordinal + 1) * kPage <= b.least && vs >= 0.0f; };
     look_at();
@@ -801,30 +790,45 @@ __global__ __launch_bounds__(64 * kWaves, 2) void pages_attend_rows_kernel(Pages
         u32x4 pa[2], pb[2] = {};
 #pragma unroll
         for (int k = 0; k < 4; ++k) vb[k] = bf16x8{};
-        wait_for_all_but_eight();
+        vr[0] = vr[1] = u32x4{};
+        if constexpr (kTiles == 1) wait_for_all();
+        else wait_for_all_but_eight();
         read_keys(at_hand, 0);
         take_keys();
         xa = logits(0);
         while (true) {
-          const float cs = factor_of(ks);
+          const float cs = factor_of(c2, ks);
           const int ev = exponent_of(vs);
           const float un = __int_as_float((127 - ev) << 23);
           auto unit_of = [&](auto number, const f32x16& x, f32x16& x_next, u32x4 (&pr)[2], const u32x4 (&before)[2]) {
-            constexpr int u = decltype(number)::value, t = u % 2;
+            constexpr int u = decltype(number)::value, t = u % kTiles;
             __builtin_amdgcn_sched_barrier(0);
-            if (u == 0) {
-              read_keys(at_hand, 1);
-              read_values(at_hand, 0);
+            if constexpr (kTiles == 1) {
+              if (u == 1) {
+                wait_for_all();
+                read_values(0, 0);
+              }
+              read_keys(0, 1 - u);
+              if (u == 0) fetch_keys(next_page, 0);
+            } else {
+              if (u == 0) {
+                read_keys(at_hand, 1);
+                read_values(at_hand, 0);
+              }
+              if (u == 2) {
+                wait_for_all();
+                read_keys(at_hand ^ 1, 0);
+                read_values(at_hand, 1);
+              }
             }
-            if (u == 2) {
-              wait_for_all();
-              read_keys(at_hand ^ 1, 0);
-              read_values(at_hand, 1);
+            if (kTiles == 1 || u % 2 == 1) take_keys();
+            x_next = logits((t + 1) % kTiles);
+            if (kTiles == 1 || u % 2 == 1) take_values();
+            add_values((t + 1) % kTiles, before);
+            if (kTiles == 1 && u == 1) {
+              read_values(0, 1);
+              fetch_values(next_page, 0);
             }
-            if (u % 2 == 1) take_keys();
-            x_next = logits(1 - t);
-            if (u % 2 == 1) take_values();
-            add_values(1 - t, before);
             const float part = weigh(x, cs, ref[t] - (float)ev, pr) * un;
             asm volatile("" : "+v"(pr[0]), "+v"(pr[1]));  // (here, and not behind the branch: until then there would be twice as many registers)
             if (__any(part > kMaxPart)) {
@@ -837,22 +841,31 @@ __global__ __launch_bounds__(64 * kWaves, 2) void pages_attend_rows_kernel(Pages
           };
           if (!unit_of(std::integral_constant<int, 0>{}, xa, xb, pa, pb)) break;
           if (!unit_of(std::integral_constant<int, 1>{}, xb, xa, pb, pa)) break;
-          if (!unit_of(std::integral_constant<int, 2>{}, xa, xb, pa, pb)) break;
-          if (!unit_of(std::integral_constant<int, 3>{}, xb, xa, pb, pa)) break;
+          if constexpr (kTiles == 2) {
+            if (!unit_of(std::integral_constant<int, 2>{}, xa, xb, pa, pb)) break;
+            if (!unit_of(std::integral_constant<int, 3>{}, xb, xa, pb, pa)) break;
+          }
           last = !mask;
           if (last) break;
           i = next;
-          at_hand ^= 1;
+          if (kTiles == 2) at_hand ^= 1;
           look_at();
           if (!plain()) break;
         }
-        if (done) add_values(1, pb);
+        if (done) {
+          if (kTiles == 1) take_values();
+          add_values(kTiles - 1, pb);
+        }
         if (last) break;
+        if (kTiles == 1 && !done) {  // (the next page's are on their way there, or there)
+          wait_for_all();
+          fetch(__builtin_amdgcn_readlane(lane_page, i), 0);
+        }
       }
-      whole(ordinal, skip, ks, vs);
+      whole(ordinal, skip, ks, vs, next_page);
       if (!mask) break;
       i = next;
-      at_hand ^= 1;
+      if (kTiles == 2) at_hand ^= 1;
       look_at();
     }
     wait_for_all();  // (the last page once more)
@@ -989,8 +1002,8 @@ hipError_t launch(PagesArgs a, const Plan& p, hipStream_t stream) {
   a.group = p.group;
   a.ranked = p.ranked;
   a.part_sums = a.part + (int64_t)a.parts * a.heads * a.rows * kD;
-  if constexpr (COLS > 32) pages_attend_rows_kernel<<<(int)(p.units * p.parts), 64 * WAVES, 0, stream>>>(a, (int)p.blocks);
-  else pages_attend_kernel<COLS, CHOSEN, WAVES><<<(int)(p.units * p.parts), 64 * WAVES, 0, stream>>>(a, (int)p.blocks);
+  if constexpr (COLS >= 32) pages_attend_rows_kernel<COLS / 32><<<(int)(p.units * p.parts), 64 * WAVES, 0, stream>>>(a, (int)p.blocks);
+  else pages_attend_kernel<CHOSEN, WAVES><<<(int)(p.units * p.parts), 64 * WAVES, 0, stream>>>(a, (int)p.blocks);
   if (p.parts > 1) pages_join_kernel<COLS, CHOSEN><<<(int)p.units, 64 * kWaves, 0, stream>>>(a, (int)p.blocks);
   return hipGetLastError();
 }

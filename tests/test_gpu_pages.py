@@ -419,8 +419,9 @@ def test_logits_that_rise_in_one_of_many_blocks(half, tile, step):
     q[:, 16 * tile:16 * tile + 16] += direction     # (two heads a key head: rows 32 tile .. of the first 64)
     q = q.to(torch.bfloat16)
     for causal in (0, 1):
-        got = _attend_many(pages, q, [0, 64], table, [64 * 20 - 7], causal=causal)
-        plain.check_attend(pool, q, got, [0, 64], table, [64 * 20 - 7], causal, heads=[0, 7])
+        few = xsv.pages_attend(pages, q.to(DEV), _int([0, 64]), _int(table), _int([64 * 20 - 7]), causal=causal)     # (32 at a time)
+        for got in (few, _attend_many(pages, q, [0, 64], table, [64 * 20 - 7], causal=causal)):
+            plain.check_attend(pool, q, got, [0, 64], table, [64 * 20 - 7], causal, heads=[0, 7])
 
 
 @pytest.mark.parametrize("kv_heads", [3, 8])
