@@ -343,7 +343,8 @@ typedef struct {
  * tokens as keys.  With `chosen` (and count > 0) row r of key head g sees only tokens of the pages chosen[r][g][..], each a number of
  * a page of its sequence (entry of its row of the table), in any order; what is none, or none that it sees a token of, is left out, and a page
  * that is listed twice counts once.  A row that sees no token has out = 0 and lse = -inf.  A NaN reaches exactly the rows that see its token.  q, out: bf16 [heads][rows][64]
- * via strides; lse: float [heads][rows].  The same bits every time. */
+ * via strides; lse: float [heads][rows].  Sums are in fp32: elements of q and values of up to 1e20 do not overflow
+ * them where fp32 holds the logits.  The same bits every time. */
 int xsv_pages_attend(void* hip_stream, const xsv_pages* pages, const xsv_pages_query* cfg, xsv_tensor q, xsv_tensor out, float* lse, void* workspace,
                      int64_t workspace_bytes);
 int xsv_pages_attend_workspace(const xsv_pages* pages, const xsv_pages_query* cfg, int64_t* bytes);

@@ -33,7 +33,7 @@ __device__ __forceinline__ Touched touched(const PagesArgs& a, int s, int i) {
   t.h = held(a, s);
   const int start = max(t.h.ahead, 0), end = t.h.ahead + t.h.n;  // (rows in front of the first token have no place)
   t.ordinal = start / kPage + i;
-  const int p0 = t.ordinal * kPage;
+  const int p0 = min(t.ordinal, a.width) * kPage;  // (behind the table: no place; tokens are at most 2^30)
   t.from = max(start - p0, 0);
   t.to = min(end - p0, kPage);
   t.any = end > start && t.from < t.to;

@@ -72,7 +72,7 @@ template <int WAVES, int N>
 __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, int queries, int pitch) {
   extern __shared__ __align__(16) float keys[];  // [queries][pitch], scores of page j of query r at j ^ key_turn(r); behind them a piece of each scoring wave
   const int lane = threadIdx.x % 64, u = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int rep = a.heads / a.kv_heads, groups = (a.longest + queries - 1) / queries;
+  const int rep = a.heads / a.kv_heads, groups = (int)(((int64_t)a.longest + queries - 1) / queries);
   const int kv = blockIdx.x % a.kv_heads, group = blockIdx.x / a.kv_heads % groups, s = blockIdx.x / a.kv_heads / groups;
   const Held h = held(a, s);
   const int query0 = group * queries, n = min(queries, h.n - query0);
@@ -373,7 +373,7 @@ Plan plan_of(const PagesArgs& a) {
 
 template <int WAVES, int N>
 hipError_t launch(const PagesArgs& a, const Plan& p, hipStream_t stream) {
-  const int bytes = (p.queries * p.pitch + WAVES * kPieceWords) * (int)sizeof(uint32_t), groups = (a.longest + p.queries - 1) / p.queries;
+  const int bytes = (p.queries * p.pitch + WAVES * kPieceWords) * (int)sizeof(uint32_t), groups = (int)(((long long)a.longest + p.queries - 1) / p.queries);
   if (bytes > (48 << 10)) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_select_kernel<WAVES, N>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
@@ -395,8 +395,10 @@ hipError_t launch_for(const PagesArgs& a, const Plan& p, hipStream_t stream) {
 }  // namespace
 
 bool pages_select_fits(const PagesArgs& a) {
-  const long long most = (1ll << 32) / 1024 - 1;
-  return pages_held(a) <= kMostPages && (long long)a.longest * a.kv_heads <= most && (long long)a.longest * a.kv_heads * a.sequences <= most;
+  if (pages_held(a) > kMostPages) return false;
+  const Plan p = plan_of(a);
+  const long long most = (1ll << 32) / 1024 - 1, groups = ((long long)a.longest + p.queries - 1) / p.queries;  // (threads of a launch are counted in 32 bits)
+  return groups * a.kv_heads <= most && groups * a.kv_heads * a.sequences <= most;
 }
 
 hipError_t launch_pages_select(const PagesArgs& a, hipStream_t stream) {

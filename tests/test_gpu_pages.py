@@ -566,6 +566,15 @@ def test_choice_among_many_pages_and_within_a_bound():
     assert all(got[r, 0].tolist() == want[r, 0] for r in range(2))
 
 
+def test_choice_within_a_bound_far_above_many_sequences_rows():
+    """The launch is sized by groups of rows, not by rows."""
+    lengths = [130 + s for s in range(64)]
+    pages, table, pool = _filled(lengths, 16, 66)
+    q = _randn(16, 16, 4200, 64).to(torch.bfloat16).to(DEV)
+    call = lambda **kw: xsv.pages_select(pages, q, _int(_begin([1] * 64)), _table_tensor(table), _int(lengths), 2, causal=1, **kw)
+    assert torch.equal(call(), call(longest_q=1))
+
+
 @pytest.mark.parametrize("count,pages_in_all", [(65, 700), (100, 90), (200, 300), (64, 64)])
 def test_choice_of_more_pages_than_lanes(count, pages_in_all):
     pages, table, pool = _filled([64 * pages_in_all - 1], 2, 86)
