@@ -51,4 +51,10 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 __device__ __forceinline__ float bf16_low(uint32_t two) { return __uint_as_float(two << 16); }
 __device__ __forceinline__ float bf16_high(uint32_t two) { return __uint_as_float(two & 0xffff0000u); }
 
+__device__ __forceinline__ uint32_t wave_largest(uint32_t x) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) x = max(x, (uint32_t)__shfl_xor((int)x, d));
+  return x;
+}
+
 }  // namespace xsv

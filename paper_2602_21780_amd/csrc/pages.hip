@@ -98,12 +98,6 @@ struct Row16 {  // 16 channels of a token
   }
 };
 
-__device__ __forceinline__ uint32_t wave_largest(uint32_t x) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) x = max(x, (uint32_t)__shfl_xor((int)x, d));
-  return x;
-}
-
 __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int most) {
   __shared__ __align__(16) uint8_t lines[2][kD][kLine];  // the codes of keys and values by channel
   __shared__ uint32_t top[2][kThreads / 64];

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
   if (n <= 0) return;
   const int32_t* table = a.table + (int64_t)s * a.width;
   const int pages = (tokens_seen(a, h, query0 + n - 1) + kPage - 1) / kPage;  // (queries ascend, and so does what they see)
-  constexpr int kTurns = WAVES == 4 ? kFewTurns : 4, kChunk = 16 * kTurns;  // pages that a wave looks up together
+  constexpr int kTurns = WAVES == 8 ? kFewTurns : 4, kChunk = 16 * kTurns;  // pages that a wave looks up together
   const int chunks = a.pages > 0 ? (pages + kChunk - 1) / kChunk : 0;
   if (rep > 1 || chunks == 0) {
     for (int i = threadIdx.x; i < n * pitch; i += 64 * WAVES) keys[i] = kNone;
@@ -222,8 +222,11 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
     // The `left` largest scores of pages [begin, end).
     const int steps = (end + 63) / 64;
     bool chosen = left <= 0 || end <= begin;
+    const int run = (steps + 1) / 2 * 2;  // pages that a lane has side by side, so that lanes are in the order of pages
+    float held_scores[N > 0 ? N : 1], most = kNone;
+    uint32_t lower = ordered(kNone);  // at least as many scores as are wanted are larger
     if (!chosen && (N > 0 || steps == 1)) {
-      // A lane has `run` pages side by side, so that lanes are in the order of pages.  As many lanes as pages are wanted have a score of at least `least`, so what is below
+      // As many lanes as pages are wanted have a score of at least `least`, so what is below
       // is not chosen; what is not is rarely more than one a lane, and is then dealt out one a lane.
       float score = kNone;
       int page = lane, found = 0;
@@ -231,8 +234,6 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
         score = lane < end ? row[lane ^ turned] : kNone;
         found = 64;
       } else if constexpr (N > 0) {
-        const int run = (steps + 1) / 2 * 2;
-        float held_scores[N], most = kNone;
 #pragma unroll
         for (int i = 0; i < N; i += 2) {
           const int at = run * lane + i;
@@ -243,7 +244,9 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
           most = fmaxf(most, fmaxf(two[0], two[1]));
         }
         if (__popcll(__ballot(most != kNone)) >= left) {
-          const float least = unordered(nth_largest<kLeastBits>(ordered(most), left));
+          const uint32_t bits = nth_largest<kLeastBits>(ordered(most), left);
+          const float least = unordered(bits);
+          lower = bits - 1;
           uint32_t those = 0;
 #pragma unroll
           for (int i = N - 1; i >= 0; --i) those = 2 * those + (held_scores[i] >= least);
@@ -291,64 +294,111 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
       }
     }
     if (!chosen) {
-      auto over = [&](auto f) {  // f(step, key) for every step of 64 pages; none: 0
-        for (int i = 0; i < steps; ++i) {
-          const int j = 64 * i + lane;
-          const float x = j < end ? row[j ^ turned] : kNone;
-          f(i, x == kNone ? 0u : ordered(x));
-        }
-      };
-      auto count_above = [&](uint32_t x) {
-        int c = 0;
-        over([&](int, uint32_t k) { c += __popcll(__ballot(k > x)); });
-        return c;
-      };
-      // More than `left` keys are above lo, at most `left` above hi.
-      const int all = count_above(0), want = min(left, all);
-      uint32_t lo = 0, hi = 0xffffffffu;
-      int above_hi = 0;
-      if (all == want) {
-        hi = 0;
-        above_hi = want;
-      } else {
-        uint32_t least = 0xfffffffeu, most = 1;
-        over([&](int, uint32_t k) {
-          if (k) {
-            least = min(least, k);
-            most = max(most, k);
-          }
-        });
+      if constexpr (N > 0) {
+        auto count_above = [&](uint32_t x) {
+          const float bound = unordered(x);
+          int c = 0;
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-          least = min(least, (uint32_t)__shfl_xor((int)least, d));
-          most = max(most, (uint32_t)__shfl_xor((int)most, d));
-        }
-        lo = __builtin_amdgcn_readfirstlane(least) - 1;
-        hi = __builtin_amdgcn_readfirstlane(most);
-        above_hi = count_above(hi);
-        while (above_hi != want && hi - lo > 1) {
-          const uint32_t mid = lo + (hi - lo) / 2;
-          const int c = count_above(mid);
-          if (c > want) lo = mid;
-          else {
-            hi = mid;
-            above_hi = c;
+          for (int i = 0; i < N; ++i) c += __popcll(__ballot(held_scores[i] > bound));
+          return c;
+        };
+        // At least `want` scores are above lo, at most `want` above hi.
+        const int all = count_above(lower), want = min(left, all);
+        uint32_t lo = lower, hi = lo;
+        int above_hi = all;
+        if (all > want) {
+          hi = __builtin_amdgcn_readfirstlane(wave_largest(ordered(most)));
+          above_hi = 0;
+          while (above_hi != want && hi - lo > 1) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            const int c = count_above(mid);
+            if (c > want) lo = mid;
+            else {
+              hi = mid;
+              above_hi = c;
+            }
           }
         }
-      }
-      // In order: the keys above hi, and of those that equal it as many of the first as are wanted.
-      int equal = want - above_hi;
-      over([&](int i, uint32_t k) {
-        uint64_t takes = __ballot(k > hi);
-        if (equal > 0) {
-          const uint64_t ties = __ballot(k == hi);
-          const bool tie = k == hi && __popcll(ties & before) < equal;
-          takes |= __ballot(tie);
-          equal = max(equal - __popcll(ties), 0);
+        // Those above hi, and of those that equal it as many of the first as are wanted.
+        const float bound = unordered(hi);
+        uint32_t takes = 0, same = 0;
+#pragma unroll
+        for (int i = N - 1; i >= 0; --i) {
+          takes = 2 * takes + (held_scores[i] > bound);
+          same = 2 * same + (held_scores[i] == bound);
         }
-        if (takes >> lane & 1) out[done + __popcll(takes & before)] = 64 * i + lane;
-        done += __popcll(takes);
-      });
+        if (want > above_hi) {
+          const int own = __popc(same), rest = want - above_hi - (sum_upto(own) - own);  // that the lanes before leave
+          while (__popc(same) > max(rest, 0)) same &= ~(0x80000000u >> __builtin_clz(same));
+          takes |= same;
+        }
+        const int own = __popc(takes), upto = sum_upto(own);
+        for (int to = done + upto - own; __any(takes != 0); ++to)
+          if (takes) {
+            out[to] = run * lane + __builtin_ctz(takes);
+            takes &= takes - 1;
+          }
+        done += __builtin_amdgcn_readlane(upto, 63);
+      } else {
+        auto over = [&](auto f) {  // f(step, key) for every step of 64 pages; none: 0
+          for (int i = 0; i < steps; ++i) {
+            const int j = 64 * i + lane;
+            const float x = j < end ? row[j ^ turned] : kNone;
+            f(i, x == kNone ? 0u : ordered(x));
+          }
+        };
+        auto count_above = [&](uint32_t x) {
+          int c = 0;
+          over([&](int, uint32_t k) { c += __popcll(__ballot(k > x)); });
+          return c;
+        };
+        // More than `left` keys are above lo, at most `left` above hi.
+        const int all = count_above(0), want = min(left, all);
+        uint32_t lo = 0, hi = 0xffffffffu;
+        int above_hi = 0;
+        if (all == want) {
+          hi = 0;
+          above_hi = want;
+        } else {
+          uint32_t least = 0xfffffffeu, most = 1;
+          over([&](int, uint32_t k) {
+            if (k) {
+              least = min(least, k);
+              most = max(most, k);
+            }
+          });
+#pragma unroll
+          for (int d = 1; d < 64; d *= 2) {
+            least = min(least, (uint32_t)__shfl_xor((int)least, d));
+            most = max(most, (uint32_t)__shfl_xor((int)most, d));
+          }
+          lo = __builtin_amdgcn_readfirstlane(least) - 1;
+          hi = __builtin_amdgcn_readfirstlane(most);
+          above_hi = count_above(hi);
+          while (above_hi != want && hi - lo > 1) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            const int c = count_above(mid);
+            if (c > want) lo = mid;
+            else {
+              hi = mid;
+              above_hi = c;
+            }
+          }
+        }
+        // In order: the keys above hi, and of those that equal it as many of the first as are wanted.
+        int equal = want - above_hi;
+        over([&](int i, uint32_t k) {
+          uint64_t takes = __ballot(k > hi);
+          if (equal > 0) {
+            const uint64_t ties = __ballot(k == hi);
+            const bool tie = k == hi && __popcll(ties & before) < equal;
+            takes |= __ballot(tie);
+            equal = max(equal - __popcll(ties), 0);
+          }
+          if (takes >> lane & 1) out[done + __popcll(takes & before)] = 64 * i + lane;
+          done += __popcll(takes);
+        });
+      }
     }
     for (int j0 = end; j0 < np; j0 += 64) {
       const uint64_t some = j0 == end ? last : last_some(j0);
@@ -404,7 +454,7 @@ bool pages_select_fits(const PagesArgs& a) {
 hipError_t launch_pages_select(const PagesArgs& a, hipStream_t stream) {
   if (a.sequences == 0 || a.longest == 0 || a.count == 0) return hipSuccess;
   const Plan p = plan_of(a);
-  if (p.queries <= 4) return launch_for<4>(a, p, stream);
+  if (p.queries <= 4) return launch_for<8>(a, p, stream);
   return launch_for<16>(a, p, stream);
 }
 
