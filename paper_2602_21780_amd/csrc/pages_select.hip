@@ -225,40 +225,73 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
     const int run = (steps + 1) / 2 * 2;  // pages that a lane has side by side, so that lanes are in the order of pages
     float held_scores[N > 0 ? N : 1], most = kNone;
     uint32_t lower = ordered(kNone);  // at least as many scores as are wanted are larger
-    if (!chosen && (N > 0 || steps == 1)) {
-      // As many lanes as pages are wanted have a score of at least `least`, so what is below
-      // is not chosen; what is not is rarely more than one a lane, and is then dealt out one a lane.
+    if (!chosen) {
+      // As many lanes as pages are wanted have a score of at least `least`, so what is below is not chosen; what is not is rarely more than one a lane, and is then
+      // dealt out one a lane.
       float score = kNone;
       int page = lane, found = 0;
       if (steps == 1) {
         score = lane < end ? row[lane ^ turned] : kNone;
         found = 64;
-      } else if constexpr (N > 0) {
-#pragma unroll
-        for (int i = 0; i < N; i += 2) {
+      } else {
+        auto two_at = [&](int i) {  // of this lane's pages
           const int at = run * lane + i;
-          f32x2 two = {kNone, kNone};
-          if (i < run && at < end) two = *reinterpret_cast<const f32x2*>(row + (at ^ turned));
-          held_scores[i] = two[0];
-          held_scores[i + 1] = two[1];
-          most = fmaxf(most, fmaxf(two[0], two[1]));
+          return i < run && at < end ? *reinterpret_cast<const f32x2*>(row + (at ^ turned)) : f32x2{kNone, kNone};
+        };
+        if constexpr (N > 0) {
+#pragma unroll
+          for (int i = 0; i < N; i += 2) {
+            const f32x2 two = two_at(i);
+            held_scores[i] = two[0];
+            held_scores[i + 1] = two[1];
+            most = fmaxf(most, fmaxf(two[0], two[1]));
+          }
+        } else {
+#pragma unroll 8
+          for (int i = 0; i < run; i += 2) {
+            const f32x2 two = two_at(i);
+            most = fmaxf(most, fmaxf(two[0], two[1]));
+          }
         }
         if (__popcll(__ballot(most != kNone)) >= left) {
           const uint32_t bits = nth_largest<kLeastBits>(ordered(most), left);
           const float least = unordered(bits);
           lower = bits - 1;
           uint32_t those = 0;
+          int own = 0;
+          if constexpr (N > 0) {
 #pragma unroll
-          for (int i = N - 1; i >= 0; --i) those = 2 * those + (held_scores[i] >= least);
-          const int own = __popc(those), upto = sum_upto(own);
+            for (int i = N - 1; i >= 0; --i) those = 2 * those + (held_scores[i] >= least);
+            own = __popc(those);
+          } else {
+#pragma unroll 8
+            for (int i = 0; i < run; i += 2) {
+              const f32x2 two = two_at(i);
+              own += (two[0] >= least) + (two[1] >= least);
+            }
+          }
+          const int upto = sum_upto(own);
           found = __builtin_amdgcn_readlane(upto, 63);
           if (found <= 64) {
-            for (int to = upto - own; __any(those != 0); ++to) {
-              if (those) {
-                const int at = run * lane + __builtin_ctz(those);
-                scratch[to] = __float_as_uint(row[at ^ turned]);
-                scratch[64 + to] = at;
-                those &= those - 1;
+            int to = upto - own;
+            auto deal = [&](int at, float x) {
+              scratch[to] = __float_as_uint(x);
+              scratch[64 + to] = at;
+              ++to;
+            };
+            if constexpr (N > 0) {
+              for (; __any(those != 0);)
+                if (those) {
+                  const int at = run * lane + __builtin_ctz(those);
+                  deal(at, row[at ^ turned]);
+                  those &= those - 1;
+                }
+            } else {
+              for (int i = 0; i < run; i += 2) {
+                const f32x2 two = two_at(i);
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                  if (two[k] >= least) deal(run * lane + i + k, two[k]);
               }
             }
             __builtin_amdgcn_wave_barrier();
