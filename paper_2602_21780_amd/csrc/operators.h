@@ -1,5 +1,5 @@
 // Internal interface of the stateless operators around the step (not part of the ABI): what operators_api.hip has checked and
-// hands to the kernels of rotate.hip and seq_attend.hip.
+// hands to the kernels of rotate.hip, seq_attend.hip, pages.hip, pages_attend.hip and pages_select.hip.
 #pragma once
 
 #include "xsv_internal.h"

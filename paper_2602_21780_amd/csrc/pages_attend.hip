@@ -3,7 +3,12 @@
 //   S = scale * k_scale * (q . code_k) over the tokens that a row sees,  lse = log sum exp(S),  out = exp(S - lse) (code_v * v_scale)
 //
 // Codes become bf16 as they are (e4m3 has 4 significant bits, bf16 has 8), one instruction for two; the page's scales are powers of two,
-// so that multiplying logits and probabilities by them instead rounds nothing.
+// so that multiplying logits and probabilities by them instead rounds nothing.  (Products in 8 bits would spare the keys' conversions, with q as the sum of two codes; but those matrix
+// instructions lose what lies 2^-11 below their largest product, also with scales for blocks: measured.)  Probabilities are rounded to bf16 once, as the second product's operands.
+//
+// One pass over the pages with a reference logit per row and a sum; a workgroup's four waves take every fourth page and are joined in LDS, and where there are too few blocks of rows
+// to fill the card, workgroups share a block's pages and a second launch joins them in their order.  Few rows (decoding) are bounded by memory: 64 streams of 60 to 32768 tokens, 32
+// heads on 8, 79 us, 4.5 TB/s of codes.  Many rows are bounded by the vector unit (below): a frame of 1374 over 5470 tokens, 16 heads, 45.5 us, 680 TFLOP/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -22,9 +27,10 @@ constexpr int kLongest = 64;
 // over 512 to 4096 tokens 12 and 16, over 8192 20 and 16; 64 over 4096 13 and 16, over 8192 20 and 18; 256 over 4096 27 and 33 (over 8192 49 and 56, but
 // there sequences of different lengths would leave compute units empty).
 constexpr int kManyUnits = 256, kManyPages = 64;
-// 64 rows to a wave, if that fills the card: two workgroups on each of 256 compute units.  us, 64 rows and 32 (16 heads): 10992 rows over 16384 tokens 756 and 860,
-// 2748 over 8192 109 and 124, 2048 behind 6144 of their own (512 blocks) 75 and 79; 1374 over 5470 (352 blocks) 51 and 46.  Fewer blocks if all parts of their pages are
-// long: 512 over 65536 tokens (4 parts of 256 pages) 172 and 187, 128 over 131072 (16 of 128) 109 and 114, but 256 over 8192 (8 of 16) 40 and 32.
+// 64 rows to a wave, if that fills the card: two workgroups on each of 256 compute units.  us, 64 rows and 32 (16 heads): 10992 rows over 16384 tokens 744 and 857,
+// 2748 over 8192 107 and 122, 2048 behind 6144 of their own (512 blocks) 75 and 79; 1374 over 5470 (352 blocks) 51 and 46.  Just above a full card they are even (2100 over
+// 8192, 528 blocks: 106 and 102).  Fewer blocks if all parts of their pages are long: 512 over 65536 tokens (4 parts of 256 pages) 169 and 192, 128 over 131072 (16 of
+// 128) 109 and 118, but 256 over 8192 (8 of 16) 40 and 32.
 constexpr long long kFull = 512, kLongPart = 128;
 constexpr int kListRows = 16;  // rows that share a list of chosen pages
 // Probabilities are taken against a reference logit per row, which moves when the sum over what a lane has of a page passes this:
@@ -328,7 +334,9 @@ __device__ __forceinline__ void leave(const PagesArgs& a, const Block& b, const 
 
 struct Empty {};
 
-// 16 rows of a key head at a time.
+// 16 rows of a key head at a time: single tokens, and chosen pages, where each row has its own and a page is worked on for all 16 once any has chosen it.  Those
+// are bounded by the vector unit, too (66 % of the cycles, and the matrix instructions that hold it up): a page is 64 conversions and 16 logits a lane whether one row
+// has it or all.  1374 queries of 16 heads that choose 32 of 1024 pages, 23 of them the same: 114 us.
 template <bool CHOSEN, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kernel(PagesArgs a, int blocks) {
   constexpr int COLS = 16;
@@ -594,7 +602,7 @@ __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kerne
 // Many rows of a sequence: kTiles times 32 of them at a time, which share a page's conversion to bf16.  A wave goes through units of 32 tokens and 32 rows; while it works on the
 // weights of one, its matrix instructions make the logits of the next and add up the values of the one before.  What bounds it are the vector unit's cycles: of a unit 16 logits a
 // lane with a multiplication, exp2, a sum and half a conversion each, 335 with 64 rows and 410 with 32 with its part of the page's conversions, and about 16 for each of its eight
-// matrix instructions, which hold up the others that long.  10992 rows over 16384 tokens, 16 heads: 756 us, 975 TFLOP/s (32 rows 860); four rows of eight heads each
+// matrix instructions, which hold up the others that long.  10992 rows over 16384 tokens, 16 heads: 744 us, 992 TFLOP/s (32 rows 857); four rows of eight heads each
 // over 32 caches of 4096 tokens: 46 us (weights and products one after the other 51).
 template <int kTiles>
 __global__ __launch_bounds__(64 * kWaves, kTiles == 1 ? 3 : 2) void pages_attend_rows_kernel(PagesArgs a, int blocks) {

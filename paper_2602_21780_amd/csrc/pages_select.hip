@@ -7,9 +7,11 @@
 // and all partial sums below 64 * 255 * 896 < 2^24, so that fp32 holds each exactly in any order: the same pages whatever
 // computes them, and equal scores are equal.  A row's `first` and `last` pages are chosen whatever their scores; equal scores go to the lower page.
 //
-// A workgroup has some queries of one key head, 32 rows (query, head) of a product if it can, whose pages it scores together, 16 a wave and turn, from
-// the pool into keys in LDS; then a wave takes a query, its keys in registers: the n-th largest of each lane's largest is a bound that few more than n keys
-// pass, and those are looked at one a lane.
+// A workgroup has some queries of one key head, 32 rows (query, head) of a product if it can, whose pages its waves score together, 16 a wave and turn, from
+// the pool into scores in LDS; then a wave takes a query, its scores in registers.  The n-th largest of each lane's largest is a bound that few more than n scores
+// pass, and those are looked at one a lane: each counts the larger ones.  Scores are read from memory once per 32 rows and never written there; what bounds it are the
+// instructions of both halves, some 6 and 5 of a workgroup's 15 us, and waits between them, with one workgroup of 16 waves on a compute unit: 1374 queries of 16 heads choose
+// 32 of 1024 pages each in 44 us (16 queries and two workgroups 48), 64 streams 32 of up to 512 in 16 (calls one behind the other, from Python).
 #include <algorithm>
 
 #include "pages.h"
@@ -20,10 +22,11 @@ namespace {
 using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
 using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
 
-constexpr int kFewTurns = 2;
-constexpr int kLeastBits = 16;   // of a bound on the scores that are chosen: sign, exponent and 7 more
+// Workgroups of a query or a few have 8 waves, which look up 32 pages at a time (64 streams over up to 512 pages 16.1 us; 4 waves 16.3, 16 waves 20.6).
+constexpr int kFewWaves = 8, kFewTurns = 2, kFewQueries = 4;
+constexpr int kLeastBits = 16;   // of a bound on the scores that are chosen: sign, exponent and 7 more (14: 64 streams 23.4 us, 16 to 20: 17)
 constexpr int kMostPages = 32768;  // scores of a row's pages are held in LDS
-constexpr int kMostKeys = 32768;   // of a workgroup: 128 KB, and 32 for the waves' pieces
+constexpr int kMostScores = 32768;   // of a workgroup: 128 KB, and 32 for the waves' pieces
 constexpr int kHole = -(1 << 20);  // the exponent of a page that is none
 
 constexpr float kNone = -kInf;  // the score of a page that is none
@@ -51,8 +54,8 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
 }
 
 constexpr int kPieceWords = 16 * kD / 2;  // of a wave: LDS to bring one of 16 pages' bounds, upper or lower, into the order of a product's rows
-// Where a query's keys are turned to, so that what 16 queries side by side write is in different banks.
-__device__ __forceinline__ int key_turn(int query) { return query % 16 * 4; }
+// Where a query's scores are turned to, so that what 16 queries side by side write is in different banks.
+__device__ __forceinline__ int score_turn(int query) { return query % 16 * 4; }
 
 // The first BITS bits of the n-th largest of a wave's keys, one a lane (0 if there are fewer), two bits at a time: the three counts do not wait for one another.
 template <int BITS>
@@ -67,10 +70,10 @@ __device__ __forceinline__ uint32_t nth_largest(uint32_t key, int n) {
   return x;
 }
 
-// N: keys of a query that a lane holds (0: as many as there are, from LDS each time).
+// N: scores of a query that a lane holds (0: as many as there are, from LDS each time).
 template <int WAVES, int N>
 __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, int queries, int pitch) {
-  extern __shared__ __align__(16) float keys[];  // [queries][pitch], scores of page j of query r at j ^ key_turn(r); behind them a piece of each scoring wave
+  extern __shared__ __align__(16) float scores[];  // [queries][pitch], of page j of query r at j ^ score_turn(r); behind them a piece of each wave
   const int lane = threadIdx.x % 64, u = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int rep = a.heads / a.kv_heads, groups = (int)(((int64_t)a.longest + queries - 1) / queries);
   const int kv = blockIdx.x % a.kv_heads, group = blockIdx.x / a.kv_heads % groups, s = blockIdx.x / a.kv_heads / groups;
@@ -79,13 +82,13 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
   if (n <= 0) return;
   const int32_t* table = a.table + (int64_t)s * a.width;
   const int pages = (tokens_seen(a, h, query0 + n - 1) + kPage - 1) / kPage;  // (queries ascend, and so does what they see)
-  constexpr int kTurns = WAVES == 8 ? kFewTurns : 4, kChunk = 16 * kTurns;  // pages that a wave looks up together
+  constexpr int kTurns = WAVES == kFewWaves ? kFewTurns : 4, kChunk = 16 * kTurns;  // pages that a wave looks up together
   const int chunks = a.pages > 0 ? (pages + kChunk - 1) / kChunk : 0;
   if (rep > 1 || chunks == 0) {
-    for (int i = threadIdx.x; i < n * pitch; i += 64 * WAVES) keys[i] = kNone;
+    for (int i = threadIdx.x; i < n * pitch; i += 64 * WAVES) scores[i] = kNone;
     __syncthreads();
   }
-  uint32_t* piece = reinterpret_cast<uint32_t*>(keys + queries * pitch) + wave * kPieceWords;
+  uint32_t* piece = reinterpret_cast<uint32_t*>(scores + queries * pitch) + wave * kPieceWords;
   auto id_of = [&](int ordinal) {  // a page of the pool, or none
     const int id = ordinal < pages ? table[ordinal] : -1;
     return id < a.pages ? id : -1;
@@ -175,7 +178,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
           const float k = __builtin_amdgcn_ldexpf(sum[c][j], min(max(t[c] + e[j], -100), 100));
           key[j] = e[j] == kHole ? kNone : k;
         }
-        float* to = keys + query[c] * pitch + ((kChunk * chunk + 16 * turn + 4 * u) ^ key_turn(query[c]));
+        float* to = scores + query[c] * pitch + ((kChunk * chunk + 16 * turn + 4 * u) ^ score_turn(query[c]));
         if (rep == 1) {
           *reinterpret_cast<f32x4*>(to) = key;
         } else {
@@ -200,8 +203,8 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
   // Then a wave takes a query.
   uint32_t* scratch = piece;
   for (int query = wave; query < n; query += WAVES) {
-    const int np = (tokens_seen(a, h, query0 + query) + kPage - 1) / kPage, turned = key_turn(query);
-    float* row = keys + query * pitch;
+    const int np = (tokens_seen(a, h, query0 + query) + kPage - 1) / kPage, turned = score_turn(query);
+    float* row = scores + query * pitch;
     int32_t* out = a.choice + ((int64_t)(h.row0 + query0 + query) * a.kv_heads + kv) * a.count;
     const uint64_t before = (1ull << lane) - 1;
     const int begin = min(a.first, np), end = max(np - a.last, begin);  // of the pages that are chosen by their scores
@@ -445,12 +448,12 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
 int pages_held(const PagesArgs& a) { return std::min(a.width, (int)(((long long)a.longest_k + kPage - 1) / kPage)); }
 
 struct Plan {
-  int queries, pitch;  // of a workgroup; keys of a query
+  int queries, pitch;  // of a workgroup; scores of a query
 };
 Plan plan_of(const PagesArgs& a) {
   Plan p;
   p.pitch = (std::max(pages_held(a), 1) + 63) / 64 * 64;
-  p.queries = std::max(std::min({32 / (a.heads / a.kv_heads), a.longest, kMostKeys / p.pitch}), 1);
+  p.queries = std::max(std::min({32 / (a.heads / a.kv_heads), a.longest, kMostScores / p.pitch}), 1);
   return p;
 }
 
@@ -487,7 +490,7 @@ bool pages_select_fits(const PagesArgs& a) {
 hipError_t launch_pages_select(const PagesArgs& a, hipStream_t stream) {
   if (a.sequences == 0 || a.longest == 0 || a.count == 0) return hipSuccess;
   const Plan p = plan_of(a);
-  if (p.queries <= 4) return launch_for<8>(a, p, stream);
+  if (p.queries <= kFewQueries) return launch_for<kFewWaves>(a, p, stream);
   return launch_for<16>(a, p, stream);
 }
 

@@ -561,6 +561,7 @@ def test_choice_among_many_pages_and_within_a_bound():
     pages, table, pool = _filled(lengths, 1, 87)
     q = _randn(17, 2, 2, 64).to(torch.bfloat16).to(DEV)
     _check_select(pages, pool, q, [0, 2], table, lengths, 64, 2, 2, 1)
+    _check_select(pages, pool, q, [0, 2], table, lengths, 9, 1, 2, 1)
     got = xsv.pages_select(pages, q, _int([0, 2]), _int(table), _int(lengths), 8, causal=0, longest_k=1000).cpu()
     want = plain.select(pool, q, [0, 2], table, [1000], 8, 1, 1, 0)
     assert all(got[r, 0].tolist() == want[r, 0] for r in range(2))
