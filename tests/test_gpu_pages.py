@@ -206,7 +206,7 @@ def test_reading_into_a_packed_tensor_and_past_pages_that_are_none():
 @pytest.mark.parametrize("causal", [0, 1, 59])
 @pytest.mark.parametrize("heads,kv_heads,new,lengths", [
     (1, 1, [1], [1]), (2, 2, [1], [63]), (4, 1, [1, 1, 1], [64, 65, 1]), (12, 4, [1, 63, 64, 0, 130], [1, 100, 64, 9, 300]), (16, 16, [17], [500]),
-    (40, 2, [3, 1], [129, 64]), (7, 7, [5, 1], [3, 700]), (33, 1, [2], [70]), (6, 2, [200], [333])])
+    (40, 2, [3, 1], [129, 64]), (7, 7, [5, 1], [3, 700]), (33, 1, [2], [70]), (6, 2, [200], [333]), (4, 2, [40, 3, 20], [5, 0, 20])])
 def test_attention_over_pages(heads, kv_heads, new, lengths, causal):
     print(f"pages_attend heads={heads}/{kv_heads} new={new} lengths={lengths} causal={causal}", flush=True)
     pages, table, pool = _filled(lengths, kv_heads, sum(lengths) + causal)
@@ -370,7 +370,7 @@ def _attend_many(pages, q, begin, table, lengths, **kw):
 
 
 @pytest.mark.parametrize("causal", [0, 1, 59])
-@pytest.mark.parametrize("new,lengths", [([1], [1]), ([70], [500]), ([300], [300]), ([33, 0, 64, 129, 5], [33, 9, 300, 128, 700])])
+@pytest.mark.parametrize("new,lengths", [([1], [1]), ([70], [500]), ([300], [300]), ([33, 0, 64, 129, 5], [33, 9, 300, 128, 700]), ([40, 3, 20], [5, 0, 20])])
 def test_many_blocks_of_rows(new, lengths, causal):
     print(f"pages_attend of 64 rows new={new} lengths={lengths} causal={causal}", flush=True)
     pages, table, pool = _filled(lengths, 8, 61 + sum(new))
