@@ -73,27 +73,33 @@ __device__ __forceinline__ uint32_t within(int at, int from, int to) {
   return m;
 }
 
+using u16x2 = __attribute__((ext_vector_type(2))) uint16_t;
 struct Row16 {  // 16 channels of a token
   u32x4 r[2];
   __device__ __forceinline__ void load(const uint16_t* p) {
     r[0] = *reinterpret_cast<const u32x4*>(p);
     r[1] = *reinterpret_cast<const u32x4*>(p + 8);
   }
-  __device__ __forceinline__ uint32_t largest() const {
-    uint32_t m = 0;
+  // of |x|, bits of fp32; `all`: also of what is not finite
+  __device__ __forceinline__ uint32_t largest(bool all) const {
+    u16x2 m = {0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t lo = (r[i / 4][i % 4] << 16) & 0x7fff0000u, hi = r[i / 4][i % 4] & 0x7fff0000u;
-      m = max(m, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+      u16x2 x = __builtin_bit_cast(u16x2, r[i / 4][i % 4] & 0x7fff7fffu);
+      if (!all) x = u16x2{(uint16_t)(x[0] < 0x7f80 ? x[0] : 0), (uint16_t)(x[1] < 0x7f80 ? x[1] : 0)};
+      m = __builtin_elementwise_max(m, x);
     }
-    return m;
+    return (uint32_t)max(m[0], m[1]) << 16;
   }
-  __device__ __forceinline__ u32x4 codes(float f) const {
+  __device__ __forceinline__ u32x4 codes(float f, bool finite) const {
     u32x4 c;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t a = r[i / 2][i % 2 * 2], b = r[i / 2][i % 2 * 2 + 1];
-      c[i] = codes4(finite_or_nan(bf16_low(a)) * f, finite_or_nan(bf16_high(a)) * f, finite_or_nan(bf16_low(b)) * f, finite_or_nan(bf16_high(b)) * f);
+      float x[4] = {bf16_low(a), bf16_high(a), bf16_low(b), bf16_high(b)};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = (finite ? x[j] : finite_or_nan(x[j])) * f;
+      c[i] = codes4(x[0], x[1], x[2], x[3]);
     }
     return c;
   }
@@ -126,7 +132,15 @@ __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int 
     if (is_old) old_k = *reinterpret_cast<const u32x4*>(to_k);
     old_v = *reinterpret_cast<const u32x4*>(to_v);
   }
-  const uint32_t mk = wave_largest(k.largest()), mv = wave_largest(v.largest());
+  // (rows that are not all finite are rare, and take the way of their own)
+  uint32_t mk = k.largest(true), mv = v.largest(true);
+  const bool finite = !__any(max(mk, mv) >= 0x7f800000u);
+  if (!finite) {
+    mk = k.largest(false);
+    mv = v.largest(false);
+  }
+  mk = wave_largest(mk);
+  mv = wave_largest(mv);
   if (tid % 64 == 0) {
     top[0][tid / 64] = mk;
     top[1][tid / 64] = mv;
@@ -142,8 +156,17 @@ __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int 
     e[x] = max(exponent_of(m), e_old);
     grown[x] = t.from > 0 ? e[x] - e_old : 0;
   }
-  u32x4 ck = k.codes(power(-e[0])), cv = v.codes(power(-e[1]));
-  const bool nan = __any(has_nan(cv[0]) || has_nan(cv[1]) || has_nan(cv[2]) || has_nan(cv[3]));
+  const float fk = power(-e[0]), fv = power(-e[1]);
+  u32x4 ck, cv;
+  bool nan = false;
+  if (finite) {
+    ck = k.codes(fk, true);
+    cv = v.codes(fv, true);
+  } else {
+    ck = k.codes(fk, false);
+    cv = v.codes(fv, false);
+    nan = __any(has_nan(cv[0]) || has_nan(cv[1]) || has_nan(cv[2]) || has_nan(cv[3]));
+  }
   if (tid % 64 == 0) none[tid / 64] = nan;
   if (is_old) {
     ck = old_k;
@@ -180,16 +203,17 @@ __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int 
   if (!a.bounds) return;
   const u32x4 line = *reinterpret_cast<const u32x4*>(&lines[0][channel][place]);
   float hi = -kInf, lo = kInf;
+  const bool full = t.to == kPage;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(line[j], false), y = __builtin_amdgcn_cvt_pk_f32_fp8(line[j], true);
     const float four[4] = {x[0], x[1], y[0], y[1]};
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
-      if (place + 4 * j + b < t.to && four[b] == four[b]) {
-        hi = fmaxf(hi, four[b]);
-        lo = fminf(lo, four[b]);
-      }
+    for (int b = 0; b < 4; ++b) {  // (the larger of a number and NaN is the number)
+      const bool here = full || place + 4 * j + b < t.to;
+      hi = fmaxf(hi, here ? four[b] : -kInf);
+      lo = fminf(lo, here ? four[b] : kInf);
+    }
   }
 #pragma unroll
   for (int d = 1; d < 4; d *= 2) {
