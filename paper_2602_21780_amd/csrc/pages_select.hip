@@ -36,6 +36,12 @@ __device__ __forceinline__ uint32_t ordered(float x) {
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float unordered(uint32_t k) { return __uint_as_float(k >> 31 ? k ^ 0x80000000u : ~k); }
+template <int CTRL>
+__device__ __forceinline__ f32x4 larger(f32x4 x) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = fmaxf(x[j], __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x[j]), CTRL, 0xf, 0xf, true)));
+  return x;
+}
 // The sum over lanes up to and with this one: rows of 16 by DPP, then what the rows before have.
 __device__ __forceinline__ int sum_upto(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
@@ -71,7 +77,8 @@ __device__ __forceinline__ uint32_t nth_largest(uint32_t key, int n) {
 }
 
 // N: scores of a query that a lane holds (0: as many as there are, from LDS each time).
-template <int WAVES, int N>
+// SETS: of 16 columns of a product, rows (query, head), that a wave has at once.
+template <int WAVES, int N, int SETS>
 __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, int queries, int pitch) {
   extern __shared__ __align__(16) float scores[];  // [queries][pitch], of page j of query r at j ^ score_turn(r); behind them a piece of each wave
   const int lane = threadIdx.x % 64, u = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -84,7 +91,9 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
   const int pages = (tokens_seen(a, h, query0 + n - 1) + kPage - 1) / kPage;  // (queries ascend, and so does what they see)
   constexpr int kTurns = WAVES == kFewWaves ? kFewTurns : 4, kChunk = 16 * kTurns;  // pages that a wave looks up together
   const int chunks = a.pages > 0 ? (pages + kChunk - 1) / kChunk : 0;
-  if (rep > 1 || chunks == 0) {
+  // The heads of a query are side by side in 16 columns, if their number divides 16: the largest of their scores is what one of them writes.
+  const bool side_by_side = rep <= 16 && (rep & (rep - 1)) == 0;
+  if (!side_by_side || chunks == 0) {
     for (int i = threadIdx.x; i < n * pitch; i += 64 * WAVES) scores[i] = kNone;
     __syncthreads();
   }
@@ -93,7 +102,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
     const int id = ordinal < pages ? table[ordinal] : -1;
     return id < a.pages ? id : -1;
   };
-  for (int c0 = 0; c0 < n * rep && wave < min(WAVES, chunks); c0 += 32) {
+  for (int c0 = 0; c0 < n * rep && wave < min(WAVES, chunks); c0 += 16 * SETS) {
     // A wave takes kChunk pages, one to a lane, that are looked up together while those before them are worked on, and then 16 at a time.  Of those, the lane has
     // page lane % 16 in the product, and 16 bytes of one of the bounds of pages lane / 8 and 8 + lane / 8 on their way there: 8 lanes side by side take 128 bytes (with
     // a page to a lane, every lane asks for a line of its own, and a load takes the memory path 59 cycles instead of 16).
@@ -111,12 +120,14 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
       return id >= 0 ? (int)((__float_as_uint(a.k_scale[(size_t)id * a.kv_heads + kv]) >> 23) & 0xffu) - 128 : kHole;
     };
     int id = id_of(kChunk * wave + lane);
-    // The lane's two columns, a query of a head each, and 8 channels of each half (columns behind the last are copies of it that change nothing)
-    int query[2], t[2];
-    f16x8 rows[2][4];  // channels 8 u .., 32 + 8 u .. above zero, and below
+    // The lane's columns, a query of a head each, and 8 channels of each half (columns behind the last are copies of it that nobody writes)
+    int query[SETS], t[SETS];
+    bool real[SETS];
+    f16x8 rows[SETS][4];  // channels 8 u .., 32 + 8 u .. above zero, and below
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
+    for (int c = 0; c < SETS; ++c) {
       const int col = min(c0 + 16 * c + lane % 16, n * rep - 1);
+      real[c] = c0 + 16 * c + lane % 16 < n * rep;
       query[c] = col / rep;
       const uint16_t* q = a.q.p + (int64_t)(kv * rep + col % rep) * a.q.sh + (h.row0 + query0 + query[c]) * a.q.st + 8 * u;
       float x[16], m = 0.0f;
@@ -150,7 +161,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
     }
     auto score = [&](const Way& w, int exponent, int chunk, int turn) {
       // through this wave's piece of LDS (its accesses stay in order); a page's 16-byte pieces are turned so that lanes that read together are in different banks
-      f32x4 sum[2] = {};
+      f32x4 sum[SETS] = {};
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
 #pragma unroll
@@ -164,14 +175,14 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int c = 0; c < 2; ++c) sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[s], rows[c][2 * half + s], sum[c], 0, 0, 0);
+          for (int c = 0; c < SETS; ++c) sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[s], rows[c][2 * half + s], sum[c], 0, 0, 0);
       }
       // the lane has pages 4 u + 0..3 of the 16 for its columns
       int e[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) e[j] = __shfl(exponent, 16 * turn + 4 * u + j);
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
+      for (int c = 0; c < SETS; ++c) {
         f32x4 key;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -179,21 +190,32 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
           key[j] = e[j] == kHole ? kNone : k;
         }
         float* to = scores + query[c] * pitch + ((kChunk * chunk + 16 * turn + 4 * u) ^ score_turn(query[c]));
-        if (rep == 1) {
+        if (rep == 1) {  // (copies write the same)
           *reinterpret_cast<f32x4*>(to) = key;
-        } else {
+        } else if (side_by_side) {
+          key = larger<0xb1>(key);   // of lane ^ 1
+          if (rep > 2) key = larger<0x4e>(key);   // lane ^ 2
+          if (rep > 4) key = larger<0x141>(key);  // the other four of eight
+          if (rep > 8) key = larger<0x140>(key);  // the other eight of sixteen
+          if (real[c] && lane % rep == 0) *reinterpret_cast<f32x4*>(to) = key;
+        } else if (real[c]) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) __hip_atomic_fetch_max(to + j, key[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
         }
       }
     };
-    Way way = fetch(id, 0);
+    constexpr int kAhead = SETS == 1 ? kTurns : 1;  // turns whose bounds are on their way
+    Way ways[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) ways[i] = fetch(id, i);
     for (int chunk = wave; chunk < chunks; chunk += WAVES) {
+      const bool more = chunk + WAVES < chunks;
       const int next = id_of(kChunk * (chunk + WAVES) + lane), exponent = exponent_of(id);
 #pragma unroll
       for (int turn = 0; turn < kTurns; ++turn) {
-        const Way now = way;
-        way = turn < kTurns - 1 ? fetch(id, turn + 1) : fetch(next, 0);
+        const Way now = ways[turn % kAhead];
+        if (turn + kAhead < kTurns) ways[turn % kAhead] = fetch(id, turn + kAhead);
+        else if (more) ways[turn % kAhead] = fetch(next, turn + kAhead - kTurns);
         score(now, exponent, chunk, turn);
       }
       id = next;
@@ -457,25 +479,25 @@ Plan plan_of(const PagesArgs& a) {
   return p;
 }
 
-template <int WAVES, int N>
+template <int WAVES, int N, int SETS>
 hipError_t launch(const PagesArgs& a, const Plan& p, hipStream_t stream) {
   const int bytes = (p.queries * p.pitch + WAVES * kPieceWords) * (int)sizeof(uint32_t), groups = (int)(((long long)a.longest + p.queries - 1) / p.queries);
   if (bytes > (48 << 10)) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_select_kernel<WAVES, N>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_select_kernel<WAVES, N, SETS>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  pages_select_kernel<WAVES, N><<<a.sequences * groups * a.kv_heads, 64 * WAVES, bytes, stream>>>(a, p.queries, p.pitch);
+  pages_select_kernel<WAVES, N, SETS><<<a.sequences * groups * a.kv_heads, 64 * WAVES, bytes, stream>>>(a, p.queries, p.pitch);
   return hipGetLastError();
 }
 
-template <int WAVES>
+template <int WAVES, int SETS>
 hipError_t launch_for(const PagesArgs& a, const Plan& p, hipStream_t stream) {
   const int held = pages_held(a);
-  if (held <= 256) return launch<WAVES, 4>(a, p, stream);
-  if (held <= 512) return launch<WAVES, 8>(a, p, stream);
-  if (held <= 1024) return launch<WAVES, 16>(a, p, stream);
-  if (held <= 2048) return launch<WAVES, 32>(a, p, stream);
-  return launch<WAVES, 0>(a, p, stream);
+  if (held <= 256) return launch<WAVES, 4, SETS>(a, p, stream);
+  if (held <= 512) return launch<WAVES, 8, SETS>(a, p, stream);
+  if (held <= 1024) return launch<WAVES, 16, SETS>(a, p, stream);
+  if (held <= 2048) return launch<WAVES, 32, SETS>(a, p, stream);
+  return launch<WAVES, 0, SETS>(a, p, stream);
 }
 
 }  // namespace
@@ -490,8 +512,8 @@ bool pages_select_fits(const PagesArgs& a) {
 hipError_t launch_pages_select(const PagesArgs& a, hipStream_t stream) {
   if (a.sequences == 0 || a.longest == 0 || a.count == 0) return hipSuccess;
   const Plan p = plan_of(a);
-  if (p.queries <= kFewQueries) return launch_for<kFewWaves>(a, p, stream);
-  return launch_for<16>(a, p, stream);
+  if (p.queries <= kFewQueries) return p.queries * (a.heads / a.kv_heads) <= 16 ? launch_for<kFewWaves, 1>(a, p, stream) : launch_for<kFewWaves, 2>(a, p, stream);
+  return launch_for<16, 2>(a, p, stream);
 }
 
 }  // namespace xsv
