@@ -11,7 +11,8 @@
 // the pool into scores in LDS; then a wave takes a query, its scores in registers.  The n-th largest of each lane's largest is a bound that few more than n scores
 // pass, and those are looked at one a lane: each counts the larger ones.  Scores are read from memory once per 32 rows and never written there; what bounds it are the
 // instructions of both halves, some 6 and 5 of a workgroup's 15 us, and waits between them, with one workgroup of 16 waves on a compute unit: 1374 queries of 16 heads choose
-// 32 of 1024 pages each in 44 us (16 queries and two workgroups 48), 64 streams 32 of up to 512 in 16 (calls one behind the other, from Python).
+// 32 of 1024 pages each in 44 us (16 queries and two workgroups 48).  A few queries (decoding) are a chain of waits, and have all bounds of four products' pages on their way
+// at once: 64 streams choose 32 of up to 512 pages in 10 us, of which the host's call is 9 (one product ahead, and heads joined by atomics: 16).
 #include <algorithm>
 
 #include "pages.h"
@@ -22,9 +23,9 @@ namespace {
 using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
 using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
 
-// Workgroups of a query or a few have 8 waves, which look up 32 pages at a time (64 streams over up to 512 pages 16.1 us; 4 waves 16.3, 16 waves 20.6).
+// Workgroups of a query or a few have 8 waves, which look up 32 pages at a time (64 streams over up to 512 pages 10.1 us, 64 at a time 13.6).
 constexpr int kFewWaves = 8, kFewTurns = 2, kFewQueries = 4;
-constexpr int kLeastBits = 16;   // of a bound on the scores that are chosen: sign, exponent and 7 more (14: 64 streams 23.4 us, 16 to 20: 17)
+constexpr int kLeastBits = 16;   // of a bound on the scores that are chosen: sign, exponent and 7 more (with 14, 64 streams took 6 us longer, with 18 or 20 as long)
 constexpr int kMostPages = 32768;  // scores of a row's pages are held in LDS
 constexpr int kMostScores = 32768;   // of a workgroup: 128 KB, and 32 for the waves' pieces
 constexpr int kHole = -(1 << 20);  // the exponent of a page that is none
