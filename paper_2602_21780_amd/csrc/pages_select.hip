@@ -7,11 +7,11 @@
 // and all partial sums below 64 * 255 * 896 < 2^24, so that fp32 holds each exactly in any order: the same pages whatever
 // computes them, and equal scores are equal.  A row's `first` and `last` pages are chosen whatever their scores; equal scores go to the lower page.
 //
-// A workgroup has some queries of one key head, 32 rows (query, head) of a product if it can, whose pages its waves score together, 16 a wave and turn, from
+// A workgroup has some queries of one key head, 16 or 32 rows (query, head) of a product if it can, whose pages its waves score together, 16 a wave and turn, from
 // the pool into scores in LDS; then a wave takes a query, its scores in registers.  The n-th largest of each lane's largest is a bound that few more than n scores
-// pass, and those are looked at one a lane: each counts the larger ones.  Scores are read from memory once per 32 rows and never written there; what bounds it are the
-// instructions of both halves, some 6 and 5 of a workgroup's 15 us, and waits between them, with one workgroup of 16 waves on a compute unit: 1374 queries of 16 heads choose
-// 32 of 1024 pages each in 44 us (16 queries and two workgroups 48).  A few queries (decoding) are a chain of waits, and have all bounds of four products' pages on their way
+// pass, and those are looked at one a lane: each counts the larger ones.  Bounds are read from memory once per workgroup and scores never written there; what bounds it are waits:
+// the two halves take some 6 and 5 of a workgroup's 15 us, with one workgroup of 16 waves on a compute unit (a quarter fewer instructions changed nothing): 1374 queries of 16 heads choose
+// 32 of 1024 pages each in 44 us.  A few queries (decoding) are a chain of waits, and have all bounds of four products' pages on their way
 // at once: 64 streams choose 32 of up to 512 pages in 10 us, of which the host's call is 9 (one product ahead, and heads joined by atomics: 16).
 #include <algorithm>
 
@@ -24,7 +24,7 @@ using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
 using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
 
 // Workgroups of a query or a few have 8 waves, which look up 32 pages at a time (64 streams over up to 512 pages 10.1 us, 64 at a time 13.6).
-constexpr int kFewWaves = 8, kFewTurns = 2, kFewQueries = 4;
+constexpr int kFewTurns = 2, kFewQueries = 4;
 constexpr int kLeastBits = 16;   // of a bound on the scores that are chosen: sign, exponent and 7 more (with 14, 64 streams took 6 us longer, with 18 or 20 as long)
 constexpr int kMostPages = 32768;  // scores of a row's pages are held in LDS
 constexpr int kMostScores = 32768;   // of a workgroup: 128 KB, and 32 for the waves' pieces
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
   if (n <= 0) return;
   const int32_t* table = a.table + (int64_t)s * a.width;
   const int pages = (tokens_seen(a, h, query0 + n - 1) + kPage - 1) / kPage;  // (queries ascend, and so does what they see)
-  constexpr int kTurns = WAVES == kFewWaves ? kFewTurns : 4, kChunk = 16 * kTurns;  // pages that a wave looks up together
+  constexpr int kTurns = WAVES == 8 ? kFewTurns : 4, kChunk = 16 * kTurns;  // pages that a wave looks up together
   const int chunks = a.pages > 0 ? (pages + kChunk - 1) / kChunk : 0;
   // The heads of a query are side by side in 16 columns, if their number divides 16: the largest of their scores is what one of them writes.
   const bool side_by_side = rep <= 16 && (rep & (rep - 1)) == 0;
@@ -470,13 +470,22 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
 
 int pages_held(const PagesArgs& a) { return std::min(a.width, (int)(((long long)a.longest_k + kPage - 1) / kPage)); }
 
+// 16 rows and 8 waves to a workgroup where several fit a compute unit, one's choice beside the other's scores; else 32 rows and 16 waves.  us, 16 rows and 32, 1374 queries of 16
+// heads: 32 of 625 pages 42 and 45, of 896 47 and 49, of 1024 51 and 51, of 1100 (one workgroup) 84 and 67; of 256 pages with four heads to a key head 71 and 89.
+// With eight, 16 rows are two queries, a choice for two waves of eight: 700 queries, 256 pages, 37 and 28.
+constexpr int kSharedPages = 960, kSharedHeads = 4;
+
 struct Plan {
   int queries, pitch;  // of a workgroup; scores of a query
+  int columns;
 };
 Plan plan_of(const PagesArgs& a) {
   Plan p;
+  const int rep = a.heads / a.kv_heads;
   p.pitch = (std::max(pages_held(a), 1) + 63) / 64 * 64;
-  p.queries = std::max(std::min({32 / (a.heads / a.kv_heads), a.longest, kMostScores / p.pitch}), 1);
+  p.columns = p.pitch <= kSharedPages && rep <= kSharedHeads ? 16 : 32;
+  p.queries = std::max(std::min({p.columns / rep, a.longest, kMostScores / p.pitch}), 1);
+  if (p.queries <= kFewQueries && p.queries * rep <= 16) p.columns = 16;
   return p;
 }
 
@@ -513,8 +522,8 @@ bool pages_select_fits(const PagesArgs& a) {
 hipError_t launch_pages_select(const PagesArgs& a, hipStream_t stream) {
   if (a.sequences == 0 || a.longest == 0 || a.count == 0) return hipSuccess;
   const Plan p = plan_of(a);
-  if (p.queries <= kFewQueries) return p.queries * (a.heads / a.kv_heads) <= 16 ? launch_for<kFewWaves, 1>(a, p, stream) : launch_for<kFewWaves, 2>(a, p, stream);
-  return launch_for<16, 2>(a, p, stream);
+  if (p.columns == 16) return launch_for<8, 1>(a, p, stream);
+  return p.queries <= kFewQueries ? launch_for<8, 2>(a, p, stream) : launch_for<16, 2>(a, p, stream);
 }
 
 }  // namespace xsv

@@ -567,6 +567,15 @@ def test_choice_among_many_pages_and_within_a_bound():
     assert all(got[r, 0].tolist() == want[r, 0] for r in range(2))
 
 
+@pytest.mark.parametrize("heads,kv_heads,length", [(2, 2, 64 * 1000 + 5), (5, 1, 2000), (6, 1, 64 * 1100), (4, 1, 64 * 900)])
+def test_choice_for_many_queries_of_a_workgroup(heads, kv_heads, length):
+    """16 and 32 rows, heads side by side and not, lists of few and of many."""
+    pages, table, pool = _filled([length], kv_heads, 88)
+    q = _randn(18, heads, 19, 64).to(torch.bfloat16).to(DEV)
+    for count in (9, 70):
+        _check_select(pages, pool, q, [0, 19], table, [length], count, 1, 2, 1)
+
+
 def test_choice_within_a_bound_far_above_many_sequences_rows():
     """The launch is sized by groups of rows, not by rows."""
     lengths = [130 + s for s in range(64)]
