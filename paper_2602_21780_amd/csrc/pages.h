@@ -43,6 +43,31 @@ __device__ __forceinline__ int tokens_seen(const PagesArgs& a, const Held& h, in
   return (int)min((int64_t)h.m, ((int64_t)(at / a.causal) + 1) * a.causal);
 }
 
+// Block number `*block` of all sequences' blocks (at most 64 sequences), `blocks_of(h)` of each, those of the sequences that see the most pages first: it becomes its number within its
+// sequence.  A lane looks a sequence up.
+template <typename F>
+__device__ __forceinline__ bool ranked_block(const PagesArgs& a, F blocks_of, int* block, int* sequence, Held* h) {
+  const int lane = threadIdx.x % 64;
+  Held own{};
+  int blocks = 0, cost = -1, before = 0;
+  if (lane < a.sequences) {
+    own = held(a, lane);
+    blocks = blocks_of(own);
+    cost = own.n > 0 ? tokens_seen(a, own, own.n - 1) : 0;
+  }
+  for (int s = 0; s < a.sequences; ++s) {
+    const int other = __builtin_amdgcn_readlane(cost, s), n = __builtin_amdgcn_readlane(blocks, s);
+    before += other > cost || (other == cost && s < lane) ? n : 0;
+  }
+  const uint64_t here = __ballot(lane < a.sequences && before <= *block && *block < before + blocks);
+  if (!here) return false;
+  const int s = __builtin_ctzll(here);
+  *sequence = s;
+  *block -= __builtin_amdgcn_readlane(before, s);
+  *h = Held{__builtin_amdgcn_readlane(own.row0, s), __builtin_amdgcn_readlane(own.n, s), __builtin_amdgcn_readlane(own.m, s), __builtin_amdgcn_readlane(own.ahead, s)};
+  return true;
+}
+
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const bf16x2 p = {(__bf16)a, (__bf16)b};
   return __builtin_bit_cast(uint32_t, p);

@@ -162,31 +162,6 @@ __device__ __forceinline__ Row row_of(const PagesArgs& a, const Block& b, int i)
   return r;
 }
 
-// Block number `*block` of all sequences' blocks of a key head (at most 64 sequences), those of the sequences that see the most pages first, of a sequence the
-// last first: it becomes the number of blocks behind it in its sequence.  A lane looks a sequence up.
-template <int COLS>
-__device__ __forceinline__ bool ranked_block(const PagesArgs& a, int* block, int* sequence, Held* h) {
-  const int lane = threadIdx.x % 64, rep = a.heads / a.kv_heads;
-  Held own{};
-  int blocks = 0, cost = -1, before = 0;
-  if (lane < a.sequences) {
-    own = held(a, lane);
-    blocks = (int)(((int64_t)own.n * rep + COLS - 1) / COLS);
-    cost = own.n > 0 ? tokens_seen(a, own, own.n - 1) : 0;
-  }
-  for (int s = 0; s < a.sequences; ++s) {
-    const int other = __builtin_amdgcn_readlane(cost, s), n = __builtin_amdgcn_readlane(blocks, s);
-    before += other > cost || (other == cost && s < lane) ? n : 0;
-  }
-  const uint64_t here = __ballot(lane < a.sequences && before <= *block && *block < before + blocks);
-  if (!here) return false;
-  const int s = __builtin_ctzll(here);
-  *sequence = s;
-  *block -= __builtin_amdgcn_readlane(before, s);
-  *h = Held{__builtin_amdgcn_readlane(own.row0, s), __builtin_amdgcn_readlane(own.n, s), __builtin_amdgcn_readlane(own.m, s), __builtin_amdgcn_readlane(own.ahead, s)};
-  return true;
-}
-
 // All pages: rows (query, head) COLS at a time.  Chosen pages: `group` queries with their heads, or 16 heads of a query that has more.
 // Sequences' blocks are counted from their ends, so that under a mask those that see the most come first, and those of a short sequence behind a long
 // cache, which see as much, among them; up to 64 sequences go by what they see (sequences of 0 to 1374 rows over up to 5470 tokens 55 -> 47 us).  Workgroups are dealt to the XCDs one by one; where eight divides the key
@@ -198,6 +173,8 @@ __device__ __forceinline__ bool block_of(const PagesArgs& a, int number, int blo
   const int heads = a.kv_heads % 8 ? a.kv_heads : a.kv_heads / 8, at = a.kv_heads % 8 ? number : number / 8;
   const int sequences = a.ranked ? 1 : a.sequences, units = heads * sequences * blocks, unit = at % units;
   b->part = at / units;
+  const int per = CHOSEN && rep > COLS ? (rep + COLS - 1) / COLS : 1;  // blocks of a query
+  auto blocks_of = [&](const Held& h) { return CHOSEN ? (int)(((int64_t)h.n + a.group - 1) / a.group) * per : (int)(((int64_t)h.n * rep + COLS - 1) / COLS); };
   int back;  // blocks of the sequence behind this one
   if (a.kv_heads % 8) {
     b->kv = unit % heads;
@@ -209,12 +186,11 @@ __device__ __forceinline__ bool block_of(const PagesArgs& a, int number, int blo
     b->kv = number % 8 * heads + unit / sequences / blocks;
   }
   if (a.ranked) {
-    if (!ranked_block<COLS>(a, &back, &b->s, &b->h)) return false;
+    if (!ranked_block(a, blocks_of, &back, &b->s, &b->h)) return false;
   } else {
     b->h = held(a, b->s);
   }
-  const int per = CHOSEN && rep > COLS ? (rep + COLS - 1) / COLS : 1;  // blocks of a query
-  const int block = (CHOSEN ? (b->h.n + a.group - 1) / a.group * per : (int)(((int64_t)b->h.n * rep + COLS - 1) / COLS)) - 1 - back;
+  const int block = blocks_of(b->h) - 1 - back;
   if (block < 0) return false;
   b->query0 = CHOSEN ? block / per * a.group : 0;
   b->queries = CHOSEN ? min(a.group, b->h.n - b->query0) : b->h.n;
@@ -967,8 +943,11 @@ Plan plan_of(const PagesArgs& a) {
   p.cols = 16;
   if (a.chosen) {
     if (rep <= kListRows) p.group = std::min(kListRows / rep, std::max(a.longest, 1));
-    p.blocks = ((long long)a.longest + p.group - 1) / p.group * ((rep + kListRows - 1) / kListRows);
-    p.units = times(times(p.blocks, a.kv_heads), a.sequences);
+    const int per = (rep + kListRows - 1) / kListRows;
+    p.blocks = ((long long)a.longest + p.group - 1) / p.group * per;
+    p.ranked = p.blocks > 1 && a.sequences > 1 && a.sequences <= 64;
+    if (p.ranked) p.blocks = std::min(times(p.blocks, a.sequences), (((long long)a.rows + p.group - 1) / p.group + a.sequences) * per);  // of all sequences
+    p.units = times(times(p.blocks, a.kv_heads), p.ranked ? 1 : a.sequences);
     p.parts = (int)std::max<long long>(std::min<long long>(512 / std::max(p.units, 1ll), (a.count + kWaves - 1) / kWaves), 1);
   } else {
     const long long rows = (long long)a.longest * rep;

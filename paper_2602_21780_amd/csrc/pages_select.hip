@@ -83,9 +83,17 @@ template <int WAVES, int N, int SETS>
 __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, int queries, int pitch) {
   extern __shared__ __align__(16) float scores[];  // [queries][pitch], of page j of query r at j ^ score_turn(r); behind them a piece of each wave
   const int lane = threadIdx.x % 64, u = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int rep = a.heads / a.kv_heads, groups = (int)(((int64_t)a.longest + queries - 1) / queries);
-  const int kv = blockIdx.x % a.kv_heads, group = blockIdx.x / a.kv_heads % groups, s = blockIdx.x / a.kv_heads / groups;
-  const Held h = held(a, s);
+  const int rep = a.heads / a.kv_heads, kv = blockIdx.x % a.kv_heads;
+  int group = blockIdx.x / a.kv_heads, s;
+  Held h;
+  if (a.ranked) {
+    if (!ranked_block(a, [&](const Held& h) { return (int)(((int64_t)h.n + queries - 1) / queries); }, &group, &s, &h)) return;
+  } else {
+    const int groups = (int)(((int64_t)a.longest + queries - 1) / queries);
+    s = group / groups;
+    group %= groups;
+    h = held(a, s);
+  }
   const int query0 = group * queries, n = min(queries, h.n - query0);
   if (n <= 0) return;
   const int32_t* table = a.table + (int64_t)s * a.width;
@@ -478,6 +486,8 @@ constexpr int kSharedPages = 960, kSharedHeads = 4;
 struct Plan {
   int queries, pitch;  // of a workgroup; scores of a query
   int columns;
+  long long groups;    // of queries of a sequence, or of all
+  bool ranked;
 };
 Plan plan_of(const PagesArgs& a) {
   Plan p;
@@ -486,17 +496,21 @@ Plan plan_of(const PagesArgs& a) {
   p.columns = p.pitch <= kSharedPages && rep <= kSharedHeads ? 16 : 32;
   p.queries = std::max(std::min({p.columns / rep, a.longest, kMostScores / p.pitch}), 1);
   if (p.queries <= kFewQueries && p.queries * rep <= 16) p.columns = 16;
+  p.groups = ((long long)a.longest + p.queries - 1) / p.queries;
+  p.ranked = p.groups > 1 && a.sequences > 1 && a.sequences <= 64;
+  if (p.ranked) p.groups = std::min(p.groups * a.sequences, ((long long)a.rows + p.queries - 1) / p.queries + a.sequences);
   return p;
 }
 
 template <int WAVES, int N, int SETS>
-hipError_t launch(const PagesArgs& a, const Plan& p, hipStream_t stream) {
-  const int bytes = (p.queries * p.pitch + WAVES * kPieceWords) * (int)sizeof(uint32_t), groups = (int)(((long long)a.longest + p.queries - 1) / p.queries);
+hipError_t launch(PagesArgs a, const Plan& p, hipStream_t stream) {
+  const int bytes = (p.queries * p.pitch + WAVES * kPieceWords) * (int)sizeof(uint32_t);
+  a.ranked = p.ranked;
   if (bytes > (48 << 10)) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_select_kernel<WAVES, N, SETS>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  pages_select_kernel<WAVES, N, SETS><<<a.sequences * groups * a.kv_heads, 64 * WAVES, bytes, stream>>>(a, p.queries, p.pitch);
+  pages_select_kernel<WAVES, N, SETS><<<(int)(p.groups * a.kv_heads * (p.ranked ? 1 : a.sequences)), 64 * WAVES, bytes, stream>>>(a, p.queries, p.pitch);
   return hipGetLastError();
 }
 
@@ -515,8 +529,8 @@ hipError_t launch_for(const PagesArgs& a, const Plan& p, hipStream_t stream) {
 bool pages_select_fits(const PagesArgs& a) {
   if (pages_held(a) > kMostPages) return false;
   const Plan p = plan_of(a);
-  const long long most = (1ll << 32) / 1024 - 1, groups = ((long long)a.longest + p.queries - 1) / p.queries;  // (threads of a launch are counted in 32 bits)
-  return groups * a.kv_heads <= most && groups * a.kv_heads * a.sequences <= most;
+  const long long most = (1ll << 32) / 1024 - 1;  // (threads of a launch are counted in 32 bits)
+  return p.groups * a.kv_heads <= most && p.groups * a.kv_heads * (p.ranked ? 1 : a.sequences) <= most;
 }
 
 hipError_t launch_pages_select(const PagesArgs& a, hipStream_t stream) {
