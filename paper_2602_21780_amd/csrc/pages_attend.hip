@@ -32,6 +32,10 @@ constexpr int kManyUnits = 256, kManyPages = 64;
 // 8192, 528 blocks: 106 and 102).  Fewer blocks if all parts of their pages are long: 512 over 65536 tokens (4 parts of 256 pages) 169 and 192, 128 over 131072 (16 of
 // 128) 109 and 118, but 256 over 8192 (8 of 16) 40 and 32.
 constexpr long long kFull = 512, kLongPart = 128;
+// Short lists of many blocks: a wave to a block, without a list in LDS and without a join, if there are this many blocks for each of a block's entries (64 at most).  us, a wave
+// and a workgroup to a block, 16 heads on 8, rows that choose 4 pages (32 entries): 512 rows, 512 blocks, 14.5 and 12, 1024 rows 15 and 18, 2048 rows 19 and 29; 8 pages
+// (64 entries): 1024 rows 38 and 30, 2048 rows 49 and 51; 256 streams, 32 heads on 8, 8 pages 30 and 37, 32 pages 102 and 99.
+constexpr long long kSoloBlocks = 32;
 constexpr int kListRows = 16;  // rows that share a list of chosen pages
 // Probabilities are taken against a reference logit per row, which moves when the sum over what a lane has of a page passes this:
 // probabilities above 1 are as exact as below.
@@ -263,10 +267,10 @@ __device__ __forceinline__ int list_window(const PagesArgs& a, const Block& b, i
 
 // The waves' results, each [COLS][64] of `pitch` pieces, 16-byte pieces of row r in the order of their number xor r, put together: a block's, or this part of them.
 template <int COLS, int WAVES>
-__device__ __forceinline__ void leave(const PagesArgs& a, const Block& b, const f32x4* acc, int pitch, const float* refs, const float* sums) {
+__device__ __forceinline__ void leave(const PagesArgs& a, const Block& b, int thread, const f32x4* acc, int pitch, const float* refs, const float* sums) {
   // All rows at once, a thread some channels of one: 4 threads further on the next 4 if it has more than 4, so that 8 side by side read different banks.
   constexpr int kRowThreads = 64 * WAVES / COLS, kChannels = kD / kRowThreads, kWide = std::min(kChannels, 4);
-  const int r = threadIdx.x / kRowThreads, first = threadIdx.x % kRowThreads;
+  const int r = thread / kRowThreads, first = thread % kRowThreads;
   const Row to = row_of(a, b, r);
   if (!to.real) return;
   const int64_t row = b.h.row0 + to.query;
@@ -310,10 +314,10 @@ __device__ __forceinline__ void leave(const PagesArgs& a, const Block& b, const 
 
 struct Empty {};
 
-// 16 rows of a key head at a time: single tokens, and chosen pages, where each row has its own and a page is worked on for all 16 once any has chosen it.  Those
+// 16 rows of a key head at a time, by a workgroup or (SOLO) by each of its waves: single tokens, and chosen pages, where each row has its own and a page is worked on for all 16 once any has chosen it.  Those
 // are bounded by the vector unit, too (66 % of the cycles, and the matrix instructions that hold it up): a page is 64 conversions and 16 logits a lane whether one row
 // has it or all.  1374 queries of 16 heads that choose 32 of 1024 pages, 23 of them the same: 114 us.
-template <bool CHOSEN, int WAVES>
+template <bool CHOSEN, int WAVES, bool SOLO>
 __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kernel(PagesArgs a, int blocks) {
   constexpr int COLS = 16;
   using S = Shape<COLS>;
@@ -324,11 +328,11 @@ __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kerne
   };
   __shared__ __align__(16) Share shares[WAVES];
   __shared__ float refs[WAVES][COLS], sums[WAVES][COLS];
-  __shared__ std::conditional_t<CHOSEN, Lists, Empty> lists;
+  __shared__ std::conditional_t<CHOSEN && !SOLO, Lists, Empty> lists;
   const int lane = threadIdx.x % 64, col = lane % COLS, quarter = lane / COLS;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   Block b;
-  if (!block_of<COLS, CHOSEN>(a, blockIdx.x, blocks, &b)) return;
+  if (!block_of<COLS, CHOSEN>(a, SOLO ? wave * gridDim.x + blockIdx.x : blockIdx.x, blocks, &b)) return;
   const Row own = row_of(a, b, col);
   const int32_t* table = a.table + (int64_t)b.s * a.width;
 
@@ -342,6 +346,14 @@ __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kerne
   float ref = -kInf, sum = 0.0f;
   const float c2 = a.scale * kLog2e;
 
+  auto look_up = [&](Next& n, bool some) {
+    n.page = some ? table[n.ordinal] : -1;
+    some = n.page >= 0 && n.page < a.pages;
+    const int64_t unit = some ? (int64_t)n.page * a.kv_heads + b.kv : 0;
+    n.ks = some ? a.k_scale[unit] : 0.0f;
+    n.vs = some ? a.v_scale[unit] : 0.0f;
+    n.mask = __ballot(some);
+  };
   // Of the pages (or entries of the list) `from`, `from` + WAVES, .. below `end`.
   // Lists from their end: the pages that all rows have listed, the last ones for the most part, then come before those of single rows, and a row's first
   // page is more work.
@@ -351,17 +363,12 @@ __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kerne
     bool some = at < end;
     n.ordinal = at;
     n.rows = 0;
-    if constexpr (CHOSEN) {
+    if constexpr (CHOSEN && !SOLO) {
       const uint32_t entry = some ? lists.found[begin + end - 1 - at] : 0u;
       n.ordinal = w0 + (int)(entry & 0xffffu);
       n.rows = entry >> 16;
     }
-    n.page = some ? table[n.ordinal] : -1;
-    some = n.page >= 0 && n.page < a.pages;
-    const int64_t unit = some ? (int64_t)n.page * a.kv_heads + b.kv : 0;
-    n.ks = some ? a.k_scale[unit] : 0.0f;
-    n.vs = some ? a.v_scale[unit] : 0.0f;
-    n.mask = __ballot(some);
+    look_up(n, some);
     return n;
   };
   u32x4 kr[4], vr[4];
@@ -495,63 +502,85 @@ __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kerne
   };
   // Pages one after the other.  The inner loop has those that need nothing but the arithmetic: the accumulators stay where they are (changed on a way of
   // its own inside the loop, they were copied on the others too, in every page).
-  auto over = [&](int begin, int end, int w0) {
-    for (int from = begin + wave; from < end; from += WAVES * 64) {
-      Next n = look(from, begin, end, w0);
-      uint64_t mask = n.mask;
-      if (!mask) continue;
-      if constexpr (kStaged) wait_for_all();  // (the last page's keys, fetched again)
-      int i = __builtin_ctzll(mask), page = __builtin_amdgcn_readlane(n.page, i);
-      fetch_keys(page);
-      asm volatile("" : "+v"(n.ks), "+v"(n.vs));  // (what look() loads is there: nothing waits for it, and so for the pages, in the loop)
+  auto pass = [&](Next& n) __attribute__((always_inline)) {
+    uint64_t mask = n.mask;
+    if (!mask) return;
+    if constexpr (kStaged) wait_for_all();  // (the last page's keys, fetched again)
+    int i = __builtin_ctzll(mask), page = __builtin_amdgcn_readlane(n.page, i);
+    fetch_keys(page);
+    asm volatile("" : "+v"(n.ks), "+v"(n.vs));  // (what look() loads is there: nothing waits for it, and so for the pages, in the loop)
+    while (true) {
+      int ordinal;
+      uint32_t rows;
+      float ks, vs;
+      bool fetched = true, done = false;  // `kr` has this page's keys; the last page is behind
+      int next, next_page;
       while (true) {
-        int ordinal;
-        uint32_t rows;
-        float ks, vs;
-        bool fetched = true, done = false;  // `kr` has this page's keys; the last page is behind
-        int next, next_page;
-        while (true) {
-          ordinal = __builtin_amdgcn_readlane(n.ordinal, i);
-          rows = CHOSEN ? __builtin_amdgcn_readlane(n.rows, i) : 0u;
-          ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(n.ks), i));
-          vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(n.vs), i));
-          mask &= mask - 1;
-          next = mask ? __builtin_ctzll(mask) : i;  // (the last one's keys are fetched again)
-          next_page = __builtin_amdgcn_readlane(n.page, next);
-          fetch_values(page);
-          if ((ordinal + 1) * kPage > b.least || vs < 0.0f) break;  // some row does not see some of its tokens, or NaN
-          const bool mine = !CHOSEN || (rows >> col & 1);
-          if (__any(mine && ref == -kInf)) break;  // a row's first page
-          take_keys();
-          first_products();
-          __builtin_amdgcn_sched_barrier(0);
-          fetch_keys(next_page);
-          weigh(factor_of(c2, ks), exponent_of(vs), mine);
-          fetched = false;
-          if (__any(part > kMaxPart)) break;
-          __builtin_amdgcn_sched_barrier(0);
-          sum += part;
-          take_values();
-          second_products();
-          done = !mask;
-          if (done) break;
-          i = next;
-          page = next_page;
-          fetched = true;
-        }
+        ordinal = __builtin_amdgcn_readlane(n.ordinal, i);
+        rows = CHOSEN ? __builtin_amdgcn_readlane(n.rows, i) : 0u;
+        ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(n.ks), i));
+        vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(n.vs), i));
+        mask &= mask - 1;
+        next = mask ? __builtin_ctzll(mask) : i;  // (the last one's keys are fetched again)
+        next_page = __builtin_amdgcn_readlane(n.page, next);
+        fetch_values(page);
+        if ((ordinal + 1) * kPage > b.least || vs < 0.0f) break;  // some row does not see some of its tokens, or NaN
+        const bool mine = !CHOSEN || (rows >> col & 1);
+        if (__any(mine && ref == -kInf)) break;  // a row's first page
+        take_keys();
+        first_products();
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_keys(next_page);
+        weigh(factor_of(c2, ks), exponent_of(vs), mine);
+        fetched = false;
+        if (__any(part > kMaxPart)) break;
+        __builtin_amdgcn_sched_barrier(0);
+        sum += part;
+        take_values();
+        second_products();
+        done = !mask;
         if (done) break;
-        if (!fetched) {
-          if constexpr (kStaged) wait_for_all();  // (what is on its way there is not this page's)
-          fetch_keys(page);
-        }
-        whole(ordinal, rows, ks, vs, next_page);
-        if (!mask) break;
         i = next;
         page = next_page;
+        fetched = true;
       }
+      if (done) break;
+      if (!fetched) {
+        if constexpr (kStaged) wait_for_all();  // (what is on its way there is not this page's)
+        fetch_keys(page);
+      }
+      whole(ordinal, rows, ks, vs, next_page);
+      if (!mask) break;
+      i = next;
+      page = next_page;
     }
   };
-  if constexpr (CHOSEN) {
+  [[maybe_unused]] auto over = [&](int begin, int end, int w0) {
+    for (int from = begin + wave; from < end; from += WAVES * 64) {
+      Next n = look(from, begin, end, w0);
+      pass(n);
+    }
+  };
+  if constexpr (SOLO) {
+    // the lists of all queries, an entry a lane; of those of a page the first has them all
+    const int rep = a.heads / a.kv_heads, q = min((int)((uint32_t)lane / (uint32_t)a.count), b.queries - 1);
+    const bool some = lane < b.queries * a.count;
+    Next n;
+    n.ordinal = some ? a.chosen[((int64_t)(b.h.row0 + b.query0 + q) * a.kv_heads + b.kv) * a.count + (lane - q * a.count)] : -1;
+    n.rows = 0;
+    const int end = (tokens_seen(a, b.h, b.query0 + q) + kPage - 1) / kPage;
+    const uint32_t bits = rep >= kListRows ? 0xffffu : ((1u << rep) - 1u) << (q * rep);
+    for (uint64_t left = __ballot(n.ordinal >= 0 && n.ordinal < end); left;) {
+      const int i = __builtin_ctzll(left), page = __builtin_amdgcn_readlane(n.ordinal, i);
+      const uint64_t same = left & __ballot(n.ordinal == page);
+      uint32_t rows = 0;
+      for (uint64_t those = same; those; those &= those - 1) rows |= __builtin_amdgcn_readlane(bits, __builtin_ctzll(those));
+      n.rows = lane == i ? rows : n.rows;
+      left &= ~same;
+    }
+    look_up(n, n.rows != 0);
+    pass(n);
+  } else if constexpr (CHOSEN) {
     for (int w0 = 0; w0 < b.pages; w0 += kWindow) {
       const int total = list_window(a, b, w0, lists);
       over((int)((uint32_t)(total * b.part) / (uint32_t)b.used), (int)((uint32_t)(total * (b.part + 1)) / (uint32_t)b.used), w0);  // (2048 pages, 64 parts)
@@ -571,8 +600,13 @@ __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kerne
     refs[wave][col] = ref;
     sums[wave][col] = total;
   }
-  __syncthreads();
-  leave<COLS, WAVES>(a, b, shares[0].acc[0], sizeof(Share) / sizeof(f32x4), refs[0], sums[0]);
+  if constexpr (SOLO) {
+    __builtin_amdgcn_wave_barrier();
+    leave<COLS, 1>(a, b, lane, shares[wave].acc[0], 0, refs[wave], sums[wave]);
+  } else {
+    __syncthreads();
+    leave<COLS, WAVES>(a, b, threadIdx.x, shares[0].acc[0], sizeof(Share) / sizeof(f32x4), refs[0], sums[0]);
+  }
 }
 
 // Many rows of a sequence: kTiles times 32 of them at a time, which share a page's conversion to bf16.  A wave goes through units of 32 tokens and 32 rows; while it works on the
@@ -869,7 +903,7 @@ __global__ __launch_bounds__(64 * kWaves, kTiles == 1 ? 3 : 2) void pages_attend
     }
   }
   __syncthreads();
-  leave<kRows, kWaves>(a, b, shares.of[0].acc[0], sizeof(Share) / sizeof(f32x4), shares.refs[0], shares.sums[0]);
+  leave<kRows, kWaves>(a, b, threadIdx.x, shares.of[0].acc[0], sizeof(Share) / sizeof(f32x4), shares.refs[0], shares.sums[0]);
 }
 
 // Over a wave, in every lane: lanes of a row of 16 by DPP, rows by swaps.
@@ -930,6 +964,7 @@ __global__ __launch_bounds__(64 * kWaves) void pages_join_kernel(PagesArgs a, in
 struct Plan {
   long long blocks, units;  // of a sequence and key head; of all
   int parts, chunk, group, cols, waves;
+  bool solo;                   // a wave to a block, four blocks to a workgroup
   bool ranked;                 // `blocks` are those of all sequences, which go by what they see
 };
 constexpr long long kMostWorkgroups = (1ll << 32) / (64 * kWaves) - 1;  // threads of a launch are counted in 32 bits
@@ -948,7 +983,9 @@ Plan plan_of(const PagesArgs& a) {
     p.ranked = p.blocks > 1 && a.sequences > 1 && a.sequences <= 64;
     if (p.ranked) p.blocks = std::min(times(p.blocks, a.sequences), (((long long)a.rows + p.group - 1) / p.group + a.sequences) * per);  // of all sequences
     p.units = times(times(p.blocks, a.kv_heads), p.ranked ? 1 : a.sequences);
-    p.parts = (int)std::max<long long>(std::min<long long>(512 / std::max(p.units, 1ll), (a.count + kWaves - 1) / kWaves), 1);
+    const long long entries = (long long)p.group * a.count;
+    p.solo = entries <= 64 && p.units >= kSoloBlocks * entries;
+    p.parts = p.solo ? 1 : (int)std::max<long long>(std::min<long long>(512 / std::max(p.units, 1ll), (a.count + kWaves - 1) / kWaves), 1);
   } else {
     const long long rows = (long long)a.longest * rep;
     auto cut = [&](int cols) {
@@ -982,7 +1019,7 @@ Plan plan_of(const PagesArgs& a) {
   return p;
 }
 
-template <bool CHOSEN, int COLS, int WAVES = kWaves>
+template <bool CHOSEN, int COLS, int WAVES = kWaves, bool SOLO = false>
 hipError_t launch(PagesArgs a, const Plan& p, hipStream_t stream) {
   a.parts = p.parts;
   a.chunk = p.chunk;
@@ -990,7 +1027,7 @@ hipError_t launch(PagesArgs a, const Plan& p, hipStream_t stream) {
   a.ranked = p.ranked;
   a.part_sums = a.part + (int64_t)a.parts * a.heads * a.rows * kD;
   if constexpr (COLS >= 32) pages_attend_rows_kernel<COLS / 32><<<(int)(p.units * p.parts), 64 * WAVES, 0, stream>>>(a, (int)p.blocks);
-  else pages_attend_kernel<CHOSEN, WAVES><<<(int)(p.units * p.parts), 64 * WAVES, 0, stream>>>(a, (int)p.blocks);
+  else pages_attend_kernel<CHOSEN, WAVES, SOLO><<<SOLO ? (int)((p.units + 8 * kWaves - 1) / (8 * kWaves) * 8) : (int)(p.units * p.parts), 64 * WAVES, 0, stream>>>(a, (int)p.blocks);
   if (p.parts > 1) pages_join_kernel<COLS, CHOSEN><<<(int)p.units, 64 * kWaves, 0, stream>>>(a, (int)p.blocks);
   return hipGetLastError();
 }
@@ -1011,7 +1048,7 @@ hipError_t launch_pages_attend(const PagesArgs& a, hipStream_t stream) {
   if (a.sequences == 0 || a.longest == 0) return hipSuccess;
   const Plan p = plan_of(a);
   if (p.waves == kManyWaves) return launch<false, 16, kManyWaves>(a, p, stream);
-  if (a.chosen) return launch<true, 16>(a, p, stream);
+  if (a.chosen) return p.solo ? launch<true, 16, kWaves, true>(a, p, stream) : launch<true, 16>(a, p, stream);
   return p.cols == 16 ? launch<false, 16>(a, p, stream) : p.cols == 32 ? launch<false, 32>(a, p, stream) : launch<false, 64>(a, p, stream);
 }
 

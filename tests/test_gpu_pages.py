@@ -474,6 +474,25 @@ def test_attention_over_listed_pages(heads, kv_heads, count):
         plain.check_attend(pool, q, got, begin, table, lengths, causal, chosen=chosen, heads=None if heads <= 8 else [0, heads // 2, heads - 1])
 
 
+@pytest.mark.parametrize("causal", [0, 1, 59])
+@pytest.mark.parametrize("count", [1, 5, 8])
+def test_short_lists_of_many_blocks(count, causal):
+    """A wave to a block of queries: pages listed twice, by many, by one, none, NaN, holes, sequences of several lengths."""
+    def edit(k, v):
+        v[0, 500, 3], k[1, 700, 2] = math.nan, math.nan
+    new, lengths = [40, 0, 3, 61], [1000, 9, 2, 61]
+    pages, table, pool = _filled(lengths, 8, 91 + count, edit=edit)
+    table[0][2] = -1
+    q = (_randn(19, 16, sum(new), 64) * 1.5).to(torch.bfloat16)
+    g = torch.Generator().manual_seed(92)
+    lists = torch.randint(-1, 18, (sum(new), 8, count), generator=g, dtype=torch.int32)
+    lists[3:20] = lists[3]
+    chosen = torch.full((MANY, 8, count), 7, dtype=torch.int32)
+    chosen[:sum(new)] = lists
+    got = _attend_many(pages, q, _begin(new), table, lengths, causal=causal, chosen=chosen.to(DEV))
+    plain.check_attend(pool, q, got, _begin(new), table, lengths, causal, chosen=lists, heads=[0, 1, 2, 15])
+
+
 def test_lists_over_many_pages_and_shared_by_workgroups():
     """More pages than are listed at a time; lists of one query long enough to be shared."""
     m = 64 * 4200 + 9
