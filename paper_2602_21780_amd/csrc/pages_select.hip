@@ -98,7 +98,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
   if (n <= 0) return;
   const int32_t* table = a.table + (int64_t)s * a.width;
   const int pages = (tokens_seen(a, h, query0 + n - 1) + kPage - 1) / kPage;  // (queries ascend, and so does what they see)
-  constexpr int kTurns = WAVES == 8 ? kFewTurns : 4, kChunk = 16 * kTurns;  // pages that a wave looks up together
+  constexpr int kTurns = WAVES < 16 ? kFewTurns : 4, kChunk = 16 * kTurns;  // pages that a wave looks up together
   const int chunks = a.pages > 0 ? (pages + kChunk - 1) / kChunk : 0;
   // The heads of a query are side by side in 16 columns, if their number divides 16: the largest of their scores is what one of them writes.
   const bool side_by_side = rep <= 16 && (rep & (rep - 1)) == 0;
@@ -479,9 +479,12 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
 int pages_held(const PagesArgs& a) { return std::min(a.width, (int)(((long long)a.longest_k + kPage - 1) / kPage)); }
 
 // 16 rows and 8 waves to a workgroup where several fit a compute unit, one's choice beside the other's scores; else 32 rows and 16 waves.  us, 16 rows and 32, 1374 queries of 16
-// heads: 32 of 625 pages 42 and 45, of 896 47 and 49, of 1024 51 and 51, of 1100 (one workgroup) 84 and 67; of 256 pages with four heads to a key head 71 and 89.
-// With eight, 16 rows are two queries, a choice for two waves of eight: 700 queries, 256 pages, 37 and 28.
+// heads: 32 of 625 pages 42 and 45, of 896 47 and 49, of 1024 51 and 51, of 1100 (one workgroup) 84 and 67; of 256 pages with four heads to a key head 50 and 89.
+// With eight, 16 rows are two queries, a choice for two waves: 700 queries, 256 pages, 25 and 21.
 constexpr int kSharedPages = 960, kSharedHeads = 4;
+// 4 waves to a workgroup, and so twice as many side by side, where there are many and four fit a compute unit's LDS (their scores 32 KB each).  us, 4 waves and 8: 1374 queries of 64
+// heads on 16, 256 pages, 50 and 71; 256 streams of 8192 tokens 18.5 and 28; 8 ragged sequences, 64 on 16 heads, 70 and 117; where scores leave less room, 16 queries of 896 pages, 64 and 47.
+constexpr int kManyGroups = 1024, kFourScores = 8192;
 
 struct Plan {
   int queries, pitch;  // of a workgroup; scores of a query
@@ -536,8 +539,10 @@ bool pages_select_fits(const PagesArgs& a) {
 hipError_t launch_pages_select(const PagesArgs& a, hipStream_t stream) {
   if (a.sequences == 0 || a.longest == 0 || a.count == 0) return hipSuccess;
   const Plan p = plan_of(a);
-  if (p.columns == 16) return launch_for<8, 1>(a, p, stream);
-  return p.queries <= kFewQueries ? launch_for<8, 2>(a, p, stream) : launch_for<16, 2>(a, p, stream);
+  if (p.columns == 32 && p.queries > kFewQueries) return launch_for<16, 2>(a, p, stream);
+  const bool four = p.groups * a.kv_heads * (p.ranked ? 1 : a.sequences) > kManyGroups && p.queries * p.pitch <= kFourScores;
+  if (p.columns == 16) return four ? launch_for<4, 1>(a, p, stream) : launch_for<8, 1>(a, p, stream);
+  return four ? launch_for<4, 2>(a, p, stream) : launch_for<8, 2>(a, p, stream);
 }
 
 }  // namespace xsv

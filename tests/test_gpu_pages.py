@@ -586,6 +586,20 @@ def test_choice_among_many_pages_and_within_a_bound():
     assert all(got[r, 0].tolist() == want[r, 0] for r in range(2))
 
 
+@pytest.mark.parametrize("heads", [8, 16, 40, 64])
+def test_choice_of_many_workgroups(heads):
+    """Rows of no sequence make the launch large: 4 waves to a workgroup, 16 rows of one, two and eight heads to a key head; five go another way."""
+    new, lengths = [40, 0, 3, 61], [1000, 9, 2, 61]
+    pages, table, pool = _filled(lengths, 8, 93)
+    table[0][2] = -1
+    q = (_randn(20, heads, sum(new), 64) * 1.5).to(torch.bfloat16)
+    for causal, count in ((1, 5), (0, 12)):
+        got = xsv.pages_select(pages, _many(q), _int(_begin(new)), _table_tensor(table), _int(lengths), count, first=1, last=2, causal=causal).cpu()
+        assert bool((got[sum(new):] == -1).all())
+        want = plain.select(pool, q, _begin(new), table, lengths, count, 1, 2, causal)
+        assert all(got[r, g].tolist() == want[r, g] for r in range(sum(new)) for g in range(8))
+
+
 @pytest.mark.parametrize("heads,kv_heads,length", [(2, 2, 64 * 1000 + 5), (5, 1, 2000), (6, 1, 64 * 1100), (4, 1, 64 * 900)])
 def test_choice_for_many_queries_of_a_workgroup(heads, kv_heads, length):
     """16 and 32 rows, heads side by side and not, lists of few and of many."""
