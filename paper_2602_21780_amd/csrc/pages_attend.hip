@@ -316,7 +316,7 @@ struct Empty {};
 
 // 16 rows of a key head at a time, by a workgroup or (SOLO) by each of its waves: single tokens, and chosen pages, where each row has its own and a page is worked on for all 16 once any has chosen it.  Those
 // are bounded by the vector unit, too (66 % of the cycles, and the matrix instructions that hold it up): a page is 64 conversions and 16 logits a lane whether one row
-// has it or all.  1374 queries of 16 heads that choose 32 of 1024 pages, 23 of them the same: 114 us.
+// has it or all.  1374 queries of 16 heads that choose 32 of 1024 pages, 23 of them the same: 115 us.
 template <bool CHOSEN, int WAVES, bool SOLO>
 __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kernel(PagesArgs a, int blocks) {
   constexpr int COLS = 16;
