@@ -733,6 +733,33 @@ def test_captured_calls_replay():
             assert torch.equal(a, b)
 
 
+def test_captured_calls_of_many_blocks_replay():
+    """Prompts behind caches, in a graph whose launches are sized by bounds: rows and lengths move between replays."""
+    pages, table, _ = _filled([1500, 900, 700], 8, 98)
+    t, begin, held = _table_tensor(table), _int([0, 0, 0, 0]), _int([0, 0, 0])
+    q = _many(_randn(99, 16, 300, 64).to(torch.bfloat16))
+
+    def step():
+        form = dict(causal=1, longest_q=300, longest_k=1500)
+        chosen = xsv.pages_select(pages, q, begin, t, held, 5, **form)
+        return (chosen, *xsv.pages_attend(pages, q, begin, t, held, **form), *xsv.pages_attend(pages, q, begin, t, held, causal=1), *xsv.pages_attend(pages, q, begin, t, held, chosen=chosen, causal=1))
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = step()
+    for rows, lengths in (([100, 1, 60], [1500, 900, 60]), ([0, 300, 0], [64, 900, 3]), ([33, 32, 31], [1400, 800, 700])):
+        begin.copy_(_int(_begin(rows)))
+        held.copy_(_int(lengths))
+        want = [y.clone() for y in step()]
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert torch.equal(x[:sum(rows)] if x.dtype == torch.int32 else x[:, :sum(rows)], y[:sum(rows)] if y.dtype == torch.int32 else y[:, :sum(rows)])
+
+
 def test_calls_on_another_stream():
     lengths = [3000, 10]
     pages, table, _ = _filled(lengths, 2, 99)
