@@ -55,6 +55,9 @@ __device__ __forceinline__ int sum_upto(int x) {
 }
 __device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
 
+// Of bits, signed: __popcll is not, and a difference of it and a larger number would be a large one.
+__device__ __forceinline__ int ones(uint64_t mask) { return (int)__popcll(mask); }
+
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const f16x2 p = {(_Float16)a, (_Float16)b};
   return __builtin_bit_cast(uint32_t, p);
@@ -71,7 +74,7 @@ __device__ __forceinline__ uint32_t nth_largest(uint32_t key, int n) {
 #pragma unroll
   for (int bit = 30; bit > 30 - BITS; bit -= 2) {
     const uint32_t y1 = x | 1u << bit, y2 = x | 2u << bit, y3 = x | 3u << bit;
-    const int c1 = __popcll(__ballot(key >= y1)), c2 = __popcll(__ballot(key >= y2)), c3 = __popcll(__ballot(key >= y3));
+    const int c1 = ones(__ballot(key >= y1)), c2 = ones(__ballot(key >= y2)), c3 = ones(__ballot(key >= y3));
     x = c3 >= n ? y3 : c2 >= n ? y2 : c1 >= n ? y1 : x;
   }
   return x;
@@ -238,19 +241,22 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
     float* row = scores + query * pitch;
     int32_t* out = a.choice + ((int64_t)(h.row0 + query0 + query) * a.kv_heads + kv) * a.count;
     const uint64_t before = (1ull << lane) - 1;
+    auto put = [&](int at, int page) {  // (never behind the row's own entries)
+      if (at < a.count) out[at] = page;
+    };
     const int begin = min(a.first, np), end = max(np - a.last, begin);  // of the pages that are chosen by their scores
     int done = 0, left = a.count;
     for (int j0 = 0; j0 < begin; j0 += 64) {
       const int j = j0 + lane;
       const uint64_t some = __ballot(j < begin && row[j ^ turned] != kNone);
       if (j < begin) row[j ^ turned] = kNone;
-      if (some >> lane & 1) out[done + __popcll(some & before)] = j;
-      done += __popcll(some);
+      if (some >> lane & 1) put(done + ones(some & before), j);
+      done += ones(some);
     }
     auto last_some = [&](int j0) { return __ballot(j0 + lane < np && row[(j0 + lane) ^ turned] != kNone); };
     const uint64_t last = end < np ? last_some(end) : 0;
-    left -= done + __popcll(last);
-    for (int j0 = end + 64; j0 < np; j0 += 64) left -= __popcll(last_some(j0));
+    left -= done + ones(last);
+    for (int j0 = end + 64; j0 < np; j0 += 64) left -= ones(last_some(j0));
     if (lane == 0 && end % 2) row[end ^ turned] = kNone;  // (scores are read two at a time)
 
     // The `left` largest scores of pages [begin, end).
@@ -287,7 +293,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
             most = fmaxf(most, fmaxf(two[0], two[1]));
           }
         }
-        if (__popcll(__ballot(most != kNone)) >= left) {
+        if (ones(__ballot(most != kNone)) >= left) {
           const uint32_t bits = nth_largest<kLeastBits>(ordered(most), left);
           const float least = unordered(bits);
           lower = bits - 1;
@@ -296,7 +302,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
           if constexpr (N > 0) {
 #pragma unroll
             for (int i = N - 1; i >= 0; --i) those = 2 * those + (held_scores[i] >= least);
-            own = __popc(those);
+            own = ones(those);
           } else {
 #pragma unroll 8
             for (int i = 0; i < run; i += 2) {
@@ -339,24 +345,24 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
       }
       if (found > 0) {
         uint64_t takes = __ballot(score != kNone);
-        if (__popcll(takes) > left) {
+        if (ones(takes) > left) {
           int rank = 0;  // scores that are larger
           for (int i = 0; i < found; i += 4)  // (behind the last, none)
 #pragma unroll
             for (int k = 0; k < 4; ++k) rank += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(score), i + k)) > score;
           takes &= __ballot(rank < left);
-          const int over = __popcll(takes) - left;
+          const int over = ones(takes) - left;
           if (over > 0) {  // of equal ones that are not all chosen, those of the first pages
             int most = takes >> lane & 1 ? rank : 0;
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) most = max(most, __shfl_xor(most, d));
             uint64_t same = takes & __ballot(rank == most);
-            const bool stays = __popcll(same & before) < __popcll(same) - over;
+            const bool stays = ones(same & before) < ones(same) - over;
             takes &= ~same | __ballot(stays);
           }
         }
-        if (takes >> lane & 1) out[done + __popcll(takes & before)] = page;
-        done += __popcll(takes);
+        if (takes >> lane & 1) put(done + ones(takes & before), page);
+        done += ones(takes);
         chosen = true;
       }
     }
@@ -366,7 +372,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
           const float bound = unordered(x);
           int c = 0;
 #pragma unroll
-          for (int i = 0; i < N; ++i) c += __popcll(__ballot(held_scores[i] > bound));
+          for (int i = 0; i < N; ++i) c += ones(__ballot(held_scores[i] > bound));
           return c;
         };
         // At least `want` scores are above lo, at most `want` above hi.
@@ -395,14 +401,14 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
           same = 2 * same + (held_scores[i] == bound);
         }
         if (want > above_hi) {
-          const int own = __popc(same), rest = want - above_hi - (sum_upto(own) - own);  // that the lanes before leave
-          while (__popc(same) > max(rest, 0)) same &= ~(0x80000000u >> __builtin_clz(same));
+          const int own = ones(same), rest = want - above_hi - (sum_upto(own) - own);  // that the lanes before leave
+          while (ones(same) > max(rest, 0)) same &= ~(0x80000000u >> __builtin_clz(same));
           takes |= same;
         }
-        const int own = __popc(takes), upto = sum_upto(own);
+        const int own = ones(takes), upto = sum_upto(own);
         for (int to = done + upto - own; __any(takes != 0); ++to)
           if (takes) {
-            out[to] = run * lane + __builtin_ctz(takes);
+            put(to, run * lane + __builtin_ctz(takes));
             takes &= takes - 1;
           }
         done += __builtin_amdgcn_readlane(upto, 63);
@@ -416,7 +422,7 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
         };
         auto count_above = [&](uint32_t x) {
           int c = 0;
-          over([&](int, uint32_t k) { c += __popcll(__ballot(k > x)); });
+          over([&](int, uint32_t k) { c += ones(__ballot(k > x)); });
           return c;
         };
         // More than `left` keys are above lo, at most `left` above hi.
@@ -458,19 +464,19 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
           uint64_t takes = __ballot(k > hi);
           if (equal > 0) {
             const uint64_t ties = __ballot(k == hi);
-            const bool tie = k == hi && __popcll(ties & before) < equal;
+            const bool tie = k == hi && ones(ties & before) < equal;
             takes |= __ballot(tie);
-            equal = max(equal - __popcll(ties), 0);
+            equal = max(equal - ones(ties), 0);
           }
-          if (takes >> lane & 1) out[done + __popcll(takes & before)] = 64 * i + lane;
-          done += __popcll(takes);
+          if (takes >> lane & 1) put(done + ones(takes & before), 64 * i + lane);
+          done += ones(takes);
         });
       }
     }
     for (int j0 = end; j0 < np; j0 += 64) {
       const uint64_t some = j0 == end ? last : last_some(j0);
-      if (some >> lane & 1) out[done + __popcll(some & before)] = j0 + lane;
-      done += __popcll(some);
+      if (some >> lane & 1) put(done + ones(some & before), j0 + lane);
+      done += ones(some);
     }
     for (int j = done + lane; j < a.count; j += 64) out[j] = -1;
   }
