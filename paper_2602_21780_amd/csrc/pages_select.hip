@@ -296,7 +296,8 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
         if (ones(__ballot(most != kNone)) >= left) {
           const uint32_t bits = nth_largest<kLeastBits>(ordered(most), left);
           const float least = unordered(bits);
-          lower = bits - 1;
+          // (in front of 0 by its bits is -0, which is not less: the number below 0 here, as scores are 0 or at least 2^-100 in size)
+          lower = bits == ordered(0.0f) ? ordered(-1.17549435e-38f) : bits - 1;
           uint32_t those = 0;
           int own = 0;
           if constexpr (N > 0) {

@@ -1,10 +1,13 @@
 """The paged cache in 8 bits at its limits (plain_pages is the definition in 64 bits)."""
+import math
+import random
+
 import pytest
 import torch
 
 import plain_pages as plain
 from paper_2602_21780_amd import xsv
-from test_gpu_pages import DEV, _filled, _int, _randn, _table_tensor
+from test_gpu_pages import DEV, _check_select, _filled, _int, _randn, _table_tensor
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +40,36 @@ def test_equal_scores_of_more_pages_than_registers_hold(pages_in_all, heads):
         got = _guarded_select(pages, q.to(DEV), [0, 4], table, [64 * pages_in_all], count, first=first, last=last)
         want = plain.select(pool, q, [0, 4], table, [64 * pages_in_all], count, first, last, 0)
         assert all(got[r, 0].tolist() == want[r, 0] for r in range(4)), (count, first, last)
+
+
+def _signed_pages(n, heads, seed):
+    """A pool whose page j has keys c_j in channel 0 and zeros elsewhere: a few c_j above zero, some below, most of them 0."""
+    rng = random.Random(seed)
+    c = [rng.choice([0.5, 1.0, 1.5]) if x < 0.05 else -1.0 if x < 0.25 else 0.0 for x in (rng.random() for _ in range(n))]
+
+    def edit(k, v):
+        k[:] = 0.0
+        k[..., 0] = torch.tensor(c).repeat_interleave(64)
+    return _filled([64 * n], heads, seed, edit=edit)
+
+
+@pytest.mark.parametrize("pages_in_all,heads", [(60, 1), (100, 1), (100, 5), (300, 2), (700, 1), (1500, 2), (2500, 1)])
+def test_scores_of_zero_are_scores(pages_in_all, heads):
+    """Zero queries, queries that are not finite, zero keys: many equal scores, 0 among numbers above and below, at every size of the choice."""
+    print(f"pages_select scores of 0, pages={pages_in_all} heads={heads}", flush=True)
+    pages, table, pool = _signed_pages(pages_in_all, 1, 200 + pages_in_all)
+    q = torch.zeros((heads, 5, 64))
+    q[:, 1] = math.nan
+    q[:, 2, 0], q[:, 3, 0] = 3.0, -3.0        # fewer scores above 0 than are wanted; then more
+    q[:, 4] = _randn(201, heads, 64)
+    q = q.to(torch.bfloat16).to(DEV)
+    for count, first, last in ((20, 0, 0), (32, 1, 1), (70, 2, 3), (pages_in_all - 1, 0, 0)):
+        _check_select(pages, pool, q, [0, 5], table, [64 * pages_in_all], count, first, last, 0)
+
+
+def test_pages_that_were_never_written_are_chosen_in_order():
+    pages = xsv.Pages.empty(200, 2, DEV)
+    table = [list(range(199, -1, -1))]
+    q = _randn(202, 4, 3, 64).to(torch.bfloat16).to(DEV)
+    got = xsv.pages_select(pages, q, _int([0, 3]), _int(table), _int([64 * 200]), 90, first=0, last=1)
+    assert bool((got.cpu() == torch.tensor(list(range(89)) + [199])).all())
