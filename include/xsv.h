@@ -353,7 +353,8 @@ int xsv_pages_attend_workspace(const xsv_pages* pages, const xsv_pages_query* cf
  *   score_j = max over the key head's heads of 2^clamp(t + e_j - 1, -100, 100) sum_c max(q'_c hi_c, q'_c lo_c),
  *   q' = q / 2^t rounded to whole numbers (ties to even; 0 where q is not finite),  t = floor(log2 max(|q|, 2^-119)) - 7,  hi, lo and e the keys' bounds and scale
  * of page j: an upper bound of the largest logit (unscaled) but for the rounding of q, in whole numbers that fp32 holds exactly, so that the choice does not
- * depend on the order of sums.  chosen: DEVICE [rows][kv_heads][count], ascending, -1 behind the last.  At most 32768 pages (longest_k <= 2^21). */
+ * depend on the order of sums.  A score that is not a number, of bounds that no call wrote, counts as the lowest.  chosen: DEVICE [rows][kv_heads][count], ascending,
+ * -1 behind the last.  At most 32768 pages (longest_k <= 2^21). */
 int xsv_pages_select(void* hip_stream, const xsv_pages* pages, const xsv_pages_query* cfg, xsv_tensor q, int32_t* chosen);
 
 const char* xsv_strerror(int code);

@@ -31,6 +31,7 @@ constexpr int kMostScores = 32768;   // of a workgroup: 128 KB, and 32 for the w
 constexpr int kHole = -(1 << 20);  // the exponent of a page that is none
 
 constexpr float kNone = -kInf;  // the score of a page that is none
+constexpr float kLowest = -3.402823466e38f;
 // Larger numbers, larger keys, and back.  (A sum that begins with +0 is never -0.)
 __device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t b = __float_as_uint(x);
@@ -198,7 +199,8 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
         f32x4 key;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float k = __builtin_amdgcn_ldexpf(sum[c][j], min(max(t[c] + e[j], -100), 100));
+          // (of bounds that are no numbers, the lowest score: NaN would be larger than no other and smaller than none)
+          const float k = fmaxf(__builtin_amdgcn_ldexpf(sum[c][j], min(max(t[c] + e[j], -100), 100)), kLowest);
           key[j] = e[j] == kHole ? kNone : k;
         }
         float* to = scores + query[c] * pitch + ((kChunk * chunk + 16 * turn + 4 * u) ^ score_turn(query[c]));

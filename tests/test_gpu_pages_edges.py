@@ -73,3 +73,38 @@ def test_pages_that_were_never_written_are_chosen_in_order():
     q = _randn(202, 4, 3, 64).to(torch.bfloat16).to(DEV)
     got = xsv.pages_select(pages, q, _int([0, 3]), _int(table), _int([64 * 200]), 90, first=0, last=1)
     assert bool((got.cpu() == torch.tensor(list(range(89)) + [199])).all())
+
+
+@pytest.mark.parametrize("heads", [1, 2, 5])
+@pytest.mark.parametrize("pages_in_all", [50, 100, 300, 700, 1500, 2500])
+def test_scores_that_are_no_numbers_count_as_the_lowest(pages_in_all, heads):
+    """Bounds that are NaN, in more pages than are wanted and than a wave has lanes: nothing behind a row's entries is written, and pages with numbers come first."""
+    print(f"pages_select NaN bounds, pages={pages_in_all} heads={heads}", flush=True)
+    pages, table, _ = _filled([64 * pages_in_all], 1, 210)
+    rng = random.Random(pages_in_all)
+    bad = rng.sample(range(pages_in_all), pages_in_all * 2 // 5)
+    pages.k_bounds[[table[0][j] for j in bad], 0, rng.randrange(2)] = math.nan
+    pool = plain.of(pages)        # (its ranking leaves NaN at the lowest)
+    q = _randn(211, heads, 4, 64).to(torch.bfloat16).to(DEV)
+    q[:, 3] = 0.0
+    for count, first, last in ((4, 0, 0), (9, 2, 3), (pages_in_all * 4 // 5, 0, 0), (pages_in_all, 1, 0)):
+        got = _guarded_select(pages, q, [0, 4], table, [64 * pages_in_all], count, first=first, last=last)
+        want = plain.select(pool, q, [0, 4], table, [64 * pages_in_all], count, first, last, 0)
+        assert all(got[r, 0].tolist() == want[r, 0] for r in range(4)), (count, first, last)
+
+
+@pytest.mark.parametrize("heads", [1, 2, 5])
+def test_bounds_of_any_bits(heads):
+    """What a pool of memory as it came may hold: lists stay lists, and the same ones every time."""
+    for n in (50, 400, 2500):
+        pages, table, _ = _filled([64 * n], 2, 212)
+        g = torch.Generator().manual_seed(n)
+        pages.k_bounds.copy_(torch.randint(-32768, 32768, pages.k_bounds.shape, generator=g, dtype=torch.int16).view(torch.float16))
+        pages.k_scale.copy_(torch.randint(-2**31, 2**31 - 1, pages.k_scale.shape, generator=g, dtype=torch.int32).view(torch.float32))
+        q = _randn(213, 2 * heads, 6, 64).to(torch.bfloat16).to(DEV)
+        for count in (4, 70):
+            got = _guarded_select(pages, q, [0, 6], table, [64 * n], count, first=1, last=1)
+            some = min(count, n)
+            assert bool((got[..., 0] == 0).all()) and bool((got[..., some - 1] == n - 1).all()) and bool((got[..., some:] == -1).all())
+            assert bool((got[..., 1:some] > got[..., :some - 1]).all())
+            assert torch.equal(got, _guarded_select(pages, q, [0, 6], table, [64 * n], count, first=1, last=1))
