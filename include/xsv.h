@@ -302,8 +302,9 @@ int xsv_seq_attend_grad_workspace(const xsv_seq_config* cfg, int64_t* bytes);
  *   Of a page and key head, keys and values each:  scale = 2^e, the smallest e in -100 .. 120 with 448 2^e >= max |x| over the finite elements;
  *   code = x / scale to the nearest e4m3 number (ties to even), NaN where x is not finite;  a code stands for code * scale.
  * All calls take the lengths that the sequences have with the call's own rows: row i of the n rows [begin[s], begin[s + 1]) of sequence s
- * stands at token i + lengths[s] - n of it (a row in front of its first token is not written, not read, and sees nothing).  What begin and lengths hold is
- * cut off at the tensors' rows and the table's width: nothing outside them is touched.  Rows of no sequence are not written. */
+ * stands at token i + lengths[s] - n of it (a row in front of its first token is not written, not read, and sees nothing).  Tokens behind the table's
+ * width are seen by nobody, not written and not read; the others keep their places.  What begin holds is cut off at the tensors' rows: nothing outside
+ * tensors and table is touched.  Rows of no sequence are not written. */
 typedef struct {
   int32_t pages;            /* of the pool, >= 0                                               */
   int32_t kv_heads;         /* 1 .. 65536                                                      */

@@ -20,16 +20,16 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 struct Held {
   int row0, n;  // rows of the call, within the bound
-  int m;        // tokens, within theirs
-  int ahead;    // the place of row 0 among them: rows stand at the end of their sequence, whatever the bounds leave out
+  int m;        // tokens, within theirs and the table
+  int ahead;    // the place of row 0 among them: rows stand at the end of their sequence, whatever the bounds and the table leave out
 };
 // Offsets and lengths are device data: whatever they hold, no row outside the tensors and no entry outside the table is touched.
 __device__ __forceinline__ Held held(const PagesArgs& a, int s) {
   Held h;
   h.row0 = min(max(a.begin[s], 0), a.rows);
   const int n = min(max(a.begin[s + 1], h.row0), a.rows) - h.row0;
-  const int m = min(max(a.lengths[s], 0), a.width * kPage);
-  h.m = min(m, a.longest_k);
+  const int m = max(a.lengths[s], 0);
+  h.m = min(min(m, a.width * kPage), a.longest_k);
   h.ahead = m - n;
   h.n = min(n, a.longest);
   return h;

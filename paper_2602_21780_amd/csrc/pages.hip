@@ -32,9 +32,9 @@ struct Touched {
 __device__ __forceinline__ Touched touched(const PagesArgs& a, int s, int i) {
   Touched t;
   t.h = held(a, s);
-  const int start = max(t.h.ahead, 0), end = t.h.ahead + t.h.n;  // (rows in front of the first token have no place)
+  const int start = max(t.h.ahead, 0), end = min(t.h.ahead + t.h.n, a.width * kPage);  // (rows in front of the first token or behind the table have no place)
   t.ordinal = start / kPage + i;
-  const int p0 = min(t.ordinal, a.width) * kPage;  // (behind the table: no place; tokens are at most 2^30)
+  const int p0 = min(t.ordinal, a.width) * kPage;  // (of a page behind the table: the end, where no row is; it holds at most 2^30 tokens)
   t.from = max(start - p0, 0);
   t.to = min(end - p0, kPage);
   t.any = end > start && t.from < t.to;

@@ -7,7 +7,7 @@ import torch
 
 import plain_pages as plain
 from paper_2602_21780_amd import xsv
-from test_gpu_pages import DEV, _check_select, _filled, _int, _randn, _table_tensor
+from test_gpu_pages import DEV, _attend_many, _check_select, _filled, _int, _randn, _table_tensor
 
 pytestmark = pytest.mark.gpu
 
@@ -108,3 +108,54 @@ def test_bounds_of_any_bits(heads):
             assert bool((got[..., 0] == 0).all()) and bool((got[..., some - 1] == n - 1).all()) and bool((got[..., some:] == -1).all())
             assert bool((got[..., 1:some] > got[..., :some - 1]).all())
             assert torch.equal(got, _guarded_select(pages, q, [0, 6], table, [64 * n], count, first=1, last=1))
+
+
+# ---- lengths behind the table ---------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("length", [129, 133, 138, 200, 1 << 20, (1 << 31) - 1])
+def test_rows_behind_the_table_are_left_out(length):
+    """They are not written over what is held, not read from there, and the others keep their places."""
+    print(f"pages behind the table: length={length}", flush=True)
+    pages, table, pool = _filled([128], 2, 220)
+    k, v = (_randn(221 + i, 2, 10, 64).to(torch.bfloat16) for i in range(2))
+    xsv.pages_write(pages, k.to(DEV), v.to(DEV), _int([0, 10]), _int(table), _int([length]))
+    inside = max(128 - (length - 10), 0)           # rows in front of the table's end
+    if inside:
+        pool.write(k[:, :inside], v[:, :inside], [0, inside], table, [128])
+    got = plain.of(pages)
+    for name in ("k", "v", "ke", "ve", "bounds"):
+        for p in table[0]:
+            assert torch.equal(getattr(got, name)[p], getattr(pool, name)[p]), (name, p)
+    out = [torch.full((2, 10, 64), 9.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    xsv.pages_read(pages, _int([0, 10]), _int(table), _int([length]), out=out)
+    for h in range(2):
+        for want, x in zip(pool.tokens(table[0], 128, h), out):
+            full = torch.full((10, 64), 9.0, dtype=torch.float64)
+            full[:inside] = want[128 - inside:]
+            assert torch.equal(x[h].cpu().double(), full)
+
+
+@pytest.mark.parametrize("causal", [0, 1, 59])
+@pytest.mark.parametrize("rows", [10, 70])
+def test_rows_keep_their_positions_where_a_length_is_behind_the_table(rows, causal):
+    held, length = 64 * 20, 64 * 20 + 25
+    pages, table, pool = _filled([held], 2, 222)
+    q = (_randn(223, 4, rows, 64) * 1.5).to(torch.bfloat16)
+    where = (_int([0, rows]), _int(table), _int([length]))
+    sees = [min(plain.limit(i, rows, length, causal), held) for i in range(rows)]
+    lists = torch.randint(0, 20, (rows, 2, 5), generator=torch.Generator().manual_seed(7), dtype=torch.int32)
+    whole = xsv.pages_attend(pages, q.to(DEV), *where, causal=causal)
+    some = xsv.pages_attend(pages, q.to(DEV), *where, causal=causal, chosen=lists.to(DEV))
+    choice = xsv.pages_select(pages, q.to(DEV), *where, 6, first=1, last=2, causal=causal).cpu()
+    for i in range(rows):
+        one = slice(i, i + 1)
+        plain.check_attend(pool, q[:, one], [x[:, one] for x in whole], [0, 1], table, [sees[i]], 0)
+        plain.check_attend(pool, q[:, one], [x[:, one] for x in some], [0, 1], table, [sees[i]], 0, chosen=lists[one])
+        want = plain.select(pool, q[:, one], [0, 1], table, [sees[i]], 6, 1, 2, 0)
+        assert [choice[i, g].tolist() for g in range(2)] == [want[0, g] for g in range(2)]
+    pages, table, pool = _filled([held], 8, 224)
+    q = q.repeat(4, 1, 1)
+    many = _attend_many(pages, q, [0, rows], table, [length], causal=causal)
+    for i in (0, rows - 26, rows - 25, rows - 1) if rows > 26 else (0, rows - 1):
+        one = slice(i, i + 1)
+        plain.check_attend(pool, q[:, one], [x[:, one] for x in many], [0, 1], table, [sees[i]], 0, heads=[0, 15])
