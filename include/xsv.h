@@ -300,7 +300,8 @@ int xsv_seq_attend_grad_workspace(const xsv_seq_config* cfg, int64_t* bytes);
  * the table is the page of its tokens [64 j, 64 j + 64).  An entry that is no page of the pool (-1) holds nothing: its tokens are seen by
  * nobody, are not written and not read.
  *   Of a page and key head, keys and values each:  scale = 2^e, the smallest e in -100 .. 120 with 448 2^e >= max |x| over the finite elements;
- *   code = x / scale to the nearest e4m3 number (ties to even), NaN where x is not finite;  a code stands for code * scale.
+ *   code = x / scale to the nearest e4m3 number (ties to even; +-240 instead of +-256 at e = 120, whose product bf16 does not hold), NaN where x is not
+ *   finite;  a code stands for code * scale.
  * All calls take the lengths that the sequences have with the call's own rows: row i of the n rows [begin[s], begin[s + 1]) of sequence s
  * stands at token i + lengths[s] - n of it (a row in front of its first token is not written, not read, and sees nothing).  Tokens behind the table's
  * width are seen by nobody, not written and not read; the others keep their places.  What begin holds is cut off at the tensors' rows: nothing outside

@@ -1,7 +1,7 @@
 // A paged cache in 8 bits: rows written into it and read back.
 //
 //   scale = 2^e, the smallest e in -100 .. 120 with 448 2^e >= max |x| over the finite elements of a page's keys (values) of one head,
-//   code = e4m3(x / scale), to nearest even; what is not finite becomes NaN
+//   code = e4m3(x / scale), to nearest even, at most 240 in size where e = 120 (256 2^120 is infinite); what is not finite becomes NaN
 //
 // e4m3 keeps four significant bits at any size down to 2^-15 of the largest, so a few channels of large keys do not cost the others
 // their bits, as they would with whole numbers under one scale.  With powers of two the division is exact, and so is a later change of the
@@ -63,7 +63,9 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t w, float f) {
   return codes4(a[0] * f, a[1] * f, b[0] * f, b[1] * f);
 }
 __device__ __forceinline__ bool has_nan(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; }  // 0x7f and 0xff are NaN
-__device__ __forceinline__ float finite_or_nan(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? __builtin_nanf("") : x; }
+__device__ __forceinline__ float number_or_nan(float x, float y) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? __builtin_nanf("") : y; }  // y where x is finite
+// The largest code under a scale: with 2^120 one that stands for a number that fp32 and bf16 hold.
+__device__ __forceinline__ float top_of(int e) { return e == 120 ? 240.0f : 448.0f; }
 
 // the bytes of a dword that stand for places `at` .. at + 3 and lie in [from, to)
 __device__ __forceinline__ uint32_t within(int at, int from, int to) {
@@ -91,14 +93,15 @@ struct Row16 {  // 16 channels of a token
     }
     return (uint32_t)max(m[0], m[1]) << 16;
   }
-  __device__ __forceinline__ u32x4 codes(float f, bool finite) const {
+  // `ordinary`: all finite, and no code above `top`
+  __device__ __forceinline__ u32x4 codes(float f, bool ordinary, float top) const {
     u32x4 c;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t a = r[i / 2][i % 2 * 2], b = r[i / 2][i % 2 * 2 + 1];
       float x[4] = {bf16_low(a), bf16_high(a), bf16_low(b), bf16_high(b)};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = (finite ? x[j] : finite_or_nan(x[j])) * f;
+      for (int j = 0; j < 4; ++j) x[j] = ordinary ? x[j] * f : number_or_nan(x[j], fminf(fmaxf(x[j] * f, -top), top));
       c[i] = codes4(x[0], x[1], x[2], x[3]);
     }
     return c;
@@ -132,7 +135,7 @@ __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int 
     if (is_old) old_k = *reinterpret_cast<const u32x4*>(to_k);
     old_v = *reinterpret_cast<const u32x4*>(to_v);
   }
-  // (rows that are not all finite are rare, and take the way of their own)
+  // (rows that are not all finite, or among the largest, are rare and take a way of their own)
   uint32_t mk = k.largest(true), mv = v.largest(true);
   const bool finite = !__any(max(mk, mv) >= 0x7f800000u);
   if (!finite) {
@@ -159,12 +162,12 @@ __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int 
   const float fk = power(-e[0]), fv = power(-e[1]);
   u32x4 ck, cv;
   bool nan = false;
-  if (finite) {
-    ck = k.codes(fk, true);
-    cv = v.codes(fv, true);
+  if (finite && max(e[0], e[1]) < 120) {
+    ck = k.codes(fk, true, 0.0f);
+    cv = v.codes(fv, true, 0.0f);
   } else {
-    ck = k.codes(fk, false);
-    cv = v.codes(fv, false);
+    ck = k.codes(fk, false, top_of(e[0]));
+    cv = v.codes(fv, false, top_of(e[1]));
     nan = __any(has_nan(cv[0]) || has_nan(cv[1]) || has_nan(cv[2]) || has_nan(cv[3]));
   }
   if (tid % 64 == 0) none[tid / 64] = nan;

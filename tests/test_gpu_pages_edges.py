@@ -159,3 +159,51 @@ def test_rows_keep_their_positions_where_a_length_is_behind_the_table(rows, caus
     for i in (0, rows - 26, rows - 25, rows - 1) if rows > 26 else (0, rows - 1):
         one = slice(i, i + 1)
         plain.check_attend(pool, q[:, one], [x[:, one] for x in many], [0, 1], table, [sees[i]], 0, heads=[0, 15])
+
+
+# ---- the largest numbers --------------------------------------------------------------------------------------------
+
+def test_the_largest_finite_numbers_stay_finite():
+    """Above 248 2^120 the nearest code would stand for 2^128, which bf16 does not hold: 240 2^120 is the largest that a page stands for."""
+    bits = [0x7f7f, 0x7f7e, 0x7f78, 0x7f77, 0x7f70, 0x7f6f, 0x7f00]      # the largest; 248 2^120 and the one below; 240 2^120 and the one below; 2^127
+    x = torch.tensor(bits, dtype=torch.int32)
+    x = torch.cat([x, x | 0x8000, torch.tensor([0x3f80, 0x7f80, 0x7fc0], dtype=torch.int32)])
+    k = torch.zeros((1, 70, 64))
+    k[0, 3, :17] = (x << 16).view(torch.float32)
+    k[0, 66, 5], k[0, 69, 6] = k[0, 3, 0], -k[0, 3, 0]
+    k, v = k.to(torch.bfloat16), (-k).to(torch.bfloat16)
+    pages, pool = xsv.Pages.empty(2, 1, DEV), plain.Pool(2, 1)
+    for begin, held in ((0, 65), (65, 70)):      # the second page in two calls, the second of which raises its scale
+        a, b = (y[:, begin:held].contiguous() for y in (k, v))
+        xsv.pages_write(pages, a.to(DEV), b.to(DEV), _int([0, held - begin]), _int([[1, 0]]), _int([held]))
+        pool.write(a, b, [0, held - begin], [[1, 0]], [held])
+    top = torch.where(pool.ke == 120, 240.0, 448.0)[:, :, None, None]
+    assert bool((pool.ke == 120).all()) and bool((pool.ve == 120).all())
+    assert int((pool.k == 256.0).sum()) == 4 and int((pool.k == -256.0).sum()) == 4      # what the definition without the limit gives
+    pool.k, pool.v, pool.bounds = (torch.maximum(torch.minimum(y, t), -t) for y, t in ((pool.k, top), (pool.v, top), (pool.bounds, 2 * top)))
+    got = plain.of(pages)
+    for name in ("k", "v", "ke", "ve", "bounds"):
+        assert torch.equal(torch.nan_to_num(getattr(got, name), 1e9), torch.nan_to_num(getattr(pool, name), 1e9)), name
+    rk, rv = xsv.pages_read(pages, _int([0, 70]), _int([[1, 0]]), _int([70]), rows=70)
+    for x, r in zip(pool.tokens([1, 0], 70, 0), (rk, rv)):
+        assert torch.equal(torch.nan_to_num(r[0].cpu().double(), 1e9), torch.nan_to_num(x, 1e9))
+    for x, r in ((k, rk), (v, rv)):
+        assert torch.equal(torch.isfinite(r.cpu()), torch.isfinite(x))
+
+
+def test_attention_over_the_largest_finite_numbers():
+    """One token, so that no sum passes what fp32 holds; small queries, so that no logit does."""
+    top = torch.tensor([0x7f7f0000], dtype=torch.int32).view(torch.float32)
+    k = torch.zeros((1, 1, 64))
+    k[0, 0, 0], k[0, 0, 1] = top, -top
+    k = k.to(torch.bfloat16).to(DEV)
+    pages = xsv.Pages.empty(1, 1, DEV)
+    xsv.pages_write(pages, k, -k, _int([0, 1]), _int([[0]]), _int([1]))
+    for heads, rows in ((1, 1), (1, 40), (40, 1)):       # (rows in front of the only token see nothing)
+        q = torch.zeros((heads, rows, 64))
+        q[..., 0] = 2.0 ** -126
+        out, lse = xsv.pages_attend(pages, q.to(torch.bfloat16).to(DEV), _int([0, rows]), _int([[0]]), _int([1]))
+        assert not out[:, :-1].any() and bool((lse[:, :-1] == -math.inf).all())
+        out, lse = out[:, -1], lse[:, -1]
+        assert bool((out[:, 0] == -240.0 * 2.0 ** 120).all()) and bool((out[:, 1] == 240.0 * 2.0 ** 120).all()) and not out[:, 2:].any()
+        assert bool(((lse.cpu().double() - 240.0 * 2.0 ** -6 / 8).abs() <= 1e-6).all())      # 0.47: a few roundings of 2^-24
