@@ -119,16 +119,22 @@ struct Shape<32> {
   }
 };
 
-// 8 codes as bf16
-__device__ __forceinline__ bf16x8 view8(uint32_t a, uint32_t b) {
-  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
-  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
+// 8 codes as bf16, times a power of two
+__device__ __forceinline__ bf16x8 view8(uint32_t a, uint32_t b, float times = 1.0f) {
+  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, times, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, times, true);
+  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, times, false), s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, times, true);
   const u32x4 w = {__builtin_bit_cast(uint32_t, p), __builtin_bit_cast(uint32_t, q), __builtin_bit_cast(uint32_t, r), __builtin_bit_cast(uint32_t, s)};
   return __builtin_bit_cast(bf16x8, w);
 }
 
 // (A page that was never written may have any scale: 0 would leave nothing of its probabilities.)
 __device__ __forceinline__ int exponent_of(float scale) { return min(max((int)((__float_as_uint(scale) >> 23) & 0xffu) - 127, -100), 120); }
+// The values' scale 2^ev goes into a weight's exponent, and comes out of the sum again.  With less than this in it, weights of 2^(-126 - ev) of the reference
+// would be lost from the sum although their logits are ordinary, as in pages whose values are all zeros (2^-100): such pages have this in the weights and
+// the rest in the values.  What is lost then is below 2^-66 of the largest weight.
+constexpr int kLeastExponent = -60;
+constexpr float kLeastScale = 0x1p-60f;
+__device__ __forceinline__ float rest_of(int ev) { return __int_as_float((127 + min(ev - kLeastExponent, 0)) << 23); }
 // What logits of a page are multiplied by, never 0: masked ones are -inf.
 __device__ __forceinline__ float factor_of(float c2, float scale) { return fmaxf(c2 * scale, 1.17549435e-38f); }
 // The NaN codes of a dword, as bytes 0xff.
@@ -420,7 +426,7 @@ __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kerne
       for (int k = 0; k < 2; ++k) x[i] = S::mfma(view8(kr[i][2 * k], kr[i][2 * k + 1]), qf[k], x[i]);
     }
   };
-  // The values' scale 2^ev goes into the exponent: what enters the second product is in the values' own units.
+  // The values' scale 2^ev, of tiny ones a part of it, goes into the exponent: what enters the second product is in the values' own units.
   auto weigh = [&](float cs, int ev, bool mine) {
     const float off = off_of(ref) - (float)ev;
     float one = 0.0f, other = 0.0f;
@@ -438,12 +444,12 @@ __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kerne
       for (int i = 0; i < 8; ++i) pr[i / 4][i % 4] = mine ? pr[i / 4][i % 4] : 0u;
     }
   };
-  auto second_products = [&] {
+  auto second_products = [&](float rest) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int k = 0; k < 2; ++k)
-        o[i] = S::mfma(view8(vr[i][2 * k], vr[i][2 * k + 1]), __builtin_bit_cast(bf16x8, pr[k]), o[i]);
+        o[i] = S::mfma(view8(vr[i][2 * k], vr[i][2 * k + 1], rest), __builtin_bit_cast(bf16x8, pr[k]), o[i]);
   };
   // A page with all that may happen: rows that do not see some of it, references that move, values that are NaN.
   auto whole = [&](int ordinal, uint32_t rows, float ks, float vs, int next_page) {
@@ -468,7 +474,8 @@ __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kerne
     sum *= f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] *= f;
-    weigh(cs, exponent_of(vs), mine);
+    const int ev = exponent_of(vs);
+    weigh(cs, max(ev, kLeastExponent), mine);
     sum += part;
     if (vs < 0.0f) {
       // 0 times NaN is NaN: values that are NaN are taken out of the product, and reach the rows that see their tokens by one of their own
@@ -498,7 +505,7 @@ __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kerne
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[i][j] = count[i][j] > 0.0f ? __builtin_nanf("") : o[i][j];
     }
-    second_products();
+    second_products(rest_of(ev));
   };
   // Pages one after the other.  The inner loop has those that need nothing but the arithmetic: the accumulators stay where they are (changed on a way of
   // its own inside the loop, they were copied on the others too, in every page).
@@ -524,7 +531,7 @@ __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kerne
         next = mask ? __builtin_ctzll(mask) : i;  // (the last one's keys are fetched again)
         next_page = __builtin_amdgcn_readlane(n.page, next);
         fetch_values(page);
-        if ((ordinal + 1) * kPage > b.least || vs < 0.0f) break;  // some row does not see some of its tokens, or NaN
+        if ((ordinal + 1) * kPage > b.least || vs < kLeastScale) break;  // some row does not see some of its tokens, or values that are NaN or tiny
         const bool mine = !CHOSEN || (rows >> col & 1);
         if (__any(mine && ref == -kInf)) break;  // a row's first page
         take_keys();
@@ -537,7 +544,7 @@ __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kerne
         __builtin_amdgcn_sched_barrier(0);
         sum += part;
         take_values();
-        second_products();
+        second_products(1.0f);
         done = !mask;
         if (done) break;
         i = next;
@@ -678,9 +685,9 @@ __global__ __launch_bounds__(64 * kWaves, kTiles == 1 ? 3 : 2) void pages_attend
 #pragma unroll
     for (int i = 0; i < 4; ++i) kb[i] = view8(kr[i / 2][i % 2 * 2], kr[i / 2][i % 2 * 2 + 1]);
   };
-  auto take_values = [&] {
+  auto take_values = [&](float rest) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) vb[i] = view8(vr[i / 2][i % 2 * 2], vr[i / 2][i % 2 * 2 + 1]);
+    for (int i = 0; i < 4; ++i) vb[i] = view8(vr[i / 2][i % 2 * 2], vr[i / 2][i % 2 * 2 + 1], rest);
   };
   auto logits = [&](int t) {
     f32x16 x = {};
@@ -708,7 +715,7 @@ __global__ __launch_bounds__(64 * kWaves, kTiles == 1 ? 3 : 2) void pages_attend
   // The page at hand with all that may happen, but for its first `skip` units.
   auto whole = [&](int ordinal, int skip, float ks, float vs, [[maybe_unused]] int next_page) __attribute__((always_inline)) {
     const float cs = factor_of(c2, ks);
-    const int ev = exponent_of(vs);
+    const int ev = max(exponent_of(vs), kLeastExponent);
     const float un = __int_as_float((127 - ev) << 23);
     if constexpr (kTiles == 1) wait_for_all();
     else wait_for_all_but_eight();
@@ -732,7 +739,7 @@ __global__ __launch_bounds__(64 * kWaves, kTiles == 1 ? 3 : 2) void pages_attend
           nb[i] = view8(nan[0] & 0x38383838u, nan[1] & 0x38383838u);  // ones
         }
       }
-      take_values();
+      take_values(rest_of(exponent_of(vs)));
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
         if (h * kTiles + t < skip) continue;
@@ -794,7 +801,7 @@ __global__ __launch_bounds__(64 * kWaves, kTiles == 1 ? 3 : 2) void pages_attend
       next_page = __builtin_amdgcn_readlane(lane_page, next);
       if constexpr (kTiles == 2) fetch(next_page, at_hand ^ 1);
     };
-    auto plain = [&] { return (ordinal + 1) * kPage <= b.least && vs >= 0.0f; };
+    auto plain = [&] { return (ordinal + 1) * kPage <= b.least && vs >= kLeastScale; };
     look_at();
     while (true) {
       bool begun = true;
@@ -841,7 +848,7 @@ __global__ __launch_bounds__(64 * kWaves, kTiles == 1 ? 3 : 2) void pages_attend
             }
             if (kTiles == 1 || u % 2 == 1) take_keys();
             x_next = logits((t + 1) % kTiles);
-            if (kTiles == 1 || u % 2 == 1) take_values();
+            if (kTiles == 1 || u % 2 == 1) take_values(1.0f);
             add_values((t + 1) % kTiles, before);
             if (kTiles == 1 && u == 1) {
               read_values(0, 1);
@@ -871,7 +878,7 @@ __global__ __launch_bounds__(64 * kWaves, kTiles == 1 ? 3 : 2) void pages_attend
           if (!plain()) break;
         }
         if (done) {
-          if (kTiles == 1) take_values();
+          if (kTiles == 1) take_values(1.0f);
           add_values(kTiles - 1, pb);
         }
         if (last) break;

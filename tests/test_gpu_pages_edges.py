@@ -7,7 +7,7 @@ import torch
 
 import plain_pages as plain
 from paper_2602_21780_amd import xsv
-from test_gpu_pages import DEV, _attend_many, _check_select, _filled, _int, _randn, _table_tensor
+from test_gpu_pages import DEV, MANY, _attend_many, _check_select, _filled, _int, _randn, _table_tensor
 
 pytestmark = pytest.mark.gpu
 
@@ -207,3 +207,92 @@ def test_attention_over_the_largest_finite_numbers():
         out, lse = out[:, -1], lse[:, -1]
         assert bool((out[:, 0] == -240.0 * 2.0 ** 120).all()) and bool((out[:, 1] == 240.0 * 2.0 ** 120).all()) and not out[:, 2:].any()
         assert bool(((lse.cpu().double() - 240.0 * 2.0 ** -6 / 8).abs() <= 1e-6).all())      # 0.47: a few roundings of 2^-24
+
+
+# ---- scales of nothing ----------------------------------------------------------------------------------------------
+
+# of a key of channel 0 and a query of it, under a scale of 1/8
+LOGITS = {20.0: (20.0, 8.0), 18.703125: (18.0, 8.3125)}
+
+
+def _one_large(logit, q_rows, heads, kv_heads, page_count):
+    """One key with a large logit among page_count pages with logits of 0 whose values are zeros but for its own page's."""
+    def edit(k, v):
+        k[:] = 0.0
+        k[:, 70, 0] = LOGITS[logit][0]
+        v[:, :64], v[:, 128:] = 0.0, 0.0
+    pages, table, pool = _filled([64 * page_count], kv_heads, 230, edit=edit)
+    q = torch.zeros((heads, q_rows, 64))
+    q[..., 0] = LOGITS[logit][1]
+    return pages, table, pool, q.to(torch.bfloat16)
+
+
+def _check_one_large(logit, pool, table, got, n):
+    heads = got[0].shape[0]
+    rep = heads // pool.k.shape[1]
+    total = math.exp(logit) + n - 1
+    # lse: six roundings of 2^-24 of numbers of at most 20 (of the factor two, the product, the difference from the reference, and two at the end), 7.2e-6;
+    # and a wave adds up its pages, at least every fourth, in two halves at most, each time rounding a sum that is near 1 by up to 2^-24
+    bound = 7.2e-6 + n / 64 / 4 * 2 * 2.0 ** -24
+    for h in (0, heads - 1):
+        _, v, _ = pool.tokens(table[0], 192, h // rep)
+        want = (v.sum(0) + (math.exp(logit) - 1.0) * v[70]) / total
+        off = (got[1][h].cpu().double() - math.log(total)).abs()
+        assert bool((off <= bound).all()), (float(off.max()), bound)
+        assert bool(((got[0][h].cpu().double() - want).abs() <= 2.0 ** -8 * 2.1 * want.abs() + 1e-6).all())
+
+
+@pytest.mark.parametrize("logit", list(LOGITS))
+@pytest.mark.parametrize("rows", [1, 3, 40])
+def test_tokens_without_values_count_in_the_sum(rows, logit):
+    """131071 logits of 0 beside one of 20 (19): 3e-4 (1e-3) of the sum, though each weight is below 2^-26 of the largest and its value is 0."""
+    pages, table, pool, q = _one_large(logit, rows, 2, 2, 2048)
+    got = xsv.pages_attend(pages, q.to(DEV), _int([0, rows]), _int(table), _int([64 * 2048]))
+    _check_one_large(logit, pool, table, got, 64 * 2048)
+    lists = torch.arange(2047, -1, -1, dtype=torch.int32, device=DEV).expand(rows, 2, 2048).contiguous()
+    got = xsv.pages_attend(pages, q.to(DEV), _int([0, rows]), _int(table), _int([64 * 2048]), chosen=lists)
+    _check_one_large(logit, pool, table, got, 64 * 2048)
+
+
+@pytest.mark.parametrize("logit", list(LOGITS))
+@pytest.mark.parametrize("form", ["32 rows", "64 rows", "chosen"])
+def test_tokens_without_values_count_in_the_sum_of_many_blocks(form, logit):
+    """Launches of so many blocks that the wave that has the large logit has many of the other pages, too."""
+    if form == "32 rows":
+        pages, table, pool, q = _one_large(logit, 1374, 8, 8, 2048)
+        got = xsv.pages_attend(pages, q.to(DEV), _int([0, 1374]), _int(table), _int([64 * 2048]))
+        _check_one_large(logit, pool, table, got, 64 * 2048)
+        return
+    pages, table, pool, q = _one_large(logit, 70, 16, 8, 1024)
+    lists = torch.arange(1024, dtype=torch.int32, device=DEV).expand(MANY, 8, 1024).contiguous()
+    got = _attend_many(pages, q, [0, 70], table, [64 * 1024], chosen=lists if form == "chosen" else None)
+    _check_one_large(logit, pool, table, got, 64 * 1024)
+
+
+@pytest.mark.parametrize("rows", [1, 40, 300])
+def test_pages_of_tiny_values(rows):
+    """Values of 2^-50 to 2^-90, a page each, some of them NaN, beside zeros: results in their size, and rows that see a NaN."""
+    def edit(k, v):
+        for i in range(12):
+            v[:, 64 * i:64 * i + 64] *= 2.0 ** (-50 - 10 * (i % 5)) if i % 6 else 0.0
+        v[0, 64 * 7 + 3, 5] = math.nan
+    pages, table, pool = _filled([64 * 12], 8, 231, edit=edit)
+    q = (_randn(232, 16, rows, 64) * 1.5).to(torch.bfloat16)
+    for causal in (0, 1):
+        got = xsv.pages_attend(pages, q.to(DEV), _int([0, rows]), _int(table), _int([64 * 12]), causal=causal)
+        plain.check_attend(pool, q, got, [0, rows], table, [64 * 12], causal, heads=[0, 1, 15])
+    got = _attend_many(pages, q, [0, rows], table, [64 * 12], causal=1)
+    plain.check_attend(pool, q, got, [0, rows], table, [64 * 12], 1, heads=[0, 1, 15])
+    for j in range(12):      # one page alone: of its own size
+        lists = torch.full((rows, 8, 1), j, dtype=torch.int32)
+        got = xsv.pages_attend(pages, q.to(DEV), _int([0, rows]), _int(table), _int([64 * 12]), chosen=lists.to(DEV))
+        for h in (0, 15):
+            k, v, _ = pool.tokens(table[0], 64 * 12, h // 2)
+            P = torch.softmax(q[h].double() @ k[64 * j:64 * j + 64].T * 0.125, 1)
+            V = v[64 * j:64 * j + 64]
+            want, weight = P @ V, P @ V.abs()
+            o = got[0][h].cpu().double()
+            assert torch.equal(torch.isnan(o), torch.isnan(want))
+            fine = ~torch.isnan(want)
+            # weights and results are rounded to 2^-8; logits below 2^-17 of what they add up from
+            assert bool(((o - want).abs()[fine] <= 2.0 ** -8 * 1.1 * (want.abs() + weight)[fine]).all()), (j, h)
