@@ -79,10 +79,10 @@ struct PagesArgs {
   float* part;                   // attention cut over workgroups: what each leaves, [part][head][row][64]
   float* part_sums;              // and its reference and sum, [part][head][row][2]
   int parts, chunk, group;       // how many share a block of rows, pages for each; queries that share a list of pages (set by the launchers)
-  int ranked;                    // blocks are numbered over all sequences, those that see the most first
+  int ranked;                    // blocks are numbered over all sequences
 };
-hipError_t launch_pages_write(const PagesArgs& a, hipStream_t stream);
-hipError_t launch_pages_read(const PagesArgs& a, hipStream_t stream);
+hipError_t launch_pages_write(PagesArgs a, hipStream_t stream);
+hipError_t launch_pages_read(PagesArgs a, hipStream_t stream);
 hipError_t launch_pages_attend(const PagesArgs& a, hipStream_t stream);
 hipError_t launch_pages_select(const PagesArgs& a, hipStream_t stream);
 int64_t pages_attend_workspace(const PagesArgs& a);  // bytes of PagesArgs::part

@@ -43,8 +43,9 @@ __device__ __forceinline__ int tokens_seen(const PagesArgs& a, const Held& h, in
   return (int)min((int64_t)h.m, ((int64_t)(at / a.causal) + 1) * a.causal);
 }
 
-// Block number `*block` of all sequences' blocks (at most 64 sequences), `blocks_of(h)` of each, those of the sequences that see the most pages first: it becomes its number within its
-// sequence.  A lane looks a sequence up.
+// Blocks of rows numbered over all sequences: launches are sized by the rows and the sequences, not by the longest sequence that there may be times the
+// sequences.  Block number `*block` becomes its number within its sequence.
+// Up to 64 sequences: `blocks_of(h)` of each, those of the sequences that see the most pages first.  A lane looks a sequence up.
 template <typename F>
 __device__ __forceinline__ bool ranked_block(const PagesArgs& a, F blocks_of, int* block, int* sequence, Held* h) {
   const int lane = threadIdx.x % 64;
@@ -67,6 +68,31 @@ __device__ __forceinline__ bool ranked_block(const PagesArgs& a, F blocks_of, in
   *h = Held{__builtin_amdgcn_readlane(own.row0, s), __builtin_amdgcn_readlane(own.n, s), __builtin_amdgcn_readlane(own.m, s), __builtin_amdgcn_readlane(own.ahead, s)};
   return true;
 }
+
+// More sequences, in their order: those in front of row r have at most `whole(r)` blocks, and `extra` more each; at that number the blocks of the sequence
+// that begins with r begin, so that it is found by 64 offsets at a time.  (Numbers between one sequence's last block and the next one's first are nobody's.)
+template <typename W>
+__device__ __forceinline__ bool numbered_block(const PagesArgs& a, W whole, int extra, int* block, int* sequence, Held* h) {
+  const int lane = threadIdx.x % 64;
+  int s = 0;
+  for (int n = a.sequences; n > 1;) {
+    const int step = (n + 63) / 64, at = s + min(lane * step, n - 1);
+    const int64_t number = (int64_t)whole(min(max(a.begin[at], 0), a.rows)) + (int64_t)at * extra;
+    const int i = 63 - __builtin_clzll(__ballot(lane * step < n && number <= *block) | 1ull);
+    s += i * step;
+    n = min(step, n - i * step);
+  }
+  *sequence = s;
+  *h = held(a, s);
+  const int64_t number = *block - ((int64_t)whole(h->row0) + (int64_t)s * extra);
+  *block = (int)number;
+  return number >= 0;
+}
+constexpr int kRanked = 64;
+// More than kRanked sequences: is the launch of all blocks by number, `numbered`, taken, or that of as many for each sequence as the longest may have, `each`?
+// Empty workgroups cost less than the search; both sides, us, each and numbered, 500 sequences of a row and one of L, 16 heads: written, L = 100
+// (each 1.5 times numbered) 38 and 45, L = 300 (2.9) 67 and 45; choice of 4 pages, L = 300 142 and 42, L = 1000 388 and 51; attention 186 and 149, 313 and 155.
+inline bool by_number(long long each, long long numbered) { return numbered <= each / 2; }
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const bf16x2 p = {(__bf16)a, (__bf16)b};

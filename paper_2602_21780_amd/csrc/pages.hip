@@ -29,9 +29,15 @@ struct Touched {
   int first;
   bool any;
 };
-__device__ __forceinline__ Touched touched(const PagesArgs& a, int s, int i) {
+__device__ __forceinline__ Touched touched(const PagesArgs& a, int number, int most) {
   Touched t;
-  t.h = held(a, s);
+  int s = number / most, i = number % most;
+  if (a.ranked) {
+    i = number;
+    if (!numbered_block(a, [](int row) { return row / kPage; }, 2, &i, &s, &t.h)) i = 1 << 30;  // (n rows are in at most n / 64 + 2 pages)
+  } else {
+    t.h = held(a, s);
+  }
   const int start = max(t.h.ahead, 0), end = min(t.h.ahead + t.h.n, a.width * kPage);  // (rows in front of the first token or behind the table have no place)
   t.ordinal = start / kPage + i;
   const int p0 = min(t.ordinal, a.width) * kPage;  // (of a page behind the table: the end, where no row is; it holds at most 2^30 tokens)
@@ -113,8 +119,8 @@ __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int 
   __shared__ uint32_t top[2][kThreads / 64];
   __shared__ int none[kThreads / 64];  // a wave's values are not all numbers
   const int tid = threadIdx.x, number = blockIdx.x;
-  const int head = number % a.kv_heads, i = number / a.kv_heads % most, s = number / a.kv_heads / most;
-  const Touched t = touched(a, s, i);
+  const int head = number % a.kv_heads;
+  const Touched t = touched(a, number / a.kv_heads, most);
   if (!t.any) return;
   const size_t unit = (size_t)t.page * a.kv_heads + head;
   const int token = tid / 4, ch0 = tid % 4 * 16;    // the row side, and keys in the page
@@ -232,8 +238,8 @@ __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int 
 __global__ __launch_bounds__(kThreads) void pages_read_kernel(PagesArgs a, int most) {
   __shared__ __align__(16) uint8_t lines[kD][kLine];
   const int tid = threadIdx.x, number = blockIdx.x;
-  const int head = number % a.kv_heads, i = number / a.kv_heads % most, s = number / a.kv_heads / most;
-  const Touched t = touched(a, s, i);
+  const int head = number % a.kv_heads;
+  const Touched t = touched(a, number / a.kv_heads, most);
   if (!t.any) return;
   const size_t unit = (size_t)t.page * a.kv_heads + head;
   const u32x4 ck = *reinterpret_cast<const u32x4*>(a.k + unit * kPageBytes + tid * 16);
@@ -266,25 +272,37 @@ __global__ __launch_bounds__(kThreads) void pages_read_kernel(PagesArgs a, int m
   }
 }
 
-int most_pages(const PagesArgs& a) { return (int)(((long long)a.longest + kPage - 2) / kPage + 1); }
+struct Plan {
+  int most;          // pages that a sequence's rows can be in
+  long long blocks;  // of a head: pages of all sequences
+  bool ranked;       // numbered over them
+};
+Plan plan_of(const PagesArgs& a) {
+  Plan p;
+  p.most = (int)(((long long)a.longest + kPage - 2) / kPage + 1);
+  const long long each = (long long)p.most * a.sequences, all = a.rows / kPage + 2ll * a.sequences;
+  p.ranked = a.sequences > 1 && by_number(each, all);
+  p.blocks = p.ranked ? all : each;
+  return p;
+}
 
 }  // namespace
 
-bool pages_move_fits(const PagesArgs& a) {
-  return (long long)most_pages(a) * a.kv_heads <= (1ll << 24) && (long long)most_pages(a) * a.kv_heads * a.sequences <= (1ll << 32) / kThreads - 1;
-}
+bool pages_move_fits(const PagesArgs& a) { return plan_of(a).blocks <= ((1ll << 32) / kThreads - 1) / a.kv_heads; }
 
-hipError_t launch_pages_write(const PagesArgs& a, hipStream_t stream) {
+hipError_t launch_pages_write(PagesArgs a, hipStream_t stream) {
   if (a.sequences == 0 || a.longest == 0 || a.pages == 0) return hipSuccess;
-  const int most = most_pages(a);
-  pages_write_kernel<<<a.sequences * a.kv_heads * most, kThreads, 0, stream>>>(a, most);
+  const Plan p = plan_of(a);
+  a.ranked = p.ranked;
+  pages_write_kernel<<<(int)(p.blocks * a.kv_heads), kThreads, 0, stream>>>(a, p.most);
   return hipGetLastError();
 }
 
-hipError_t launch_pages_read(const PagesArgs& a, hipStream_t stream) {
+hipError_t launch_pages_read(PagesArgs a, hipStream_t stream) {
   if (a.sequences == 0 || a.longest == 0 || a.pages == 0) return hipSuccess;
-  const int most = most_pages(a);
-  pages_read_kernel<<<a.sequences * a.kv_heads * most, kThreads, 0, stream>>>(a, most);
+  const Plan p = plan_of(a);
+  a.ranked = p.ranked;
+  pages_read_kernel<<<(int)(p.blocks * a.kv_heads), kThreads, 0, stream>>>(a, p.most);
   return hipGetLastError();
 }
 

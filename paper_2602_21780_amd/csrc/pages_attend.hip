@@ -196,7 +196,8 @@ __device__ __forceinline__ bool block_of(const PagesArgs& a, int number, int blo
     b->kv = number % 8 * heads + unit / sequences / blocks;
   }
   if (a.ranked) {
-    if (!ranked_block(a, blocks_of, &back, &b->s, &b->h)) return false;
+    auto whole = [&](int row) { return CHOSEN ? (int64_t)(row / a.group) * per : (int64_t)row * rep / COLS; };
+    if (!(a.sequences <= kRanked ? ranked_block(a, blocks_of, &back, &b->s, &b->h) : numbered_block(a, whole, per, &back, &b->s, &b->h))) return false;
   } else {
     b->h = held(a, b->s);
   }
@@ -972,10 +973,16 @@ struct Plan {
   long long blocks, units;  // of a sequence and key head; of all
   int parts, chunk, group, cols, waves;
   bool solo;                   // a wave to a block, four blocks to a workgroup
-  bool ranked;                 // `blocks` are those of all sequences, which go by what they see
+  bool ranked;                 // `blocks` are those of all sequences
 };
 constexpr long long kMostWorkgroups = (1ll << 32) / (64 * kWaves) - 1;  // threads of a launch are counted in 32 bits
 long long times(long long a, long long b) { return b != 0 && a > kMostWorkgroups / b ? kMostWorkgroups + 1 : a * b; }  // as far as it matters
+// Are blocks numbered over all sequences, `all` at most?  Then they are the plan's.
+void number(Plan& p, const PagesArgs& a, long long all) {
+  const long long each = times(p.blocks, a.sequences);
+  p.ranked = p.blocks > 1 && a.sequences > 1 && (a.sequences <= kRanked || by_number(each, all));
+  if (p.ranked) p.blocks = a.sequences <= kRanked ? std::min(each, all) : all;
+}
 Plan plan_of(const PagesArgs& a) {
   Plan p{};
   const int rep = a.heads / a.kv_heads;
@@ -987,8 +994,7 @@ Plan plan_of(const PagesArgs& a) {
     if (rep <= kListRows) p.group = std::min(kListRows / rep, std::max(a.longest, 1));
     const int per = (rep + kListRows - 1) / kListRows;
     p.blocks = ((long long)a.longest + p.group - 1) / p.group * per;
-    p.ranked = p.blocks > 1 && a.sequences > 1 && a.sequences <= 64;
-    if (p.ranked) p.blocks = std::min(times(p.blocks, a.sequences), (((long long)a.rows + p.group - 1) / p.group + a.sequences) * per);  // of all sequences
+    number(p, a, (((long long)a.rows + p.group - 1) / p.group + a.sequences) * per);
     p.units = times(times(p.blocks, a.kv_heads), p.ranked ? 1 : a.sequences);
     const long long entries = (long long)p.group * a.count;
     p.solo = entries <= 64 && p.units >= kSoloBlocks * entries;
@@ -998,8 +1004,7 @@ Plan plan_of(const PagesArgs& a) {
     auto cut = [&](int cols) {
       p.cols = cols;
       p.blocks = (rows + cols - 1) / cols;
-      p.ranked = p.blocks > 1 && a.sequences > 1 && a.sequences <= 64;
-      if (p.ranked) p.blocks = std::min(times(p.blocks, a.sequences), ((long long)a.rows * rep + cols - 1) / cols + a.sequences);  // of all sequences
+      number(p, a, ((long long)a.rows * rep + cols - 1) / cols + a.sequences);
       p.units = times(times(p.blocks, a.kv_heads), p.ranked ? 1 : a.sequences);
     };
     long long workgroups = 1024;

@@ -91,7 +91,9 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
   int group = blockIdx.x / a.kv_heads, s;
   Held h;
   if (a.ranked) {
-    if (!ranked_block(a, [&](const Held& h) { return (int)(((int64_t)h.n + queries - 1) / queries); }, &group, &s, &h)) return;
+    auto blocks_of = [&](const Held& h) { return (int)(((int64_t)h.n + queries - 1) / queries); };
+    auto whole = [&](int row) { return row / queries; };
+    if (!(a.sequences <= kRanked ? ranked_block(a, blocks_of, &group, &s, &h) : numbered_block(a, whole, 1, &group, &s, &h))) return;
   } else {
     const int groups = (int)(((int64_t)a.longest + queries - 1) / queries);
     s = group / groups;
@@ -497,9 +499,9 @@ constexpr int kManyGroups = 1024, kFourScores = 8192;
 
 struct Plan {
   int queries, pitch;  // of a workgroup; scores of a query
-  int columns;
-  long long groups;    // of queries of a sequence, or of all
-  bool ranked;
+  int columns, waves;
+  long long groups;    // of queries of all sequences
+  bool ranked;         // numbered over them
 };
 Plan plan_of(const PagesArgs& a) {
   Plan p;
@@ -508,9 +510,12 @@ Plan plan_of(const PagesArgs& a) {
   p.columns = p.pitch <= kSharedPages && rep <= kSharedHeads ? 16 : 32;
   p.queries = std::max(std::min({p.columns / rep, a.longest, kMostScores / p.pitch}), 1);
   if (p.queries <= kFewQueries && p.queries * rep <= 16) p.columns = 16;
-  p.groups = ((long long)a.longest + p.queries - 1) / p.queries;
-  p.ranked = p.groups > 1 && a.sequences > 1 && a.sequences <= 64;
-  if (p.ranked) p.groups = std::min(p.groups * a.sequences, ((long long)a.rows + p.queries - 1) / p.queries + a.sequences);
+  const long long of_one = ((long long)a.longest + p.queries - 1) / p.queries, each = of_one * a.sequences;
+  const long long all = ((long long)a.rows + p.queries - 1) / p.queries + a.sequences;
+  p.ranked = of_one > 1 && a.sequences > 1 && (a.sequences <= kRanked || by_number(each, all));
+  p.groups = !p.ranked ? each : a.sequences <= kRanked ? std::min(each, all) : all;
+  const bool four = p.groups > kManyGroups / a.kv_heads && p.queries * p.pitch <= kFourScores;
+  p.waves = p.columns == 32 && p.queries > kFewQueries ? 16 : four ? 4 : 8;
   return p;
 }
 
@@ -522,7 +527,7 @@ hipError_t launch(PagesArgs a, const Plan& p, hipStream_t stream) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_select_kernel<WAVES, N, SETS>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  pages_select_kernel<WAVES, N, SETS><<<(int)(p.groups * a.kv_heads * (p.ranked ? 1 : a.sequences)), 64 * WAVES, bytes, stream>>>(a, p.queries, p.pitch);
+  pages_select_kernel<WAVES, N, SETS><<<(int)(p.groups * a.kv_heads), 64 * WAVES, bytes, stream>>>(a, p.queries, p.pitch);
   return hipGetLastError();
 }
 
@@ -541,17 +546,15 @@ hipError_t launch_for(const PagesArgs& a, const Plan& p, hipStream_t stream) {
 bool pages_select_fits(const PagesArgs& a) {
   if (pages_held(a) > kMostPages) return false;
   const Plan p = plan_of(a);
-  const long long most = (1ll << 32) / 1024 - 1;  // (threads of a launch are counted in 32 bits)
-  return p.groups * a.kv_heads <= most && p.groups * a.kv_heads * (p.ranked ? 1 : a.sequences) <= most;
+  return p.groups <= ((1ll << 32) / (64 * p.waves) - 1) / a.kv_heads;  // (threads of a launch are counted in 32 bits)
 }
 
 hipError_t launch_pages_select(const PagesArgs& a, hipStream_t stream) {
   if (a.sequences == 0 || a.longest == 0 || a.count == 0) return hipSuccess;
   const Plan p = plan_of(a);
-  if (p.columns == 32 && p.queries > kFewQueries) return launch_for<16, 2>(a, p, stream);
-  const bool four = p.groups * a.kv_heads * (p.ranked ? 1 : a.sequences) > kManyGroups && p.queries * p.pitch <= kFourScores;
-  if (p.columns == 16) return four ? launch_for<4, 1>(a, p, stream) : launch_for<8, 1>(a, p, stream);
-  return four ? launch_for<4, 2>(a, p, stream) : launch_for<8, 2>(a, p, stream);
+  if (p.waves == 16) return launch_for<16, 2>(a, p, stream);
+  if (p.columns == 16) return p.waves == 4 ? launch_for<4, 1>(a, p, stream) : launch_for<8, 1>(a, p, stream);
+  return p.waves == 4 ? launch_for<4, 2>(a, p, stream) : launch_for<8, 2>(a, p, stream);
 }
 
 }  // namespace xsv

@@ -7,7 +7,7 @@ import torch
 
 import plain_pages as plain
 from paper_2602_21780_amd import xsv
-from test_gpu_pages import DEV, MANY, _attend_many, _check_select, _filled, _int, _randn, _table_tensor
+from test_gpu_pages import DEV, MANY, _attend_many, _begin, _check_select, _filled, _int, _randn, _table, _table_tensor
 
 pytestmark = pytest.mark.gpu
 
@@ -296,3 +296,102 @@ def test_pages_of_tiny_values(rows):
             fine = ~torch.isnan(want)
             # weights and results are rounded to 2^-8; logits below 2^-17 of what they add up from
             assert bool(((o - want).abs()[fine] <= 2.0 ** -8 * 1.1 * (want.abs() + weight)[fine]).all()), (j, h)
+
+
+# ---- many sequences -------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("sequences,rows", [(65, 100000), (200, 40000), (4200, 5000)])
+def test_choice_for_any_number_of_sequences_within_a_bound_far_above_their_rows(sequences, rows):
+    """The launch is sized by the rows and the sequences, not by their product."""
+    lengths = [130 + s % 64 for s in range(sequences)]
+    pages, table, pool = _filled(lengths, 16, 240)
+    q = torch.zeros((16, rows, 64), dtype=torch.bfloat16, device=DEV)
+    q[:, :sequences] = _randn(241, 16, sequences, 64).to(torch.bfloat16).to(DEV)
+    call = lambda **kw: xsv.pages_select(pages, q, _int(_begin([1] * sequences)), _table_tensor(table), _int(lengths), 2, causal=1, **kw)
+    assert torch.equal(call(), call(longest_q=1))
+
+
+@pytest.mark.parametrize("sequences,rows", [(1000, 100000), (5000, 20000)])
+def test_writes_of_any_number_of_sequences_within_a_bound_far_above_their_rows(sequences, rows):
+    lengths = [1 + s % 130 for s in range(sequences)]
+    k, v = (torch.zeros((16, rows, 64), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    k[:, :sequences], v[:, :sequences] = (_randn(242 + i, 16, sequences, 64).to(torch.bfloat16).to(DEV) for i in range(2))
+    total = sum(-(-m // 64) for m in lengths)
+    where = (_int(_begin([1] * sequences)), _table_tensor(_table(lengths, total, 7)), _int(lengths))
+    pools, read = [xsv.Pages.empty(total, 16, DEV) for _ in range(2)], []
+    for pages, longest in zip(pools, (None, 1)):
+        xsv.pages_write(pages, k, v, *where, longest=longest)
+        read.append(xsv.pages_read(pages, *where, rows=rows, longest=longest))
+        assert bool(read[-1][0][:, :sequences].any(2).all())
+    for name in ("k", "v", "k_scale", "v_scale", "k_bounds"):
+        a, b = (getattr(p, name) for p in pools)
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), name
+    assert torch.equal(read[0][0], read[1][0]) and torch.equal(read[0][1], read[1][1])
+
+
+def _uneven(sequences, seed, rows):
+    """Rows and lengths of many sequences, some of no rows, some of no tokens, one far longer than the others."""
+    rng = random.Random(seed)
+    new = [rng.choice([0, 1, 1, 2, 5, 37]) for _ in range(sequences)]
+    new[sequences // 3] = rows
+    lengths = [max(n + rng.choice([-2, 0, 0, 5, 100]), 0) for n in new]
+    return new, lengths
+
+
+@pytest.mark.parametrize("sequences", [65, 200, 4200])
+def test_rows_of_many_uneven_sequences(sequences):
+    """Written, read, attended to and chosen for within no bound: blocks are found by number among 64 offsets at a time, twice and more."""
+    print(f"pages of many sequences {sequences}", flush=True)
+    new, lengths = _uneven(sequences, sequences, 700)
+    begin = _begin(new, 3)
+    total, rows = sum(-(-m // 64) for m in lengths) + 2, sum(new) + 5
+    table = _table(lengths, total, 9)
+    where = (_int(begin), _table_tensor(table), _int(lengths))
+    pages, pool = xsv.Pages.empty(total, 2, DEV), plain.Pool(total, 2)
+    k, v = (_randn(250 + i, 2, rows, 64).to(torch.bfloat16) for i in range(2))
+    xsv.pages_write(pages, k.to(DEV), v.to(DEV), *where)
+    pool.write(k, v, begin, table, lengths)
+    got = plain.of(pages)
+    for name in ("k", "v", "bounds"):
+        assert torch.equal(getattr(got, name)[pool.written], getattr(pool, name)[pool.written]), name
+    assert not got.k[~pool.written].any()
+    pool = got
+    for x, y in zip(xsv.pages_read(pages, *where, rows=rows), xsv.pages_read(pages, *where, rows=rows, longest=max(new))):
+        assert torch.equal(x, y)
+    q = _randn(252, 4, rows, 64).to(torch.bfloat16).to(DEV)
+    lists = torch.randint(-1, 12, (rows, 2, 3), generator=torch.Generator().manual_seed(8), dtype=torch.int32)
+    some = range(sequences) if sequences < 1000 else sorted({0, 1, sequences // 3, sequences - 1, *random.Random(1).sample(range(sequences), 400)})
+    parts = ([begin[s] for s in some], [begin[s + 1] for s in some])
+
+    def each(check):
+        for s, a, b in zip(some, *parts):
+            if s == sequences // 3 and sequences > 65:
+                b = a + 40                  # (the long one's first rows: its length goes by the cut)
+            check([a, b], [table[s]], [lengths[s] - (begin[s + 1] - b)], s)
+    whole, chosen = xsv.pages_attend(pages, q, *where, causal=1), xsv.pages_attend(pages, q, *where, causal=1, chosen=lists.to(DEV))
+    choice = xsv.pages_select(pages, q, *where, 3, first=0, last=1, causal=1)
+    each(lambda be, t, m, s: plain.check_attend(pool, q, whole, be, t, m, 1, heads=[0, 3]))
+    each(lambda be, t, m, s: plain.check_attend(pool, q, chosen, be, t, m, 1, chosen=lists, heads=[3]))
+    for x in (*whole, *chosen):
+        assert not x[:, :3].any() and not x[:, begin[-1]:].any()
+    assert torch.equal(choice, xsv.pages_select(pages, q, *where, 3, first=0, last=1, causal=1, longest_q=max(new)))
+
+    def check(be, t, m, s):
+        for (r, g), want in plain.select(pool, q, be, t, m, 3, 0, 1, 1).items():
+            assert choice[r, g].tolist() == want, (s, r, g)
+    choice = choice.cpu()
+    each(check)
+
+
+def test_offsets_that_do_not_ascend_are_within_bounds():
+    """Offsets that begin again: what is written is written within the tensors, and the first and last sequences' rows are answered."""
+    sequences = 300
+    lengths = [70] * sequences
+    pages, table, pool = _filled(lengths, 1, 253)
+    begin = [min(s * 10, 1500) if s < 150 else max(1500 - 10 * (s - 150), -50) for s in range(sequences + 1)]
+    q = _randn(254, 2, 1500, 64).to(torch.bfloat16).to(DEV)
+    out = torch.zeros((2, 1564, 64), dtype=torch.bfloat16, device=DEV)
+    room = out[:, :1500]
+    got = xsv.pages_attend(pages, q, _int(begin), _table_tensor(table), _int(lengths), out=room, causal=1)
+    assert not out[:, 1500:].any() and bool(torch.isfinite(got[0]).all())
+    plain.check_attend(pool, q, got, begin[:2], table[:1], lengths[:1], 1)

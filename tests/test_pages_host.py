@@ -115,3 +115,14 @@ def test_bindings_refuse_tensors_that_are_not_a_pool():
         xsv.Pages.empty(2, 2, "cpu")
     with pytest.raises(ValueError):
         xsv.Pages(None, None, None, None)
+
+
+def test_launches_are_sized_by_the_rows_and_the_sequences(lib):
+    """Not by the rows of all that one sequence may have, for each of them."""
+    nbytes = C.c_int64()
+    pages = _pages(kv_heads=16, sequences=2000)
+    for count, chosen in ((3, None), (3, PTR)):
+        c = _query(heads=16, rows=100000, longest_q=100000, count=count, chosen=chosen)
+        assert lib.xsv_pages_attend_workspace(C.byref(pages), C.byref(c), C.byref(nbytes)) == xsv.XSV_OK and nbytes.value == 0
+    pages = _pages(kv_heads=16, sequences=1 << 24)
+    assert lib.xsv_pages_attend_workspace(C.byref(pages), C.byref(c), C.byref(nbytes)) == xsv.XSV_ERR_UNSUPPORTED
