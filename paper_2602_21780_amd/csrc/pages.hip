@@ -11,7 +11,7 @@
 // to look for them nowhere else.
 //
 // A workgroup has one page of one head: a thread 16 channels of a token on the row side, 16 bytes of a line of the page on the other; values change
-// sides in LDS.  Memory bounds both: 32976 tokens of 16 heads are written in 46 us and read back in 47, 4.5 and 4.3 TB/s of what is read and written (a
+// sides in LDS.  Memory bounds both: 32976 tokens of 16 heads are written in 47 us and read back in 47, 4.4 and 4.3 TB/s of what is read and written (a
 // large copy: 4.9); a token each of 64 streams takes 6.3 us, the chain of offsets, table, scale, page and its way back.
 #include "pages.h"
 

@@ -2,13 +2,15 @@
 //
 //   S = scale * k_scale * (q . code_k) over the tokens that a row sees,  lse = log sum exp(S),  out = exp(S - lse) (code_v * v_scale)
 //
-// Codes become bf16 as they are (e4m3 has 4 significant bits, bf16 has 8), one instruction for two; the page's scales are powers of two,
-// so that multiplying logits and probabilities by them instead rounds nothing.  (Products in 8 bits would spare the keys' conversions, with q as the sum of two codes; but those matrix
-// instructions lose what lies 2^-11 below their largest product, also with scales for blocks: measured.)  Probabilities are rounded to bf16 once, as the second product's operands.
+// Codes become bf16 as they are (e4m3 has 4 significant bits, bf16 has 8), one instruction for two; the page's scales are powers of two, so that
+// multiplying logits and probabilities by them instead rounds nothing. (Products in 8 bits would spare the keys' conversions, with q as the sum of
+// two codes; but those matrix instructions lose what lies 2^-11 below their largest product, also with scales for blocks: measured.) Probabilities
+// are rounded to bf16 once, as the second product's operands.
 //
-// One pass over the pages with a reference logit per row and a sum; a workgroup's four waves take every fourth page and are joined in LDS, and where there are too few blocks of rows
-// to fill the card, workgroups share a block's pages and a second launch joins them in their order.  Few rows (decoding) are bounded by memory: 64 streams of 60 to 32768 tokens, 32
-// heads on 8, 79 us, 4.5 TB/s of codes.  Many rows are bounded by the vector unit (below): a frame of 1374 over 5470 tokens, 16 heads, 45.5 us, 680 TFLOP/s.
+// One pass over the pages with a reference logit per row and a sum; a workgroup's four waves take every fourth page and are joined in LDS, and where
+// there are too few blocks of rows to fill the card, workgroups share a block's pages and a second launch joins them in their order. Few rows
+// (decoding) are bounded by memory: 64 streams of 60 to 32768 tokens, 32 heads on 8, 79 us, 4.5 TB/s of codes. Many rows are bounded by the vector
+// unit (below): a frame of 1374 over 5470 tokens, 16 heads, 46 us, 670 TFLOP/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -20,21 +22,23 @@ namespace {
 constexpr int kWaves = 4;       // of a workgroup, or all that a compute unit holds
 constexpr int kManyWaves = 16;
 constexpr int kMostParts = 64;
-// Pages that the waves of a workgroup share where every sequence has one block: their lengths are known on the device alone, so a long one is cut as if it were
-// alone, and workgroups without a share end at once.  64 streams of 60 to 32768 tokens, 8 key heads, us: 32 pages 78, 48 77, 64 77, 80 77, 128 91, 256 91.
+// Pages that the waves of a workgroup share where every sequence has one block: their lengths are known on the device alone, so a long one is cut as
+// if it were alone, and workgroups without a share end at once. 64 streams of 60 to 32768 tokens, 8 key heads, us: 32 pages 78, 48 77, 64 77, 80 77,
+// 128 91, 256 91.
 constexpr int kLongest = 64;
-// Short caches of few blocks: one workgroup of 16 waves to a block instead of parts and their join, which is a launch more.  us from Python, one workgroup and parts: 16 blocks
-// over 512 to 4096 tokens 12 and 16, over 8192 20 and 16; 64 over 4096 13 and 16, over 8192 20 and 18; 256 over 4096 27 and 33 (over 8192 49 and 56, but
-// there sequences of different lengths would leave compute units empty).
+// Short caches of few blocks: one workgroup of 16 waves to a block instead of parts and their join, which is a launch more. us from Python, one
+// workgroup and parts: 16 blocks over 512 to 4096 tokens 12 and 16, over 8192 20 and 16; 64 over 4096 13 and 16, over 8192 20 and 18; 256 over 4096
+// 27 and 33 (over 8192 49 and 56, but there sequences of different lengths would leave compute units empty).
 constexpr int kManyUnits = 256, kManyPages = 64;
-// 64 rows to a wave, if that fills the card: two workgroups on each of 256 compute units.  us, 64 rows and 32 (16 heads): 10992 rows over 16384 tokens 744 and 857,
-// 2748 over 8192 107 and 122, 2048 behind 6144 of their own (512 blocks) 75 and 79; 1374 over 5470 (352 blocks) 51 and 46.  Just above a full card they are even (2100 over
-// 8192, 528 blocks: 106 and 102).  Fewer blocks if all parts of their pages are long: 512 over 65536 tokens (4 parts of 256 pages) 169 and 192, 128 over 131072 (16 of
-// 128) 109 and 118, but 256 over 8192 (8 of 16) 40 and 32.
+// 64 rows to a wave, if that fills the card: two workgroups on each of 256 compute units. us, 64 rows and 32 (16 heads): 10992 rows over 16384 tokens
+// 744 and 857, 2748 over 8192 107 and 122, 2048 behind 6144 of their own (512 blocks) 75 and 79; 1374 over 5470 (352 blocks) 51 and 46. Just above a
+// full card they are even (2100 over 8192, 528 blocks: 106 and 102). Fewer blocks if all parts of their pages are long: 512 over 65536 tokens (4
+// parts of 256 pages) 169 and 192, 128 over 131072 (16 of 128) 109 and 118, but 256 over 8192 (8 of 16) 40 and 32.
 constexpr long long kFull = 512, kLongPart = 128;
-// Short lists of many blocks: a wave to a block, without a list in LDS and without a join, if there are this many blocks for each of a block's entries (64 at most).  us, a wave
-// and a workgroup to a block, 16 heads on 8, rows that choose 4 pages (32 entries): 512 rows, 512 blocks, 14.5 and 12, 1024 rows 15 and 18, 2048 rows 19 and 29; 8 pages
-// (64 entries): 1024 rows 38 and 30, 2048 rows 49 and 51; 256 streams, 32 heads on 8, 8 pages 30 and 37, 32 pages 102 and 99.
+// Short lists of many blocks: a wave to a block, without a list in LDS and without a join, if there are this many blocks for each of a block's
+// entries (64 at most). us, a wave and a workgroup to a block, 16 heads on 8, rows that choose 4 pages (32 entries): 512 rows, 512 blocks, 14.5 and
+// 12, 1024 rows 15 and 18, 2048 rows 19 and 29; 8 pages (64 entries): 1024 rows 38 and 30, 2048 rows 49 and 51; 256 streams, 32 heads on 8, 8 pages
+// 30 and 37, 32 pages 102 and 99.
 constexpr long long kSoloBlocks = 32;
 constexpr int kListRows = 16;  // rows that share a list of chosen pages
 // Probabilities are taken against a reference logit per row, which moves when the sum over what a lane has of a page passes this:
@@ -52,11 +56,11 @@ __device__ __forceinline__ float off_of(float ref) { return ref == -kInf ? 0.0f 
 template <int COLS>
 struct Shape;
 
-// Pages go through LDS.  A lane's pieces are 64 bytes apart, a row of the page each, and the 16 lanes whose loads the memory path takes together would ask
-// for eight lines; it then takes 30 cycles for a load of 1 KB that takes 16 in order.  In order, each load brings 16 rows to LDS by itself, without
-// registers in between, and the lanes read their pieces there.  The four 16-byte pieces of a row are turned by an amount that goes by the row, so that the
-// eight lanes that read together are in different banks: keys' rows by key_turn(row of 4, which 16 rows), values' by value_turn(row).  (64 streams 82 -> 79 us,
-// a frame over chosen pages 121 -> 115.)
+// Pages go through LDS. A lane's pieces are 64 bytes apart, a row of the page each, and the 16 lanes whose loads the memory path takes together would
+// ask for eight lines; it then takes 30 cycles for a load of 1 KB that takes 16 in order. In order, each load brings 16 rows to LDS by itself,
+// without registers in between, and the lanes read their pieces there. The four 16-byte pieces of a row are turned by an amount that goes by the row,
+// so that the eight lanes that read together are in different banks: keys' rows by key_turn(row of 4, which 16 rows), values' by value_turn(row). (64
+// streams 82 -> 79 us, a frame over chosen pages 121 -> 115.)
 constexpr int kStagedBytes = 2 * kPageBytes;  // of a wave: keys and values of a page
 __device__ __forceinline__ int key_turn(int row, int rows) { return row / 2 % 2 + 2 * (rows % 2); }
 __device__ __forceinline__ int value_turn(int row) { return row / 2 % 4; }
@@ -172,11 +176,12 @@ __device__ __forceinline__ Row row_of(const PagesArgs& a, const Block& b, int i)
   return r;
 }
 
-// All pages: rows (query, head) COLS at a time.  Chosen pages: `group` queries with their heads, or 16 heads of a query that has more.
-// Sequences' blocks are counted from their ends, so that under a mask those that see the most come first, and those of a short sequence behind a long
-// cache, which see as much, among them; up to 64 sequences go by what they see (sequences of 0 to 1374 rows over up to 5470 tokens 55 -> 47 us).  Workgroups are dealt to the XCDs one by one; where eight divides the key
-// heads, each XCD has its own, one after the other, whose pages are then in one L2, and all of whose blocks go through them at about the same time.  A block's parts are far apart: side by side, with eight of them,
-// those of short sequences, which have little or nothing to do, were dealt to the same compute units (64 streams 89 us, 77).
+// All pages: rows (query, head) COLS at a time. Chosen pages: `group` queries with their heads, or 16 heads of a query that has more. Sequences'
+// blocks are counted from their ends, so that under a mask those that see the most come first, and those of a short sequence behind a long cache,
+// which see as much, among them; up to 64 sequences go by what they see (sequences of 0 to 1374 rows over up to 5470 tokens 55 -> 47 us). Workgroups
+// are dealt to the XCDs one by one; where eight divides the key heads, each XCD has its own, one after the other, whose pages are then in one L2, and
+// all of whose blocks go through them at about the same time. A block's parts are far apart: side by side, with eight of them, those of short
+// sequences, which have little or nothing to do, were dealt to the same compute units (64 streams 89 us, 77).
 template <int COLS, bool CHOSEN>
 __device__ __forceinline__ bool block_of(const PagesArgs& a, int number, int blocks, Block* b) {
   const int rep = a.heads / a.kv_heads;
@@ -272,7 +277,8 @@ __device__ __forceinline__ int list_window(const PagesArgs& a, const Block& b, i
   return total;
 }
 
-// The waves' results, each [COLS][64] of `pitch` pieces, 16-byte pieces of row r in the order of their number xor r, put together: a block's, or this part of them.
+// The waves' results, each [COLS][64] of `pitch` pieces, 16-byte pieces of row r in the order of their number xor r, put together: a block's, or this
+// part of them.
 template <int COLS, int WAVES>
 __device__ __forceinline__ void leave(const PagesArgs& a, const Block& b, int thread, const f32x4* acc, int pitch, const float* refs, const float* sums) {
   // All rows at once, a thread some channels of one: 4 threads further on the next 4 if it has more than 4, so that 8 side by side read different banks.
@@ -321,9 +327,10 @@ __device__ __forceinline__ void leave(const PagesArgs& a, const Block& b, int th
 
 struct Empty {};
 
-// 16 rows of a key head at a time, by a workgroup or (SOLO) by each of its waves: single tokens, and chosen pages, where each row has its own and a page is worked on for all 16 once any has chosen it.  Those
-// are bounded by the vector unit, too (66 % of the cycles, and the matrix instructions that hold it up): a page is 64 conversions and 16 logits a lane whether one row
-// has it or all.  1374 queries of 16 heads that choose 32 of 1024 pages, 23 of them the same: 115 us.
+// 16 rows of a key head at a time, by a workgroup or (SOLO) by each of its waves: single tokens, and chosen pages, where each row has its own and a
+// page is worked on for all 16 once any has chosen it. Those are bounded by the vector unit, too (66 % of the cycles, and the matrix instructions
+// that hold it up): a page is 64 conversions and 16 logits a lane whether one row has it or all. 1374 queries of 16 heads that choose 32 of 1024
+// pages, 23 of them the same: 114 us.
 template <bool CHOSEN, int WAVES, bool SOLO>
 __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kernel(PagesArgs a, int blocks) {
   constexpr int COLS = 16;
@@ -617,11 +624,12 @@ __global__ __launch_bounds__(64 * WAVES, CHOSEN ? 3 : 4) void pages_attend_kerne
   }
 }
 
-// Many rows of a sequence: kTiles times 32 of them at a time, which share a page's conversion to bf16.  A wave goes through units of 32 tokens and 32 rows; while it works on the
-// weights of one, its matrix instructions make the logits of the next and add up the values of the one before.  What bounds it are the vector unit's cycles: of a unit 16 logits a
-// lane with a multiplication, exp2, a sum and half a conversion each, 335 with 64 rows and 410 with 32 with its part of the page's conversions, and about 16 for each of its eight
-// matrix instructions, which hold up the others that long.  10992 rows over 16384 tokens, 16 heads: 744 us, 992 TFLOP/s (32 rows 857); four rows of eight heads each
-// over 32 caches of 4096 tokens: 46 us (weights and products one after the other 51).
+// Many rows of a sequence: kTiles times 32 of them at a time, which share a page's conversion to bf16. A wave goes through units of 32 tokens and 32
+// rows; while it works on the weights of one, its matrix instructions make the logits of the next and add up the values of the one before. What
+// bounds it are the vector unit's cycles: of a unit 16 logits a lane with a multiplication, exp2, a sum and half a conversion each, 335 with 64 rows
+// and 410 with 32 with its part of the page's conversions, and about 16 for each of its eight matrix instructions, which hold up the others that
+// long. 10992 rows over 16384 tokens, 16 heads: 744 us, 992 TFLOP/s (32 rows 857); four rows of eight heads each over 32 caches of 4096 tokens: 46 us
+// (weights and products one after the other 51).
 template <int kTiles>
 __global__ __launch_bounds__(64 * kWaves, kTiles == 1 ? 3 : 2) void pages_attend_rows_kernel(PagesArgs a, int blocks) {
   using S = Shape<32>;

@@ -7,12 +7,12 @@
 // and all partial sums below 64 * 255 * 896 < 2^24, so that fp32 holds each exactly in any order: the same pages whatever
 // computes them, and equal scores are equal.  A row's `first` and `last` pages are chosen whatever their scores; equal scores go to the lower page.
 //
-// A workgroup has some queries of one key head, 16 or 32 rows (query, head) of a product if it can, whose pages its waves score together, 16 a wave and turn, from
-// the pool into scores in LDS; then a wave takes a query, its scores in registers.  The n-th largest of each lane's largest is a bound that few more than n scores
-// pass, and those are looked at one a lane: each counts the larger ones.  Bounds are read from memory once per workgroup and scores never written there; what bounds it are waits:
-// the two halves take some 6 and 5 of a workgroup's 15 us, with one workgroup of 16 waves on a compute unit (a quarter fewer instructions changed nothing): 1374 queries of 16 heads choose
-// 32 of 1024 pages each in 44 us.  A few queries (decoding) are a chain of waits, and have all bounds of four products' pages on their way
-// at once: 64 streams choose 32 of up to 512 pages in 10 us, of which the host's call is 9 (one product ahead, and heads joined by atomics: 16).
+// A workgroup has some queries of one key head, 16 or 32 rows (query, head) of a product if it can, whose pages its waves score together, 16 a wave
+// and turn, from the pool into scores in LDS; then a wave takes a query, its scores in registers. The n-th largest of each lane's largest is a bound
+// that few more than n scores pass, and those are looked at one a lane: each counts the larger ones. Bounds are read from memory once per workgroup
+// and scores never written there; what bounds it are waits: the two halves take some 6 and 5 of a workgroup's 15 us, with one workgroup of 16 waves on
+// a compute unit: 1374 queries of 16 heads choose 32 of 1024 pages each in 45 us. A few queries (decoding) are a chain of waits, and have all bounds
+// of four products' pages on their way at once: 64 streams choose 32 of up to 512 pages in 10 us.
 #include <algorithm>
 
 #include "pages.h"
@@ -68,7 +68,8 @@ constexpr int kPieceWords = 16 * kD / 2;  // of a wave: LDS to bring one of 16 p
 // Where a query's scores are turned to, so that what 16 queries side by side write is in different banks.
 __device__ __forceinline__ int score_turn(int query) { return query % 16 * 4; }
 
-// The first BITS bits of the n-th largest of a wave's keys, one a lane (0 if there are fewer), two bits at a time: the three counts do not wait for one another.
+// The first BITS bits of the n-th largest of a wave's keys, one a lane (0 if there are fewer), two bits at a time: the three counts do not wait for
+// one another.
 template <int BITS>
 __device__ __forceinline__ uint32_t nth_largest(uint32_t key, int n) {
   uint32_t x = 0;
@@ -118,9 +119,10 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
     return id < a.pages ? id : -1;
   };
   for (int c0 = 0; c0 < n * rep && wave < min(WAVES, chunks); c0 += 16 * SETS) {
-    // A wave takes kChunk pages, one to a lane, that are looked up together while those before them are worked on, and then 16 at a time.  Of those, the lane has
-    // page lane % 16 in the product, and 16 bytes of one of the bounds of pages lane / 8 and 8 + lane / 8 on their way there: 8 lanes side by side take 128 bytes (with
-    // a page to a lane, every lane asks for a line of its own, and a load takes the memory path 59 cycles instead of 16).
+    // A wave takes kChunk pages, one to a lane, that are looked up together while those before them are worked on, and then 16 at a time. Of those,
+    // the lane has page lane % 16 in the product, and 16 bytes of one of the bounds of pages lane / 8 and 8 + lane / 8 on their way there: 8 lanes
+    // side by side take 128 bytes (with a page to a lane, every lane asks for a line of its own, and a load takes the memory path 59 cycles instead
+    // of 16).
     struct Way {
       u32x4 bounds[4];
     };
@@ -175,7 +177,8 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
       }
     }
     auto score = [&](const Way& w, int exponent, int chunk, int turn) {
-      // through this wave's piece of LDS (its accesses stay in order); a page's 16-byte pieces are turned so that lanes that read together are in different banks
+      // through this wave's piece of LDS (its accesses stay in order); a page's 16-byte pieces are turned so that lanes that read together are in
+      // different banks
       f32x4 sum[SETS] = {};
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
@@ -270,8 +273,8 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
     float held_scores[N > 0 ? N : 1], most = kNone;
     uint32_t lower = ordered(kNone);  // at least as many scores as are wanted are larger
     if (!chosen) {
-      // As many lanes as pages are wanted have a score of at least `least`, so what is below is not chosen; what is not is rarely more than one a lane, and is then
-      // dealt out one a lane.
+      // As many lanes as pages are wanted have a score of at least `least`, so what is below is not chosen; what is not is rarely more than one a
+      // lane, and is then dealt out one a lane.
       float score = kNone;
       int page = lane, found = 0;
       if (steps == 1) {
@@ -489,12 +492,22 @@ __global__ __launch_bounds__(64 * WAVES) void pages_select_kernel(PagesArgs a, i
 
 int pages_held(const PagesArgs& a) { return std::min(a.width, (int)(((long long)a.longest_k + kPage - 1) / kPage)); }
 
-// 16 rows and 8 waves to a workgroup where several fit a compute unit, one's choice beside the other's scores; else 32 rows and 16 waves.  us, 16 rows and 32, 1374 queries of 16
-// heads: 32 of 625 pages 42 and 45, of 896 47 and 49, of 1024 51 and 51, of 1100 (one workgroup) 84 and 67; of 256 pages with four heads to a key head 50 and 89.
-// With eight, 16 rows are two queries, a choice for two waves: 700 queries, 256 pages, 25 and 21.
+// Rows of a product and waves to a workgroup.  us for 1374 queries that choose 32 pages each:
+//                                          16 rows, 4 waves   16 rows, 8 waves   32 rows, 16 waves
+//   16 heads on 16, 256 pages                          27.7               28.9                31.3
+//                   512                                33.7               34.0                35.3
+//                   625                                39.7               37.3                40.4
+//                   896                                56.4               42.6                44.6
+//                   1024                               60.7               47.0                45.9
+//                   1100                               67.5               76.7                69.8
+//   64 heads on 16, 256 pages                          50.9               73.7                88.8
+//                   896                               101.2                117                 141
+// 16 rows, where two workgroups of 16 queries fit a compute unit (kSharedPages) and their queries are 4 or more (kSharedHeads): one's choice runs
+// beside the other's scores. Of eight heads to a key head, 16 rows are two queries, a choice for two waves: 700 queries, 128 on 16 heads, 256 pages,
+// 32 rows are better with 4 waves (37.5 and 48.4) and with 8 (48.7 and 73.3).
 constexpr int kSharedPages = 960, kSharedHeads = 4;
-// 4 waves to a workgroup, and so twice as many side by side, where there are many and four fit a compute unit's LDS (their scores 32 KB each).  us, 4 waves and 8: 1374 queries of 64
-// heads on 16, 256 pages, 50 and 71; 256 streams of 8192 tokens 18.5 and 28; 8 ragged sequences, 64 on 16 heads, 70 and 117; where scores leave less room, 16 queries of 896 pages, 64 and 47.
+// 4 waves where there are many workgroups, twice as many side by side, if four fit a compute unit's LDS (their scores 32 KB each; 512 and 625 pages
+// above): 256 streams of 8192 tokens, 32 on 8 heads, 21.4 and with 8 waves 31.2; eight ragged sequences, 64 on 16 heads, 105 and 173.
 constexpr int kManyGroups = 1024, kFourScores = 8192;
 
 struct Plan {
