@@ -305,7 +305,9 @@ int xsv_seq_attend_grad_workspace(const xsv_seq_config* cfg, int64_t* bytes);
  * All calls take the lengths that the sequences have with the call's own rows: row i of the n rows [begin[s], begin[s + 1]) of sequence s
  * stands at token i + lengths[s] - n of it (a row in front of its first token is not written, not read, and sees nothing).  Tokens behind the table's
  * width are seen by nobody, not written and not read; the others keep their places.  What begin holds is cut off at the tensors' rows: nothing outside
- * tensors and table is touched.  Rows of no sequence are not written. */
+ * tensors and table is touched.  Rows of no sequence are not written.
+ * Pages of a new pool hold zeros, or are written from their first token on before a row sees them: memory as it came may hold codes of NaN under a scale
+ * that does not say so, which then reach rows of the call that do not see their tokens. */
 typedef struct {
   int32_t pages;            /* of the pool, >= 0                                               */
   int32_t kv_heads;         /* 1 .. 65536                                                      */
