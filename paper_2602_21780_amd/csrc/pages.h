@@ -93,7 +93,7 @@ constexpr int kRanked = 64;
 // have, `each`? Empty workgroups cost less than the search; both sides, us, each and numbered, 500 sequences of a row and one of L, 16 heads:
 // written, L = 100 (each 1.5 times numbered) 38 and 45, L = 300 (2.9) 67 and 45; choice of 4 pages, L = 300 142 and 42, L = 1000 388 and 51;
 // attention 186 and 149, 313 and 155.
-inline bool by_number(long long each, long long numbered) { return numbered <= each / 2; }
+inline bool by_number(double each, long long numbered) { return (double)numbered <= each / 2; }  // (the product may pass 64 bits)
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const bf16x2 p = {(__bf16)a, (__bf16)b};

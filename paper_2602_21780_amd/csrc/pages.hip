@@ -281,7 +281,7 @@ Plan plan_of(const PagesArgs& a) {
   Plan p;
   p.most = (int)(((long long)a.longest + kPage - 2) / kPage + 1);
   const long long each = (long long)p.most * a.sequences, all = a.rows / kPage + 2ll * a.sequences;
-  p.ranked = a.sequences > 1 && by_number(each, all);
+  p.ranked = a.sequences > 1 && by_number((double)each, all);
   p.blocks = p.ranked ? all : each;
   return p;
 }

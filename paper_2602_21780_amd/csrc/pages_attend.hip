@@ -987,9 +987,8 @@ constexpr long long kMostWorkgroups = (1ll << 32) / (64 * kWaves) - 1;  // threa
 long long times(long long a, long long b) { return b != 0 && a > kMostWorkgroups / b ? kMostWorkgroups + 1 : a * b; }  // as far as it matters
 // Are blocks numbered over all sequences, `all` at most?  Then they are the plan's.
 void number(Plan& p, const PagesArgs& a, long long all) {
-  const long long each = times(p.blocks, a.sequences);
-  p.ranked = p.blocks > 1 && a.sequences > 1 && (a.sequences <= kRanked || by_number(each, all));
-  if (p.ranked) p.blocks = a.sequences <= kRanked ? std::min(each, all) : all;
+  p.ranked = p.blocks > 1 && a.sequences > 1 && (a.sequences <= kRanked || by_number((double)p.blocks * a.sequences, all));
+  if (p.ranked) p.blocks = a.sequences <= kRanked ? std::min(times(p.blocks, a.sequences), all) : all;
 }
 Plan plan_of(const PagesArgs& a) {
   Plan p{};

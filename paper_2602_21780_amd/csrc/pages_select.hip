@@ -525,7 +525,7 @@ Plan plan_of(const PagesArgs& a) {
   if (p.queries <= kFewQueries && p.queries * rep <= 16) p.columns = 16;
   const long long of_one = ((long long)a.longest + p.queries - 1) / p.queries, each = of_one * a.sequences;
   const long long all = ((long long)a.rows + p.queries - 1) / p.queries + a.sequences;
-  p.ranked = of_one > 1 && a.sequences > 1 && (a.sequences <= kRanked || by_number(each, all));
+  p.ranked = of_one > 1 && a.sequences > 1 && (a.sequences <= kRanked || by_number((double)each, all));
   p.groups = !p.ranked ? each : a.sequences <= kRanked ? std::min(each, all) : all;
   const bool four = p.groups > kManyGroups / a.kv_heads && p.queries * p.pitch <= kFourScores;
   p.waves = p.columns == 32 && p.queries > kFewQueries ? 16 : four ? 4 : 8;

@@ -126,3 +126,5 @@ def test_launches_are_sized_by_the_rows_and_the_sequences(lib):
         assert lib.xsv_pages_attend_workspace(C.byref(pages), C.byref(c), C.byref(nbytes)) == xsv.XSV_OK and nbytes.value == 0
     pages = _pages(kv_heads=16, sequences=1 << 24)
     assert lib.xsv_pages_attend_workspace(C.byref(pages), C.byref(c), C.byref(nbytes)) == xsv.XSV_ERR_UNSUPPORTED
+    pages, c = _pages(sequences=9000000, kv_heads=1), _query(heads=1, rows=100000000, longest_q=100000000)
+    assert lib.xsv_pages_attend_workspace(C.byref(pages), C.byref(c), C.byref(nbytes)) == xsv.XSV_OK
